@@ -12,12 +12,17 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libacdc.so"
 
 _lib = None
 
-# Exported symbols and their signatures (mirrors include/acdc.h).
+# Exported symbols and their signatures (mirrors include/acdc.h and
+# include/acdc_train.h).
 _P = ctypes.c_void_p
 _I64 = ctypes.c_int64
 _I32 = ctypes.c_int32
 _U32 = ctypes.c_uint32
 _SZ = ctypes.c_size_t
+_F = ctypes.c_float
+_D = ctypes.c_double
+# logits, dtype, stride, targets, target_bits: the head of every loss's arguments
+_LOGITS = [_P, _I32, _I64, _P, _I32]
 SIGNATURES = {
     "acdc_supported": (ctypes.c_int, [_I32, _U32]),
     "acdc_prepare": (ctypes.c_int, [_I32, _U32]),
@@ -33,6 +38,18 @@ SIGNATURES = {
     "acdc_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "acdc_last_hip_error": (ctypes.c_int, []),
     "acdc_sync_timeouts": (ctypes.c_int, [ctypes.POINTER(ctypes.c_int64), ctypes.c_int]),
+    "acdc_logprob_forward": (ctypes.c_int, [*_LOGITS, _I64, _I32, _P, _P, _P, _P, _SZ, _P]),
+    "acdc_logprob_workspace_size": (_SZ, [_I64, _I32, _I32]),
+    "acdc_logprob_backward": (ctypes.c_int, [*_LOGITS, _P, _P, _P, _P, _P, _I64, _I64, _I32, _P]),
+    "acdc_policy_loss": (ctypes.c_int,
+                         [*_LOGITS, _P, _P, _P, _P, _I64, _I32, _P, _P, _P, _P, _I64, _P, _P, _P, _SZ, _P]),
+    "acdc_policy_workspace_size": (_SZ, [_I64, _I32, _I32]),
+    "acdc_preference_loss": (ctypes.c_int,
+                             [*_LOGITS, _P, _I32, _P, _I64, _I32, _I64, _P, _P, _P, _P, _I64, _P, _P, _P, _SZ, _P]),
+    "acdc_preference_workspace_size": (_SZ, [_I64, _I32, _I32, _I64]),
+    "acdc_adamw_step": (ctypes.c_int, [_P, _I32, _D, _D, _D, _I64, _P, _P]),
+    "acdc_grad_norm": (ctypes.c_int, [_P, _P, _P, _I32, _F, _P, _P, _SZ, _P]),
+    "acdc_grad_norm_workspace_size": (_SZ, [_P, _I32]),
 }
 
 

@@ -25,14 +25,16 @@ HIP_FLAGS = [
 
 
 def source_digest() -> str:
-    """sha256 over the kernel sources (csrc/*, include/*), in name order: the
-    version tag that recorded profiler counters are tied to."""
+    """sha256 over the cascade's kernel sources (csrc/*, include/*), in name
+    order: the version tag that recorded profiler counters are tied to.  The
+    training operators' files (acdc_train*) are not in it: no cascade kernel
+    includes them."""
     import hashlib
     h = hashlib.sha256()
     for d in (CSRC, INCLUDE):
         for name in sorted(os.listdir(d)):
             path = os.path.join(d, name)
-            if os.path.isfile(path):
+            if os.path.isfile(path) and not name.startswith("acdc_train"):
                 h.update(name.encode())
                 with open(path, "rb") as f:
                     h.update(f.read())

@@ -25,6 +25,7 @@
 #include "acdc_devctx.hpp"
 #include "acdc_multipass.hpp"
 #include "acdc_registry.hpp"
+#include "acdc_status.hpp"
 
 namespace acdc {
 
@@ -278,18 +279,18 @@ static __device__ __align__(256) float4 scratch[kNoAllocScratchBytes / sizeof(fl
 
 // ------------------------------------------------------------------ host side
 
-namespace {
-
-thread_local int g_last_hip = 0;
-std::mutex g_mu;
-std::map<std::tuple<int, int, int>, void*> g_tables;  // (device, N, complex) -> device table
-
-size_t align256(size_t b) { return (b + 255) & ~size_t(255); }
-
+static thread_local int g_last_hip = 0;
 int hip_fail(hipError_t e) {
   g_last_hip = int(e);
   return ACDC_ERR_HIP;
 }
+
+namespace {
+
+std::mutex g_mu;
+std::map<std::tuple<int, int, int>, void*> g_tables;  // (device, N, complex) -> device table
+
+size_t align256(size_t b) { return (b + 255) & ~size_t(255); }
 
 // ----------------------------------------------------------- kernel timing
 // While enabled, every main kernel launch is bracketed by HIP events on its

@@ -1,0 +1,402 @@
+// The optimiser's operators (acdc_train.h): an AdamW step over a list of
+// tensors and the global norm of their gradients.
+//
+// Mathematics.  Every element is on its own (m, v, w of one element), but for
+// the scales of 8-bit moments, one per 256 elements: the block's maximum has
+// to be known before its first code is written.
+//
+// A launch takes up to kBatch tensors, whose addresses travel in the kernel's
+// arguments: nothing is uploaded, and no table outlives the call.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "acdc_train.hpp"
+
+namespace acdc {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBatch = 48;      // tensors a launch: their records fill the 4 KB of kernel arguments
+constexpr int kBlock = 256;     // elements that share a scale: 4 of each lane of a wave
+constexpr int kChunk = 4096;    // elements a workgroup
+constexpr float kPerTop = 1.f / 448.f;  // 448: largest e4m3 value
+constexpr float kTiny = 0x1p-9f;  // smallest positive one
+
+struct Tensor {
+  void* param;
+  float* master;
+  const void* grad;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  long long n;
+  float rate, decay;  // lr / (1 - beta1^step), 1 - lr * weight_decay
+};
+struct Batch {
+  int first[kBatch];  // first workgroup of each tensor; unused entries are INT_MAX
+  Tensor t[kBatch];
+};
+static_assert(sizeof(Batch) <= 3840, "kernel arguments");
+
+struct Step {
+  double one1, one2;      // 1 - beta
+  float beta1, beta2;
+  float root_scale, eps;  // 1 / sqrt(1 - beta2^step)
+  const float* grad_scale;
+};
+
+// The tensor that a workgroup works on: the last one whose first workgroup is
+// not after it.  One load per lane and a ballot instead of a search.
+__device__ __forceinline__ int tensor_of(const int* first, int count, int block) {
+  const int lane = threadIdx.x % 64;
+  const bool past = lane < count ? first[lane] <= block : false;
+  return __builtin_amdgcn_readfirstlane(__popcll(__ballot(past)) - 1);
+}
+
+// Four elements, the first of them at p; `have` of them exist.
+template <class T>
+__device__ __forceinline__ void load4(const void* base, long long at, int have, float (&v)[4]) {
+  typedef typename T::Elem V4 __attribute__((ext_vector_type(4), aligned(sizeof(typename T::Elem))));
+  const typename T::Elem* p = static_cast<const typename T::Elem*>(base) + at;
+  if (have == 4) {
+    const V4 r = *reinterpret_cast<const V4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = float(r[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = i < have ? float(p[i]) : 0.f;
+  }
+}
+template <class T>
+__device__ __forceinline__ void store4(void* base, long long at, int have, const float (&v)[4]) {
+  typedef typename T::Elem V4 __attribute__((ext_vector_type(4), aligned(sizeof(typename T::Elem))));
+  typename T::Elem* p = static_cast<typename T::Elem*>(base) + at;
+  if (have == 4) {
+    *reinterpret_cast<V4*>(p) = V4{T::to(v[0]), T::to(v[1]), T::to(v[2]), T::to(v[3])};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < have) p[i] = T::to(v[i]);
+  }
+}
+
+// Four e4m3 codes as one word.
+typedef unsigned Word1 __attribute__((aligned(1)));
+__device__ __forceinline__ unsigned load_codes(const void* base, long long at, int have) {
+  const unsigned char* p = static_cast<const unsigned char*>(base) + at;
+  if (have == 4) return *reinterpret_cast<const Word1*>(p);
+  unsigned w = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < have) w |= unsigned(p[i]) << (8 * i);
+  return w;
+}
+__device__ __forceinline__ void store_codes(void* base, long long at, int have, unsigned w) {
+  unsigned char* p = static_cast<unsigned char*>(base) + at;
+  if (have == 4) {
+    *reinterpret_cast<Word1*>(p) = w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < have) p[i] = (unsigned char)(w >> (8 * i));
+  }
+}
+__device__ __forceinline__ void decode4(unsigned w, float scale, float (&v)[4]) {
+  const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(int(w), false), b = __builtin_amdgcn_cvt_pk_f32_fp8(int(w), true);
+  v[0] = a[0] * scale;
+  v[1] = a[1] * scale;
+  v[2] = b[0] * scale;
+  v[3] = b[1] * scale;
+}
+// Codes of four values of a block with this scale; positive values stay
+// positive with POSITIVE.  A NaN keeps its own code (the block's scale comes
+// from the others).
+template <bool POSITIVE>
+__device__ __forceinline__ unsigned encode4(const float (&v)[4], float scale) {
+  float q[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    q[i] = scale > 0.f ? v[i] / scale : v[i] * 0.f;
+    if (POSITIVE && v[i] > 0.f && q[i] < kTiny && scale > 0.f) q[i] = kTiny;
+  }
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
+  return unsigned(w);
+}
+// Scale of a wave's block out of each lane's four values.  Blocks below 2^-100
+// are 0: their scale would leave the normal numbers.  (The product may leave the
+// largest element a rounding away from 448, which its code does not see.)
+__device__ __forceinline__ float scale_of(const float (&v)[4]) {
+  float top = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  return top < 0x1p-100f ? 0.f : top * kPerTop;
+}
+
+template <class P, class G, int BITS, bool MASTER>
+__global__ __launch_bounds__(kThreads) void k_adamw(Batch b, int count, Step s) {
+  const int i = tensor_of(b.first, count, blockIdx.x);
+  const Tensor& t = b.t[i];
+  const float gs = s.grad_scale != nullptr ? *s.grad_scale : 1.f;
+  if (!(gs - gs == 0.f)) return;
+  // the gradient's scale goes into the factors of g and g^2, each rounded once
+  const float c1 = float(s.one1 * double(gs)), c2 = float(s.one2 * (double(gs) * double(gs)));
+  const long long begin = (long long)(int(blockIdx.x) - b.first[i]) * kChunk;
+  const long long end = begin + kChunk < t.n ? begin + kChunk : t.n;
+  // whole waves leave together: a wave's 256 elements are one block of scales
+  for (long long base = begin + (threadIdx.x / 64) * kBlock; base < end; base += kThreads * 4) {
+    const long long at = base + (threadIdx.x % 64) * 4;
+    const long long left = end - at;
+    const int have = left >= 4 ? 4 : left > 0 ? int(left) : 0;
+    float g[4], m[4], v[4], w[4];
+    load4<G>(t.grad, at, have, g);
+    if constexpr (MASTER) load4<F32>(t.master, at, have, w);
+    else load4<P>(t.param, at, have, w);
+    if constexpr (BITS == 32) {
+      load4<F32>(t.m, at, have, m);
+      load4<F32>(t.v, at, have, v);
+    } else {
+      decode4(load_codes(t.m, at, have), t.m_scale[base / kBlock], m);
+      decode4(load_codes(t.v, at, have), t.v_scale[base / kBlock], v);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] *= v[k];
+    }
+    float root[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      // each product and sum rounded on its own, as the formula written out in
+      // 32 bits is: an 8-bit code that a fused product turned the other way would
+      // stand a whole step of its format off
+#pragma clang fp contract(off)
+      m[k] = s.beta1 * m[k] + c1 * g[k];
+      v[k] = s.beta2 * v[k] + c2 * g[k] * g[k];
+      root[k] = sqrtf(v[k]);
+      w[k] = w[k] * t.decay - t.rate * (m[k] / (root[k] * s.root_scale + s.eps));
+    }
+    if constexpr (MASTER) store4<F32>(t.master, at, have, w);
+    store4<P>(t.param, at, have, w);
+    if constexpr (BITS == 32) {
+      store4<F32>(t.m, at, have, m);
+      store4<F32>(t.v, at, have, v);
+    } else {
+      const float ms = scale_of(m), vs = scale_of(root);
+      store_codes(t.m, at, have, encode4<false>(m, ms));
+      store_codes(t.v, at, have, encode4<true>(root, vs));
+      if (threadIdx.x % 64 == 0) {
+        t.m_scale[base / kBlock] = ms;
+        t.v_scale[base / kBlock] = vs;
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------ gradient norm
+
+constexpr int kNormBatch = 64;
+constexpr int kNormChunk = 16384;  // elements a workgroup
+struct NormTensor {
+  const void* grad;
+  long long n;
+  int type;
+};
+struct NormBatch {
+  int first[kNormBatch];
+  NormTensor t[kNormBatch];
+};
+
+__device__ __forceinline__ double sum_workgroup(double v, double* part, int waves) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = v;
+  __syncthreads();
+  double s = 0.0;
+  for (int w = 0; w < waves; ++w) s += part[w];
+  return s;
+}
+
+template <class G>
+__device__ __forceinline__ float square_sum(const NormTensor& t, long long begin, long long end) {
+  float s = 0.f;
+  for (long long at = begin + threadIdx.x * 4; at < end; at += kThreads * 4) {
+    float v[4];
+    load4<G>(t.grad, at, end - at >= 4 ? 4 : int(end - at), v);
+    s += (v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3]);
+  }
+  return s;
+}
+
+__global__ __launch_bounds__(kThreads) void k_square_sums(NormBatch b, int count, double* __restrict__ sums) {
+  __shared__ double part[kThreads / 64];
+  const int i = tensor_of(b.first, count, blockIdx.x);
+  const NormTensor& t = b.t[i];
+  const long long begin = (long long)(int(blockIdx.x) - b.first[i]) * kNormChunk;
+  const long long end = begin + kNormChunk < t.n ? begin + kNormChunk : t.n;
+  const float s = t.type == ACDC_F32 ? square_sum<F32>(t, begin, end) : square_sum<BF16>(t, begin, end);
+  const double total = sum_workgroup(double(s), part, kThreads / 64);
+  if (threadIdx.x == 0) sums[blockIdx.x] = total;
+}
+
+constexpr int kWide = 1024;
+__global__ __launch_bounds__(kWide) void k_norm(const double* __restrict__ sums, long long n, float max_norm,
+                                                float* __restrict__ out) {
+  __shared__ double part[kWide / 64];
+  double s = 0.0;
+  for (long long i = threadIdx.x; i < n; i += kWide) s += sums[i];
+  s = sum_workgroup(s, part, kWide / 64);
+  if (threadIdx.x == 0) {
+    const float norm = float(sqrt(s));
+    out[0] = norm;
+    const float c = max_norm / (norm + 1e-6f);
+    out[1] = max_norm > 0.f ? (c > 1.f ? 1.f : c) : 1.f;  // NaN stays
+  }
+}
+
+// ------------------------------------------------------------------ host side
+
+int done() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? ACDC_OK : hip_fail(e);
+}
+
+constexpr long long kMaxBlocks = 1LL << 30;
+
+// The kernel of a class of tensors: parameter and gradient types, moments, master.
+int class_of(const acdc_adamw_tensor& t) {
+  return t.param_type * 8 + t.grad_type * 4 + (t.m_scale != nullptr ? 2 : 0) + (t.master != nullptr ? 1 : 0);
+}
+constexpr int kClasses = 16;
+
+void launch_class(int cls, const Batch& b, int count, long long blocks, const Step& s, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(blocks)), block(kThreads);
+  auto moments = [&]<class P, class G, bool MASTER>() {
+    if (cls & 2) hipLaunchKernelGGL((k_adamw<P, G, 8, MASTER>), grid, block, 0, stream, b, count, s);
+    else hipLaunchKernelGGL((k_adamw<P, G, 32, MASTER>), grid, block, 0, stream, b, count, s);
+  };
+  auto grads = [&]<class P, bool MASTER>() {
+    if (cls & 4) moments.template operator()<P, BF16, MASTER>();
+    else moments.template operator()<P, F32, MASTER>();
+  };
+  if (!(cls & 8)) grads.template operator()<F32, false>();
+  else if (cls & 1) grads.template operator()<BF16, true>();
+  else grads.template operator()<BF16, false>();
+}
+
+bool tensor_ok(const acdc_adamw_tensor& t) {
+  const size_t pb = dtype_bytes(t.param_type), gb = dtype_bytes(t.grad_type);
+  if (pb == 0 || gb == 0 || t.n < 0 || t.n > (int64_t(1) << 40)) return false;
+  if (!(t.lr - t.lr == 0.f) || !(t.weight_decay - t.weight_decay == 0.f)) return false;
+  if ((t.m_scale == nullptr) != (t.v_scale == nullptr)) return false;
+  if (t.master != nullptr && t.param_type != ACDC_BF16) return false;
+  if (t.n == 0) return true;
+  const size_t mb = t.m_scale != nullptr ? 1 : 4;
+  if (t.param == nullptr || t.grad == nullptr || t.m == nullptr || t.v == nullptr) return false;
+  if (t.param == t.grad || t.m == t.v || t.m == t.param || t.v == t.param || t.master == t.param) return false;
+  return aligned_to(t.param, pb) && aligned_to(t.grad, gb) && aligned_to(t.master, 4) && aligned_to(t.m, mb) &&
+         aligned_to(t.v, mb) && aligned_to(t.m_scale, 4) && aligned_to(t.v_scale, 4);
+}
+
+}  // namespace
+}  // namespace acdc
+
+using namespace acdc;
+
+extern "C" int acdc_adamw_step(const acdc_adamw_tensor* tensors, int32_t count, double beta1, double beta2, double eps,
+                               int64_t step, const float* grad_scale, acdc_stream_t stream) {
+  if (count < 0 || (count > 0 && tensors == nullptr) || step < 1 || !aligned_to(grad_scale, 4))
+    return ACDC_ERR_INVALID_ARG;
+  if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) || !(eps - eps == 0.0))
+    return ACDC_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < count; ++i)
+    if (!tensor_ok(tensors[i])) return ACDC_ERR_INVALID_ARG;
+  const double c1 = 1.0 - std::pow(beta1, double(step)), c2 = 1.0 - std::pow(beta2, double(step));
+  const Step s{1.0 - beta1, 1.0 - beta2, float(beta1), float(beta2), float(1.0 / std::sqrt(c2)), float(eps), grad_scale};
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  unsigned seen = 0;
+  for (int32_t i = 0; i < count; ++i) seen |= 1u << class_of(tensors[i]);
+  for (int cls = 0; cls < kClasses; ++cls) {
+    if (!(seen >> cls & 1)) continue;
+    Batch b;
+    int used = 0;
+    long long blocks = 0;
+    auto flush = [&]() -> int {
+      if (used == 0) return ACDC_OK;
+      launch_class(cls, b, used, blocks, s, st);
+      used = 0;
+      blocks = 0;
+      return done();
+    };
+    for (int32_t i = 0; i < count; ++i) {
+      const acdc_adamw_tensor& t = tensors[i];
+      if (t.n == 0 || class_of(t) != cls) continue;
+      const long long need = (t.n + kChunk - 1) / kChunk;
+      if (used == kBatch || blocks + need > kMaxBlocks) {
+        const int rc = flush();
+        if (rc != ACDC_OK) return rc;
+      }
+      b.first[used] = int(blocks);
+      b.t[used] = Tensor{t.param, t.master, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.n,
+                         float(double(t.lr) / c1), float(1.0 - double(t.lr) * double(t.weight_decay))};
+      ++used;
+      blocks += need;
+    }
+    const int rc = flush();
+    if (rc != ACDC_OK) return rc;
+  }
+  return ACDC_OK;
+}
+
+static long long norm_blocks(const int64_t* sizes, int32_t count) {
+  long long blocks = 0;
+  for (int32_t i = 0; i < count; ++i) blocks += (sizes[i] + kNormChunk - 1) / kNormChunk;
+  return blocks;
+}
+
+extern "C" size_t acdc_grad_norm_workspace_size(const int64_t* sizes, int32_t count) {
+  if (count < 0 || (count > 0 && sizes == nullptr)) return 0;
+  for (int32_t i = 0; i < count; ++i)
+    if (sizes[i] < 0 || sizes[i] > (int64_t(1) << 40)) return 0;
+  return size_t(norm_blocks(sizes, count)) * sizeof(double);
+}
+
+extern "C" int acdc_grad_norm(const void* const* grads, const int64_t* sizes, const int32_t* types, int32_t count,
+                              float max_norm, float* out, void* workspace, size_t workspace_bytes,
+                              acdc_stream_t stream) {
+  if (count < 0 || (count > 0 && (grads == nullptr || sizes == nullptr || types == nullptr))) return ACDC_ERR_INVALID_ARG;
+  if (out == nullptr || !aligned_to(out, 4) || !aligned_to(workspace, 8) || max_norm != max_norm) return ACDC_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < count; ++i) {
+    const size_t eb = dtype_bytes(types[i]);
+    if (eb == 0 || sizes[i] < 0 || sizes[i] > (int64_t(1) << 40)) return ACDC_ERR_INVALID_ARG;
+    if (sizes[i] > 0 && (grads[i] == nullptr || !aligned_to(grads[i], eb))) return ACDC_ERR_INVALID_ARG;
+  }
+  const long long total = norm_blocks(sizes, count);
+  if (total > 0 && (workspace == nullptr || workspace_bytes < size_t(total) * sizeof(double))) return ACDC_ERR_WORKSPACE;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  double* sums = static_cast<double*>(workspace);
+  NormBatch b;
+  int used = 0;
+  long long blocks = 0, at = 0;
+  auto flush = [&]() -> int {
+    if (used == 0) return ACDC_OK;
+    hipLaunchKernelGGL(k_square_sums, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, st, b, used, sums + at);
+    at += blocks;
+    used = 0;
+    blocks = 0;
+    return done();
+  };
+  for (int32_t i = 0; i < count; ++i) {
+    if (sizes[i] == 0) continue;
+    const long long need = (sizes[i] + kNormChunk - 1) / kNormChunk;
+    if (used == kNormBatch || blocks + need > kMaxBlocks) {
+      const int rc = flush();
+      if (rc != ACDC_OK) return rc;
+    }
+    b.first[used] = int(blocks);
+    b.t[used] = NormTensor{grads[i], sizes[i], types[i]};
+    ++used;
+    blocks += need;
+  }
+  int rc = flush();
+  if (rc != ACDC_OK) return rc;
+  hipLaunchKernelGGL(k_norm, dim3(1), dim3(kWide), 0, st, sums, total, max_norm, out);
+  return done();
+}
