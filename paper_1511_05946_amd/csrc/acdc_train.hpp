@@ -52,6 +52,59 @@ template <class T>
 __device__ __forceinline__ void store_chunk(typename T::Elem* p, const typename T::Raw& r) {
   *reinterpret_cast<typename T::Raw*>(p) = r;
 }
+// The same at a lane's byte offset from an address that the whole wave shares:
+// the address stays in scalar registers, and a thread keeps one offset.
+template <class T>
+__device__ __forceinline__ typename T::Raw load_chunk_at(const typename T::Elem* p, unsigned fixed, unsigned lane) {
+  return *reinterpret_cast<const typename T::Raw*>((reinterpret_cast<const char*>(p) + fixed) + lane);
+}
+template <class T>
+__device__ __forceinline__ void store_chunk_at(typename T::Elem* p, unsigned fixed, unsigned lane,
+                                               const typename T::Raw& r) {
+  *reinterpret_cast<typename T::Raw*>((reinterpret_cast<char*>(p) + fixed) + lane) = r;
+}
+// A value that all lanes of the wave hold, moved to a scalar register.
+__device__ __forceinline__ float uniform(float v) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
+}
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// -------------------------------------------------- over the lanes of a wave
+// Every lane gets the result: within 16 lanes by DPP (a neighbour's register
+// read as an operand), then across them by the lane swaps of gfx950.  A
+// shuffle through LDS would take its latency six times over.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+struct Pair {
+  float a, b;
+};
+__device__ __forceinline__ Pair swap16(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return {__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ Pair swap32(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return {__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+template <class F>
+__device__ __forceinline__ float over_wave(float v, F&& f) {
+  v = f(v, dpp<0xB1>(v));   // quad_perm 1,0,3,2
+  v = f(v, dpp<0x4E>(v));   // quad_perm 2,3,0,1
+  v = f(v, dpp<0x141>(v));  // row_half_mirror
+  v = f(v, dpp<0x140>(v));  // row_mirror
+  Pair p = swap16(v);
+  v = f(p.a, p.b);
+  p = swap32(v);
+  return f(p.a, p.b);
+}
+__device__ __forceinline__ float wave_max(float v) {
+  return over_wave(v, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  return over_wave(v, [](float a, float b) { return a + b; });
+}
 
 // ------------------------------------------------------------- host checks
 inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }

@@ -9,6 +9,7 @@
 // the rounding of log S, 2^-24 |log S| relative.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "acdc_train.hpp"
@@ -58,41 +59,108 @@ __device__ __forceinline__ Run merge_wave(Run r) {
   return r;
 }
 
-// One workgroup per row: (M, S, H, logp).
+// (M, S, H, logp) of a row from its whole run and its target's logit.
+__device__ __forceinline__ float4 stat_of(const Run& run, float xt) {
+  const float log_s = logf(run.s);
+  // a row of zero-probability classes only has S = 0
+  const float nan = run.s > 0.f ? 0.f : __builtin_nanf("");
+  return make_float4(run.m, run.s, log_s - run.u / run.s + nan, (xt - run.m) - log_s + nan);
+}
+// The logit of target t >= 0; NaN past the classes.
+template <class T>
+__device__ __forceinline__ float target_logit(const typename T::Elem* row, long long t, int classes) {
+  return t < classes ? T::one(row[t]) : __builtin_nanf("");
+}
+
+// A row as chunks at aligned addresses and the elements around them: `head`
+// elements before the first chunk, `full` chunks, and `extra` elements in all
+// outside of them (fewer than 2 kPer), one for each of the first lanes.  A
+// chunk that lies across two cache lines costs both: rows of 65535 bfloat16
+// ran 20 % slower as chunks from the row's first element.
+template <class T>
+struct Cut {
+  int head, full, extra;
+  __device__ __forceinline__ Cut(const typename T::Elem* row, int classes) {
+    const unsigned off = unsigned(reinterpret_cast<uintptr_t>(row)) & 15u;
+    const int h = off != 0u ? int((16u - off) / sizeof(typename T::Elem)) : 0;
+    head = uniform(h < classes ? h : classes);
+    full = (classes - head) / T::kPer;
+    extra = classes - full * T::kPer;
+  }
+  // the element outside of the chunks that is lane's (lane < extra)
+  __device__ __forceinline__ int element(int lane) const { return lane < head ? lane : full * T::kPer + lane; }
+  // class t's chunk, or -1 if it lies outside of them (then it is lane_of(t)'s)
+  __device__ __forceinline__ int chunk_of(int t) const {
+    const int i = t - head;
+    return i >= 0 && i < full * T::kPer ? i / T::kPer : -1;
+  }
+  __device__ __forceinline__ int lane_of(int t) const { return t < head ? t : t - full * T::kPer; }
+};
+
+// Chunks (16 bytes) that one of `split` workgroups of a row takes: from, to.
+__device__ __forceinline__ void chunks_of(int full, int split, int k, int& from, int& to) {
+  const int per = (full + split - 1) / split;
+  from = min(full, k * per);
+  to = min(full, from + per);
+}
+
+// What a row leaves besides its gradient (null: not wanted).
+struct RowOut {
+  float* logp;
+  float* entropy;
+  float4* stat;
+  float *g, *h;
+};
+__device__ __forceinline__ void put_row(const RowOut& o, long long r, const float4& st, float g, float h) {
+  if (o.logp != nullptr) o.logp[r] = st.w;
+  if (o.entropy != nullptr) o.entropy[r] = st.z;
+  if (o.stat != nullptr) o.stat[r] = st;
+  if (o.g != nullptr) {
+    o.g[r] = g;
+    o.h[r] = h;
+  }
+}
+
+// A workgroup's part of a row, streamed: every thread keeps a run of its own.
+// Workgroup r * split + k takes part k of row r; with split = 1 it writes the
+// row's (M, S, H, logp), otherwise the runs of the parts.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_row_stats(const typename T::Elem* __restrict__ x, long long stride,
                                                         const void* __restrict__ targets, int bits, int classes,
-                                                        float4* __restrict__ stat) {
+                                                        int split, RowOut out, float4* __restrict__ parts) {
   __shared__ Run part[kThreads / 64];
-  const long long r = blockIdx.x;
+  const int k = blockIdx.x % unsigned(split);
+  const long long r = blockIdx.x / unsigned(split);
   const long long t = target_of(targets, bits, r);
   if (t < 0) {
-    if (threadIdx.x == 0) stat[r] = make_float4(0.f, 1.f, 0.f, 0.f);
+    if (threadIdx.x == 0 && k == 0) put_row(out, r, make_float4(0.f, 1.f, 0.f, 0.f), 0.f, 0.f);
     return;
   }
   const typename T::Elem* row = x + r * stride;
   Run run = empty_run();
-  const int full = classes / T::kPer;
-  for (int c = threadIdx.x; c < full; c += kThreads) {
-    const auto raw = load_chunk<T>(row + (long long)c * T::kPer);
+  const Cut<T> cut(row, classes);
+  int from, to;
+  chunks_of(cut.full, split, k, from, to);
+  for (int c = from + threadIdx.x; c < to; c += kThreads) {
+    const auto raw = load_chunk<T>(row + cut.head + (long long)c * T::kPer);
     Run b = empty_run();
 #pragma unroll
     for (int i = 0; i < T::kPer; ++i) b.m = fmaxf(b.m, T::get(raw, i));
 #pragma unroll
     for (int i = 0; i < T::kPer; ++i) {
-      const float d = below(T::get(raw, i), b.m), e = exp_of(d);
+      const float d = T::get(raw, i) - b.m, e = exp_of(d);
       b.s += e;
-      b.u += e * d;
+      b.u += e * fmaxf(d, -1e30f);
     }
     run = merge(run, b);
   }
-  for (int j = full * T::kPer + threadIdx.x; j < classes; j += kThreads) {
-    const float v = T::one(row[j]);
+  if (k == split - 1 && int(threadIdx.x) < cut.extra) {
+    const float v = T::one(row[cut.element(threadIdx.x)]);
     Run b = empty_run();
     b.m = fmaxf(b.m, v);
-    const float d = below(v, b.m), e = exp_of(d);
+    const float d = v - b.m, e = exp_of(d);
     b.s = e;
-    b.u = e * d;
+    b.u = e * fmaxf(d, -1e30f);
     run = merge(run, b);
   }
   run = merge_wave(run);
@@ -100,15 +168,55 @@ __global__ __launch_bounds__(kThreads) void k_row_stats(const typename T::Elem* 
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 1; w < kThreads / 64; ++w) run = merge(run, part[w]);
-    const float xt = t < classes ? T::one(row[t]) : __builtin_nanf("");
-    const float log_s = logf(run.s);
-    // a row of zero-probability classes only: S = 0
-    const float nan = run.s > 0.f ? 0.f : __builtin_nanf("");
-    stat[r] = make_float4(run.m, run.s, log_s - run.u / run.s + nan, (xt - run.m) - log_s + nan);
+    if (split == 1) put_row(out, r, stat_of(run, target_logit<T>(row, t, classes)), 0.f, 0.f);
+    else parts[r * split + k] = make_float4(run.m, run.s, run.u, 0.f);
   }
 }
 
-// dL/dlogits of one row per workgroup from its (M, S, H, logp), g and h.
+// The row's statistics out of its parts (at most 64), for a whole wave.
+template <class T>
+__device__ __forceinline__ float4 join_parts(const float4* __restrict__ parts, int split, long long r, float xt) {
+  const int lane = threadIdx.x % 64;
+  Run run = empty_run();
+  if (lane < split) {
+    const float4 p = parts[r * split + lane];
+    run = Run{p.x, p.y, p.z};
+  }
+  return stat_of(merge_wave(run), xt);
+}
+
+// Statistics of rows in parts: one wave per row; logp and entropy too.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_row_join(const typename T::Elem* __restrict__ x, long long stride,
+                                                       const void* __restrict__ targets, int bits, int classes,
+                                                       const float4* __restrict__ parts, int split, long long rows,
+                                                       RowOut out) {
+  const long long r = (long long)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
+  if (r >= rows) return;
+  const long long t = target_of(targets, bits, r);
+  float4 st = make_float4(0.f, 1.f, 0.f, 0.f);
+  if (t >= 0) st = join_parts<T>(parts, split, r, target_logit<T>(x + r * stride, t, classes));
+  if (threadIdx.x % 64 == 0) put_row(out, r, st, 0.f, 0.f);
+}
+
+// What turns a logit into its gradient: y_j = e_j (a + b d_j), d_j = x_j - M,
+// and g more for the target.
+struct Slope {
+  float m, a, b;
+};
+__device__ __forceinline__ Slope slope_of(float m, float s, float h_row, float g, float h) {
+  const float inv = 1.f / s;
+  return {m, -inv * (g + h * (h_row - logf(s))), -inv * h};
+}
+__device__ __forceinline__ float slope_value(const Slope& k, float x) {
+  const float d = x - k.m;
+  // a class of probability 0 has d = -inf or nearly: its 0 is not to meet an infinity
+  return exp_of(d) * (k.a + k.b * fmaxf(d, -1e30f));
+}
+
+// dL/dlogits from each row's (M, S, H, logp), g and h; workgroups as in
+// k_row_stats, the last rows first: what a forward read last is what the cache
+// still holds.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x, long long stride,
                                                        const void* __restrict__ targets, int bits, int classes,
@@ -116,8 +224,10 @@ __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x
                                                        const float* __restrict__ grad_logp,
                                                        const float* __restrict__ grad_entropy,
                                                        const float* __restrict__ scale, float scale_host,
-                                                       typename T::Elem* grad, long long grad_stride) {
-  const long long r = blockIdx.x;
+                                                       typename T::Elem* grad, long long grad_stride, int split) {
+  const unsigned at = gridDim.x - 1 - blockIdx.x;
+  const int k = at % unsigned(split);
+  const long long r = at / unsigned(split);
   const long long t = target_of(targets, bits, r);
   typename T::Elem* out = grad + r * grad_stride;
   const typename T::Elem* row = x + r * stride;
@@ -127,41 +237,42 @@ __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x
     g = grad_logp[r];
     h = grad_entropy != nullptr ? grad_entropy[r] : 0.f;
   }
-  const int full = classes / T::kPer;
+  const Cut<T> cut(row, classes);
+  int from, to;
+  chunks_of(cut.full, split, k, from, to);
+  const int one = cut.element(threadIdx.x);
+  const bool has_one = k == split - 1 && int(threadIdx.x) < cut.extra;
+  const typename T::Elem* body = row + cut.head;
+  typename T::Elem* out_body = out + cut.head;
   if (g == 0.f && h == 0.f) {
     float zero[T::kPer] = {};
-    for (int k = threadIdx.x; k < full; k += kThreads) store_chunk<T>(out + (long long)k * T::kPer, T::pack(zero));
-    for (int j = full * T::kPer + threadIdx.x; j < classes; j += kThreads) out[j] = T::to(0.f);
+    for (int i = from + threadIdx.x; i < to; i += kThreads)
+      store_chunk<T>(out_body + (long long)i * T::kPer, T::pack(zero));
+    if (has_one) out[one] = T::to(0.f);
     return;
   }
   g *= c;
   h *= c;
   const float4 st = stat[r];
-  const float inv = 1.f / st.y;
-  // log p_j + H = d_j + (H - log S)
-  const float k0 = g + h * (st.z - logf(st.y)) + (t < classes ? 0.f : __builtin_nanf(""));
-  auto value = [&](float v, long long j) {
-    const float d = below(v, st.x);
-    const float y = -(exp_of(d) * inv) * (k0 + h * d);
-    return j == t ? y + g : y;
-  };
-  for (int k = threadIdx.x; k < full; k += kThreads) {
-    const auto raw = load_chunk<T>(row + (long long)k * T::kPer);
+  Slope sl = slope_of(st.x, st.y, st.z, g, h);
+  if (t >= classes) sl.a = __builtin_nanf("");
+  // the thread that writes the target's chunk writes the target again, with its g
+  bool mine = false;
+  if (t < classes) {
+    const int tc = cut.chunk_of(int(t));
+    mine = tc >= 0 ? tc >= from && tc < to && (tc - from) % kThreads == int(threadIdx.x)
+                   : has_one && cut.lane_of(int(t)) == int(threadIdx.x);
+  }
+  const float yt = mine ? slope_value(sl, T::one(row[t])) + g : 0.f;
+  for (int i = from + threadIdx.x; i < to; i += kThreads) {
+    const auto raw = load_chunk<T>(body + (long long)i * T::kPer);
     float y[T::kPer];
 #pragma unroll
-    for (int i = 0; i < T::kPer; ++i) y[i] = value(T::get(raw, i), (long long)k * T::kPer + i);
-    store_chunk<T>(out + (long long)k * T::kPer, T::pack(y));
+    for (int e = 0; e < T::kPer; ++e) y[e] = slope_value(sl, T::get(raw, e));
+    store_chunk<T>(out_body + (long long)i * T::kPer, T::pack(y));
   }
-  for (int j = full * T::kPer + threadIdx.x; j < classes; j += kThreads) out[j] = T::to(value(T::one(row[j]), j));
-}
-
-// logp and entropy of every row out of its statistics.
-__global__ __launch_bounds__(kThreads) void k_row_values(const float4* __restrict__ stat, long long rows,
-                                                         float* __restrict__ logp, float* __restrict__ entropy) {
-  const long long r = (long long)blockIdx.x * kThreads + threadIdx.x;
-  if (r >= rows) return;
-  logp[r] = stat[r].w;
-  if (entropy != nullptr) entropy[r] = stat[r].z;
+  if (has_one) out[one] = T::to(slope_value(sl, T::one(row[one])));
+  if (mine) out[t] = T::to(yt);
 }
 
 // Sum of v over the workgroup in a fixed order, for every thread.
@@ -178,8 +289,7 @@ __device__ __forceinline__ double total_of(double v, double* part) {
   return s;
 }
 
-// The policy loss of all rows: one workgroup.  Writes stats, logp and
-// row_grads = (dL/dlogp, dL/dH).
+// --------------------------------------------------------- the policy loss
 constexpr int kWide = 1024;
 struct PolicyArgs {
   const void* targets;
@@ -192,121 +302,512 @@ __device__ __forceinline__ float weight_of(const PolicyArgs& a, long long r) {
   if (target_of(a.targets, a.bits, r) < 0) return 0.f;
   return a.weights != nullptr ? a.weights[r] : 1.f;
 }
-__global__ __launch_bounds__(kWide) void k_policy_rows(PolicyArgs a, const float4* __restrict__ stat,
-                                                       float* __restrict__ stats, float* __restrict__ logp,
-                                                       float* __restrict__ grads) {
-  __shared__ double part[kWide / 64];
+__device__ __forceinline__ float norm_of(const PolicyArgs& a, double total) {
+  return !a.p.mean ? 1.f : total != 0.0 ? float(1.0 / total) : 0.f;
+}
+
+constexpr int kStats = 6;
+struct PolicyRow {
+  float g, h;        // dL/dlogp, dL/dH
+  float v[kStats];   // what the row adds to the stats
+};
+// One row that takes part, of normalised weight w.
+__device__ __forceinline__ PolicyRow policy_row(const acdc_policy_params& p, float w, float logp, float entropy,
+                                                float old, float adv, bool has_ref, float ref) {
+  const float ratio = expf(logp - old), lo = 1.f - p.clip_low, hi = 1.f + p.clip_high;
+  const float free_ = ratio * adv, bounded = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv;
+  const bool cut = bounded < free_;
+  const float policy = -(cut ? bounded : free_);
+  float em = 0.f, kl = 0.f;
+  if (has_ref) {
+    const float k = ref - logp;
+    em = expm1f(k);  // exp(k) - 1 - k of policies close to each other is a small difference
+    kl = em - k;
+  }
+  PolicyRow r;
+  r.g = w * ((cut ? 0.f : -free_) - p.kl_coef * em);
+  r.h = -p.entropy_coef * w;
+  r.v[0] = w * (policy + p.kl_coef * kl - p.entropy_coef * entropy);
+  r.v[1] = w * policy;
+  r.v[2] = w * kl;
+  r.v[3] = w * entropy;
+  r.v[4] = cut ? w : 0.f;
+  r.v[5] = w * ratio;
+  return r;
+}
+
+// Sums of the weights, for the kernels that need 1 / W: rows in at most
+// kWeightSums groups, one workgroup each.
+constexpr int kWeightSums = 256;
+__host__ __device__ inline long long weight_group(long long rows) {
+  const long long per = (rows + kWeightSums - 1) / kWeightSums;
+  return per > kThreads ? per : kThreads;
+}
+__global__ __launch_bounds__(kThreads) void k_weight_sums(PolicyArgs a, double* __restrict__ sums) {
+  __shared__ double part[kThreads / 64];
+  const long long per = weight_group(a.rows), from = blockIdx.x * per;
+  const long long to = from + per < a.rows ? from + per : a.rows;
   double w = 0.0;
-  for (long long r = threadIdx.x; r < a.rows; r += kWide) w += weight_of(a, r);
-  const double total = total_of<kWide>(w, part);
-  const float norm = !a.p.mean ? 1.f : total != 0.0 ? float(1.0 / total) : 0.f;
-  double sum[6] = {};
-  for (long long r = threadIdx.x; r < a.rows; r += kWide) {
-    const float wr = weight_of(a, r) * norm;
-    float g = 0.f, h = 0.f, lp = 0.f;
-    if (wr != 0.f) {
-      const float4 st = stat[r];
-      lp = st.w;
-      const float adv = a.advantages[r], ratio = expf(lp - a.old[r]);
-      const float lo = 1.f - a.p.clip_low, hi = 1.f + a.p.clip_high;
-      const float free_ = ratio * adv, bounded = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv;
-      const bool cut = bounded < free_;
-      const float policy = -(cut ? bounded : free_);
-      float em = 0.f, kl = 0.f;
-      if (a.ref != nullptr) {
-        const float k = a.ref[r] - lp;
-        em = expm1f(k);
-        kl = em - k;
-      }
-      g = wr * ((cut ? 0.f : -free_) - a.p.kl_coef * em);
-      h = -a.p.entropy_coef * wr;
-      const float loss = policy + a.p.kl_coef * kl - a.p.entropy_coef * st.z;
-      const float v[6] = {loss, policy, kl, st.z, cut ? 1.f : 0.f, ratio};
+#pragma unroll 4
+  for (long long r = from + threadIdx.x; r < to; r += kThreads) w += double(weight_of(a, r));
+  w = total_of<kThreads>(w, part);
+  if (threadIdx.x == 0) sums[blockIdx.x] = w;
+}
+// W out of the sums, for a whole wave.
+__device__ __forceinline__ double weight_total(const double* __restrict__ sums, int groups) {
+  double w = 0.0;
+  for (int i = threadIdx.x % 64; i < groups; i += 64) w += sums[i];
 #pragma unroll
-      for (int i = 0; i < 6; ++i) sum[i] += double(wr) * double(v[i]);
+  for (int o = 32; o > 0; o >>= 1) w += __shfl_xor(w, o);
+  return w;
+}
+
+// The policy loss of rows whose statistics stand in `stat` (in parts of
+// `split`, where that is more than 1): one thread per row (wave per row with
+// parts).  With one workgroup it sums the weights and writes the stats itself;
+// with more, `sums` holds the weights' sums and `partial` gets each
+// workgroup's stats.
+template <class T>
+__global__ __launch_bounds__(kWide) void k_policy_rows(PolicyArgs a, const typename T::Elem* __restrict__ x,
+                                                       long long stride, int classes, const float4* __restrict__ parts,
+                                                       int split, const double* __restrict__ sums, int groups,
+                                                       const float4* stat, RowOut out, float* __restrict__ partial) {
+  __shared__ double part[kWide / 64];
+  double total;
+  if (gridDim.x == 1) {
+    double w = 0.0;
+    for (long long r = threadIdx.x; r < a.rows; r += kWide) w += double(weight_of(a, r));
+    total = total_of<kWide>(w, part);
+  } else {
+    total = weight_total(sums, groups);
+  }
+  const float norm = norm_of(a, total);
+  double sum[kStats] = {};
+  const int per = split > 1 ? kWide / 64 : kWide, me = split > 1 ? threadIdx.x / 64 : threadIdx.x;
+  for (long long r = (long long)blockIdx.x * per + me; r < a.rows; r += (long long)gridDim.x * per) {
+    const float w = weight_of(a, r) * norm;
+    float4 st = make_float4(0.f, 1.f, 0.f, 0.f);
+    PolicyRow row{};
+    if (w != 0.f) {
+      if (split > 1) {
+        const long long t = target_of(a.targets, a.bits, r);
+        st = join_parts<T>(parts, split, r, target_logit<T>(x + r * stride, t, classes));
+      } else {
+        st = stat[r];
+      }
+      row = policy_row(a.p, w, st.w, st.z, a.old[r], a.advantages[r], a.ref != nullptr, a.ref != nullptr ? a.ref[r] : 0.f);
     }
-    logp[r] = lp;
-    grads[r] = g;
-    grads[a.rows + r] = h;
+    if (split == 1 || threadIdx.x % 64 == 0) {
+      put_row(out, r, st, row.g, row.h);
+#pragma unroll
+      for (int i = 0; i < kStats; ++i) sum[i] += double(row.v[i]);
+    }
   }
 #pragma unroll
-  for (int i = 0; i < 6; ++i) {
+  for (int i = 0; i < kStats; ++i) {
     const double s = total_of<kWide>(sum[i], part);
-    if (threadIdx.x == 0) stats[i] = float(s);
+    if (threadIdx.x == 0) partial[(long long)i * gridDim.x + blockIdx.x] = float(s);
   }
 }
 
+// stats[i] = sum of partial[i][0 .. n - 1]: one workgroup.
+template <int STATS>
+__global__ __launch_bounds__(kWide) void k_total(const float* __restrict__ partial, int n, float factor,
+                                                 float* __restrict__ stats) {
+  __shared__ float part[kWide / 64][STATS];
+  double sum[STATS] = {};
+#pragma unroll 4
+  for (int j = threadIdx.x; j < n; j += kWide)
+#pragma unroll
+    for (int i = 0; i < STATS; ++i) sum[i] += double(partial[(long long)i * n + j]);
+#pragma unroll
+  for (int i = 0; i < STATS; ++i) {
+    const float v = wave_sum(float(sum[i]));
+    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64][i] = v;
+  }
+  __syncthreads();
+  if (threadIdx.x < STATS) {
+    double s = 0.0;
+#pragma unroll
+    for (int w = 0; w < kWide / 64; ++w) s += double(part[w][threadIdx.x]);
+    stats[threadIdx.x] = float(s * double(factor));
+  }
+}
+
+// Workgroup over a row that THREADS lanes share: a wave (64), which needs no
+// barrier, or the workgroup.
+template <int THREADS>
+struct Group {
+  float* slots;  // 3 * THREADS / 64 floats of LDS
+  __device__ __forceinline__ float max(float v) {
+    v = wave_max(v);
+    if constexpr (THREADS > 64) {
+      if (threadIdx.x % 64 == 0) slots[threadIdx.x / 64] = v;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < THREADS / 64; ++w) v = fmaxf(v, slots[w]);
+    }
+    return v;
+  }
+  // s and u over the group; the slots are those that max does not use, so that
+  // a barrier a call is enough (the next row's max comes after this one's barrier)
+  __device__ __forceinline__ void sum(float& s, float& u) {
+    s = wave_sum(s);
+    u = wave_sum(u);
+    if constexpr (THREADS > 64) {
+      constexpr int W = THREADS / 64;
+      if (threadIdx.x % 64 == 0) {
+        slots[W + threadIdx.x / 64] = s;
+        slots[2 * W + threadIdx.x / 64] = u;
+      }
+      __syncthreads();
+      s = u = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        s += slots[W + w];
+        u += slots[2 * W + w];
+      }
+    }
+  }
+};
+
+// The policy loss and its gradient in one pass over the logits: a row stays in
+// the registers of its THREADS lanes, NC chunks each, from its load to its
+// gradient's store.  Rows blockIdx, blockIdx + gridDim, ... of a workgroup;
+// its rows' stats go into partial[.][blockIdx], or with one workgroup (which
+// then sums the weights itself) into stats.
+constexpr int fused_waves(int nc) { return nc <= 4 ? 8 : nc <= 8 ? 6 : nc <= 12 ? 5 : 4; }
+template <class T, int WG, int THREADS, int NC>
+__global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(fused_waves(NC)))) void k_policy_fused(
+    PolicyArgs a, const typename T::Elem* x, long long stride, int classes, const double* __restrict__ sums, int groups,
+    typename T::Elem* grad, long long grad_stride, RowOut out, float* __restrict__ partial) {
+  constexpr int ROWS = WG / THREADS;
+  __shared__ float slots[3 * (WG / 64)];
+  __shared__ double wide[WG / 64];
+  __shared__ double acc[ROWS][kStats];  // each row's stats: too seldom to hold registers
+  Group<THREADS> group{slots};
+  const int lane = threadIdx.x % THREADS;
+  const int sub = ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0;
+  double total;
+  if (gridDim.x == 1) {
+    double w = 0.0;
+    for (long long r = threadIdx.x; r < a.rows; r += WG) w += double(weight_of(a, r));
+    total = total_of<WG>(w, wide);
+  } else {
+    total = weight_total(sums, groups);
+  }
+  const float norm = norm_of(a, total);
+  if (threadIdx.x < ROWS * kStats) (&acc[0][0])[threadIdx.x] = 0.0;
+  __syncthreads();
+  const unsigned at = unsigned(lane) * 16u;
+  for (long long r = (long long)blockIdx.x * ROWS + sub; r < a.rows; r += (long long)gridDim.x * ROWS) {
+    const long long target = target_of(a.targets, a.bits, r);
+    const int t = uniform(target < 0 ? -1 : target < classes ? int(target) : classes);
+    const float w = uniform(t < 0 ? 0.f : (a.weights != nullptr ? a.weights[r] : 1.f) * norm);
+    const typename T::Elem* row = x + r * stride;
+    typename T::Elem* to = grad + r * grad_stride;
+    const Cut<T> cut(row, classes);
+    const typename T::Elem* body = row + cut.head;
+    typename T::Elem* to_body = to + cut.head;
+    const int one = cut.element(lane);
+    const bool has_one = lane < cut.extra;
+    auto chunk = [&](int c) { return c * THREADS + lane < cut.full; };
+    if (w == 0.f) {
+      float zero[T::kPer] = {};
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (chunk(c)) store_chunk_at<T>(to_body, c * THREADS * 16u, at, T::pack(zero));
+      if (has_one) to[one] = T::to(0.f);
+      if (lane == 0) put_row(out, r, make_float4(0.f, 1.f, 0.f, 0.f), 0.f, 0.f);
+      continue;
+    }
+    typename T::Raw raw[NC];
+    // between two passes over the registers: without it the compiler keeps every
+    // value's difference and exponential from one pass for the next, two or three
+    // registers a value, and spills
+    auto forget = [&] {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(raw[c]));
+    };
+#pragma unroll
+    for (int c = 0; c < NC; ++c) raw[c] = typename T::Raw{};
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      if (chunk(c)) raw[c] = load_chunk_at<T>(body, c * THREADS * 16u, at);
+    const float last = has_one ? T::one(row[one]) : kNegMax;
+    const float xt = uniform(target_logit<T>(row, t, classes));
+    const float old = uniform(a.old[r]), adv = uniform(a.advantages[r]);
+    const float ref = uniform(a.ref != nullptr ? a.ref[r] : 0.f);
+    float m = fmaxf(kNegMax, last);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      if (chunk(c)) {
+#pragma unroll
+        for (int i = 0; i < T::kPer; ++i) m = fmaxf(m, T::get(raw[c], i));
+      }
+    forget();
+    m = uniform(group.max(m));
+    float s = 0.f, u = 0.f;
+    auto add = [&](float v) {
+      const float d = v - m, e = exp_of(d);
+      s += e;
+      u += e * fmaxf(d, -1e30f);
+    };
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      if (chunk(c)) {
+#pragma unroll
+        for (int i = 0; i < T::kPer; ++i) add(T::get(raw[c], i));
+      }
+    if (has_one) add(last);
+    forget();
+    group.sum(s, u);
+    const float4 st = stat_of(Run{m, s, u}, xt);
+    const PolicyRow p = policy_row(a.p, w, st.w, st.z, old, adv, a.ref != nullptr, ref);
+    const float g = uniform(p.g * a.p.grad_scale);
+    Slope sl = slope_of(m, s, st.z, g, p.h * a.p.grad_scale);
+    sl.a = uniform(sl.a);
+    sl.b = uniform(sl.b);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      if (chunk(c)) {
+        float y[T::kPer];
+#pragma unroll
+        for (int i = 0; i < T::kPer; ++i) y[i] = slope_value(sl, T::get(raw[c], i));
+        store_chunk_at<T>(to_body, c * THREADS * 16u, at, T::pack(y));
+      }
+    if (has_one) to[one] = T::to(slope_value(sl, last));
+    // the lane that wrote the target's chunk writes the target again, with its g
+    const int tc = cut.chunk_of(t);
+    if (t < classes && (tc >= 0 ? tc % THREADS : cut.lane_of(t)) == lane) to[t] = T::to(slope_value(sl, xt) + g);
+    if (lane == 0) {
+      put_row(out, r, st, p.g, p.h);
+#pragma unroll
+      for (int i = 0; i < kStats; ++i) acc[sub][i] += double(p.v[i]);
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < kStats) {
+    double v = 0.0;
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q) v += acc[q][threadIdx.x];
+    partial[(long long)threadIdx.x * gridDim.x + blockIdx.x] = float(v);
+  }
+}
+
+// The same for short rows (up to 4 chunks a lane of a wave): WAVES waves hold RPW
+// rows each, and one of them does the arithmetic of all rows, a lane for each.
+// Left to every wave for its own row, that arithmetic (three exponentials, two
+// logarithms, two quotients) is most of its work: 20000 rows of 257 bfloat16
+// classes took 33 us with a wave per row.
+template <class T, int WAVES, int RPW, int NC>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(WAVES > 8 ? 4 : 5))) void k_policy_tile(
+    PolicyArgs a, const typename T::Elem* x, long long stride, int classes, const double* __restrict__ sums, int groups,
+    typename T::Elem* grad, long long grad_stride, RowOut out, float* __restrict__ partial) {
+  constexpr int ROWS = WAVES * RPW;
+  __shared__ float4 stat[ROWS];   // M, S, U, x_t
+  __shared__ float slope[ROWS][3];
+  __shared__ double acc[kStats];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const unsigned at = unsigned(lane) * 16u;
+  float norm = 1.f;
+  if (gridDim.x > 1 && wave == 0) norm = norm_of(a, weight_total(sums, groups));
+  if (threadIdx.x < kStats) acc[threadIdx.x] = 0.0;
+  for (long long base = (long long)blockIdx.x * ROWS; base < a.rows; base += (long long)gridDim.x * ROWS) {
+    typename T::Raw raw[RPW][NC];
+    float last[RPW];
+    int t[RPW];
+    bool on[RPW];
+#pragma unroll
+    for (int q = 0; q < RPW; ++q) {
+      const long long r = base + wave * RPW + q;
+      t[q] = -1;
+      on[q] = false;
+      if (r < a.rows) {
+        const long long target = target_of(a.targets, a.bits, r);
+        t[q] = uniform(target < 0 ? -1 : target < classes ? int(target) : classes);
+        on[q] = t[q] >= 0 && (a.weights == nullptr || uniform(a.weights[r]) != 0.f);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < RPW; ++q) {
+      last[q] = kNegMax;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) raw[q][c] = typename T::Raw{};
+      if (!on[q]) continue;
+      const typename T::Elem* row = x + (base + wave * RPW + q) * stride;
+      const Cut<T> cut(row, classes);
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (c * 64 + lane < cut.full) raw[q][c] = load_chunk_at<T>(row + cut.head, c * 1024u, at);
+      if (lane < cut.extra) last[q] = T::one(row[cut.element(lane)]);
+    }
+#pragma unroll
+    for (int q = 0; q < RPW; ++q) {
+      if (!on[q]) continue;
+      const typename T::Elem* row = x + (base + wave * RPW + q) * stride;
+      const Cut<T> cut(row, classes);
+      float m = last[q];
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (c * 64 + lane < cut.full) {
+#pragma unroll
+          for (int i = 0; i < T::kPer; ++i) m = fmaxf(m, T::get(raw[q][c], i));
+        }
+      m = wave_max(fmaxf(m, kNegMax));
+      float s = 0.f, u = 0.f;
+      auto add = [&](float v) {
+        const float d = v - m, e = exp_of(d);
+        s += e;
+        u += e * fmaxf(d, -1e30f);
+      };
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (c * 64 + lane < cut.full) {
+#pragma unroll
+          for (int i = 0; i < T::kPer; ++i) add(T::get(raw[q][c], i));
+        }
+      if (lane < cut.extra) add(last[q]);
+      s = wave_sum(s);
+      u = wave_sum(u);
+      const float xt = target_logit<T>(row, t[q], classes);
+      if (lane == 0) stat[wave * RPW + q] = make_float4(m, s, u, xt);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(raw[q][c]));
+    }
+    __syncthreads();
+    if (wave == 0) {
+      const long long r = base + lane;
+      float w = lane < ROWS && r < a.rows ? weight_of(a, r) : 0.f;
+      if (gridDim.x == 1) {  // these are all rows
+        double total = double(w);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
+        norm = norm_of(a, total);
+      }
+      w *= norm;
+      float4 st = make_float4(0.f, 1.f, 0.f, 0.f);
+      PolicyRow p{};
+      Slope sl{};
+      if (w != 0.f) {
+        const float4 z = stat[lane];
+        st = stat_of(Run{z.x, z.y, z.z}, z.w);
+        p = policy_row(a.p, w, st.w, st.z, a.old[r], a.advantages[r], a.ref != nullptr, a.ref != nullptr ? a.ref[r] : 0.f);
+        sl = slope_of(st.x, st.y, st.z, p.g * a.p.grad_scale, p.h * a.p.grad_scale);
+      }
+      if (lane < ROWS && r < a.rows) {
+        put_row(out, r, st, p.g, p.h);
+        slope[lane][0] = sl.a;
+        slope[lane][1] = sl.b;
+        slope[lane][2] = w != 0.f ? p.g * a.p.grad_scale : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < kStats; ++i) {
+        const float v = wave_sum(p.v[i]);
+        if (lane == 0) acc[i] += double(v);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < RPW; ++q) {
+      const long long r = base + wave * RPW + q;
+      if (r >= a.rows) continue;
+      const typename T::Elem* row = x + r * stride;
+      typename T::Elem* to = grad + r * grad_stride;
+      const Cut<T> cut(row, classes);
+      const int i0 = wave * RPW + q;
+      // a row that takes no part has a = b = g = 0 and zeros for logits: its gradient is 0
+      const Slope sl{on[q] ? uniform(stat[i0].x) : 0.f, uniform(slope[i0][0]), uniform(slope[i0][1])};
+      const float g = uniform(slope[i0][2]);
+      if (!on[q]) last[q] = 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (c * 64 + lane < cut.full) {
+          float y[T::kPer];
+#pragma unroll
+          for (int i = 0; i < T::kPer; ++i) y[i] = slope_value(sl, T::get(raw[q][c], i));
+          store_chunk_at<T>(to + cut.head, c * 1024u, at, T::pack(y));
+        }
+      if (lane < cut.extra) to[cut.element(lane)] = T::to(slope_value(sl, last[q]));
+      if (on[q] && t[q] < classes) {
+        const int tc = cut.chunk_of(t[q]);
+        if ((tc >= 0 ? tc % 64 : cut.lane_of(t[q])) == lane) to[t[q]] = T::to(slope_value(sl, stat[i0].w) + g);
+      }
+    }
+    __syncthreads();  // before the next tile's statistics
+  }
+  __syncthreads();
+  if (threadIdx.x < kStats) partial[(long long)threadIdx.x * gridDim.x + blockIdx.x] = float(acc[threadIdx.x]);
+}
+
+// ----------------------------------------------------- the preference loss
 __device__ __forceinline__ long long offset_of(const void* offsets, int bits, long long s, long long rows) {
   const long long o = bits == 64 ? static_cast<const long long*>(offsets)[s]
                                  : (long long)static_cast<const int*>(offsets)[s];
   return o < 0 ? 0 : o > rows ? rows : o;
 }
 
-// reward of every sequence: one workgroup per sequence.
-__global__ __launch_bounds__(kThreads) void k_rewards(const void* __restrict__ targets, int bits,
-                                                      const void* __restrict__ offsets, int offset_bits,
-                                                      const float* __restrict__ ref, long long rows, float beta,
-                                                      const float4* __restrict__ stat, float* __restrict__ reward) {
-  __shared__ double part[kThreads / 64];
-  const long long s = blockIdx.x;
-  const long long a = offset_of(offsets, offset_bits, s, rows), b = offset_of(offsets, offset_bits, s + 1, rows);
-  double v = 0.0;
-  for (long long r = a + threadIdx.x; r < b; r += kThreads)
-    if (target_of(targets, bits, r) >= 0) v += double(stat[r].w) - double(ref[r]);
-  v = total_of<kThreads>(v, part);
-  if (threadIdx.x == 0) reward[s] = float(beta * v);
-}
-
 // log(1 + exp(z))
 __device__ __forceinline__ float softplus(float z) { return fmaxf(z, 0.f) + log1pf(expf(-fabsf(z))); }
 
-// Losses and slopes dL/dlogp of every sequence's rows: one workgroup.
-__global__ __launch_bounds__(kWide) void k_pairs(const float* __restrict__ reward, long long pairs, float beta, float e,
-                                                 float* __restrict__ stats, float* __restrict__ slope) {
-  __shared__ double part[kWide / 64];
-  double sum[5] = {};
-  for (long long p = threadIdx.x; p < pairs; p += kWide) {
-    const float good = reward[2 * p], bad = reward[2 * p + 1], m = good - bad;
-    const float loss = (1.f - e) * softplus(-m) + e * softplus(m);
-    // NaN margins are not counted as wins, and give NaN slopes
-    const float s = (e / (1.f + expf(-m)) - (1.f - e) / (1.f + expf(m))) * (beta / float(pairs));
-    slope[2 * p] = s;
-    slope[2 * p + 1] = -s;
-    const float v[5] = {loss, m > 0.f ? 1.f : 0.f, m, good, bad};
-#pragma unroll
-    for (int i = 0; i < 5; ++i) sum[i] += double(v[i]);
-  }
-#pragma unroll
-  for (int i = 0; i < 5; ++i) {
-    const double s = total_of<kWide>(sum[i], part);
-    if (threadIdx.x == 0) stats[i] = pairs > 0 ? float(s / double(pairs)) : 0.f;
-  }
+constexpr int kPairStats = 5;
+struct PairArgs {
+  const void *targets, *offsets;
+  int bits, offset_bits;
+  const float* ref;
+  long long rows, pairs;
+  float beta, smoothing;
+};
+
+// Sum of logp - logp_ref over a sequence, by a group of N threads.
+__device__ __forceinline__ double excess(const PairArgs& a, const float4* __restrict__ stat, long long from, long long to,
+                                         int lane, int n) {
+  double v = 0.0;
+#pragma unroll 4
+  for (long long r = from + lane; r < to; r += n)
+    if (target_of(a.targets, a.bits, r) >= 0) v += double(stat[r].w) - double(a.ref[r]);
+  return v;
 }
 
-// logp and row_grads of the preference loss.
-__global__ __launch_bounds__(kThreads) void k_preference_rows(const void* __restrict__ targets, int bits,
-                                                              const void* __restrict__ offsets, int offset_bits,
-                                                              long long rows, long long pairs,
-                                                              const float4* __restrict__ stat,
-                                                              const float* __restrict__ slope, float* __restrict__ logp,
-                                                              float* __restrict__ grads) {
-  const long long r = (long long)blockIdx.x * kThreads + threadIdx.x;
-  if (r >= rows) return;
-  const bool on = target_of(targets, bits, r) >= 0;
-  // the sequence s with offsets[s] <= r < offsets[s + 1], if any
-  long long lo = 0, hi = 2 * pairs;  // offsets[lo] <= r < offsets[hi] once both ends hold
-  float g = 0.f;
-  if (on && pairs > 0 && offset_of(offsets, offset_bits, 0, rows) <= r && r < offset_of(offsets, offset_bits, hi, rows)) {
-    while (hi - lo > 1) {
-      const long long mid = (lo + hi) / 2;
-      if (offset_of(offsets, offset_bits, mid, rows) <= r) lo = mid;
-      else hi = mid;
+// Rewards, margin and loss of pairs, and dL/dlogp of their rows: a wave per
+// pair, pairs wave, wave + waves, ...; the rows' g are 0 before it.  Each
+// workgroup's sums over its pairs go into partial[.][blockIdx] (stats, divided
+// by the pairs, with one workgroup).
+__global__ __launch_bounds__(kWide) void k_pairs(PairArgs a, const float4* __restrict__ stat, float* __restrict__ g,
+                                                 float* __restrict__ partial) {
+  __shared__ double acc[kWide / 64][kPairStats];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
+  double sum[kPairStats] = {};
+  for (long long p = (long long)blockIdx.x * waves + wave; p < a.pairs; p += (long long)gridDim.x * waves) {
+    const long long o0 = offset_of(a.offsets, a.offset_bits, 2 * p, a.rows);
+    const long long o1 = offset_of(a.offsets, a.offset_bits, 2 * p + 1, a.rows);
+    const long long o2 = offset_of(a.offsets, a.offset_bits, 2 * p + 2, a.rows);
+    double v0 = excess(a, stat, o0, o1, lane, 64), v1 = excess(a, stat, o1, o2, lane, 64);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      v0 += __shfl_xor(v0, o);
+      v1 += __shfl_xor(v1, o);
     }
-    g = slope[lo];
+    const float good = float(a.beta * v0), bad = float(a.beta * v1), m = float(a.beta * (v0 - v1)), e = a.smoothing;
+    const float loss = (1.f - e) * softplus(-m) + e * softplus(m);
+    // a NaN margin is no win, and gives NaN slopes
+    const float slope = (e / (1.f + expf(-m)) - (1.f - e) / (1.f + expf(m))) * (a.beta / float(a.pairs));
+    for (long long r = o0 + lane; r < o2; r += 64)
+      if (target_of(a.targets, a.bits, r) >= 0) g[r] = r < o1 ? slope : -slope;
+    const float v[kPairStats] = {loss, m > 0.f ? 1.f : 0.f, m, good, bad};
+#pragma unroll
+    for (int i = 0; i < kPairStats; ++i) sum[i] += double(v[i]);
   }
-  logp[r] = on ? stat[r].w : 0.f;
-  grads[r] = g;
-  grads[rows + r] = 0.f;
+  if (lane == 0)
+#pragma unroll
+    for (int i = 0; i < kPairStats; ++i) acc[wave][i] = sum[i];
+  __syncthreads();
+  if (threadIdx.x < kPairStats) {
+    double s = 0.0;
+    for (int w = 0; w < waves; ++w) s += acc[w][threadIdx.x];
+    if (gridDim.x == 1) s = a.pairs > 0 ? s / double(a.pairs) : 0.0;
+    partial[(long long)threadIdx.x * gridDim.x + blockIdx.x] = float(s);
+  }
 }
 
 // ------------------------------------------------------------------ host side
@@ -348,10 +849,22 @@ bool floats_ok(std::initializer_list<const void*> must, std::initializer_list<co
 }
 
 size_t up256(size_t b) { return (b + 255) & ~size_t(255); }
+// Workgroups that share a row.  One for each while the rows fill the card
+// (kFewRows of them do); with fewer, long rows are cut into parts of at least
+// 4096 values, up to about four workgroups a CU.
+constexpr int64_t kFewRows = 128;
+int split_of(int64_t rows, int32_t classes) {
+  if (rows < 1 || rows >= kFewRows) return 1;
+  const int64_t parts = std::min<int64_t>({64, 1024 / rows, classes / 4096});
+  return int(std::max<int64_t>(1, parts));
+}
+// Workgroups (and so partial stats) of the kernels that sum the policy's stats.
+constexpr int64_t kMaxPartials = 8192;
+
 struct Workspace {
-  size_t stat, grads, reward, slope, total;
+  size_t stat, grads, parts, sums, partial, total;
 };
-Workspace layout(int64_t rows, int64_t pairs) {
+Workspace layout(int64_t rows, int32_t classes, int64_t pairs) {
   Workspace w{};
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -359,10 +872,13 @@ Workspace layout(int64_t rows, int64_t pairs) {
     at += up256(bytes);
     return o;
   };
+  const int split = split_of(rows, classes);
   w.stat = take(size_t(rows) * sizeof(float4));
   w.grads = take(size_t(rows) * 2 * sizeof(float));
-  w.reward = take(size_t(pairs) * 2 * sizeof(float));
-  w.slope = take(size_t(pairs) * 2 * sizeof(float));
+  w.parts = take(split > 1 ? size_t(rows) * split * sizeof(float4) : 0);
+  w.sums = take(kWeightSums * sizeof(double));
+  // at least two workgroups, see acdc_policy_loss
+  w.partial = take(size_t(std::max<int64_t>(2, std::min(std::max(rows, pairs), kMaxPartials))) * kStats * sizeof(float));
   w.total = at;
   return w;
 }
@@ -381,26 +897,68 @@ void with_type(int32_t dtype, F&& f) {
   else f.template operator()<BF16>();
 }
 
-int launch_stats(const void* logits, int32_t dtype, int64_t stride, const void* targets, int32_t bits, int64_t rows,
-                 int32_t classes, float4* stat, hipStream_t s) {
-  with_type(dtype, [&]<class T>() {
-    hipLaunchKernelGGL(k_row_stats<T>, dim3(unsigned(rows)), dim3(kThreads), 0, s,
-                       static_cast<const typename T::Elem*>(logits), (long long)stride, targets, bits, classes, stat);
+// The logits as every launch takes them.
+struct Logits {
+  const void* x;
+  int32_t dtype;
+  int64_t stride;
+  const void* targets;
+  int32_t bits;
+  int64_t rows;
+  int32_t classes;
+};
+
+// Row statistics into `out`; rows in parts (split > 1) leave their parts only.
+int launch_stats(const Logits& l, int split, const RowOut& out, float4* parts, hipStream_t s) {
+  with_type(l.dtype, [&]<class T>() {
+    hipLaunchKernelGGL(k_row_stats<T>, dim3(unsigned(l.rows * split)), dim3(kThreads), 0, s,
+                       static_cast<const typename T::Elem*>(l.x), (long long)l.stride, l.targets, l.bits, l.classes,
+                       split, out, parts);
   });
   return done();
 }
-int launch_grad(const void* logits, int32_t dtype, int64_t stride, const void* targets, int32_t bits, int64_t rows,
-                int32_t classes, const float4* stat, const float* g, const float* h, const float* scale, float scale_host,
-                void* grad, int64_t grad_stride, hipStream_t s) {
-  with_type(dtype, [&]<class T>() {
-    hipLaunchKernelGGL(k_row_grad<T>, dim3(unsigned(rows)), dim3(kThreads), 0, s,
-                       static_cast<const typename T::Elem*>(logits), (long long)stride, targets, bits, classes, stat, g,
-                       h, scale, scale_host, static_cast<typename T::Elem*>(grad), (long long)grad_stride);
+// The same, joined where they came in parts.
+int launch_values(const Logits& l, const RowOut& out, float4* parts, hipStream_t s) {
+  const int split = split_of(l.rows, l.classes);
+  const int rc = launch_stats(l, split, out, parts, s);
+  if (rc != ACDC_OK || split == 1) return rc;
+  with_type(l.dtype, [&]<class T>() {
+    constexpr int per = kThreads / 64;
+    hipLaunchKernelGGL(k_row_join<T>, dim3(unsigned((l.rows + per - 1) / per)), dim3(kThreads), 0, s,
+                       static_cast<const typename T::Elem*>(l.x), (long long)l.stride, l.targets, l.bits, l.classes,
+                       parts, split, (long long)l.rows, out);
+  });
+  return done();
+}
+int launch_grad(const Logits& l, const float4* stat, const float* g, const float* h, const float* scale,
+                float scale_host, void* grad, int64_t grad_stride, hipStream_t s) {
+  const int split = split_of(l.rows, l.classes);
+  with_type(l.dtype, [&]<class T>() {
+    hipLaunchKernelGGL(k_row_grad<T>, dim3(unsigned(l.rows * split)), dim3(kThreads), 0, s,
+                       static_cast<const typename T::Elem*>(l.x), (long long)l.stride, l.targets, l.bits, l.classes,
+                       stat, g, h, scale, scale_host, static_cast<typename T::Elem*>(grad), (long long)grad_stride,
+                       split);
   });
   return done();
 }
 
-unsigned blocks_for(int64_t rows) { return unsigned((rows + kThreads - 1) / kThreads); }
+// f.template operator()<THREADS, NC>() for the fewest lanes and registers that
+// hold a row of `chunks` chunks; false where none does.
+template <class F>
+bool with_row_shape(int chunks, F&& f) {
+  if (chunks <= 64) f.template operator()<64, 1>();
+  else if (chunks <= 128) f.template operator()<64, 2>();
+  else if (chunks <= 256) f.template operator()<64, 4>();
+  else if (chunks <= 512) f.template operator()<64, 8>();
+  else if (chunks <= 1024) f.template operator()<256, 4>();
+  else if (chunks <= 2048) f.template operator()<256, 8>();
+  else if (chunks <= 3072) f.template operator()<256, 12>();
+  else if (chunks <= 4096) f.template operator()<256, 16>();
+  else if (chunks <= 8192) f.template operator()<512, 16>();
+  else if (chunks <= 16384) f.template operator()<1024, 16>();
+  else return false;
+  return true;
+}
 
 }  // namespace
 }  // namespace acdc
@@ -408,7 +966,7 @@ unsigned blocks_for(int64_t rows) { return unsigned((rows + kThreads - 1) / kThr
 using namespace acdc;
 
 extern "C" size_t acdc_logprob_workspace_size(int64_t rows, int32_t classes, int32_t dtype) {
-  return sizes_ok(rows, classes, dtype) ? layout(rows, 0).total : 0;
+  return sizes_ok(rows, classes, dtype) ? layout(rows, classes, 0).total : 0;
 }
 
 extern "C" int acdc_logprob_forward(const void* logits, int32_t dtype, int64_t stride, const void* targets,
@@ -418,14 +976,12 @@ extern "C" int acdc_logprob_forward(const void* logits, int32_t dtype, int64_t s
   if (!logits_ok(logits, dtype, stride, targets, target_bits, rows, classes, &rc)) return rc;
   if (rows == 0) return ACDC_OK;
   if (!floats_ok({logp}, {entropy}) || !aligned_to(saved, 16) || !aligned_to(workspace, 16)) return ACDC_ERR_INVALID_ARG;
-  const Workspace w = layout(rows, 0);
+  const Workspace w = layout(rows, classes, 0);
   if (workspace == nullptr || workspace_bytes < w.total) return ACDC_ERR_WORKSPACE;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  float4* stat = reinterpret_cast<float4*>(saved != nullptr ? saved : workspace);
-  rc = launch_stats(logits, dtype, stride, targets, target_bits, rows, classes, stat, s);
-  if (rc != ACDC_OK) return rc;
-  hipLaunchKernelGGL(k_row_values, dim3(blocks_for(rows)), dim3(kThreads), 0, s, stat, (long long)rows, logp, entropy);
-  return done();
+  const Logits l{logits, dtype, stride, targets, target_bits, rows, classes};
+  const RowOut out{logp, entropy, reinterpret_cast<float4*>(saved), nullptr, nullptr};
+  return launch_values(l, out, reinterpret_cast<float4*>(static_cast<char*>(workspace) + w.parts), s);
 }
 
 extern "C" int acdc_logprob_backward(const void* logits, int32_t dtype, int64_t stride, const void* targets,
@@ -439,13 +995,13 @@ extern "C" int acdc_logprob_backward(const void* logits, int32_t dtype, int64_t 
       !floats_ok({grad_logp}, {grad_entropy, scale}) ||
       !grad_ok(logits, stride, grad_logits, grad_stride, dtype, rows, classes))
     return ACDC_ERR_INVALID_ARG;
-  return launch_grad(logits, dtype, stride, targets, target_bits, rows, classes, reinterpret_cast<const float4*>(saved),
-                     grad_logp, grad_entropy, scale, 1.f, grad_logits, grad_stride,
-                     reinterpret_cast<hipStream_t>(stream));
+  const Logits l{logits, dtype, stride, targets, target_bits, rows, classes};
+  return launch_grad(l, reinterpret_cast<const float4*>(saved), grad_logp, grad_entropy, scale, 1.f, grad_logits,
+                     grad_stride, reinterpret_cast<hipStream_t>(stream));
 }
 
 extern "C" size_t acdc_policy_workspace_size(int64_t rows, int32_t classes, int32_t dtype) {
-  return sizes_ok(rows, classes, dtype) ? layout(rows, 0).total : 0;
+  return sizes_ok(rows, classes, dtype) ? layout(rows, classes, 0).total : 0;
 }
 
 extern "C" int acdc_policy_loss(const void* logits, int32_t dtype, int64_t stride, const void* targets,
@@ -467,27 +1023,89 @@ extern "C" int acdc_policy_loss(const void* logits, int32_t dtype, int64_t strid
   if (rows > 0 && (logp_old == nullptr || advantages == nullptr || logp == nullptr)) return ACDC_ERR_INVALID_ARG;
   if (grad_logits != nullptr && !grad_ok(logits, stride, grad_logits, grad_stride, dtype, rows, classes))
     return ACDC_ERR_INVALID_ARG;
-  const Workspace w = layout(rows, 0);
+  const Workspace w = layout(rows, classes, 0);
   if (w.total > 0 && (workspace == nullptr || workspace_bytes < w.total)) return ACDC_ERR_WORKSPACE;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
+  const Logits l{logits, dtype, stride, targets, target_bits, rows, classes};
+  const PolicyArgs a{targets, target_bits, logp_old, logp_ref, advantages, weights, rows, p};
+  double* sums = reinterpret_cast<double*>(ws + w.sums);
+  float* partial = reinterpret_cast<float*>(ws + w.partial);
+  float4* parts = reinterpret_cast<float4*>(ws + w.parts);
+  const int groups = rows > 0 ? int((rows + weight_group(rows) - 1) / weight_group(rows)) : 0;
+  auto sum_weights = [&] {
+    hipLaunchKernelGGL(k_weight_sums, dim3(unsigned(groups)), dim3(kThreads), 0, s, a, sums);
+  };
+  auto sum_stats = [&](unsigned blocks) {
+    hipLaunchKernelGGL(k_total<kStats>, dim3(1), dim3(kWide), 0, s, partial, int(blocks), 1.f, stats);
+  };
+
+  // Enough rows to fill the card, or rows of a wave each: one pass.
+  bool fused = false;
+  const int split = split_of(rows, classes);
+  if (rows > 0 && grad_logits != nullptr && split == 1)
+    with_type(dtype, [&]<class T>() {
+      fused = with_row_shape(classes / T::kPer, [&]<int THREADS, int NC>() {
+        const RowOut out{logp, nullptr, reinterpret_cast<float4*>(saved), row_grads,
+                         row_grads != nullptr ? row_grads + rows : nullptr};
+        auto go = [&](auto kernel, unsigned blocks, int wg, float* to) {
+          hipLaunchKernelGGL(kernel, dim3(blocks), dim3(wg), 0, s, a, static_cast<const typename T::Elem*>(logits),
+                             (long long)stride, classes, sums, groups, static_cast<typename T::Elem*>(grad_logits),
+                             (long long)grad_stride, out, to);
+        };
+        auto blocks_of = [&](int per) { return unsigned(std::min<int64_t>((rows + per - 1) / per, kMaxPartials)); };
+        if constexpr (THREADS == 64 && NC <= 4) {
+          constexpr int RPW = 4 / NC;
+          // up to 64 rows in one workgroup: a launch instead of three
+          if (rows <= 16 * RPW) {
+            go(k_policy_tile<T, 16, RPW, NC>, 1, 1024, stats);
+          } else {
+            const unsigned blocks = blocks_of(8 * RPW);
+            sum_weights();
+            go(k_policy_tile<T, 8, RPW, NC>, blocks, 512, partial);
+            sum_stats(blocks);
+          }
+        } else {
+          constexpr int WG = THREADS < kThreads ? kThreads : THREADS;
+          // two workgroups at least: one alone would take the weights for its own to sum
+          const unsigned blocks = std::max(2u, blocks_of(WG / THREADS));
+          sum_weights();
+          go(k_policy_fused<T, WG, THREADS, NC>, blocks, WG, partial);
+          sum_stats(blocks);
+        }
+      });
+    });
+  if (fused) return done();
+
   float4* stat = saved != nullptr ? reinterpret_cast<float4*>(saved) : reinterpret_cast<float4*>(ws + w.stat);
   float* grads = row_grads != nullptr ? row_grads : reinterpret_cast<float*>(ws + w.grads);
   if (rows > 0) {
-    rc = launch_stats(logits, dtype, stride, targets, target_bits, rows, classes, stat, s);
+    rc = launch_stats(l, split, RowOut{nullptr, nullptr, stat, nullptr, nullptr}, parts, s);
     if (rc != ACDC_OK) return rc;
   }
-  const PolicyArgs a{targets, target_bits, logp_old, logp_ref, advantages, weights, rows, p};
-  hipLaunchKernelGGL(k_policy_rows, dim3(1), dim3(kWide), 0, s, a, stat, stats, logp, grads);
+  const RowOut out{logp, nullptr, split > 1 ? stat : nullptr, grads, grads + rows};
+  with_type(dtype, [&]<class T>() {
+    auto go = [&](unsigned blocks, float* to) {
+      hipLaunchKernelGGL(k_policy_rows<T>, dim3(blocks), dim3(kWide), 0, s, a, static_cast<const typename T::Elem*>(logits),
+                         (long long)stride, classes, parts, split, sums, groups, stat, out, to);
+    };
+    if (rows <= kWide) {
+      go(1, stats);
+    } else {
+      const unsigned blocks = unsigned(std::min<int64_t>((rows + kWide - 1) / kWide, kMaxPartials / 8));
+      sum_weights();
+      go(blocks, partial);
+      sum_stats(blocks);
+    }
+  });
   rc = done();
   if (rc != ACDC_OK || rows == 0 || grad_logits == nullptr) return rc;
-  return launch_grad(logits, dtype, stride, targets, target_bits, rows, classes, stat, grads, grads + rows, nullptr,
-                     p.grad_scale, grad_logits, grad_stride, s);
+  return launch_grad(l, stat, grads, grads + rows, nullptr, p.grad_scale, grad_logits, grad_stride, s);
 }
 
 extern "C" size_t acdc_preference_workspace_size(int64_t rows, int32_t classes, int32_t dtype, int64_t pairs) {
   if (!sizes_ok(rows, classes, dtype) || pairs < 0 || pairs > 0x3fffffff) return 0;
-  return layout(rows, pairs).total;
+  return layout(rows, classes, pairs).total;
 }
 
 extern "C" int acdc_preference_loss(const void* logits, int32_t dtype, int64_t stride, const void* targets,
@@ -509,28 +1127,31 @@ extern "C" int acdc_preference_loss(const void* logits, int32_t dtype, int64_t s
   if (rows > 0 && (logp_ref == nullptr || logp == nullptr)) return ACDC_ERR_INVALID_ARG;
   if (grad_logits != nullptr && !grad_ok(logits, stride, grad_logits, grad_stride, dtype, rows, classes))
     return ACDC_ERR_INVALID_ARG;
-  const Workspace w = layout(rows, pairs);
+  const Workspace w = layout(rows, classes, pairs);
   if (w.total > 0 && (workspace == nullptr || workspace_bytes < w.total)) return ACDC_ERR_WORKSPACE;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
   float4* stat = saved != nullptr ? reinterpret_cast<float4*>(saved) : reinterpret_cast<float4*>(ws + w.stat);
   float* grads = row_grads != nullptr ? row_grads : reinterpret_cast<float*>(ws + w.grads);
-  float* reward = reinterpret_cast<float*>(ws + w.reward);
-  float* slope = reinterpret_cast<float*>(ws + w.slope);
+  float* partial = reinterpret_cast<float*>(ws + w.partial);
+  const Logits l{logits, dtype, stride, targets, target_bits, rows, classes};
   if (rows > 0) {
-    rc = launch_stats(logits, dtype, stride, targets, target_bits, rows, classes, stat, s);
+    // with g and h of 0 for every row; the pairs then give their rows a g
+    rc = launch_values(l, RowOut{logp, nullptr, stat, grads, grads + rows}, reinterpret_cast<float4*>(ws + w.parts), s);
     if (rc != ACDC_OK) return rc;
   }
-  if (pairs > 0)
-    hipLaunchKernelGGL(k_rewards, dim3(unsigned(2 * pairs)), dim3(kThreads), 0, s, targets, target_bits, offsets,
-                       offset_bits, logp_ref, (long long)rows, p.beta, stat, reward);
-  hipLaunchKernelGGL(k_pairs, dim3(1), dim3(kWide), 0, s, reward, (long long)pairs, p.beta, p.label_smoothing, stats,
-                     slope);
-  if (rows > 0)
-    hipLaunchKernelGGL(k_preference_rows, dim3(blocks_for(rows)), dim3(kThreads), 0, s, targets, target_bits, offsets,
-                       offset_bits, (long long)rows, (long long)pairs, stat, slope, logp, grads);
+  // one workgroup, a wave for each pair, saves the launch that adds the stats
+  const PairArgs a{targets, offsets, target_bits, offset_bits, logp_ref, rows, pairs, p.beta, p.label_smoothing};
+  if (pairs <= kWide / 64) {
+    hipLaunchKernelGGL(k_pairs, dim3(1), dim3(kWide), 0, s, a, stat, grads, stats);
+  } else {
+    const int waves = kThreads / 64;
+    const unsigned blocks = unsigned(std::min<int64_t>((pairs + waves - 1) / waves, kMaxPartials));
+    hipLaunchKernelGGL(k_pairs, dim3(blocks), dim3(kThreads), 0, s, a, stat, grads, partial);
+    hipLaunchKernelGGL(k_total<kPairStats>, dim3(1), dim3(kWide), 0, s, partial, int(blocks), float(1.0 / double(pairs)),
+                       stats);
+  }
   rc = done();
   if (rc != ACDC_OK || rows == 0 || grad_logits == nullptr) return rc;
-  return launch_grad(logits, dtype, stride, targets, target_bits, rows, classes, stat, grads, grads + rows, nullptr,
-                     p.grad_scale, grad_logits, grad_stride, s);
+  return launch_grad(l, stat, grads, grads + rows, nullptr, p.grad_scale, grad_logits, grad_stride, s);
 }
