@@ -73,5 +73,25 @@ def lib():
     return _lib
 
 
+_binding = None
+
+
+def binding():
+    """The native part of the training operators' binding (loaded once)."""
+    global _binding
+    if _binding is None:
+        lib()
+        path = os.path.join(os.path.dirname(LIB_PATH), "_train_binding.so")
+        if not os.path.exists(path):
+            raise LibraryMissing(f"{path} is not built; run `python -m paper_1511_05946_amd.build`")
+        import importlib.util
+
+        import torch  # noqa: F401  (the module's own libraries)
+        spec = importlib.util.spec_from_file_location("paper_1511_05946_amd._train_binding", path)
+        _binding = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(_binding)
+    return _binding
+
+
 def status_string(rc: int) -> str:
     return lib().acdc_status_string(int(rc)).decode()

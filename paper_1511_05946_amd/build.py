@@ -1,4 +1,5 @@
-"""Build libacdc.so (HIP, gfx950) in-tree with hipcc.
+"""Build libacdc.so (HIP, gfx950) in-tree with hipcc, and the native part of the
+training operators' binding (_train_binding.so) with the host compiler.
 
 Usage: python -m paper_1511_05946_amd.build   (or build() from Python)
 """
@@ -15,6 +16,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libacdc.so")
+BINDING = os.path.join(PKG, "_train_binding.so")
 
 # -packed-fp32-ops: keep every fp32 operation a plain VOP (no v_pk_*_f32).
 HIP_FLAGS = [
@@ -49,7 +51,8 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = False, extra_flags: list[str] | None = None) -> str:
-    """Compile every csrc/*.hip to an object (in parallel), then link libacdc.so."""
+    """Compile every csrc/*.hip to an object (in parallel), then link libacdc.so
+    and, against it, the binding's native part."""
     import tempfile
     srcs = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".hip"))
     with tempfile.TemporaryDirectory(prefix="acdc_build_") as tmpdir:
@@ -78,7 +81,33 @@ def build(verbose: bool = False, extra_flags: list[str] | None = None) -> str:
             sys.stderr.write(proc.stdout + proc.stderr)
             raise RuntimeError(f"hipcc link failed ({proc.returncode})")
         os.replace(tmp, LIB)
+    build_binding(verbose)
     return LIB
+
+
+def build_binding(verbose: bool = False) -> str:
+    """Compile csrc/acdc_train_binding.cpp against torch and libacdc.so."""
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths
+    cxx = shutil.which(os.environ.get("CXX", "g++"))
+    if cxx is None:
+        raise RuntimeError("no host C++ compiler (g++) found")
+    includes = [a for p in (*include_paths(), sysconfig.get_paths()["include"]) for a in ("-isystem", p)]
+    tmp = BINDING + ".tmp"
+    cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *includes, "-I", INCLUDE, os.path.join(CSRC, "acdc_train_binding.cpp"), "-o", tmp,
+           "-L", os.path.join(os.path.dirname(torch.__file__), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
+           "-L", PKG, "-l:libacdc.so", "-Wl,-rpath,$ORIGIN"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    proc = subprocess.run(cmd, capture_output=True, text=True)
+    if proc.returncode != 0:
+        sys.stderr.write(proc.stdout + proc.stderr)
+        raise RuntimeError(f"{cxx} failed ({proc.returncode})")
+    os.replace(tmp, BINDING)
+    return BINDING
 
 
 if __name__ == "__main__":

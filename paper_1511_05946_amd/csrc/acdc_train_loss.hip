@@ -49,6 +49,7 @@ __device__ __forceinline__ Run merge(const Run& a, const Run& b) {
 }
 
 constexpr int kThreads = 256;
+constexpr int kAhead = 4;  // chunks that a thread of the streaming kernels asks for at a time
 
 __device__ __forceinline__ Run merge_wave(Run r) {
 #pragma unroll
@@ -141,19 +142,29 @@ __global__ __launch_bounds__(kThreads) void k_row_stats(const typename T::Elem* 
   const Cut<T> cut(row, classes);
   int from, to;
   chunks_of(cut.full, split, k, from, to);
-  for (int c = from + threadIdx.x; c < to; c += kThreads) {
-    const auto raw = load_chunk<T>(row + cut.head + (long long)c * T::kPer);
+  const typename T::Elem* body = row + cut.head;
+  auto take = [&]<int N>(int c) {  // N chunks, asked for together: c, c + kThreads, ...
+    typename T::Raw raw[N];
+#pragma unroll
+    for (int q = 0; q < N; ++q) raw[q] = load_chunk<T>(body + (long long)(c + q * kThreads) * T::kPer);
     Run b = empty_run();
 #pragma unroll
-    for (int i = 0; i < T::kPer; ++i) b.m = fmaxf(b.m, T::get(raw, i));
+    for (int q = 0; q < N; ++q)
 #pragma unroll
-    for (int i = 0; i < T::kPer; ++i) {
-      const float d = T::get(raw, i) - b.m, e = exp_of(d);
-      b.s += e;
-      b.u += e * fmaxf(d, -1e30f);
-    }
+      for (int i = 0; i < T::kPer; ++i) b.m = fmaxf(b.m, T::get(raw[q], i));
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+#pragma unroll
+      for (int i = 0; i < T::kPer; ++i) {
+        const float d = T::get(raw[q], i) - b.m, e = exp_of(d);
+        b.s += e;
+        b.u += e * fmaxf(d, -1e30f);
+      }
     run = merge(run, b);
-  }
+  };
+  int c = from + threadIdx.x;
+  for (; c + (kAhead - 1) * kThreads < to; c += kAhead * kThreads) take.template operator()<kAhead>(c);
+  for (; c < to; c += kThreads) take.template operator()<1>(c);
   if (k == split - 1 && int(threadIdx.x) < cut.extra) {
     const float v = T::one(row[cut.element(threadIdx.x)]);
     Run b = empty_run();
@@ -264,13 +275,23 @@ __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x
                    : has_one && cut.lane_of(int(t)) == int(threadIdx.x);
   }
   const float yt = mine ? slope_value(sl, T::one(row[t])) + g : 0.f;
-  for (int i = from + threadIdx.x; i < to; i += kThreads) {
-    const auto raw = load_chunk<T>(body + (long long)i * T::kPer);
-    float y[T::kPer];
+  auto give = [&]<int N>(int i) {
+    // the loads of a group stand before its stores: out may be x, so that the
+    // compiler would not move a load ahead of an earlier store by itself
+    typename T::Raw raw[N];
 #pragma unroll
-    for (int e = 0; e < T::kPer; ++e) y[e] = slope_value(sl, T::get(raw, e));
-    store_chunk<T>(out_body + (long long)i * T::kPer, T::pack(y));
-  }
+    for (int q = 0; q < N; ++q) raw[q] = load_chunk<T>(body + (long long)(i + q * kThreads) * T::kPer);
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+      float y[T::kPer];
+#pragma unroll
+      for (int e = 0; e < T::kPer; ++e) y[e] = slope_value(sl, T::get(raw[q], e));
+      store_chunk<T>(out_body + (long long)(i + q * kThreads) * T::kPer, T::pack(y));
+    }
+  };
+  int i = from + threadIdx.x;
+  for (; i + (kAhead - 1) * kThreads < to; i += kAhead * kThreads) give.template operator()<kAhead>(i);
+  for (; i < to; i += kThreads) give.template operator()<1>(i);
   if (has_one) out[one] = T::to(slope_value(sl, T::one(row[one])));
   if (mine) out[t] = T::to(yt);
 }
@@ -416,10 +437,18 @@ __global__ __launch_bounds__(kWide) void k_total(const float* __restrict__ parti
                                                  float* __restrict__ stats) {
   __shared__ float part[kWide / 64][STATS];
   double sum[STATS] = {};
-#pragma unroll 4
-  for (int j = threadIdx.x; j < n; j += kWide)
+  typedef float Four __attribute__((ext_vector_type(4), aligned(4)));
+  const int quads = n / 4;
+#pragma unroll 2
+  for (int j = threadIdx.x; j < quads; j += kWide)
 #pragma unroll
-    for (int i = 0; i < STATS; ++i) sum[i] += double(partial[(long long)i * n + j]);
+    for (int i = 0; i < STATS; ++i) {
+      const Four v = *reinterpret_cast<const Four*>(partial + (long long)i * n + 4 * j);
+      sum[i] += (double(v[0]) + double(v[1])) + (double(v[2]) + double(v[3]));
+    }
+  if (4 * quads + int(threadIdx.x) < n)
+#pragma unroll
+    for (int i = 0; i < STATS; ++i) sum[i] += double(partial[(long long)i * n + 4 * quads + threadIdx.x]);
 #pragma unroll
   for (int i = 0; i < STATS; ++i) {
     const float v = wave_sum(float(sum[i]));
@@ -615,8 +644,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(WAVE
   if (threadIdx.x < kStats) acc[threadIdx.x] = 0.0;
   for (long long base = (long long)blockIdx.x * ROWS; base < a.rows; base += (long long)gridDim.x * ROWS) {
     typename T::Raw raw[RPW][NC];
-    float last[RPW];
-    int t[RPW];
+    float last[RPW], xt[RPW];
+    int t[RPW], full[RPW];
     bool on[RPW];
 #pragma unroll
     for (int q = 0; q < RPW; ++q) {
@@ -632,53 +661,69 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(WAVE
 #pragma unroll
     for (int q = 0; q < RPW; ++q) {
       last[q] = kNegMax;
+      xt[q] = 0.f;
 #pragma unroll
       for (int c = 0; c < NC; ++c) raw[q][c] = typename T::Raw{};
-      if (!on[q]) continue;
       const typename T::Elem* row = x + (base + wave * RPW + q) * stride;
       const Cut<T> cut(row, classes);
+      full[q] = cut.full;
+      if (!on[q]) continue;
+      xt[q] = target_logit<T>(row, t[q], classes);
 #pragma unroll
       for (int c = 0; c < NC; ++c)
         if (c * 64 + lane < cut.full) raw[q][c] = load_chunk_at<T>(row + cut.head, c * 1024u, at);
       if (lane < cut.extra) last[q] = T::one(row[cut.element(lane)]);
     }
+    // what wave 0 needs of each row, asked for ahead of the rows' arithmetic
+    const long long mine = base + lane;
+    float w = 0.f, old = 0.f, adv = 0.f, ref = 0.f;
+    if (wave == 0 && lane < ROWS && mine < a.rows) {
+      w = weight_of(a, mine);
+      old = a.old[mine];
+      adv = a.advantages[mine];
+      if (a.ref != nullptr) ref = a.ref[mine];
+    }
+    // rows that take no part go through the same arithmetic on zeros: without a
+    // branch between them the rows' reductions overlap
+    float m[RPW], s[RPW], u[RPW];
 #pragma unroll
     for (int q = 0; q < RPW; ++q) {
-      if (!on[q]) continue;
-      const typename T::Elem* row = x + (base + wave * RPW + q) * stride;
-      const Cut<T> cut(row, classes);
-      float m = last[q];
+      m[q] = fmaxf(last[q], kNegMax);
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
-        if (c * 64 + lane < cut.full) {
+      for (int c = 0; c < NC; ++c) {
+        const bool has = c * 64 + lane < full[q];
 #pragma unroll
-          for (int i = 0; i < T::kPer; ++i) m = fmaxf(m, T::get(raw[q][c], i));
-        }
-      m = wave_max(fmaxf(m, kNegMax));
-      float s = 0.f, u = 0.f;
-      auto add = [&](float v) {
-        const float d = v - m, e = exp_of(d);
-        s += e;
-        u += e * fmaxf(d, -1e30f);
+        for (int i = 0; i < T::kPer; ++i) m[q] = fmaxf(m[q], has ? T::get(raw[q][c], i) : kNegMax);
+      }
+      m[q] = wave_max(m[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < RPW; ++q) {
+      s[q] = u[q] = 0.f;
+      auto add = [&](float v, bool has) {
+        const float d = v - m[q], e = has ? exp_of(d) : 0.f;
+        s[q] += e;
+        u[q] += e * fmaxf(d, -1e30f);
       };
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
-        if (c * 64 + lane < cut.full) {
+      for (int c = 0; c < NC; ++c) {
+        const bool has = c * 64 + lane < full[q];
 #pragma unroll
-          for (int i = 0; i < T::kPer; ++i) add(T::get(raw[q][c], i));
-        }
-      if (lane < cut.extra) add(last[q]);
-      s = wave_sum(s);
-      u = wave_sum(u);
-      const float xt = target_logit<T>(row, t[q], classes);
-      if (lane == 0) stat[wave * RPW + q] = make_float4(m, s, u, xt);
+        for (int i = 0; i < T::kPer; ++i) add(T::get(raw[q][c], i), has);
+      }
+      add(last[q], lane < classes - full[q] * T::kPer);
+      s[q] = wave_sum(s[q]);
+      u[q] = wave_sum(u[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < RPW; ++q) {
+      if (lane == 0) stat[wave * RPW + q] = make_float4(m[q], s[q], u[q], xt[q]);
 #pragma unroll
       for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(raw[q][c]));
     }
     __syncthreads();
     if (wave == 0) {
-      const long long r = base + lane;
-      float w = lane < ROWS && r < a.rows ? weight_of(a, r) : 0.f;
+      const long long r = mine;
       if (gridDim.x == 1) {  // these are all rows
         double total = double(w);
 #pragma unroll
@@ -692,7 +737,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(WAVE
       if (w != 0.f) {
         const float4 z = stat[lane];
         st = stat_of(Run{z.x, z.y, z.z}, z.w);
-        p = policy_row(a.p, w, st.w, st.z, a.old[r], a.advantages[r], a.ref != nullptr, a.ref != nullptr ? a.ref[r] : 0.f);
+        p = policy_row(a.p, w, st.w, st.z, old, adv, a.ref != nullptr, ref);
         sl = slope_of(st.x, st.y, st.z, p.g * a.p.grad_scale, p.h * a.p.grad_scale);
       }
       if (lane < ROWS && r < a.rows) {
@@ -759,7 +804,7 @@ struct PairArgs {
   float beta, smoothing;
 };
 
-// Sum of logp - logp_ref over a sequence, by a group of N threads.
+// Sum of logp - logp_ref over rows from .. to - 1, by a group of n threads.
 __device__ __forceinline__ double excess(const PairArgs& a, const float4* __restrict__ stat, long long from, long long to,
                                          int lane, int n) {
   double v = 0.0;
@@ -769,30 +814,39 @@ __device__ __forceinline__ double excess(const PairArgs& a, const float4* __rest
   return v;
 }
 
-// Rewards, margin and loss of pairs, and dL/dlogp of their rows: a wave per
-// pair, pairs wave, wave + waves, ...; the rows' g are 0 before it.  Each
-// workgroup's sums over its pairs go into partial[.][blockIdx] (stats, divided
-// by the pairs, with one workgroup).
-__global__ __launch_bounds__(kWide) void k_pairs(PairArgs a, const float4* __restrict__ stat, float* __restrict__ g,
-                                                 float* __restrict__ partial) {
-  __shared__ double acc[kWide / 64][kPairStats];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
+// Rewards, margin and loss of pairs, and dL/dlogp of their rows, whose g and h
+// are 0 before it.  WG / GROUP pairs a workgroup at a time: a wave each in the
+// one workgroup of a call with few pairs, which writes the stats itself, else
+// a workgroup each, whose sums go into partial[.][blockIdx].
+template <int WG, int GROUP>
+__global__ __launch_bounds__(WG) void k_pairs(PairArgs a, const float4* __restrict__ stat, float* __restrict__ g,
+                                              float* __restrict__ partial) {
+  constexpr int PAIRS = WG / GROUP;
+  __shared__ double acc[PAIRS][kPairStats];
+  __shared__ double part[WG / 64];
+  const int lane = threadIdx.x % GROUP, mine = threadIdx.x / GROUP;
   double sum[kPairStats] = {};
-  for (long long p = (long long)blockIdx.x * waves + wave; p < a.pairs; p += (long long)gridDim.x * waves) {
+  for (long long p = (long long)blockIdx.x * PAIRS + mine; p < a.pairs; p += (long long)gridDim.x * PAIRS) {
     const long long o0 = offset_of(a.offsets, a.offset_bits, 2 * p, a.rows);
     const long long o1 = offset_of(a.offsets, a.offset_bits, 2 * p + 1, a.rows);
     const long long o2 = offset_of(a.offsets, a.offset_bits, 2 * p + 2, a.rows);
-    double v0 = excess(a, stat, o0, o1, lane, 64), v1 = excess(a, stat, o1, o2, lane, 64);
+    double v0 = excess(a, stat, o0, o1, lane, GROUP), v1 = excess(a, stat, o1, o2, lane, GROUP);
+    if constexpr (GROUP == 64) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      v0 += __shfl_xor(v0, o);
-      v1 += __shfl_xor(v1, o);
+      for (int o = 32; o > 0; o >>= 1) {
+        v0 += __shfl_xor(v0, o);
+        v1 += __shfl_xor(v1, o);
+      }
+    } else {
+      v0 = total_of<WG>(v0, part);
+      v1 = total_of<WG>(v1, part);
     }
     const float good = float(a.beta * v0), bad = float(a.beta * v1), m = float(a.beta * (v0 - v1)), e = a.smoothing;
     const float loss = (1.f - e) * softplus(-m) + e * softplus(m);
     // a NaN margin is no win, and gives NaN slopes
     const float slope = (e / (1.f + expf(-m)) - (1.f - e) / (1.f + expf(m))) * (a.beta / float(a.pairs));
-    for (long long r = o0 + lane; r < o2; r += 64)
+#pragma unroll 4
+    for (long long r = o0 + lane; r < o2; r += GROUP)
       if (target_of(a.targets, a.bits, r) >= 0) g[r] = r < o1 ? slope : -slope;
     const float v[kPairStats] = {loss, m > 0.f ? 1.f : 0.f, m, good, bad};
 #pragma unroll
@@ -800,12 +854,13 @@ __global__ __launch_bounds__(kWide) void k_pairs(PairArgs a, const float4* __res
   }
   if (lane == 0)
 #pragma unroll
-    for (int i = 0; i < kPairStats; ++i) acc[wave][i] = sum[i];
+    for (int i = 0; i < kPairStats; ++i) acc[mine][i] = sum[i];
   __syncthreads();
   if (threadIdx.x < kPairStats) {
     double s = 0.0;
-    for (int w = 0; w < waves; ++w) s += acc[w][threadIdx.x];
-    if (gridDim.x == 1) s = a.pairs > 0 ? s / double(a.pairs) : 0.0;
+#pragma unroll
+    for (int w = 0; w < PAIRS; ++w) s += acc[w][threadIdx.x];
+    if (PAIRS > 1) s = a.pairs > 0 ? s / double(a.pairs) : 0.0;
     partial[(long long)threadIdx.x * gridDim.x + blockIdx.x] = float(s);
   }
 }
@@ -1143,11 +1198,10 @@ extern "C" int acdc_preference_loss(const void* logits, int32_t dtype, int64_t s
   // one workgroup, a wave for each pair, saves the launch that adds the stats
   const PairArgs a{targets, offsets, target_bits, offset_bits, logp_ref, rows, pairs, p.beta, p.label_smoothing};
   if (pairs <= kWide / 64) {
-    hipLaunchKernelGGL(k_pairs, dim3(1), dim3(kWide), 0, s, a, stat, grads, stats);
+    hipLaunchKernelGGL((k_pairs<kWide, 64>), dim3(1), dim3(kWide), 0, s, a, stat, grads, stats);
   } else {
-    const int waves = kThreads / 64;
-    const unsigned blocks = unsigned(std::min<int64_t>((pairs + waves - 1) / waves, kMaxPartials));
-    hipLaunchKernelGGL(k_pairs, dim3(blocks), dim3(kThreads), 0, s, a, stat, grads, partial);
+    const unsigned blocks = unsigned(std::min<int64_t>(pairs, kMaxPartials));
+    hipLaunchKernelGGL((k_pairs<kThreads, kThreads>), dim3(blocks), dim3(kThreads), 0, s, a, stat, grads, partial);
     hipLaunchKernelGGL(k_total<kPairStats>, dim3(1), dim3(kWide), 0, s, partial, int(blocks), float(1.0 / double(pairs)),
                        stats);
   }

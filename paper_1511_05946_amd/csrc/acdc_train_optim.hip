@@ -19,7 +19,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kBatch = 48;      // tensors a launch: their records fill the 4 KB of kernel arguments
 constexpr int kBlock = 256;     // elements that share a scale: 4 of each lane of a wave
-constexpr int kChunk = 4096;    // elements a workgroup
+constexpr int kChunk = kThreads * 4;  // elements a workgroup: four a thread, and no loop
 constexpr float kPerTop = 1.f / 448.f;  // 448: largest e4m3 value
 constexpr float kTiny = 0x1p-9f;  // smallest positive one
 
@@ -127,9 +127,7 @@ __device__ __forceinline__ unsigned encode4(const float (&v)[4], float scale) {
 // are 0: their scale would leave the normal numbers.  (The product may leave the
 // largest element a rounding away from 448, which its code does not see.)
 __device__ __forceinline__ float scale_of(const float (&v)[4]) {
-  float top = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  const float top = wave_max(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
   return top < 0x1p-100f ? 0.f : top * kPerTop;
 }
 
@@ -141,69 +139,71 @@ __global__ __launch_bounds__(kThreads) void k_adamw(Batch b, int count, Step s) 
   if (!(gs - gs == 0.f)) return;
   // the gradient's scale goes into the factors of g and g^2, each rounded once
   const float c1 = float(s.one1 * double(gs)), c2 = float(s.one2 * (double(gs) * double(gs)));
-  const long long begin = (long long)(int(blockIdx.x) - b.first[i]) * kChunk;
-  const long long end = begin + kChunk < t.n ? begin + kChunk : t.n;
-  // whole waves leave together: a wave's 256 elements are one block of scales
-  for (long long base = begin + (threadIdx.x / 64) * kBlock; base < end; base += kThreads * 4) {
-    const long long at = base + (threadIdx.x % 64) * 4;
-    const long long left = end - at;
-    const int have = left >= 4 ? 4 : left > 0 ? int(left) : 0;
-    float g[4], m[4], v[4], w[4];
-    load4<G>(t.grad, at, have, g);
-    if constexpr (MASTER) load4<F32>(t.master, at, have, w);
-    else load4<P>(t.param, at, have, w);
-    if constexpr (BITS == 32) {
-      load4<F32>(t.m, at, have, m);
-      load4<F32>(t.v, at, have, v);
-    } else {
-      decode4(load_codes(t.m, at, have), t.m_scale[base / kBlock], m);
-      decode4(load_codes(t.v, at, have), t.v_scale[base / kBlock], v);
+  // a wave's 256 elements are one block of scales
+  const long long base = (long long)(int(blockIdx.x) - b.first[i]) * kChunk + (threadIdx.x / 64) * kBlock;
+  if (base >= t.n) return;
+  const int lane = (threadIdx.x % 64) * 4;
+  const long long at = base + lane, left = t.n - at;
+  const int have = left >= 4 ? 4 : left > 0 ? int(left) : 0;
+  float g[4], m[4], v[4], w[4];
+  load4<G>(t.grad, at, have, g);
+  if constexpr (MASTER) load4<F32>(t.master, at, have, w);
+  else load4<P>(t.param, at, have, w);
+  if constexpr (BITS == 32) {
+    load4<F32>(t.m, at, have, m);
+    load4<F32>(t.v, at, have, v);
+  } else {
+    decode4(load_codes(t.m, at, have), t.m_scale[base / kBlock], m);
+    decode4(load_codes(t.v, at, have), t.v_scale[base / kBlock], v);
+  }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] *= v[k];
-    }
-    float root[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      // each product and sum rounded on its own, as the formula written out in
-      // 32 bits is: an 8-bit code that a fused product turned the other way would
-      // stand a whole step of its format off
+  for (int k = 0; k < 4; ++k) {
+    // each product and sum rounded on its own, as the formula written out in
+    // 32 bits is: an 8-bit code that a fused product turned the other way would
+    // stand a whole step of its format off
 #pragma clang fp contract(off)
-      m[k] = s.beta1 * m[k] + c1 * g[k];
-      v[k] = s.beta2 * v[k] + c2 * g[k] * g[k];
-      root[k] = sqrtf(v[k]);
-      w[k] = w[k] * t.decay - t.rate * (m[k] / (root[k] * s.root_scale + s.eps));
-    }
-    if constexpr (MASTER) store4<F32>(t.master, at, have, w);
-    store4<P>(t.param, at, have, w);
-    if constexpr (BITS == 32) {
-      store4<F32>(t.m, at, have, m);
-      store4<F32>(t.v, at, have, v);
-    } else {
-      const float ms = scale_of(m), vs = scale_of(root);
-      store_codes(t.m, at, have, encode4<false>(m, ms));
-      store_codes(t.v, at, have, encode4<true>(root, vs));
-      if (threadIdx.x % 64 == 0) {
-        t.m_scale[base / kBlock] = ms;
-        t.v_scale[base / kBlock] = vs;
-      }
+    if constexpr (BITS == 8) v[k] *= v[k];
+    m[k] = s.beta1 * m[k] + c1 * g[k];
+    v[k] = s.beta2 * v[k] + c2 * g[k] * g[k];
+  }
+  float root[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    root[k] = sqrtf(v[k]);
+    w[k] = w[k] * t.decay - t.rate * (m[k] / (root[k] * s.root_scale + s.eps));
+  }
+  if constexpr (MASTER) store4<F32>(t.master, at, have, w);
+  store4<P>(t.param, at, have, w);
+  if constexpr (BITS == 32) {
+    store4<F32>(t.m, at, have, m);
+    store4<F32>(t.v, at, have, v);
+  } else {
+    const float ms = scale_of(m), vs = scale_of(root);
+    store_codes(t.m, at, have, encode4<false>(m, ms));
+    store_codes(t.v, at, have, encode4<true>(root, vs));
+    if (lane == 0) {
+      t.m_scale[base / kBlock] = ms;
+      t.v_scale[base / kBlock] = vs;
     }
   }
 }
 
 // ------------------------------------------------------------ gradient norm
 
-constexpr int kNormBatch = 64;
-constexpr int kNormChunk = 16384;  // elements a workgroup
+constexpr int kNormBatch = 180;
+constexpr int kNormRounds = 4;     // chunks of 16 bytes that a thread asks for at a time
+constexpr int kNormChunk = 8192;   // elements a workgroup
 struct NormTensor {
   const void* grad;
-  long long n;
-  int type;
+  unsigned long long n_type;  // elements << 1 | bfloat16
 };
 struct NormBatch {
   int first[kNormBatch];
   NormTensor t[kNormBatch];
 };
+static_assert(sizeof(NormBatch) <= 3840, "kernel arguments");
 
+// Sum over the workgroup's waves in a fixed order, for thread 0.
 __device__ __forceinline__ double sum_workgroup(double v, double* part, int waves) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
@@ -215,24 +215,50 @@ __device__ __forceinline__ double sum_workgroup(double v, double* part, int wave
 }
 
 template <class G>
-__device__ __forceinline__ float square_sum(const NormTensor& t, long long begin, long long end) {
-  float s = 0.f;
-  for (long long at = begin + threadIdx.x * 4; at < end; at += kThreads * 4) {
-    float v[4];
-    load4<G>(t.grad, at, end - at >= 4 ? 4 : int(end - at), v);
-    s += (v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3]);
+__device__ __forceinline__ double square_sum(const typename G::Elem* p, long long n) {
+  constexpr int kStep = kThreads * G::kPer;
+  const int count = n < kNormChunk ? int(n) : kNormChunk, full = count / G::kPer * G::kPer;
+  double total = 0.0;
+  for (int base = 0; base < full; base += kStep * kNormRounds) {
+    typename G::Raw raw[kNormRounds];
+    const int at = base + int(threadIdx.x) * G::kPer;
+#pragma unroll
+    for (int q = 0; q < kNormRounds; ++q) {
+      raw[q] = typename G::Raw{};
+      if (at + q * kStep < full) raw[q] = load_chunk<G>(p + at + q * kStep);
+    }
+    float s = 0.f;  // up to 32 squares in 32 bits
+#pragma unroll
+    for (int q = 0; q < kNormRounds; ++q)
+#pragma unroll
+      for (int i = 0; i < G::kPer; ++i) s += G::get(raw[q], i) * G::get(raw[q], i);
+    total += double(s);
   }
-  return s;
+  if (full + int(threadIdx.x) < count) {
+    const float v = G::one(p[full + threadIdx.x]);
+    total += double(v * v);
+  }
+  return total;
+}
+
+// The tensor of this workgroup: as tensor_of, for up to kNormBatch of them.
+__device__ __forceinline__ int norm_tensor_of(const int* first, int count, int block) {
+  int i = -1;
+  for (int base = 0; base < count; base += 64) {
+    const int k = base + int(threadIdx.x) % 64;
+    i += __popcll(__ballot(k < count ? first[k] <= block : false));
+  }
+  return __builtin_amdgcn_readfirstlane(i);
 }
 
 __global__ __launch_bounds__(kThreads) void k_square_sums(NormBatch b, int count, double* __restrict__ sums) {
   __shared__ double part[kThreads / 64];
-  const int i = tensor_of(b.first, count, blockIdx.x);
-  const NormTensor& t = b.t[i];
+  const int i = norm_tensor_of(b.first, count, blockIdx.x);
   const long long begin = (long long)(int(blockIdx.x) - b.first[i]) * kNormChunk;
-  const long long end = begin + kNormChunk < t.n ? begin + kNormChunk : t.n;
-  const float s = t.type == ACDC_F32 ? square_sum<F32>(t, begin, end) : square_sum<BF16>(t, begin, end);
-  const double total = sum_workgroup(double(s), part, kThreads / 64);
+  const long long left = (long long)(b.t[i].n_type >> 1) - begin;
+  const double s = b.t[i].n_type & 1 ? square_sum<BF16>(static_cast<const __bf16*>(b.t[i].grad) + begin, left)
+                                     : square_sum<F32>(static_cast<const float*>(b.t[i].grad) + begin, left);
+  const double total = sum_workgroup(s, part, kThreads / 64);
   if (threadIdx.x == 0) sums[blockIdx.x] = total;
 }
 
@@ -241,6 +267,7 @@ __global__ __launch_bounds__(kWide) void k_norm(const double* __restrict__ sums,
                                                 float* __restrict__ out) {
   __shared__ double part[kWide / 64];
   double s = 0.0;
+#pragma unroll 8
   for (long long i = threadIdx.x; i < n; i += kWide) s += sums[i];
   s = sum_workgroup(s, part, kWide / 64);
   if (threadIdx.x == 0) {
@@ -391,7 +418,7 @@ extern "C" int acdc_grad_norm(const void* const* grads, const int64_t* sizes, co
       if (rc != ACDC_OK) return rc;
     }
     b.first[used] = int(blocks);
-    b.t[used] = NormTensor{grads[i], sizes[i], types[i]};
+    b.t[used] = NormTensor{grads[i], (unsigned long long)sizes[i] << 1 | (types[i] == ACDC_BF16 ? 1u : 0u)};
     ++used;
     blocks += need;
   }

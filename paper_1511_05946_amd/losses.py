@@ -27,7 +27,7 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from ._lib import lib
+from ._lib import binding, lib
 from .acdc import _call, _check, _ptr
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
@@ -54,6 +54,19 @@ class PreferenceLoss(NamedTuple):
     grad_logits: Optional[torch.Tensor]
     saved: Optional[torch.Tensor]      # [rows, 4]
     row_grads: Optional[torch.Tensor]  # [2, rows]
+
+
+def _native(logits, name, *args):
+    """The call by the binding's native part, or None where the logits are not
+    on the current device or an argument is not plainly what it should be (the
+    code below then says what is wrong)."""
+    device = logits.get_device()
+    if device < 0 or device != torch._C._cuda_getDevice():
+        return None
+    r = getattr(binding(), name)(logits, *args, torch._C._cuda_getCurrentRawStream(device))
+    if r.__class__ is int:
+        _check(r, f"acdc_{name}")
+    return r
 
 
 def _logits(x, name="logits"):
@@ -140,6 +153,9 @@ def token_logprobs(logits, targets, entropy: bool = False, save: bool = False, w
     """Log-probability of each row's target under softmax(logits), with
     ``entropy`` the entropy of each row, with ``save`` what
     ``token_logprobs_backward`` needs."""
+    r = _native(logits, "logprobs", targets, entropy, save, workspace)
+    if r is not None:
+        return TokenLogprobs(*r)
     rows, classes, stride = _logits(logits)
     device = logits.device
     bits = _index("targets", targets, rows, device)
@@ -158,6 +174,9 @@ def token_logprobs(logits, targets, entropy: bool = False, save: bool = False, w
 def token_logprobs_backward(logits, targets, saved, grad_logp, grad_entropy=None, scale=None, out=None):
     """dL/dlogits from dL/dlogp and dL/dentropy of each row, times ``scale`` (a
     tensor of one value on the device) if given."""
+    r = _native(logits, "logprobs_backward", targets, saved, grad_logp, grad_entropy, scale, out)
+    if r is not None:
+        return r
     rows, classes, stride = _logits(logits)
     device = logits.device
     bits = _index("targets", targets, rows, device)
@@ -197,12 +216,16 @@ def policy_loss(logits, actions, logp_old, advantages, logp_ref=None, weights=No
     gradient of the logits (a loss scale, or 1 / steps of an accumulation).
     ``grad`` off computes the values alone; ``save`` returns what
     ``token_logprobs_backward`` needs to compute the gradient later."""
+    low, high = clip
+    r = _native(logits, "policy", actions, logp_old, advantages, logp_ref, weights, low, high, kl_coef, entropy_coef,
+                grad_scale, mean, grad, save, out, workspace)
+    if r is not None:
+        return PolicyLoss(*r)
     rows, classes, stride = _logits(logits)
     device = logits.device
     bits = _index("actions", actions, rows, device)
     if kl_coef != 0.0 and logp_ref is None:
         raise ValueError("kl_coef needs logp_ref")
-    low, high = clip
     if not (low >= 0 and high >= 0):
         raise ValueError(f"clip must be two distances >= 0, got {clip}")
     for name, t in (("logp_old", logp_old), ("logp_ref", logp_ref), ("advantages", advantages), ("weights", weights)):
@@ -231,6 +254,10 @@ def preference_loss(logits, targets, offsets, logp_ref, beta: float = 0.1, label
 
         -(1 - label_smoothing) log sigmoid(margin) - label_smoothing log sigmoid(-margin)
     """
+    r = _native(logits, "preference", targets, offsets, logp_ref, beta, label_smoothing, grad_scale, grad, save, out,
+                workspace)
+    if r is not None:
+        return PreferenceLoss(*r)
     rows, classes, stride = _logits(logits)
     device = logits.device
     bits = _index("targets", targets, rows, device)

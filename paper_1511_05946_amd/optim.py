@@ -22,7 +22,7 @@ import struct
 
 import torch
 
-from ._lib import lib
+from ._lib import binding, lib
 from .acdc import _call, _check
 
 SCALE_BLOCK = 256
@@ -32,6 +32,18 @@ _RECORD = struct.Struct("=7Qqffii")   # struct acdc_adamw_tensor
 
 def _real_numel(t) -> int:
     return 2 * t.numel() if t.dtype is torch.complex64 else t.numel()
+
+
+def _native_stream(tensors):
+    """The current stream, if the native part of the binding can take tensors
+    of the first one's device; None leaves them to the code that checks one by
+    one and says what is wrong."""
+    if not tensors or not isinstance(tensors[0], torch.Tensor):
+        return None
+    device = tensors[0].get_device()
+    if device < 0 or device != torch._C._cuda_getDevice():
+        return None
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def moments(param, bits: int = 32):
@@ -85,6 +97,12 @@ def adamw_step(params, grads, moments, step: int, lr=1e-3, betas=(0.9, 0.999), e
     rounded into it, or None.  ``grad_scale``: a float32 tensor of one value
     that multiplies every gradient, such as ``grad_norm(...)[1:]``; where it is
     not finite the step leaves everything as it is."""
+    stream = _native_stream(params)
+    if stream is not None:
+        rc = binding().adamw(params, grads, moments, masters, lr, weight_decay, betas[0], betas[1], eps, step, grad_scale,
+                             stream)
+        if rc is not None:
+            return _check(rc, "acdc_adamw_step")
     count = len(params)
     if len(grads) != count or len(moments) != count or (masters is not None and len(masters) != count):
         raise ValueError("params, grads, moments and masters must be lists of one length")
@@ -122,6 +140,13 @@ def grad_norm(grads, max_norm=None, out=None):
     """[norm, scale] on the device: the 2-norm of all gradients together and the
     factor min(1, max_norm / (norm + 1e-6)) that clips them (1 without
     ``max_norm``), which ``adamw_step`` takes as ``grad_scale=result[1:]``."""
+    stream = _native_stream(grads)
+    if stream is not None and (max_norm is None or max_norm > 0):
+        r = binding().grad_norm(grads, max_norm or 0.0, out, stream)
+        if r.__class__ is int:
+            _check(r, "acdc_grad_norm")
+        elif r is not None:
+            return r
     count = len(grads)
     if count == 0:
         raise ValueError("grad_norm needs a tensor at least")
