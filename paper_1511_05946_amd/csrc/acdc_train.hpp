@@ -44,24 +44,37 @@ struct BF16 {
   }
   __device__ __forceinline__ static Elem to(float v) { return __bf16(v); }
 };
+// Loads and stores of data that passes through the card once (NT) carry the
+// hint that the caches need not keep it: what they hold of other data stays,
+// and a write goes out without its line being brought in.
+template <bool NT, class V>
+__device__ __forceinline__ V load_as(const V* p) {
+  if constexpr (NT) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+template <bool NT, class V>
+__device__ __forceinline__ void store_as(V* p, const V& v) {
+  if constexpr (NT) __builtin_nontemporal_store(v, p);
+  else *p = v;
+}
 template <class T>
 __device__ __forceinline__ typename T::Raw load_chunk(const typename T::Elem* p) {
   return *reinterpret_cast<const typename T::Raw*>(p);
 }
 template <class T>
 __device__ __forceinline__ void store_chunk(typename T::Elem* p, const typename T::Raw& r) {
-  *reinterpret_cast<typename T::Raw*>(p) = r;
+  store_as<true>(reinterpret_cast<typename T::Raw*>(p), r);
 }
 // The same at a lane's byte offset from an address that the whole wave shares:
 // the address stays in scalar registers, and a thread keeps one offset.
-template <class T>
+template <class T, bool NT = false>
 __device__ __forceinline__ typename T::Raw load_chunk_at(const typename T::Elem* p, unsigned fixed, unsigned lane) {
-  return *reinterpret_cast<const typename T::Raw*>((reinterpret_cast<const char*>(p) + fixed) + lane);
+  return load_as<NT>(reinterpret_cast<const typename T::Raw*>((reinterpret_cast<const char*>(p) + fixed) + lane));
 }
 template <class T>
 __device__ __forceinline__ void store_chunk_at(typename T::Elem* p, unsigned fixed, unsigned lane,
                                                const typename T::Raw& r) {
-  *reinterpret_cast<typename T::Raw*>((reinterpret_cast<char*>(p) + fixed) + lane) = r;
+  store_as<true>(reinterpret_cast<typename T::Raw*>((reinterpret_cast<char*>(p) + fixed) + lane), r);
 }
 // A value that all lanes of the wave hold, moved to a scalar register.
 __device__ __forceinline__ float uniform(float v) {

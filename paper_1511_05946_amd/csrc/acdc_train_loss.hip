@@ -122,6 +122,34 @@ __device__ __forceinline__ void put_row(const RowOut& o, long long r, const floa
   }
 }
 
+// f.template operator()<N>(c) for the chunks c, c + step, ... below `to`, AHEAD at a time.
+template <int AHEAD, class F>
+__device__ __forceinline__ void stream(int c, int to, int step, F&& f) {
+  for (; c + (AHEAD - 1) * step < to; c += AHEAD * step) f.template operator()<AHEAD>(c);
+  for (; c < to; c += step) f.template operator()<1>(c);
+}
+// The run of N chunks c, c + step, ..., asked for together.
+template <class T, int N>
+__device__ __forceinline__ Run run_of(const typename T::Elem* body, int c, int step) {
+  typename T::Raw raw[N];
+#pragma unroll
+  for (int q = 0; q < N; ++q) raw[q] = load_chunk<T>(body + (long long)(c + q * step) * T::kPer);
+  Run b = empty_run();
+#pragma unroll
+  for (int q = 0; q < N; ++q)
+#pragma unroll
+    for (int i = 0; i < T::kPer; ++i) b.m = fmaxf(b.m, T::get(raw[q], i));
+#pragma unroll
+  for (int q = 0; q < N; ++q)
+#pragma unroll
+    for (int i = 0; i < T::kPer; ++i) {
+      const float d = T::get(raw[q], i) - b.m, e = exp_of(d);
+      b.s += e;
+      b.u += e * fmaxf(d, -1e30f);
+    }
+  return b;
+}
+
 // A workgroup's part of a row, streamed: every thread keeps a run of its own.
 // Workgroup r * split + k takes part k of row r; with split = 1 it writes the
 // row's (M, S, H, logp), otherwise the runs of the parts.
@@ -143,28 +171,7 @@ __global__ __launch_bounds__(kThreads) void k_row_stats(const typename T::Elem* 
   int from, to;
   chunks_of(cut.full, split, k, from, to);
   const typename T::Elem* body = row + cut.head;
-  auto take = [&]<int N>(int c) {  // N chunks, asked for together: c, c + kThreads, ...
-    typename T::Raw raw[N];
-#pragma unroll
-    for (int q = 0; q < N; ++q) raw[q] = load_chunk<T>(body + (long long)(c + q * kThreads) * T::kPer);
-    Run b = empty_run();
-#pragma unroll
-    for (int q = 0; q < N; ++q)
-#pragma unroll
-      for (int i = 0; i < T::kPer; ++i) b.m = fmaxf(b.m, T::get(raw[q], i));
-#pragma unroll
-    for (int q = 0; q < N; ++q)
-#pragma unroll
-      for (int i = 0; i < T::kPer; ++i) {
-        const float d = T::get(raw[q], i) - b.m, e = exp_of(d);
-        b.s += e;
-        b.u += e * fmaxf(d, -1e30f);
-      }
-    run = merge(run, b);
-  };
-  int c = from + threadIdx.x;
-  for (; c + (kAhead - 1) * kThreads < to; c += kAhead * kThreads) take.template operator()<kAhead>(c);
-  for (; c < to; c += kThreads) take.template operator()<1>(c);
+  stream<kAhead>(from + threadIdx.x, to, kThreads, [&]<int N>(int c) { run = merge(run, run_of<T, N>(body, c, kThreads)); });
   if (k == split - 1 && int(threadIdx.x) < cut.extra) {
     const float v = T::one(row[cut.element(threadIdx.x)]);
     Run b = empty_run();
@@ -182,6 +189,22 @@ __global__ __launch_bounds__(kThreads) void k_row_stats(const typename T::Elem* 
     if (split == 1) put_row(out, r, stat_of(run, target_logit<T>(row, t, classes)), 0.f, 0.f);
     else parts[r * split + k] = make_float4(run.m, run.s, run.u, 0.f);
   }
+}
+
+// The row's statistics out of its parts, by one thread.
+__device__ __forceinline__ float4 join_alone(const float4* __restrict__ parts, int split, long long r, float xt) {
+  const float4* p = parts + r * split;
+  float m = kNegMax, s = 0.f, u = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < split; ++k) m = fmaxf(m, p[k].x);
+#pragma unroll 8
+  for (int k = 0; k < split; ++k) {
+    const float4 v = p[k];
+    const float d = below(v.x, m), f = exp_of(d);
+    s += v.y * f;
+    u += f * (v.z + d * v.y);
+  }
+  return stat_of(Run{m, s, u}, xt);
 }
 
 // The row's statistics out of its parts (at most 64), for a whole wave.
@@ -223,6 +246,23 @@ __device__ __forceinline__ float slope_value(const Slope& k, float x) {
   const float d = x - k.m;
   // a class of probability 0 has d = -inf or nearly: its 0 is not to meet an infinity
   return exp_of(d) * (k.a + k.b * fmaxf(d, -1e30f));
+}
+
+// The gradients of N chunks c, c + step, ....  Their loads stand before their
+// stores: the gradient may be the logits' own memory, so that the compiler
+// would not move a load ahead of an earlier store by itself.
+template <class T, int N>
+__device__ __forceinline__ void slopes(const Slope& sl, const typename T::Elem* body, typename T::Elem* out, int c, int step) {
+  typename T::Raw raw[N];
+#pragma unroll
+  for (int q = 0; q < N; ++q) raw[q] = load_chunk<T>(body + (long long)(c + q * step) * T::kPer);
+#pragma unroll
+  for (int q = 0; q < N; ++q) {
+    float y[T::kPer];
+#pragma unroll
+    for (int i = 0; i < T::kPer; ++i) y[i] = slope_value(sl, T::get(raw[q], i));
+    store_chunk<T>(out + (long long)(c + q * step) * T::kPer, T::pack(y));
+  }
 }
 
 // dL/dlogits from each row's (M, S, H, logp), g and h; workgroups as in
@@ -275,23 +315,7 @@ __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x
                    : has_one && cut.lane_of(int(t)) == int(threadIdx.x);
   }
   const float yt = mine ? slope_value(sl, T::one(row[t])) + g : 0.f;
-  auto give = [&]<int N>(int i) {
-    // the loads of a group stand before its stores: out may be x, so that the
-    // compiler would not move a load ahead of an earlier store by itself
-    typename T::Raw raw[N];
-#pragma unroll
-    for (int q = 0; q < N; ++q) raw[q] = load_chunk<T>(body + (long long)(i + q * kThreads) * T::kPer);
-#pragma unroll
-    for (int q = 0; q < N; ++q) {
-      float y[T::kPer];
-#pragma unroll
-      for (int e = 0; e < T::kPer; ++e) y[e] = slope_value(sl, T::get(raw[q], e));
-      store_chunk<T>(out_body + (long long)(i + q * kThreads) * T::kPer, T::pack(y));
-    }
-  };
-  int i = from + threadIdx.x;
-  for (; i + (kAhead - 1) * kThreads < to; i += kAhead * kThreads) give.template operator()<kAhead>(i);
-  for (; i < to; i += kThreads) give.template operator()<1>(i);
+  stream<kAhead>(from + threadIdx.x, to, kThreads, [&]<int N>(int i) { slopes<T, N>(sl, body, out_body, i, kThreads); });
   if (has_one) out[one] = T::to(slope_value(sl, T::one(row[one])));
   if (mine) out[t] = T::to(yt);
 }
@@ -320,8 +344,8 @@ struct PolicyArgs {
   acdc_policy_params p;
 };
 __device__ __forceinline__ float weight_of(const PolicyArgs& a, long long r) {
-  if (target_of(a.targets, a.bits, r) < 0) return 0.f;
-  return a.weights != nullptr ? a.weights[r] : 1.f;
+  const float w = a.weights != nullptr ? a.weights[r] : 1.f;  // (asked for along with the target)
+  return target_of(a.targets, a.bits, r) < 0 ? 0.f : w;
 }
 __device__ __forceinline__ float norm_of(const PolicyArgs& a, double total) {
   return !a.p.mean ? 1.f : total != 0.0 ? float(1.0 / total) : 0.f;
@@ -384,8 +408,8 @@ __device__ __forceinline__ double weight_total(const double* __restrict__ sums, 
 }
 
 // The policy loss of rows whose statistics stand in `stat` (in parts of
-// `split`, where that is more than 1): one thread per row (wave per row with
-// parts).  With one workgroup it sums the weights and writes the stats itself;
+// `split`, where that is more than 1): one thread per row, or a wave for each
+// of up to 16 rows in parts.  With one workgroup it sums the weights and writes the stats itself;
 // with more, `sums` holds the weights' sums and `partial` gets each
 // workgroup's stats.
 template <class T>
@@ -404,7 +428,8 @@ __global__ __launch_bounds__(kWide) void k_policy_rows(PolicyArgs a, const typen
   }
   const float norm = norm_of(a, total);
   double sum[kStats] = {};
-  const int per = split > 1 ? kWide / 64 : kWide, me = split > 1 ? threadIdx.x / 64 : threadIdx.x;
+  const bool by_wave = split > 1 && a.rows <= kWide / 64;
+  const int per = by_wave ? kWide / 64 : kWide, me = by_wave ? threadIdx.x / 64 : threadIdx.x;
   for (long long r = (long long)blockIdx.x * per + me; r < a.rows; r += (long long)gridDim.x * per) {
     const float w = weight_of(a, r) * norm;
     float4 st = make_float4(0.f, 1.f, 0.f, 0.f);
@@ -412,13 +437,14 @@ __global__ __launch_bounds__(kWide) void k_policy_rows(PolicyArgs a, const typen
     if (w != 0.f) {
       if (split > 1) {
         const long long t = target_of(a.targets, a.bits, r);
-        st = join_parts<T>(parts, split, r, target_logit<T>(x + r * stride, t, classes));
+        const float xt = target_logit<T>(x + r * stride, t, classes);
+        st = by_wave ? join_parts<T>(parts, split, r, xt) : join_alone(parts, split, r, xt);
       } else {
         st = stat[r];
       }
       row = policy_row(a.p, w, st.w, st.z, a.old[r], a.advantages[r], a.ref != nullptr, a.ref != nullptr ? a.ref[r] : 0.f);
     }
-    if (split == 1 || threadIdx.x % 64 == 0) {
+    if (!by_wave || threadIdx.x % 64 == 0) {
       put_row(out, r, st, row.g, row.h);
 #pragma unroll
       for (int i = 0; i < kStats; ++i) sum[i] += double(row.v[i]);
@@ -503,29 +529,21 @@ struct Group {
 // The policy loss and its gradient in one pass over the logits: a row stays in
 // the registers of its THREADS lanes, NC chunks each, from its load to its
 // gradient's store.  Rows blockIdx, blockIdx + gridDim, ... of a workgroup;
-// its rows' stats go into partial[.][blockIdx], or with one workgroup (which
-// then sums the weights itself) into stats.
+// its rows' stats go into partial[.][blockIdx].  LONG: what the registers do
+// not hold of a row is streamed for the statistics and read again (out of the
+// Infinity Cache, which a row a CU fits) for the gradient.
 constexpr int fused_waves(int nc) { return nc <= 4 ? 8 : nc <= 8 ? 6 : nc <= 12 ? 5 : 4; }
-template <class T, int WG, int THREADS, int NC>
-__global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(fused_waves(NC)))) void k_policy_fused(
+template <class T, int WG, int THREADS, int NC, bool LONG, bool NT>
+__global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(LONG ? 4 : fused_waves(NC)))) void k_policy_fused(
     PolicyArgs a, const typename T::Elem* x, long long stride, int classes, const double* __restrict__ sums, int groups,
     typename T::Elem* grad, long long grad_stride, RowOut out, float* __restrict__ partial) {
   constexpr int ROWS = WG / THREADS;
   __shared__ float slots[3 * (WG / 64)];
-  __shared__ double wide[WG / 64];
   __shared__ double acc[ROWS][kStats];  // each row's stats: too seldom to hold registers
   Group<THREADS> group{slots};
   const int lane = threadIdx.x % THREADS;
   const int sub = ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0;
-  double total;
-  if (gridDim.x == 1) {
-    double w = 0.0;
-    for (long long r = threadIdx.x; r < a.rows; r += WG) w += double(weight_of(a, r));
-    total = total_of<WG>(w, wide);
-  } else {
-    total = weight_total(sums, groups);
-  }
-  const float norm = norm_of(a, total);
+  const float norm = norm_of(a, weight_total(sums, groups));
   if (threadIdx.x < ROWS * kStats) (&acc[0][0])[threadIdx.x] = 0.0;
   __syncthreads();
   const unsigned at = unsigned(lane) * 16u;
@@ -546,6 +564,9 @@ __global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(fused_waves(
 #pragma unroll
       for (int c = 0; c < NC; ++c)
         if (chunk(c)) store_chunk_at<T>(to_body, c * THREADS * 16u, at, T::pack(zero));
+      if constexpr (LONG)
+        for (int c = NC * THREADS + lane; c < cut.full; c += THREADS)
+          store_chunk<T>(to_body + (long long)c * T::kPer, T::pack(zero));
       if (has_one) to[one] = T::to(0.f);
       if (lane == 0) put_row(out, r, make_float4(0.f, 1.f, 0.f, 0.f), 0.f, 0.f);
       continue;
@@ -562,12 +583,17 @@ __global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(fused_waves(
     for (int c = 0; c < NC; ++c) raw[c] = typename T::Raw{};
 #pragma unroll
     for (int c = 0; c < NC; ++c)
-      if (chunk(c)) raw[c] = load_chunk_at<T>(body, c * THREADS * 16u, at);
+      if (chunk(c)) raw[c] = load_chunk_at<T, NT>(body, c * THREADS * 16u, at);
     const float last = has_one ? T::one(row[one]) : kNegMax;
     const float xt = uniform(target_logit<T>(row, t, classes));
     const float old = uniform(a.old[r]), adv = uniform(a.advantages[r]);
     const float ref = uniform(a.ref != nullptr ? a.ref[r] : 0.f);
-    float m = fmaxf(kNegMax, last);
+    Run run = empty_run();  // of what is streamed
+    if constexpr (LONG)
+      stream<kAhead>(NC * THREADS + lane, cut.full, THREADS, [&]<int N>(int c) {
+        run = merge(run, run_of<T, N>(body, c, THREADS));
+      });
+    float m = fmaxf(run.m, last);
 #pragma unroll
     for (int c = 0; c < NC; ++c)
       if (chunk(c)) {
@@ -577,6 +603,11 @@ __global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(fused_waves(
     forget();
     m = uniform(group.max(m));
     float s = 0.f, u = 0.f;
+    if constexpr (LONG) {
+      const float d = below(run.m, m), f = exp_of(d);
+      s = run.s * f;
+      u = f * (run.u + d * run.s);
+    }
     auto add = [&](float v) {
       const float d = v - m, e = exp_of(d);
       s += e;
@@ -605,6 +636,8 @@ __global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(fused_waves(
         for (int i = 0; i < T::kPer; ++i) y[i] = slope_value(sl, T::get(raw[c], i));
         store_chunk_at<T>(to_body, c * THREADS * 16u, at, T::pack(y));
       }
+    if constexpr (LONG)
+      stream<kAhead>(NC * THREADS + lane, cut.full, THREADS, [&]<int N>(int c) { slopes<T, N>(sl, body, to_body, c, THREADS); });
     if (has_one) to[one] = T::to(slope_value(sl, last));
     // the lane that wrote the target's chunk writes the target again, with its g
     const int tc = cut.chunk_of(t);
@@ -653,9 +686,10 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(WAVE
       t[q] = -1;
       on[q] = false;
       if (r < a.rows) {
+        const float weight = a.weights != nullptr ? a.weights[r] : 1.f;
         const long long target = target_of(a.targets, a.bits, r);
         t[q] = uniform(target < 0 ? -1 : target < classes ? int(target) : classes);
-        on[q] = t[q] >= 0 && (a.weights == nullptr || uniform(a.weights[r]) != 0.f);
+        on[q] = t[q] >= 0 && uniform(weight) != 0.f;
       }
     }
 #pragma unroll
@@ -915,6 +949,14 @@ int split_of(int64_t rows, int32_t classes) {
 }
 // Workgroups (and so partial stats) of the kernels that sum the policy's stats.
 constexpr int64_t kMaxPartials = 8192;
+// Bytes of logits from which on the one pass over them reads them with the hint
+// that no cache need keep them (they are past half of the Infinity Cache, and
+// nothing reads them again): 8192 rows of 65536 bfloat16 394 us instead of 400,
+// 2048 rows of 4096 floats, 34 MB, 20 us without it and 22 with it.  Gradients
+// are always written with the hint: 8192 rows of 4096 61 -> 57 us, 2048 rows
+// 23 -> 20 us; the cascade's backward that reads them next takes as much
+// longer, so that the two together are the same within 2 % at any size.
+constexpr double kKeepBytes = 128e6;
 
 struct Workspace {
   size_t stat, grads, parts, sums, partial, total;
@@ -932,8 +974,7 @@ Workspace layout(int64_t rows, int32_t classes, int64_t pairs) {
   w.grads = take(size_t(rows) * 2 * sizeof(float));
   w.parts = take(split > 1 ? size_t(rows) * split * sizeof(float4) : 0);
   w.sums = take(kWeightSums * sizeof(double));
-  // at least two workgroups, see acdc_policy_loss
-  w.partial = take(size_t(std::max<int64_t>(2, std::min(std::max(rows, pairs), kMaxPartials))) * kStats * sizeof(float));
+  w.partial = take(size_t(std::min(std::max(rows, pairs), kMaxPartials)) * kStats * sizeof(float));
   w.total = at;
   return w;
 }
@@ -997,22 +1038,21 @@ int launch_grad(const Logits& l, const float4* stat, const float* g, const float
   return done();
 }
 
-// f.template operator()<THREADS, NC>() for the fewest lanes and registers that
-// hold a row of `chunks` chunks; false where none does.
+// f.template operator()<THREADS, NC, LONG>() for the fewest lanes and registers
+// that hold a row of `chunks` chunks; LONG where none do.
 template <class F>
-bool with_row_shape(int chunks, F&& f) {
-  if (chunks <= 64) f.template operator()<64, 1>();
-  else if (chunks <= 128) f.template operator()<64, 2>();
-  else if (chunks <= 256) f.template operator()<64, 4>();
-  else if (chunks <= 512) f.template operator()<64, 8>();
-  else if (chunks <= 1024) f.template operator()<256, 4>();
-  else if (chunks <= 2048) f.template operator()<256, 8>();
-  else if (chunks <= 3072) f.template operator()<256, 12>();
-  else if (chunks <= 4096) f.template operator()<256, 16>();
-  else if (chunks <= 8192) f.template operator()<512, 16>();
-  else if (chunks <= 16384) f.template operator()<1024, 16>();
-  else return false;
-  return true;
+void with_row_shape(int chunks, F&& f) {
+  if (chunks <= 64) f.template operator()<64, 1, false>();
+  else if (chunks <= 128) f.template operator()<64, 2, false>();
+  else if (chunks <= 256) f.template operator()<64, 4, false>();
+  else if (chunks <= 512) f.template operator()<64, 8, false>();
+  else if (chunks <= 1024) f.template operator()<256, 4, false>();
+  else if (chunks <= 2048) f.template operator()<256, 8, false>();
+  else if (chunks <= 3072) f.template operator()<256, 12, false>();
+  else if (chunks <= 4096) f.template operator()<256, 16, false>();
+  else if (chunks <= 8192) f.template operator()<512, 16, false>();
+  else if (chunks <= 16384) f.template operator()<1024, 16, false>();
+  else f.template operator()<1024, 12, true>();
 }
 
 }  // namespace
@@ -1096,11 +1136,10 @@ extern "C" int acdc_policy_loss(const void* logits, int32_t dtype, int64_t strid
   };
 
   // Enough rows to fill the card, or rows of a wave each: one pass.
-  bool fused = false;
   const int split = split_of(rows, classes);
-  if (rows > 0 && grad_logits != nullptr && split == 1)
+  if (rows > 0 && grad_logits != nullptr && split == 1) {
     with_type(dtype, [&]<class T>() {
-      fused = with_row_shape(classes / T::kPer, [&]<int THREADS, int NC>() {
+      with_row_shape(classes / T::kPer, [&]<int THREADS, int NC, bool LONG>() {
         const RowOut out{logp, nullptr, reinterpret_cast<float4*>(saved), row_grads,
                          row_grads != nullptr ? row_grads + rows : nullptr};
         auto go = [&](auto kernel, unsigned blocks, int wg, float* to) {
@@ -1122,15 +1161,18 @@ extern "C" int acdc_policy_loss(const void* logits, int32_t dtype, int64_t strid
           }
         } else {
           constexpr int WG = THREADS < kThreads ? kThreads : THREADS;
-          // two workgroups at least: one alone would take the weights for its own to sum
-          const unsigned blocks = std::max(2u, blocks_of(WG / THREADS));
+          const unsigned blocks = blocks_of(WG / THREADS);
           sum_weights();
-          go(k_policy_fused<T, WG, THREADS, NC>, blocks, WG, partial);
+          if (double(rows) * double(stride) * sizeof(typename T::Elem) >= kKeepBytes)
+            go(k_policy_fused<T, WG, THREADS, NC, LONG, true>, blocks, WG, partial);
+          else
+            go(k_policy_fused<T, WG, THREADS, NC, LONG, false>, blocks, WG, partial);
           sum_stats(blocks);
         }
       });
     });
-  if (fused) return done();
+    return done();
+  }
 
   float4* stat = saved != nullptr ? reinterpret_cast<float4*>(saved) : reinterpret_cast<float4*>(ws + w.stat);
   float* grads = row_grads != nullptr ? row_grads : reinterpret_cast<float*>(ws + w.grads);

@@ -46,20 +46,23 @@ struct Step {
 };
 
 // The tensor that a workgroup works on: the last one whose first workgroup is
-// not after it.  One load per lane and a ballot instead of a search.
+// not after it.  One load per lane and a ballot for 64 tensors at a time.
 __device__ __forceinline__ int tensor_of(const int* first, int count, int block) {
-  const int lane = threadIdx.x % 64;
-  const bool past = lane < count ? first[lane] <= block : false;
-  return __builtin_amdgcn_readfirstlane(__popcll(__ballot(past)) - 1);
+  int i = -1;
+  for (int base = 0; base < count; base += 64) {
+    const int k = base + int(threadIdx.x) % 64;
+    i += __popcll(__ballot(k < count ? first[k] <= block : false));
+  }
+  return __builtin_amdgcn_readfirstlane(i);
 }
 
 // Four elements, the first of them at p; `have` of them exist.
-template <class T>
+template <class T, bool NT>
 __device__ __forceinline__ void load4(const void* base, long long at, int have, float (&v)[4]) {
   typedef typename T::Elem V4 __attribute__((ext_vector_type(4), aligned(sizeof(typename T::Elem))));
   const typename T::Elem* p = static_cast<const typename T::Elem*>(base) + at;
   if (have == 4) {
-    const V4 r = *reinterpret_cast<const V4*>(p);
+    const V4 r = load_as<NT>(reinterpret_cast<const V4*>(p));
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = float(r[i]);
   } else {
@@ -67,12 +70,12 @@ __device__ __forceinline__ void load4(const void* base, long long at, int have, 
     for (int i = 0; i < 4; ++i) v[i] = i < have ? float(p[i]) : 0.f;
   }
 }
-template <class T>
+template <class T, bool NT>
 __device__ __forceinline__ void store4(void* base, long long at, int have, const float (&v)[4]) {
   typedef typename T::Elem V4 __attribute__((ext_vector_type(4), aligned(sizeof(typename T::Elem))));
   typename T::Elem* p = static_cast<typename T::Elem*>(base) + at;
   if (have == 4) {
-    *reinterpret_cast<V4*>(p) = V4{T::to(v[0]), T::to(v[1]), T::to(v[2]), T::to(v[3])};
+    store_as<NT>(reinterpret_cast<V4*>(p), V4{T::to(v[0]), T::to(v[1]), T::to(v[2]), T::to(v[3])});
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -82,19 +85,21 @@ __device__ __forceinline__ void store4(void* base, long long at, int have, const
 
 // Four e4m3 codes as one word.
 typedef unsigned Word1 __attribute__((aligned(1)));
+template <bool NT>
 __device__ __forceinline__ unsigned load_codes(const void* base, long long at, int have) {
   const unsigned char* p = static_cast<const unsigned char*>(base) + at;
-  if (have == 4) return *reinterpret_cast<const Word1*>(p);
+  if (have == 4) return load_as<NT>(reinterpret_cast<const Word1*>(p));
   unsigned w = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (i < have) w |= unsigned(p[i]) << (8 * i);
   return w;
 }
+template <bool NT>
 __device__ __forceinline__ void store_codes(void* base, long long at, int have, unsigned w) {
   unsigned char* p = static_cast<unsigned char*>(base) + at;
   if (have == 4) {
-    *reinterpret_cast<Word1*>(p) = w;
+    store_as<NT>(reinterpret_cast<Word1*>(p), Word1(w));
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -131,7 +136,7 @@ __device__ __forceinline__ float scale_of(const float (&v)[4]) {
   return top < 0x1p-100f ? 0.f : top * kPerTop;
 }
 
-template <class P, class G, int BITS, bool MASTER>
+template <class P, class G, int BITS, bool MASTER, bool NT>
 __global__ __launch_bounds__(kThreads) void k_adamw(Batch b, int count, Step s) {
   const int i = tensor_of(b.first, count, blockIdx.x);
   const Tensor& t = b.t[i];
@@ -146,15 +151,15 @@ __global__ __launch_bounds__(kThreads) void k_adamw(Batch b, int count, Step s) 
   const long long at = base + lane, left = t.n - at;
   const int have = left >= 4 ? 4 : left > 0 ? int(left) : 0;
   float g[4], m[4], v[4], w[4];
-  load4<G>(t.grad, at, have, g);
-  if constexpr (MASTER) load4<F32>(t.master, at, have, w);
-  else load4<P>(t.param, at, have, w);
+  load4<G, NT>(t.grad, at, have, g);
+  if constexpr (MASTER) load4<F32, NT>(t.master, at, have, w);
+  else load4<P, NT>(t.param, at, have, w);
   if constexpr (BITS == 32) {
-    load4<F32>(t.m, at, have, m);
-    load4<F32>(t.v, at, have, v);
+    load4<F32, NT>(t.m, at, have, m);
+    load4<F32, NT>(t.v, at, have, v);
   } else {
-    decode4(load_codes(t.m, at, have), t.m_scale[base / kBlock], m);
-    decode4(load_codes(t.v, at, have), t.v_scale[base / kBlock], v);
+    decode4(load_codes<NT>(t.m, at, have), t.m_scale[base / kBlock], m);
+    decode4(load_codes<NT>(t.v, at, have), t.v_scale[base / kBlock], v);
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -172,15 +177,15 @@ __global__ __launch_bounds__(kThreads) void k_adamw(Batch b, int count, Step s) 
     root[k] = sqrtf(v[k]);
     w[k] = w[k] * t.decay - t.rate * (m[k] / (root[k] * s.root_scale + s.eps));
   }
-  if constexpr (MASTER) store4<F32>(t.master, at, have, w);
-  store4<P>(t.param, at, have, w);
+  if constexpr (MASTER) store4<F32, NT>(t.master, at, have, w);
+  store4<P, NT>(t.param, at, have, w);
   if constexpr (BITS == 32) {
-    store4<F32>(t.m, at, have, m);
-    store4<F32>(t.v, at, have, v);
+    store4<F32, NT>(t.m, at, have, m);
+    store4<F32, NT>(t.v, at, have, v);
   } else {
     const float ms = scale_of(m), vs = scale_of(root);
-    store_codes(t.m, at, have, encode4<false>(m, ms));
-    store_codes(t.v, at, have, encode4<true>(root, vs));
+    store_codes<NT>(t.m, at, have, encode4<false>(m, ms));
+    store_codes<NT>(t.v, at, have, encode4<true>(root, vs));
     if (lane == 0) {
       t.m_scale[base / kBlock] = ms;
       t.v_scale[base / kBlock] = vs;
@@ -192,7 +197,17 @@ __global__ __launch_bounds__(kThreads) void k_adamw(Batch b, int count, Step s) 
 
 constexpr int kNormBatch = 180;
 constexpr int kNormRounds = 4;     // chunks of 16 bytes that a thread asks for at a time
-constexpr int kNormChunk = 8192;   // elements a workgroup
+// Elements a workgroup takes, a power of two by the list's whole size: long
+// enough that finding its tensor is a small part of its time, and short enough
+// that there are thousands of workgroups (about 4096 where the list allows it).
+constexpr long long kNormLeast = 4096, kNormMost = 65536;
+long long norm_chunk(const int64_t* sizes, int32_t count) {
+  long long all = 0;
+  for (int32_t i = 0; i < count; ++i) all += sizes[i];
+  long long chunk = kNormLeast;
+  while (chunk < kNormMost && all / (2 * chunk) >= 4096) chunk *= 2;
+  return chunk;
+}
 struct NormTensor {
   const void* grad;
   unsigned long long n_type;  // elements << 1 | bfloat16
@@ -215,9 +230,9 @@ __device__ __forceinline__ double sum_workgroup(double v, double* part, int wave
 }
 
 template <class G>
-__device__ __forceinline__ double square_sum(const typename G::Elem* p, long long n) {
+__device__ __forceinline__ double square_sum(const typename G::Elem* p, int count) {
   constexpr int kStep = kThreads * G::kPer;
-  const int count = n < kNormChunk ? int(n) : kNormChunk, full = count / G::kPer * G::kPer;
+  const int full = count / G::kPer * G::kPer;
   double total = 0.0;
   for (int base = 0; base < full; base += kStep * kNormRounds) {
     typename G::Raw raw[kNormRounds];
@@ -241,23 +256,14 @@ __device__ __forceinline__ double square_sum(const typename G::Elem* p, long lon
   return total;
 }
 
-// The tensor of this workgroup: as tensor_of, for up to kNormBatch of them.
-__device__ __forceinline__ int norm_tensor_of(const int* first, int count, int block) {
-  int i = -1;
-  for (int base = 0; base < count; base += 64) {
-    const int k = base + int(threadIdx.x) % 64;
-    i += __popcll(__ballot(k < count ? first[k] <= block : false));
-  }
-  return __builtin_amdgcn_readfirstlane(i);
-}
-
-__global__ __launch_bounds__(kThreads) void k_square_sums(NormBatch b, int count, double* __restrict__ sums) {
+__global__ __launch_bounds__(kThreads) void k_square_sums(NormBatch b, int count, int chunk, double* __restrict__ sums) {
   __shared__ double part[kThreads / 64];
-  const int i = norm_tensor_of(b.first, count, blockIdx.x);
-  const long long begin = (long long)(int(blockIdx.x) - b.first[i]) * kNormChunk;
+  const int i = tensor_of(b.first, count, blockIdx.x);
+  const long long begin = (long long)(int(blockIdx.x) - b.first[i]) * chunk;
   const long long left = (long long)(b.t[i].n_type >> 1) - begin;
-  const double s = b.t[i].n_type & 1 ? square_sum<BF16>(static_cast<const __bf16*>(b.t[i].grad) + begin, left)
-                                     : square_sum<F32>(static_cast<const float*>(b.t[i].grad) + begin, left);
+  const int n = left < chunk ? int(left) : chunk;
+  const double s = b.t[i].n_type & 1 ? square_sum<BF16>(static_cast<const __bf16*>(b.t[i].grad) + begin, n)
+                                     : square_sum<F32>(static_cast<const float*>(b.t[i].grad) + begin, n);
   const double total = sum_workgroup(s, part, kThreads / 64);
   if (threadIdx.x == 0) sums[blockIdx.x] = total;
 }
@@ -293,11 +299,21 @@ int class_of(const acdc_adamw_tensor& t) {
 }
 constexpr int kClasses = 16;
 
-void launch_class(int cls, const Batch& b, int count, long long blocks, const Step& s, hipStream_t stream) {
+// Bytes of a step's tensors from which on they are not to stay in the caches: half
+// of the 256 MB Infinity Cache, as the passes between two steps use it too.  (With
+// the hint 160 MB of float tensors took 49 us instead of 56, 4.5 GB of bfloat16
+// ones with masters 775 instead of 900; without it 80 MB took 23 instead of 26.)
+constexpr double kKeepBytes = 128e6;
+
+void launch_class(int cls, bool nt, const Batch& b, int count, long long blocks, const Step& s, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(blocks)), block(kThreads);
+  auto hint = [&]<class P, class G, int BITS, bool MASTER>() {
+    if (nt) hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, true>), grid, block, 0, stream, b, count, s);
+    else hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, false>), grid, block, 0, stream, b, count, s);
+  };
   auto moments = [&]<class P, class G, bool MASTER>() {
-    if (cls & 2) hipLaunchKernelGGL((k_adamw<P, G, 8, MASTER>), grid, block, 0, stream, b, count, s);
-    else hipLaunchKernelGGL((k_adamw<P, G, 32, MASTER>), grid, block, 0, stream, b, count, s);
+    if (cls & 2) hint.template operator()<P, G, 8, MASTER>();
+    else hint.template operator()<P, G, 32, MASTER>();
   };
   auto grads = [&]<class P, bool MASTER>() {
     if (cls & 4) moments.template operator()<P, BF16, MASTER>();
@@ -339,7 +355,13 @@ extern "C" int acdc_adamw_step(const acdc_adamw_tensor* tensors, int32_t count, 
   const Step s{1.0 - beta1, 1.0 - beta2, float(beta1), float(beta2), float(1.0 / std::sqrt(c2)), float(eps), grad_scale};
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   unsigned seen = 0;
-  for (int32_t i = 0; i < count; ++i) seen |= 1u << class_of(tensors[i]);
+  double bytes = 0.0;
+  for (int32_t i = 0; i < count; ++i) {
+    const acdc_adamw_tensor& t = tensors[i];
+    seen |= 1u << class_of(t);
+    bytes += double(t.n) * double(dtype_bytes(t.param_type) + dtype_bytes(t.grad_type) + (t.master != nullptr ? 4 : 0) +
+                                  (t.m_scale != nullptr ? 2 : 8));
+  }
   for (int cls = 0; cls < kClasses; ++cls) {
     if (!(seen >> cls & 1)) continue;
     Batch b;
@@ -347,7 +369,7 @@ extern "C" int acdc_adamw_step(const acdc_adamw_tensor* tensors, int32_t count, 
     long long blocks = 0;
     auto flush = [&]() -> int {
       if (used == 0) return ACDC_OK;
-      launch_class(cls, b, used, blocks, s, st);
+      launch_class(cls, bytes >= kKeepBytes, b, used, blocks, s, st);
       used = 0;
       blocks = 0;
       return done();
@@ -373,8 +395,9 @@ extern "C" int acdc_adamw_step(const acdc_adamw_tensor* tensors, int32_t count, 
 }
 
 static long long norm_blocks(const int64_t* sizes, int32_t count) {
+  const long long chunk = norm_chunk(sizes, count);
   long long blocks = 0;
-  for (int32_t i = 0; i < count; ++i) blocks += (sizes[i] + kNormChunk - 1) / kNormChunk;
+  for (int32_t i = 0; i < count; ++i) blocks += (sizes[i] + chunk - 1) / chunk;
   return blocks;
 }
 
@@ -395,7 +418,7 @@ extern "C" int acdc_grad_norm(const void* const* grads, const int64_t* sizes, co
     if (eb == 0 || sizes[i] < 0 || sizes[i] > (int64_t(1) << 40)) return ACDC_ERR_INVALID_ARG;
     if (sizes[i] > 0 && (grads[i] == nullptr || !aligned_to(grads[i], eb))) return ACDC_ERR_INVALID_ARG;
   }
-  const long long total = norm_blocks(sizes, count);
+  const long long total = norm_blocks(sizes, count), chunk = norm_chunk(sizes, count);
   if (total > 0 && (workspace == nullptr || workspace_bytes < size_t(total) * sizeof(double))) return ACDC_ERR_WORKSPACE;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   double* sums = static_cast<double*>(workspace);
@@ -404,7 +427,8 @@ extern "C" int acdc_grad_norm(const void* const* grads, const int64_t* sizes, co
   long long blocks = 0, at = 0;
   auto flush = [&]() -> int {
     if (used == 0) return ACDC_OK;
-    hipLaunchKernelGGL(k_square_sums, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, st, b, used, sums + at);
+    hipLaunchKernelGGL(k_square_sums, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, st, b, used, int(chunk),
+                       sums + at);
     at += blocks;
     used = 0;
     blocks = 0;
@@ -412,7 +436,7 @@ extern "C" int acdc_grad_norm(const void* const* grads, const int64_t* sizes, co
   };
   for (int32_t i = 0; i < count; ++i) {
     if (sizes[i] == 0) continue;
-    const long long need = (sizes[i] + kNormChunk - 1) / kNormChunk;
+    const long long need = (sizes[i] + chunk - 1) / chunk;
     if (used == kNormBatch || blocks + need > kMaxBlocks) {
       const int rc = flush();
       if (rc != ACDC_OK) return rc;

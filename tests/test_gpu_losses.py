@@ -24,7 +24,12 @@ SHAPES = [(1, 1, 1, "float32", 64), (3, 7, 7, "float32", 32), (300, 8, 8, "float
           (130, 33, 40, "bfloat16", 64), (6, 9216, 9216, "float32", 64), (2, 16387, 16387, "float32", 32),
           (3, 50001, 50001, "bfloat16", 64), (2, 131073, 131073, "float32", 64), (1, 262144, 262144, "bfloat16", 64),
           (700, 513, 513, "float32", 64), (1100, 2048, 2056, "bfloat16", 32), (600, 20000, 20000, "bfloat16", 64),
-          (520, 40001, 40001, "float32", 64), (4, 300001, 300001, "float32", 64)]
+          (520, 40001, 40001, "float32", 64), (4, 300001, 300001, "float32", 64),
+          # more than a workgroup's registers hold, with rows enough for one pass; rows in parts, more than 16
+          (130, 66001, 66003, "float32", 64), (128, 132001, 132001, "bfloat16", 32), (40, 20001, 20001, "float32", 64),
+          # tiles of short rows: several of them, each number of chunks a lane
+          (5000, 9, 9, "bfloat16", 64), (300, 400, 401, "float32", 64), (200, 1500, 1504, "bfloat16", 64),
+          (150, 4000, 4001, "bfloat16", 64)]
 
 
 def make(torch, shape, seed=0, spread=2.0, idle=0.2):
