@@ -150,14 +150,51 @@ __device__ __forceinline__ Run run_of(const typename T::Elem* body, int c, int s
   return b;
 }
 
+// Workgroup over a row that THREADS lanes share: a wave (64), which needs no
+// barrier, or the workgroup.
+template <int THREADS>
+struct Group {
+  float* slots;  // 3 * THREADS / 64 floats of LDS
+  __device__ __forceinline__ float max(float v) {
+    v = wave_max(v);
+    if constexpr (THREADS > 64) {
+      if (threadIdx.x % 64 == 0) slots[threadIdx.x / 64] = v;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < THREADS / 64; ++w) v = fmaxf(v, slots[w]);
+    }
+    return v;
+  }
+  // s and u over the group; the slots are those that max does not use, so that
+  // a barrier a call is enough (the next row's max comes after this one's barrier)
+  __device__ __forceinline__ void sum(float& s, float& u) {
+    s = wave_sum(s);
+    u = wave_sum(u);
+    if constexpr (THREADS > 64) {
+      constexpr int W = THREADS / 64;
+      if (threadIdx.x % 64 == 0) {
+        slots[W + threadIdx.x / 64] = s;
+        slots[2 * W + threadIdx.x / 64] = u;
+      }
+      __syncthreads();
+      s = u = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        s += slots[W + w];
+        u += slots[2 * W + w];
+      }
+    }
+  }
+};
+
 // A workgroup's part of a row, streamed: every thread keeps a run of its own.
 // Workgroup r * split + k takes part k of row r; with split = 1 it writes the
 // row's (M, S, H, logp), otherwise the runs of the parts.
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_row_stats(const typename T::Elem* __restrict__ x, long long stride,
-                                                        const void* __restrict__ targets, int bits, int classes,
-                                                        int split, RowOut out, float4* __restrict__ parts) {
-  __shared__ Run part[kThreads / 64];
+template <class T, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_row_stats(const typename T::Elem* __restrict__ x, long long stride,
+                                                       const void* __restrict__ targets, int bits, int classes,
+                                                       int split, RowOut out, float4* __restrict__ parts) {
+  __shared__ float slots[3 * (THREADS / 64)];
   const int k = blockIdx.x % unsigned(split);
   const long long r = blockIdx.x / unsigned(split);
   const long long t = target_of(targets, bits, r);
@@ -166,12 +203,13 @@ __global__ __launch_bounds__(kThreads) void k_row_stats(const typename T::Elem* 
     return;
   }
   const typename T::Elem* row = x + r * stride;
+  const float xt = split == 1 ? target_logit<T>(row, t, classes) : 0.f;
   Run run = empty_run();
   const Cut<T> cut(row, classes);
   int from, to;
   chunks_of(cut.full, split, k, from, to);
   const typename T::Elem* body = row + cut.head;
-  stream<kAhead>(from + threadIdx.x, to, kThreads, [&]<int N>(int c) { run = merge(run, run_of<T, N>(body, c, kThreads)); });
+  stream<kAhead>(from + threadIdx.x, to, THREADS, [&]<int N>(int c) { run = merge(run, run_of<T, N>(body, c, THREADS)); });
   if (k == split - 1 && int(threadIdx.x) < cut.extra) {
     const float v = T::one(row[cut.element(threadIdx.x)]);
     Run b = empty_run();
@@ -181,13 +219,13 @@ __global__ __launch_bounds__(kThreads) void k_row_stats(const typename T::Elem* 
     b.u = e * fmaxf(d, -1e30f);
     run = merge(run, b);
   }
-  run = merge_wave(run);
-  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = run;
-  __syncthreads();
+  Group<THREADS> group{slots};
+  const float m = group.max(run.m), d = below(run.m, m), f = exp_of(d);
+  float s = run.s * f, u = f * (run.u + d * run.s);
+  group.sum(s, u);
   if (threadIdx.x == 0) {
-    for (int w = 1; w < kThreads / 64; ++w) run = merge(run, part[w]);
-    if (split == 1) put_row(out, r, stat_of(run, target_logit<T>(row, t, classes)), 0.f, 0.f);
-    else parts[r * split + k] = make_float4(run.m, run.s, run.u, 0.f);
+    if (split == 1) put_row(out, r, stat_of(Run{m, s, u}, xt), 0.f, 0.f);
+    else parts[r * split + k] = make_float4(m, s, u, 0.f);
   }
 }
 
@@ -283,11 +321,9 @@ __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x
   typename T::Elem* out = grad + r * grad_stride;
   const typename T::Elem* row = x + r * stride;
   const float c = scale_host * (scale != nullptr ? *scale : 1.f);
-  float g = 0.f, h = 0.f;
-  if (t >= 0) {
-    g = grad_logp[r];
-    h = grad_entropy != nullptr ? grad_entropy[r] : 0.f;
-  }
+  const float4 st = stat[r];
+  float g = grad_logp[r], h = grad_entropy != nullptr ? grad_entropy[r] : 0.f;  // (asked for along with the target)
+  if (t < 0) g = h = 0.f;
   const Cut<T> cut(row, classes);
   int from, to;
   chunks_of(cut.full, split, k, from, to);
@@ -304,7 +340,6 @@ __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x
   }
   g *= c;
   h *= c;
-  const float4 st = stat[r];
   Slope sl = slope_of(st.x, st.y, st.z, g, h);
   if (t >= classes) sl.a = __builtin_nanf("");
   // the thread that writes the target's chunk writes the target again, with its g
@@ -457,74 +492,29 @@ __global__ __launch_bounds__(kWide) void k_policy_rows(PolicyArgs a, const typen
   }
 }
 
-// stats[i] = sum of partial[i][0 .. n - 1]: one workgroup.
+// stats[i] = factor times the sum of partial[i][0 .. n - 1]: one workgroup, two
+// waves a stat.  (A launch this small takes about as long as its instructions
+// take to be fetched: 50 ns for each 64 bytes of them.  So no lane handles more
+// than one stat, and the small kernels here keep their loops rolled.)
 template <int STATS>
-__global__ __launch_bounds__(kWide) void k_total(const float* __restrict__ partial, int n, float factor,
-                                                 float* __restrict__ stats) {
-  __shared__ float part[kWide / 64][STATS];
-  double sum[STATS] = {};
+__global__ __launch_bounds__(128 * STATS) void k_total(const float* __restrict__ partial, int n, float factor,
+                                                       float* __restrict__ stats) {
+  __shared__ float part[2 * STATS];
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
   typedef float Four __attribute__((ext_vector_type(4), aligned(4)));
-  const int quads = n / 4;
-#pragma unroll 2
-  for (int j = threadIdx.x; j < quads; j += kWide)
-#pragma unroll
-    for (int i = 0; i < STATS; ++i) {
-      const Four v = *reinterpret_cast<const Four*>(partial + (long long)i * n + 4 * j);
-      sum[i] += (double(v[0]) + double(v[1])) + (double(v[2]) + double(v[3]));
-    }
-  if (4 * quads + int(threadIdx.x) < n)
-#pragma unroll
-    for (int i = 0; i < STATS; ++i) sum[i] += double(partial[(long long)i * n + 4 * quads + threadIdx.x]);
-#pragma unroll
-  for (int i = 0; i < STATS; ++i) {
-    const float v = wave_sum(float(sum[i]));
-    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64][i] = v;
+  const float* p = partial + (long long)(wave / 2) * n;
+  const int quads = n / 4, me = wave % 2 * 64 + lane;
+  double sum = 4 * quads + me < n ? double(p[4 * quads + me]) : 0.0;
+#pragma unroll 8
+  for (int j = me; j < quads; j += 128) {
+    const Four v = reinterpret_cast<const Four*>(p)[j];
+    sum += double((v[0] + v[1]) + (v[2] + v[3]));
   }
+  const float v = wave_sum(float(sum));
+  if (lane == 0) part[wave] = v;
   __syncthreads();
-  if (threadIdx.x < STATS) {
-    double s = 0.0;
-#pragma unroll
-    for (int w = 0; w < kWide / 64; ++w) s += double(part[w][threadIdx.x]);
-    stats[threadIdx.x] = float(s * double(factor));
-  }
+  if (threadIdx.x < STATS) stats[threadIdx.x] = (part[2 * threadIdx.x] + part[2 * threadIdx.x + 1]) * factor;
 }
-
-// Workgroup over a row that THREADS lanes share: a wave (64), which needs no
-// barrier, or the workgroup.
-template <int THREADS>
-struct Group {
-  float* slots;  // 3 * THREADS / 64 floats of LDS
-  __device__ __forceinline__ float max(float v) {
-    v = wave_max(v);
-    if constexpr (THREADS > 64) {
-      if (threadIdx.x % 64 == 0) slots[threadIdx.x / 64] = v;
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < THREADS / 64; ++w) v = fmaxf(v, slots[w]);
-    }
-    return v;
-  }
-  // s and u over the group; the slots are those that max does not use, so that
-  // a barrier a call is enough (the next row's max comes after this one's barrier)
-  __device__ __forceinline__ void sum(float& s, float& u) {
-    s = wave_sum(s);
-    u = wave_sum(u);
-    if constexpr (THREADS > 64) {
-      constexpr int W = THREADS / 64;
-      if (threadIdx.x % 64 == 0) {
-        slots[W + threadIdx.x / 64] = s;
-        slots[2 * W + threadIdx.x / 64] = u;
-      }
-      __syncthreads();
-      s = u = 0.f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        s += slots[W + w];
-        u += slots[2 * W + w];
-      }
-    }
-  }
-};
 
 // The policy loss and its gradient in one pass over the logits: a row stays in
 // the registers of its THREADS lanes, NC chunks each, from its load to its
@@ -543,16 +533,25 @@ __global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(LONG ? 4 : f
   Group<THREADS> group{slots};
   const int lane = threadIdx.x % THREADS;
   const int sub = ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0;
+  // a row's target and weight, asked for while the last row (or the weights' sum) is worked on
+  long long target = -1;
+  float weight = 0.f;
+  auto head = [&](long long r) {
+    if (r >= a.rows) return;
+    target = target_of(a.targets, a.bits, r);
+    weight = a.weights != nullptr ? a.weights[r] : 1.f;
+  };
+  head((long long)blockIdx.x * ROWS + sub);
   const float norm = norm_of(a, weight_total(sums, groups));
   if (threadIdx.x < ROWS * kStats) (&acc[0][0])[threadIdx.x] = 0.0;
   __syncthreads();
   const unsigned at = unsigned(lane) * 16u;
   for (long long r = (long long)blockIdx.x * ROWS + sub; r < a.rows; r += (long long)gridDim.x * ROWS) {
-    const long long target = target_of(a.targets, a.bits, r);
     const int t = uniform(target < 0 ? -1 : target < classes ? int(target) : classes);
-    const float w = uniform(t < 0 ? 0.f : (a.weights != nullptr ? a.weights[r] : 1.f) * norm);
+    const float w = uniform(t < 0 ? 0.f : weight * norm);
     const typename T::Elem* row = x + r * stride;
     typename T::Elem* to = grad + r * grad_stride;
+    head(r + (long long)gridDim.x * ROWS);
     const Cut<T> cut(row, classes);
     const typename T::Elem* body = row + cut.head;
     typename T::Elem* to_body = to + cut.head;
@@ -658,165 +657,166 @@ __global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(LONG ? 4 : f
 }
 
 // The same for short rows (up to 4 chunks a lane of a wave): WAVES waves hold RPW
-// rows each, and one of them does the arithmetic of all rows, a lane for each.
-// Left to every wave for its own row, that arithmetic (three exponentials, two
-// logarithms, two quotients) is most of its work: 20000 rows of 257 bfloat16
-// classes took 33 us with a wave per row.
+// rows each in LDS, and one of them does the arithmetic of all rows, a lane for
+// each.  Left to every wave for its own row, that arithmetic (two exponentials,
+// two logarithms, three quotients) is most of its work: 20000 rows of 257
+// bfloat16 classes took 33 us with a wave per row.
 template <class T, int WAVES, int RPW, int NC>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(WAVES > 8 ? 4 : 5))) void k_policy_tile(
+__global__ __launch_bounds__(64 * WAVES) void k_policy_tile(
     PolicyArgs a, const typename T::Elem* x, long long stride, int classes, const double* __restrict__ sums, int groups,
     typename T::Elem* grad, long long grad_stride, RowOut out, float* __restrict__ partial) {
   constexpr int ROWS = WAVES * RPW;
-  __shared__ float4 stat[ROWS];   // M, S, U, x_t
-  __shared__ float slope[ROWS][3];
-  __shared__ double acc[kStats];
+  typedef typename T::Raw Slot __attribute__((aligned(16)));
+  __shared__ Slot held[ROWS][NC][64];
+  __shared__ float rest[ROWS][64];  // the element outside of the chunks that is a lane's
+  __shared__ float4 stat[ROWS];     // M, S, U, x_t
+  __shared__ float4 slope[ROWS];    // a, b, g
+  __shared__ int target[ROWS];      // -1: the row takes no part
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const unsigned at = unsigned(lane) * 16u;
   float norm = 1.f;
   if (gridDim.x > 1 && wave == 0) norm = norm_of(a, weight_total(sums, groups));
-  if (threadIdx.x < kStats) acc[threadIdx.x] = 0.0;
+  double acc = 0.0;  // lane i of wave 0: stat i
   for (long long base = (long long)blockIdx.x * ROWS; base < a.rows; base += (long long)gridDim.x * ROWS) {
-    typename T::Raw raw[RPW][NC];
-    float last[RPW], xt[RPW];
-    int t[RPW], full[RPW];
-    bool on[RPW];
-#pragma unroll
-    for (int q = 0; q < RPW; ++q) {
-      const long long r = base + wave * RPW + q;
-      t[q] = -1;
-      on[q] = false;
-      if (r < a.rows) {
-        const float weight = a.weights != nullptr ? a.weights[r] : 1.f;
-        const long long target = target_of(a.targets, a.bits, r);
-        t[q] = uniform(target < 0 ? -1 : target < classes ? int(target) : classes);
-        on[q] = t[q] >= 0 && uniform(weight) != 0.f;
-      }
-    }
-#pragma unroll
-    for (int q = 0; q < RPW; ++q) {
-      last[q] = kNegMax;
-      xt[q] = 0.f;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) raw[q][c] = typename T::Raw{};
-      const typename T::Elem* row = x + (base + wave * RPW + q) * stride;
-      const Cut<T> cut(row, classes);
-      full[q] = cut.full;
-      if (!on[q]) continue;
-      xt[q] = target_logit<T>(row, t[q], classes);
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-        if (c * 64 + lane < cut.full) raw[q][c] = load_chunk_at<T>(row + cut.head, c * 1024u, at);
-      if (lane < cut.extra) last[q] = T::one(row[cut.element(lane)]);
-    }
+    const int rows = a.rows - base < ROWS ? int(a.rows - base) : ROWS;
+    const int first = wave * RPW, last = min(first + RPW, rows);
     // what wave 0 needs of each row, asked for ahead of the rows' arithmetic
     const long long mine = base + lane;
     float w = 0.f, old = 0.f, adv = 0.f, ref = 0.f;
-    if (wave == 0 && lane < ROWS && mine < a.rows) {
+    if (wave == 0 && lane < rows) {
       w = weight_of(a, mine);
       old = a.old[mine];
       adv = a.advantages[mine];
       if (a.ref != nullptr) ref = a.ref[mine];
     }
-    // rows that take no part go through the same arithmetic on zeros: without a
-    // branch between them the rows' reductions overlap
-    float m[RPW], s[RPW], u[RPW];
+    // the wave's rows' targets, a lane for each
+    int own = -1;
+    if (first + lane < last) {
+      const float weight = a.weights != nullptr ? a.weights[base + first + lane] : 1.f;
+      const long long tt = target_of(a.targets, a.bits, base + first + lane);
+      if (tt >= 0 && weight != 0.f) own = tt < classes ? int(tt) : classes;
+    }
+    typename T::Raw raw[RPW][NC];
+    float extra[RPW];
 #pragma unroll
     for (int q = 0; q < RPW; ++q) {
-      m[q] = fmaxf(last[q], kNegMax);
+      // the one workgroup of a small call does not wait for the targets before it
+      // asks for the logits; what it gets of an idle row is not looked at
+      if (first + q < last && (WAVES > 8 || __builtin_amdgcn_readlane(own, q) >= 0)) {
+        const typename T::Elem* row = x + (base + first + q) * stride;
+        const Cut<T> cut(row, classes);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          if (c * 64 + lane < cut.full) raw[q][c] = load_chunk_at<T>(row + cut.head, c * 1024u, at);
+        if (lane < cut.extra) extra[q] = T::one(row[cut.element(lane)]);
+      }
+    }
+    if (first + lane < last) target[first + lane] = own;
+#pragma unroll
+    for (int q = 0; q < RPW; ++q) {
+      if (first + q >= last) continue;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) held[first + q][c][lane] = raw[q][c];
+      rest[first + q][lane] = extra[q];
+    }
+#pragma unroll 1
+    for (int i = first; i < last; ++i) {
+      const int t = uniform(target[i]);
+      if (t < 0) continue;
+      const typename T::Elem* row = x + (base + i) * stride;
+      const Cut<T> cut(row, classes);
+      const bool has_one = lane < cut.extra;
+      const float one = has_one ? rest[i][lane] : kNegMax;
+      const int tc = cut.chunk_of(t);
+      const typename T::Elem* held_row = reinterpret_cast<const typename T::Elem*>(held[i]);
+      const float xt = t >= classes ? __builtin_nanf("") : tc >= 0 ? T::one(held_row[t - cut.head]) : rest[i][cut.lane_of(t)];
+      typename T::Raw v[NC];
+      float m = fmaxf(one, kNegMax);
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const bool has = c * 64 + lane < full[q];
+        v[c] = held[i][c][lane];
+        if (c * 64 + lane < cut.full) {
 #pragma unroll
-        for (int i = 0; i < T::kPer; ++i) m[q] = fmaxf(m[q], has ? T::get(raw[q][c], i) : kNegMax);
+          for (int e = 0; e < T::kPer; ++e) m = fmaxf(m, T::get(v[c], e));
+        }
       }
-      m[q] = wave_max(m[q]);
-    }
-#pragma unroll
-    for (int q = 0; q < RPW; ++q) {
-      s[q] = u[q] = 0.f;
-      auto add = [&](float v, bool has) {
-        const float d = v - m[q], e = has ? exp_of(d) : 0.f;
-        s[q] += e;
-        u[q] += e * fmaxf(d, -1e30f);
+      m = wave_max(m);
+      float s = 0.f, u = 0.f;
+      auto add = [&](float z) {
+        const float d = z - m, e = exp_of(d);
+        s += e;
+        u += e * fmaxf(d, -1e30f);
       };
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const bool has = c * 64 + lane < full[q];
+      for (int c = 0; c < NC; ++c)
+        if (c * 64 + lane < cut.full) {
 #pragma unroll
-        for (int i = 0; i < T::kPer; ++i) add(T::get(raw[q][c], i), has);
-      }
-      add(last[q], lane < classes - full[q] * T::kPer);
-      s[q] = wave_sum(s[q]);
-      u[q] = wave_sum(u[q]);
-    }
-#pragma unroll
-    for (int q = 0; q < RPW; ++q) {
-      if (lane == 0) stat[wave * RPW + q] = make_float4(m[q], s[q], u[q], xt[q]);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(raw[q][c]));
+          for (int e = 0; e < T::kPer; ++e) add(T::get(v[c], e));
+        }
+      if (has_one) add(one);
+      s = wave_sum(s);
+      u = wave_sum(u);
+      if (lane == 0) stat[i] = make_float4(m, s, u, xt);
     }
     __syncthreads();
     if (wave == 0) {
-      const long long r = mine;
       if (gridDim.x == 1) {  // these are all rows
         double total = double(w);
-#pragma unroll
+#pragma unroll 1
         for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
         norm = norm_of(a, total);
       }
       w *= norm;
-      float4 st = make_float4(0.f, 1.f, 0.f, 0.f);
+      float4 st = make_float4(0.f, 1.f, 0.f, 0.f), sl = make_float4(0.f, 0.f, 0.f, 0.f);
       PolicyRow p{};
-      Slope sl{};
       if (w != 0.f) {
         const float4 z = stat[lane];
         st = stat_of(Run{z.x, z.y, z.z}, z.w);
         p = policy_row(a.p, w, st.w, st.z, old, adv, a.ref != nullptr, ref);
-        sl = slope_of(st.x, st.y, st.z, p.g * a.p.grad_scale, p.h * a.p.grad_scale);
+        const float g = p.g * a.p.grad_scale;
+        const Slope k = slope_of(st.x, st.y, st.z, g, p.h * a.p.grad_scale);
+        sl = make_float4(k.a, k.b, g, 0.f);
       }
-      if (lane < ROWS && r < a.rows) {
-        put_row(out, r, st, p.g, p.h);
-        slope[lane][0] = sl.a;
-        slope[lane][1] = sl.b;
-        slope[lane][2] = w != 0.f ? p.g * a.p.grad_scale : 0.f;
+      if (lane < rows) {
+        put_row(out, mine, st, p.g, p.h);
+        slope[lane] = sl;
+        if (w == 0.f) target[lane] = -1;
       }
 #pragma unroll
       for (int i = 0; i < kStats; ++i) {
         const float v = wave_sum(p.v[i]);
-        if (lane == 0) acc[i] += double(v);
+        if (lane == i) acc += double(v);
       }
     }
     __syncthreads();
-#pragma unroll
-    for (int q = 0; q < RPW; ++q) {
-      const long long r = base + wave * RPW + q;
-      if (r >= a.rows) continue;
-      const typename T::Elem* row = x + r * stride;
-      typename T::Elem* to = grad + r * grad_stride;
-      const Cut<T> cut(row, classes);
-      const int i0 = wave * RPW + q;
-      // a row that takes no part has a = b = g = 0 and zeros for logits: its gradient is 0
-      const Slope sl{on[q] ? uniform(stat[i0].x) : 0.f, uniform(slope[i0][0]), uniform(slope[i0][1])};
-      const float g = uniform(slope[i0][2]);
-      if (!on[q]) last[q] = 0.f;
+#pragma unroll 1
+    for (int i = first; i < last; ++i) {
+      const int t = uniform(target[i]);
+      typename T::Elem* to = grad + (base + i) * grad_stride;
+      const Cut<T> cut(x + (base + i) * stride, classes);
+      const float4 k = slope[i], z = stat[i];
+      const Slope sl{z.x, k.x, k.y};
+      // of a row that takes no part nothing but its length is looked at
 #pragma unroll
       for (int c = 0; c < NC; ++c)
         if (c * 64 + lane < cut.full) {
-          float y[T::kPer];
+          float y[T::kPer] = {};
+          if (t >= 0) {
+            const typename T::Raw v = held[i][c][lane];
 #pragma unroll
-          for (int i = 0; i < T::kPer; ++i) y[i] = slope_value(sl, T::get(raw[q][c], i));
+            for (int e = 0; e < T::kPer; ++e) y[e] = slope_value(sl, T::get(v, e));
+          }
           store_chunk_at<T>(to + cut.head, c * 1024u, at, T::pack(y));
         }
-      if (lane < cut.extra) to[cut.element(lane)] = T::to(slope_value(sl, last[q]));
-      if (on[q] && t[q] < classes) {
-        const int tc = cut.chunk_of(t[q]);
-        if ((tc >= 0 ? tc % 64 : cut.lane_of(t[q])) == lane) to[t[q]] = T::to(slope_value(sl, stat[i0].w) + g);
+      if (lane < cut.extra) to[cut.element(lane)] = T::to(t >= 0 ? slope_value(sl, rest[i][lane]) : 0.f);
+      if (t >= 0 && t < classes) {
+        const int tc = cut.chunk_of(t);
+        if ((tc >= 0 ? tc % 64 : cut.lane_of(t)) == lane) to[t] = T::to(slope_value(sl, z.w) + k.z);
       }
     }
-    __syncthreads();  // before the next tile's statistics
+    __syncthreads();  // before the next tile's rows
   }
-  __syncthreads();
-  if (threadIdx.x < kStats) partial[(long long)threadIdx.x * gridDim.x + blockIdx.x] = float(acc[threadIdx.x]);
+  if (wave == 0 && lane < kStats) partial[(long long)lane * gridDim.x + blockIdx.x] = float(acc);
 }
 
 // ----------------------------------------------------- the preference loss
@@ -825,9 +825,6 @@ __device__ __forceinline__ long long offset_of(const void* offsets, int bits, lo
                                  : (long long)static_cast<const int*>(offsets)[s];
   return o < 0 ? 0 : o > rows ? rows : o;
 }
-
-// log(1 + exp(z))
-__device__ __forceinline__ float softplus(float z) { return fmaxf(z, 0.f) + log1pf(expf(-fabsf(z))); }
 
 constexpr int kPairStats = 5;
 struct PairArgs {
@@ -843,8 +840,10 @@ __device__ __forceinline__ double excess(const PairArgs& a, const float4* __rest
                                          int lane, int n) {
   double v = 0.0;
 #pragma unroll 4
-  for (long long r = from + lane; r < to; r += n)
-    if (target_of(a.targets, a.bits, r) >= 0) v += double(stat[r].w) - double(a.ref[r]);
+  for (long long r = from + lane; r < to; r += n) {
+    const double d = double(stat[r].w) - double(a.ref[r]);  // (asked for along with the target)
+    v += target_of(a.targets, a.bits, r) >= 0 ? d : 0.0;
+  }
   return v;
 }
 
@@ -876,9 +875,12 @@ __global__ __launch_bounds__(WG) void k_pairs(PairArgs a, const float4* __restri
       v1 = total_of<WG>(v1, part);
     }
     const float good = float(a.beta * v0), bad = float(a.beta * v1), m = float(a.beta * (v0 - v1)), e = a.smoothing;
-    const float loss = (1.f - e) * softplus(-m) + e * softplus(m);
-    // a NaN margin is no win, and gives NaN slopes
-    const float slope = (e / (1.f + expf(-m)) - (1.f - e) / (1.f + expf(m))) * (a.beta / float(a.pairs));
+    // -log sigmoid(+-m) and sigmoid(+-m) out of one exponential, z = exp(-|m|) <= 1.
+    // A NaN margin is no win, and gives NaN slopes.
+    const float z = expf(-fabsf(m)), q = 1.f / (1.f + z);
+    const float loss = log1pf(z) + (m < 0.f ? -(1.f - e) * m : e * m);
+    const float up = m < 0.f ? z * q : q, down = m < 0.f ? q : z * q;
+    const float slope = (e * up - (1.f - e) * down) * (a.beta / float(a.pairs));
 #pragma unroll 4
     for (long long r = o0 + lane; r < o2; r += GROUP)
       if (target_of(a.targets, a.bits, r) >= 0) g[r] = r < o1 ? slope : -slope;
@@ -1007,9 +1009,16 @@ struct Logits {
 // Row statistics into `out`; rows in parts (split > 1) leave their parts only.
 int launch_stats(const Logits& l, int split, const RowOut& out, float4* parts, hipStream_t s) {
   with_type(l.dtype, [&]<class T>() {
-    hipLaunchKernelGGL(k_row_stats<T>, dim3(unsigned(l.rows * split)), dim3(kThreads), 0, s,
-                       static_cast<const typename T::Elem*>(l.x), (long long)l.stride, l.targets, l.bits, l.classes,
-                       split, out, parts);
+    auto go = [&](auto kernel, int threads) {
+      hipLaunchKernelGGL(kernel, dim3(unsigned(l.rows * split)), dim3(threads), 0, s,
+                         static_cast<const typename T::Elem*>(l.x), (long long)l.stride, l.targets, l.bits, l.classes,
+                         split, out, parts);
+    };
+    // as many lanes as ask for a part of a row in one or two rounds of kAhead chunks
+    // (20.7 k rows of 32768 bfloat16: 250 us with 256 lanes, 238 with 512)
+    const int64_t chunks = l.classes / T::kPer / split;
+    if (chunks > 2 * kAhead * kThreads) go(k_row_stats<T, 512>, 512);
+    else go(k_row_stats<T, kThreads>, kThreads);
   });
   return done();
 }
@@ -1132,7 +1141,7 @@ extern "C" int acdc_policy_loss(const void* logits, int32_t dtype, int64_t strid
     hipLaunchKernelGGL(k_weight_sums, dim3(unsigned(groups)), dim3(kThreads), 0, s, a, sums);
   };
   auto sum_stats = [&](unsigned blocks) {
-    hipLaunchKernelGGL(k_total<kStats>, dim3(1), dim3(kWide), 0, s, partial, int(blocks), 1.f, stats);
+    hipLaunchKernelGGL(k_total<kStats>, dim3(1), dim3(128 * kStats), 0, s, partial, int(blocks), 1.f, stats);
   };
 
   // Enough rows to fill the card, or rows of a wave each: one pass.
@@ -1244,7 +1253,7 @@ extern "C" int acdc_preference_loss(const void* logits, int32_t dtype, int64_t s
   } else {
     const unsigned blocks = unsigned(std::min<int64_t>(pairs, kMaxPartials));
     hipLaunchKernelGGL((k_pairs<kThreads, kThreads>), dim3(blocks), dim3(kThreads), 0, s, a, stat, grads, partial);
-    hipLaunchKernelGGL(k_total<kPairStats>, dim3(1), dim3(kWide), 0, s, partial, int(blocks), float(1.0 / double(pairs)),
+    hipLaunchKernelGGL(k_total<kPairStats>, dim3(1), dim3(128 * kPairStats), 0, s, partial, int(blocks), float(1.0 / double(pairs)),
                        stats);
   }
   rc = done();
