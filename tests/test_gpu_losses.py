@@ -392,3 +392,29 @@ def test_rows_past_32_bit_offsets(env):
     got = r.row_grads.double().cpu().numpy()[:, -3:]
     check_gradient(full[-3:], x.double().numpy(), tail, np.ones(3, bool), got[0], got[1], True)
     assert not full[-4].any() and not full[0].any()
+
+
+def test_wrong_arguments_on_the_gpu(env):
+    """What the native part of the binding does not take is refused as on the CPU."""
+    torch, losses = env
+    x, t, f = torch.zeros(4, 10, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, device="cuda")
+    saved, off = torch.zeros(4, 4, device="cuda"), torch.tensor([0, 2, 4], device="cuda")
+    for call in (lambda: losses.token_logprobs(x.double(), t), lambda: losses.token_logprobs(x, t[:3]),
+                 lambda: losses.token_logprobs(x, t.float()), lambda: losses.token_logprobs(x, t.cpu()),
+                 lambda: losses.token_logprobs(torch.zeros(10, 4, device="cuda").t(), t),
+                 lambda: losses.token_logprobs(x, t, workspace=torch.zeros(1, dtype=torch.uint8, device="cuda")),
+                 lambda: losses.token_logprobs_backward(x, t, saved[:3], f),
+                 lambda: losses.token_logprobs_backward(x, t, saved, f[:1].expand(4)),
+                 lambda: losses.token_logprobs_backward(x, t, saved, f, out=x.bfloat16()),
+                 lambda: losses.policy_loss(x, t, f, f.cpu()), lambda: losses.policy_loss(x, t, f, f, kl_coef=0.1),
+                 lambda: losses.policy_loss(x, t, f, f, clip=(-1, 0.2)), lambda: losses.policy_loss(x, t, f, f.double()),
+                 lambda: losses.preference_loss(x, t, off[:2], f), lambda: losses.preference_loss(x, t, off.float(), f),
+                 lambda: losses.preference_loss(x, t, off, f, label_smoothing=2.0)):
+        with pytest.raises(ValueError):
+            call()
+    from paper_1511_05946_amd.acdc import ACDCError
+    with pytest.raises(ACDCError, match="invalid argument"):   # memory that overlaps the logits': seen by the library
+        wide = torch.zeros(64, device="cuda")
+        losses.token_logprobs_backward(wide[:40].view(4, 10), t, saved, f, out=wide[2:42].view(4, 10))
+    with pytest.raises(ValueError):
+        losses.token_logprobs(x.cpu(), t.cpu())

@@ -278,3 +278,32 @@ def test_another_stream(env):
                 optim.adamw_step(one[0], one[1], one[2], step, grad_scale=clip[1:])
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(a[0], b[0]))
+
+
+def test_wrong_arguments_on_the_gpu(env):
+    """What the native part of the binding does not take is refused as on the CPU,
+    and leaves every tensor as it is."""
+    torch, optim = env
+    p, g = torch.ones(300, device="cuda"), torch.ones(300, device="cuda")
+    s32, s8 = optim.moments(p, 32), optim.moments(p, 8)
+    half = p.bfloat16()
+    for args, kw in ((([p], [g.cpu()], [s32]), {}), (([p], [g[:-1]], [s32]), {}), (([p], [None], [s32]), {}),
+                     (([p], [g[:1].expand(300)], [s32]), {}), (([p], [g], [s32[:1]]), {}), (([p], [g], [(s32[0], s8[1])]), {}),
+                     (([p], [g], [(*s8[:3], s8[3][:1])]), {}), (([p, p], [g], [s32]), {}), (([p], [g], [s32]), dict(lr=[1.0, 2.0])),
+                     (([p], [g], [s32]), dict(masters=[p])), (([half], [g], [s32]), dict(masters=[half])),
+                     (([p], [g], [s32]), dict(grad_scale=torch.ones(2, device="cuda"))),
+                     (([p], [g], [s32]), dict(grad_scale=torch.ones(1))), (([p.double()], [g], [s32]), {})):
+        with pytest.raises(ValueError):
+            optim.adamw_step(*args, 1, **kw)
+    from paper_1511_05946_amd.acdc import ACDCError
+    for kw in (dict(betas=(1.0, 0.999)), dict(eps=-1.0), dict(lr=float("nan"))):
+        with pytest.raises(ACDCError, match="invalid argument"):
+            optim.adamw_step([p], [g], [s32], 1, **kw)
+    with pytest.raises(ACDCError, match="invalid argument"):
+        optim.adamw_step([p], [g], [s32], 0)
+    assert (p == 1).all() and not s32[0].any()
+    for bad in ([g.cpu(), g], [g, g.cpu()], [g[::2]], [g.half()]):
+        with pytest.raises(ValueError):
+            optim.grad_norm(bad, max_norm=1.0)
+    with pytest.raises(ValueError):
+        optim.grad_norm([g], max_norm=-1.0)
