@@ -940,12 +940,15 @@ bool floats_ok(std::initializer_list<const void*> must, std::initializer_list<co
 }
 
 size_t up256(size_t b) { return (b + 255) & ~size_t(255); }
-// Workgroups that share a row.  One for each while the rows fill the card
-// (kFewRows of them do); with fewer, long rows are cut into parts of at least
-// 4096 values, up to about four workgroups a CU.
-constexpr int64_t kFewRows = 128;
-int split_of(int64_t rows, int32_t classes) {
-  if (rows < 1 || rows >= kFewRows) return 1;
+// Workgroups that share a row.  One, but for few long rows, which are cut into
+// parts of at least 4096 values, up to about four workgroups a CU.  Parts cost
+// a launch that joins them and a second pass over the logits: 80 rows of 20000
+// floats take 14 us whole and 20 in parts, 40 rows of 100000 24 and 25, 40 rows
+// of 200000 bfloat16 39 and 25; past the 256 KB that a CU's registers hold of a
+// row, 80 rows of 200000 41 and 30, 160 rows 44 and 45.
+int split_of(int64_t rows, int32_t classes, int32_t dtype) {
+  const int64_t few = int64_t(classes) * int64_t(dtype_bytes(dtype)) > 262144 ? 128 : 64;
+  if (rows < 1 || rows >= few) return 1;
   const int64_t parts = std::min<int64_t>({64, 1024 / rows, classes / 4096});
   return int(std::max<int64_t>(1, parts));
 }
@@ -963,7 +966,7 @@ constexpr double kKeepBytes = 128e6;
 struct Workspace {
   size_t stat, grads, parts, sums, partial, total;
 };
-Workspace layout(int64_t rows, int32_t classes, int64_t pairs) {
+Workspace layout(int64_t rows, int32_t classes, int32_t dtype, int64_t pairs) {
   Workspace w{};
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -971,7 +974,7 @@ Workspace layout(int64_t rows, int32_t classes, int64_t pairs) {
     at += up256(bytes);
     return o;
   };
-  const int split = split_of(rows, classes);
+  const int split = split_of(rows, classes, dtype);
   w.stat = take(size_t(rows) * sizeof(float4));
   w.grads = take(size_t(rows) * 2 * sizeof(float));
   w.parts = take(split > 1 ? size_t(rows) * split * sizeof(float4) : 0);
@@ -1024,7 +1027,7 @@ int launch_stats(const Logits& l, int split, const RowOut& out, float4* parts, h
 }
 // The same, joined where they came in parts.
 int launch_values(const Logits& l, const RowOut& out, float4* parts, hipStream_t s) {
-  const int split = split_of(l.rows, l.classes);
+  const int split = split_of(l.rows, l.classes, l.dtype);
   const int rc = launch_stats(l, split, out, parts, s);
   if (rc != ACDC_OK || split == 1) return rc;
   with_type(l.dtype, [&]<class T>() {
@@ -1037,7 +1040,7 @@ int launch_values(const Logits& l, const RowOut& out, float4* parts, hipStream_t
 }
 int launch_grad(const Logits& l, const float4* stat, const float* g, const float* h, const float* scale,
                 float scale_host, void* grad, int64_t grad_stride, hipStream_t s) {
-  const int split = split_of(l.rows, l.classes);
+  const int split = split_of(l.rows, l.classes, l.dtype);
   with_type(l.dtype, [&]<class T>() {
     hipLaunchKernelGGL(k_row_grad<T>, dim3(unsigned(l.rows * split)), dim3(kThreads), 0, s,
                        static_cast<const typename T::Elem*>(l.x), (long long)l.stride, l.targets, l.bits, l.classes,
@@ -1048,8 +1051,13 @@ int launch_grad(const Logits& l, const float4* stat, const float* g, const float
 }
 
 // f.template operator()<THREADS, NC, LONG>() for the fewest lanes and registers
-// that hold a row of `chunks` chunks; LONG where none do.
-template <class F>
+// that hold a row of `chunks` chunks; LONG where none do.  A workgroup of 1024
+// lanes has a CU for itself, so that nothing else runs while it loads or stores.
+// Rows of bfloat16, with twice the values to work on for each byte, are better
+// off with two workgroups of 512 and a part of the row read twice: 4096 rows of
+// 131072 take 438 us against 485, 3000 rows of 70000 185 against 224.  Rows of
+// floats are not: 2048 of 65536 216 against 205, 512 of 300000 341 against 288.
+template <class T, class F>
 void with_row_shape(int chunks, F&& f) {
   if (chunks <= 64) f.template operator()<64, 1, false>();
   else if (chunks <= 128) f.template operator()<64, 2, false>();
@@ -1060,6 +1068,7 @@ void with_row_shape(int chunks, F&& f) {
   else if (chunks <= 3072) f.template operator()<256, 12, false>();
   else if (chunks <= 4096) f.template operator()<256, 16, false>();
   else if (chunks <= 8192) f.template operator()<512, 16, false>();
+  else if constexpr (T::kPer == 8) f.template operator()<512, 12, true>();
   else if (chunks <= 16384) f.template operator()<1024, 16, false>();
   else f.template operator()<1024, 12, true>();
 }
@@ -1070,7 +1079,7 @@ void with_row_shape(int chunks, F&& f) {
 using namespace acdc;
 
 extern "C" size_t acdc_logprob_workspace_size(int64_t rows, int32_t classes, int32_t dtype) {
-  return sizes_ok(rows, classes, dtype) ? layout(rows, classes, 0).total : 0;
+  return sizes_ok(rows, classes, dtype) ? layout(rows, classes, dtype, 0).total : 0;
 }
 
 extern "C" int acdc_logprob_forward(const void* logits, int32_t dtype, int64_t stride, const void* targets,
@@ -1080,7 +1089,7 @@ extern "C" int acdc_logprob_forward(const void* logits, int32_t dtype, int64_t s
   if (!logits_ok(logits, dtype, stride, targets, target_bits, rows, classes, &rc)) return rc;
   if (rows == 0) return ACDC_OK;
   if (!floats_ok({logp}, {entropy}) || !aligned_to(saved, 16) || !aligned_to(workspace, 16)) return ACDC_ERR_INVALID_ARG;
-  const Workspace w = layout(rows, classes, 0);
+  const Workspace w = layout(rows, classes, dtype, 0);
   if (workspace == nullptr || workspace_bytes < w.total) return ACDC_ERR_WORKSPACE;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const Logits l{logits, dtype, stride, targets, target_bits, rows, classes};
@@ -1105,7 +1114,7 @@ extern "C" int acdc_logprob_backward(const void* logits, int32_t dtype, int64_t 
 }
 
 extern "C" size_t acdc_policy_workspace_size(int64_t rows, int32_t classes, int32_t dtype) {
-  return sizes_ok(rows, classes, dtype) ? layout(rows, classes, 0).total : 0;
+  return sizes_ok(rows, classes, dtype) ? layout(rows, classes, dtype, 0).total : 0;
 }
 
 extern "C" int acdc_policy_loss(const void* logits, int32_t dtype, int64_t stride, const void* targets,
@@ -1127,7 +1136,7 @@ extern "C" int acdc_policy_loss(const void* logits, int32_t dtype, int64_t strid
   if (rows > 0 && (logp_old == nullptr || advantages == nullptr || logp == nullptr)) return ACDC_ERR_INVALID_ARG;
   if (grad_logits != nullptr && !grad_ok(logits, stride, grad_logits, grad_stride, dtype, rows, classes))
     return ACDC_ERR_INVALID_ARG;
-  const Workspace w = layout(rows, classes, 0);
+  const Workspace w = layout(rows, classes, dtype, 0);
   if (w.total > 0 && (workspace == nullptr || workspace_bytes < w.total)) return ACDC_ERR_WORKSPACE;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
@@ -1145,10 +1154,10 @@ extern "C" int acdc_policy_loss(const void* logits, int32_t dtype, int64_t strid
   };
 
   // Enough rows to fill the card, or rows of a wave each: one pass.
-  const int split = split_of(rows, classes);
+  const int split = split_of(rows, classes, dtype);
   if (rows > 0 && grad_logits != nullptr && split == 1) {
     with_type(dtype, [&]<class T>() {
-      with_row_shape(classes / T::kPer, [&]<int THREADS, int NC, bool LONG>() {
+      with_row_shape<T>(classes / T::kPer, [&]<int THREADS, int NC, bool LONG>() {
         const RowOut out{logp, nullptr, reinterpret_cast<float4*>(saved), row_grads,
                          row_grads != nullptr ? row_grads + rows : nullptr};
         auto go = [&](auto kernel, unsigned blocks, int wg, float* to) {
@@ -1211,7 +1220,7 @@ extern "C" int acdc_policy_loss(const void* logits, int32_t dtype, int64_t strid
 
 extern "C" size_t acdc_preference_workspace_size(int64_t rows, int32_t classes, int32_t dtype, int64_t pairs) {
   if (!sizes_ok(rows, classes, dtype) || pairs < 0 || pairs > 0x3fffffff) return 0;
-  return layout(rows, classes, pairs).total;
+  return layout(rows, classes, dtype, pairs).total;
 }
 
 extern "C" int acdc_preference_loss(const void* logits, int32_t dtype, int64_t stride, const void* targets,
@@ -1233,7 +1242,7 @@ extern "C" int acdc_preference_loss(const void* logits, int32_t dtype, int64_t s
   if (rows > 0 && (logp_ref == nullptr || logp == nullptr)) return ACDC_ERR_INVALID_ARG;
   if (grad_logits != nullptr && !grad_ok(logits, stride, grad_logits, grad_stride, dtype, rows, classes))
     return ACDC_ERR_INVALID_ARG;
-  const Workspace w = layout(rows, classes, pairs);
+  const Workspace w = layout(rows, classes, dtype, pairs);
   if (w.total > 0 && (workspace == nullptr || workspace_bytes < w.total)) return ACDC_ERR_WORKSPACE;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
