@@ -5,8 +5,8 @@
 // the scales of 8-bit moments, one per 256 elements: the block's maximum has
 // to be known before its first code is written.
 //
-// A launch takes up to kBatch tensors, whose addresses travel in the kernel's
-// arguments: nothing is uploaded, and no table outlives the call.
+// The tensors' addresses travel in the kernels' arguments, 62 to 104 tensors a
+// launch: nothing is uploaded, and no table outlives the call.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -17,26 +17,33 @@ namespace acdc {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBatch = 48;      // tensors a launch: their records fill the 4 KB of kernel arguments
 constexpr int kBlock = 256;     // elements that share a scale: 4 of each lane of a wave
 constexpr int kChunk = kThreads * 4;  // elements a workgroup: four a thread, and no loop
 constexpr float kPerTop = 1.f / 448.f;  // 448: largest e4m3 value
 constexpr float kTiny = 0x1p-9f;  // smallest positive one
 
-struct Tensor {
-  void* param;
-  float* master;
-  const void* grad;
-  void *m, *v;
-  float *m_scale, *v_scale;
-  long long n;
+// A tensor is a few words of an address each, below 2^48, with 16 bits of
+// something else on top: its length in the first three, the index of its rate
+// in the fourth.  More tensors fit a launch's arguments that way, and fewer
+// launches drain and fill the card: 300 tensors, 560 MB, took 118 us with 48
+// whole records a launch.
+//   0 param | n, 1 grad | n, 2 m | n, 3 v | rate, then m_scale and v_scale (8 bits), master
+constexpr int kArguments = 3840;  // bytes, of the 4 KB that a launch has
+constexpr int kRates = 8;
+struct Rate {
   float rate, decay;  // lr / (1 - beta1^step), 1 - lr * weight_decay
 };
+template <int WORDS>
 struct Batch {
-  int first[kBatch];  // first workgroup of each tensor; unused entries are INT_MAX
-  Tensor t[kBatch];
+  static constexpr int kMost = int((kArguments - kRates * sizeof(Rate)) / (4 + 8 * WORDS));
+  unsigned long long word[kMost][WORDS];
+  Rate rate[kRates];
+  int first[kMost];  // first workgroup of each tensor
 };
-static_assert(sizeof(Batch) <= 3840, "kernel arguments");
+constexpr int words_of(int bits, bool master) { return 4 + (bits == 8 ? 2 : 0) + (master ? 1 : 0); }
+static_assert(sizeof(Batch<4>) <= kArguments && sizeof(Batch<5>) <= kArguments && sizeof(Batch<6>) <= kArguments &&
+              sizeof(Batch<7>) <= kArguments);
+constexpr unsigned long long kAddress = (1ull << 48) - 1;
 
 struct Step {
   double one1, one2;      // 1 - beta
@@ -137,9 +144,33 @@ __device__ __forceinline__ float scale_of(const float (&v)[4]) {
 }
 
 template <class P, class G, int BITS, bool MASTER, bool NT>
-__global__ __launch_bounds__(kThreads) void k_adamw(Batch b, int count, Step s) {
+__global__ __launch_bounds__(kThreads) void k_adamw(Batch<words_of(BITS, MASTER)> b, int count, Step s) {
   const int i = tensor_of(b.first, count, blockIdx.x);
-  const Tensor& t = b.t[i];
+  const auto& word = b.word[i];
+  // (named as global memory: of a pointer made out of a number the compiler would not know)
+  auto address = [&](int k) {
+    return (void*)reinterpret_cast<__attribute__((address_space(1))) void*>(word[k] & kAddress);
+  };
+  struct {
+    void *param, *grad, *m, *v;
+    float *m_scale, *v_scale;
+    void* master;
+    long long n;
+    float rate, decay;
+  } t;
+  t.param = address(0);
+  t.grad = address(1);
+  t.m = address(2);
+  t.v = address(3);
+  if constexpr (BITS == 8) {
+    t.m_scale = static_cast<float*>(address(4));
+    t.v_scale = static_cast<float*>(address(5));
+  }
+  if constexpr (MASTER) t.master = address(words_of(BITS, MASTER) - 1);
+  t.n = (long long)(word[0] >> 48 | word[1] >> 48 << 16 | word[2] >> 48 << 32);
+  const Rate rate = b.rate[word[3] >> 48];
+  t.rate = rate.rate;
+  t.decay = rate.decay;
   const float gs = s.grad_scale != nullptr ? *s.grad_scale : 1.f;
   if (!(gs - gs == 0.f)) return;
   // the gradient's scale goes into the factors of g and g^2, each rounded once
@@ -305,15 +336,12 @@ constexpr int kClasses = 16;
 // ones with masters 775 instead of 900; without it 80 MB took 23 instead of 26.)
 constexpr double kKeepBytes = 128e6;
 
-void launch_class(int cls, bool nt, const Batch& b, int count, long long blocks, const Step& s, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>(blocks)), block(kThreads);
-  auto hint = [&]<class P, class G, int BITS, bool MASTER>() {
-    if (nt) hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, true>), grid, block, 0, stream, b, count, s);
-    else hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, false>), grid, block, 0, stream, b, count, s);
-  };
+// f.template operator()<P, G, BITS, MASTER>() for a class.
+template <class F>
+void with_class(int cls, F&& f) {
   auto moments = [&]<class P, class G, bool MASTER>() {
-    if (cls & 2) hint.template operator()<P, G, 8, MASTER>();
-    else hint.template operator()<P, G, 32, MASTER>();
+    if (cls & 2) f.template operator()<P, G, 8, MASTER>();
+    else f.template operator()<P, G, 32, MASTER>();
   };
   auto grads = [&]<class P, bool MASTER>() {
     if (cls & 4) moments.template operator()<P, BF16, MASTER>();
@@ -323,6 +351,8 @@ void launch_class(int cls, bool nt, const Batch& b, int count, long long blocks,
   else if (cls & 1) grads.template operator()<BF16, true>();
   else grads.template operator()<BF16, false>();
 }
+
+bool low48(const void* p) { return reinterpret_cast<uintptr_t>(p) <= kAddress; }
 
 bool tensor_ok(const acdc_adamw_tensor& t) {
   const size_t pb = dtype_bytes(t.param_type), gb = dtype_bytes(t.grad_type);
@@ -334,6 +364,9 @@ bool tensor_ok(const acdc_adamw_tensor& t) {
   const size_t mb = t.m_scale != nullptr ? 1 : 4;
   if (t.param == nullptr || t.grad == nullptr || t.m == nullptr || t.v == nullptr) return false;
   if (t.param == t.grad || t.m == t.v || t.m == t.param || t.v == t.param || t.master == t.param) return false;
+  if (!low48(t.param) || !low48(t.grad) || !low48(t.m) || !low48(t.v) || !low48(t.m_scale) || !low48(t.v_scale) ||
+      !low48(t.master))
+    return false;
   return aligned_to(t.param, pb) && aligned_to(t.grad, gb) && aligned_to(t.master, 4) && aligned_to(t.m, mb) &&
          aligned_to(t.v, mb) && aligned_to(t.m_scale, 4) && aligned_to(t.v_scale, 4);
 }
@@ -362,36 +395,57 @@ extern "C" int acdc_adamw_step(const acdc_adamw_tensor* tensors, int32_t count, 
     bytes += double(t.n) * double(dtype_bytes(t.param_type) + dtype_bytes(t.grad_type) + (t.master != nullptr ? 4 : 0) +
                                   (t.m_scale != nullptr ? 2 : 8));
   }
-  for (int cls = 0; cls < kClasses; ++cls) {
+  int rc = ACDC_OK;
+  for (int cls = 0; cls < kClasses && rc == ACDC_OK; ++cls) {
     if (!(seen >> cls & 1)) continue;
-    Batch b;
-    int used = 0;
-    long long blocks = 0;
-    auto flush = [&]() -> int {
-      if (used == 0) return ACDC_OK;
-      launch_class(cls, bytes >= kKeepBytes, b, used, blocks, s, st);
-      used = 0;
-      blocks = 0;
-      return done();
-    };
-    for (int32_t i = 0; i < count; ++i) {
-      const acdc_adamw_tensor& t = tensors[i];
-      if (t.n == 0 || class_of(t) != cls) continue;
-      const long long need = (t.n + kChunk - 1) / kChunk;
-      if (used == kBatch || blocks + need > kMaxBlocks) {
-        const int rc = flush();
-        if (rc != ACDC_OK) return rc;
+    with_class(cls, [&]<class P, class G, int BITS, bool MASTER>() {
+      Batch<words_of(BITS, MASTER)> b;
+      int used = 0, rates = 0;
+      long long blocks = 0;
+      auto flush = [&] {
+        if (used == 0 || rc != ACDC_OK) return;
+        const dim3 grid(static_cast<unsigned>(blocks)), block(kThreads);
+        if (bytes >= kKeepBytes) hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, true>), grid, block, 0, st, b, used, s);
+        else hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, false>), grid, block, 0, st, b, used, s);
+        used = rates = 0;
+        blocks = 0;
+        rc = done();
+      };
+      for (int32_t i = 0; i < count; ++i) {
+        const acdc_adamw_tensor& t = tensors[i];
+        if (t.n == 0 || class_of(t) != cls) continue;
+        const Rate rate{float(double(t.lr) / c1), float(1.0 - double(t.lr) * double(t.weight_decay))};
+        const long long need = (t.n + kChunk - 1) / kChunk;
+        int k = 0;
+        while (k < rates && !(b.rate[k].rate == rate.rate && b.rate[k].decay == rate.decay)) ++k;
+        if (used == b.kMost || blocks + need > kMaxBlocks || k == kRates) {
+          flush();
+          if (rc != ACDC_OK) return;
+          k = 0;
+        }
+        if (k == rates) b.rate[rates++] = rate;
+        const unsigned long long n = (unsigned long long)t.n;
+        auto word = [](const void* p, unsigned long long top) {
+          return (unsigned long long)reinterpret_cast<uintptr_t>(p) | top << 48;
+        };
+        auto& w = b.word[used];
+        w[0] = word(t.param, n & 0xffff);
+        w[1] = word(t.grad, n >> 16 & 0xffff);
+        w[2] = word(t.m, n >> 32);
+        w[3] = word(t.v, (unsigned long long)k);
+        if constexpr (BITS == 8) {
+          w[4] = word(t.m_scale, 0);
+          w[5] = word(t.v_scale, 0);
+        }
+        if constexpr (MASTER) w[words_of(BITS, MASTER) - 1] = word(t.master, 0);
+        b.first[used] = int(blocks);
+        ++used;
+        blocks += need;
       }
-      b.first[used] = int(blocks);
-      b.t[used] = Tensor{t.param, t.master, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.n,
-                         float(double(t.lr) / c1), float(1.0 - double(t.lr) * double(t.weight_decay))};
-      ++used;
-      blocks += need;
-    }
-    const int rc = flush();
-    if (rc != ACDC_OK) return rc;
+      flush();
+    });
   }
-  return ACDC_OK;
+  return rc;
 }
 
 static long long norm_blocks(const int64_t* sizes, int32_t count) {
