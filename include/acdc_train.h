@@ -111,7 +111,7 @@ size_t acdc_preference_workspace_size(int64_t rows, int32_t classes, int32_t dty
 
 /* ---------------------------------------------------------- the optimiser */
 
-/* One tensor of an AdamW step: n contiguous elements (n = 0 is allowed).
+/* One tensor of an AdamW step: n contiguous elements (0 <= n < 2^34 - 1024).
  * Moments in 32 bits (m_scale = v_scale = null): m and v are float [n].
  * Moments in 8 bits: m and v are codes, uint8 [n], each an OCP e4m3 value q;
  * elements 256 b .. 256 b + 255 share the scales m_scale[b] and v_scale[b]

@@ -344,7 +344,8 @@ PyObject* adamw(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Numbers lr(args[4], count), decay(args[5], count);
     if (masters.count != count || !lr.ok || !decay.ok) Py_RETURN_NONE;
     const double beta1 = a.number(6), beta2 = a.number(7), eps = a.number(8);
-    const long long step = PyLong_Check(args[9]) ? PyLong_AsLongLong(args[9]) : -1;
+    if (!PyLong_Check(args[9])) Py_RETURN_NONE;
+    const long long step = PyLong_AsLongLong(args[9]);
     const Tensor* scale = a.may(10);
     const acdc_stream_t stream = a.stream(11);
     if (PyErr_Occurred()) {

@@ -188,44 +188,48 @@ struct Group {
 };
 
 // A workgroup's part of a row, streamed: every thread keeps a run of its own.
-// Workgroup r * split + k takes part k of row r; with split = 1 it writes the
-// row's (M, S, H, logp), otherwise the runs of the parts.
+// Item r * split + k is part k of row r; with split = 1 its workgroup writes the
+// row's (M, S, H, logp), otherwise the runs of the parts.  Bound by HBM: 20.7 k
+// rows of 32768 bfloat16, 1.36 GB, in 238 us (5.7 TB/s).
 template <class T, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_row_stats(const typename T::Elem* __restrict__ x, long long stride,
                                                        const void* __restrict__ targets, int bits, int classes,
-                                                       int split, RowOut out, float4* __restrict__ parts) {
+                                                       int split, unsigned items, RowOut out,
+                                                       float4* __restrict__ parts) {
   __shared__ float slots[3 * (THREADS / 64)];
-  const int k = blockIdx.x % unsigned(split);
-  const long long r = blockIdx.x / unsigned(split);
-  const long long t = target_of(targets, bits, r);
-  if (t < 0) {
-    if (threadIdx.x == 0 && k == 0) put_row(out, r, make_float4(0.f, 1.f, 0.f, 0.f), 0.f, 0.f);
-    return;
-  }
-  const typename T::Elem* row = x + r * stride;
-  const float xt = split == 1 ? target_logit<T>(row, t, classes) : 0.f;
-  Run run = empty_run();
-  const Cut<T> cut(row, classes);
-  int from, to;
-  chunks_of(cut.full, split, k, from, to);
-  const typename T::Elem* body = row + cut.head;
-  stream<kAhead>(from + threadIdx.x, to, THREADS, [&]<int N>(int c) { run = merge(run, run_of<T, N>(body, c, THREADS)); });
-  if (k == split - 1 && int(threadIdx.x) < cut.extra) {
-    const float v = T::one(row[cut.element(threadIdx.x)]);
-    Run b = empty_run();
-    b.m = fmaxf(b.m, v);
-    const float d = v - b.m, e = exp_of(d);
-    b.s = e;
-    b.u = e * fmaxf(d, -1e30f);
-    run = merge(run, b);
-  }
   Group<THREADS> group{slots};
-  const float m = group.max(run.m), d = below(run.m, m), f = exp_of(d);
-  float s = run.s * f, u = f * (run.u + d * run.s);
-  group.sum(s, u);
-  if (threadIdx.x == 0) {
-    if (split == 1) put_row(out, r, stat_of(Run{m, s, u}, xt), 0.f, 0.f);
-    else parts[r * split + k] = make_float4(m, s, u, 0.f);
+  for (unsigned item = blockIdx.x; item < items; item += gridDim.x) {
+    const int k = item % unsigned(split);
+    const long long r = item / unsigned(split);
+    const long long t = target_of(targets, bits, r);
+    if (t < 0) {
+      if (threadIdx.x == 0 && k == 0) put_row(out, r, make_float4(0.f, 1.f, 0.f, 0.f), 0.f, 0.f);
+      continue;
+    }
+    const typename T::Elem* row = x + r * stride;
+    const float xt = split == 1 ? target_logit<T>(row, t, classes) : 0.f;
+    Run run = empty_run();
+    const Cut<T> cut(row, classes);
+    int from, to;
+    chunks_of(cut.full, split, k, from, to);
+    const typename T::Elem* body = row + cut.head;
+    stream<kAhead>(from + threadIdx.x, to, THREADS, [&]<int N>(int c) { run = merge(run, run_of<T, N>(body, c, THREADS)); });
+    if (k == split - 1 && int(threadIdx.x) < cut.extra) {
+      const float v = T::one(row[cut.element(threadIdx.x)]);
+      Run b = empty_run();
+      b.m = fmaxf(b.m, v);
+      const float d = v - b.m, e = exp_of(d);
+      b.s = e;
+      b.u = e * fmaxf(d, -1e30f);
+      run = merge(run, b);
+    }
+    const float m = group.max(run.m), d = below(run.m, m), f = exp_of(d);
+    float s = run.s * f, u = f * (run.u + d * run.s);
+    group.sum(s, u);
+    if (threadIdx.x == 0) {
+      if (split == 1) put_row(out, r, stat_of(Run{m, s, u}, xt), 0.f, 0.f);
+      else parts[r * split + k] = make_float4(m, s, u, 0.f);
+    }
   }
 }
 
@@ -303,9 +307,10 @@ __device__ __forceinline__ void slopes(const Slope& sl, const typename T::Elem* 
   }
 }
 
-// dL/dlogits from each row's (M, S, H, logp), g and h; workgroups as in
-// k_row_stats, the last rows first: what a forward read last is what the cache
-// still holds.
+// dL/dlogits from each row's (M, S, H, logp), g and h; items as in k_row_stats,
+// the last rows first: what a forward read last is what the cache still holds.
+// Bound by HBM: 27.6 k rows of 32768 bfloat16, a quarter of them idle, read 1.36
+// and write 1.81 GB in 515 us (6.1 TB/s).
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x, long long stride,
                                                        const void* __restrict__ targets, int bits, int classes,
@@ -313,46 +318,49 @@ __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x
                                                        const float* __restrict__ grad_logp,
                                                        const float* __restrict__ grad_entropy,
                                                        const float* __restrict__ scale, float scale_host,
-                                                       typename T::Elem* grad, long long grad_stride, int split) {
-  const unsigned at = gridDim.x - 1 - blockIdx.x;
-  const int k = at % unsigned(split);
-  const long long r = at / unsigned(split);
-  const long long t = target_of(targets, bits, r);
-  typename T::Elem* out = grad + r * grad_stride;
-  const typename T::Elem* row = x + r * stride;
-  const float c = scale_host * (scale != nullptr ? *scale : 1.f);
-  const float4 st = stat[r];
-  float g = grad_logp[r], h = grad_entropy != nullptr ? grad_entropy[r] : 0.f;  // (asked for along with the target)
-  if (t < 0) g = h = 0.f;
-  const Cut<T> cut(row, classes);
-  int from, to;
-  chunks_of(cut.full, split, k, from, to);
-  const int one = cut.element(threadIdx.x);
-  const bool has_one = k == split - 1 && int(threadIdx.x) < cut.extra;
-  const typename T::Elem* body = row + cut.head;
-  typename T::Elem* out_body = out + cut.head;
-  if (g == 0.f && h == 0.f) {
-    float zero[T::kPer] = {};
-    for (int i = from + threadIdx.x; i < to; i += kThreads)
-      store_chunk<T>(out_body + (long long)i * T::kPer, T::pack(zero));
-    if (has_one) out[one] = T::to(0.f);
-    return;
+                                                       typename T::Elem* grad, long long grad_stride, int split,
+                                                       unsigned items) {
+  for (unsigned item = blockIdx.x; item < items; item += gridDim.x) {
+    const unsigned at = items - 1 - item;
+    const int k = at % unsigned(split);
+    const long long r = at / unsigned(split);
+    const long long t = target_of(targets, bits, r);
+    typename T::Elem* out = grad + r * grad_stride;
+    const typename T::Elem* row = x + r * stride;
+    const float c = scale_host * (scale != nullptr ? *scale : 1.f);
+    const float4 st = stat[r];
+    float g = grad_logp[r], h = grad_entropy != nullptr ? grad_entropy[r] : 0.f;  // (asked for along with the target)
+    if (t < 0) g = h = 0.f;
+    const Cut<T> cut(row, classes);
+    int from, to;
+    chunks_of(cut.full, split, k, from, to);
+    const int one = cut.element(threadIdx.x);
+    const bool has_one = k == split - 1 && int(threadIdx.x) < cut.extra;
+    const typename T::Elem* body = row + cut.head;
+    typename T::Elem* out_body = out + cut.head;
+    if (g == 0.f && h == 0.f) {
+      float zero[T::kPer] = {};
+      for (int i = from + threadIdx.x; i < to; i += kThreads)
+        store_chunk<T>(out_body + (long long)i * T::kPer, T::pack(zero));
+      if (has_one) out[one] = T::to(0.f);
+      continue;
+    }
+    g *= c;
+    h *= c;
+    Slope sl = slope_of(st.x, st.y, st.z, g, h);
+    if (t >= classes) sl.a = __builtin_nanf("");
+    // the thread that writes the target's chunk writes the target again, with its g
+    bool mine = false;
+    if (t < classes) {
+      const int tc = cut.chunk_of(int(t));
+      mine = tc >= 0 ? tc >= from && tc < to && (tc - from) % kThreads == int(threadIdx.x)
+                     : has_one && cut.lane_of(int(t)) == int(threadIdx.x);
+    }
+    const float yt = mine ? slope_value(sl, T::one(row[t])) + g : 0.f;
+    stream<kAhead>(from + threadIdx.x, to, kThreads, [&]<int N>(int i) { slopes<T, N>(sl, body, out_body, i, kThreads); });
+    if (has_one) out[one] = T::to(slope_value(sl, T::one(row[one])));
+    if (mine) out[t] = T::to(yt);
   }
-  g *= c;
-  h *= c;
-  Slope sl = slope_of(st.x, st.y, st.z, g, h);
-  if (t >= classes) sl.a = __builtin_nanf("");
-  // the thread that writes the target's chunk writes the target again, with its g
-  bool mine = false;
-  if (t < classes) {
-    const int tc = cut.chunk_of(int(t));
-    mine = tc >= 0 ? tc >= from && tc < to && (tc - from) % kThreads == int(threadIdx.x)
-                   : has_one && cut.lane_of(int(t)) == int(threadIdx.x);
-  }
-  const float yt = mine ? slope_value(sl, T::one(row[t])) + g : 0.f;
-  stream<kAhead>(from + threadIdx.x, to, kThreads, [&]<int N>(int i) { slopes<T, N>(sl, body, out_body, i, kThreads); });
-  if (has_one) out[one] = T::to(slope_value(sl, T::one(row[one])));
-  if (mine) out[t] = T::to(yt);
 }
 
 // Sum of v over the workgroup in a fixed order, for every thread.
@@ -444,9 +452,10 @@ __device__ __forceinline__ double weight_total(const double* __restrict__ sums, 
 
 // The policy loss of rows whose statistics stand in `stat` (in parts of
 // `split`, where that is more than 1): one thread per row, or a wave for each
-// of up to 16 rows in parts.  With one workgroup it sums the weights and writes the stats itself;
-// with more, `sums` holds the weights' sums and `partial` gets each
-// workgroup's stats.
+// of up to 16 rows in parts.  With one workgroup it sums the weights and writes
+// the stats itself; with more, `sums` holds the weights' sums and `partial` gets
+// each workgroup's stats.  A few us of latency: what it reads is nothing beside
+// the logits.
 template <class T>
 __global__ __launch_bounds__(kWide) void k_policy_rows(PolicyArgs a, const typename T::Elem* __restrict__ x,
                                                        long long stride, int classes, const float4* __restrict__ parts,
@@ -522,6 +531,14 @@ __global__ __launch_bounds__(128 * STATS) void k_total(const float* __restrict__
 // its rows' stats go into partial[.][blockIdx].  LONG: what the registers do
 // not hold of a row is streamed for the statistics and read again (out of the
 // Infinity Cache, which a row a CU fits) for the gradient.
+//
+// Bound by HBM, each logit read once and its gradient written once: 8192 rows of
+// 4096 floats, 246 MB, in 47 us (5.2 TB/s), of 65536 bfloat16, 2.04 GB, in 380
+// us (5.4 TB/s); statistics and gradient as two passes took 61 and 640 us.  The
+// vector unit has room for it: about 22 instructions a value against 30 that fit
+// a bfloat16's 4 bytes at 5 TB/s.  So many chunks a lane as a row needs, that
+// the loads of a whole row are in flight together; several workgroups a CU, so
+// that one loads while another stores.
 constexpr int fused_waves(int nc) { return nc <= 4 ? 8 : nc <= 8 ? 6 : nc <= 12 ? 5 : 4; }
 template <class T, int WG, int THREADS, int NC, bool LONG, bool NT>
 __global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(LONG ? 4 : fused_waves(NC)))) void k_policy_fused(
@@ -1009,13 +1026,17 @@ struct Logits {
   int32_t classes;
 };
 
+// Workgroups of a launch over `items`: a grid holds fewer than 2^32 lanes.
+unsigned grid_for(unsigned items) { return std::min(items, 1u << 22); }
+
 // Row statistics into `out`; rows in parts (split > 1) leave their parts only.
 int launch_stats(const Logits& l, int split, const RowOut& out, float4* parts, hipStream_t s) {
   with_type(l.dtype, [&]<class T>() {
     auto go = [&](auto kernel, int threads) {
-      hipLaunchKernelGGL(kernel, dim3(unsigned(l.rows * split)), dim3(threads), 0, s,
+      const unsigned items = unsigned(l.rows * split);
+      hipLaunchKernelGGL(kernel, dim3(grid_for(items)), dim3(threads), 0, s,
                          static_cast<const typename T::Elem*>(l.x), (long long)l.stride, l.targets, l.bits, l.classes,
-                         split, out, parts);
+                         split, items, out, parts);
     };
     // as many lanes as ask for a part of a row in one or two rounds of kAhead chunks
     // (20.7 k rows of 32768 bfloat16: 250 us with 256 lanes, 238 with 512)
@@ -1042,10 +1063,11 @@ int launch_grad(const Logits& l, const float4* stat, const float* g, const float
                 float scale_host, void* grad, int64_t grad_stride, hipStream_t s) {
   const int split = split_of(l.rows, l.classes, l.dtype);
   with_type(l.dtype, [&]<class T>() {
-    hipLaunchKernelGGL(k_row_grad<T>, dim3(unsigned(l.rows * split)), dim3(kThreads), 0, s,
+    const unsigned items = unsigned(l.rows * split);
+    hipLaunchKernelGGL(k_row_grad<T>, dim3(grid_for(items)), dim3(kThreads), 0, s,
                        static_cast<const typename T::Elem*>(l.x), (long long)l.stride, l.targets, l.bits, l.classes,
                        stat, g, h, scale, scale_host, static_cast<typename T::Elem*>(grad), (long long)grad_stride,
-                       split);
+                       split, items);
   });
   return done();
 }

@@ -418,3 +418,25 @@ def test_wrong_arguments_on_the_gpu(env):
         losses.token_logprobs_backward(wide[:40].view(4, 10), t, saved, f, out=wide[2:42].view(4, 10))
     with pytest.raises(ValueError):
         losses.token_logprobs(x.cpu(), t.cpu())
+
+
+def test_more_rows_than_a_grid_has_workgroups(env):
+    """Over 2^22 rows: the streaming kernels take several each."""
+    torch, losses = env
+    rows, V = (1 << 22) + 1000, 8
+    print(f"[case] {rows} x {V}", flush=True)
+    x = 2 * torch.randn(rows, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    t = torch.arange(rows, device="cuda") % V
+    t[::7] = -1
+    r = losses.token_logprobs(x, t, entropy=True, save=True)
+    g = torch.ones(rows, device="cuda")
+    grad = losses.token_logprobs_backward(x, t, r.saved, g)
+    pick = torch.cat([torch.arange(2000), torch.arange(rows - 3000, rows)])
+    xs, ts = x.cpu()[pick].double().numpy(), t.cpu()[pick].numpy()
+    on = ts >= 0
+    p, logp, ent, spread = R.rows(xs, np.clip(ts, 0, None))
+    close(r.logp[pick.cuda()], np.where(on, logp, 0.0), R.logp_tolerance(logp, spread), "logp")
+    check_gradient(grad[pick.cuda()], xs, ts, on, np.ones(len(ts)), np.zeros(len(ts)), False)
+    q = losses.policy_loss(x, t, r.logp, g, grad=False)
+    # every ratio is 1 and every advantage 1
+    assert q.stats[:2].tolist() == pytest.approx([-1.0, -1.0], rel=1e-6) and q.stats[5].item() == pytest.approx(1.0, rel=1e-6)

@@ -307,3 +307,13 @@ def test_wrong_arguments_on_the_gpu(env):
             optim.grad_norm(bad, max_norm=1.0)
     with pytest.raises(ValueError):
         optim.grad_norm([g], max_norm=-1.0)
+
+
+def test_numbers_of_other_types(env):
+    """Steps and rates as numpy numbers, moments and tensors as tuples."""
+    torch, optim = env
+    a, b = (problem(torch, optim, [700, 33], "f32", 8, 12) for _ in range(2))
+    optim.adamw_step(a[0], a[1], a[2], 4, lr=0.01, weight_decay=0.1)
+    optim.adamw_step(tuple(b[0]), tuple(b[1]), [list(m) for m in b[2]], np.int64(4), lr=[np.float64(0.01), 0.01],
+                     betas=[0.9, 0.999], weight_decay=(0.1, np.float32(0.1)))
+    assert all(torch.allclose(x, y, rtol=1e-6) for x, y in zip(a[0], b[0]))
