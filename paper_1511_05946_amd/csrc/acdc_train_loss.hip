@@ -425,21 +425,30 @@ __device__ __forceinline__ PolicyRow policy_row(const acdc_policy_params& p, flo
 }
 
 // Sums of the weights, for the kernels that need 1 / W: rows in at most
-// kWeightSums groups, one workgroup each.
+// kWeightSums groups, a workgroup each.  (One workgroup of 1024 for up to 16384
+// rows, and one number for the others to read, took 3 us longer with the kernel
+// after it at 8192 rows and 4 at 16384.)
 constexpr int kWeightSums = 256;
 __host__ __device__ inline long long weight_group(long long rows) {
   const long long per = (rows + kWeightSums - 1) / kWeightSums;
   return per > kThreads ? per : kThreads;
 }
 __global__ __launch_bounds__(kThreads) void k_weight_sums(PolicyArgs a, double* __restrict__ sums) {
-  __shared__ double part[kThreads / 64];
+  __shared__ float part[kThreads / 64];
   const long long per = weight_group(a.rows), from = blockIdx.x * per;
   const long long to = from + per < a.rows ? from + per : a.rows;
   double w = 0.0;
 #pragma unroll 4
   for (long long r = from + threadIdx.x; r < to; r += kThreads) w += double(weight_of(a, r));
-  w = total_of<kThreads>(w, part);
-  if (threadIdx.x == 0) sums[blockIdx.x] = w;
+  const float wave = wave_sum(float(w));
+  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = wave;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double total = 0.0;
+#pragma unroll
+    for (int k = 0; k < kThreads / 64; ++k) total += double(part[k]);
+    sums[blockIdx.x] = total;
+  }
 }
 // W out of the sums, for a whole wave.
 __device__ __forceinline__ double weight_total(const double* __restrict__ sums, int groups) {
@@ -462,15 +471,17 @@ __global__ __launch_bounds__(kWide) void k_policy_rows(PolicyArgs a, const typen
                                                        int split, const double* __restrict__ sums, int groups,
                                                        const float4* stat, RowOut out, float* __restrict__ partial) {
   __shared__ double part[kWide / 64];
-  double total;
-  if (gridDim.x == 1) {
-    double w = 0.0;
-    for (long long r = threadIdx.x; r < a.rows; r += kWide) w += double(weight_of(a, r));
-    total = total_of<kWide>(w, part);
-  } else {
-    total = weight_total(sums, groups);
+  __shared__ float waves[kWide / 64][kStats];
+  float norm = 1.f;
+  if (a.p.mean) {
+    if (gridDim.x == 1) {
+      double w = 0.0;
+      for (long long r = threadIdx.x; r < a.rows; r += kWide) w += double(weight_of(a, r));
+      norm = norm_of(a, total_of<kWide>(w, part));
+    } else {
+      norm = norm_of(a, weight_total(sums, groups));
+    }
   }
-  const float norm = norm_of(a, total);
   double sum[kStats] = {};
   const bool by_wave = split > 1 && a.rows <= kWide / 64;
   const int per = by_wave ? kWide / 64 : kWide, me = by_wave ? threadIdx.x / 64 : threadIdx.x;
@@ -496,8 +507,15 @@ __global__ __launch_bounds__(kWide) void k_policy_rows(PolicyArgs a, const typen
   }
 #pragma unroll
   for (int i = 0; i < kStats; ++i) {
-    const double s = total_of<kWide>(sum[i], part);
-    if (threadIdx.x == 0) partial[(long long)i * gridDim.x + blockIdx.x] = float(s);
+    const float v = wave_sum(float(sum[i]));
+    if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64][i] = v;
+  }
+  __syncthreads();
+  if (threadIdx.x < kStats) {
+    double s = 0.0;
+#pragma unroll
+    for (int k = 0; k < kWide / 64; ++k) s += double(waves[k][threadIdx.x]);
+    partial[(long long)threadIdx.x * gridDim.x + blockIdx.x] = float(s);
   }
 }
 
@@ -559,7 +577,7 @@ __global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(LONG ? 4 : f
     weight = a.weights != nullptr ? a.weights[r] : 1.f;
   };
   head((long long)blockIdx.x * ROWS + sub);
-  const float norm = norm_of(a, weight_total(sums, groups));
+  const float norm = a.p.mean ? norm_of(a, weight_total(sums, groups)) : 1.f;
   if (threadIdx.x < ROWS * kStats) (&acc[0][0])[threadIdx.x] = 0.0;
   __syncthreads();
   const unsigned at = unsigned(lane) * 16u;
@@ -692,7 +710,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_policy_tile(
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const unsigned at = unsigned(lane) * 16u;
   float norm = 1.f;
-  if (gridDim.x > 1 && wave == 0) norm = norm_of(a, weight_total(sums, groups));
+  if (gridDim.x > 1 && wave == 0 && a.p.mean) norm = norm_of(a, weight_total(sums, groups));
   double acc = 0.0;  // lane i of wave 0: stat i
   for (long long base = (long long)blockIdx.x * ROWS; base < a.rows; base += (long long)gridDim.x * ROWS) {
     const int rows = a.rows - base < ROWS ? int(a.rows - base) : ROWS;
@@ -1169,7 +1187,7 @@ extern "C" int acdc_policy_loss(const void* logits, int32_t dtype, int64_t strid
   float4* parts = reinterpret_cast<float4*>(ws + w.parts);
   const int groups = rows > 0 ? int((rows + weight_group(rows) - 1) / weight_group(rows)) : 0;
   auto sum_weights = [&] {
-    hipLaunchKernelGGL(k_weight_sums, dim3(unsigned(groups)), dim3(kThreads), 0, s, a, sums);
+    if (p.mean != 0) hipLaunchKernelGGL(k_weight_sums, dim3(unsigned(groups)), dim3(kThreads), 0, s, a, sums);
   };
   auto sum_stats = [&](unsigned blocks) {
     hipLaunchKernelGGL(k_total<kStats>, dim3(1), dim3(128 * kStats), 0, s, partial, int(blocks), 1.f, stats);
