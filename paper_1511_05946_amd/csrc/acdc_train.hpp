@@ -102,11 +102,15 @@ __device__ __forceinline__ Pair swap32(float v) {
   return {__uint_as_float(r[0]), __uint_as_float(r[1])};
 }
 template <class F>
+__device__ __forceinline__ float over_16(float v, F&& f) {
+  v = f(v, dpp<0xB1>(v));     // quad_perm 1,0,3,2
+  v = f(v, dpp<0x4E>(v));     // quad_perm 2,3,0,1
+  v = f(v, dpp<0x141>(v));    // row_half_mirror
+  return f(v, dpp<0x140>(v));  // row_mirror
+}
+template <class F>
 __device__ __forceinline__ float over_wave(float v, F&& f) {
-  v = f(v, dpp<0xB1>(v));   // quad_perm 1,0,3,2
-  v = f(v, dpp<0x4E>(v));   // quad_perm 2,3,0,1
-  v = f(v, dpp<0x141>(v));  // row_half_mirror
-  v = f(v, dpp<0x140>(v));  // row_mirror
+  v = over_16(v, f);
   Pair p = swap16(v);
   v = f(p.a, p.b);
   p = swap32(v);

@@ -78,13 +78,14 @@ __device__ __forceinline__ float target_logit(const typename T::Elem* row, long 
 // outside of them (fewer than 2 kPer), one for each of the first lanes.  A
 // chunk that lies across two cache lines costs both: rows of 65535 bfloat16
 // ran 20 % slower as chunks from the row's first element.
-template <class T>
+template <class T, bool UNIFORM = true>
 struct Cut {
   int head, full, extra;
   __device__ __forceinline__ Cut(const typename T::Elem* row, int classes) {
     const unsigned off = unsigned(reinterpret_cast<uintptr_t>(row)) & 15u;
-    const int h = off != 0u ? int((16u - off) / sizeof(typename T::Elem)) : 0;
-    head = uniform(h < classes ? h : classes);
+    int h = off != 0u ? int((16u - off) / sizeof(typename T::Elem)) : 0;
+    if (h > classes) h = classes;
+    head = UNIFORM ? uniform(h) : h;
     full = (classes - head) / T::kPer;
     extra = classes - full * T::kPer;
   }
@@ -691,11 +692,156 @@ __global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(LONG ? 4 : f
   }
 }
 
-// The same for short rows (up to 4 chunks a lane of a wave): WAVES waves hold RPW
-// rows each in LDS, and one of them does the arithmetic of all rows, a lane for
-// each.  Left to every wave for its own row, that arithmetic (two exponentials,
-// two logarithms, three quotients) is most of its work: 20000 rows of 257
-// bfloat16 classes took 33 us with a wave per row.
+// What one wave does for the rows of a tile (up to 64), a lane for each: the
+// row's loss out of its (M, S, U, x_t), its slope, and the stats.  Left to every
+// wave for its own row, that arithmetic (two exponentials, two logarithms, three
+// quotients) is most of its work: 20000 rows of 257 bfloat16 classes took 33 us
+// with a wave per row.
+struct RowIn {
+  float w, old, adv, ref;
+};
+__device__ __forceinline__ RowIn row_in(const PolicyArgs& a, long long r, bool any) {
+  RowIn v{0.f, 0.f, 0.f, 0.f};
+  if (any) {
+    v.w = weight_of(a, r);
+    v.old = a.old[r];
+    v.adv = a.advantages[r];
+    if (a.ref != nullptr) v.ref = a.ref[r];
+  }
+  return v;
+}
+__device__ __forceinline__ void tile_rows(const PolicyArgs& a, long long base, int rows, int lane, float norm, RowIn in,
+                                          const float4* stat, float4* slope, int* target, const RowOut& out,
+                                          double& acc) {
+  if (gridDim.x == 1 && a.p.mean) {  // these are all rows
+    double total = double(in.w);
+#pragma unroll 1
+    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
+    norm = norm_of(a, total);
+  }
+  const float w = in.w * norm;
+  float4 st = make_float4(0.f, 1.f, 0.f, 0.f), sl = make_float4(0.f, 0.f, 0.f, 0.f);
+  PolicyRow p{};
+  if (w != 0.f) {
+    const float4 z = stat[lane];
+    st = stat_of(Run{z.x, z.y, z.z}, z.w);
+    p = policy_row(a.p, w, st.w, st.z, in.old, in.adv, a.ref != nullptr, in.ref);
+    const float g = p.g * a.p.grad_scale;
+    const Slope k = slope_of(st.x, st.y, st.z, g, p.h * a.p.grad_scale);
+    sl = make_float4(k.a, k.b, g, 0.f);
+  }
+  if (lane < rows) {
+    put_row(out, base + lane, st, p.g, p.h);
+    slope[lane] = sl;
+    if (w == 0.f) target[lane] = -1;
+  }
+#pragma unroll
+  for (int i = 0; i < kStats; ++i) {
+    const float v = wave_sum(p.v[i]);
+    if (lane == i) acc += double(v);
+  }
+}
+
+// One pass over rows of at most 64 chunks: 16 lanes a row, NC chunks each, four
+// rows a wave.  A wave for a row would spend its instructions on lanes that have
+// nothing to do and on reductions over 64 lanes: 64 rows of 256 floats, which
+// one workgroup takes (a launch instead of three), took 9.3 us that way, bound by
+// the one CU's vector unit, and take 5.4 this way.
+template <class T, int WAVES, int NC>
+__global__ __launch_bounds__(64 * WAVES) void k_policy_short(
+    PolicyArgs a, const typename T::Elem* x, long long stride, int classes, const double* __restrict__ sums, int groups,
+    typename T::Elem* grad, long long grad_stride, RowOut out, float* __restrict__ partial) {
+  constexpr int ROWS = WAVES * 4;
+  __shared__ float4 stat[ROWS];   // M, S, U, x_t
+  __shared__ float4 slope[ROWS];  // a, b, g
+  __shared__ int target[ROWS];    // -1: the row takes no part
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int mine = threadIdx.x / 16, part = threadIdx.x % 16;
+  float norm = 1.f;
+  if (gridDim.x > 1 && wave == 0 && a.p.mean) norm = norm_of(a, weight_total(sums, groups));
+  double acc = 0.0;  // lane i of wave 0: stat i
+  for (long long base = (long long)blockIdx.x * ROWS; base < a.rows; base += (long long)gridDim.x * ROWS) {
+    const int rows = a.rows - base < ROWS ? int(a.rows - base) : ROWS;
+    RowIn in{};
+    if (wave == 0) in = row_in(a, base + lane, lane < rows);
+    const bool any = mine < rows;
+    const long long r = any ? base + mine : base;
+    const typename T::Elem* row = x + r * stride;
+    const Cut<T, false> cut(row, classes);
+    const float weight = a.weights != nullptr ? a.weights[r] : 1.f;
+    const long long tt = target_of(a.targets, a.bits, r);
+    const int t = any && tt >= 0 && weight != 0.f ? (tt < classes ? int(tt) : classes) : -1;
+    // the one workgroup of a small call does not wait for the targets before it
+    // asks for the logits; what it gets of an idle row is not looked at
+    const bool ask = WAVES > 8 ? any : t >= 0;
+    const bool has_one = part < cut.extra;
+    typename T::Raw raw[NC];
+    float one = kNegMax, xt = __builtin_nanf("");
+    if (ask) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (c * 16 + part < cut.full) raw[c] = load_chunk<T>(row + cut.head + (c * 16 + part) * T::kPer);
+      if (has_one) one = T::one(row[cut.element(part)]);
+    }
+    if (t >= 0 && t < classes) xt = T::one(row[t]);
+    if (part == 0 && any) target[mine] = t;
+    if (t >= 0) {
+      float m = fmaxf(one, kNegMax);
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (c * 16 + part < cut.full) {
+#pragma unroll
+          for (int e = 0; e < T::kPer; ++e) m = fmaxf(m, T::get(raw[c], e));
+        }
+      m = over_16(m, [](float p, float q) { return fmaxf(p, q); });
+      float s = 0.f, u = 0.f;
+      auto add = [&](float z) {
+        const float d = z - m, e = exp_of(d);
+        s += e;
+        u += e * fmaxf(d, -1e30f);
+      };
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (c * 16 + part < cut.full) {
+#pragma unroll
+          for (int e = 0; e < T::kPer; ++e) add(T::get(raw[c], e));
+        }
+      if (has_one) add(one);
+      s = over_16(s, [](float p, float q) { return p + q; });
+      u = over_16(u, [](float p, float q) { return p + q; });
+      if (part == 0) stat[mine] = make_float4(m, s, u, xt);
+    }
+    __syncthreads();
+    if (wave == 0) tile_rows(a, base, rows, lane, norm, in, stat, slope, target, out, acc);
+    __syncthreads();
+    if (any) {
+      const bool on = target[mine] >= 0;
+      typename T::Elem* to = grad + r * grad_stride;
+      const float4 k = slope[mine], z = stat[mine];
+      const Slope sl{z.x, k.x, k.y};
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (c * 16 + part < cut.full) {
+          float y[T::kPer] = {};
+          if (on) {
+#pragma unroll
+            for (int e = 0; e < T::kPer; ++e) y[e] = slope_value(sl, T::get(raw[c], e));
+          }
+          store_chunk<T>(to + cut.head + (c * 16 + part) * T::kPer, T::pack(y));
+        }
+      if (has_one) to[cut.element(part)] = T::to(on ? slope_value(sl, one) : 0.f);
+      // the lane that wrote the target's chunk writes the target again, with its g
+      if (on && t < classes) {
+        const int tc = cut.chunk_of(t);
+        if ((tc >= 0 ? tc % 16 : cut.lane_of(t)) == part) to[t] = T::to(slope_value(sl, z.w) + k.z);
+      }
+    }
+    __syncthreads();  // before the next tile's rows
+  }
+  if (wave == 0 && lane < kStats) partial[(long long)lane * gridDim.x + blockIdx.x] = float(acc);
+}
+
+// The same for rows of 65 to 256 chunks: WAVES waves hold RPW rows each in LDS.
 template <class T, int WAVES, int RPW, int NC>
 __global__ __launch_bounds__(64 * WAVES) void k_policy_tile(
     PolicyArgs a, const typename T::Elem* x, long long stride, int classes, const double* __restrict__ sums, int groups,
@@ -715,15 +861,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_policy_tile(
   for (long long base = (long long)blockIdx.x * ROWS; base < a.rows; base += (long long)gridDim.x * ROWS) {
     const int rows = a.rows - base < ROWS ? int(a.rows - base) : ROWS;
     const int first = wave * RPW, last = min(first + RPW, rows);
-    // what wave 0 needs of each row, asked for ahead of the rows' arithmetic
-    const long long mine = base + lane;
-    float w = 0.f, old = 0.f, adv = 0.f, ref = 0.f;
-    if (wave == 0 && lane < rows) {
-      w = weight_of(a, mine);
-      old = a.old[mine];
-      adv = a.advantages[mine];
-      if (a.ref != nullptr) ref = a.ref[mine];
-    }
+    RowIn in{};  // asked for ahead of the rows' arithmetic
+    if (wave == 0) in = row_in(a, base + lane, lane < rows);
     // the wave's rows' targets, a lane for each
     int own = -1;
     if (first + lane < last) {
@@ -794,35 +933,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_policy_tile(
       if (lane == 0) stat[i] = make_float4(m, s, u, xt);
     }
     __syncthreads();
-    if (wave == 0) {
-      if (gridDim.x == 1) {  // these are all rows
-        double total = double(w);
-#pragma unroll 1
-        for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
-        norm = norm_of(a, total);
-      }
-      w *= norm;
-      float4 st = make_float4(0.f, 1.f, 0.f, 0.f), sl = make_float4(0.f, 0.f, 0.f, 0.f);
-      PolicyRow p{};
-      if (w != 0.f) {
-        const float4 z = stat[lane];
-        st = stat_of(Run{z.x, z.y, z.z}, z.w);
-        p = policy_row(a.p, w, st.w, st.z, old, adv, a.ref != nullptr, ref);
-        const float g = p.g * a.p.grad_scale;
-        const Slope k = slope_of(st.x, st.y, st.z, g, p.h * a.p.grad_scale);
-        sl = make_float4(k.a, k.b, g, 0.f);
-      }
-      if (lane < rows) {
-        put_row(out, mine, st, p.g, p.h);
-        slope[lane] = sl;
-        if (w == 0.f) target[lane] = -1;
-      }
-#pragma unroll
-      for (int i = 0; i < kStats; ++i) {
-        const float v = wave_sum(p.v[i]);
-        if (lane == i) acc += double(v);
-      }
-    }
+    if (wave == 0) tile_rows(a, base, rows, lane, norm, in, stat, slope, target, out, acc);
     __syncthreads();
 #pragma unroll 1
     for (int i = first; i < last; ++i) {
@@ -1099,7 +1210,9 @@ int launch_grad(const Logits& l, const float4* stat, const float* g, const float
 // floats are not: 2048 of 65536 216 against 205, 512 of 300000 341 against 288.
 template <class T, class F>
 void with_row_shape(int chunks, F&& f) {
-  if (chunks <= 64) f.template operator()<64, 1, false>();
+  if (chunks <= 16) f.template operator()<16, 1, false>();
+  else if (chunks <= 32) f.template operator()<16, 2, false>();
+  else if (chunks <= 64) f.template operator()<16, 4, false>();
   else if (chunks <= 128) f.template operator()<64, 2, false>();
   else if (chunks <= 256) f.template operator()<64, 4, false>();
   else if (chunks <= 512) f.template operator()<64, 8, false>();
@@ -1206,17 +1319,22 @@ extern "C" int acdc_policy_loss(const void* logits, int32_t dtype, int64_t strid
                              (long long)grad_stride, out, to);
         };
         auto blocks_of = [&](int per) { return unsigned(std::min<int64_t>((rows + per - 1) / per, kMaxPartials)); };
-        if constexpr (THREADS == 64 && NC <= 4) {
-          constexpr int RPW = 4 / NC;
-          // up to 64 rows in one workgroup: a launch instead of three
-          if (rows <= 16 * RPW) {
-            go(k_policy_tile<T, 16, RPW, NC>, 1, 1024, stats);
+        // one workgroup's rows: a launch instead of three
+        auto tiles = [&](auto one, int most, auto many, int each) {
+          if (rows <= most) {
+            go(one, 1, 1024, stats);
           } else {
-            const unsigned blocks = blocks_of(8 * RPW);
+            const unsigned blocks = blocks_of(each);
             sum_weights();
-            go(k_policy_tile<T, 8, RPW, NC>, blocks, 512, partial);
+            go(many, blocks, 512, partial);
             sum_stats(blocks);
           }
+        };
+        if constexpr (THREADS == 16) {
+          tiles(k_policy_short<T, 16, NC>, 64, k_policy_short<T, 8, NC>, 32);
+        } else if constexpr (THREADS == 64 && NC <= 4) {
+          constexpr int RPW = 4 / NC;
+          tiles(k_policy_tile<T, 16, RPW, NC>, 16 * RPW, k_policy_tile<T, 8, RPW, NC>, 8 * RPW);
         } else {
           constexpr int WG = THREADS < kThreads ? kThreads : THREADS;
           const unsigned blocks = blocks_of(WG / THREADS);
