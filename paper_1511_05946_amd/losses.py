@@ -64,7 +64,7 @@ def _native(logits, name, *args):
     if device < 0 or device != torch._C._cuda_getDevice():
         return None
     r = getattr(binding(), name)(logits, *args, torch._C._cuda_getCurrentRawStream(device))
-    if r.__class__ is int:
+    if type(r) is int:
         _check(r, f"acdc_{name}")
     return r
 
