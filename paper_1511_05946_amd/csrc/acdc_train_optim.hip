@@ -47,6 +47,7 @@ constexpr unsigned long long kAddress = (1ull << 48) - 1;
 
 struct Step {
   double one1, one2;      // 1 - beta
+  float c1, c2;           // the same, for gradients without a scale
   float beta1, beta2;
   float root_scale, eps;  // 1 / sqrt(1 - beta2^step)
   const float* grad_scale;
@@ -122,18 +123,43 @@ __device__ __forceinline__ void decode4(unsigned w, float scale, float (&v)[4]) 
 }
 // Codes of four values of a block with this scale; positive values stay
 // positive with POSITIVE.  A NaN keeps its own code (the block's scale comes
-// from the others).
+// from the others), and so does an infinity, as NaN.  The quotient v / scale is
+// correctly rounded: with r the rounded reciprocal, q + r (v - q scale) of q = v r
+// is (Markstein's division), three instructions a value and one division a block.
 template <bool POSITIVE>
 __device__ __forceinline__ unsigned encode4(const float (&v)[4], float scale) {
+  // a scale of 0 or infinity has codes of 0 (and NaN)
+  const float s = scale < 0x1.fffffep127f ? scale : 0.f, r = s > 0.f ? 1.f / s : 0.f;
   float q[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    q[i] = scale > 0.f ? v[i] / scale : v[i] * 0.f;
-    if (POSITIVE && v[i] > 0.f && q[i] < kTiny && scale > 0.f) q[i] = kTiny;
+    const float q0 = v[i] * r;
+    q[i] = fmaf(fmaf(-q0, s, v[i]), r, q0);
+    if (POSITIVE) q[i] = v[i] > 0.f ? fmaxf(q[i], kTiny) : q[i];
   }
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
   w = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
   return unsigned(w);
+}
+// Square roots of four values, correctly rounded but for rare cases a unit in
+// the last place off: s = v rsq(v), then s + rsq(v) / 2 (v - s s).  Denormal
+// values, infinities and NaN, which the instruction does not take, go the long
+// way, all lanes together.
+__device__ __forceinline__ void roots4(const float (&v)[4], float (&root)[4]) {
+  constexpr int kOdd = 0x3 | 0x204 | 0x90;  // NaN, infinities, denormals
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) odd |= __builtin_amdgcn_classf(v[i], kOdd);
+  if (__any(odd)) {
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) root[i] = sqrtf(v[i]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float r = __builtin_amdgcn_rsqf(fmaxf(v[i], 0x1p-126f)), s = v[i] * r;
+    root[i] = fmaf(fmaf(-s, s, v[i]), 0.5f * r, s);
+  }
 }
 // Scale of a wave's block out of each lane's four values.  Blocks below 2^-100
 // are 0: their scale would leave the normal numbers.  (The product may leave the
@@ -144,11 +170,13 @@ __device__ __forceinline__ float scale_of(const float (&v)[4]) {
 }
 
 // The step of 1024 elements, four a thread.  Bound by HBM: 100 M floats with
-// 32-bit moments, 2.8 GB, in 460-480 us (5.9 TB/s), 400 M with 8-bit ones, 6.4
-// GB, in 1130 us (5.7 TB/s).  Workgroups of one round: with two and four times
-// the elements in flight a thread, 20 M elements in 300 tensors took 105 and 121
-// us instead of 93.  8-bit: a wave's 64 x 4 elements are one block, whose
-// maximum is a reduction by lane swaps; its scales are one scalar load each.
+// 32-bit moments, 2.8 GB, in 470 us (6.0 TB/s), 400 M with 8-bit ones, 6.4 GB, in
+// 1043 us (6.2 TB/s).  Workgroups of one round: with two and four times the
+// elements in flight a thread, 20 M elements in 300 tensors took 105 and 121 us
+// instead of 93.  8-bit: a wave's 64 x 4 elements are one block, whose maximum is
+// a reduction by lane swaps; its scales are one scalar load each.  With the
+// compiler's quotients and roots the vector unit bound it (106 % of its cycles
+// at 1138 us); the step itself needs neither to the last bit.
 template <class P, class G, int BITS, bool MASTER, bool NT>
 __global__ __launch_bounds__(kThreads) void k_adamw(Batch<words_of(BITS, MASTER)> b, int count, Step s) {
   const int i = tensor_of(b.first, count, blockIdx.x);
@@ -177,10 +205,14 @@ __global__ __launch_bounds__(kThreads) void k_adamw(Batch<words_of(BITS, MASTER)
   const Rate rate = b.rate[word[3] >> 48];
   t.rate = rate.rate;
   t.decay = rate.decay;
-  const float gs = s.grad_scale != nullptr ? *s.grad_scale : 1.f;
-  if (!(gs - gs == 0.f)) return;
-  // the gradient's scale goes into the factors of g and g^2, each rounded once
-  const float c1 = float(s.one1 * double(gs)), c2 = float(s.one2 * (double(gs) * double(gs)));
+  float c1 = s.c1, c2 = s.c2;
+  if (s.grad_scale != nullptr) {
+    const float gs = *s.grad_scale;
+    if (!(gs - gs == 0.f)) return;
+    // the gradient's scale goes into the factors of g and g^2, each rounded once
+    c1 = float(s.one1 * double(gs));
+    c2 = float(s.one2 * (double(gs) * double(gs)));
+  }
   // a wave's 256 elements are one block of scales
   const long long base = (long long)(int(blockIdx.x) - b.first[i]) * kChunk + (threadIdx.x / 64) * kBlock;
   if (base >= t.n) return;
@@ -209,11 +241,10 @@ __global__ __launch_bounds__(kThreads) void k_adamw(Batch<words_of(BITS, MASTER)
     v[k] = s.beta2 * v[k] + c2 * g[k] * g[k];
   }
   float root[4];
+  roots4(v, root);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    root[k] = sqrtf(v[k]);
-    w[k] = w[k] * t.decay - t.rate * (m[k] / (root[k] * s.root_scale + s.eps));
-  }
+  for (int k = 0; k < 4; ++k)
+    w[k] = w[k] * t.decay - t.rate * (m[k] * __builtin_amdgcn_rcpf(root[k] * s.root_scale + s.eps));
   if constexpr (MASTER) store4<F32, NT>(t.master, at, have, w);
   store4<P, NT>(t.param, at, have, w);
   if constexpr (BITS == 32) {
@@ -396,7 +427,8 @@ extern "C" int acdc_adamw_step(const acdc_adamw_tensor* tensors, int32_t count, 
   for (int32_t i = 0; i < count; ++i)
     if (!tensor_ok(tensors[i])) return ACDC_ERR_INVALID_ARG;
   const double c1 = 1.0 - std::pow(beta1, double(step)), c2 = 1.0 - std::pow(beta2, double(step));
-  const Step s{1.0 - beta1, 1.0 - beta2, float(beta1), float(beta2), float(1.0 / std::sqrt(c2)), float(eps), grad_scale};
+  const Step s{1.0 - beta1, 1.0 - beta2, float(1.0 - beta1), float(1.0 - beta2), float(beta1), float(beta2),
+               float(1.0 / std::sqrt(c2)), float(eps), grad_scale};
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   unsigned seen = 0;
   double bytes = 0.0;

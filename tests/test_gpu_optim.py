@@ -317,3 +317,34 @@ def test_numbers_of_other_types(env):
     optim.adamw_step(tuple(b[0]), tuple(b[1]), [list(m) for m in b[2]], np.int64(4), lr=[np.float64(0.01), 0.01],
                      betas=[0.9, 0.999], weight_decay=(0.1, np.float32(0.1)))
     assert all(torch.allclose(x, y, rtol=1e-6) for x, y in zip(a[0], b[0]))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_gradients_of_every_size(env, bits):
+    """Second moments from denormal numbers to 1e36 in one block and in blocks of
+    their own: nothing becomes NaN, and every moment keeps its size."""
+    torch, optim = env
+    sizes = [1e-22, 3e-21, 1e-15, 1e-8, 1.0, 1e9, 1e18]
+    g = np.concatenate([np.full(256, x) for x in sizes] + [np.tile(sizes, 40)]).astype(np.float32)
+    n = len(g)
+    p, gt = torch.ones(n, device="cuda"), torch.from_numpy(g).cuda()
+    state = optim.moments(p, bits)
+    optim.adamw_step([p], [gt], [state], 1, lr=LR, betas=BETAS, eps=EPS, weight_decay=0.0)
+    w, m, v, move = R.adamw(np.ones(n), g.astype(float), np.zeros(n), np.zeros(n), 1, LR, BETAS, EPS, 0.0)
+    # v is rounded to a multiple of 2^-149 where it is that small: sqrt(v) by up to 2^-74.5, eps being 1e-8
+    assert np.all(np.abs(p.double().cpu().numpy() - w) <= 4 * R.EPS + 20 * R.EPS * move)
+    for k, x in enumerate((m, np.sqrt(v))):
+        got = state[k].double().cpu().numpy()
+        if bits == 32:
+            want = x if k == 0 else v
+            assert np.all(np.abs(got - want) <= 4 * R.EPS * want + 2.0 ** -149)
+            continue
+        each = np.repeat(state[2 + k].double().cpu().numpy(), R.BLOCK)[:n]
+        top = np.repeat(R.block_scale(x), R.BLOCK)[:n] * R.TOP
+        off = np.abs(got * each - x)
+        # half a step of the code, or of the smallest one, and the rounding of denormal v
+        bound = np.maximum(x / 16, each * R.TINY / 2) * (1 + 1e-5) + (0.0 if k == 0 else 2.0 ** -74)
+        bound = np.where(top < 2.0 ** -99, top, bound)   # blocks below 2^-100 are 0
+        if k == 1:
+            off = np.where(x < each * R.TINY, 0.0, off)   # positive ones never are, unless all are
+        assert np.all(off <= bound), (k, np.argmax(off - bound))
