@@ -17,7 +17,7 @@
  * columns of wider rows can be read in place.  Pointers need the alignment
  * of their element only.  targets: one class per row, int32 or int64
  * (target_bits 32 or 64).  A negative target marks a row that takes no part:
- * its logits are not read and may hold anything, its outputs are 0 and its
+ * its logits do not matter and may hold anything, its outputs are 0 and its
  * gradient is written as 0.  A target >= classes gives NaN for its row.
  * Logits of -inf are classes of probability 0; a row that has only such
  * classes has no distribution and gives NaN, as does one that holds NaN or

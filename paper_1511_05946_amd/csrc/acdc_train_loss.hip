@@ -190,8 +190,8 @@ struct Group {
 
 // A workgroup's part of a row, streamed: every thread keeps a run of its own.
 // Item r * split + k is part k of row r; with split = 1 its workgroup writes the
-// row's (M, S, H, logp), otherwise the runs of the parts.  Bound by HBM: 20.7 k
-// rows of 32768 bfloat16, 1.36 GB, in 238 us (5.7 TB/s).
+// row's (M, S, H, logp), otherwise the runs of the parts.  Bound by HBM: 19.9 k
+// rows of 32768 bfloat16, 1.3 GB, in 220 us (5.9 TB/s; the vector unit 81 % busy).
 template <class T, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_row_stats(const typename T::Elem* __restrict__ x, long long stride,
                                                        const void* __restrict__ targets, int bits, int classes,
@@ -262,7 +262,8 @@ __device__ __forceinline__ float4 join_parts(const float4* __restrict__ parts, i
   return stat_of(merge_wave(run), xt);
 }
 
-// Statistics of rows in parts: one wave per row; logp and entropy too.
+// Statistics of rows in parts: one wave per row; logp and entropy too.  2 us, which
+// is what a launch takes.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_row_join(const typename T::Elem* __restrict__ x, long long stride,
                                                        const void* __restrict__ targets, int bits, int classes,
@@ -310,8 +311,8 @@ __device__ __forceinline__ void slopes(const Slope& sl, const typename T::Elem* 
 
 // dL/dlogits from each row's (M, S, H, logp), g and h; items as in k_row_stats,
 // the last rows first: what a forward read last is what the cache still holds.
-// Bound by HBM: 27.6 k rows of 32768 bfloat16, a quarter of them idle, read 1.36
-// and write 1.81 GB in 515 us (6.1 TB/s).
+// Bound by HBM: 26.4 k rows of 32768 bfloat16, a quarter of them idle, read 1.3
+// and write 1.73 GB in 545 us (5.6 TB/s).
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x, long long stride,
                                                        const void* __restrict__ targets, int bits, int classes,
@@ -571,10 +572,9 @@ __global__ __launch_bounds__(128 * STATS) void k_total(const float* __restrict__
 // Infinity Cache, which a row a CU fits) for the gradient.
 //
 // Bound by HBM, each logit read once and its gradient written once: 8192 rows of
-// 4096 floats, 246 MB, in 47 us (5.2 TB/s), of 65536 bfloat16, 2.04 GB, in 380
+// 4096 floats, 255 MB, in 49 us (5.2 TB/s), of 65536 bfloat16, 2.04 GB, in 380
 // us (5.4 TB/s); statistics and gradient as two passes took 61 and 640 us.  The
-// vector unit has room for it: about 22 instructions a value against 30 that fit
-// a bfloat16's 4 bytes at 5 TB/s.  So many chunks a lane as a row needs, that
+// vector unit is 54 and 67 % busy.  So many chunks a lane as a row needs, that
 // the loads of a whole row are in flight together; several workgroups a CU, so
 // that one loads while another stores.
 constexpr int fused_waves(int nc) { return nc <= 4 ? 8 : nc <= 8 ? 6 : nc <= 12 ? 5 : 4; }
@@ -1017,7 +1017,7 @@ __device__ __forceinline__ double excess(const PairArgs& a, const float4* __rest
 }
 
 // Rewards, margin and loss of pairs, and dL/dlogp of their rows, whose g and h
-// are 0 before it.  WG / GROUP pairs a workgroup at a time: a wave each in the
+// are 0 before it: 5 to 7 us of latency, beside passes over the logits.  WG / GROUP pairs a workgroup at a time: a wave each in the
 // one workgroup of a call with few pairs, which writes the stats itself, else
 // a workgroup each, whose sums go into partial[.][blockIdx].
 template <int WG, int GROUP>
@@ -1191,7 +1191,7 @@ int launch_stats(const Logits& l, int split, const RowOut& out, float4* parts, h
                          split, items, out, parts);
     };
     // as many lanes as ask for a part of a row in one or two rounds of kAhead chunks
-    // (20.7 k rows of 32768 bfloat16: 250 us with 256 lanes, 238 with 512)
+    // (19.9 k rows of 32768 bfloat16: 250 us with 256 lanes, 238 with 512)
     const int64_t chunks = l.classes / T::kPer / split;
     if (chunks > 2 * kAhead * kThreads) go(k_row_stats<T, 512>, 512);
     else go(k_row_stats<T, kThreads>, kThreads);

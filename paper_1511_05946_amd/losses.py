@@ -14,8 +14,8 @@ computation runs in HIP kernels on the current torch stream.  Logits are
 float32 or bfloat16, [rows, classes], each row contiguous and the rows any
 distance apart; gradients have the logits' dtype.  ``out`` may be the logits
 themselves.  Targets are int32 or int64, one class per row; a row with a
-negative target takes no part (its logits are not read, its gradient is 0), and
-a target past the classes gives NaN.  The ``*_autograd`` functions are the
+negative target takes no part (its logits do not matter, its gradient is 0), and a
+target past the classes gives NaN.  The ``*_autograd`` functions are the
 differentiable forms.
 """
 
