@@ -123,30 +123,36 @@ __device__ __forceinline__ void put_row(const RowOut& o, long long r, const floa
   }
 }
 
-// f.template operator()<N>(c) for the chunks c, c + step, ... below `to`, AHEAD at a time.
+// f.template operator()<N, ALL>(c) for the chunks c, c + step, ... below `to`, AHEAD
+// at a time; what is left at the end (fewer, ALL false) is asked for together too.
 template <int AHEAD, class F>
 __device__ __forceinline__ void stream(int c, int to, int step, F&& f) {
-  for (; c + (AHEAD - 1) * step < to; c += AHEAD * step) f.template operator()<AHEAD>(c);
-  for (; c < to; c += step) f.template operator()<1>(c);
+  for (; c + (AHEAD - 1) * step < to; c += AHEAD * step) f.template operator()<AHEAD, true>(c);
+  if (c < to) f.template operator()<AHEAD - 1, false>(c);
 }
-// The run of N chunks c, c + step, ..., asked for together.
-template <class T, int N>
-__device__ __forceinline__ Run run_of(const typename T::Elem* body, int c, int step) {
+// The run of N chunks c, c + step, ...; without ALL only of those below `to`.
+template <class T, int N, bool ALL>
+__device__ __forceinline__ Run run_of(const typename T::Elem* body, int c, int step, int to) {
   typename T::Raw raw[N];
 #pragma unroll
-  for (int q = 0; q < N; ++q) raw[q] = load_chunk<T>(body + (long long)(c + q * step) * T::kPer);
+  for (int q = 0; q < N; ++q)
+    if (ALL || c + q * step < to) raw[q] = load_chunk<T>(body + (long long)(c + q * step) * T::kPer);
   Run b = empty_run();
 #pragma unroll
   for (int q = 0; q < N; ++q)
+    if (ALL || c + q * step < to) {
 #pragma unroll
-    for (int i = 0; i < T::kPer; ++i) b.m = fmaxf(b.m, T::get(raw[q], i));
+      for (int i = 0; i < T::kPer; ++i) b.m = fmaxf(b.m, T::get(raw[q], i));
+    }
 #pragma unroll
   for (int q = 0; q < N; ++q)
+    if (ALL || c + q * step < to) {
 #pragma unroll
-    for (int i = 0; i < T::kPer; ++i) {
-      const float d = T::get(raw[q], i) - b.m, e = exp_of(d);
-      b.s += e;
-      b.u += e * fmaxf(d, -1e30f);
+      for (int i = 0; i < T::kPer; ++i) {
+        const float d = T::get(raw[q], i) - b.m, e = exp_of(d);
+        b.s += e;
+        b.u += e * fmaxf(d, -1e30f);
+      }
     }
   return b;
 }
@@ -214,7 +220,9 @@ __global__ __launch_bounds__(THREADS) void k_row_stats(const typename T::Elem* _
     int from, to;
     chunks_of(cut.full, split, k, from, to);
     const typename T::Elem* body = row + cut.head;
-    stream<kAhead>(from + threadIdx.x, to, THREADS, [&]<int N>(int c) { run = merge(run, run_of<T, N>(body, c, THREADS)); });
+    stream<kAhead>(from + threadIdx.x, to, THREADS, [&]<int N, bool ALL>(int c) {
+      run = merge(run, run_of<T, N, ALL>(body, c, THREADS, to));
+    });
     if (k == split - 1 && int(threadIdx.x) < cut.extra) {
       const float v = T::one(row[cut.element(threadIdx.x)]);
       Run b = empty_run();
@@ -292,21 +300,24 @@ __device__ __forceinline__ float slope_value(const Slope& k, float x) {
   return exp_of(d) * (k.a + k.b * fmaxf(d, -1e30f));
 }
 
-// The gradients of N chunks c, c + step, ....  Their loads stand before their
+// The gradients of N chunks c, c + step, ... as in run_of.  Their loads stand before their
 // stores: the gradient may be the logits' own memory, so that the compiler
 // would not move a load ahead of an earlier store by itself.
-template <class T, int N>
-__device__ __forceinline__ void slopes(const Slope& sl, const typename T::Elem* body, typename T::Elem* out, int c, int step) {
+template <class T, int N, bool ALL>
+__device__ __forceinline__ void slopes(const Slope& sl, const typename T::Elem* body, typename T::Elem* out, int c, int step,
+                                       int to) {
   typename T::Raw raw[N];
 #pragma unroll
-  for (int q = 0; q < N; ++q) raw[q] = load_chunk<T>(body + (long long)(c + q * step) * T::kPer);
+  for (int q = 0; q < N; ++q)
+    if (ALL || c + q * step < to) raw[q] = load_chunk<T>(body + (long long)(c + q * step) * T::kPer);
 #pragma unroll
-  for (int q = 0; q < N; ++q) {
-    float y[T::kPer];
+  for (int q = 0; q < N; ++q)
+    if (ALL || c + q * step < to) {
+      float y[T::kPer];
 #pragma unroll
-    for (int i = 0; i < T::kPer; ++i) y[i] = slope_value(sl, T::get(raw[q], i));
-    store_chunk<T>(out + (long long)(c + q * step) * T::kPer, T::pack(y));
-  }
+      for (int i = 0; i < T::kPer; ++i) y[i] = slope_value(sl, T::get(raw[q], i));
+      store_chunk<T>(out + (long long)(c + q * step) * T::kPer, T::pack(y));
+    }
 }
 
 // dL/dlogits from each row's (M, S, H, logp), g and h; items as in k_row_stats,
@@ -359,7 +370,9 @@ __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x
                      : has_one && cut.lane_of(int(t)) == int(threadIdx.x);
     }
     const float yt = mine ? slope_value(sl, T::one(row[t])) + g : 0.f;
-    stream<kAhead>(from + threadIdx.x, to, kThreads, [&]<int N>(int i) { slopes<T, N>(sl, body, out_body, i, kThreads); });
+    stream<kAhead>(from + threadIdx.x, to, kThreads, [&]<int N, bool ALL>(int i) {
+      slopes<T, N, ALL>(sl, body, out_body, i, kThreads, to);
+    });
     if (has_one) out[one] = T::to(slope_value(sl, T::one(row[one])));
     if (mine) out[t] = T::to(yt);
   }
@@ -646,8 +659,8 @@ __global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(LONG ? 4 : f
     const float ref = uniform(a.ref != nullptr ? a.ref[r] : 0.f);
     Run run = empty_run();  // of what is streamed
     if constexpr (LONG)
-      stream<kAhead>(NC * THREADS + lane, cut.full, THREADS, [&]<int N>(int c) {
-        run = merge(run, run_of<T, N>(body, c, THREADS));
+      stream<kAhead>(NC * THREADS + lane, cut.full, THREADS, [&]<int N, bool ALL>(int c) {
+        run = merge(run, run_of<T, N, ALL>(body, c, THREADS, cut.full));
       });
     float m = fmaxf(run.m, last);
 #pragma unroll
@@ -693,7 +706,9 @@ __global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(LONG ? 4 : f
         store_chunk_at<T>(to_body, c * THREADS * 16u, at, T::pack(y));
       }
     if constexpr (LONG)
-      stream<kAhead>(NC * THREADS + lane, cut.full, THREADS, [&]<int N>(int c) { slopes<T, N>(sl, body, to_body, c, THREADS); });
+      stream<kAhead>(NC * THREADS + lane, cut.full, THREADS, [&]<int N, bool ALL>(int c) {
+        slopes<T, N, ALL>(sl, body, to_body, c, THREADS, cut.full);
+      });
     if (has_one) to[one] = T::to(slope_value(sl, last));
     // the lane that wrote the target's chunk writes the target again, with its g
     const int tc = cut.chunk_of(t);
