@@ -5,11 +5,12 @@
 // the scales of 8-bit moments, one per 256 elements: the block's maximum has
 // to be known before its first code is written.
 //
-// The tensors' addresses travel in the kernels' arguments, 62 to 104 tensors a
-// launch: nothing is uploaded, and no table outlives the call.
+// The tensors' addresses travel in the kernels' arguments, up to 62 to 104 tensors
+// a launch: nothing is uploaded, and no table outlives the call.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <cstring>
 
 #include "acdc_train.hpp"
 
@@ -26,23 +27,29 @@ constexpr float kTiny = 0x1p-9f;  // smallest positive one
 // something else on top: its length in the first three, the index of its rate
 // in the fourth.  More tensors fit a launch's arguments that way, and fewer
 // launches drain and fill the card: 300 tensors, 560 MB, took 118 us with 48
-// whole records a launch.
+// whole records a launch, and 106 so.
+// A list that fits an eighth of that goes in arguments of that size: they are
+// copied whole at each launch, and three tensors of 256 floats, step after step,
+// take 4.8 us so and 6.2 with the long ones (eleven 4.8 and 5.2, and with 1024
+// bytes 5.1).
 //   0 param | n, 1 grad | n, 2 m | n, 3 v | rate, then m_scale and v_scale (8 bits), master
 constexpr int kArguments = 3840;  // bytes, of the 4 KB that a launch has
+constexpr int kFewArguments = 480;
 constexpr int kRates = 8;
 struct Rate {
   float rate, decay;  // lr / (1 - beta1^step), 1 - lr * weight_decay
 };
-template <int WORDS>
+template <int WORDS, int BYTES>
 struct Batch {
-  static constexpr int kMost = int((kArguments - kRates * sizeof(Rate)) / (4 + 8 * WORDS));
+  static constexpr int kMost = int((BYTES - kRates * sizeof(Rate)) / (4 + 8 * WORDS));
   unsigned long long word[kMost][WORDS];
   Rate rate[kRates];
   int first[kMost];  // first workgroup of each tensor
 };
 constexpr int words_of(int bits, bool master) { return 4 + (bits == 8 ? 2 : 0) + (master ? 1 : 0); }
-static_assert(sizeof(Batch<4>) <= kArguments && sizeof(Batch<5>) <= kArguments && sizeof(Batch<6>) <= kArguments &&
-              sizeof(Batch<7>) <= kArguments);
+template <int WORDS>
+constexpr bool fits = sizeof(Batch<WORDS, kArguments>) <= kArguments && sizeof(Batch<WORDS, kFewArguments>) <= kFewArguments;
+static_assert(fits<4> && fits<5> && fits<6> && fits<7>);
 constexpr unsigned long long kAddress = (1ull << 48) - 1;
 
 struct Step {
@@ -171,14 +178,14 @@ __device__ __forceinline__ float scale_of(const float (&v)[4]) {
 
 // The step of 1024 elements, four a thread.  Bound by HBM: 100 M floats with
 // 32-bit moments, 2.8 GB, in 470 us (6.0 TB/s), 400 M with 8-bit ones, 6.4 GB, in
-// 1043 us (6.2 TB/s).  Workgroups of one round: with two and four times the
+// 1043 us (6.2 TB/s).  No loop in a workgroup: with two and four times the
 // elements in flight a thread, 20 M elements in 300 tensors took 105 and 121 us
 // instead of 93.  8-bit: a wave's 64 x 4 elements are one block, whose maximum is
 // a reduction by lane swaps; its scales are one scalar load each.  With the
 // compiler's quotients and roots the vector unit bound it (106 % of its cycles
 // at 1138 us); the step itself needs neither to the last bit.
-template <class P, class G, int BITS, bool MASTER, bool NT>
-__global__ __launch_bounds__(kThreads) void k_adamw(Batch<words_of(BITS, MASTER)> b, int count, Step s) {
+template <class P, class G, int BITS, bool MASTER, bool NT, int BYTES>
+__global__ __launch_bounds__(kThreads) void k_adamw(Batch<words_of(BITS, MASTER), BYTES> b, int count, Step s) {
   const int i = tensor_of(b.first, count, blockIdx.x);
   const auto& word = b.word[i];
   // (named as global memory: of a pointer made out of a number the compiler would not know)
@@ -444,14 +451,23 @@ extern "C" int acdc_adamw_step(const acdc_adamw_tensor* tensors, int32_t count, 
   for (int cls = 0; cls < kClasses && rc == ACDC_OK; ++cls) {
     if (!(seen >> cls & 1)) continue;
     with_class(cls, [&]<class P, class G, int BITS, bool MASTER>() {
-      Batch<words_of(BITS, MASTER)> b;
+      Batch<words_of(BITS, MASTER), kArguments> b;
       int used = 0, rates = 0;
       long long blocks = 0;
       auto flush = [&] {
         if (used == 0 || rc != ACDC_OK) return;
         const dim3 grid(static_cast<unsigned>(blocks)), block(kThreads);
-        if (bytes >= kKeepBytes) hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, true>), grid, block, 0, st, b, used, s);
-        else hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, false>), grid, block, 0, st, b, used, s);
+        Batch<words_of(BITS, MASTER), kFewArguments> few;
+        if (bytes >= kKeepBytes) {
+          hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, true, kArguments>), grid, block, 0, st, b, used, s);
+        } else if (used > few.kMost) {
+          hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, false, kArguments>), grid, block, 0, st, b, used, s);
+        } else {
+          std::memcpy(few.word, b.word, size_t(used) * sizeof few.word[0]);
+          std::memcpy(few.rate, b.rate, size_t(rates) * sizeof few.rate[0]);
+          std::memcpy(few.first, b.first, size_t(used) * sizeof few.first[0]);
+          hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, false, kFewArguments>), grid, block, 0, st, few, used, s);
+        }
         used = rates = 0;
         blocks = 0;
         rc = done();

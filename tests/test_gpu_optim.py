@@ -152,6 +152,30 @@ def test_many_tensors_of_every_kind_in_one_call(env, bits):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("kind", ["f32", "master_f32"])
+@pytest.mark.parametrize("rates", [1, 11])
+def test_lists_of_every_length(env, kind, bits, rates):
+    """One kind of tensor: lists about as long as short and long arguments hold, and longer than any
+    launch's, with as many rates as a launch has and with more, to the bit as the tensors one by one."""
+    torch, optim = env
+    for count in (1, 6, 7, 8, 9, 10, 11, 12, 61, 62, 63, 64, 65, 70, 74, 75, 104, 105, 210):
+        print(f"[case] adamw list of {count} {kind} {bits} {rates}", flush=True)
+        lr = [LR * (1 + k % rates) for k in range(count)]
+        state = []
+        for together in (True, False):
+            params, grads, moments, masters, _ = problem(torch, optim, [1 + 37 * k % 1500 for k in range(count)], kind, bits,
+                                                         count)
+            for at in [slice(None)] if together else [slice(k, k + 1) for k in range(count)]:
+                optim.adamw_step(params[at], grads[at], moments[at], 5, lr=lr[at], betas=BETAS, eps=EPS, weight_decay=DECAY,
+                                 masters=masters[at] if masters else None)
+            state.append((params, moments, masters or []))
+        (p, m, w), (p1, m1, w1) = state
+        for a, b in zip([*p, *w, *(x for t in m for x in t)], [*p1, *w1, *(x for t in m1 for x in t)]):
+            bytes_a, bytes_b = a.view(torch.uint8), b.view(torch.uint8)
+            assert torch.equal(bytes_a, bytes_b)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_steps_follow_each_other(env, bits):
     """Fifty steps towards a minimum, first from zero moments: within the 8-bit
     moments' own error (one step in 16 of each update) of the steps in 64 bits."""
