@@ -5,12 +5,13 @@
 // the scales of 8-bit moments, one per 256 elements: the block's maximum has
 // to be known before its first code is written.
 //
-// The tensors' addresses travel in the kernels' arguments, up to 62 to 104 tensors
+// The tensors' addresses travel in the kernels' arguments, up to 62 to 157 tensors
 // a launch: nothing is uploaded, and no table outlives the call.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 #include "acdc_train.hpp"
 
@@ -23,34 +24,72 @@ constexpr int kChunk = kThreads * 4;  // elements a workgroup: four a thread, an
 constexpr float kPerTop = 1.f / 448.f;  // 448: largest e4m3 value
 constexpr float kTiny = 0x1p-9f;  // smallest positive one
 
-// A tensor is a few words of an address each, below 2^48, with 16 bits of
-// something else on top: its length in the first three, the index of its rate
-// in the fourth.  More tensors fit a launch's arguments that way, and fewer
-// launches drain and fill the card: 300 tensors, 560 MB, took 118 us with 48
-// whole records a launch, and 106 so.
-// A list that fits an eighth of that goes in arguments of that size: they are
-// copied whole at each launch, and three tensors of 256 floats, step after step,
-// take 4.8 us so and 6.2 with the long ones (eleven 4.8 and 5.2, and with 1024
-// bytes 5.1).
-//   0 param | n, 1 grad | n, 2 m | n, 3 v | rate, then m_scale and v_scale (8 bits), master
+// A tensor is a few words of an address each, below 2^48: param, grad, m, v, then
+// m_scale and v_scale (8 bits), master.  Three words have 16 bits of its length
+// on top, the fourth the index of its rate.  More tensors fit a launch's arguments
+// that way, and fewer launches drain and fill the card: 300 tensors, 560 MB, took
+// 118 us with 48 whole records a launch, and 106 so.
 constexpr int kArguments = 3840;  // bytes, of the 4 KB that a launch has
 constexpr int kFewArguments = 480;
 constexpr int kRates = 8;
+constexpr unsigned long long kAddress = (1ull << 48) - 1;
 struct Rate {
   float rate, decay;  // lr / (1 - beta1^step), 1 - lr * weight_decay
 };
+// A list that fits an eighth of the arguments goes in as many: they are copied
+// whole at each launch, and three tensors of 256 floats, step after step, take
+// 4.8 us so and 6.2 with the long ones (eleven 4.8 and 5.2, and with 1024 bytes
+// 5.1).
 template <int WORDS, int BYTES>
 struct Batch {
   static constexpr int kMost = int((BYTES - kRates * sizeof(Rate)) / (4 + 8 * WORDS));
   unsigned long long word[kMost][WORDS];
   Rate rate[kRates];
   int first[kMost];  // first workgroup of each tensor
+  void put(int i, const void* const (&p)[WORDS], unsigned long long n, int begin, int r) {
+    for (int k = 0; k < WORDS; ++k) {
+      const unsigned long long top = k < 3 ? n >> 16 * k & 0xffff : k == 3 ? (unsigned long long)r : 0;
+      word[i][k] = (unsigned long long)reinterpret_cast<uintptr_t>(p[k]) | top << 48;
+    }
+    first[i] = begin;
+  }
+  __device__ __forceinline__ unsigned long long address(int i, int k) const { return word[i][k] & kAddress; }
+  __device__ __forceinline__ long long length(int i) const {
+    return (long long)(word[i][0] >> 48 | word[i][1] >> 48 << 16 | word[i][2] >> 48 << 32);
+  }
+  __device__ __forceinline__ int rate_of(int i) const { return int(word[i][3] >> 48); }
+};
+// Longer lists go as 32-bit offsets from the lowest address of each kind where
+// those reach: in units of 16 bytes, and of 4 for the scales.  300 tensors with
+// 8-bit moments, 327 MB, take three launches for five so, 70 us for 75, and 200
+// with copies two for three, 765 us for 768.  In both forms the rate's index
+// lies with what is loaded anyway: beside the first workgroup, where its load
+// begins a little later, 400 M elements with 8-bit moments took 1050 us for 1032.
+template <int WORDS>
+struct NearBatch {
+  static constexpr int kMost = int((kArguments - kRates * sizeof(Rate) - 8 * WORDS) / (8 + 4 * WORDS));
+  static constexpr int shift(int k) { return WORDS >= 6 && (k == 4 || k == 5) ? 2 : 4; }
+  unsigned long long base[WORDS];
+  Rate rate[kRates];
+  unsigned offset[kMost][WORDS];
+  unsigned n[kMost];  // length | index of the rate << 29
+  int first[kMost];
+  void put(int i, const void* const (&p)[WORDS], unsigned long long length, int begin, int r) {
+    for (int k = 0; k < WORDS; ++k) offset[i][k] = unsigned((reinterpret_cast<uintptr_t>(p[k]) - base[k]) >> shift(k));
+    n[i] = unsigned(length) | unsigned(r) << 29;
+    first[i] = begin;
+  }
+  __device__ __forceinline__ unsigned long long address(int i, int k) const {
+    return base[k] + ((unsigned long long)offset[i][k] << shift(k));
+  }
+  __device__ __forceinline__ long long length(int i) const { return n[i] & ((1u << 29) - 1); }
+  __device__ __forceinline__ int rate_of(int i) const { return int(n[i] >> 29); }
 };
 constexpr int words_of(int bits, bool master) { return 4 + (bits == 8 ? 2 : 0) + (master ? 1 : 0); }
 template <int WORDS>
-constexpr bool fits = sizeof(Batch<WORDS, kArguments>) <= kArguments && sizeof(Batch<WORDS, kFewArguments>) <= kFewArguments;
-static_assert(fits<4> && fits<5> && fits<6> && fits<7>);
-constexpr unsigned long long kAddress = (1ull << 48) - 1;
+constexpr bool fits = sizeof(Batch<WORDS, kArguments>) <= kArguments &&
+                      sizeof(Batch<WORDS, kFewArguments>) <= kFewArguments && sizeof(NearBatch<WORDS>) <= kArguments;
+static_assert(kRates <= 8 && fits<4> && fits<5> && fits<6> && fits<7>);
 
 struct Step {
   double one1, one2;      // 1 - beta
@@ -184,13 +223,12 @@ __device__ __forceinline__ float scale_of(const float (&v)[4]) {
 // a reduction by lane swaps; its scales are one scalar load each.  With the
 // compiler's quotients and roots the vector unit bound it (106 % of its cycles
 // at 1138 us); the step itself needs neither to the last bit.
-template <class P, class G, int BITS, bool MASTER, bool NT, int BYTES>
-__global__ __launch_bounds__(kThreads) void k_adamw(Batch<words_of(BITS, MASTER), BYTES> b, int count, Step s) {
+template <class P, class G, int BITS, bool MASTER, bool NT, class LIST>
+__global__ __launch_bounds__(kThreads) void k_adamw(LIST b, int count, Step s) {
   const int i = tensor_of(b.first, count, blockIdx.x);
-  const auto& word = b.word[i];
   // (named as global memory: of a pointer made out of a number the compiler would not know)
   auto address = [&](int k) {
-    return (void*)reinterpret_cast<__attribute__((address_space(1))) void*>(word[k] & kAddress);
+    return (void*)reinterpret_cast<__attribute__((address_space(1))) void*>(b.address(i, k));
   };
   struct {
     void *param, *grad, *m, *v;
@@ -208,8 +246,8 @@ __global__ __launch_bounds__(kThreads) void k_adamw(Batch<words_of(BITS, MASTER)
     t.v_scale = static_cast<float*>(address(5));
   }
   if constexpr (MASTER) t.master = address(words_of(BITS, MASTER) - 1);
-  t.n = (long long)(word[0] >> 48 | word[1] >> 48 << 16 | word[2] >> 48 << 32);
-  const Rate rate = b.rate[word[3] >> 48];
+  t.n = b.length(i);
+  const Rate rate = b.rate[b.rate_of(i)];
   t.rate = rate.rate;
   t.decay = rate.decay;
   float c1 = s.c1, c2 = s.c2;
@@ -451,59 +489,100 @@ extern "C" int acdc_adamw_step(const acdc_adamw_tensor* tensors, int32_t count, 
   for (int cls = 0; cls < kClasses && rc == ACDC_OK; ++cls) {
     if (!(seen >> cls & 1)) continue;
     with_class(cls, [&]<class P, class G, int BITS, bool MASTER>() {
-      Batch<words_of(BITS, MASTER), kArguments> b;
-      int used = 0, rates = 0;
-      long long blocks = 0;
-      auto flush = [&] {
-        if (used == 0 || rc != ACDC_OK) return;
+      constexpr int kWords = words_of(BITS, MASTER);
+      using Long = Batch<kWords, kArguments>;
+      using Few = Batch<kWords, kFewArguments>;
+      using Near = NearBatch<kWords>;
+      auto launch = [&]<class LIST>(const LIST& b, int used, long long blocks) {
         const dim3 grid(static_cast<unsigned>(blocks)), block(kThreads);
-        Batch<words_of(BITS, MASTER), kFewArguments> few;
-        if (bytes >= kKeepBytes) {
-          hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, true, kArguments>), grid, block, 0, st, b, used, s);
-        } else if (used > few.kMost) {
-          hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, false, kArguments>), grid, block, 0, st, b, used, s);
-        } else {
-          std::memcpy(few.word, b.word, size_t(used) * sizeof few.word[0]);
-          std::memcpy(few.rate, b.rate, size_t(rates) * sizeof few.rate[0]);
-          std::memcpy(few.first, b.first, size_t(used) * sizeof few.first[0]);
-          hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, false, kFewArguments>), grid, block, 0, st, few, used, s);
+        if constexpr (!std::is_same_v<LIST, Few>) {
+          if (bytes >= kKeepBytes) {
+            hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, true, LIST>), grid, block, 0, st, b, used, s);
+            return;
+          }
         }
-        used = rates = 0;
-        blocks = 0;
-        rc = done();
+        hipLaunchKernelGGL((k_adamw<P, G, BITS, MASTER, false, LIST>), grid, block, 0, st, b, used, s);
       };
-      for (int32_t i = 0; i < count; ++i) {
+      auto addresses = [](const acdc_adamw_tensor& t, const void* (&p)[kWords]) {
+        p[0] = t.param;
+        p[1] = t.grad;
+        p[2] = t.m;
+        p[3] = t.v;
+        if constexpr (BITS == 8) {
+          p[4] = t.m_scale;
+          p[5] = t.v_scale;
+        }
+        if constexpr (MASTER) p[kWords - 1] = t.master;
+      };
+      auto all = [&]<class LIST>(LIST& b) {
+        int used = 0, rates = 0;
+        long long blocks = 0;
+        auto flush = [&] {
+          if (used == 0) return;
+          bool launched = false;
+          if constexpr (std::is_same_v<LIST, Long>) {
+            if (used <= Few::kMost && bytes < kKeepBytes) {
+              Few few;
+              std::memcpy(few.word, b.word, size_t(used) * sizeof few.word[0]);
+              std::memcpy(few.rate, b.rate, size_t(rates) * sizeof few.rate[0]);
+              std::memcpy(few.first, b.first, size_t(used) * sizeof few.first[0]);
+              launch(few, used, blocks);
+              launched = true;
+            }
+          }
+          if (!launched) launch(b, used, blocks);
+          used = rates = 0;
+          blocks = 0;
+          rc = done();
+        };
+        for (int32_t i = 0; i < count; ++i) {
+          const acdc_adamw_tensor& t = tensors[i];
+          if (t.n == 0 || class_of(t) != cls) continue;
+          const Rate rate{float(double(t.lr) / c1), float(1.0 - double(t.lr) * double(t.weight_decay))};
+          const long long need = (t.n + kChunk - 1) / kChunk;
+          int k = 0;
+          while (k < rates && !(b.rate[k].rate == rate.rate && b.rate[k].decay == rate.decay)) ++k;
+          if (used == LIST::kMost || blocks + need > kMaxBlocks || k == kRates) {
+            flush();
+            if (rc != ACDC_OK) return;
+            k = 0;
+          }
+          if (k == rates) b.rate[rates++] = rate;
+          const void* p[kWords];
+          addresses(t, p);
+          b.put(used, p, (unsigned long long)t.n, int(blocks), k);
+          ++used;
+          blocks += need;
+        }
+        flush();
+      };
+      int of_class = 0;
+      bool near = count > Long::kMost;
+      uintptr_t low[kWords], high[kWords];
+      for (int k = 0; k < kWords; ++k) low[k] = ~uintptr_t(0), high[k] = 0;
+      for (int32_t i = 0; near && i < count; ++i) {
         const acdc_adamw_tensor& t = tensors[i];
         if (t.n == 0 || class_of(t) != cls) continue;
-        const Rate rate{float(double(t.lr) / c1), float(1.0 - double(t.lr) * double(t.weight_decay))};
-        const long long need = (t.n + kChunk - 1) / kChunk;
-        int k = 0;
-        while (k < rates && !(b.rate[k].rate == rate.rate && b.rate[k].decay == rate.decay)) ++k;
-        if (used == b.kMost || blocks + need > kMaxBlocks || k == kRates) {
-          flush();
-          if (rc != ACDC_OK) return;
-          k = 0;
+        ++of_class;
+        near = near && t.n < 1ll << 29;
+        const void* p[kWords];
+        addresses(t, p);
+        for (int k = 0; k < kWords; ++k) {
+          const uintptr_t a = reinterpret_cast<uintptr_t>(p[k]);
+          near = near && (a & ((1u << Near::shift(k)) - 1)) == 0;
+          low[k] = a < low[k] ? a : low[k];
+          high[k] = a > high[k] ? a : high[k];
         }
-        if (k == rates) b.rate[rates++] = rate;
-        const unsigned long long n = (unsigned long long)t.n;
-        auto word = [](const void* p, unsigned long long top) {
-          return (unsigned long long)reinterpret_cast<uintptr_t>(p) | top << 48;
-        };
-        auto& w = b.word[used];
-        w[0] = word(t.param, n & 0xffff);
-        w[1] = word(t.grad, n >> 16 & 0xffff);
-        w[2] = word(t.m, n >> 32);
-        w[3] = word(t.v, (unsigned long long)k);
-        if constexpr (BITS == 8) {
-          w[4] = word(t.m_scale, 0);
-          w[5] = word(t.v_scale, 0);
-        }
-        if constexpr (MASTER) w[words_of(BITS, MASTER) - 1] = word(t.master, 0);
-        b.first[used] = int(blocks);
-        ++used;
-        blocks += need;
       }
-      flush();
+      for (int k = 0; k < kWords; ++k) near = near && (high[k] - low[k]) >> Near::shift(k) >> 32 == 0;
+      if (near && of_class > Long::kMost) {
+        Near b;
+        for (int k = 0; k < kWords; ++k) b.base[k] = low[k];
+        all(b);
+      } else {
+        Long b;
+        all(b);
+      }
     });
   }
   return rc;

@@ -175,6 +175,90 @@ def test_lists_of_every_length(env, kind, bits, rates):
             assert torch.equal(bytes_a, bytes_b)
 
 
+def same_as_one_by_one(torch, optim, make):
+    """The step of a list, to the bit that of its tensors one by one; `make` builds the same list twice."""
+    state = []
+    for together in (True, False):
+        params, grads, moments, masters = make()
+        count = len(params)
+        lr = [LR * (1 + k % 3) for k in range(count)]
+        for at in [slice(None)] if together else [slice(k, k + 1) for k in range(count)]:
+            optim.adamw_step(params[at], grads[at], moments[at], 5, lr=lr[at], betas=BETAS, eps=EPS, weight_decay=DECAY,
+                             masters=masters[at] if masters else None)
+        state.append([x.clone().view(torch.uint8) for x in [*params, *(masters or []), *(x for t in moments for x in t)]])
+    assert all(torch.equal(a, b) for a, b in zip(*state))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("kind", ["f32", "master"])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_long_lists(env, kind, bits, shift):
+    """Lists about as long as a launch takes as offsets, and with one tensor off their alignment."""
+    torch, optim = env
+    for count in (102, 103, 116, 117, 133, 134, 156, 157, 320):
+        print(f"[case] adamw long list of {count} {kind} {bits} shift={shift}", flush=True)
+
+        def make():
+            lists = problem(torch, optim, [1 + 53 * k % 2900 for k in range(count)], kind, bits, count)[:4]
+            if bits == 8:  # all scales in one buffer, a float apart
+                scales = [torch.cat([m[j] for m in lists[2]]) for j in (2, 3)]
+                at = np.cumsum([0, *(len(m[2]) for m in lists[2])])
+                for k, m in enumerate(lists[2]):
+                    lists[2][k] = (*m[:2], *(x[at[k]:at[k + 1]] for x in scales))
+            if shift:
+                odd = problem(torch, optim, [777], kind, bits, 1, shift)[:4]
+                for x, y in zip(lists, odd):
+                    if x is not None:
+                        x[count // 2] = y[0]
+            return lists
+
+        same_as_one_by_one(torch, optim, make)
+
+
+def test_long_list_with_a_large_tensor(env):
+    """A list of offsets holds tensors of up to 2^29 - 1 elements: one at that length, one longer."""
+    torch, optim = env
+    for large in ((1 << 29) - 1, (1 << 29) + 5):
+        print(f"[case] adamw long list with {large} elements", flush=True)
+
+        def make():
+            lists = problem(torch, optim, [1 + 53 * k % 2900 for k in range(110)], "bf16", 8, 4)[:4]
+            lists[0][70] = torch.full((large,), 1.0, dtype=torch.bfloat16, device="cuda")
+            lists[1][70] = torch.full((large,), 0.5, dtype=torch.bfloat16, device="cuda")
+            lists[1][70][-3:] = 2.0
+            lists[2][70] = optim.moments(lists[0][70], 8)
+            return lists
+
+        same_as_one_by_one(torch, optim, make)
+        torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("span", [60, 66])
+def test_lists_far_apart(env, span):
+    """Tensors up to `span` GiB from each other, inside and outside what 32 bits of 16 bytes reach."""
+    torch, optim = env
+    if torch.cuda.mem_get_info()[0] < 90e9:
+        pytest.skip("not enough free memory")
+    size = (span << 30) + (5 << 30)
+    room = torch.empty(size, dtype=torch.uint8, device="cuda")
+    count, n = 130, 1000
+    rng = np.random.RandomState(9)
+    values = [torch.from_numpy((0.1 * rng.randn(4, n)).astype(np.float32)) for _ in range(count)]
+
+    def make():
+        lists = [[], [], [], []]
+        for k in range(count):
+            for j in range(4):
+                at = ((span << 30) * (k % 7) // 6 + 16384 * (k + 200 * j)) // 16 * 16
+                t = room[at:at + 4 * n].view(torch.float32)
+                t.copy_(values[k][j].abs() if j == 3 else values[k][j])
+                lists[j].append(t)
+        return lists[0], lists[1], list(zip(lists[2], lists[3])), None
+
+    print(f"[case] adamw list over {span} GB", flush=True)
+    same_as_one_by_one(torch, optim, make)
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_steps_follow_each_other(env, bits):
     """Fifty steps towards a minimum, first from zero moments: within the 8-bit
