@@ -157,12 +157,13 @@ __device__ __forceinline__ Run run_of(const typename T::Elem* body, int c, int s
   return b;
 }
 
-// Workgroup over a row that THREADS lanes share: a wave (64), which needs no
-// barrier, or the workgroup.
+// Over a row that THREADS lanes share: 16 or a wave (64), which need no barrier,
+// or the workgroup.
 template <int THREADS>
 struct Group {
   float* slots;  // 3 * THREADS / 64 floats of LDS
   __device__ __forceinline__ float max(float v) {
+    if constexpr (THREADS == 16) return over_16(v, [](float p, float q) { return fmaxf(p, q); });
     v = wave_max(v);
     if constexpr (THREADS > 64) {
       if (threadIdx.x % 64 == 0) slots[threadIdx.x / 64] = v;
@@ -175,6 +176,11 @@ struct Group {
   // s and u over the group; the slots are those that max does not use, so that
   // a barrier a call is enough (the next row's max comes after this one's barrier)
   __device__ __forceinline__ void sum(float& s, float& u) {
+    if constexpr (THREADS == 16) {
+      s = over_16(s, [](float p, float q) { return p + q; });
+      u = over_16(u, [](float p, float q) { return p + q; });
+      return;
+    }
     s = wave_sum(s);
     u = wave_sum(u);
     if constexpr (THREADS > 64) {
@@ -194,37 +200,50 @@ struct Group {
   }
 };
 
-// A workgroup's part of a row, streamed: every thread keeps a run of its own.
-// Item r * split + k is part k of row r; with split = 1 its workgroup writes the
+// Rows that LANES lanes share, several to a workgroup where those are few.
+template <int LANES>
+struct Share {
+  static constexpr int WG = LANES < kThreads ? kThreads : LANES, ROWS = WG / LANES;
+  static __device__ __forceinline__ int lane() { return ROWS == 1 ? int(threadIdx.x) : int(threadIdx.x) % LANES; }
+  static __device__ __forceinline__ unsigned first() {
+    if constexpr (ROWS == 1) return blockIdx.x;
+    const int row = int(threadIdx.x) / LANES;
+    return blockIdx.x * ROWS + unsigned(LANES == 64 ? uniform(row) : row);
+  }
+};
+
+// A part of a row, streamed: every thread keeps a run of its own.
+// Item r * split + k is part k of row r; with split = 1 its lanes write the
 // row's (M, S, H, logp), otherwise the runs of the parts.  Bound by HBM: 19.9 k
 // rows of 32768 bfloat16, 1.3 GB, in 220 us (5.9 TB/s; the vector unit 81 % busy).
-template <class T, int THREADS>
-__global__ __launch_bounds__(THREADS) void k_row_stats(const typename T::Elem* __restrict__ x, long long stride,
-                                                       const void* __restrict__ targets, int bits, int classes,
-                                                       int split, unsigned items, RowOut out,
-                                                       float4* __restrict__ parts) {
-  __shared__ float slots[3 * (THREADS / 64)];
-  Group<THREADS> group{slots};
-  for (unsigned item = blockIdx.x; item < items; item += gridDim.x) {
+template <class T, int LANES>
+__global__ __launch_bounds__(Share<LANES>::WG) void k_row_stats(const typename T::Elem* __restrict__ x,
+                                                                long long stride, const void* __restrict__ targets,
+                                                                int bits, int classes, int split, unsigned items,
+                                                                RowOut out, float4* __restrict__ parts) {
+  __shared__ float slots[3 * Share<LANES>::WG / 64];
+  Group<LANES> group{slots};
+  const int lane = Share<LANES>::lane();
+  for (unsigned item = Share<LANES>::first(); item < items; item += gridDim.x * Share<LANES>::ROWS) {
     const int k = item % unsigned(split);
     const long long r = item / unsigned(split);
     const long long t = target_of(targets, bits, r);
     if (t < 0) {
-      if (threadIdx.x == 0 && k == 0) put_row(out, r, make_float4(0.f, 1.f, 0.f, 0.f), 0.f, 0.f);
+      if (lane == 0 && k == 0) put_row(out, r, make_float4(0.f, 1.f, 0.f, 0.f), 0.f, 0.f);
       continue;
     }
     const typename T::Elem* row = x + r * stride;
     const float xt = split == 1 ? target_logit<T>(row, t, classes) : 0.f;
     Run run = empty_run();
-    const Cut<T> cut(row, classes);
+    const Cut<T, (LANES >= 64)> cut(row, classes);
     int from, to;
     chunks_of(cut.full, split, k, from, to);
     const typename T::Elem* body = row + cut.head;
-    stream<kAhead>(from + threadIdx.x, to, THREADS, [&]<int N, bool ALL>(int c) {
-      run = merge(run, run_of<T, N, ALL>(body, c, THREADS, to));
+    stream<kAhead>(from + lane, to, LANES, [&]<int N, bool ALL>(int c) {
+      run = merge(run, run_of<T, N, ALL>(body, c, LANES, to));
     });
-    if (k == split - 1 && int(threadIdx.x) < cut.extra) {
-      const float v = T::one(row[cut.element(threadIdx.x)]);
+    if (k == split - 1 && lane < cut.extra) {
+      const float v = T::one(row[cut.element(lane)]);
       Run b = empty_run();
       b.m = fmaxf(b.m, v);
       const float d = v - b.m, e = exp_of(d);
@@ -235,7 +254,7 @@ __global__ __launch_bounds__(THREADS) void k_row_stats(const typename T::Elem* _
     const float m = group.max(run.m), d = below(run.m, m), f = exp_of(d);
     float s = run.s * f, u = f * (run.u + d * run.s);
     group.sum(s, u);
-    if (threadIdx.x == 0) {
+    if (lane == 0) {
       if (split == 1) put_row(out, r, stat_of(Run{m, s, u}, xt), 0.f, 0.f);
       else parts[r * split + k] = make_float4(m, s, u, 0.f);
     }
@@ -324,7 +343,7 @@ __device__ __forceinline__ void slopes(const Slope& sl, const typename T::Elem* 
 // the last rows first: what a forward read last is what the cache still holds.
 // Bound by HBM: 26.4 k rows of 32768 bfloat16, a quarter of them idle, read 1.3
 // and write 1.73 GB in 545 us (5.6 TB/s).
-template <class T>
+template <class T, int LANES>
 __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x, long long stride,
                                                        const void* __restrict__ targets, int bits, int classes,
                                                        const float4* __restrict__ stat,
@@ -333,7 +352,9 @@ __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x
                                                        const float* __restrict__ scale, float scale_host,
                                                        typename T::Elem* grad, long long grad_stride, int split,
                                                        unsigned items) {
-  for (unsigned item = blockIdx.x; item < items; item += gridDim.x) {
+  static_assert(LANES <= kThreads);
+  const int lane = Share<LANES>::lane();
+  for (unsigned item = Share<LANES>::first(); item < items; item += gridDim.x * Share<LANES>::ROWS) {
     const unsigned at = items - 1 - item;
     const int k = at % unsigned(split);
     const long long r = at / unsigned(split);
@@ -344,16 +365,16 @@ __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x
     const float4 st = stat[r];
     float g = grad_logp[r], h = grad_entropy != nullptr ? grad_entropy[r] : 0.f;  // (asked for along with the target)
     if (t < 0) g = h = 0.f;
-    const Cut<T> cut(row, classes);
+    const Cut<T, (LANES >= 64)> cut(row, classes);
     int from, to;
     chunks_of(cut.full, split, k, from, to);
-    const int one = cut.element(threadIdx.x);
-    const bool has_one = k == split - 1 && int(threadIdx.x) < cut.extra;
+    const int one = cut.element(lane);
+    const bool has_one = k == split - 1 && lane < cut.extra;
     const typename T::Elem* body = row + cut.head;
     typename T::Elem* out_body = out + cut.head;
     if (g == 0.f && h == 0.f) {
       float zero[T::kPer] = {};
-      for (int i = from + threadIdx.x; i < to; i += kThreads)
+      for (int i = from + lane; i < to; i += LANES)
         store_chunk<T>(out_body + (long long)i * T::kPer, T::pack(zero));
       if (has_one) out[one] = T::to(0.f);
       continue;
@@ -366,12 +387,12 @@ __global__ __launch_bounds__(kThreads) void k_row_grad(const typename T::Elem* x
     bool mine = false;
     if (t < classes) {
       const int tc = cut.chunk_of(int(t));
-      mine = tc >= 0 ? tc >= from && tc < to && (tc - from) % kThreads == int(threadIdx.x)
-                     : has_one && cut.lane_of(int(t)) == int(threadIdx.x);
+      mine = tc >= 0 ? tc >= from && tc < to && (tc - from) % LANES == lane
+                     : has_one && cut.lane_of(int(t)) == lane;
     }
     const float yt = mine ? slope_value(sl, T::one(row[t])) + g : 0.f;
-    stream<kAhead>(from + threadIdx.x, to, kThreads, [&]<int N, bool ALL>(int i) {
-      slopes<T, N, ALL>(sl, body, out_body, i, kThreads, to);
+    stream<kAhead>(from + lane, to, LANES, [&]<int N, bool ALL>(int i) {
+      slopes<T, N, ALL>(sl, body, out_body, i, LANES, to);
     });
     if (has_one) out[one] = T::to(slope_value(sl, T::one(row[one])));
     if (mine) out[t] = T::to(yt);
@@ -1196,20 +1217,29 @@ struct Logits {
 // Workgroups of a launch over `items`: a grid holds fewer than 2^32 lanes.
 unsigned grid_for(unsigned items) { return std::min(items, 1u << 22); }
 
+// Chunks up to which a wave takes a row in the passes over logits; up to a round of
+// 16 lanes those do.  A workgroup a row is bound by how fast workgroups begin, some
+// 700 a us: 40000 rows, statistics and gradient, of 78 floats take 16 us for 95, of
+// 600 47 for 99, of 1500 104 for 117, 10000 of 78 14 for 28, of 2040 42 for 41.
+constexpr int64_t kWaveChunks = 512;
+
 // Row statistics into `out`; rows in parts (split > 1) leave their parts only.
 int launch_stats(const Logits& l, int split, const RowOut& out, float4* parts, hipStream_t s) {
   with_type(l.dtype, [&]<class T>() {
-    auto go = [&](auto kernel, int threads) {
+    auto go = [&]<int LANES>() {
       const unsigned items = unsigned(l.rows * split);
-      hipLaunchKernelGGL(kernel, dim3(grid_for(items)), dim3(threads), 0, s,
+      using Rows = Share<LANES>;
+      hipLaunchKernelGGL((k_row_stats<T, LANES>), dim3(grid_for((items + Rows::ROWS - 1) / Rows::ROWS)), dim3(Rows::WG), 0, s,
                          static_cast<const typename T::Elem*>(l.x), (long long)l.stride, l.targets, l.bits, l.classes,
                          split, items, out, parts);
     };
     // as many lanes as ask for a part of a row in one or two rounds of kAhead chunks
     // (19.9 k rows of 32768 bfloat16: 250 us with 256 lanes, 238 with 512)
     const int64_t chunks = l.classes / T::kPer / split;
-    if (chunks > 2 * kAhead * kThreads) go(k_row_stats<T, 512>, 512);
-    else go(k_row_stats<T, kThreads>, kThreads);
+    if (chunks <= 16 * kAhead) go.template operator()<16>();
+    else if (chunks <= kWaveChunks) go.template operator()<64>();
+    else if (chunks <= 2 * kAhead * kThreads) go.template operator()<kThreads>();
+    else go.template operator()<512>();
   });
   return done();
 }
@@ -1231,10 +1261,17 @@ int launch_grad(const Logits& l, const float4* stat, const float* g, const float
   const int split = split_of(l.rows, l.classes, l.dtype);
   with_type(l.dtype, [&]<class T>() {
     const unsigned items = unsigned(l.rows * split);
-    hipLaunchKernelGGL(k_row_grad<T>, dim3(grid_for(items)), dim3(kThreads), 0, s,
-                       static_cast<const typename T::Elem*>(l.x), (long long)l.stride, l.targets, l.bits, l.classes,
-                       stat, g, h, scale, scale_host, static_cast<typename T::Elem*>(grad), (long long)grad_stride,
-                       split, items);
+    auto go = [&]<int LANES>() {
+      constexpr unsigned per = Share<LANES>::ROWS;
+      hipLaunchKernelGGL((k_row_grad<T, LANES>), dim3(grid_for((items + per - 1) / per)), dim3(kThreads), 0, s,
+                         static_cast<const typename T::Elem*>(l.x), (long long)l.stride, l.targets, l.bits, l.classes,
+                         stat, g, h, scale, scale_host, static_cast<typename T::Elem*>(grad), (long long)grad_stride,
+                         split, items);
+    };
+    const int64_t chunks = l.classes / T::kPer / split;
+    if (chunks <= 16 * kAhead) go.template operator()<16>();
+    else if (chunks <= kWaveChunks) go.template operator()<64>();
+    else go.template operator()<kThreads>();
   });
   return done();
 }

@@ -440,3 +440,38 @@ def test_more_rows_than_a_grid_has_workgroups(env):
     q = losses.policy_loss(x, t, r.logp, g, grad=False)
     # every ratio is 1 and every advantage 1
     assert q.stats[:2].tolist() == pytest.approx([-1.0, -1.0], rel=1e-6) and q.stats[5].item() == pytest.approx(1.0, rel=1e-6)
+
+
+# around the chunks that 16 lanes, a wave and a workgroup take a row at, a chunk being 16 bytes;
+# rows that fill no whole workgroup, on and off their chunks' alignment
+WIDTHS = [(dtype, per * chunks + more) for dtype, per in (("float32", 4), ("bfloat16", 8))
+          for chunks, more in ((0, 2), (16, 1), (48, 0), (63, 1), (64, 0), (65, 0), (192, 3), (256, 1), (512, 0), (513, 0))]
+
+
+@pytest.mark.parametrize("dtype,classes", WIDTHS)
+@pytest.mark.parametrize("apart", [0, 3])
+def test_rows_that_share_a_workgroup(env, dtype, classes, apart):
+    for rows in (1, 3, 18, 133):
+        shape = rows, classes, classes + apart, dtype, 64
+        test_token_logprobs_and_gradient(env, shape)
+        if rows > 3:
+            test_preference_loss(env, shape)
+
+
+def test_more_short_rows_than_a_grid_has_lanes_for(env):
+    """Over 2^26 rows, 16 to a workgroup: each workgroup takes several lots."""
+    torch, losses = env
+    rows, V = (1 << 26) + 1000, 2
+    print(f"[case] {rows} x {V}", flush=True)
+    x = torch.randn(rows, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    t = torch.arange(rows, device="cuda", dtype=torch.int32) % V
+    t[::7] = -1
+    r = losses.token_logprobs(x, t, entropy=True, save=True)
+    g = torch.ones(rows, device="cuda")
+    grad = losses.token_logprobs_backward(x, t, r.saved, g)
+    pick = torch.cat([torch.arange(2000), torch.arange(rows - 3000, rows)]).cuda()
+    xs, ts = x[pick].double().cpu().numpy(), t[pick].cpu().numpy()
+    on = ts >= 0
+    p, logp, ent, spread = R.rows(xs, np.clip(ts, 0, None))
+    close(r.logp[pick], np.where(on, logp, 0.0), R.logp_tolerance(logp, spread), "logp")
+    check_gradient(grad[pick], xs, ts, on, np.ones(len(ts)), np.zeros(len(ts)), False)
