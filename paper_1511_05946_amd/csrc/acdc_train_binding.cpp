@@ -61,6 +61,8 @@ int32_t type_of(const Tensor& t) {
   const auto s = t.scalar_type();
   return s == at::kFloat ? ACDC_F32 : s == at::kBFloat16 ? ACDC_BF16 : -1;
 }
+// A view marked as conjugated or negated: its memory does not hold its values.
+bool lazy(const Tensor& t) { return t.is_conj() || t.is_neg(); }
 bool vector_of(const Tensor* t, int64_t n, const at::Device& device, at::ScalarType type) {
   return t == nullptr || (t->dim() == 1 && t->size(0) == n && t->scalar_type() == type && t->device() == device &&
                           t->is_contiguous());
@@ -329,7 +331,8 @@ struct Numbers {
 };
 
 bool plain(const Tensor* t, int64_t numel, const at::Device& device, at::ScalarType type) {
-  return t != nullptr && t->scalar_type() == type && t->numel() == numel && t->device() == device && t->is_contiguous();
+  return t != nullptr && t->scalar_type() == type && t->numel() == numel && t->device() == device && t->is_contiguous() &&
+         !lazy(*t);
 }
 
 // (params, grads, moments, masters, lr, weight_decay, beta1, beta2, eps, step, grad_scale, stream) -> status
@@ -360,7 +363,8 @@ PyObject* adamw(PyObject*, PyObject* const* args, Py_ssize_t n) {
     for (Py_ssize_t i = 0; i < count; ++i) {
       const Tensor *p = params.tensor(i), *g = grads.tensor(i);
       if (p == nullptr || g == nullptr || type_of(*p) < 0 || type_of(*g) < 0 || !p->is_contiguous() ||
-          p->device() != device || g->sizes() != p->sizes() || g->device() != device || !g->is_contiguous())
+          p->device() != device || g->sizes() != p->sizes() || g->device() != device || !g->is_contiguous() || lazy(*p) ||
+          lazy(*g))
         Py_RETURN_NONE;
       const int64_t numel = p->numel();
       acdc_adamw_tensor& r = records[size_t(i)];
@@ -413,7 +417,7 @@ PyObject* grad_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
       sizes[size_t(i)] = g->numel();
       types[size_t(i)] = type_of(*g);
     }
-    if (!floats(out, 2, device)) Py_RETURN_NONE;
+    if (!floats(out, 2, device) || (out != nullptr && lazy(*out))) Py_RETURN_NONE;
     const size_t need = acdc_grad_norm_workspace_size(sizes.data(), int32_t(count));
     Tensor ws = at::empty({int64_t(std::max<size_t>(need, 1))}, first->options().dtype(at::kByte));
     Tensor result = out != nullptr ? *out : at::empty({2}, first->options().dtype(at::kFloat));

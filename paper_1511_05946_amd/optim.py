@@ -5,7 +5,8 @@ libacdc.so: the step that turns a cascade's ``grad_A``, ``grad_D`` and
 Argument marshalling only; the work is enqueued on the current torch stream.
 Parameters are float32, bfloat16 or complex64 (stepped as pairs of reals, as
 the cascade's gradients of complex layers are dL/dRe + i dL/dIm), contiguous;
-gradients float32 or bfloat16 (complex64 for complex parameters).
+gradients float32 or bfloat16 (complex64 for complex parameters), conjugate
+views among them.
 
 The moments of a tensor are made by ``moments(param, bits)``:
 
@@ -32,6 +33,12 @@ _RECORD = struct.Struct("=7Qqffii")   # struct acdc_adamw_tensor
 
 def _real_numel(t) -> int:
     return 2 * t.numel() if t.dtype is torch.complex64 else t.numel()
+
+
+def _lazy(t) -> bool:
+    """A view that torch marks as conjugated or negated without touching the
+    memory that it shares with its base."""
+    return t.is_conj() or t.is_neg()
 
 
 def _native_stream(tensors):
@@ -68,6 +75,8 @@ def _refuse_moments(i, state, n, device):
         if t.dtype is not want or t.numel() != size or not t.is_contiguous() or t.device != device:
             raise ValueError(f"moments[{i}][{k}] must be {size} contiguous {want} values on {device}, got "
                              f"{tuple(t.shape)} {t.dtype} on {t.device}")
+        if _lazy(t):
+            raise ValueError(f"moments[{i}][{k}] is a conjugate or negative view")
 
 
 def _refuse(i, p, g, master, n, device):
@@ -82,6 +91,8 @@ def _refuse(i, p, g, master, n, device):
     if master is not None and (p.dtype is not torch.bfloat16 or master.dtype is not torch.float32 or
                                master.numel() != n or not master.is_contiguous() or master.device != device):
         raise ValueError(f"masters[{i}] must be the contiguous float32 copy of a bfloat16 parameter of {n} elements")
+    if _lazy(p) or (master is not None and _lazy(master)):
+        raise ValueError(f"params[{i}] and its master must not be conjugate or negative views: they are written in place")
 
 
 def adamw_step(params, grads, moments, step: int, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01,
@@ -115,12 +126,16 @@ def adamw_step(params, grads, moments, step: int, lr=1e-3, betas=(0.9, 0.999), e
     device = params[0].device
     size = _RECORD.size
     records = bytearray(size * count)
+    resolved = []   # (kept until the step is enqueued)
     for i in range(count):
         p, g, state = params[i], grads[i], moments[i]
         master = masters[i] if masters is not None else None
         n = _real_numel(p)
         _refuse(i, p, g, master, n, device)
         _refuse_moments(i, state, n, device)
+        if _lazy(g):   # as autograd hands out the gradient of a parameter that was used conjugated
+            g = g.resolve_conj().resolve_neg()
+            resolved.append(g)
         scales = (state[2].data_ptr(), state[3].data_ptr()) if len(state) == 4 else (0, 0)
         if len(state) == 4 and n > 0 and not (scales[0] and scales[1]):
             raise ValueError(f"moments[{i}] has scales without memory")
@@ -130,6 +145,8 @@ def adamw_step(params, grads, moments, step: int, lr=1e-3, betas=(0.9, 0.999), e
     if grad_scale is not None and (grad_scale.numel() != 1 or grad_scale.dtype is not torch.float32 or
                                    grad_scale.device != device):
         raise ValueError(f"grad_scale must be one float32 value on {device}")
+    if grad_scale is not None:
+        grad_scale = grad_scale.resolve_neg()
     buf = (ctypes.c_char * len(records)).from_buffer(records)
     rc = _call(lib().acdc_adamw_step, device, ctypes.addressof(buf), count, float(betas[0]), float(betas[1]),
                float(eps), int(step), None if grad_scale is None else grad_scale.data_ptr())
@@ -163,7 +180,8 @@ def grad_norm(grads, max_norm=None, out=None):
         types.append(_TYPES[g.dtype])
     if out is None:
         out = torch.empty(2, device=device)
-    elif out.shape != (2,) or out.dtype is not torch.float32 or out.device != device or not out.is_contiguous():
+    elif out.shape != (2,) or out.dtype is not torch.float32 or out.device != device or not out.is_contiguous() or \
+            _lazy(out):
         raise ValueError(f"out must be a contiguous float32 vector of 2 values on {device}")
     ptrs, sizes, types = struct.pack(f"{count}Q", *ptrs), struct.pack(f"{count}q", *sizes), struct.pack(f"{count}i", *types)
     need = lib().acdc_grad_norm_workspace_size(sizes, count)

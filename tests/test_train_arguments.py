@@ -1,0 +1,60 @@
+"""Arguments of the losses and the optimiser whose memory is not what their
+values say, or that no call may take (CPU: the binding's own checks)."""
+
+import ctypes
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The binding on CPU tensors: the arguments of its library calls instead of the calls."""
+    from paper_1511_05946_amd import losses, optim
+    made = []
+
+    def call(fn, device, *args):
+        made.append(args)
+        return 0
+
+    monkeypatch.setattr(losses, "_call", call)
+    monkeypatch.setattr(optim, "_call", call)
+    return made
+
+
+def conjugate_gradient(n=6):
+    """A parameter and its gradient as autograd hands it out where the loss takes the conjugate."""
+    w = torch.randn(n, dtype=torch.complex64).requires_grad_(True)
+    (w.conj() * torch.randn(n, dtype=torch.complex64)).real.sum().backward()
+    assert w.grad.is_conj()
+    return w.detach(), w.grad
+
+
+def test_step_takes_the_values_of_a_conjugate_gradient(calls, monkeypatch):
+    from paper_1511_05946_amd import optim
+    seen = []
+
+    def call(fn, device, records, count, *rest):
+        grad = ctypes.c_void_p.from_address(records + 16).value
+        seen.extend((ctypes.c_float * 12).from_address(grad))
+        return 0
+
+    monkeypatch.setattr(optim, "_call", call)
+    p, g = conjugate_gradient()
+    optim.adamw_step([p], [g], [optim.moments(p)], 1)
+    assert seen == torch.view_as_real(g.resolve_conj()).reshape(-1).tolist()
+
+
+def test_step_refuses_views_that_it_would_write_wrongly(calls):
+    from paper_1511_05946_amd import optim
+    p, g = conjugate_gradient()
+    r = torch.ones(6)
+    half, neg = r.bfloat16(), torch._neg_view(r)
+    for args, kw in ((([p.conj()], [g], [optim.moments(p)]), {}), (([neg], [r], [optim.moments(r)]), {}),
+                     (([r], [r.clone()], [(neg, r.clone())]), {}), (([half], [r], [optim.moments(r)]), dict(masters=[neg]))):
+        with pytest.raises(ValueError, match="view"):
+            optim.adamw_step(*args, 1, **kw)
+    with pytest.raises(ValueError):
+        optim.grad_norm([r], out=torch._neg_view(torch.zeros(2)))
+    assert not calls
