@@ -65,7 +65,7 @@ int32_t type_of(const Tensor& t) {
 bool lazy(const Tensor& t) { return t.is_conj() || t.is_neg(); }
 bool vector_of(const Tensor* t, int64_t n, const at::Device& device, at::ScalarType type) {
   return t == nullptr || (t->dim() == 1 && t->size(0) == n && t->scalar_type() == type && t->device() == device &&
-                          t->is_contiguous());
+                          t->is_contiguous() && !lazy(*t));
 }
 bool floats(const Tensor* t, int64_t n, const at::Device& device) { return vector_of(t, n, device, at::kFloat); }
 int32_t index_bits(const Tensor& t, int64_t n, const at::Device& device) {
@@ -91,7 +91,7 @@ struct Logits {
   static int64_t step(const Tensor& t) { return t.size(0) <= 1 ? std::max(t.stride(0), t.size(1)) : t.stride(0); }
   static bool plain(const Tensor& t) {
     return t.dim() == 2 && t.is_cuda() && type_of(t) >= 0 && t.size(1) >= 1 && t.size(1) <= 0x7fffffff &&
-           (t.size(1) == 1 || t.stride(1) == 1) && step(t) >= t.size(1);
+           (t.size(1) == 1 || t.stride(1) == 1) && step(t) >= t.size(1) && !lazy(t);
   }
   Tensor make(at::IntArrayRef size) const { return at::empty(size, x->options().dtype(at::kFloat)); }
   // the gradient's tensor: `out`, or a new one
@@ -200,7 +200,7 @@ PyObject* logprobs_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (a.bad || !l.read(x, t)) Py_RETURN_NONE;
     const at::Device device = x->device();
     if (saved->dim() != 2 || saved->size(0) != l.rows || saved->size(1) != 4 || saved->scalar_type() != at::kFloat ||
-        saved->device() != device || !saved->is_contiguous() || !floats(g, l.rows, device) || !floats(h, l.rows, device) ||
+        saved->device() != device || !saved->is_contiguous() || lazy(*saved) || !floats(g, l.rows, device) || !floats(h, l.rows, device) ||
         !floats(scale, 1, device))
       Py_RETURN_NONE;
     Tensor grad;
@@ -417,7 +417,7 @@ PyObject* grad_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
       sizes[size_t(i)] = g->numel();
       types[size_t(i)] = type_of(*g);
     }
-    if (!floats(out, 2, device) || (out != nullptr && lazy(*out))) Py_RETURN_NONE;
+    if (!floats(out, 2, device)) Py_RETURN_NONE;
     const size_t need = acdc_grad_norm_workspace_size(sizes.data(), int32_t(count));
     Tensor ws = at::empty({int64_t(std::max<size_t>(need, 1))}, first->options().dtype(at::kByte));
     Tensor result = out != nullptr ? *out : at::empty({2}, first->options().dtype(at::kFloat));

@@ -69,6 +69,11 @@ def _native(logits, name, *args):
     return r
 
 
+def _values(name, t):
+    if t.is_neg():
+        raise ValueError(f"{name} is a view that stands for the negative of its memory: give its resolve_neg()")
+
+
 def _logits(x, name="logits"):
     if x.dim() != 2:
         raise ValueError(f"{name} must be [rows, classes], got {tuple(x.shape)}")
@@ -84,6 +89,7 @@ def _logits(x, name="logits"):
         stride = max(stride, classes)
     if stride < classes:
         raise ValueError(f"{name} has overlapping rows (stride {stride}, {classes} classes)")
+    _values(name, x)
     return rows, classes, stride
 
 
@@ -93,6 +99,7 @@ def _vector(name, t, n, device, dtype=torch.float32):
     if t.shape != (n,) or t.device != device or t.dtype is not dtype or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} vector of {n} values on {device}, got "
                          f"{tuple(t.shape)} {t.dtype} on {t.device}")
+    _values(name, t)
 
 
 def _index(name, t, n, device):
@@ -115,6 +122,7 @@ def _saved(saved, rows, device):
     if saved.shape != (rows, 4) or saved.dtype is not torch.float32 or saved.device != device or \
             not saved.is_contiguous():
         raise ValueError(f"saved must be the contiguous float32 [{rows}, 4] tensor of the forward call")
+    _values("saved", saved)
 
 
 @functools.lru_cache(maxsize=512)

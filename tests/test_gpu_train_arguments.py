@@ -48,3 +48,16 @@ def test_step_of_negative_views(env):
     with pytest.raises(ValueError, match="view"):
         optim.adamw_step([torch._neg_view(p)], [g], [optim.moments(p)], 1)
     assert (p == 1).all()
+
+
+def test_losses_of_negative_views(env):
+    torch, losses, _ = env
+    x, t, f = torch.randn(4, 10, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda"), torch.ones(4, device="cuda")
+    off, saved = torch.tensor([0, 2, 4], device="cuda"), torch.ones(4, 4, device="cuda")
+    n = torch._neg_view
+    for call in (lambda: losses.token_logprobs(n(x), t), lambda: losses.policy_loss(x, t, f, n(f)),
+                 lambda: losses.preference_loss(x, t, off, n(f)), lambda: losses.policy_loss(x, t, f, f, out=n(x)),
+                 lambda: losses.token_logprobs_backward(x, t, n(saved), f)):
+        with pytest.raises(ValueError, match="negative"):
+            call()
+    assert torch.equal(losses.token_logprobs(n(x).resolve_neg(), t).logp, losses.token_logprobs(-x, t).logp)

@@ -58,3 +58,23 @@ def test_step_refuses_views_that_it_would_write_wrongly(calls):
     with pytest.raises(ValueError):
         optim.grad_norm([r], out=torch._neg_view(torch.zeros(2)))
     assert not calls
+
+
+def test_losses_refuse_negative_views(calls):
+    from paper_1511_05946_amd import losses
+    x, t, f, saved = torch.randn(4, 10), torch.zeros(4, dtype=torch.int64), torch.zeros(4), torch.zeros(4, 4)
+    off = torch.tensor([0, 2, 4])
+    n = torch._neg_view
+    one = torch.randn(1, 1, dtype=torch.complex64).conj().imag   # one that torch makes by itself
+    assert one.is_neg()
+    for call in (lambda: losses.token_logprobs(n(x), t), lambda: losses.token_logprobs(one, t[:1]),
+                 lambda: losses.token_logprobs_backward(x, t, n(saved), f),
+                 lambda: losses.token_logprobs_backward(x, t, saved, n(f)),
+                 lambda: losses.token_logprobs_backward(x, t, saved, f, scale=n(f[:1])),
+                 lambda: losses.token_logprobs_backward(x, t, saved, f, out=n(x)),
+                 lambda: losses.policy_loss(x, t, n(f), f), lambda: losses.policy_loss(x, t, f, n(f)),
+                 lambda: losses.policy_loss(x, t, f, f, logp_ref=n(f)), lambda: losses.policy_loss(x, t, f, f, weights=n(f)),
+                 lambda: losses.preference_loss(x, t, off, n(f))):
+        with pytest.raises(ValueError, match="negative"):
+            call()
+    assert not calls
