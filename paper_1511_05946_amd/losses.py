@@ -310,8 +310,11 @@ class _Loss(torch.autograd.Function):
     and writes the gradient, times the loss's own upstream gradient."""
 
     @staticmethod
-    def forward(ctx, logits, targets, call):
-        r = call(logits, targets)
+    def forward(ctx, logits, targets, loss, args, options):
+        if options.get("out") is not None:
+            raise ValueError("out is not for the differentiable form: autograd makes the gradient's tensor")
+        r = loss(logits, targets, *args, grad=False, save=True, **options)
+        ctx.grad_scale = options.get("grad_scale", 1.0)
         ctx.save_for_backward(logits, targets, r.saved, r.row_grads)
         ctx.mark_non_differentiable(r.stats, r.logp)
         return r.stats[0].clone(), r.stats, r.logp
@@ -320,7 +323,10 @@ class _Loss(torch.autograd.Function):
     def backward(ctx, grad_loss, _stats, _logp):
         logits, targets, saved, row_grads = ctx.saved_tensors
         scale = grad_loss.reshape(1).float()
-        return token_logprobs_backward(logits, targets, saved, row_grads[0], row_grads[1], scale=scale), None, None
+        if ctx.grad_scale != 1.0:
+            scale = scale * ctx.grad_scale
+        grad = token_logprobs_backward(logits, targets, saved, row_grads[0], row_grads[1], scale=scale)
+        return grad, None, None, None, None
 
 
 def token_logprobs_autograd(logits, targets):
@@ -329,12 +335,12 @@ def token_logprobs_autograd(logits, targets):
 
 
 def policy_loss_autograd(logits, actions, logp_old, advantages, **options):
-    """(loss, stats, logp) of ``policy_loss``; the loss is differentiable in the logits."""
-    return _Loss.apply(logits, actions, lambda x, t: policy_loss(x, t, logp_old, advantages, grad=False, save=True,
-                                                                 **options))
+    """(loss, stats, logp) of ``policy_loss``; the loss is differentiable in the
+    logits, and ``grad_scale`` multiplies their gradient as it does there."""
+    return _Loss.apply(logits, actions, policy_loss, (logp_old, advantages), options)
 
 
 def preference_loss_autograd(logits, targets, offsets, logp_ref, **options):
-    """(loss, stats, logp) of ``preference_loss``; the loss is differentiable in the logits."""
-    return _Loss.apply(logits, targets, lambda x, t: preference_loss(x, t, offsets, logp_ref, grad=False, save=True,
-                                                                     **options))
+    """(loss, stats, logp) of ``preference_loss``; the loss is differentiable in the
+    logits, and ``grad_scale`` multiplies their gradient as it does there."""
+    return _Loss.apply(logits, targets, preference_loss, (offsets, logp_ref), options)

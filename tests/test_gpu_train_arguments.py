@@ -61,3 +61,39 @@ def test_losses_of_negative_views(env):
         with pytest.raises(ValueError, match="negative"):
             call()
     assert torch.equal(losses.token_logprobs(n(x).resolve_neg(), t).logp, losses.token_logprobs(-x, t).logp)
+
+
+def losses_of(torch, losses, **options):
+    """Per loss: its logits, its gradient by the differentiable form, and by the call itself."""
+    gen = torch.Generator().manual_seed(3)
+    x, a = torch.randn(12, 50, generator=gen).cuda(), torch.randn(12, generator=gen).cuda()
+    t, off = torch.arange(12, device="cuda"), torch.tensor([0, 3, 6, 9, 12], device="cuda")
+    old = torch.full((12,), -4.0, device="cuda")
+    for auto, plain, args in ((losses.policy_loss_autograd, losses.policy_loss, (t, old, a)),
+                              (losses.preference_loss_autograd, losses.preference_loss, (t, off, old))):
+        leaf = x.clone().requires_grad_(True)
+        loss, stats, _ = auto(leaf, *args, **options)
+        loss.backward()
+        yield leaf.grad, plain(x, *args, **options).grad_logits, loss.detach(), plain(x, *args).stats[0]
+
+
+def test_differentiable_losses_take_a_gradient_scale(env):
+    """As the calls themselves: 0.25 is a power of two, so that the scaled gradient is a
+    quarter of the unscaled one to the bit; the two forms differ by roundings of the row's factors."""
+    torch, losses, _ = env
+    unscaled = list(losses_of(torch, losses))
+    for (got, want, loss, value), (full, *_) in zip(losses_of(torch, losses, grad_scale=0.25), unscaled):
+        assert torch.equal(got, 0.25 * full)
+        assert torch.allclose(got, want, rtol=1e-5, atol=1e-9) and loss == value
+
+
+def test_differentiable_losses_refuse_a_tensor_for_the_gradient(env):
+    torch, losses, _ = env
+    x, t, f = torch.randn(4, 10, device="cuda", requires_grad=True), torch.zeros(4, dtype=torch.int64, device="cuda"), \
+        torch.zeros(4, device="cuda")
+    off, out = torch.tensor([0, 2, 4], device="cuda"), torch.full((4, 10), 7.0, device="cuda")
+    with pytest.raises(ValueError, match="out"):
+        losses.policy_loss_autograd(x, t, f, f, out=out)
+    with pytest.raises(ValueError, match="out"):
+        losses.preference_loss_autograd(x, t, off, f, out=out)
+    assert (out == 7).all()
