@@ -54,6 +54,14 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def _wrote(*tensors):
+    """Tells torch of a caller's tensors that a kernel writes, so that autograd
+    refuses a backward pass over what it saved of their old values."""
+    for t in tensors:
+        if t is not None and not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
 def _nbytes(t) -> int:
     return 0 if t is None else t.numel() * t.element_size()
 

@@ -128,6 +128,11 @@ template <class T = float>
 T* ptr(const Tensor& t) {
   return t.defined() ? static_cast<T*>(t.data_ptr()) : nullptr;
 }
+// A caller's tensor that a kernel writes: torch is told, so that autograd refuses
+// a backward pass over what it saved of the old values.
+void wrote(const Tensor* t) {
+  if (t != nullptr && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
 PyObject* wrap(const Tensor& t) {
   if (t.defined()) return THPVariable_Wrap(t);
   Py_RETURN_NONE;
@@ -209,6 +214,7 @@ PyObject* logprobs_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int rc = acdc_logprob_backward(x->data_ptr(), l.dtype, l.stride, t->data_ptr(), l.bits, ptr(saved), ptr(g), ptr(h),
                                          ptr(scale), grad.data_ptr(), grad_stride, l.rows, l.classes, stream);
     if (rc != ACDC_OK) return PyLong_FromLong(rc);
+    wrote(out);
     return wrap(grad);
   });
 }
@@ -248,6 +254,7 @@ PyObject* policy(PyObject*, PyObject* const* args, Py_ssize_t n) {
                                     ptr(w), l.rows, l.classes, &p, ptr(stats), ptr(logp), ptr<void>(grad), grad_stride,
                                     ptr(saved), ptr(row_grads), ws.data_ptr(), need, stream);
     if (rc != ACDC_OK) return PyLong_FromLong(rc);
+    if (grad.defined()) wrote(out);
     return tuple_of({stats, logp, grad, saved, row_grads});
   });
 }
@@ -285,6 +292,7 @@ PyObject* preference(PyObject*, PyObject* const* args, Py_ssize_t n) {
                                         ptr(ref), l.rows, l.classes, pairs, &p, ptr(stats), ptr(logp), ptr<void>(grad),
                                         grad_stride, ptr(saved), ptr(row_grads), ws.data_ptr(), need, stream);
     if (rc != ACDC_OK) return PyLong_FromLong(rc);
+    if (grad.defined()) wrote(out);
     return tuple_of({stats, logp, grad, saved, row_grads});
   });
 }
@@ -390,7 +398,16 @@ PyObject* adamw(PyObject*, PyObject* const* args, Py_ssize_t n) {
       }
     }
     if (!lr.ok || !decay.ok) Py_RETURN_NONE;
-    return PyLong_FromLong(acdc_adamw_step(records.data(), int32_t(count), beta1, beta2, eps, step, ptr(scale), stream));
+    const int rc = acdc_adamw_step(records.data(), int32_t(count), beta1, beta2, eps, step, ptr(scale), stream);
+    if (rc == ACDC_OK) {
+      for (Py_ssize_t i = 0; i < count; ++i) {
+        wrote(params.tensor(i));
+        if (records[size_t(i)].master != nullptr) wrote(masters.tensor(i));
+        const Items m(moments.at[i]);
+        for (Py_ssize_t k = 0; k < m.count; ++k) wrote(m.tensor(k));
+      }
+    }
+    return PyLong_FromLong(rc);
   });
 }
 
@@ -424,6 +441,7 @@ PyObject* grad_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int rc = acdc_grad_norm(ptrs.data(), sizes.data(), types.data(), int32_t(count), most, ptr(result), ws.data_ptr(),
                                   need, stream);
     if (rc != ACDC_OK) return PyLong_FromLong(rc);
+    wrote(out);
     return wrap(result);
   });
 }

@@ -28,7 +28,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from ._lib import binding, lib
-from .acdc import _call, _check, _ptr
+from .acdc import _call, _check, _ptr, _wrote
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 _BITS = {torch.int32: 32, torch.int64: 64}
@@ -198,6 +198,7 @@ def token_logprobs_backward(logits, targets, saved, grad_logp, grad_entropy=None
                targets.data_ptr(), bits, saved.data_ptr(), grad_logp.data_ptr(), _ptr(grad_entropy), _ptr(scale),
                grad.data_ptr(), grad_stride, rows, classes)
     _check(rc, "acdc_logprob_backward")
+    _wrote(out)
     return grad
 
 
@@ -248,6 +249,7 @@ def policy_loss(logits, actions, logp_old, advantages, logp_ref=None, weights=No
                stats.data_ptr(), logp.data_ptr(), _ptr(g), grad_stride, _ptr(saved), _ptr(row_grads), ws.data_ptr(),
                need)
     _check(rc, "acdc_policy_loss")
+    _wrote(out if grad else None)
     return PolicyLoss(stats, logp, g, saved, row_grads)
 
 
@@ -285,6 +287,7 @@ def preference_loss(logits, targets, offsets, logp_ref, beta: float = 0.1, label
                offsets.data_ptr(), offset_bits, logp_ref.data_ptr(), rows, classes, pairs, params, stats.data_ptr(),
                logp.data_ptr(), _ptr(g), grad_stride, _ptr(saved), _ptr(row_grads), ws.data_ptr(), need)
     _check(rc, "acdc_preference_loss")
+    _wrote(out if grad else None)
     return PreferenceLoss(stats, logp, g, saved, row_grads)
 
 

@@ -24,7 +24,7 @@ import struct
 import torch
 
 from ._lib import binding, lib
-from .acdc import _call, _check
+from .acdc import _call, _check, _wrote
 
 SCALE_BLOCK = 256
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.complex64: 0}
@@ -151,6 +151,7 @@ def adamw_step(params, grads, moments, step: int, lr=1e-3, betas=(0.9, 0.999), e
     rc = _call(lib().acdc_adamw_step, device, ctypes.addressof(buf), count, float(betas[0]), float(betas[1]),
                float(eps), int(step), None if grad_scale is None else grad_scale.data_ptr())
     _check(rc, "acdc_adamw_step")
+    _wrote(*params, *(masters or ()), *(t for state in moments for t in state))
 
 
 def grad_norm(grads, max_norm=None, out=None):
@@ -178,6 +179,7 @@ def grad_norm(grads, max_norm=None, out=None):
         ptrs.append(g.data_ptr())
         sizes.append(_real_numel(g))
         types.append(_TYPES[g.dtype])
+    given = out
     if out is None:
         out = torch.empty(2, device=device)
     elif out.shape != (2,) or out.dtype is not torch.float32 or out.device != device or not out.is_contiguous() or \
@@ -189,4 +191,5 @@ def grad_norm(grads, max_norm=None, out=None):
     rc = _call(lib().acdc_grad_norm, device, ptrs, sizes, types, count, float(max_norm or 0.0), out.data_ptr(),
                ws.data_ptr(), need)
     _check(rc, "acdc_grad_norm")
+    _wrote(given)
     return out

@@ -97,3 +97,49 @@ def test_differentiable_losses_refuse_a_tensor_for_the_gradient(env):
     with pytest.raises(ValueError, match="out"):
         losses.preference_loss_autograd(x, t, off, f, out=out)
     assert (out == 7).all()
+
+
+def test_step_between_the_passes_of_a_cascade_is_noticed(env):
+    """The backward pass needs A and D as they were."""
+    torch, losses, optim = env
+    from paper_1511_05946_amd import acdc
+    A, D = (torch.ones(2, 64, device="cuda", requires_grad=True) for _ in range(2))
+    x = torch.randn(8, 64, device="cuda")
+    for k in range(2):
+        loss = acdc.acdc_cascade(x, A, D).square().sum()
+        p = [A.detach(), D.detach()][k:k + 1]
+        optim.adamw_step(p, [torch.ones(2, 64, device="cuda")], [optim.moments(p[0])], 1)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+
+
+def test_gradient_over_saved_logits_is_noticed(env):
+    torch, losses, _ = env
+    x, t, f = torch.randn(4, 10, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, device="cuda")
+    off = torch.tensor([0, 2, 4], device="cuda")
+    saved = losses.token_logprobs(x, t, save=True).saved
+    for over in (lambda y: losses.policy_loss(y, t, f, f, out=y), lambda y: losses.preference_loss(y, t, off, f, out=y),
+                 lambda y: losses.token_logprobs_backward(y, t, saved, f, out=y)):
+        leaf = x.clone().requires_grad_(True)
+        y = leaf * 1.0
+        logp, _ = losses.token_logprobs_autograd(y, t)
+        over(y.detach()[:, :10])
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            logp.sum().backward()
+
+
+def test_versions_of_the_optimisers_tensors(env):
+    torch, _, optim = env
+    p, g, w = torch.ones(600, device="cuda").bfloat16(), torch.ones(600, device="cuda"), torch.ones(600, device="cuda")
+    for bits in (32, 8):
+        state = optim.moments(p, bits)
+        out = torch.zeros(2, device="cuda")
+        watched = [p, w, *state, out]
+        before = [t._version for t in watched]
+        optim.adamw_step([p], [g], [state], 1, masters=[w])
+        optim.grad_norm([g], out=out)
+        assert all(t._version > b for t, b in zip(watched, before)) and g._version == 0
+    with torch.inference_mode():   # tensors without a version
+        q = torch.ones(600, device="cuda")
+        optim.adamw_step([q], [g], [optim.moments(q)], 1)
+        optim.grad_norm([q], out=torch.zeros(2, device="cuda"))

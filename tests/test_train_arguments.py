@@ -78,3 +78,26 @@ def test_losses_refuse_negative_views(calls):
         with pytest.raises(ValueError, match="negative"):
             call()
     assert not calls
+
+
+def test_torch_is_told_what_is_written(calls):
+    from paper_1511_05946_amd import losses, optim
+    x, t, f, saved = torch.randn(4, 10), torch.zeros(4, dtype=torch.int64), torch.zeros(4), torch.zeros(4, 4)
+    off = torch.tensor([0, 2, 4])
+    for call in (lambda o: losses.token_logprobs_backward(x, t, saved, f, out=o), lambda o: losses.policy_loss(x, t, f, f, out=o),
+                 lambda o: losses.preference_loss(x, t, off, f, out=o)):
+        out = torch.zeros(4, 10)
+        call(out)
+        assert out._version > 0 and x._version == f._version == saved._version == 0
+    p, g, w = torch.ones(6).bfloat16(), torch.ones(6), torch.ones(6)
+    state = optim.moments(p, 8)
+    before = [s._version for s in state]
+    optim.adamw_step([p], [g], [state], 1, masters=[w])
+    assert p._version > 0 and w._version > 0 and g._version == 0 and all(s._version > b for s, b in zip(state, before))
+    out = torch.zeros(2)
+    optim.grad_norm([g], out=out)
+    assert out._version > 0 and g._version == 0
+    with torch.inference_mode():   # tensors without a version
+        p = torch.ones(6)
+        optim.adamw_step([p], [torch.ones(6)], [optim.moments(p)], 2)
+        losses.policy_loss(torch.zeros(4, 10), t, f, f, out=torch.zeros(4, 10))
