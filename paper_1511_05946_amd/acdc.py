@@ -294,6 +294,27 @@ def backward(x, grad_y, A, D, perm=None, flags: int = 0, saved=None, bias=None, 
     return (gx, gA, gD, gB) if bias is not None else (gx, gA, gD)
 
 
+class _Once(torch.autograd.Function):
+    """Gradients as a kernel computed them: functions of what the call read, whose
+    own derivative is not there.  (A backward pass that is asked for a graph would
+    else hand them out as constants, and what depends on them would drop out of a
+    second one without an error.)"""
+
+    @staticmethod
+    def forward(ctx, call, grad, *read):
+        ctx.call = call
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError(f"the gradient of {ctx.call} cannot be differentiated again")
+
+
+def _once(call, grad, *read):
+    """`grad`, computed from `read` by the backward pass of `call`."""
+    return _Once.apply(call, grad, *read) if torch.is_grad_enabled() and grad is not None else grad
+
+
 class ACDCCascade(torch.autograd.Function):
     """autograd wrapper: stores the layer inputs in the forward pass."""
 

@@ -28,7 +28,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from ._lib import binding, lib
-from .acdc import _call, _check, _ptr, _wrote
+from .acdc import _call, _check, _once, _ptr, _wrote
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 _BITS = {torch.int32: 32, torch.int64: 64}
@@ -304,7 +304,8 @@ class _TokenLogprobs(torch.autograd.Function):
     @staticmethod
     def backward(ctx, grad_logp, grad_entropy):
         logits, targets, saved = ctx.saved_tensors
-        return token_logprobs_backward(logits, targets, saved, grad_logp.contiguous(), grad_entropy.contiguous()), None
+        grad = token_logprobs_backward(logits, targets, saved, grad_logp.contiguous(), grad_entropy.contiguous())
+        return _once("token_logprobs_autograd", grad, logits, grad_logp, grad_entropy), None
 
 
 class _Loss(torch.autograd.Function):
@@ -317,7 +318,7 @@ class _Loss(torch.autograd.Function):
         if options.get("out") is not None:
             raise ValueError("out is not for the differentiable form: autograd makes the gradient's tensor")
         r = loss(logits, targets, *args, grad=False, save=True, **options)
-        ctx.grad_scale = options.get("grad_scale", 1.0)
+        ctx.grad_scale, ctx.call = options.get("grad_scale", 1.0), loss.__name__ + "_autograd"
         ctx.save_for_backward(logits, targets, r.saved, r.row_grads)
         ctx.mark_non_differentiable(r.stats, r.logp)
         return r.stats[0].clone(), r.stats, r.logp
@@ -329,7 +330,7 @@ class _Loss(torch.autograd.Function):
         if ctx.grad_scale != 1.0:
             scale = scale * ctx.grad_scale
         grad = token_logprobs_backward(logits, targets, saved, row_grads[0], row_grads[1], scale=scale)
-        return grad, None, None, None, None
+        return _once(ctx.call, grad, logits, grad_loss), None, None, None, None
 
 
 def token_logprobs_autograd(logits, targets):

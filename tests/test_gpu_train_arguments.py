@@ -143,3 +143,20 @@ def test_versions_of_the_optimisers_tensors(env):
         q = torch.ones(600, device="cuda")
         optim.adamw_step([q], [g], [optim.moments(q)], 1)
         optim.grad_norm([q], out=torch.zeros(2, device="cuda"))
+
+
+def test_second_derivatives_are_refused(env):
+    """A gradient penalty beside another term: an error, not the other term's gradient alone."""
+    torch, losses, _ = env
+    x, t, f = torch.randn(4, 10, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, device="cuda")
+    off = torch.tensor([0, 2, 4], device="cuda")
+    for form in (lambda y: losses.token_logprobs_autograd(y, t)[0].sum(), lambda y: losses.policy_loss_autograd(y, t, f - 2, f + 1)[0],
+                 lambda y: losses.preference_loss_autograd(y, t, off, f)[0]):
+        leaf = x.clone().requires_grad_(True)
+        loss = form(leaf)
+        grad, = torch.autograd.grad(loss, leaf, create_graph=True)
+        with pytest.raises(RuntimeError, match="cannot be differentiated again"):
+            (grad.square().sum() + form(leaf)).backward()
+        first = x.clone().requires_grad_(True)
+        form(first).backward()
+        assert torch.equal(first.grad, grad.detach())
