@@ -333,7 +333,8 @@ class ACDCCascade(torch.autograd.Function):
     def backward(ctx, gy):
         x, A, D, perm, bias, saved = ctx.saved_tensors
         out = backward(x, gy.contiguous(), A, D, perm, ctx.flags, saved, bias=bias)
-        return out[0], out[1], out[2], None, None, out[3] if bias is not None else None
+        gx, gA, gD, *gB = (_once("acdc_cascade", g, gy, x, A, D, bias) for g in out)
+        return gx, gA, gD, None, None, gB[0] if gB else None
 
 
 def acdc_cascade(x, A, D, perm=None, flags: int = 0, bias=None):
