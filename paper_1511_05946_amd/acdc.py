@@ -54,6 +54,15 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def _has_memory(t) -> bool:
+    """Whether a tensor's storage holds it: one whose storage was freed (resized to
+    nothing) still has its shape, and an address that is null or stands for nothing."""
+    if t.numel() == 0:
+        return True
+    last = t.storage_offset() + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
+    return (last + 1) * t.element_size() <= t.untyped_storage().nbytes()
+
+
 def _wrote(*tensors):
     """Tells torch of a caller's tensors that a kernel writes, so that autograd
     refuses a backward pass over what it saved of their old values."""

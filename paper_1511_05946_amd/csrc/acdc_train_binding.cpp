@@ -11,6 +11,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/EmptyTensor.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <vector>
@@ -63,9 +64,16 @@ int32_t type_of(const Tensor& t) {
 }
 // A view marked as conjugated or negated: its memory does not hold its values.
 bool lazy(const Tensor& t) { return t.is_conj() || t.is_neg(); }
+// A tensor that its storage does not hold (any more): its address is null, which the
+// library would take for an argument left out, or stands for nothing.
+bool gone(const Tensor& t) {
+  return t.numel() > 0 &&
+         at::detail::computeStorageNbytes(t.sizes(), t.strides(), t.itemsize(), size_t(t.storage_offset())) > t.storage().nbytes();
+}
+bool readable(const Tensor& t) { return !lazy(t) && !gone(t); }
 bool vector_of(const Tensor* t, int64_t n, const at::Device& device, at::ScalarType type) {
   return t == nullptr || (t->dim() == 1 && t->size(0) == n && t->scalar_type() == type && t->device() == device &&
-                          t->is_contiguous() && !lazy(*t));
+                          t->is_contiguous() && readable(*t));
 }
 bool floats(const Tensor* t, int64_t n, const at::Device& device) { return vector_of(t, n, device, at::kFloat); }
 int32_t index_bits(const Tensor& t, int64_t n, const at::Device& device) {
@@ -91,7 +99,7 @@ struct Logits {
   static int64_t step(const Tensor& t) { return t.size(0) <= 1 ? std::max(t.stride(0), t.size(1)) : t.stride(0); }
   static bool plain(const Tensor& t) {
     return t.dim() == 2 && t.is_cuda() && type_of(t) >= 0 && t.size(1) >= 1 && t.size(1) <= 0x7fffffff &&
-           (t.size(1) == 1 || t.stride(1) == 1) && step(t) >= t.size(1) && !lazy(t);
+           (t.size(1) == 1 || t.stride(1) == 1) && step(t) >= t.size(1) && readable(t);
   }
   Tensor make(at::IntArrayRef size) const { return at::empty(size, x->options().dtype(at::kFloat)); }
   // the gradient's tensor: `out`, or a new one
@@ -113,7 +121,7 @@ struct Logits {
       return true;
     }
     if (given->scalar_type() != at::kByte || given->dim() != 1 || size_t(given->numel()) < need ||
-        given->device() != x->device() || !given->is_contiguous())
+        given->device() != x->device() || !given->is_contiguous() || gone(*given))
       return false;
     *ws = *given;
     return true;
@@ -205,7 +213,7 @@ PyObject* logprobs_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (a.bad || !l.read(x, t)) Py_RETURN_NONE;
     const at::Device device = x->device();
     if (saved->dim() != 2 || saved->size(0) != l.rows || saved->size(1) != 4 || saved->scalar_type() != at::kFloat ||
-        saved->device() != device || !saved->is_contiguous() || lazy(*saved) || !floats(g, l.rows, device) || !floats(h, l.rows, device) ||
+        saved->device() != device || !saved->is_contiguous() || !readable(*saved) || !floats(g, l.rows, device) || !floats(h, l.rows, device) ||
         !floats(scale, 1, device))
       Py_RETURN_NONE;
     Tensor grad;
@@ -340,7 +348,7 @@ struct Numbers {
 
 bool plain(const Tensor* t, int64_t numel, const at::Device& device, at::ScalarType type) {
   return t != nullptr && t->scalar_type() == type && t->numel() == numel && t->device() == device && t->is_contiguous() &&
-         !lazy(*t);
+         readable(*t);
 }
 
 // (params, grads, moments, masters, lr, weight_decay, beta1, beta2, eps, step, grad_scale, stream) -> status
@@ -371,8 +379,8 @@ PyObject* adamw(PyObject*, PyObject* const* args, Py_ssize_t n) {
     for (Py_ssize_t i = 0; i < count; ++i) {
       const Tensor *p = params.tensor(i), *g = grads.tensor(i);
       if (p == nullptr || g == nullptr || type_of(*p) < 0 || type_of(*g) < 0 || !p->is_contiguous() ||
-          p->device() != device || g->sizes() != p->sizes() || g->device() != device || !g->is_contiguous() || lazy(*p) ||
-          lazy(*g))
+          p->device() != device || g->sizes() != p->sizes() || g->device() != device || !g->is_contiguous() || !readable(*p) ||
+          !readable(*g))
         Py_RETURN_NONE;
       const int64_t numel = p->numel();
       acdc_adamw_tensor& r = records[size_t(i)];
@@ -429,7 +437,7 @@ PyObject* grad_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
     std::vector<int32_t> types(static_cast<size_t>(count));
     for (Py_ssize_t i = 0; i < count; ++i) {
       const Tensor* g = grads.tensor(i);
-      if (g == nullptr || type_of(*g) < 0 || !g->is_contiguous() || g->device() != device) Py_RETURN_NONE;
+      if (g == nullptr || type_of(*g) < 0 || !g->is_contiguous() || g->device() != device || gone(*g)) Py_RETURN_NONE;
       ptrs[size_t(i)] = g->data_ptr();
       sizes[size_t(i)] = g->numel();
       types[size_t(i)] = type_of(*g);

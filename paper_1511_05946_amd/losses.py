@@ -28,7 +28,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from ._lib import binding, lib
-from .acdc import _call, _check, _once, _ptr, _wrote
+from .acdc import _call, _check, _has_memory, _once, _ptr, _wrote
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 _BITS = {torch.int32: 32, torch.int64: 64}
@@ -72,6 +72,8 @@ def _native(logits, name, *args):
 def _values(name, t):
     if t.is_neg():
         raise ValueError(f"{name} is a view that stands for the negative of its memory: give its resolve_neg()")
+    if not _has_memory(t):
+        raise ValueError(f"{name} is without memory: its storage was freed")
 
 
 def _logits(x, name="logits"):
@@ -154,6 +156,7 @@ def _workspace(ws, need, device):
         return torch.empty(max(need, 1), dtype=torch.uint8, device=device)
     if ws.dtype is not torch.uint8 or ws.dim() != 1 or ws.numel() < need or ws.device != device:
         raise ValueError(f"workspace must be a uint8 vector of at least {need} bytes on {device}")
+    _values("workspace", ws)
     return ws
 
 

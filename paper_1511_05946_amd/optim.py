@@ -24,7 +24,7 @@ import struct
 import torch
 
 from ._lib import binding, lib
-from .acdc import _call, _check, _wrote
+from .acdc import _call, _check, _has_memory, _wrote
 
 SCALE_BLOCK = 256
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.complex64: 0}
@@ -77,6 +77,8 @@ def _refuse_moments(i, state, n, device):
                              f"{tuple(t.shape)} {t.dtype} on {t.device}")
         if _lazy(t):
             raise ValueError(f"moments[{i}][{k}] is a conjugate or negative view")
+        if not _has_memory(t):
+            raise ValueError(f"moments[{i}][{k}] is without memory")
 
 
 def _refuse(i, p, g, master, n, device):
@@ -93,6 +95,9 @@ def _refuse(i, p, g, master, n, device):
         raise ValueError(f"masters[{i}] must be the contiguous float32 copy of a bfloat16 parameter of {n} elements")
     if _lazy(p) or (master is not None and _lazy(master)):
         raise ValueError(f"params[{i}] and its master must not be conjugate or negative views: they are written in place")
+    for name, t in (("params", p), ("grads", g), ("masters", master)):
+        if t is not None and not _has_memory(t):
+            raise ValueError(f"{name}[{i}] is without memory")
 
 
 def adamw_step(params, grads, moments, step: int, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01,
@@ -137,13 +142,11 @@ def adamw_step(params, grads, moments, step: int, lr=1e-3, betas=(0.9, 0.999), e
             g = g.resolve_conj().resolve_neg()
             resolved.append(g)
         scales = (state[2].data_ptr(), state[3].data_ptr()) if len(state) == 4 else (0, 0)
-        if len(state) == 4 and n > 0 and not (scales[0] and scales[1]):
-            raise ValueError(f"moments[{i}] has scales without memory")
         _RECORD.pack_into(records, size * i, p.data_ptr(), 0 if master is None else master.data_ptr(), g.data_ptr(),
                           state[0].data_ptr(), state[1].data_ptr(), *scales, n, lrs[i], decays[i],
                           _TYPES[p.dtype], _TYPES[g.dtype])
     if grad_scale is not None and (grad_scale.numel() != 1 or grad_scale.dtype is not torch.float32 or
-                                   grad_scale.device != device):
+                                   grad_scale.device != device or not _has_memory(grad_scale)):
         raise ValueError(f"grad_scale must be one float32 value on {device}")
     if grad_scale is not None:
         grad_scale = grad_scale.resolve_neg()
@@ -176,6 +179,8 @@ def grad_norm(grads, max_norm=None, out=None):
         if g.dtype not in _TYPES or not g.is_contiguous() or g.device != device:
             raise ValueError(f"grads[{i}] must be a contiguous float32, bfloat16 or complex64 tensor, all on one device; "
                              f"got {g.dtype} on {g.device}")
+        if not _has_memory(g):
+            raise ValueError(f"grads[{i}] is without memory")
         ptrs.append(g.data_ptr())
         sizes.append(_real_numel(g))
         types.append(_TYPES[g.dtype])
@@ -183,7 +188,7 @@ def grad_norm(grads, max_norm=None, out=None):
     if out is None:
         out = torch.empty(2, device=device)
     elif out.shape != (2,) or out.dtype is not torch.float32 or out.device != device or not out.is_contiguous() or \
-            _lazy(out):
+            _lazy(out) or not _has_memory(out):
         raise ValueError(f"out must be a contiguous float32 vector of 2 values on {device}")
     ptrs, sizes, types = struct.pack(f"{count}Q", *ptrs), struct.pack(f"{count}q", *sizes), struct.pack(f"{count}i", *types)
     need = lib().acdc_grad_norm_workspace_size(sizes, count)

@@ -175,3 +175,41 @@ def test_second_derivatives_of_a_cascade_are_refused(env):
             assert all(torch.equal(u, v.detach()) for u, v in zip(first, grad))
             with pytest.raises(RuntimeError, match="cannot be differentiated again"):
                 (grad[k].square().sum() + y).backward()
+
+
+@pytest.mark.parametrize("part", [False, True])
+def test_tensors_without_memory_are_refused(env, part):
+    """Nothing is launched: the library would take a null address for an argument left out
+    (8-bit moments without scales for 32-bit ones), and another for memory."""
+    torch, losses, optim = env
+
+    def gone(t):
+        t = torch.stack([t, t])[1] if part else t.clone()
+        t.untyped_storage().resize_(0)
+        return t
+
+    x, t, f = torch.randn(4, 10, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, device="cuda")
+    saved, off = torch.zeros(4, 4, device="cuda"), torch.tensor([0, 2, 4], device="cuda")
+    ws = torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
+    for call in (lambda: losses.token_logprobs(gone(x), t), lambda: losses.token_logprobs(x, gone(t)),
+                 lambda: losses.token_logprobs(x, t, workspace=gone(ws)),
+                 lambda: losses.token_logprobs_backward(x, t, gone(saved), f),
+                 lambda: losses.token_logprobs_backward(x, t, saved, f, gone(f)),
+                 lambda: losses.token_logprobs_backward(x, t, saved, f, scale=gone(f[:1])),
+                 lambda: losses.token_logprobs_backward(x, t, saved, f, out=gone(x)),
+                 lambda: losses.policy_loss(x, t, f, f, weights=gone(f)), lambda: losses.policy_loss(x, t, f, f, logp_ref=gone(f)),
+                 lambda: losses.policy_loss(x, t, f, f, out=gone(x)), lambda: losses.preference_loss(x, t, gone(off), f)):
+        with pytest.raises(ValueError, match="without memory"):
+            call()
+    p, g = torch.ones(300, device="cuda"), torch.ones(300, device="cuda")
+    half = p.bfloat16()
+    s32, s8 = optim.moments(p), optim.moments(p, 8)
+    for args, kw in ((([gone(p)], [g], [s32]), {}), (([p], [gone(g)], [s32]), {}), (([p], [g], [(gone(g), g)]), {}),
+                     (([p], [g], [(*s8[:2], gone(s8[2]), gone(s8[3]))]), {}),
+                     (([half], [g], [s32]), dict(masters=[gone(p)])), (([p], [g], [s32]), dict(grad_scale=gone(p[:1])))):
+        with pytest.raises(ValueError):
+            optim.adamw_step(*args, 1, **kw)
+    for kw in (dict(grads=[gone(p)]), dict(grads=[p], out=gone(p[:2]))):
+        with pytest.raises(ValueError):
+            optim.grad_norm(**kw)
+    assert (p == 1).all() and (half == 1).all() and not s32[0].any()

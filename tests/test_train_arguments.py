@@ -101,3 +101,44 @@ def test_torch_is_told_what_is_written(calls):
         p = torch.ones(6)
         optim.adamw_step([p], [torch.ones(6)], [optim.moments(p)], 2)
         losses.policy_loss(torch.zeros(4, 10), t, f, f, out=torch.zeros(4, 10))
+
+
+def freed(t):
+    t = t.clone()
+    t.untyped_storage().resize_(0)
+    return t
+
+
+def freed_part(t):
+    """A part of a larger tensor whose storage was freed: its address is not even null."""
+    t = torch.stack([t, t])[1]
+    t.untyped_storage().resize_(0)
+    return t
+
+
+@pytest.mark.parametrize("gone", [freed, freed_part])
+def test_tensors_without_memory_are_refused(calls, gone):
+    from paper_1511_05946_amd import losses, optim
+    x, t, f, saved = torch.randn(4, 10), torch.zeros(4, dtype=torch.int64), torch.zeros(4), torch.zeros(4, 4)
+    off, ws = torch.tensor([0, 2, 4]), torch.zeros(1 << 16, dtype=torch.uint8)
+    for call in (lambda: losses.token_logprobs(gone(x), t), lambda: losses.token_logprobs(x, gone(t)),
+                 lambda: losses.token_logprobs(x, t, workspace=gone(ws)),
+                 lambda: losses.token_logprobs_backward(x, t, gone(saved), f),
+                 lambda: losses.token_logprobs_backward(x, t, saved, f, gone(f)),
+                 lambda: losses.token_logprobs_backward(x, t, saved, f, scale=gone(f[:1])),
+                 lambda: losses.token_logprobs_backward(x, t, saved, f, out=gone(x)),
+                 lambda: losses.policy_loss(x, t, f, f, weights=gone(f)), lambda: losses.policy_loss(x, t, f, f, logp_ref=gone(f)),
+                 lambda: losses.policy_loss(x, t, f, f, out=gone(x)), lambda: losses.preference_loss(x, t, gone(off), f)):
+        with pytest.raises(ValueError, match="without memory"):
+            call()
+    p, half = torch.ones(300), torch.ones(300).bfloat16()
+    s32, s8 = optim.moments(p), optim.moments(p, 8)
+    for args, kw in ((([gone(p)], [p], [s32]), {}), (([p], [gone(p)], [s32]), {}), (([p], [p], [(gone(p), p)]), {}),
+                     (([p], [p], [(*s8[:2], gone(s8[2]), gone(s8[3]))]), {}),
+                     (([half], [half], [s32]), dict(masters=[gone(p)])), (([p], [p], [s32]), dict(grad_scale=gone(p[:1])))):
+        with pytest.raises(ValueError):
+            optim.adamw_step(*args, 1, **kw)
+    for kw in (dict(grads=[gone(p)]), dict(grads=[p], out=gone(p[:2]))):
+        with pytest.raises(ValueError):
+            optim.grad_norm(**kw)
+    assert not calls
