@@ -154,8 +154,8 @@ def workspace_bytes(logits, pairs: int = 0) -> int:
 def _workspace(ws, need, device):
     if ws is None:
         return torch.empty(max(need, 1), dtype=torch.uint8, device=device)
-    if ws.dtype is not torch.uint8 or ws.dim() != 1 or ws.numel() < need or ws.device != device:
-        raise ValueError(f"workspace must be a uint8 vector of at least {need} bytes on {device}")
+    if ws.dtype is not torch.uint8 or ws.dim() != 1 or ws.numel() < need or ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 vector of at least {need} bytes on {device}")
     _values("workspace", ws)
     return ws
 

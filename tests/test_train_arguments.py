@@ -142,3 +142,14 @@ def test_tensors_without_memory_are_refused(calls, gone):
         with pytest.raises(ValueError):
             optim.grad_norm(**kw)
     assert not calls
+
+
+def test_workspaces_that_do_not_hold_their_size_are_refused(calls):
+    """One byte read as many: the kernels write bytes next to each other."""
+    from paper_1511_05946_amd import losses
+    x, t = torch.randn(4, 10), torch.zeros(4, dtype=torch.int64)
+    byte, apart = torch.zeros(1, dtype=torch.uint8).expand(1 << 16), torch.zeros(1 << 17, dtype=torch.uint8)[::2]
+    for ws in (byte, apart):
+        with pytest.raises(ValueError, match="workspace"):
+            losses.token_logprobs(x, t, workspace=ws)
+    assert not calls
