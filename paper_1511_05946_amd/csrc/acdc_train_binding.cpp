@@ -47,7 +47,14 @@ struct Args {
     }
     return v;
   }
-  bool flag(int i) { return PyObject_IsTrue(a[i]) == 1; }
+  bool flag(int i) {  // (what has no truth value raises in the caller's Python code)
+    const int v = PyObject_IsTrue(a[i]);
+    if (v < 0) {
+      PyErr_Clear();
+      bad = true;
+    }
+    return v == 1;
+  }
   acdc_stream_t stream(int i) {
     void* p = PyLong_AsVoidPtr(a[i]);
     if (p == nullptr && PyErr_Occurred()) {
@@ -186,6 +193,7 @@ PyObject* logprobs(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return guarded(n, 6, [&]() -> PyObject* {
     Args a{args};
     const Tensor *x = a.must(0), *t = a.must(1), *given = a.may(4);
+    const bool want_entropy = a.flag(2), save = a.flag(3);
     const acdc_stream_t stream = a.stream(5);
     Logits l;
     Tensor ws;
@@ -193,8 +201,8 @@ PyObject* logprobs(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const size_t need = acdc_logprob_workspace_size(l.rows, l.classes, l.dtype);
     if (!l.workspace(given, need, &ws)) Py_RETURN_NONE;
     Tensor logp = l.make({l.rows}), entropy, saved;
-    if (a.flag(2)) entropy = l.make({l.rows});
-    if (a.flag(3)) saved = l.make({l.rows, 4});
+    if (want_entropy) entropy = l.make({l.rows});
+    if (save) saved = l.make({l.rows, 4});
     const int rc = acdc_logprob_forward(x->data_ptr(), l.dtype, l.stride, t->data_ptr(), l.bits, l.rows, l.classes,
                                         ptr(logp), ptr(entropy), ptr(saved), ws.data_ptr(), need, stream);
     if (rc != ACDC_OK) return PyLong_FromLong(rc);
@@ -241,6 +249,7 @@ PyObject* policy(PyObject*, PyObject* const* args, Py_ssize_t n) {
     p.entropy_coef = float(a.number(9));
     p.grad_scale = float(a.number(10));
     p.mean = a.flag(11) ? 1 : 0;
+    const bool want_grad = a.flag(12), save = a.flag(13);
     const acdc_stream_t stream = a.stream(16);
     Logits l;
     if (a.bad || !l.read(x, t)) Py_RETURN_NONE;
@@ -250,11 +259,11 @@ PyObject* policy(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (!(p.clip_low >= 0.f) || !(p.clip_high >= 0.f) || (p.kl_coef != 0.f && ref == nullptr)) Py_RETURN_NONE;
     Tensor grad, saved, row_grads, ws;
     int64_t grad_stride = l.classes;
-    if (a.flag(12) && !l.gradient(out, &grad, &grad_stride)) Py_RETURN_NONE;
+    if (want_grad && !l.gradient(out, &grad, &grad_stride)) Py_RETURN_NONE;
     const size_t need = acdc_policy_workspace_size(l.rows, l.classes, l.dtype);
     if (!l.workspace(given, need, &ws)) Py_RETURN_NONE;
     Tensor stats = l.make({6}), logp = l.make({l.rows});
-    if (a.flag(13)) {
+    if (save) {
       saved = l.make({l.rows, 4});
       row_grads = l.make({2, l.rows});
     }
@@ -277,6 +286,7 @@ PyObject* preference(PyObject*, PyObject* const* args, Py_ssize_t n) {
     p.beta = float(a.number(4));
     p.label_smoothing = float(a.number(5));
     p.grad_scale = float(a.number(6));
+    const bool want_grad = a.flag(7), save = a.flag(8);
     const acdc_stream_t stream = a.stream(11);
     Logits l;
     if (a.bad || !l.read(x, t)) Py_RETURN_NONE;
@@ -288,11 +298,11 @@ PyObject* preference(PyObject*, PyObject* const* args, Py_ssize_t n) {
       Py_RETURN_NONE;
     Tensor grad, saved, row_grads, ws;
     int64_t grad_stride = l.classes;
-    if (a.flag(7) && !l.gradient(out, &grad, &grad_stride)) Py_RETURN_NONE;
+    if (want_grad && !l.gradient(out, &grad, &grad_stride)) Py_RETURN_NONE;
     const size_t need = acdc_preference_workspace_size(l.rows, l.classes, l.dtype, pairs);
     if (!l.workspace(given, need, &ws)) Py_RETURN_NONE;
     Tensor stats = l.make({5}), logp = l.make({l.rows});
-    if (a.flag(8)) {
+    if (save) {
       saved = l.make({l.rows, 4});
       row_grads = l.make({2, l.rows});
     }

@@ -213,3 +213,14 @@ def test_tensors_without_memory_are_refused(env, part):
         with pytest.raises(ValueError):
             optim.grad_norm(**kw)
     assert (p == 1).all() and (half == 1).all() and not s32[0].any()
+
+
+def test_options_without_a_truth_value(env):
+    torch, losses, _ = env
+    x, t, f = torch.randn(4, 10, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, device="cuda")
+    off, two = torch.tensor([0, 2, 4], device="cuda"), torch.ones(2)
+    for call in (lambda: losses.token_logprobs(x, t, entropy=two), lambda: losses.token_logprobs(x, t, save=two),
+                 lambda: losses.policy_loss(x, t, f, f, mean=two), lambda: losses.policy_loss(x, t, f, f, grad=two),
+                 lambda: losses.preference_loss(x, t, off, f, save=two)):
+        with pytest.raises(RuntimeError, match="[Bb]oolean"):
+            call()
