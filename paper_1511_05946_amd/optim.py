@@ -41,6 +41,10 @@ def _lazy(t) -> bool:
     return t.is_conj() or t.is_neg()
 
 
+def _listed(items):
+    return items if isinstance(items, (list, tuple)) else list(items)
+
+
 def _native_stream(tensors):
     """The current stream, if the native part of the binding can take tensors
     of the first one's device; None leaves them to the code that checks one by
@@ -102,7 +106,7 @@ def _refuse(i, p, g, master, n, device):
 
 def adamw_step(params, grads, moments, step: int, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01,
                masters=None, grad_scale=None):
-    """One AdamW step of every tensor, in place:
+    """One AdamW step of every tensor, in place (lists or other iterables of as many each):
 
         m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2
         w = w (1 - lr weight_decay) - lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps)
@@ -113,6 +117,9 @@ def adamw_step(params, grads, moments, step: int, lr=1e-3, betas=(0.9, 0.999), e
     rounded into it, or None.  ``grad_scale``: a float32 tensor of one value
     that multiplies every gradient, such as ``grad_norm(...)[1:]``; where it is
     not finite the step leaves everything as it is."""
+    params, grads, moments = _listed(params), _listed(grads), _listed(moments)
+    if masters is not None:
+        masters = _listed(masters)
     stream = _native_stream(params)
     if stream is not None:
         rc = binding().adamw(params, grads, moments, masters, lr, weight_decay, betas[0], betas[1], eps, step, grad_scale,
@@ -161,6 +168,7 @@ def grad_norm(grads, max_norm=None, out=None):
     """[norm, scale] on the device: the 2-norm of all gradients together and the
     factor min(1, max_norm / (norm + 1e-6)) that clips them (1 without
     ``max_norm``), which ``adamw_step`` takes as ``grad_scale=result[1:]``."""
+    grads = _listed(grads)
     stream = _native_stream(grads)
     if stream is not None and (max_norm is None or max_norm > 0):
         r = binding().grad_norm(grads, max_norm or 0.0, out, stream)

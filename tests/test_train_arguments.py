@@ -153,3 +153,23 @@ def test_workspaces_that_do_not_hold_their_size_are_refused(calls):
         with pytest.raises(ValueError, match="workspace"):
             losses.token_logprobs(x, t, workspace=ws)
     assert not calls
+
+
+def test_any_iterable_of_tensors(calls):
+    """Generators, as modules give their parameters, and views of dictionaries."""
+    from paper_1511_05946_amd import optim
+    layer = torch.nn.Linear(4, 3)
+    for p in layer.parameters():
+        p.grad = torch.ones_like(p)
+    state = {name: optim.moments(p) for name, p in layer.named_parameters()}
+    optim.adamw_step(layer.parameters(), (p.grad for p in layer.parameters()), state.values(), 1)
+    optim.grad_norm(p.grad for p in layer.parameters())
+    half = {k: torch.ones(4).bfloat16() for k in "ab"}
+    full = {k: torch.ones(4) for k in "ab"}
+    optim.adamw_step(half.values(), full.values(), [optim.moments(p) for p in full.values()], 1,
+                     masters=(full[k].clone() for k in "ab"))
+    assert len(calls) == 3 and [c[1] for c in calls if len(c) == 7] == [2, 2]
+    with pytest.raises(ValueError, match="one length"):
+        optim.adamw_step(layer.parameters(), iter([]), state.values(), 1)
+    with pytest.raises(ValueError, match="a tensor at least"):
+        optim.grad_norm(iter([]))
