@@ -51,8 +51,21 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = False, extra_flags: list[str] | None = None) -> str:
-    """Compile every csrc/*.hip to an object (in parallel), then link libacdc.so
-    and, against it, the binding's native part."""
+    """libacdc.so and, where the host has what that takes, the binding's native
+    part against it.  The library and its C ABI need hipcc alone."""
+    build_library(verbose, extra_flags)
+    missing = missing_for_binding()
+    if missing is None:
+        build_binding(verbose)
+    else:
+        if os.path.exists(BINDING):
+            os.remove(BINDING)   # an older library's
+        sys.stderr.write(f"no {missing}: {os.path.basename(BINDING)} is not built, which losses and optim need\n")
+    return LIB
+
+
+def build_library(verbose: bool = False, extra_flags: list[str] | None = None) -> str:
+    """Compile every csrc/*.hip to an object (in parallel), then link libacdc.so."""
     import tempfile
     srcs = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".hip"))
     with tempfile.TemporaryDirectory(prefix="acdc_build_") as tmpdir:
@@ -81,8 +94,22 @@ def build(verbose: bool = False, extra_flags: list[str] | None = None) -> str:
             sys.stderr.write(proc.stdout + proc.stderr)
             raise RuntimeError(f"hipcc link failed ({proc.returncode})")
         os.replace(tmp, LIB)
-    build_binding(verbose)
     return LIB
+
+
+def host_compiler() -> str | None:
+    return shutil.which(os.environ.get("CXX", "g++"))
+
+
+def missing_for_binding() -> str | None:
+    """What this host lacks for the binding's native part."""
+    import importlib.util
+    import sysconfig
+    if host_compiler() is None:
+        return "host C++ compiler (g++)"
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return "Python.h"
+    return None if importlib.util.find_spec("torch") is not None else "torch"
 
 
 def build_binding(verbose: bool = False) -> str:
@@ -91,9 +118,9 @@ def build_binding(verbose: bool = False) -> str:
 
     import torch
     from torch.utils.cpp_extension import include_paths
-    cxx = shutil.which(os.environ.get("CXX", "g++"))
-    if cxx is None:
-        raise RuntimeError("no host C++ compiler (g++) found")
+    missing, cxx = missing_for_binding(), host_compiler()
+    if missing is not None:
+        raise RuntimeError(f"no {missing} found")
     includes = [a for p in (*include_paths(), sysconfig.get_paths()["include"]) for a in ("-isystem", p)]
     tmp = BINDING + ".tmp"
     cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
