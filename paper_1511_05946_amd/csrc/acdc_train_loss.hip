@@ -1081,9 +1081,11 @@ __global__ __launch_bounds__(WG) void k_pairs(PairArgs a, const float4* __restri
     }
     const float good = float(a.beta * v0), bad = float(a.beta * v1), m = float(a.beta * (v0 - v1)), e = a.smoothing;
     // -log sigmoid(+-m) and sigmoid(+-m) out of one exponential, z = exp(-|m|) <= 1.
-    // A NaN margin is no win, and gives NaN slopes.
+    // A NaN margin is no win, and gives NaN slopes.  An infinite one (a token of
+    // probability 0) costs nothing on the side that the smoothing leaves out.
     const float z = expf(-fabsf(m)), q = 1.f / (1.f + z);
-    const float loss = log1pf(z) + (m < 0.f ? -(1.f - e) * m : e * m);
+    const float share = m < 0.f ? 1.f - e : e;
+    const float loss = log1pf(z) + (share > 0.f ? share * fabsf(m) : 0.f);
     const float up = m < 0.f ? z * q : q, down = m < 0.f ? q : z * q;
     const float slope = (e * up - (1.f - e) * down) * (a.beta / float(a.pairs));
 #pragma unroll 4

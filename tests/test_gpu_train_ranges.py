@@ -1,0 +1,56 @@
+"""The losses and the optimiser on the GPU where values are infinite, 0, or near
+the ends of what 32 bits hold."""
+
+import numpy as np
+import pytest
+
+import train_reference as R
+
+pytestmark = pytest.mark.gpu
+
+INF = float("inf")
+
+
+@pytest.fixture(scope="module")
+def env():
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1511_05946_amd import losses, optim
+    return torch, losses, optim
+
+
+@pytest.mark.parametrize("pairs", [4, 20])   # a wave for each, a workgroup for each
+def test_preference_with_tokens_of_probability_0(env, pairs):
+    """Pair 0 has one in the other sequence, pair 1 none: the loss of a margin of +inf
+    is 0 without smoothing, and its gradient. With smoothing, or in the preferred
+    sequence, the loss is infinite and the slope is not."""
+    torch, losses, _ = env
+    print(f"[case] preference probability 0, {pairs} pairs", flush=True)
+    V, rows = 33, 4 * pairs
+    x = torch.randn(rows, V, generator=torch.Generator().manual_seed(pairs))
+    t = torch.full((rows,), 2)
+    offsets = torch.arange(0, rows + 1, 2)
+    ref = torch.full((rows,), -3.0)
+    for sequence, e, loss_is_finite in ((1, 0.0, True), (1, 0.25, False), (0, 0.0, False), (0, 1.0, True)):
+        y = x.clone()
+        y[2 * sequence, 2] = -INF
+        r = losses.preference_loss(y.cuda(), t.cuda(), offsets.cuda(), ref.cuda(), beta=0.5, label_smoothing=e, save=True)
+        p, logp, ent, spread = R.rows(y.double().numpy(), t.numpy())
+        reward = 0.5 * (logp - ref.double().numpy()).reshape(-1, 2).sum(1)
+        m = reward[0::2] - reward[1::2]
+        assert m[0] == (INF if sequence else -INF) and np.isfinite(m[1:]).all()
+        loss = (0.0 if e == 1 else (1 - e) * np.logaddexp(0, -m)) + (0.0 if e == 0 else e * np.logaddexp(0, m))
+        assert np.isfinite(loss.mean()) == loss_is_finite
+        # a margin moves by beta times its rows' errors, the loss by no more
+        tol = 0.5 * R.logp_tolerance(logp, spread).sum() + 16 * R.EPS * (np.abs(m[1:]).mean() + 1)
+        got = r.stats.double().cpu().numpy()
+        assert got[0] == loss.mean() or abs(got[0] - loss.mean()) <= tol
+        assert got[1] == pytest.approx((m > 0).mean(), abs=1e-6) and got[2] == m.mean()
+        slope = (e / (1 + np.exp(-m)) - (1 - e) / (1 + np.exp(m))) * 0.5 / pairs
+        g = np.repeat(np.stack([slope, -slope], 1).reshape(-1), 2)
+        want = R.gradient(p, ent, t.numpy(), g, np.zeros(rows))
+        gtol = R.gradient_tolerance(p, want, ent, spread, t.numpy(), g, np.zeros(rows), False) + tol * 0.5
+        assert np.all(np.abs(r.grad_logits.double().cpu().numpy() - want) <= gtol)
+        if loss_is_finite:
+            assert not r.grad_logits[:4].any()
