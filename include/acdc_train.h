@@ -65,7 +65,8 @@ int acdc_logprob_backward(const void* logits, int32_t dtype, int64_t stride, con
  * and the total sum_r w_r loss_r / W, W = sum_r w_r (with mean = 0: not
  * divided).  weights >= 0 (null: 1 each); a row of weight 0 takes no part,
  * like one with a negative target.  W = 0 gives a loss and gradients of 0.
- * logp_ref may be null when kl_coef = 0 (kl is then 0).
+ * logp_ref may be null when kl_coef = 0 (kl is then 0); where it is given all the
+ * same, it serves the stats alone.
  *
  * stats, 6 floats: the total, and the weighted sums (means with mean != 0) of
  * policy, kl, H, the share of rows whose ratio was clipped away, and ratio.

@@ -449,9 +449,12 @@ __device__ __forceinline__ PolicyRow policy_row(const acdc_policy_params& p, flo
     kl = em - k;
   }
   PolicyRow r;
-  r.g = w * ((cut ? 0.f : -free_) - p.kl_coef * em);
+  // (a coefficient of 0, with the reference's values for the stats alone, leaves
+  // them out: far from the reference they are infinite)
+  const bool counts = p.kl_coef != 0.f;
+  r.g = w * ((cut ? 0.f : -free_) - (counts ? p.kl_coef * em : 0.f));
   r.h = -p.entropy_coef * w;
-  r.v[0] = w * (policy + p.kl_coef * kl - p.entropy_coef * entropy);
+  r.v[0] = w * (policy + (counts ? p.kl_coef * kl : 0.f) - p.entropy_coef * entropy);
   r.v[1] = w * policy;
   r.v[2] = w * kl;
   r.v[3] = w * entropy;

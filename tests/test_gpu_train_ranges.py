@@ -54,3 +54,30 @@ def test_preference_with_tokens_of_probability_0(env, pairs):
         assert np.all(np.abs(r.grad_logits.double().cpu().numpy() - want) <= gtol)
         if loss_is_finite:
             assert not r.grad_logits[:4].any()
+
+
+# every way the policy loss takes: rows in one workgroup and in several, of 16 lanes, a wave
+# and a workgroup each, in one pass; rows in parts
+PLANS = [(4, 10, "float32"), (100, 20, "bfloat16"), (10, 300, "float32"), (100, 300, "float32"), (80, 5000, "float32"),
+         (3, 70000, "bfloat16"), (130, 70000, "float32")]
+
+
+@pytest.mark.parametrize("rows,V,dtype", PLANS)
+def test_reference_for_the_stats_alone(env, rows, V, dtype):
+    """With a coefficient of 0 the loss and the gradient are those without the reference,
+    to the bit, however far it is; the KL of a row far from it is infinite."""
+    torch, losses, _ = env
+    print(f"[case] reference without a coefficient {rows} x {V} {dtype}", flush=True)
+    x = torch.randn(rows, V, generator=torch.Generator().manual_seed(V)).to(getattr(torch, dtype)).cuda()
+    t = torch.full((rows,), 3, device="cuda")
+    x[1, 3] = -INF   # a token of probability 0, which the reference thinks possible
+    old, adv = torch.full((rows,), -4.0, device="cuda"), torch.linspace(-1, 1, rows, device="cuda")
+    ref = torch.full((rows,), -4.0, device="cuda")
+    ref[0], ref[2] = 200.0, -INF
+    for grad in (True, False):
+        a = losses.policy_loss(x, t, old, adv, entropy_coef=0.01, grad=grad, save=True)
+        b = losses.policy_loss(x, t, old, adv, logp_ref=ref, entropy_coef=0.01, grad=grad, save=True)
+        assert torch.isfinite(a.stats).all()
+        keep = [0, 1, 3, 4, 5]
+        assert torch.equal(a.stats[keep], b.stats[keep]) and torch.equal(a.row_grads, b.row_grads)
+        assert not grad or (torch.isfinite(b.grad_logits).all() and torch.equal(a.grad_logits, b.grad_logits))
