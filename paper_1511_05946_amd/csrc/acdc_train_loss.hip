@@ -446,7 +446,7 @@ __device__ __forceinline__ PolicyRow policy_row(const acdc_policy_params& p, flo
   if (has_ref) {
     const float k = ref - logp;
     em = expm1f(k);  // exp(k) - 1 - k of policies close to each other is a small difference
-    kl = em - k;
+    kl = k < __builtin_inff() ? em - k : em;  // (a token of probability 0: infinite, not inf - inf)
   }
   PolicyRow r;
   // (a coefficient of 0, with the reference's values for the stats alone, leaves

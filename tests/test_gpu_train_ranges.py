@@ -81,3 +81,26 @@ def test_reference_for_the_stats_alone(env, rows, V, dtype):
         keep = [0, 1, 3, 4, 5]
         assert torch.equal(a.stats[keep], b.stats[keep]) and torch.equal(a.row_grads, b.row_grads)
         assert not grad or (torch.isfinite(b.grad_logits).all() and torch.equal(a.grad_logits, b.grad_logits))
+
+
+@pytest.mark.parametrize("rows,V,dtype", PLANS)
+def test_kl_of_infinite_ratios(env, rows, V, dtype):
+    """exp(k) - k - 1 grows without bound on both sides: a token that only one of the
+    policies thinks possible has an infinite KL, not NaN."""
+    torch, losses, _ = env
+    print(f"[case] infinite KL {rows} x {V} {dtype}", flush=True)
+    x = torch.randn(rows, V, generator=torch.Generator().manual_seed(V)).to(getattr(torch, dtype)).cuda()
+    t = torch.full((rows,), 3, device="cuda")
+    old, adv = torch.full((rows,), -4.0, device="cuda"), torch.linspace(-1, 1, rows, device="cuda")
+    for policy_possible in (True, False):
+        y, ref = x.clone(), torch.full((rows,), -4.0, device="cuda")
+        if policy_possible:
+            ref[1] = -INF
+        else:
+            y[1, 3] = -INF
+        for coef in (0.0, 0.5):
+            for grad in (True, False):
+                r = losses.policy_loss(y, t, old, adv, logp_ref=ref, kl_coef=coef, grad=grad)
+                assert r.stats[2].item() == INF and (r.stats[0].item() == INF if coef else torch.isfinite(r.stats[0]))
+                if grad:   # the other rows' gradients are what they are
+                    assert torch.isfinite(r.grad_logits[0]).all() and torch.isfinite(r.grad_logits[2:]).all()
