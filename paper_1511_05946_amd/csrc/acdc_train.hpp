@@ -123,6 +123,15 @@ __device__ __forceinline__ float wave_sum(float v) {
   return over_wave(v, [](float a, float b) { return a + b; });
 }
 
+// What a wave's lanes wrote to LDS before it, all of its lanes may read after it.
+// (The lanes run together, but without it the compiler may order one lane's load
+// before another's store: to a single thread they are different addresses.)
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // ------------------------------------------------------------- host checks
 inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline size_t dtype_bytes(int32_t dtype) { return dtype == ACDC_F32 ? 4 : dtype == ACDC_BF16 ? 2 : 0; }

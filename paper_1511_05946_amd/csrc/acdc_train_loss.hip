@@ -955,6 +955,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_policy_tile(
       for (int c = 0; c < NC; ++c) held[first + q][c][lane] = raw[q][c];
       rest[first + q][lane] = extra[q];
     }
+    wave_sync();  // the rows' targets and a target's logit are other lanes'
 #pragma unroll 1
     for (int i = first; i < last; ++i) {
       const int t = uniform(target[i]);
