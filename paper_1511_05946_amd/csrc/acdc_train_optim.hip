@@ -355,16 +355,18 @@ __device__ __forceinline__ double square_sum(const typename G::Elem* p, int coun
       raw[q] = typename G::Raw{};
       if (at + q * kStep < full) raw[q] = load_chunk<G>(p + at + q * kStep);
     }
-    float s = 0.f;  // up to 32 squares in 32 bits
+    // in 64 bits, which no square of a gradient leaves: 32 end at 1.8e19 and 1e-23
 #pragma unroll
     for (int q = 0; q < kNormRounds; ++q)
 #pragma unroll
-      for (int i = 0; i < G::kPer; ++i) s += G::get(raw[q], i) * G::get(raw[q], i);
-    total += double(s);
+      for (int i = 0; i < G::kPer; ++i) {
+        const double v = G::get(raw[q], i);
+        total += v * v;
+      }
   }
   if (full + int(threadIdx.x) < count) {
-    const float v = G::one(p[full + threadIdx.x]);
-    total += double(v * v);
+    const double v = G::one(p[full + threadIdx.x]);
+    total += v * v;
   }
   return total;
 }
@@ -395,10 +397,11 @@ __global__ __launch_bounds__(kWide) void k_norm(const double* __restrict__ sums,
   for (long long i = threadIdx.x; i < n; i += kWide) s += sums[i];
   s = sum_workgroup(s, part, kWide / 64);
   if (threadIdx.x == 0) {
-    const float norm = float(sqrt(s));
-    out[0] = norm;
-    const float c = max_norm / (norm + 1e-6f);
-    out[1] = max_norm > 0.f ? (c > 1.f ? 1.f : c) : 1.f;  // NaN stays
+    const double norm = sqrt(s);
+    out[0] = float(norm);
+    // (of the norm in 64 bits: one past what a float holds still clips to max_norm)
+    const double c = double(max_norm) / (norm + 1e-6);
+    out[1] = max_norm > 0.f ? float(c > 1.0 ? 1.0 : c) : 1.f;  // NaN stays
   }
 }
 

@@ -104,3 +104,22 @@ def test_kl_of_infinite_ratios(env, rows, V, dtype):
                 assert r.stats[2].item() == INF and (r.stats[0].item() == INF if coef else torch.isfinite(r.stats[0]))
                 if grad:   # the other rows' gradients are what they are
                     assert torch.isfinite(r.grad_logits[0]).all() and torch.isfinite(r.grad_logits[2:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("size", [1e-35, 1e-25, 1e-12, 1e12, 1e20, 1e30, 3e38])
+def test_norm_of_gradients_of_every_size(env, dtype, size):
+    """Squares of what 32 bits hold, past what 32 bits hold: tensors with a value far
+    below, of odd lengths, and a norm that a float does not hold."""
+    torch, _, optim = env
+    print(f"[case] norm {size} {dtype}", flush=True)
+    rng = np.random.RandomState(3)
+    grads = [torch.from_numpy((size * rng.choice([-1, 1, 0.25], n)).astype(np.float32)).to(getattr(torch, dtype)).cuda()
+             for n in (1, 1003, 70001)]
+    grads.append(torch.full((5,), 1e-30, device="cuda"))
+    want = np.sqrt(sum(float(g.double().square().sum()) for g in grads))
+    # one rounding of a sum in 64 bits, and of the coefficient
+    got = optim.grad_norm(grads, max_norm=0.5).double().tolist()
+    assert got[0] == pytest.approx(want, rel=2 * R.EPS, abs=0) if want < 3.4e38 else got[0] == INF
+    coef = min(1.0, 0.5 / (want + 1e-6))
+    assert abs(got[1] - coef) <= 2 * R.EPS * coef + 2.0 ** -149
