@@ -250,13 +250,21 @@ __global__ __launch_bounds__(kThreads) void k_adamw(LIST b, int count, Step s) {
   const Rate rate = b.rate[b.rate_of(i)];
   t.rate = rate.rate;
   t.decay = rate.decay;
-  float c1 = s.c1, c2 = s.c2;
+  float c1 = s.c1, c2 = s.c2, first = 1.f;
   if (s.grad_scale != nullptr) {
     const float gs = *s.grad_scale;
     if (!(gs - gs == 0.f)) return;
-    // the gradient's scale goes into the factors of g and g^2, each rounded once
+    // The gradient's scale goes into the factors of g and g^2, each rounded once.
+    // Where a factor is not a normal number (the scale's square leaves 32 bits from
+    // about 1e-18 and 1e20 on), the gradient is scaled first and rounded itself.
     c1 = float(s.one1 * double(gs));
     c2 = float(s.one2 * (double(gs) * double(gs)));
+    auto normal = [](float c) { return fabsf(c) >= 0x1p-126f && fabsf(c) < __builtin_inff(); };
+    if (!normal(c1) || !normal(c2)) {
+      first = gs;
+      c1 = s.c1;
+      c2 = s.c2;
+    }
   }
   // a wave's 256 elements are one block of scales
   const long long base = (long long)(int(blockIdx.x) - b.first[i]) * kChunk + (threadIdx.x / 64) * kBlock;
@@ -282,8 +290,9 @@ __global__ __launch_bounds__(kThreads) void k_adamw(LIST b, int count, Step s) {
     // stand a whole step of its format off
 #pragma clang fp contract(off)
     if constexpr (BITS == 8) v[k] *= v[k];
-    m[k] = s.beta1 * m[k] + c1 * g[k];
-    v[k] = s.beta2 * v[k] + c2 * g[k] * g[k];
+    const float x = first * g[k];
+    m[k] = s.beta1 * m[k] + c1 * x;
+    v[k] = s.beta2 * v[k] + c2 * x * x;
   }
   float root[4];
   roots4(v, root);

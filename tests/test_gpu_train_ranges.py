@@ -123,3 +123,29 @@ def test_norm_of_gradients_of_every_size(env, dtype, size):
     assert got[0] == pytest.approx(want, rel=2 * R.EPS, abs=0) if want < 3.4e38 else got[0] == INF
     coef = min(1.0, 0.5 / (want + 1e-6))
     assert abs(got[1] - coef) <= 2 * R.EPS * coef + 2.0 ** -149
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("scale", [1e-35, 1e-22, 1e-18, 1e18, 1e22, 1e30])
+def test_scales_of_every_size(env, bits, scale):
+    """Gradients whose scaled values are ordinary: the steps of those values. First from
+    zero moments, where a second moment of 0 would divide by eps alone; and gradients
+    of 0, which no scale makes anything else."""
+    torch, _, optim = env
+    print(f"[case] adamw scale {scale} {bits} bits", flush=True)
+    rng = np.random.RandomState(4)
+    gs = torch.tensor([scale], dtype=torch.float32, device="cuda")
+    g = (rng.choice([-1, 1], 1000) * (0.5 + rng.rand(1000)) / scale).astype(np.float32)
+    g[100:120] = 0
+    p = torch.ones(1000, device="cuda")
+    state = optim.moments(p, bits)
+    w, m, v = np.ones(1000), np.zeros(1000), np.zeros(1000)
+    scaled = g.astype(float) * gs.double().item()
+    for step in (1, 2):
+        optim.adamw_step([p], [torch.from_numpy(g).cuda()], [state], step, lr=0.01, eps=1e-8, weight_decay=0.0, grad_scale=gs)
+        w, m, v, move = R.adamw(w, scaled, m, v, step, 0.01, (0.9, 0.999), 1e-8, 0.0)
+    # two steps: roundings of w and of each step; with 8 bits a code of m and one of the
+    # root of v, each within 1/16, in the second
+    bound = 8 * R.EPS * 2 + move * (32 * R.EPS if bits == 32 else 2 / 16 + 1 / 64)
+    assert np.all(np.abs(p.double().cpu().numpy() - w) <= bound)
+    assert (p[100:120] == 1).all()
