@@ -168,14 +168,12 @@ __device__ __forceinline__ void decode4(unsigned w, float scale, float (&v)[4]) 
   v[3] = b[1] * scale;
 }
 // Codes of four values of a block with this scale; positive values stay
-// positive with POSITIVE.  A NaN keeps its own code (the block's scale comes
-// from the others), and so does an infinity, as NaN.  The quotient v / scale is
+// positive with POSITIVE.  A NaN keeps its own code.  The quotient v / scale is
 // correctly rounded: with r the rounded reciprocal, q + r (v - q scale) of q = v r
 // is (Markstein's division), three instructions a value and one division a block.
 template <bool POSITIVE>
 __device__ __forceinline__ unsigned encode4(const float (&v)[4], float scale) {
-  // a scale of 0 or infinity has codes of 0 (and NaN)
-  const float s = scale < 0x1.fffffep127f ? scale : 0.f, r = s > 0.f ? 1.f / s : 0.f;
+  const float s = scale, r = s > 0.f ? 1.f / s : 0.f;  // (a scale of 0 has codes of 0, and NaN)
   float q[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -210,8 +208,19 @@ __device__ __forceinline__ void roots4(const float (&v)[4], float (&root)[4]) {
 // Scale of a wave's block out of each lane's four values.  Blocks below 2^-100
 // are 0: their scale would leave the normal numbers.  (The product may leave the
 // largest element a rounding away from 448, which its code does not see.)
-__device__ __forceinline__ float scale_of(const float (&v)[4]) {
-  const float top = wave_max(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
+// Infinities become NaN, which no maximum sees: their block keeps a scale for
+// the others.
+__device__ __forceinline__ float block_top(const float (&v)[4]) {
+  return wave_max(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
+}
+__device__ __forceinline__ float scale_of(float (&v)[4]) {
+  float top = block_top(v);
+  if (top == __builtin_inff()) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (fabsf(v[i]) == __builtin_inff()) v[i] = __builtin_nanf("");
+    top = block_top(v);
+  }
   return top < 0x1p-100f ? 0.f : top * kPerTop;
 }
 

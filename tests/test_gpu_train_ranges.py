@@ -149,3 +149,34 @@ def test_scales_of_every_size(env, bits, scale):
     bound = 8 * R.EPS * 2 + move * (32 * R.EPS if bits == 32 else 2 / 16 + 1 / 64)
     assert np.all(np.abs(p.double().cpu().numpy() - w) <= bound)
     assert (p[100:120] == 1).all()
+
+
+@pytest.mark.parametrize("value", [INF, -INF, 1e25])
+def test_infinity_stays_in_its_element(env, value):
+    """8-bit moments: an infinite gradient, or one whose square is, spoils its element at
+    most; the others go as beside a NaN, to the bit, the block's scale with them."""
+    torch, _, optim = env
+    got = []
+    for g_value in (value, float("nan")):
+        p, state = torch.ones(700, device="cuda"), optim.moments(torch.ones(700, device="cuda"), 8)
+        gen = torch.Generator().manual_seed(7)
+        for step in (1, 2, 3):
+            g = torch.randn(700, generator=gen)
+            if step == 2:
+                g[300] = g_value
+            optim.adamw_step([p], [g.cuda()], [state], step, lr=0.01)
+        got.append((p, [s.float() for s in state]))
+        assert all(torch.isfinite(s).all() for s in state[2:])
+    (p, state), (q, beside) = got
+    others = torch.arange(700, device="cuda") != 300
+    assert torch.isfinite(p[others]).all()
+    if abs(value) == INF:
+        assert torch.equal(p[others], q[others])
+        assert all(torch.equal(a[others] if a.numel() == 700 else a, b[others] if a.numel() == 700 else b)
+                   for a, b in zip(state, beside))
+    else:   # a finite m takes its block's scale of m, v's is that of the others
+        apart = torch.arange(700, device="cuda") // 256 != 1
+        assert torch.equal(p[apart], q[apart]) and torch.equal(state[1][others], beside[1][others])
+        assert torch.equal(state[3], beside[3])
+    assert torch.isnan(state[1][300]) and torch.isfinite(state[1][others]).all()
+    assert torch.isnan(state[0][300]) == (abs(value) == INF)
