@@ -135,14 +135,18 @@ typedef struct acdc_adamw_tensor {
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
  *   w = w (1 - lr weight_decay) - lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps)
  * in 32 bits, w the master or the parameter; step counts from 1.  A grad_scale
- * that is not finite leaves every tensor as it is.  `tensors` is a host array
+ * that is not finite, or is -0, leaves every tensor as it is: what acdc_grad_norm
+ * gives for gradients that hold a NaN or an infinity.  `tensors` is a host array
  * that is read before the call returns; no two tensors may overlap. */
 int acdc_adamw_step(const acdc_adamw_tensor* tensors, int32_t count, double beta1, double beta2, double eps,
                     int64_t step, const float* grad_scale, acdc_stream_t stream);
 
 /* out[0] = 2-norm of all gradients together, out[1] = min(1, max_norm /
  * (out[0] + 1e-6)), or 1 with max_norm <= 0 (no clipping): a grad_scale for
- * acdc_adamw_step.  `grads`, `sizes`, `types` are host arrays of `count`. */
+ * acdc_adamw_step.  The norm is computed in 64 bits, as is the quotient.  An
+ * infinite gradient gives inf and -0, a NaN gives NaN twice, so that the step
+ * with that scale changes nothing (with 1, without clipping, it spoils the
+ * elements in question).  `grads`, `sizes`, `types` are host arrays of `count`. */
 int acdc_grad_norm(const void* const* grads, const int64_t* sizes, const int32_t* types, int32_t count,
                    float max_norm, float* out, void* workspace, size_t workspace_bytes, acdc_stream_t stream);
 size_t acdc_grad_norm_workspace_size(const int64_t* sizes, int32_t count);

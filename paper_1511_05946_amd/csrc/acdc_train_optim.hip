@@ -262,7 +262,8 @@ __global__ __launch_bounds__(kThreads) void k_adamw(LIST b, int count, Step s) {
   float c1 = s.c1, c2 = s.c2, first = 1.f;
   if (s.grad_scale != nullptr) {
     const float gs = *s.grad_scale;
-    if (!(gs - gs == 0.f)) return;
+    // not finite, or -0: a gradient is NaN or infinite, and 0 * inf would spoil its element
+    if (!(gs - gs == 0.f) || __float_as_uint(gs) == 0x80000000u) return;
     // The gradient's scale goes into the factors of g and g^2, each rounded once.
     // Where a factor is not a normal number (the scale's square leaves 32 bits from
     // about 1e-18 and 1e20 on), the gradient is scaled first and rounded itself.
@@ -419,7 +420,8 @@ __global__ __launch_bounds__(kWide) void k_norm(const double* __restrict__ sums,
     out[0] = float(norm);
     // (of the norm in 64 bits: one past what a float holds still clips to max_norm)
     const double c = double(max_norm) / (norm + 1e-6);
-    out[1] = max_norm > 0.f ? float(c > 1.0 ? 1.0 : c) : 1.f;  // NaN stays
+    // NaN stays; the 0 of an infinite norm goes as -0, which the step knows
+    out[1] = max_norm > 0.f ? (norm == double(__builtin_inff()) ? -0.f : float(c > 1.0 ? 1.0 : c)) : 1.f;
   }
 }
 

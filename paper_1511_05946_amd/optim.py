@@ -116,7 +116,8 @@ def adamw_step(params, grads, moments, step: int, lr=1e-3, betas=(0.9, 0.999), e
     per tensor the float32 copy of a bfloat16 parameter that is updated and
     rounded into it, or None.  ``grad_scale``: a float32 tensor of one value
     that multiplies every gradient, such as ``grad_norm(...)[1:]``; where it is
-    not finite the step leaves everything as it is."""
+    not finite, or -0, the step leaves everything as it is: what ``grad_norm`` with
+    a ``max_norm`` gives for gradients that hold a NaN or an infinity."""
     params, grads, moments = _listed(params), _listed(grads), _listed(moments)
     if masters is not None:
         masters = _listed(masters)
@@ -167,7 +168,8 @@ def adamw_step(params, grads, moments, step: int, lr=1e-3, betas=(0.9, 0.999), e
 def grad_norm(grads, max_norm=None, out=None):
     """[norm, scale] on the device: the 2-norm of all gradients together and the
     factor min(1, max_norm / (norm + 1e-6)) that clips them (1 without
-    ``max_norm``), which ``adamw_step`` takes as ``grad_scale=result[1:]``."""
+    ``max_norm``), which ``adamw_step`` takes as ``grad_scale=result[1:]``. The 0 of
+    an infinite norm is -0, with which the step is left out as with NaN."""
     grads = _listed(grads)
     stream = _native_stream(grads)
     if stream is not None and (max_norm is None or max_norm > 0):

@@ -180,3 +180,38 @@ def test_infinity_stays_in_its_element(env, value):
         assert torch.equal(state[3], beside[3])
     assert torch.isnan(state[1][300]) and torch.isfinite(state[1][others]).all()
     assert torch.isnan(state[0][300]) == (abs(value) == INF)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("kind", ["f32", "master"])
+@pytest.mark.parametrize("value", [INF, -INF, float("nan"), 1e20])
+def test_clipped_step_of_infinite_gradients(env, bits, kind, value):
+    """grad_norm and adamw_step together: an overflow leaves every tensor as it is, also
+    where the coefficient is divided by a loss scale; finite gradients of any size are clipped."""
+    torch, _, optim = env
+    print(f"[case] clipped step with a gradient of {value}, {kind} {bits} bits", flush=True)
+    dt = torch.float32 if kind == "f32" else torch.bfloat16
+    w = torch.linspace(0.5, 1.5, 900, device="cuda")
+    params = [w.to(dt).clone(), w[:5].to(dt).clone()]
+    masters = None if kind == "f32" else [w.clone(), w[:5].clone()]
+    moments = [optim.moments(p, bits) for p in params]
+    grads = [torch.ones_like(p) for p in params]
+    optim.adamw_step(params, grads, moments, 1, masters=masters)
+    tensors = [*params, *(masters or []), *(s for m in moments for s in m)]
+    before = [t.clone().view(torch.uint8) for t in tensors]
+    grads[0][300] = value
+    clip = optim.grad_norm(grads, max_norm=1.0)
+    for scale in (clip[1:], clip[1:] / 1024):
+        optim.adamw_step(params, grads, moments, 2, masters=masters, grad_scale=scale)
+    same = [torch.equal(a, b.view(torch.uint8)) for a, b in zip(before, tensors)]
+    if value == 1e20:
+        assert clip[1].item() == pytest.approx(1 / grads[0][300].item(), rel=4 * R.EPS, abs=0) and not all(same)
+        assert all(torch.isfinite(t.float()).all() for t in tensors)
+    else:
+        assert all(same)
+        assert clip[1].item() == 0 if abs(value) == INF else torch.isnan(clip).all()
+    # a scale of 0 is a scale: decay alone
+    zero = [p.clone() for p in params[:1]]
+    optim.adamw_step(zero, [torch.ones_like(zero[0])], [optim.moments(zero[0], bits)], 1, lr=0.5, weight_decay=0.5,
+                     grad_scale=torch.zeros(1, device="cuda"))
+    assert torch.allclose(zero[0].float(), 0.75 * params[0].float(), rtol=2.0 ** -7)
