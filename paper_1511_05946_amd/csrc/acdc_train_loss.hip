@@ -1194,6 +1194,11 @@ Workspace layout(int64_t rows, int32_t classes, int32_t dtype, int64_t pairs) {
   w.total = at;
   return w;
 }
+// Of the log-probabilities alone: the parts of rows, where they come in parts.
+size_t logprob_bytes(int64_t rows, int32_t classes, int32_t dtype) {
+  const int split = split_of(rows, classes, dtype);
+  return up256(std::max<size_t>(1, split > 1 ? size_t(rows) * split * sizeof(float4) : 0));
+}
 bool sizes_ok(int64_t rows, int32_t classes, int32_t dtype) {
   return dtype_bytes(dtype) != 0 && rows >= 0 && rows <= 0x7fffffff && classes >= 1;
 }
@@ -1313,7 +1318,7 @@ void with_row_shape(int chunks, F&& f) {
 using namespace acdc;
 
 extern "C" size_t acdc_logprob_workspace_size(int64_t rows, int32_t classes, int32_t dtype) {
-  return sizes_ok(rows, classes, dtype) ? layout(rows, classes, dtype, 0).total : 0;
+  return sizes_ok(rows, classes, dtype) ? logprob_bytes(rows, classes, dtype) : 0;
 }
 
 extern "C" int acdc_logprob_forward(const void* logits, int32_t dtype, int64_t stride, const void* targets,
@@ -1323,12 +1328,11 @@ extern "C" int acdc_logprob_forward(const void* logits, int32_t dtype, int64_t s
   if (!logits_ok(logits, dtype, stride, targets, target_bits, rows, classes, &rc)) return rc;
   if (rows == 0) return ACDC_OK;
   if (!floats_ok({logp}, {entropy}) || !aligned_to(saved, 16) || !aligned_to(workspace, 16)) return ACDC_ERR_INVALID_ARG;
-  const Workspace w = layout(rows, classes, dtype, 0);
-  if (workspace == nullptr || workspace_bytes < w.total) return ACDC_ERR_WORKSPACE;
+  if (workspace == nullptr || workspace_bytes < logprob_bytes(rows, classes, dtype)) return ACDC_ERR_WORKSPACE;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const Logits l{logits, dtype, stride, targets, target_bits, rows, classes};
   const RowOut out{logp, entropy, reinterpret_cast<float4*>(saved), nullptr, nullptr};
-  return launch_values(l, out, reinterpret_cast<float4*>(static_cast<char*>(workspace) + w.parts), s);
+  return launch_values(l, out, static_cast<float4*>(workspace), s);
 }
 
 extern "C" int acdc_logprob_backward(const void* logits, int32_t dtype, int64_t stride, const void* targets,

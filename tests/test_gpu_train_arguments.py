@@ -224,3 +224,21 @@ def test_options_without_a_truth_value(env):
                  lambda: losses.preference_loss(x, t, off, f, save=two)):
         with pytest.raises(RuntimeError, match="[Bb]oolean"):
             call()
+
+
+@pytest.mark.parametrize("rows,V,dtype", [(1, 1 << 18, "float32"), (8, 131072, "bfloat16"), (40, 100000, "float32"), (63, 20000, "bfloat16"),
+                                          (3000, 40, "float32")])
+def test_log_probabilities_stay_in_their_workspace(env, rows, V, dtype):
+    torch, losses, _ = env
+    print(f"[case] workspace of {rows} x {V} {dtype}", flush=True)
+    x = torch.randn(rows, V, generator=torch.Generator().manual_seed(rows)).to(getattr(torch, dtype)).cuda()
+    t = torch.arange(rows, device="cuda") % V
+    need = losses._logprob_bytes(rows, V, 0 if dtype == "float32" else 1)
+    room = torch.full((need + 8192,), 77, dtype=torch.uint8, device="cuda")
+    r = losses.token_logprobs(x, t, entropy=True, workspace=room[4096:4096 + need])
+    assert (room[:4096] == 77).all() and (room[4096 + need:] == 77).all()
+    want = x.double().log_softmax(1)[torch.arange(rows, device="cuda"), t]
+    # x_t - M, log S and their difference rounded, S's terms and sums: under 100 units of these sizes
+    assert ((r.logp.double() - want).abs() <= 100 * 2.0 ** -24 * want.abs().clamp(min=1)).all()
+    with pytest.raises(ValueError, match="workspace"):
+        losses.token_logprobs(x, t, workspace=room[4096:4096 + need - 1])

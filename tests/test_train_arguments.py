@@ -173,3 +173,15 @@ def test_any_iterable_of_tensors(calls):
         optim.adamw_step(layer.parameters(), iter([]), state.values(), 1)
     with pytest.raises(ValueError, match="a tensor at least"):
         optim.grad_norm(iter([]))
+
+
+def test_log_probabilities_ask_for_what_they_use():
+    """Rows whole take no workspace to speak of, however many; few long ones the 16 bytes of
+    each part, at least 4096 values long."""
+    from paper_1511_05946_amd import _lib
+    size = _lib.lib().acdc_logprob_workspace_size
+    for dtype in (0, 1):
+        for rows, classes in ((1 << 26, 2), (1 << 20, 1000), (64, 4096), (8, 4000), (0, 10)):
+            assert 0 < size(rows, classes, dtype) <= 256
+        for rows, classes in ((1, 1 << 18), (8, 131072), (40, 100000), (63, 20000)):
+            assert 256 < size(rows, classes, dtype) <= 256 + 16 * rows * (classes // 4096)
