@@ -1133,14 +1133,19 @@ Span span_of(const void* p, int64_t rows, int64_t stride, int32_t classes, size_
   const uintptr_t a = reinterpret_cast<uintptr_t>(p);
   return {a, rows > 0 ? a + uintptr_t((rows - 1) * stride + classes) * eb : a};
 }
-// grad_logits: the logits themselves, or memory apart from them.
+// grad_logits: the logits themselves, or memory apart from them: before or after
+// them, or other columns of the same wider rows.
 bool grad_ok(const void* logits, int64_t stride, const void* grad, int64_t grad_stride, int32_t dtype, int64_t rows,
              int32_t classes) {
   const size_t eb = dtype_bytes(dtype);
   if (grad_stride < classes || grad_stride > (int64_t(1) << 40) || !aligned_to(grad, eb)) return false;
   if (grad == logits) return grad_stride == stride;
   const Span x = span_of(logits, rows, stride, classes, eb), g = span_of(grad, rows, grad_stride, classes, eb);
-  return x.b <= g.a || g.b <= x.a;
+  if (x.b <= g.a || g.b <= x.a) return true;
+  if (grad_stride != stride) return false;
+  const uintptr_t row = uintptr_t(stride) * eb, width = uintptr_t(classes) * eb;
+  const uintptr_t at = g.a >= x.a ? (g.a - x.a) % row : (row - (x.a - g.a) % row) % row;
+  return at >= width && at + width <= row;
 }
 bool floats_ok(std::initializer_list<const void*> must, std::initializer_list<const void*> may) {
   for (const void* p : must)
