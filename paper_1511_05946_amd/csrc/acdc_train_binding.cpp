@@ -78,6 +78,10 @@ bool gone(const Tensor& t) {
          at::detail::computeStorageNbytes(t.sizes(), t.strides(), t.itemsize(), size_t(t.storage_offset())) > t.storage().nbytes();
 }
 bool readable(const Tensor& t) { return !lazy(t) && !gone(t); }
+// The same of a contiguous tensor of n elements, of which a step has a thousand.
+bool whole(const Tensor& t, int64_t n) {
+  return !lazy(t) && (n == 0 || size_t(t.storage_offset() + n) * t.itemsize() <= t.storage().nbytes());
+}
 bool vector_of(const Tensor* t, int64_t n, const at::Device& device, at::ScalarType type) {
   return t == nullptr || (t->dim() == 1 && t->size(0) == n && t->scalar_type() == type && t->device() == device &&
                           t->is_contiguous() && readable(*t));
@@ -358,7 +362,7 @@ struct Numbers {
 
 bool plain(const Tensor* t, int64_t numel, const at::Device& device, at::ScalarType type) {
   return t != nullptr && t->scalar_type() == type && t->numel() == numel && t->device() == device && t->is_contiguous() &&
-         readable(*t);
+         whole(*t, numel);
 }
 
 // (params, grads, moments, masters, lr, weight_decay, beta1, beta2, eps, step, grad_scale, stream) -> status
@@ -389,10 +393,10 @@ PyObject* adamw(PyObject*, PyObject* const* args, Py_ssize_t n) {
     for (Py_ssize_t i = 0; i < count; ++i) {
       const Tensor *p = params.tensor(i), *g = grads.tensor(i);
       if (p == nullptr || g == nullptr || type_of(*p) < 0 || type_of(*g) < 0 || !p->is_contiguous() ||
-          p->device() != device || g->sizes() != p->sizes() || g->device() != device || !g->is_contiguous() || !readable(*p) ||
-          !readable(*g))
+          p->device() != device || g->sizes() != p->sizes() || g->device() != device || !g->is_contiguous())
         Py_RETURN_NONE;
       const int64_t numel = p->numel();
+      if (!whole(*p, numel) || !whole(*g, numel)) Py_RETURN_NONE;
       acdc_adamw_tensor& r = records[size_t(i)];
       r = acdc_adamw_tensor{p->data_ptr(), nullptr, g->data_ptr(), nullptr, nullptr, nullptr, nullptr, numel,
                             lr.of(i), decay.of(i), type_of(*p), type_of(*g)};
