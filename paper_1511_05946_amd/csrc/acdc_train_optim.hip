@@ -5,8 +5,9 @@
 // the scales of 8-bit moments, one per 256 elements: the block's maximum has
 // to be known before its first code is written.
 //
-// The tensors' addresses travel in the kernels' arguments, up to 62 to 157 tensors
-// a launch: nothing is uploaded, and no table outlives the call.
+// The tensors' addresses travel in the kernels' arguments, 62 to 104 tensors a
+// launch and as offsets 103 to 156: nothing is uploaded, and no table outlives
+// the call.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -90,6 +91,8 @@ template <int WORDS>
 constexpr bool fits = sizeof(Batch<WORDS, kArguments>) <= kArguments &&
                       sizeof(Batch<WORDS, kFewArguments>) <= kFewArguments && sizeof(NearBatch<WORDS>) <= kArguments;
 static_assert(kRates <= 8 && fits<4> && fits<5> && fits<6> && fits<7>);
+static_assert(Batch<7, kArguments>::kMost == 62 && Batch<4, kArguments>::kMost == 104 && NearBatch<7>::kMost == 103 &&
+              NearBatch<4>::kMost == 156);
 
 struct Step {
   double one1, one2;      // 1 - beta

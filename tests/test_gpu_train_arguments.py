@@ -272,3 +272,14 @@ def test_gradient_beside_the_logits_in_wider_rows(env):
         with pytest.raises(ACDCError, match="invalid argument"):
             losses.policy_loss(room[:rows - 1, :V], t[:-1], f[:-1], f[:-1], out=room[1 if second == 0 else 0:][:rows - 1, second:second + V])
     assert not room.any()
+
+
+@pytest.mark.parametrize("kind,bits,most", [("f32", 32, 156), ("master", 32, 133), ("f32", 8, 116), ("master", 8, 103)])
+def test_lists_around_a_full_launch_of_offsets(env, kind, bits, most):
+    """The first list that a launch does not hold, and twice that: to the bit as one by one."""
+    torch, _, optim = env
+    import test_gpu_optim as T
+    for count in (most - 1, most, most + 1, 2 * most, 2 * most + 1):
+        print(f"[case] adamw list of {count} {kind} {bits} bits", flush=True)
+        T.same_as_one_by_one(torch, optim, lambda: T.problem(torch, optim, [1 + 53 * k % 900 for k in range(count)], kind, bits,
+                                                             count)[:4])
