@@ -22,8 +22,8 @@
  * Logits of -inf are classes of probability 0; a row that has only such
  * classes has no distribution and gives NaN, as does one that holds NaN or
  * +inf.  grad_logits has rows grad_stride apart and the logits' dtype; it
- * may be the logits' own memory (same pointer and stride), otherwise it must
- * not overlap them.
+ * may be the logits' own memory (same pointer and stride) or other columns of
+ * the same wider rows (same stride), otherwise it must not overlap them.
  */
 #ifndef ACDC_TRAIN_H_
 #define ACDC_TRAIN_H_
@@ -118,7 +118,8 @@ size_t acdc_preference_workspace_size(int64_t rows, int32_t classes, int32_t dty
  * elements 256 b .. 256 b + 255 share the scales m_scale[b] and v_scale[b]
  * (ceil(n / 256) floats each): m = q m_scale, sqrt(v) = q v_scale.  A scale is
  * the block's largest magnitude / 448, so that the largest element keeps its
- * value and the block follows its decay; a positive v never becomes 0.
+ * value and the block follows its decay; a positive v never becomes 0.  A NaN or
+ * infinite moment is a NaN code and does not count for its block's scale.
  * Pointers need the alignment of their element only. */
 typedef struct acdc_adamw_tensor {
   void* param;        /* param_type */
@@ -137,7 +138,9 @@ typedef struct acdc_adamw_tensor {
  * in 32 bits, w the master or the parameter; step counts from 1.  A grad_scale
  * that is not finite, or is -0, leaves every tensor as it is: what acdc_grad_norm
  * gives for gradients that hold a NaN or an infinity.  `tensors` is a host array
- * that is read before the call returns; no two tensors may overlap. */
+ * that is read before the call returns; no two tensors may overlap.  Its numbers
+ * and step travel in the launches' arguments: captured into a graph, every replay
+ * is the step that was captured, with its lr and its bias correction. */
 int acdc_adamw_step(const acdc_adamw_tensor* tensors, int32_t count, double beta1, double beta2, double eps,
                     int64_t step, const float* grad_scale, acdc_stream_t stream);
 

@@ -13,10 +13,10 @@ Argument marshalling only, like the cascade's binding: every step of the
 computation runs in HIP kernels on the current torch stream.  Logits are
 float32 or bfloat16, [rows, classes], each row contiguous and the rows any
 distance apart; gradients have the logits' dtype.  ``out`` may be the logits
-themselves.  Targets are int32 or int64, one class per row; a row with a
+themselves, or other columns of the same rows.  Targets are int32 or int64, one class per row; a row with a
 negative target takes no part (its logits do not matter, its gradient is 0), and a
 target past the classes gives NaN.  The ``*_autograd`` functions are the
-differentiable forms.
+differentiable forms (first derivatives; a second one raises).
 """
 
 from __future__ import annotations
@@ -224,7 +224,8 @@ def policy_loss(logits, actions, logp_old, advantages, logp_ref=None, weights=No
         + kl_coef (exp(k) - k - 1) - entropy_coef entropy
 
     and the total its mean (or, with ``mean`` off, its sum) under ``weights``
-    (>= 0; a row of weight 0 takes no part).  ``grad_scale`` multiplies the
+    (>= 0; a row of weight 0 takes no part).  With ``kl_coef`` 0 ``logp_ref``
+    serves the stats alone.  ``grad_scale`` multiplies the
     gradient of the logits (a loss scale, or 1 / steps of an accumulation).
     ``grad`` off computes the values alone; ``save`` returns what
     ``token_logprobs_backward`` needs to compute the gradient later."""
