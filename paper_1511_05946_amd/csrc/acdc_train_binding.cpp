@@ -226,8 +226,8 @@ PyObject* logprobs_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (a.bad || !l.read(x, t)) Py_RETURN_NONE;
     const at::Device device = x->device();
     if (saved->dim() != 2 || saved->size(0) != l.rows || saved->size(1) != 4 || saved->scalar_type() != at::kFloat ||
-        saved->device() != device || !saved->is_contiguous() || !readable(*saved) || !floats(g, l.rows, device) || !floats(h, l.rows, device) ||
-        !floats(scale, 1, device))
+        saved->device() != device || !saved->is_contiguous() || !readable(*saved) || !floats(g, l.rows, device) ||
+        !floats(h, l.rows, device) || !floats(scale, 1, device))
       Py_RETURN_NONE;
     Tensor grad;
     int64_t grad_stride = 0;

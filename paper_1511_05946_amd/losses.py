@@ -13,10 +13,11 @@ Argument marshalling only, like the cascade's binding: every step of the
 computation runs in HIP kernels on the current torch stream.  Logits are
 float32 or bfloat16, [rows, classes], each row contiguous and the rows any
 distance apart; gradients have the logits' dtype.  ``out`` may be the logits
-themselves, or other columns of the same rows.  Targets are int32 or int64, one class per row; a row with a
-negative target takes no part (its logits do not matter, its gradient is 0), and a
-target past the classes gives NaN.  The ``*_autograd`` functions are the
-differentiable forms (first derivatives; a second one raises).
+themselves, or other columns of the same rows.  Targets are int32 or int64, one
+class per row; a row with a negative target takes no part (its logits do not
+matter, its gradient is 0), and a target past the classes gives NaN.  The
+``*_autograd`` functions are the differentiable forms (first derivatives; a
+second one raises).
 """
 
 from __future__ import annotations
@@ -225,8 +226,8 @@ def policy_loss(logits, actions, logp_old, advantages, logp_ref=None, weights=No
 
     and the total its mean (or, with ``mean`` off, its sum) under ``weights``
     (>= 0; a row of weight 0 takes no part).  With ``kl_coef`` 0 ``logp_ref``
-    serves the stats alone.  ``grad_scale`` multiplies the
-    gradient of the logits (a loss scale, or 1 / steps of an accumulation).
+    serves the stats alone.  ``grad_scale`` multiplies the gradient of the logits
+    (a loss scale, or 1 / steps of an accumulation).
     ``grad`` off computes the values alone; ``save`` returns what
     ``token_logprobs_backward`` needs to compute the gradient later."""
     low, high = clip

@@ -112,13 +112,13 @@ def adamw_step(params, grads, moments, step: int, lr=1e-3, betas=(0.9, 0.999), e
         w = w (1 - lr weight_decay) - lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps)
 
     ``step`` counts from 1 (captured into a graph, every replay is the captured
-    step, with its ``lr`` and bias correction).  ``lr`` and ``weight_decay`` are numbers or one
-    number per tensor (diagonals near 1 are usually not decayed).  ``masters``:
-    per tensor the float32 copy of a bfloat16 parameter that is updated and
-    rounded into it, or None.  ``grad_scale``: a float32 tensor of one value
-    that multiplies every gradient, such as ``grad_norm(...)[1:]``; where it is
-    not finite, or -0, the step leaves everything as it is: what ``grad_norm`` with
-    a ``max_norm`` gives for gradients that hold a NaN or an infinity."""
+    step, with its ``lr`` and bias correction).  ``lr`` and ``weight_decay`` are
+    numbers or one number per tensor (diagonals near 1 are usually not decayed).
+    ``masters``: per tensor the float32 copy of a bfloat16 parameter that is
+    updated and rounded into it, or None.  ``grad_scale``: a float32 tensor of one
+    value that multiplies every gradient, such as ``grad_norm(...)[1:]``; where it
+    is not finite, or -0, the step leaves everything as it is: what ``grad_norm``
+    with a ``max_norm`` gives for gradients that hold a NaN or an infinity."""
     params, grads, moments = _listed(params), _listed(grads), _listed(moments)
     if masters is not None:
         masters = _listed(masters)
