@@ -12,8 +12,8 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libacdc.so"
 
 _lib = None
 
-# Exported symbols and their signatures (mirrors include/acdc.h and
-# include/acdc_train.h).
+# Exported symbols and their signatures (mirrors include/acdc.h,
+# include/acdc_train.h and include/acdc_train_lm.h).
 _P = ctypes.c_void_p
 _I64 = ctypes.c_int64
 _I32 = ctypes.c_int32
@@ -50,6 +50,17 @@ SIGNATURES = {
     "acdc_adamw_step": (ctypes.c_int, [_P, _I32, _D, _D, _D, _I64, _P, _P]),
     "acdc_grad_norm": (ctypes.c_int, [_P, _P, _P, _I32, _F, _P, _P, _SZ, _P]),
     "acdc_grad_norm_workspace_size": (_SZ, [_P, _I32]),
+    "acdc_vocab_logprob": (ctypes.c_int, [_P, _P, _P, _P, _SZ, _P]),
+    "acdc_vocab_backward": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "acdc_vocab_loss": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "acdc_vocab_workspace_size": (_SZ, [_I64, _I32, _I32, _I32, _I32]),
+    "acdc_norm_forward": (ctypes.c_int, [_P, _I32, _I64, _P, _P, _I32, _F, _P, _I32, _I64, _P, _I64, _I32, _P]),
+    "acdc_norm_backward": (ctypes.c_int, [_P, _I32, _I64, _P, _I32, _I64, _P, _I32, _P, _P, _I64, _P, _P, _I32, _I32, _I64, _I32,
+                                          _P, _SZ, _P]),
+    "acdc_norm_workspace_size": (_SZ, [_I64, _I32]),
+    "acdc_embedding_forward": (ctypes.c_int, [_P, _I32, _P, _I32, _I64, _F, _P, _I32, _I64, _I64, _I32, _I32, _P]),
+    "acdc_embedding_backward": (ctypes.c_int, [_P, _I32, _P, _I32, _I64, _F, _P, _I32, _I64, _I32, _I64, _I32, _I32, _P, _SZ, _P]),
+    "acdc_embedding_workspace_size": (_SZ, [_I64, _I32, _I32]),
 }
 
 

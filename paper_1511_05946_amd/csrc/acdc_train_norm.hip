@@ -1,0 +1,476 @@
+// Layer norm of rows and its backward pass (acdc_train_lm.h).
+//
+// Mathematics.  Mean and variance of a row are taken of the values in registers,
+// the variance of their differences from the mean, not of their squares, whose
+// difference would lose the digits of a variance below the mean's square.  Backward, with u = (x - mean) rstd and a = grad_y weight:
+//   grad_x = rstd (a - mean(a) - u mean(a u)),
+// and grad_weight = sum grad_y u, grad_bias = sum grad_y over the rows: a group
+// of lanes keeps its columns' sums in registers over all rows that it takes,
+// each workgroup leaves one row of sums, and a second launch adds those up.
+// Both passes are bound by HBM: each value is read and written once.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "acdc_train_lm.h"
+#include "acdc_train_rows.hpp"
+
+namespace acdc {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Sums over the LANES lanes that share a row; the slots take turns, so that one
+// barrier a sum is enough.
+template <int LANES>
+struct RowSum {
+  float* slots;  // 2 x LANES / 64
+  int turn = 0;
+  __device__ __forceinline__ float operator()(float v) {
+    if constexpr (LANES == 16) return over_16(v, [](float p, float q) { return p + q; });
+    v = wave_sum(v);
+    if constexpr (LANES > 64) {
+      constexpr int W = LANES / 64;
+      float* s = slots + turn * W;
+      turn ^= 1;
+      if (threadIdx.x % 64 == 0) s[threadIdx.x / 64] = v;
+      __syncthreads();
+      v = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) v += s[w];
+    }
+    return v;
+  }
+};
+
+template <int LANES>
+struct Group {
+  static constexpr int WG = LANES < kThreads ? kThreads : LANES, ROWS = WG / LANES;
+};
+
+// A row in the registers of LANES lanes, NC times eight values each.
+template <class TX, class TY, int LANES, int NC>
+__global__ __launch_bounds__(Group<LANES>::WG) void k_norm(const typename TX::Elem* __restrict__ x, long long x_stride,
+                                                           Vector weight, Vector bias, float eps,
+                                                           typename TY::Elem* __restrict__ y, long long y_stride,
+                                                           float2* __restrict__ saved, int rows, int width) {
+  constexpr int ROWS = Group<LANES>::ROWS;
+  __shared__ float slots[2 * Group<LANES>::WG / 64];
+  RowSum<LANES> sum{slots};
+  const int lane = threadIdx.x % LANES;
+  const float inv = 1.f / float(width);
+  for (int r = blockIdx.x * ROWS + threadIdx.x / LANES; r < rows; r += gridDim.x * ROWS) {
+    const typename TX::Elem* row = x + r * x_stride;
+    float v[NC][kEight];
+    float s = 0.f;
+#pragma unroll
+    for (int q = 0; q < NC; ++q) {
+      const int col = (lane + q * LANES) * kEight;
+      load_some<TX>(row + col, width - col, 0.f, v[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < NC; ++q)
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) s += v[q][i];
+    const float mean = sum(s) * inv;
+    s = 0.f;
+#pragma unroll
+    for (int q = 0; q < NC; ++q) {
+      const int col = (lane + q * LANES) * kEight;
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) {
+        v[q][i] -= mean;
+        s += col + i < width ? v[q][i] * v[q][i] : 0.f;
+      }
+    }
+    const float rstd = 1.f / sqrtf(sum(s) * inv + eps);
+    if (saved != nullptr && lane == 0) saved[r] = make_float2(mean, rstd);
+    typename TY::Elem* to = y + r * y_stride;
+#pragma unroll
+    for (int q = 0; q < NC; ++q) {
+      const int col = (lane + q * LANES) * kEight;
+      if (col >= width) continue;
+      float w[kEight], b[kEight];
+      load_vector(weight, col, width - col, 1.f, w);
+      load_vector(bias, col, width - col, 0.f, b);
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) v[q][i] = v[q][i] * rstd * w[i] + b[i];
+      store_some<TY>(to + col, width - col, v[q]);
+    }
+  }
+}
+
+// Longer rows: a workgroup reads its row three times, the second and third time from
+// its XCD's L2.
+template <class TX, class TY, int LANES>
+__global__ __launch_bounds__(LANES) void k_norm_long(const typename TX::Elem* __restrict__ x, long long x_stride, Vector weight,
+                                                     Vector bias, float eps, typename TY::Elem* __restrict__ y,
+                                                     long long y_stride, float2* __restrict__ saved, int rows, int width) {
+  __shared__ float slots[2 * LANES / 64];
+  RowSum<LANES> sum{slots};
+  const float inv = 1.f / float(width);
+  for (int r = blockIdx.x; r < rows; r += gridDim.x) {
+    const typename TX::Elem* row = x + r * x_stride;
+    float s = 0.f, v[kEight];
+#pragma unroll 4
+    for (int col = threadIdx.x * kEight; col < width; col += LANES * kEight) {
+      load_some<TX>(row + col, width - col, 0.f, v);
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) s += v[i];
+    }
+    const float mean = sum(s) * inv;
+    s = 0.f;
+#pragma unroll 4
+    for (int col = threadIdx.x * kEight; col < width; col += LANES * kEight) {
+      load_some<TX>(row + col, width - col, mean, v);
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) s += (v[i] - mean) * (v[i] - mean);
+    }
+    const float rstd = 1.f / sqrtf(sum(s) * inv + eps);
+    if (saved != nullptr && threadIdx.x == 0) saved[r] = make_float2(mean, rstd);
+    typename TY::Elem* to = y + r * y_stride;
+#pragma unroll 2
+    for (int col = threadIdx.x * kEight; col < width; col += LANES * kEight) {
+      float w[kEight], b[kEight];
+      load_some<TX>(row + col, width - col, 0.f, v);
+      load_vector(weight, col, width - col, 1.f, w);
+      load_vector(bias, col, width - col, 0.f, b);
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) v[i] = (v[i] - mean) * rstd * w[i] + b[i];
+      store_some<TY>(to + col, width - col, v);
+    }
+  }
+}
+
+// What the backward pass reads and writes.
+template <class TX, class TY>
+struct BackArgs {
+  const typename TX::Elem* x;
+  const typename TY::Elem* gy;
+  typename TX::Elem* gx;  // null: not wanted
+  long long x_stride, gy_stride, gx_stride;
+  const float2* saved;
+  Vector weight;
+  float* sums;  // [workgroups][2][width], null: not wanted
+  int rows, width;
+};
+
+template <class TX, class TY, int LANES, int NC>
+__global__ __launch_bounds__(Group<LANES>::WG) void k_norm_back(BackArgs<TX, TY> a) {
+  constexpr int WG = Group<LANES>::WG, ROWS = Group<LANES>::ROWS, SPAN = LANES * NC * kEight;
+  __shared__ float slots[2 * WG / 64];
+  __shared__ float both[ROWS > 1 ? ROWS : 1][ROWS > 1 ? SPAN : 1];
+  RowSum<LANES> sum{slots};
+  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, width = a.width;
+  const float inv = 1.f / float(width);
+  float w[NC][kEight], gw[NC][kEight] = {}, gb[NC][kEight] = {};
+#pragma unroll
+  for (int q = 0; q < NC; ++q) {
+    const int col = (lane + q * LANES) * kEight;
+    load_vector(a.weight, col, width - col, 1.f, w[q]);
+  }
+  for (int r = blockIdx.x * ROWS + group; r < a.rows; r += gridDim.x * ROWS) {
+    const float2 st = a.saved[r];
+    float u[NC][kEight], g[NC][kEight];
+#pragma unroll
+    for (int q = 0; q < NC; ++q) {
+      const int col = (lane + q * LANES) * kEight;
+      load_some<TX>(a.x + r * a.x_stride + col, width - col, st.x, u[q]);
+      load_some<TY>(a.gy + r * a.gy_stride + col, width - col, 0.f, g[q]);
+    }
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int q = 0; q < NC; ++q)
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) {
+        u[q][i] = (u[q][i] - st.x) * st.y;
+        gb[q][i] += g[q][i];
+        gw[q][i] += g[q][i] * u[q][i];
+        g[q][i] *= w[q][i];
+        s1 += g[q][i];
+        s2 += g[q][i] * u[q][i];
+      }
+    if (a.gx == nullptr) continue;
+    const float m1 = sum(s1) * inv, m2 = sum(s2) * inv;
+    typename TX::Elem* to = a.gx + r * a.gx_stride;
+#pragma unroll
+    for (int q = 0; q < NC; ++q) {
+      const int col = (lane + q * LANES) * kEight;
+      if (col >= width) continue;
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) g[q][i] = st.y * (g[q][i] - m1 - u[q][i] * m2);
+      store_some<TX>(to + col, width - col, g[q]);
+    }
+  }
+  if (a.sums == nullptr) return;
+  float* out = a.sums + (long long)blockIdx.x * 2 * width;
+  if constexpr (ROWS == 1) {
+#pragma unroll
+    for (int q = 0; q < NC; ++q) {
+      const int col = (lane + q * LANES) * kEight;
+      if (col >= width) continue;
+      store_some<F32, false>(out + col, width - col, gw[q]);
+      store_some<F32, false>(out + width + col, width - col, gb[q]);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (k == 1) __syncthreads();
+#pragma unroll
+      for (int q = 0; q < NC; ++q)
+#pragma unroll
+        for (int i = 0; i < kEight; ++i) both[group][(lane + q * LANES) * kEight + i] = k == 0 ? gw[q][i] : gb[q][i];
+      __syncthreads();
+      for (int col = threadIdx.x; col < width; col += WG) {
+        float s = 0.f;
+#pragma unroll
+        for (int p = 0; p < ROWS; ++p) s += both[p][col];
+        out[k * width + col] = s;
+      }
+    }
+  }
+}
+
+// Longer rows: grad_x, a workgroup a row, which it reads twice.
+template <class TX, class TY, int LANES>
+__global__ __launch_bounds__(LANES) void k_norm_back_long(BackArgs<TX, TY> a) {
+  __shared__ float slots[2 * LANES / 64];
+  RowSum<LANES> sum{slots};
+  const int width = a.width;
+  const float inv = 1.f / float(width);
+  for (int r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const float2 st = a.saved[r];
+    const typename TX::Elem* x = a.x + r * a.x_stride;
+    const typename TY::Elem* gy = a.gy + r * a.gy_stride;
+    float s1 = 0.f, s2 = 0.f, u[kEight], g[kEight], w[kEight];
+#pragma unroll 2
+    for (int col = threadIdx.x * kEight; col < width; col += LANES * kEight) {
+      load_some<TX>(x + col, width - col, st.x, u);
+      load_some<TY>(gy + col, width - col, 0.f, g);
+      load_vector(a.weight, col, width - col, 1.f, w);
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) {
+        s1 += g[i] * w[i];
+        s2 += g[i] * w[i] * ((u[i] - st.x) * st.y);
+      }
+    }
+    const float m1 = sum(s1) * inv, m2 = sum(s2) * inv;
+    typename TX::Elem* to = a.gx + r * a.gx_stride;
+#pragma unroll 2
+    for (int col = threadIdx.x * kEight; col < width; col += LANES * kEight) {
+      load_some<TX>(x + col, width - col, st.x, u);
+      load_some<TY>(gy + col, width - col, 0.f, g);
+      load_vector(a.weight, col, width - col, 1.f, w);
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) g[i] = st.y * (g[i] * w[i] - m1 - (u[i] - st.x) * st.y * m2);
+      store_some<TX>(to + col, width - col, g);
+    }
+  }
+}
+
+// Their columns' sums: a wave takes 512 columns of a part of the rows.
+template <class TX, class TY>
+__global__ __launch_bounds__(64) void k_norm_columns(BackArgs<TX, TY> a, int each) {
+  const int col = (blockIdx.x * 64 + threadIdx.x) * kEight, from = blockIdx.y * each, to = min(a.rows, from + each);
+  if (col >= a.width) return;
+  const int left = a.width - col;
+  float gw[kEight] = {}, gb[kEight] = {};
+#pragma unroll 4
+  for (int r = from; r < to; ++r) {
+    const float2 st = a.saved[r];
+    float u[kEight], g[kEight];
+    load_some<TX>(a.x + r * a.x_stride + col, left, st.x, u);
+    load_some<TY>(a.gy + r * a.gy_stride + col, left, 0.f, g);
+#pragma unroll
+    for (int i = 0; i < kEight; ++i) {
+      gb[i] += g[i];
+      gw[i] += g[i] * ((u[i] - st.x) * st.y);
+    }
+  }
+  float* out = a.sums + (long long)blockIdx.y * 2 * a.width;
+  store_some<F32, false>(out + col, left, gw);
+  store_some<F32, false>(out + a.width + col, left, gb);
+}
+
+// The parts' sums together, in order: 64 columns a workgroup, its waves take the parts
+// in turn.
+constexpr int kSumWaves = 8;
+__global__ __launch_bounds__(64 * kSumWaves) void k_norm_sums(const float* __restrict__ sums, int parts, int width, void* gw,
+                                                             void* gb, int dtype, bool add) {
+  __shared__ float slots[kSumWaves][64];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, at = blockIdx.x * 64 + lane;  // of 2 width
+  float s = 0.f;
+  if (at < 2 * width) {
+#pragma unroll 8
+    for (int p = wave; p < parts; p += kSumWaves) s += sums[(long long)p * 2 * width + at];
+  }
+  slots[wave][lane] = s;
+  __syncthreads();
+  if (wave != 0 || at >= 2 * width) return;
+  s = 0.f;
+#pragma unroll
+  for (int w = 0; w < kSumWaves; ++w) s += slots[w][lane];
+  void* out = at < width ? gw : gb;
+  const int col = at < width ? at : at - width;
+  if (out == nullptr) return;
+  if (dtype == ACDC_F32) {
+    float* to = static_cast<float*>(out) + col;
+    *to = add ? *to + s : s;
+  } else {
+    __bf16* to = static_cast<__bf16*>(out) + col;
+    *to = __bf16(add ? float(*to) + s : s);
+  }
+}
+
+// ------------------------------------------------------------------ on the host
+
+constexpr int kMostWidth = 1 << 24;
+constexpr int kHeld = 16384;  // values of a row that registers hold
+constexpr int kMostParts = 512;
+
+int done() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? ACDC_OK : hip_fail(e);
+}
+// f.template operator()<LANES, NC>() for rows of up to kHeld values.
+template <class F>
+void with_row(int width, F&& f) {
+  if (width <= 128) f.template operator()<16, 1>();
+  else if (width <= 256) f.template operator()<16, 2>();
+  else if (width <= 512) f.template operator()<64, 1>();
+  else if (width <= 1024) f.template operator()<64, 2>();
+  else if (width <= 2048) f.template operator()<256, 1>();
+  else if (width <= 4096) f.template operator()<256, 2>();
+  else if (width <= 8192) f.template operator()<512, 2>();
+  else f.template operator()<512, 4>();
+}
+template <class F>
+int with_types(int32_t x, int32_t y, F&& f) {
+  if (x == ACDC_F32) return y == ACDC_F32 ? f.template operator()<F32, F32>() : f.template operator()<F32, BF16>();
+  return y == ACDC_F32 ? f.template operator()<BF16, F32>() : f.template operator()<BF16, BF16>();
+}
+bool rows_ok(const void* p, int32_t dtype, int64_t stride, int64_t rows, int32_t width) {
+  const size_t e = dtype_bytes(dtype);
+  return e != 0 && stride >= width && stride <= (int64_t(1) << 40) && aligned_to(p, e) && (rows == 0 || p != nullptr);
+}
+bool sizes_ok(int64_t rows, int32_t width) { return rows >= 0 && rows <= 0x3fffffff && width >= 1 && width <= kMostWidth; }
+struct Span {
+  const char* from;
+  const char* to;
+};
+Span span_of(const void* p, int64_t rows, int64_t stride, int64_t width, int32_t dtype) {
+  const char* a = static_cast<const char*>(p);
+  return {a, p == nullptr || rows == 0 ? a : a + (size_t(rows - 1) * size_t(stride) + size_t(width)) * dtype_bytes(dtype)};
+}
+bool apart(const Span& a, const Span& b) { return a.to <= b.from || b.to <= a.from; }
+
+// Parts whose columns' sums the backward pass leaves: the workgroups of its launch (long
+// rows: those of the second one).
+int parts_of(int64_t rows, int32_t width) {
+  if (rows == 0) return 0;
+  if (width > kHeld) return int(std::min<int64_t>(rows, 64));
+  int per = 1;
+  with_row(width, [&]<int LANES, int NC>() { per = Group<LANES>::ROWS; });
+  return int(std::min<int64_t>((rows + per - 1) / per, kMostParts));
+}
+
+}  // namespace
+}  // namespace acdc
+
+using namespace acdc;
+
+extern "C" int acdc_norm_forward(const void* x, int32_t x_type, int64_t x_stride, const void* weight, const void* bias,
+                                 int32_t vector_type, float eps, void* y, int32_t y_type, int64_t y_stride, float* saved,
+                                 int64_t rows, int32_t width, acdc_stream_t stream) {
+  if (!sizes_ok(rows, width) || !rows_ok(x, x_type, x_stride, rows, width) || !rows_ok(y, y_type, y_stride, rows, width) ||
+      !(eps >= 0.f) || !(eps - eps == 0.f) || !aligned_to(saved, 8))
+    return ACDC_ERR_INVALID_ARG;
+  const size_t e = dtype_bytes(vector_type);
+  if (e == 0 || !aligned_to(weight, e) || !aligned_to(bias, e)) return ACDC_ERR_INVALID_ARG;
+  const Span out = span_of(y, rows, y_stride, width, y_type);
+  if (rows > 0 && (!apart(out, span_of(x, rows, x_stride, width, x_type)) || !apart(out, span_of(weight, 1, width, width, vector_type)) ||
+                   !apart(out, span_of(bias, 1, width, width, vector_type))))
+    return ACDC_ERR_INVALID_ARG;
+  if (rows == 0) return ACDC_OK;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  return with_types(x_type, y_type, [&]<class TX, class TY>() {
+    auto go = [&](auto kernel, int64_t groups, int wg) {
+      hipLaunchKernelGGL(kernel, dim3(unsigned(std::min<int64_t>(groups, 1 << 16))), dim3(wg), 0, s,
+                         static_cast<const typename TX::Elem*>(x), (long long)x_stride, Vector{weight, vector_type},
+                         Vector{bias, vector_type}, eps, static_cast<typename TY::Elem*>(y), (long long)y_stride,
+                         reinterpret_cast<float2*>(saved), int(rows), width);
+    };
+    if (width > kHeld) {
+      go(k_norm_long<TX, TY, 1024>, rows, 1024);
+    } else {
+      with_row(width, [&]<int LANES, int NC>() {
+        constexpr int per = Group<LANES>::ROWS;
+        go(k_norm<TX, TY, LANES, NC>, (rows + per - 1) / per, Group<LANES>::WG);
+      });
+    }
+    return done();
+  });
+}
+
+extern "C" size_t acdc_norm_workspace_size(int64_t rows, int32_t width) {
+  return sizes_ok(rows, width) ? std::max<size_t>(256, size_t(parts_of(rows, width)) * 2 * size_t(width) * 4) : 0;
+}
+
+extern "C" int acdc_norm_backward(const void* x, int32_t x_type, int64_t x_stride, const void* grad_y, int32_t y_type,
+                                  int64_t grad_y_stride, const void* weight, int32_t vector_type, const float* saved,
+                                  void* grad_x, int64_t grad_x_stride, void* grad_weight, void* grad_bias, int32_t grads_type,
+                                  int32_t accumulate, int64_t rows, int32_t width, void* workspace, size_t workspace_bytes,
+                                  acdc_stream_t stream) {
+  if (!sizes_ok(rows, width) || !rows_ok(x, x_type, x_stride, rows, width) ||
+      !rows_ok(grad_y, y_type, grad_y_stride, rows, width) || !aligned_to(saved, 8) || (rows > 0 && saved == nullptr))
+    return ACDC_ERR_INVALID_ARG;
+  const size_t e = dtype_bytes(vector_type), ge = dtype_bytes(grads_type);
+  if (e == 0 || ge == 0 || !aligned_to(weight, e) || !aligned_to(grad_weight, ge) || !aligned_to(grad_bias, ge))
+    return ACDC_ERR_INVALID_ARG;
+  const Span in[3] = {span_of(x, rows, x_stride, width, x_type), span_of(grad_y, rows, grad_y_stride, width, y_type),
+                      span_of(weight, 1, width, width, vector_type)};
+  const Span out[3] = {span_of(grad_x, grad_x != nullptr ? rows : 0, grad_x_stride, width, x_type),
+                       span_of(grad_weight, 1, width, width, grads_type), span_of(grad_bias, 1, width, width, grads_type)};
+  if (grad_x != nullptr && !rows_ok(grad_x, x_type, grad_x_stride, rows, width)) return ACDC_ERR_INVALID_ARG;
+  // in place of grad_y: each value is read by the lane that writes it, before it does
+  const bool in_place = grad_x == grad_y && grad_x_stride == grad_y_stride && x_type == y_type;
+  for (int o = 0; o < 3; ++o) {
+    for (int i = 0; i < 3; ++i)
+      if (!(o == 0 && i == 1 && in_place) && !apart(out[o], in[i])) return ACDC_ERR_INVALID_ARG;
+    for (int q = 0; q < o; ++q)
+      if (!apart(out[o], out[q])) return ACDC_ERR_INVALID_ARG;
+  }
+  const bool sums = grad_weight != nullptr || grad_bias != nullptr;
+  const size_t need = acdc_norm_workspace_size(rows, width);
+  if (sums && (workspace == nullptr || workspace_bytes < need)) return ACDC_ERR_WORKSPACE;
+  if (!aligned_to(workspace, 16)) return ACDC_ERR_INVALID_ARG;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const int parts = parts_of(rows, width);
+  if (rows > 0 && (sums || grad_x != nullptr)) {
+    const int rc = with_types(x_type, y_type, [&]<class TX, class TY>() {
+      const BackArgs<TX, TY> a{static_cast<const typename TX::Elem*>(x), static_cast<const typename TY::Elem*>(grad_y),
+                               static_cast<typename TX::Elem*>(grad_x), x_stride, grad_y_stride, grad_x_stride,
+                               reinterpret_cast<const float2*>(saved), Vector{weight, vector_type},
+                               sums ? static_cast<float*>(workspace) : nullptr, int(rows), width};
+      if (width > kHeld) {
+        // the sums first: grad_x may take grad_y's place
+        if (sums) {
+          const int each = int((rows + parts - 1) / parts), blocks = (width + 64 * kEight - 1) / (64 * kEight);
+          hipLaunchKernelGGL((k_norm_columns<TX, TY>), dim3(unsigned(blocks), unsigned(parts)), dim3(64), 0, s, a, each);
+        }
+        if (grad_x != nullptr)
+          hipLaunchKernelGGL((k_norm_back_long<TX, TY, 1024>), dim3(unsigned(std::min<int64_t>(rows, 1 << 16))), dim3(1024), 0, s, a);
+      } else {
+        with_row(width, [&]<int LANES, int NC>() {
+          hipLaunchKernelGGL((k_norm_back<TX, TY, LANES, NC>), dim3(unsigned(parts)), dim3(Group<LANES>::WG), 0, s, a);
+        });
+      }
+      return done();
+    });
+    if (rc != ACDC_OK) return rc;
+  }
+  if (!sums || (rows == 0 && accumulate != 0)) return ACDC_OK;
+  hipLaunchKernelGGL(k_norm_sums, dim3(unsigned((2 * int64_t(width) + 63) / 64)), dim3(64 * kSumWaves), 0, s,
+                     static_cast<const float*>(workspace), parts, width, grad_weight, grad_bias, grads_type, accumulate != 0);
+  return done();
+}

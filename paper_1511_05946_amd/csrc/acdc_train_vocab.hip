@@ -1,0 +1,777 @@
+// Losses over a vocabulary whose logits are never stored (acdc_train_lm.h).
+//
+// Mathematics.  With x = hidden weight^T, a row enters a loss through logp =
+// x_t - M - log S only, M = max_v x_v, S = sum_v exp(x_v - M).  The first pass
+// computes the logits tile by tile on the matrix cores and leaves (max, sum)
+// of every row and tile, which are joined.  With g = dL/dlogp,
+//   G = dL/dx = g ([v = t] - exp(x - M) / S),  dL/dhidden = G weight,
+//   dL/dweight = G^T hidden,
+// and the second pass computes the logits of a piece of the vocabulary again,
+// writes the piece of G in the inputs' type and runs both products on it.
+//
+// Rows that take no part are left out from the start: the others are packed
+// together (`order`), so that they cost nothing and what they hold is never
+// read.  The packed rows are padded with zeros to whole tiles and steps.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "acdc_train_gemm.hpp"
+#include "acdc_train_lm.h"
+
+namespace acdc {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kNegMax = -3.402823466e38f;
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+
+// ------------------------------------------------------------ the rows in use
+
+// What is known of the packed rows (`order` and the rest are indexed by a packed
+// row, `at` by a row of the caller's).
+struct Rows {
+  int* order;    // [padded] row of the caller's
+  int* target;   // [padded] its class; -1 past the rows in use, -2 for one past the classes
+  float* share;  // [padded] its weight, or dL/dlogp
+  int* at;       // [rows] packed row, -1: takes no part
+  int* count;    // rows in use
+  double* total;  // sum of the weights
+  float* factor;  // what the gradients of the products are multiplied by
+};
+// The factor all rows share: grad_scale, over the weights' sum for a mean, or *scale.
+struct Factor {
+  const float* device;
+  float host;
+  bool mean;
+};
+
+constexpr int kWide = 1024, kEach = 8;
+
+// Packs the rows in use, in order, and clears the outputs of the others.  One
+// workgroup, 8192 rows a round: the rows are a few MB at the most.
+__global__ __launch_bounds__(kWide) void k_vocab_rows(const void* __restrict__ targets, int bits,
+                                                      const float* __restrict__ weights, int rows, int padded, int classes,
+                                                      Factor factor, Rows out, float* logp, float2* saved, float* row_grads) {
+  __shared__ int counts[kWide / 64];
+  __shared__ double sums[kWide / 64];
+  const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
+  int done = 0;
+  double sum = 0.0;
+  for (int base = 0; base < rows; base += kWide * kEach) {
+    const int first = base + tid * kEach;
+    int t[kEach];
+    float w[kEach];
+    unsigned in_use = 0;
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+      const int r = first + q;
+      t[q] = -1;
+      w[q] = 1.f;
+      if (r < rows) {
+        const long long v = bits == 64 ? static_cast<const long long*>(targets)[r] : (long long)static_cast<const int*>(targets)[r];
+        t[q] = v < 0 ? -1 : v >= classes ? -2 : int(v);
+        if (weights != nullptr) w[q] = weights[r];
+        if (t[q] != -1 && w[q] != 0.f) in_use |= 1u << q;
+      }
+    }
+    const int mine = __popc(in_use);
+    int before = mine;  // inclusive over the wave
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(before, o);
+      if (lane >= o) before += up;
+    }
+    if (lane == 63) counts[wave] = before;
+    __syncthreads();
+    int place = done + before - mine;
+#pragma unroll
+    for (int k = 0; k < kWide / 64; ++k) {
+      if (k < wave) place += counts[k];
+      done += counts[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+      const int r = first + q;
+      if (r >= rows) break;
+      if (in_use >> q & 1) {
+        out.order[place] = r;
+        out.target[place] = t[q];
+        out.share[place] = w[q];
+        out.at[r] = place++;
+        sum += double(w[q]);
+      } else {
+        out.at[r] = -1;
+        if (logp != nullptr) logp[r] = 0.f;
+        if (saved != nullptr) saved[r] = make_float2(0.f, 1.f);
+        if (row_grads != nullptr) row_grads[r] = 0.f;
+      }
+    }
+  }
+  for (int i = done + tid; i < padded; i += kWide) {
+    out.order[i] = 0;
+    out.target[i] = -1;
+    out.share[i] = 0.f;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  if (tid == 0) {
+    double all = 0.0;
+    for (int k = 0; k < kWide / 64; ++k) all += sums[k];
+    *out.total = all;
+    *out.count = done;
+    const float f = factor.device != nullptr ? *factor.device : factor.host;
+    *out.factor = !factor.mean ? f : all == 0.0 ? 0.f : float(double(f) / all);
+  }
+}
+
+// Rows as the matrix cores take them: bfloat16 (three planes for float32), `padded`
+// wide, at multiples of 16 bytes.  With `order` the packed rows, zeros past *count.
+template <class T>
+__global__ __launch_bounds__(256) void k_vocab_pack(const typename T::Elem* __restrict__ x, long long stride,
+                                                    const int* __restrict__ order, const int* __restrict__ count, int rows,
+                                                    int width, __bf16* __restrict__ out, long long plane, int padded) {
+  const int per = padded / 8, used = order != nullptr ? *count : rows;
+  const long long chunks = (long long)rows * per;
+  for (long long c = blockIdx.x * 256ll + threadIdx.x; c < chunks; c += gridDim.x * 256ll) {
+    const int r = int(c / per), col = int(c % per) * 8;
+    float v[8] = {};
+    if (r < used) {
+      const typename T::Elem* from = x + (order != nullptr ? order[r] : r) * stride + col;
+      if (col + 8 <= width) {
+#pragma unroll
+        for (int q = 0; q < 8 / T::kPer; ++q) {
+          const typename T::Raw raw = load_chunk<T>(from + q * T::kPer);
+#pragma unroll
+          for (int i = 0; i < T::kPer; ++i) v[q * T::kPer + i] = T::get(raw, i);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (col + i < width) v[i] = T::one(from[i]);
+      }
+    }
+    __bf16* to = out + (long long)r * padded + col;
+    if constexpr (std::is_same_v<T, BF16>) {
+      bf16x8 o;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = __bf16(v[i]);
+      *reinterpret_cast<bf16x8*>(to) = o;
+    } else {
+      bf16x8 o[3];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const Split3 s = split3(v[i]);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) o[p][i] = s.p[p];
+      }
+#pragma unroll
+      for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8*>(to + p * plane) = o[p];
+    }
+  }
+}
+
+// ------------------------------------------------------ what follows a product
+
+// Statistics of a tile's rows: their (max, sum) into parts[tile][row], and the target's
+// logit.  m runs over classes, n over packed rows; `classes` are those of the piece.
+struct StatsOut {
+  const int* target;
+  float2* parts;
+  float* logit;
+  int first, classes, rows, tile;
+  template <int BM, int BN, int WM, int WN, int MI, int NI, class S>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const S& spot, const Place& at, int wave,
+                                             float2* slots) const {
+    const int lane = spot.lane;
+    __syncthreads();  // the tiles have been read
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+      const int r = spot.n(n), t = target[r] - first;
+      float top = kNegMax;
+#pragma unroll
+      for (int m = 0; m < MI; ++m) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int v = spot.m(m) + i;
+          if (v >= classes) acc[m][n][i] = -__builtin_inff();
+          else if (v == t) logit[r] = acc[m][n][i];
+          top = fmaxf(top, acc[m][n][i]);
+        }
+      }
+      Pair p = swap16(top);
+      top = fmaxf(p.a, p.b);
+      p = swap32(top);
+      top = fmaxf(p.a, p.b);
+      float sum = 0.f;
+#pragma unroll
+      for (int m = 0; m < MI; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += exp_of(acc[m][n][i] - top);
+      p = swap16(sum);
+      sum = p.a + p.b;
+      p = swap32(sum);
+      sum = p.a + p.b;
+      if (lane < 16) slots[(r - at.tn * BN) * WM + wave % WM] = make_float2(top, sum);
+    }
+    __syncthreads();
+    if (int(threadIdx.x) < BN) {
+      float2 all = slots[threadIdx.x * WM];
+#pragma unroll
+      for (int w = 1; w < WM; ++w) {
+        const float2 s = slots[threadIdx.x * WM + w];
+        const float top = fmaxf(all.x, s.x);
+        all = make_float2(top, all.y * exp_of(all.x - top) + s.y * exp_of(s.x - top));
+      }
+      parts[(long long)(tile + at.tm) * rows + at.tn * BN + threadIdx.x] = all;
+    }
+  }
+};
+
+// What turns a row's logits into G: M, g / S, g and the target.  g without the factor that
+// all rows share, which the sums of the products are multiplied by: 1 / W in every target's
+// g would be rounded to bfloat16 the same way in all of them, and the errors add up.
+struct RowSlope {
+  float top, slope, g;
+  int target;
+};
+
+// The piece of G, rows `ld` apart, zeros past the classes and for padding rows.
+template <int PLANES>
+struct SlopeOut {
+  const RowSlope* row;
+  __bf16* out;
+  long long plane;
+  int ld, first, classes;
+  template <int BM, int BN, int WM, int WN, int MI, int NI, class S>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const S& spot, const Place&, int, float2*) const {
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+      const int r = spot.n(n);
+      const RowSlope k = row[r];
+      const int t = k.target - first;
+      __bf16* to = out + (long long)r * ld + spot.m(0);
+#pragma unroll
+      for (int m = 0; m < MI; m += 2) {
+        bf16x8 o[PLANES];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int v = spot.m(m + i / 4) + i % 4;
+          float y = -exp_of(acc[m + i / 4][n][i % 4] - k.top) * k.slope;
+          if (v == t) y += k.g;
+          if (v >= classes) y = 0.f;
+          if constexpr (PLANES == 1) {
+            o[0][i] = __bf16(y);  // the one rounding between the logits and the gradients
+          } else {
+            const Split3 s = split3(y);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) o[p][i] = s.p[p];
+          }
+        }
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p) *reinterpret_cast<bf16x8*>(to + p * plane + m * 4) = o[p];
+      }
+    }
+  }
+};
+
+// 32-bit sums of a part: out[part][n][m], added to what earlier pieces left.
+struct PartOut {
+  float* out;
+  long long part;
+  int ld, rows;
+  bool add;
+  template <int BM, int BN, int WM, int WN, int MI, int NI, class S>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const S& spot, const Place& at, int, float2*) const {
+#pragma unroll
+    for (int n = 0; n < NI; ++n)
+#pragma unroll
+      for (int m = 0; m < MI; ++m) {
+        if (spot.m(m) >= ld || spot.n(n) >= rows) continue;
+        f32x4* to = reinterpret_cast<f32x4*>(out + at.part * part + (long long)spot.n(n) * ld + spot.m(m));
+        *to = add ? *to + acc[m][n] : acc[m][n];
+      }
+  }
+};
+
+// Four values of a row of a gradient.  `whole`: rows at multiples of four elements.
+template <class T>
+__device__ __forceinline__ void put4(typename T::Elem* to, f32x4 v, int left, bool whole, bool add) {
+  using E = typename T::Elem;
+  typedef E Four __attribute__((ext_vector_type(4)));
+  if (whole && left >= 4) {
+    if (add) {
+      const Four old = *reinterpret_cast<const Four*>(to);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] += float(old[i]);
+    }
+    *reinterpret_cast<Four*>(to) = Four{T::to(v[0]), T::to(v[1]), T::to(v[2]), T::to(v[3])};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < left) to[i] = T::to(add ? v[i] + float(to[i]) : v[i]);
+  }
+}
+
+// The gradient itself: m runs over the width, n over the piece's classes.
+template <class T>
+struct GradOut {
+  typename T::Elem* out;
+  const float* factor;
+  long long ld;
+  int width, classes;
+  bool whole, add;
+  template <int BM, int BN, int WM, int WN, int MI, int NI, class S>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const S& spot, const Place&, int, float2*) const {
+    const float f = *factor;
+#pragma unroll
+    for (int n = 0; n < NI; ++n)
+#pragma unroll
+      for (int m = 0; m < MI; ++m)
+        if (spot.n(n) < classes)
+          put4<T>(out + spot.n(n) * ld + spot.m(m), acc[m][n] * f, width - spot.m(m), whole, add);
+  }
+};
+
+// The parts of a sum together, in order, into the gradient's rows.  With `at` the rows
+// that take no part get zeros.
+template <class T>
+__global__ __launch_bounds__(256) void k_vocab_sum(const float* __restrict__ sums, int parts, long long part, int padded,
+                                                   const int* __restrict__ at, const float* __restrict__ factor,
+                                                   long long rows, int width,
+                                                   typename T::Elem* __restrict__ out, long long ld, bool whole, bool add) {
+  const int per = (width + 3) / 4;
+  for (long long c = blockIdx.x * 256ll + threadIdx.x; c < rows * per; c += gridDim.x * 256ll) {
+    const long long r = c / per;
+    const int col = int(c % per) * 4;
+    const long long from = at != nullptr ? at[r] : r;
+    f32x4 v = {};
+    if (from >= 0) {
+      const float* p = sums + from * padded + col;
+      for (int k = 0; k < parts; ++k) v += *reinterpret_cast<const f32x4*>(p + k * part);
+      v *= *factor;
+    }
+    put4<T>(out + r * ld + col, v, width - col, whole, add);
+  }
+}
+
+// --------------------------------------------------------- the rows' statistics
+
+// The tiles' statistics of 64 packed rows together, a row a lane, 16 waves along the
+// tiles; then what the row leaves.
+struct JoinOut {
+  float* logp;
+  float2* saved;
+  float* row_grads;
+  RowSlope* slope;     // null: no gradient
+  float* loss;         // [padded] weight times logp, null: not wanted
+  bool mean;
+};
+__global__ __launch_bounds__(1024) void k_vocab_join(Rows rows, const float2* __restrict__ parts, const float* __restrict__ logit,
+                                                     int tiles, int padded, JoinOut out) {
+  __shared__ float2 slots[16][64];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, i = blockIdx.x * 64 + lane;
+  const int used = *rows.count;
+  float top = kNegMax, sum = 0.f;
+  if (i < used) {
+    constexpr int AHEAD = 8;
+    for (int k = wave; k < tiles; k += 16 * AHEAD) {
+      float2 p[AHEAD];
+#pragma unroll
+      for (int q = 0; q < AHEAD; ++q)
+        p[q] = k + 16 * q < tiles ? parts[(long long)(k + 16 * q) * padded + i] : make_float2(kNegMax, 0.f);
+      float m = top;
+#pragma unroll
+      for (int q = 0; q < AHEAD; ++q) m = fmaxf(m, p[q].x);
+      sum *= exp_of(top - m);
+#pragma unroll
+      for (int q = 0; q < AHEAD; ++q) sum += p[q].y * exp_of(p[q].x - m);
+      top = m;
+    }
+  }
+  slots[wave][lane] = make_float2(top, sum);
+  __syncthreads();
+  if (wave != 0) return;
+  top = kNegMax;
+  sum = 0.f;
+  for (int w = 0; w < 16; ++w) top = fmaxf(top, slots[w][lane].x);
+  for (int w = 0; w < 16; ++w) sum += slots[w][lane].y * exp_of(slots[w][lane].x - top);
+  if (i >= used) {
+    if (out.slope != nullptr) out.slope[i] = RowSlope{0.f, 0.f, 0.f, -1};
+    if (out.loss != nullptr) out.loss[i] = 0.f;
+    return;
+  }
+  const int r = rows.order[i], t = rows.target[i];
+  // no class with a probability: no distribution
+  const float nan = sum > 0.f ? 0.f : __builtin_nanf("");
+  const float logp = t >= 0 ? (logit[i] - top) - logf(sum) + nan : __builtin_nanf("");
+  out.logp[r] = logp;
+  if (out.saved != nullptr) out.saved[r] = make_float2(top, sum);
+  if (out.loss == nullptr) return;
+  const float w = rows.share[i];
+  out.loss[i] = w * logp;
+  if (out.row_grads != nullptr) out.row_grads[r] = -(out.mean ? float(double(w) / *rows.total) : w);
+  if (out.slope != nullptr) {
+    const float g = t >= 0 ? -w : __builtin_nanf("");
+    out.slope[i] = RowSlope{top, g / sum, g, t};
+  }
+}
+
+// RowSlope from what an earlier call saved.
+__global__ __launch_bounds__(256) void k_vocab_slope(Rows rows, const float2* __restrict__ saved, int padded, RowSlope* __restrict__ slope) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= padded) return;
+  if (i >= *rows.count) {
+    slope[i] = RowSlope{0.f, 0.f, 0.f, -1};
+    return;
+  }
+  const float2 st = saved[rows.order[i]];
+  const int t = rows.target[i];
+  const float g = t >= 0 ? rows.share[i] : __builtin_nanf("");
+  slope[i] = RowSlope{st.x, g / st.y, g, t};
+}
+
+// stats = (loss, W), summed in 64 bits by one workgroup.
+__global__ __launch_bounds__(kWide) void k_vocab_total(Rows rows, const float* __restrict__ loss, bool mean, float* stats) {
+  __shared__ double sums[kWide / 64];
+  const int used = *rows.count;
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < used; i += kWide) sum += double(loss[i]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double all = 0.0;
+    for (int k = 0; k < kWide / 64; ++k) all += sums[k];
+    const double total = *rows.total;
+    stats[0] = used == 0 ? 0.f : float(mean ? -all / total : -all);
+    stats[1] = float(total);
+  }
+}
+
+// ------------------------------------------------------------------ on the host
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
+
+constexpr int kTile = 256;
+// Bytes of the piece of G: a quarter of a tile's products per byte are enough to hide
+// what each piece costs once, and the rest of the card's memory is the caller's.
+constexpr int64_t kPieceBytes = int64_t(512) << 20;
+
+// How a call is cut up: fixed by its sizes alone.
+struct Plan {
+  int64_t rows, padded_rows;
+  int32_t width, padded_width, classes, planes;
+  int tile_n;             // packed rows of a tile
+  int32_t piece, pieces;  // classes of a piece, a multiple of kTile
+  int hidden_parts, weight_parts;
+};
+int parts_for(int64_t tiles, int64_t steps) {
+  // as many as give every CU a tile, of 8 steps at least
+  return int(std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), steps / 8, 64})));
+}
+Plan plan_for(int64_t rows, int32_t width, int32_t classes, int32_t dtype) {
+  Plan p{};
+  p.rows = rows;
+  p.width = width;
+  p.classes = classes;
+  p.planes = dtype == ACDC_F32 ? 3 : 1;
+  p.tile_n = rows <= 64 ? 64 : kTile;
+  p.padded_rows = up(std::max<int64_t>(rows, 1), p.tile_n);
+  p.padded_width = int32_t(up(width, kStepK));
+  const int64_t values = std::max<int64_t>(p.padded_rows, p.padded_width);  // of a class: in the piece of G, in the packed weight
+  const int64_t most = std::max<int64_t>(kTile, kPieceBytes / (2 * p.planes * values) / kTile * kTile);
+  p.pieces = int32_t((classes + most - 1) / most);
+  p.piece = int32_t(up((classes + p.pieces - 1) / p.pieces, kTile));
+  const int64_t wide = up(p.padded_width, kTile) / kTile, pairs = p.planes == 1 ? 1 : 6;
+  p.hidden_parts = parts_for(wide * (p.padded_rows / p.tile_n), pairs * (std::min<int64_t>(p.piece, up(classes, kStepK)) / kStepK));
+  p.weight_parts = parts_for(wide * (up(std::min(p.piece, classes), kTile) / kTile), pairs * (p.padded_rows / kStepK));
+  return p;
+}
+
+struct Layout {
+  size_t order, target, share, at, count, total, factor, logit, parts, slope, loss, hidden, weight, grad, hidden_sums, weight_sums, bytes;
+};
+Layout layout(const Plan& p, bool gradient) {
+  Layout w{};
+  size_t next = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = next;
+    next += up256(bytes);
+    return o;
+  };
+  const size_t R = size_t(p.padded_rows);
+  w.order = take(R * 4);
+  w.target = take(R * 4);
+  w.share = take(R * 4);
+  w.at = take(size_t(p.rows) * 4);
+  w.count = take(4);
+  w.total = take(8);
+  w.factor = take(4);
+  w.logit = take(R * 4);
+  w.parts = take(R * 8 * size_t(up(p.classes, kTile) / kTile));
+  w.slope = take(R * sizeof(RowSlope));
+  w.loss = take(R * 4);
+  w.hidden = take(R * p.padded_width * 2 * p.planes);
+  w.weight = take(size_t(p.piece) * p.padded_width * 2 * p.planes);
+  if (gradient) {
+    w.grad = take(R * p.piece * 2 * p.planes);
+    w.hidden_sums = take(size_t(p.hidden_parts) * R * p.padded_width * 4);
+    w.weight_sums = take(p.weight_parts > 1 ? size_t(p.weight_parts) * p.piece * p.padded_width * 4 : 0);
+  }
+  w.bytes = next;
+  return w;
+}
+
+int done() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? ACDC_OK : hip_fail(e);
+}
+
+// A call on its way: the plan, where its buffers are, and the launches.
+template <class T>
+struct Call {
+  static constexpr int P = std::is_same_v<T, F32> ? 3 : 1;
+  const acdc_vocab_head& head;
+  const Plan p;
+  const Layout w;
+  char* ws;
+  hipStream_t s;
+  Rows rows;
+  bool direct;  // the weight as it is
+
+  Call(const acdc_vocab_head& h, bool gradient, void* workspace, acdc_stream_t stream)
+      : head(h), p(plan_for(h.rows, h.width, h.classes, h.dtype)), w(layout(p, gradient)), ws(static_cast<char*>(workspace)),
+        s(reinterpret_cast<hipStream_t>(stream)) {
+    rows = Rows{get<int>(w.order), get<int>(w.target), get<float>(w.share), get<int>(w.at), get<int>(w.count), get<double>(w.total), get<float>(w.factor)};
+    direct = P == 1 && h.width % 8 == 0 && h.weight_stride % 8 == 0 && h.weight_stride < (1 << 22) && aligned_to(h.weight, 16);
+  }
+  template <class E>
+  E* get(size_t at) const { return reinterpret_cast<E*>(ws + at); }
+
+  static unsigned grid(int64_t items) { return unsigned(std::min<int64_t>((items + 255) / 256, 1 << 16)); }
+
+  void pack(const void* x, int64_t stride, const int* order, int64_t n, __bf16* to, int64_t plane) const {
+    hipLaunchKernelGGL(k_vocab_pack<T>, dim3(grid(n * (p.padded_width / 8))), dim3(256), 0, s,
+                       static_cast<const typename T::Elem*>(x), (long long)stride, order, rows.count, int(n), p.width, to,
+                       (long long)plane, p.padded_width);
+  }
+  void pack_rows(const float* weights, const Factor& factor, float* logp, float2* saved, float* row_grads) const {
+    hipLaunchKernelGGL(k_vocab_rows, dim3(1), dim3(kWide), 0, s, head.targets, head.target_bits, weights, int(p.rows),
+                       int(p.padded_rows), p.classes, factor, rows, logp, saved, row_grads);
+    pack(head.hidden, head.hidden_stride, rows.order, p.padded_rows, get<__bf16>(w.hidden), hidden_plane());
+  }
+  int64_t hidden_plane() const { return p.padded_rows * p.padded_width; }
+  int classes_of(int k) const { return std::min(p.piece, p.classes - k * p.piece); }
+  Operand hidden() const {
+    return Operand{get<__bf16>(w.hidden), p.padded_width, hidden_plane(), int(p.padded_rows), p.padded_width};
+  }
+  Operand weight(int k, bool again) const {
+    const int n = classes_of(k);
+    const typename T::Elem* from = static_cast<const typename T::Elem*>(head.weight) + int64_t(k) * p.piece * head.weight_stride;
+    if (direct) return Operand{reinterpret_cast<const __bf16*>(from), head.weight_stride, 0, n, p.width};
+    const int64_t plane = int64_t(p.piece) * p.padded_width;
+    if (!again) pack(from, head.weight_stride, nullptr, n, get<__bf16>(w.weight), plane);
+    return Operand{get<__bf16>(w.weight), p.padded_width, plane, n, p.padded_width};
+  }
+  Operand grad(int k) const {
+    return Operand{get<__bf16>(w.grad), p.piece, p.padded_rows * p.piece, int(p.padded_rows), int(up(classes_of(k), kStepK))};
+  }
+
+  template <int BM, int BN, int WM, int WN, bool XA, bool XB, Count COUNT, class E>
+  void gemm(const Operand& a, const Operand& b, int64_t m, int64_t n, int ksteps, int parts, const E& e) const {
+    const int mt = int((m + BM - 1) / BM), nt = int((n + BN - 1) / BN);
+    hipLaunchKernelGGL((k_gemm<BM, BN, WM, WN, P, XA, XB, COUNT, E>), dim3(unsigned(int64_t(mt) * nt * parts)), dim3(WM * WN * 64),
+                       0, s, a, b, ksteps, mt, nt, parts, rows.count, e);
+  }
+  // classes x packed rows
+  template <class E>
+  void logits(const Operand& weight, const E& e) const {
+    const int steps = p.padded_width / kStepK;
+    if (p.tile_n == 64) gemm<kTile, 64, 4, 1, false, false, Count::kN>(weight, hidden(), weight.rows, p.padded_rows, steps, 1, e);
+    else gemm<kTile, kTile, 2, 4, false, false, Count::kN>(weight, hidden(), weight.rows, p.padded_rows, steps, 1, e);
+  }
+
+  int statistics(const JoinOut& out) const {
+    for (int k = 0; k < p.pieces; ++k)
+      logits(weight(k, false), StatsOut{rows.target, get<float2>(w.parts), get<float>(w.logit), k * p.piece, classes_of(k),
+                                        int(p.padded_rows), k * (p.piece / kTile)});
+    hipLaunchKernelGGL(k_vocab_join, dim3(unsigned(p.padded_rows / 64)), dim3(1024), 0, s, rows, get<float2>(w.parts),
+                       get<float>(w.logit), int(up(p.classes, kTile) / kTile), int(p.padded_rows), out);
+    return done();
+  }
+
+  template <class O>
+  void sum(size_t at, int parts, int64_t part, const int* place, int64_t n, void* out, int64_t ld, bool add) const {
+    using E = typename O::Elem;
+    const bool whole = aligned_to(out, 4 * sizeof(E)) && ld % 4 == 0;
+    hipLaunchKernelGGL(k_vocab_sum<O>, dim3(grid(n * ((p.width + 3) / 4))), dim3(256), 0, s, get<float>(at), parts,
+                       (long long)part, p.padded_width, place, rows.factor, (long long)n, p.width, static_cast<E*>(out), (long long)ld, whole, add);
+  }
+  template <class O>
+  void weight_grad(const acdc_vocab_grads& g, int k) const {
+    using E = typename O::Elem;
+    const int n = classes_of(k), steps = int(p.padded_rows / kStepK);
+    E* out = static_cast<E*>(g.weight) + int64_t(k) * p.piece * g.weight_stride;
+    const bool whole = aligned_to(out, 4 * sizeof(E)) && g.weight_stride % 4 == 0, add = g.accumulate != 0;
+    if (p.weight_parts == 1) {
+      gemm<kTile, kTile, 2, 4, true, true, Count::kK>(hidden(), grad(k), p.width, n, steps, 1,
+                                                      GradOut<O>{out, rows.factor, g.weight_stride, p.width, n, whole, add});
+    } else {
+      const int64_t part = int64_t(p.piece) * p.padded_width;
+      gemm<kTile, kTile, 2, 4, true, true, Count::kK>(hidden(), grad(k), p.width, n, steps, p.weight_parts,
+                                                      PartOut{get<float>(w.weight_sums), part, p.padded_width, n, false});
+      sum<O>(w.weight_sums, p.weight_parts, part, nullptr, n, out, g.weight_stride, add);
+    }
+  }
+  // with the rows' slopes in place; `again`: the only piece's weight is packed already
+  int gradients(const acdc_vocab_grads& g, bool again) const {
+    const int64_t part = p.padded_rows * p.padded_width;
+    for (int k = 0; k < p.pieces; ++k) {
+      const Operand wk = weight(k, again && p.pieces == 1);
+      logits(wk, SlopeOut<P>{get<RowSlope>(w.slope), get<__bf16>(w.grad), p.padded_rows * p.piece, p.piece, k * p.piece, classes_of(k)});
+      if (g.hidden != nullptr) {
+        const int steps = int(up(classes_of(k), kStepK) / kStepK);
+        const PartOut out{get<float>(w.hidden_sums), part, p.padded_width, int(p.padded_rows), k > 0};
+        if (p.tile_n == 64)
+          gemm<kTile, 64, 4, 1, true, false, Count::kN>(wk, grad(k), p.width, p.padded_rows, steps, p.hidden_parts, out);
+        else
+          gemm<kTile, kTile, 2, 4, true, false, Count::kN>(wk, grad(k), p.width, p.padded_rows, steps, p.hidden_parts, out);
+      }
+      if (g.weight != nullptr) {
+        if (g.weight_type == head.dtype) weight_grad<T>(g, k);
+        else weight_grad<F32>(g, k);
+      }
+    }
+    if (g.hidden != nullptr) sum<T>(w.hidden_sums, p.hidden_parts, part, rows.at, p.rows, g.hidden, g.hidden_stride, false);
+    return done();
+  }
+};
+
+// ---------------------------------------------------------------------- checks
+
+constexpr int64_t kMostRows = 1 << 24, kMostClasses = 1 << 27, kMostWidth = 1 << 17, kMostStride = int64_t(1) << 40;
+
+bool sizes_ok(int64_t rows, int32_t width, int32_t classes, int32_t dtype) {
+  return dtype_bytes(dtype) != 0 && rows >= 0 && rows <= kMostRows && width >= 1 && width <= kMostWidth && classes >= 1 &&
+         classes <= kMostClasses;
+}
+struct Span {
+  const char* from;
+  const char* to;
+};
+Span span_of(const void* p, int64_t rows, int64_t stride, int64_t width, size_t bytes) {
+  const char* a = static_cast<const char*>(p);
+  return {a, p == nullptr || rows == 0 ? a : a + (size_t(rows - 1) * size_t(stride) + size_t(width)) * bytes};
+}
+bool apart(const Span& a, const Span& b) { return a.to <= b.from || b.to <= a.from; }
+
+bool head_ok(const acdc_vocab_head* h) {
+  if (h == nullptr || !sizes_ok(h->rows, h->width, h->classes, h->dtype) || (h->target_bits != 32 && h->target_bits != 64))
+    return false;
+  const size_t e = dtype_bytes(h->dtype);
+  if (h->hidden_stride < h->width || h->hidden_stride > kMostStride || h->weight_stride < h->width || h->weight_stride > kMostStride)
+    return false;
+  if (h->weight == nullptr || !aligned_to(h->weight, e)) return false;
+  return h->rows == 0 || (h->hidden != nullptr && aligned_to(h->hidden, e) && h->targets != nullptr &&
+                          aligned_to(h->targets, size_t(h->target_bits) / 8));
+}
+bool grads_ok(const acdc_vocab_head& h, const acdc_vocab_grads& g) {
+  const size_t e = dtype_bytes(h.dtype);
+  const Span x = span_of(h.hidden, h.rows, h.hidden_stride, h.width, e), w = span_of(h.weight, h.classes, h.weight_stride, h.width, e);
+  Span gx{}, gw{};
+  if (g.hidden != nullptr) {
+    if (!aligned_to(g.hidden, e) || g.hidden_stride < h.width || g.hidden_stride > kMostStride) return false;
+    gx = span_of(g.hidden, h.rows, g.hidden_stride, h.width, e);
+    if (!apart(gx, x) || !apart(gx, w)) return false;
+  }
+  if (g.weight != nullptr) {
+    const size_t we = dtype_bytes(g.weight_type);
+    if ((g.weight_type != ACDC_F32 && g.weight_type != h.dtype) || !aligned_to(g.weight, we) || g.weight_stride < h.width ||
+        g.weight_stride > kMostStride)
+      return false;
+    gw = span_of(g.weight, h.classes, g.weight_stride, h.width, we);
+    if (!apart(gw, x) || !apart(gw, w) || (g.hidden != nullptr && !apart(gw, gx))) return false;
+  }
+  return true;
+}
+bool wants(const acdc_vocab_grads* g) { return g != nullptr && (g->hidden != nullptr || g->weight != nullptr); }
+
+int workspace_ok(const acdc_vocab_head& h, bool gradient, const void* workspace, size_t bytes) {
+  if (!aligned_to(workspace, 256)) return ACDC_ERR_INVALID_ARG;
+  if (workspace == nullptr || bytes < layout(plan_for(h.rows, h.width, h.classes, h.dtype), gradient).bytes) return ACDC_ERR_WORKSPACE;
+  return ACDC_OK;
+}
+template <class F>
+int with_type(int32_t dtype, F&& f) {
+  return dtype == ACDC_F32 ? f.template operator()<F32>() : f.template operator()<BF16>();
+}
+
+}  // namespace
+}  // namespace acdc
+
+using namespace acdc;
+
+extern "C" size_t acdc_vocab_workspace_size(int64_t rows, int32_t width, int32_t classes, int32_t dtype, int32_t gradient) {
+  return sizes_ok(rows, width, classes, dtype) ? layout(plan_for(rows, width, classes, dtype), gradient != 0).bytes : 0;
+}
+
+extern "C" int acdc_vocab_logprob(const acdc_vocab_head* head, float* logp, float* saved, void* workspace,
+                                  size_t workspace_bytes, acdc_stream_t stream) {
+  if (!head_ok(head)) return ACDC_ERR_INVALID_ARG;
+  if (head->rows == 0) return ACDC_OK;
+  if (logp == nullptr || !aligned_to(logp, 4) || !aligned_to(saved, 8)) return ACDC_ERR_INVALID_ARG;
+  if (const int rc = workspace_ok(*head, false, workspace, workspace_bytes); rc != ACDC_OK) return rc;
+  return with_type(head->dtype, [&]<class T>() {
+    const Call<T> c(*head, false, workspace, stream);
+    c.pack_rows(nullptr, Factor{nullptr, 1.f, false}, logp, reinterpret_cast<float2*>(saved), nullptr);
+    return c.statistics(JoinOut{logp, reinterpret_cast<float2*>(saved), nullptr, nullptr, nullptr, false});
+  });
+}
+
+extern "C" int acdc_vocab_backward(const acdc_vocab_head* head, const float* saved, const float* grad_logp, const float* scale,
+                                   const acdc_vocab_grads* grads, void* workspace, size_t workspace_bytes, acdc_stream_t stream) {
+  if (!head_ok(head) || grads == nullptr || !grads_ok(*head, *grads) || !aligned_to(scale, 4)) return ACDC_ERR_INVALID_ARG;
+  if (head->rows > 0 && (saved == nullptr || !aligned_to(saved, 8) || grad_logp == nullptr || !aligned_to(grad_logp, 4)))
+    return ACDC_ERR_INVALID_ARG;
+  if (!wants(grads)) return ACDC_OK;
+  if (const int rc = workspace_ok(*head, true, workspace, workspace_bytes); rc != ACDC_OK) return rc;
+  return with_type(head->dtype, [&]<class T>() {
+    const Call<T> c(*head, true, workspace, stream);
+    c.pack_rows(grad_logp, Factor{scale, 1.f, false}, nullptr, nullptr, nullptr);
+    hipLaunchKernelGGL(k_vocab_slope, dim3(Call<T>::grid(c.p.padded_rows)), dim3(256), 0, c.s, c.rows,
+                       reinterpret_cast<const float2*>(saved), int(c.p.padded_rows), c.template get<RowSlope>(c.w.slope));
+    return c.gradients(*grads, false);
+  });
+}
+
+extern "C" int acdc_vocab_loss(const acdc_vocab_head* head, const float* weights, const acdc_vocab_params* params, float* stats,
+                               float* logp, float* saved, float* row_grads, const acdc_vocab_grads* grads, void* workspace,
+                               size_t workspace_bytes, acdc_stream_t stream) {
+  if (!head_ok(head) || params == nullptr || stats == nullptr || !aligned_to(stats, 4) || !aligned_to(weights, 4) ||
+      !aligned_to(logp, 4) || !aligned_to(saved, 8) || !aligned_to(row_grads, 4))
+    return ACDC_ERR_INVALID_ARG;
+  const acdc_vocab_params q = *params;
+  if (!(q.grad_scale - q.grad_scale == 0.f) || (head->rows > 0 && logp == nullptr) || (grads != nullptr && !grads_ok(*head, *grads)))
+    return ACDC_ERR_INVALID_ARG;
+  const bool gradient = wants(grads);
+  if (const int rc = workspace_ok(*head, gradient, workspace, workspace_bytes); rc != ACDC_OK) return rc;
+  return with_type(head->dtype, [&]<class T>() {
+    const Call<T> c(*head, gradient, workspace, stream);
+    float2* stat = reinterpret_cast<float2*>(saved);
+    float* loss = c.template get<float>(c.w.loss);
+    c.pack_rows(weights, Factor{nullptr, q.grad_scale, q.mean != 0}, logp, stat, row_grads);
+    int rc = c.statistics(JoinOut{logp, stat, row_grads, gradient ? c.template get<RowSlope>(c.w.slope) : nullptr, loss,
+                                  q.mean != 0});
+    if (rc != ACDC_OK) return rc;
+    hipLaunchKernelGGL(k_vocab_total, dim3(1), dim3(kWide), 0, c.s, c.rows, loss, q.mean != 0, stats);
+    rc = done();
+    return rc != ACDC_OK || !gradient ? rc : c.gradients(*grads, true);
+  });
+}

@@ -9,6 +9,14 @@ gradient that a loss returns is the ``grad_y`` that ``acdc.backward`` takes.
 * ``policy_loss``       clipped policy loss with a KL term and an entropy bonus;
 * ``preference_loss``   preference loss over pairs of sequences of rows.
 
+Where a vocabulary is wider than a row, the logits are ``hidden @ weight.T`` of a
+cascade's rows and a weight [classes, width], and they are not kept:
+
+* ``vocab_loss``        cross entropy over the vocabulary, with the gradients of
+                        rows and weight;
+* ``vocab_logprobs``    log-probability of one class per row, with
+                        ``vocab_logprobs_backward`` for the gradients.
+
 Argument marshalling only, like the cascade's binding: every step of the
 computation runs in HIP kernels on the current torch stream.  Logits are
 float32 or bfloat16, [rows, classes], each row contiguous and the rows any
@@ -55,6 +63,20 @@ class PreferenceLoss(NamedTuple):
     grad_logits: Optional[torch.Tensor]
     saved: Optional[torch.Tensor]      # [rows, 4]
     row_grads: Optional[torch.Tensor]  # [2, rows]
+
+
+class VocabLogprobs(NamedTuple):
+    logp: torch.Tensor                 # [rows]
+    saved: Optional[torch.Tensor]      # [rows, 2], for vocab_logprobs_backward
+
+
+class VocabLoss(NamedTuple):
+    stats: torch.Tensor                # [2]: loss, sum of the weights
+    logp: torch.Tensor                 # [rows]
+    grad_hidden: Optional[torch.Tensor]
+    grad_weight: Optional[torch.Tensor]
+    saved: Optional[torch.Tensor]      # [rows, 2]
+    row_grads: Optional[torch.Tensor]  # [rows]: dL/dlogp
 
 
 def _native(logits, name, *args):
@@ -296,6 +318,185 @@ def preference_loss(logits, targets, offsets, logp_ref, beta: float = 0.1, label
     return PreferenceLoss(stats, logp, g, saved, row_grads)
 
 
+# ----------------------------------------------------- losses over a vocabulary
+
+
+def _matrix(name, t, device=None):
+    """(rows, width, stride) of float32 or bfloat16 rows."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be [rows, width], got {tuple(t.shape)}")
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    rows, width = t.shape
+    if width < 1:
+        raise ValueError(f"{name} must have a column at least")
+    stride, inner = t.stride()
+    if width > 1 and inner != 1:
+        raise ValueError(f"{name} must have contiguous rows (stride 1 along the width, got {inner})")
+    if rows <= 1:
+        stride = max(stride, width)
+    if stride < width:
+        raise ValueError(f"{name} has overlapping rows (stride {stride}, width {width})")
+    _values(name, t)
+    return rows, width, stride
+
+
+@functools.lru_cache(maxsize=512)
+def _vocab_bytes(rows, width, classes, dtype, gradient):
+    need = lib().acdc_vocab_workspace_size(rows, width, classes, dtype, gradient)
+    if need == 0:
+        raise ValueError(f"{rows} rows of {width} over {classes} classes: at most 2^24 rows, a width of 2^17 and 2^27 classes "
+                         "are supported")
+    return need
+
+
+def vocab_workspace_bytes(hidden, weight, grad: bool = True) -> int:
+    """Bytes of workspace of the calls below for this hidden and weight."""
+    return _vocab_bytes(*hidden.shape, weight.shape[0], _DTYPES[hidden.dtype], 1 if grad else 0)
+
+
+def _vocab_head(hidden, weight, targets, grad, workspace):
+    """The packed description of the inputs, and the workspace."""
+    rows, width, stride = _matrix("hidden", hidden)
+    device = hidden.device
+    classes, weight_width, weight_stride = _matrix("weight", weight, device)
+    if weight.dtype is not hidden.dtype:
+        raise ValueError(f"hidden and weight must have one type, got {hidden.dtype} and {weight.dtype}")
+    if weight_width != width:
+        raise ValueError(f"weight is {tuple(weight.shape)}: its rows must have hidden's width {width}")
+    if classes < 1:
+        raise ValueError("weight must have a class at least")
+    bits = _index("targets", targets, rows, device)
+    dtype = _DTYPES[hidden.dtype]
+    need = _vocab_bytes(rows, width, classes, dtype, 1 if grad else 0)
+    head = struct.pack("3Q3q4i", hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), stride, weight_stride, rows,
+                       width, classes, dtype, bits)
+    return head, _vocab_workspace(workspace, need, device), need
+
+
+def _vocab_workspace(ws, need, device):
+    ws = _workspace(ws, need, device)
+    if ws.data_ptr() % 256 != 0:
+        raise ValueError("workspace must begin at a multiple of 256 bytes")
+    return ws
+
+
+def _apart(name, out, *others):
+    """Whether `out` shares memory with an input: refused, as it is written while they are read."""
+    if out.numel() == 0:
+        return
+    def span(t):
+        last = sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
+        return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
+    a, b = span(out)
+    for other, t in others:
+        if t is not None and t.numel() > 0:
+            c, d = span(t)
+            if a < d and c < b:
+                raise ValueError(f"{name} overlaps {other}")
+
+
+def _vocab_grads(hidden, weight, out, grad_weight, accumulate, wanted):
+    """(packed description, grad_hidden, grad_weight) for the gradients in `wanted`."""
+    gh = gw = None
+    gh_stride = gw_stride = 0
+    if wanted[0]:
+        gh = torch.empty(hidden.shape, dtype=hidden.dtype, device=hidden.device) if out is None else out
+        _, _, gh_stride = _matrix("out", gh, hidden.device)
+        if gh.shape != hidden.shape or gh.dtype is not hidden.dtype:
+            raise ValueError(f"out must be like hidden, {tuple(hidden.shape)} {hidden.dtype}")
+    if wanted[1]:
+        if grad_weight is None:
+            if accumulate:
+                raise ValueError("accumulate needs the grad_weight to add to")
+            gw = torch.empty(weight.shape, dtype=weight.dtype, device=weight.device)
+        else:
+            gw = grad_weight
+        _, _, gw_stride = _matrix("grad_weight", gw, hidden.device)
+        if gw.shape != weight.shape or (gw.dtype is not weight.dtype and gw.dtype is not torch.float32):
+            raise ValueError(f"grad_weight must be {tuple(weight.shape)} {weight.dtype} or float32, got {tuple(gw.shape)} {gw.dtype}")
+    if out is not None and gh is not None:
+        _apart("out", gh, ("hidden", hidden), ("weight", weight), ("grad_weight", gw))
+    if grad_weight is not None and gw is not None:
+        _apart("grad_weight", gw, ("hidden", hidden), ("weight", weight))
+    record = struct.pack("2Q2q2i", 0 if gh is None else gh.data_ptr(), 0 if gw is None else gw.data_ptr(), gh_stride, gw_stride,
+                         0 if gw is None else _DTYPES[gw.dtype], 1 if accumulate else 0)
+    return record, gh, gw
+
+
+def _wants(grad):
+    """Which of (grad_hidden, grad_weight) a call computes."""
+    if grad in (True, False):
+        return bool(grad), bool(grad)
+    if grad not in ("hidden", "weight"):
+        raise ValueError(f"grad must be True, False, 'hidden' or 'weight', not {grad!r}")
+    return grad == "hidden", grad == "weight"
+
+
+def vocab_logprobs(hidden, weight, targets, save: bool = False, workspace=None) -> VocabLogprobs:
+    """Log-probability of each row's target under softmax(hidden @ weight.T),
+    with ``save`` what ``vocab_logprobs_backward`` needs."""
+    head, ws, need = _vocab_head(hidden, weight, targets, False, workspace)
+    rows, device = hidden.shape[0], hidden.device
+    logp = torch.empty(rows, device=device)
+    saved = torch.empty(rows, 2, device=device) if save else None
+    rc = _call(lib().acdc_vocab_logprob, device, head, logp.data_ptr(), _ptr(saved), ws.data_ptr(), need)
+    _check(rc, "acdc_vocab_logprob")
+    return VocabLogprobs(logp, saved)
+
+
+def vocab_logprobs_backward(hidden, weight, targets, saved, grad_logp, scale=None, grad=True, out=None, grad_weight=None,
+                            accumulate: bool = False, workspace=None):
+    """(grad_hidden, grad_weight) from dL/dlogp of each row, times ``scale`` (a
+    tensor of one value on the device) if given.  ``grad`` may be "hidden" or
+    "weight" for one of them (the other is None).  ``out``: a tensor to write
+    grad_hidden into; ``grad_weight``: one to write, or with ``accumulate`` to
+    add, the weight's gradient into, float32 or of the weight's type."""
+    wanted = _wants(grad)
+    head, ws, need = _vocab_head(hidden, weight, targets, True, workspace)
+    rows, device = hidden.shape[0], hidden.device
+    if saved.shape != (rows, 2) or saved.dtype is not torch.float32 or saved.device != device or not saved.is_contiguous():
+        raise ValueError(f"saved must be the contiguous float32 [{rows}, 2] tensor of the forward call")
+    _values("saved", saved)
+    _vector("grad_logp", grad_logp, rows, device)
+    if scale is not None:
+        _vector("scale", scale.reshape(-1), 1, device)
+    record, gh, gw = _vocab_grads(hidden, weight, out, grad_weight, accumulate, wanted)
+    rc = _call(lib().acdc_vocab_backward, device, head, saved.data_ptr(), grad_logp.data_ptr(), _ptr(scale), record,
+               ws.data_ptr(), need)
+    _check(rc, "acdc_vocab_backward")
+    _wrote(out if wanted[0] else None, grad_weight if wanted[1] else None)
+    return gh, gw
+
+
+def vocab_loss(hidden, weight, targets, weights=None, mean: bool = True, grad_scale: float = 1.0, grad=True,
+               save: bool = False, out=None, grad_weight=None, accumulate: bool = False, workspace=None) -> VocabLoss:
+    """Cross entropy of softmax(hidden @ weight.T) at one target per row: the
+    mean (or, with ``mean`` off, the sum) of -logp under ``weights`` (>= 0; a row
+    of weight 0, or with a negative target, takes no part).  The logits are
+    computed in pieces of the vocabulary and not kept.  ``grad``, ``out``,
+    ``grad_weight`` and ``accumulate`` as in ``vocab_logprobs_backward``;
+    ``grad_scale`` multiplies the gradients.  ``save`` returns what
+    ``vocab_logprobs_backward`` needs to compute them later."""
+    wanted = _wants(grad)
+    any_grad = wanted[0] or wanted[1]
+    head, ws, need = _vocab_head(hidden, weight, targets, any_grad, workspace)
+    rows, device = hidden.shape[0], hidden.device
+    _vector("weights", weights, rows, device)
+    record, gh, gw = _vocab_grads(hidden, weight, out, grad_weight, accumulate, wanted) if any_grad else (None, None, None)
+    stats, logp = torch.empty(2, device=device), torch.empty(rows, device=device)
+    saved = torch.empty(rows, 2, device=device) if save else None
+    row_grads = torch.empty(rows, device=device) if save else None
+    params = struct.pack("fi", grad_scale, 1 if mean else 0)
+    rc = _call(lib().acdc_vocab_loss, device, head, _ptr(weights), params, stats.data_ptr(), logp.data_ptr(), _ptr(saved),
+               _ptr(row_grads), record, ws.data_ptr(), need)
+    _check(rc, "acdc_vocab_loss")
+    _wrote(out if wanted[0] else None, grad_weight if wanted[1] else None)
+    return VocabLoss(stats, logp, gh, gw, saved, row_grads)
+
+
 # ------------------------------------------------------------------- autograd
 
 
@@ -336,6 +537,56 @@ class _Loss(torch.autograd.Function):
             scale = scale * ctx.grad_scale
         grad = token_logprobs_backward(logits, targets, saved, row_grads[0], row_grads[1], scale=scale)
         return _once(ctx.call, grad, logits, grad_loss), None, None, None, None
+
+
+class _VocabLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, weight, targets):
+        r = vocab_logprobs(hidden, weight, targets, save=True)
+        ctx.save_for_backward(hidden, weight, targets, r.saved)
+        return r.logp
+
+    @staticmethod
+    def backward(ctx, grad_logp):
+        return *_vocab_gradients(ctx, "vocab_logprobs_autograd", grad_logp.contiguous(), None, grad_logp), None
+
+
+def _vocab_gradients(ctx, call, grad_logp, scale, upstream):
+    hidden, weight, targets, saved = ctx.saved_tensors[:4]
+    wanted = ctx.needs_input_grad[:2]
+    if not any(wanted):
+        return None, None
+    grad = True if all(wanted) else "hidden" if wanted[0] else "weight"
+    got = vocab_logprobs_backward(hidden, weight, targets, saved, grad_logp, scale=scale, grad=grad)
+    return tuple(_once(call, g, hidden, weight, upstream) for g in got)
+
+
+class _VocabLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, weight, targets, weights, mean, grad_scale):
+        r = vocab_loss(hidden, weight, targets, weights, mean, grad=False, save=True)
+        ctx.grad_scale = grad_scale
+        ctx.save_for_backward(hidden, weight, targets, r.saved, r.row_grads)
+        ctx.mark_non_differentiable(r.stats, r.logp)
+        return r.stats[0].clone(), r.stats, r.logp
+
+    @staticmethod
+    def backward(ctx, grad_loss, _stats, _logp):
+        scale = grad_loss.reshape(1).float()
+        if ctx.grad_scale != 1.0:
+            scale = scale * ctx.grad_scale
+        return *_vocab_gradients(ctx, "vocab_loss_autograd", ctx.saved_tensors[4], scale, grad_loss), None, None, None, None
+
+
+def vocab_logprobs_autograd(hidden, weight, targets):
+    """``vocab_logprobs(...).logp``, differentiable in hidden and weight."""
+    return _VocabLogprobs.apply(hidden, weight, targets)
+
+
+def vocab_loss_autograd(hidden, weight, targets, weights=None, mean: bool = True, grad_scale: float = 1.0):
+    """(loss, stats, logp) of ``vocab_loss``; the loss is differentiable in hidden
+    and weight, and ``grad_scale`` multiplies their gradients as it does there."""
+    return _VocabLoss.apply(hidden, weight, targets, weights, mean, grad_scale)
 
 
 def token_logprobs_autograd(logits, targets):

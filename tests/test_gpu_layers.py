@@ -1,0 +1,307 @@
+"""Layer norm and embedding on the GPU against their definitions in 64 bits."""
+
+import numpy as np
+import pytest
+
+import lm_reference as R
+from test_gpu_vocab import close
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1511_05946_amd import layers
+    return torch, layers
+
+
+# rows, width, distance of x's rows beyond the width, type of x, of y, of weight and bias: one of each, every number of
+# lanes and registers on both sides of its bounds, rows that only a workgroup's loop covers, odd widths, more rows than
+# there are workgroups
+NORM = [(1, 1, 0, "float32", "float32", "float32"), (2, 2, 1, "bfloat16", "float32", "float32"),
+        (5, 7, 0, "float32", "bfloat16", "bfloat16"), (17, 128, 0, "bfloat16", "bfloat16", "float32"),
+        (33, 129, 0, "float32", "float32", "float32"), (64, 256, 0, "float32", "float32", "float32"),
+        (9, 257, 3, "bfloat16", "bfloat16", "bfloat16"), (11, 512, 0, "float32", "bfloat16", "float32"),
+        (700, 513, 0, "bfloat16", "float32", "float32"), (3000, 1000, 24, "bfloat16", "bfloat16", "float32"),
+        (5, 1025, 0, "float32", "float32", "bfloat16"), (600, 2048, 0, "bfloat16", "bfloat16", "float32"),
+        (7, 2049, 0, "float32", "float32", "float32"), (1100, 4096, 0, "float32", "bfloat16", "float32"),
+        (3, 4097, 5, "bfloat16", "bfloat16", "float32"), (6, 8192, 0, "float32", "float32", "float32"),
+        (4, 8200, 0, "bfloat16", "float32", "float32"), (520, 9216, 0, "float32", "float32", "float32"),
+        (3, 16384, 0, "bfloat16", "bfloat16", "float32"), (3, 16385, 0, "float32", "bfloat16", "float32"),
+        (70, 33001, 7, "bfloat16", "bfloat16", "bfloat16"), (2, 65536, 0, "float32", "float32", "float32"),
+        (9000, 16, 0, "float32", "float32", "float32"), (20000, 3, 2, "bfloat16", "float32", "float32")]
+
+
+def make(torch, shape, seed=0, offset=0.5):
+    rows, width, more, xt, yt, wt = shape
+    print(f"[case] norm {shape} seed={seed}", flush=True)
+    gen = torch.Generator().manual_seed(17 * seed + rows + width)
+    x = torch.randn(rows, width + more, generator=gen) + offset * torch.randn(rows, 1, generator=gen)
+    x[:, ::5] *= 4
+    x = x.to(getattr(torch, xt))
+    w = (1 + 0.2 * torch.randn(width, generator=gen)).to(getattr(torch, wt))
+    b = (0.2 * torch.randn(width, generator=gen)).to(getattr(torch, wt))
+    g = torch.randn(rows, width, generator=gen).to(getattr(torch, yt))
+    return x, w, b, g
+
+
+def check_back(got, ref, wanted_type, torch):
+    for t, name in zip(got, ("grad_x", "grad_weight", "grad_bias")):
+        value, tol = ref[name]
+        close(t, value, tol + R.out_rounding(value, t.dtype is torch.bfloat16) + 2 * R.EPS * np.abs(value), name)
+
+
+@pytest.mark.parametrize("shape", NORM)
+def test_layer_norm(env, shape):
+    torch, layers = env
+    x, w, b, g = make(torch, shape)
+    rows, width = shape[:2]
+    x64, w64, b64 = x[:, :width].double().numpy(), w.double().numpy(), b.double().numpy()
+    xc, wc, bc, gc = x.cuda()[:, :width], w.cuda(), b.cuda(), g.cuda()
+    ydt = getattr(torch, shape[4])
+    r = layers.layer_norm(xc, wc, bc, dtype=ydt, save=True)
+    assert r.y.dtype is ydt
+    ref = R.Norm(x64, w64, b64, 1e-5)
+    close(r.y, ref.y, ref.y_tol + R.out_rounding(ref.y, ydt is torch.bfloat16), "y")
+    close(r.saved[:, 0], ref.mean[:, 0], ref.dmean[:, 0] + 1e-37, "mean")
+    close(r.saved[:, 1], ref.rstd[:, 0], (ref.rstd * ref.rel)[:, 0], "rstd")
+    got = layers.layer_norm_backward(xc, gc, wc, r.saved)
+    assert got[1].dtype is w.dtype and got[0].dtype is x.dtype
+    check_back(got, ref.backward(g.double().numpy()), None, torch)
+    again = layers.layer_norm_backward(xc, gc, wc, r.saved, dtype=torch.float32)
+    assert torch.equal(again[0], got[0]) and torch.equal(again[1].to(w.dtype), got[1])
+    # into wider rows; grad_x alone; the sums alone; added
+    wide = torch.full((rows, width + 4), 3.0, dtype=ydt, device="cuda")
+    layers.layer_norm(xc, wc, bc, out=wide[:, 1:-3])
+    assert torch.equal(wide[:, 1:-3], r.y) and (wide[:, 0] == 3).all() and (wide[:, -3:] == 3).all()
+    alone = layers.layer_norm_backward(xc, gc, wc, r.saved, grad=(True, False, False))
+    assert torch.equal(alone[0], got[0]) and alone[1] is None and alone[2] is None
+    none, sw, sb = layers.layer_norm_backward(xc, gc, wc, r.saved, grad=(False, True, True))
+    assert none is None and torch.equal(sw, got[1]) and torch.equal(sb, got[2])
+    start = [torch.randn(width, generator=torch.Generator().manual_seed(2)).cuda() for _ in range(2)]
+    added = [t.clone() for t in start]
+    layers.layer_norm_backward(xc, gc, wc, r.saved, grads=added, accumulate=True)
+    for t, s, f in zip(added, start, again[1:]):
+        assert torch.equal(t, s + f)
+    if x.dtype is ydt:   # in place of grad_y
+        place = gc.clone()
+        back = layers.layer_norm_backward(xc, place, wc, r.saved, out=place)
+        assert back[0] is place and torch.equal(place, got[0]) and torch.equal(back[1], got[1])
+
+
+def test_without_weight_and_bias(env):
+    torch, layers = env
+    x, w, b, g = make(torch, (40, 300, 0, "float32", "float32", "float32"), seed=1)
+    ref = R.Norm(x.double().numpy(), None, None, 1e-5)
+    r = layers.layer_norm(x.cuda(), save=True)
+    close(r.y, ref.y, ref.y_tol + R.out_rounding(ref.y, False), "y")
+    check_back(layers.layer_norm_backward(x.cuda(), g.cuda(), None, r.saved), ref.backward(g.double().numpy()), None, torch)
+    only = layers.layer_norm(x.cuda(), None, b.cuda()).y
+    assert torch.equal(only, r.y + b.cuda()) or (only - r.y - b.cuda()).abs().max().item() <= 4 * R.EPS * 30
+
+
+@pytest.mark.parametrize("width", [40, 3000, 20000])
+def test_norm_of_rows_far_from_zero(env, width):
+    """Means a thousand deviations away, constant rows, zeros."""
+    torch, layers = env
+    print(f"[case] far rows {width}", flush=True)
+    gen = torch.Generator().manual_seed(width)
+    x = torch.randn(6, width, generator=gen) + 1000.0
+    x[1] = 3.0
+    x[2] = 0.0
+    x[3] *= 1e15
+    x[4] *= 1e-20
+    ref = R.Norm(x.double().numpy(), None, None, 1e-5)
+    r = layers.layer_norm(x.cuda(), save=True)
+    close(r.y, ref.y, ref.y_tol + R.out_rounding(ref.y, False), "y")
+    assert (r.y[2] == 0).all()
+    # rows that are not numbers stay by themselves
+    x[0, width // 2] = float("inf")
+    x[5, 0] = float("nan")
+    y = layers.layer_norm(x.cuda()).y
+    assert torch.isnan(y[0]).all() and torch.isnan(y[5]).all() and torch.equal(y[1:5], r.y[1:5])
+
+
+def test_norm_of_no_rows(env):
+    torch, layers = env
+    x, w = torch.empty(0, 70, device="cuda"), torch.ones(70, device="cuda")
+    r = layers.layer_norm(x, w, save=True)
+    assert r.y.shape == (0, 70)
+    gx, gw, gb = layers.layer_norm_backward(x, x, w, r.saved)
+    assert gx.shape == (0, 70) and (gw == 0).all() and (gb == 0).all()
+    total = w.clone()
+    layers.layer_norm_backward(x, x, w, r.saved, grads=(total, None), accumulate=True)
+    assert (total == 1).all()
+
+
+def test_norm_gradient_against_differences(env):
+    torch, layers = env
+    x, w, b, g = (t.double() for t in make(torch, (3, 11, 0, "float32", "float32", "float32"), seed=2))
+
+    def value(x, w, b):
+        return (torch.nn.functional.layer_norm(x, (11,), w, b, 1e-5) * g).sum().item()
+
+    xc, wc = x.float().cuda(), w.float().cuda()
+    r = layers.layer_norm(xc, wc, b.float().cuda(), save=True)
+    got = layers.layer_norm_backward(xc, g.float().cuda(), wc, r.saved)
+    for which, t in enumerate((x, w, b)):
+        for i in range(0, t.numel(), 3):
+            vals = []
+            for sign in (1, -1):
+                args = [x, w, b]
+                args[which] = t.clone()
+                args[which].view(-1)[i] += sign * 1e-5
+                vals.append(value(*args))
+            diff = (vals[0] - vals[1]) / 2e-5
+            assert abs(got[which].reshape(-1)[i].item() - diff) <= 1e-7 + 1e-5 * abs(diff) + 200 * R.EPS
+
+
+def test_norm_autograd(env):
+    torch, layers = env
+    x, w, b, g = (t.cuda() for t in make(torch, (30, 200, 0, "float32", "bfloat16", "float32"), seed=3))
+    leaves = [t.clone().requires_grad_(True) for t in (x, w, b)]
+    y = layers.layer_norm_autograd(*leaves, dtype=torch.bfloat16)
+    y.backward(g)
+    r = layers.layer_norm(x, w, b, dtype=torch.bfloat16, save=True)
+    want = layers.layer_norm_backward(x, g, w, r.saved)
+    assert torch.equal(y, r.y) and all(torch.equal(a.grad, v) for a, v in zip(leaves, want))
+    x2 = x.clone().requires_grad_(True)
+    first, = torch.autograd.grad(layers.layer_norm_autograd(x2, w).sum(), x2, create_graph=True)
+    with pytest.raises(RuntimeError, match="differentiated again"):
+        first.sum().backward()
+
+
+# tokens, width, classes, weight's type, rows' type, bits: one of each; classes that need one, two and three passes of the
+# sort; runs of one token within 64 rows, over many, ending at them; tokens of several tiles of the sort
+EMBED = [(1, 1, 1, "float32", "float32", 64), (3, 7, 5, "bfloat16", "float32", 32), (64, 8, 2, "float32", "float32", 64),
+         (65, 513, 255, "float32", "bfloat16", 64), (128, 33, 1, "bfloat16", "bfloat16", 64), (500, 64, 256, "float32", "float32", 32),
+         (2048, 16, 65535, "bfloat16", "bfloat16", 64), (2049, 9, 65536, "float32", "float32", 64), (5000, 20, 7, "float32", "float32", 64),
+         (30000, 3, 70000, "float32", "float32", 32), (70000, 2, 3, "bfloat16", "float32", 64), (300, 1025, 40, "bfloat16", "bfloat16", 64),
+         (16, 4096, 1000, "float32", "float32", 64)]
+
+
+def tokens_of(torch, n, classes, bits, gen, idle=0.1):
+    u = torch.rand(n, generator=gen, dtype=torch.float64)
+    t = ((u * np.log(classes + 1)).exp() - 1).long().clamp_(0, classes - 1)
+    off = torch.rand(n, generator=gen) < idle
+    t[off] = -1 - torch.randint(0, 9, (int(off.sum()),), generator=gen)
+    return t.to(getattr(torch, f"int{bits}"))
+
+
+@pytest.mark.parametrize("shape", EMBED)
+def test_embedding(env, shape):
+    torch, layers = env
+    n, width, classes, wt, ot, bits = shape
+    print(f"[case] embedding {shape}", flush=True)
+    gen = torch.Generator().manual_seed(n + width + classes)
+    t = tokens_of(torch, n, classes, bits, gen)
+    w = torch.randn(classes, width + 2, generator=gen).to(getattr(torch, wt))
+    odt = getattr(torch, ot)
+    tc, wc = t.cuda(), w.cuda()[:, :width]
+    y = layers.embedding(tc, wc, 1.7, dtype=odt)
+    ref = R.embedding(t.numpy(), w[:, :width].double().numpy(), float(np.float32(1.7)))
+    close(y, ref, R.EPS * np.abs(ref) + R.out_rounding(ref, ot == "bfloat16"), "rows")
+    g = torch.randn(n, width + 1, generator=gen).to(odt)
+    g[t < 0] = float("nan")   # not read
+    gc = g.cuda()[:, :width]
+    gw = layers.embedding_backward(tc, gc, classes, 1.7, dtype=w.dtype)
+    g64 = np.nan_to_num(g[:, :width].double().numpy())
+    ref, tol = R.embedding_gradient(t.numpy(), g64, classes, float(np.float32(1.7)))
+    close(gw, ref, tol + R.out_rounding(ref, wt == "bfloat16"), "grad_weight")
+    assert torch.equal(layers.embedding_backward(tc, gc, classes, 1.7, dtype=w.dtype), gw)
+    # whole numbers add up exactly: no row is lost or taken twice
+    whole = torch.randint(-8, 9, (n, width), generator=gen).to(odt)
+    got = layers.embedding_backward(tc, whole.cuda(), classes, dtype=torch.float32)
+    want, _ = R.embedding_gradient(t.numpy(), whole.double().numpy(), classes, 1.0)
+    assert (got.double().cpu().numpy() == want).all()
+    # added to what is there, in wider rows; classes without a token stay
+    start = torch.randint(-8, 9, (classes, width + 3), generator=gen).float().cuda()
+    total = start.clone()
+    layers.embedding_backward(tc, whole.cuda(), classes, grad_weight=total[:, 1:-2], accumulate=True)
+    assert torch.equal(total[:, 1:-2], start[:, 1:-2] + got) and torch.equal(total[:, 0], start[:, 0])
+    assert torch.equal(total[:, -2:], start[:, -2:])
+
+
+def test_tokens_past_the_classes_and_none(env):
+    torch, layers = env
+    w = torch.randn(10, 12, device="cuda")
+    t = torch.tensor([3, 10, -1, 1 << 40, 9, -(1 << 40)], device="cuda")
+    y = layers.embedding(t, w)
+    assert torch.equal(y[0], w[3]) and torch.equal(y[4], w[9]) and torch.isnan(y[1]).all() and torch.isnan(y[3]).all()
+    assert (y[2] == 0).all() and (y[5] == 0).all()
+    g = torch.full((6, 12), float("inf"), device="cuda")
+    g[0], g[4] = 1.0, 2.0
+    gw = layers.embedding_backward(t, g, 10)
+    want = torch.zeros(10, 12, device="cuda")
+    want[3], want[9] = 1.0, 2.0
+    assert torch.equal(gw, want)
+    assert layers.embedding(t[:0], w).shape == (0, 12)
+    assert (layers.embedding_backward(t[:0], g[:0], 10) == 0).all()
+    layers.embedding_backward(t[:0], g[:0], 10, grad_weight=want, accumulate=True)
+    assert want.sum().item() == 36
+    assert (layers.embedding_backward(t[2:3], g[2:3], 10) == 0).all()   # no token takes part
+
+
+@pytest.mark.parametrize("n,first", [(64, 64), (128, 64), (129, 65), (200, 63), (640, 320)])
+def test_runs_at_the_pieces_borders(env, n, first):
+    """`first` rows of one class, then another: runs that end at, before and behind a multiple of 64."""
+    torch, layers = env
+    print(f"[case] runs {n} {first}", flush=True)
+    t = torch.tensor([2] * first + [5] * (n - first), device="cuda")
+    g = torch.randint(-8, 9, (n, 30), generator=torch.Generator().manual_seed(n)).float().cuda()
+    got = layers.embedding_backward(t.flip(0).contiguous(), g.flip(0).contiguous(), 7)
+    assert torch.equal(got[2], g[:first].sum(0)) and torch.equal(got[5], g[first:].sum(0) if first < n else torch.zeros_like(got[5]))
+    assert (got[[0, 1, 3, 4, 6]] == 0).all()
+
+
+def test_embedding_autograd(env):
+    torch, layers = env
+    gen = torch.Generator().manual_seed(1)
+    t = tokens_of(torch, 100, 40, 64, gen).cuda()
+    w = torch.randn(40, 24, generator=gen).cuda()
+    leaf = w.clone().requires_grad_(True)
+    y = layers.embedding_autograd(t, leaf, 2.0)
+    g = torch.randn(100, 24, generator=gen).cuda()
+    y.backward(g)
+    assert torch.equal(y, layers.embedding(t, w, 2.0)) and torch.equal(leaf.grad, layers.embedding_backward(t, g, 40, 2.0))
+
+
+def test_captured_and_on_another_stream(env):
+    torch, layers = env
+    gen = torch.Generator().manual_seed(4)
+    t = tokens_of(torch, 3000, 500, 64, gen).cuda()
+    w = torch.randn(500, 96, generator=gen).cuda()
+    g = torch.randn(3000, 96, generator=gen).cuda()
+    nw, nb = torch.randn(96, generator=gen).cuda(), torch.randn(96, generator=gen).cuda()
+    ws = torch.empty(layers.workspace_bytes(3000, 96, 500), dtype=torch.uint8, device="cuda")
+
+    def run(ws=None):
+        y = layers.embedding(t, w, 0.5)
+        r = layers.layer_norm(y, nw, nb, save=True)
+        gx, gw, gb = layers.layer_norm_backward(y, g, nw, r.saved, workspace=ws)
+        return r.y, gx, gw, gb, layers.embedding_backward(t, gx, 500, 0.5, workspace=ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        first = run(ws)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run(ws)
+    for k in range(4):
+        if k == 2:
+            t.copy_(t.flip(0))
+            g.mul_(2)
+        ws.fill_(255)
+        graph.replay()
+        want = run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), k
+        if k == 0:
+            assert all(torch.equal(a, b) for a, b in zip(first, want))
+        junk = torch.randn(1 << 20, device="cuda").sum().item()
+        assert junk == junk
