@@ -18,6 +18,7 @@
 #include <vector>
 
 #include "acdc_train.h"
+#include "acdc_train_lm.h"
 
 namespace {
 
@@ -469,9 +470,315 @@ PyObject* grad_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// ------------------------------------------------ the language-model operators
+
+// Rows of float32 or bfloat16 values on one device; `bad` where something is not plain.
+struct Matrix {
+  const Tensor* t = nullptr;
+  int64_t rows = 0, width = 0, stride = 0;
+  int32_t dtype = 0;
+  bool read(const Tensor* m) {
+    if (m == nullptr || !Logits::plain(*m)) return false;
+    t = m;
+    rows = m->size(0);
+    width = m->size(1);
+    stride = Logits::step(*m);
+    dtype = type_of(*m);
+    return true;
+  }
+  bool like(const Matrix& m) const { return rows == m.rows && width == m.width && t->device() == m.t->device(); }
+  at::Device device() const { return t->device(); }
+  Tensor make(at::IntArrayRef size, at::ScalarType type) const { return at::empty(size, t->options().dtype(type)); }
+  Tensor floats(at::IntArrayRef size) const { return make(size, at::kFloat); }
+  // a workspace of `need` bytes that begins at a multiple of 256
+  bool workspace(const Tensor* given, size_t need, Tensor* ws) const {
+    if (given == nullptr) {
+      *ws = make({int64_t(std::max<size_t>(need, 1))}, at::kByte);
+      return true;
+    }
+    if (given->scalar_type() != at::kByte || given->dim() != 1 || size_t(given->numel()) < need ||
+        given->device() != t->device() || !given->is_contiguous() || gone(*given) ||
+        reinterpret_cast<uintptr_t>(given->data_ptr()) % 256 != 0)
+      return false;
+    *ws = *given;
+    return true;
+  }
+};
+at::ScalarType scalar(int32_t dtype) { return dtype == ACDC_F32 ? at::kFloat : at::kBFloat16; }
+// A tensor that the call writes: the caller's, or a new one.
+bool target_matrix(const Tensor* given, const Matrix& like, int64_t rows, int64_t width, at::ScalarType type, bool any_type,
+                   Tensor* out, Matrix* m) {
+  if (given == nullptr) *out = like.make({rows, width}, type);
+  else *out = *given;
+  if (given != nullptr && (!m->read(given) || (!any_type && given->scalar_type() != type))) return false;
+  if (given == nullptr) {
+    m->t = out;
+    m->rows = rows;
+    m->width = width;
+    m->stride = width;
+    m->dtype = type == at::kFloat ? ACDC_F32 : ACDC_BF16;
+  }
+  return m->rows == rows && m->width == width && out->device() == like.device();
+}
+// weights and biases: a vector of either type
+bool width_vector(const Tensor* t, int64_t n, const at::Device& device) {
+  return t == nullptr || (type_of(*t) >= 0 && vector_of(t, n, device, t->scalar_type()));
+}
+// What the C entry point refuses, the caller's Python code puts into words.
+bool refused(int rc) { return rc == ACDC_ERR_INVALID_ARG; }
+
+struct Head {
+  Matrix hidden, weight;
+  acdc_vocab_head h;
+  size_t need = 0;
+  Tensor ws;
+  bool read(const Tensor* x, const Tensor* w, const Tensor* targets, bool gradient, const Tensor* given) {
+    if (!hidden.read(x) || !weight.read(w) || targets == nullptr || hidden.width != weight.width || weight.rows < 1 ||
+        weight.rows > 0x7fffffff || hidden.dtype != weight.dtype || hidden.device() != weight.device())
+      return false;
+    const int32_t bits = index_bits(*targets, hidden.rows, hidden.device());
+    if (bits == 0) return false;
+    h = acdc_vocab_head{x->data_ptr(), w->data_ptr(), targets->data_ptr(), hidden.stride, weight.stride, hidden.rows,
+                        int32_t(hidden.width), int32_t(weight.rows), hidden.dtype, bits};
+    need = acdc_vocab_workspace_size(h.rows, h.width, h.classes, h.dtype, gradient ? 1 : 0);
+    return need != 0 && hidden.workspace(given, need, &ws);
+  }
+  bool grads(const Tensor* out, const Tensor* grad_weight, bool accumulate, bool want_hidden, bool want_weight, Tensor* gh,
+             Tensor* gw, acdc_vocab_grads* g) const {
+    *g = acdc_vocab_grads{nullptr, nullptr, 0, 0, 0, accumulate ? 1 : 0};
+    Matrix m;
+    if (want_hidden) {
+      if (!target_matrix(out, hidden, h.rows, h.width, scalar(h.dtype), false, gh, &m)) return false;
+      g->hidden = gh->data_ptr();
+      g->hidden_stride = m.stride;
+    }
+    if (want_weight) {
+      if (accumulate && grad_weight == nullptr) return false;
+      if (!target_matrix(grad_weight, hidden, h.classes, h.width, scalar(h.dtype), true, gw, &m)) return false;
+      if (m.dtype != h.dtype && m.dtype != ACDC_F32) return false;
+      g->weight = gw->data_ptr();
+      g->weight_stride = m.stride;
+      g->weight_type = m.dtype;
+    }
+    return true;
+  }
+};
+
+// (hidden, weight, targets, save, workspace, stream) -> (logp, saved)
+PyObject* vocab_logprobs(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(n, 6, [&]() -> PyObject* {
+    Args a{args};
+    const Tensor *x = a.must(0), *w = a.must(1), *t = a.must(2), *given = a.may(4);
+    const bool save = a.flag(3);
+    const acdc_stream_t stream = a.stream(5);
+    Head head;
+    if (a.bad || !head.read(x, w, t, false, given)) Py_RETURN_NONE;
+    Tensor logp = head.hidden.floats({head.h.rows}), saved;
+    if (save) saved = head.hidden.floats({head.h.rows, 2});
+    const int rc = acdc_vocab_logprob(&head.h, ptr(logp), ptr(saved), head.ws.data_ptr(), head.need, stream);
+    if (refused(rc)) Py_RETURN_NONE;
+    if (rc != ACDC_OK) return PyLong_FromLong(rc);
+    return tuple_of({logp, saved});
+  });
+}
+
+// (hidden, weight, targets, saved, grad_logp, scale, want_hidden, want_weight, out, grad_weight, accumulate, workspace,
+//  stream) -> (grad_hidden, grad_weight)
+PyObject* vocab_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(n, 13, [&]() -> PyObject* {
+    Args a{args};
+    const Tensor *x = a.must(0), *w = a.must(1), *t = a.must(2), *saved = a.must(3), *g = a.must(4), *scale = a.may(5),
+                 *out = a.may(8), *gw_given = a.may(9), *given = a.may(11);
+    const bool want_hidden = a.flag(6), want_weight = a.flag(7), accumulate = a.flag(10);
+    const acdc_stream_t stream = a.stream(12);
+    Head head;
+    if (a.bad || !head.read(x, w, t, true, given)) Py_RETURN_NONE;
+    const at::Device device = head.hidden.device();
+    if (saved->dim() != 2 || saved->size(0) != head.h.rows || saved->size(1) != 2 || saved->scalar_type() != at::kFloat ||
+        saved->device() != device || !saved->is_contiguous() || !readable(*saved) || !floats(g, head.h.rows, device) ||
+        !floats(scale, 1, device))
+      Py_RETURN_NONE;
+    Tensor gh, gw;
+    acdc_vocab_grads grads;
+    if (!head.grads(out, gw_given, accumulate, want_hidden, want_weight, &gh, &gw, &grads)) Py_RETURN_NONE;
+    const int rc = acdc_vocab_backward(&head.h, ptr(saved), ptr(g), ptr(scale), &grads, head.ws.data_ptr(), head.need, stream);
+    if (refused(rc)) Py_RETURN_NONE;
+    if (rc != ACDC_OK) return PyLong_FromLong(rc);
+    if (want_hidden) wrote(out);
+    if (want_weight) wrote(gw_given);
+    return tuple_of({gh, gw});
+  });
+}
+
+// (hidden, weight, targets, weights, mean, grad_scale, want_hidden, want_weight, save, out, grad_weight, accumulate,
+//  workspace, stream) -> (stats, logp, grad_hidden, grad_weight, saved, row_grads)
+PyObject* vocab_loss(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(n, 14, [&]() -> PyObject* {
+    Args a{args};
+    const Tensor *x = a.must(0), *w = a.must(1), *t = a.must(2), *weights = a.may(3), *out = a.may(9), *gw_given = a.may(10),
+                 *given = a.may(12);
+    acdc_vocab_params p;
+    p.mean = a.flag(4) ? 1 : 0;
+    p.grad_scale = float(a.number(5));
+    const bool want_hidden = a.flag(6), want_weight = a.flag(7), save = a.flag(8), accumulate = a.flag(11);
+    const acdc_stream_t stream = a.stream(13);
+    Head head;
+    if (a.bad || !head.read(x, w, t, want_hidden || want_weight, given)) Py_RETURN_NONE;
+    if (!floats(weights, head.h.rows, head.hidden.device())) Py_RETURN_NONE;
+    Tensor gh, gw, saved, row_grads;
+    acdc_vocab_grads grads;
+    if (!head.grads(out, gw_given, accumulate, want_hidden, want_weight, &gh, &gw, &grads)) Py_RETURN_NONE;
+    Tensor stats = head.hidden.floats({2}), logp = head.hidden.floats({head.h.rows});
+    if (save) {
+      saved = head.hidden.floats({head.h.rows, 2});
+      row_grads = head.hidden.floats({head.h.rows});
+    }
+    const int rc = acdc_vocab_loss(&head.h, ptr(weights), &p, ptr(stats), ptr(logp), ptr(saved), ptr(row_grads), &grads,
+                                   head.ws.data_ptr(), head.need, stream);
+    if (refused(rc)) Py_RETURN_NONE;
+    if (rc != ACDC_OK) return PyLong_FromLong(rc);
+    if (want_hidden) wrote(out);
+    if (want_weight) wrote(gw_given);
+    return tuple_of({stats, logp, gh, gw, saved, row_grads});
+  });
+}
+
+// dtype: 0 or 1, or -1 for `otherwise`
+at::ScalarType type_or(double dtype, at::ScalarType otherwise) { return dtype < 0 ? otherwise : scalar(int32_t(dtype)); }
+
+// (x, weight, bias, eps, dtype, save, out, stream) -> (y, saved)
+PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(n, 8, [&]() -> PyObject* {
+    Args a{args};
+    const Tensor *x = a.must(0), *weight = a.may(1), *bias = a.may(2), *out = a.may(6);
+    const double eps = a.number(3), dtype = a.number(4);
+    const bool save = a.flag(5);
+    const acdc_stream_t stream = a.stream(7);
+    Matrix m, to;
+    if (a.bad || !m.read(x) || !width_vector(weight, m.width, m.device()) || !width_vector(bias, m.width, m.device()) ||
+        (weight != nullptr && bias != nullptr && weight->scalar_type() != bias->scalar_type()))
+      Py_RETURN_NONE;
+    Tensor y, saved;
+    if (!target_matrix(out, m, m.rows, m.width, type_or(dtype, out != nullptr ? out->scalar_type() : x->scalar_type()), false, &y, &to))
+      Py_RETURN_NONE;
+    if (save) saved = m.floats({m.rows, 2});
+    const Tensor* v = weight != nullptr ? weight : bias;
+    const int rc = acdc_norm_forward(x->data_ptr(), m.dtype, m.stride, ptr<void>(weight), ptr<void>(bias), v != nullptr ? type_of(*v) : 0,
+                                     float(eps), y.data_ptr(), to.dtype, to.stride, ptr(saved), m.rows, int32_t(m.width), stream);
+    if (refused(rc)) Py_RETURN_NONE;
+    if (rc != ACDC_OK) return PyLong_FromLong(rc);
+    wrote(out);
+    return tuple_of({y, saved});
+  });
+}
+
+// (x, grad_y, weight, saved, out, grad_weight, grad_bias, given, accumulate, want_x, want_weight, want_bias, dtype, workspace,
+//  stream) -> (grad_x, grad_weight, grad_bias); given: the two sums go into grad_weight and grad_bias (None: not wanted)
+PyObject* norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(n, 15, [&]() -> PyObject* {
+    Args a{args};
+    const Tensor *x = a.must(0), *gy = a.must(1), *weight = a.may(2), *saved = a.must(3), *out = a.may(4), *gw_in = a.may(5),
+                 *gb_in = a.may(6), *ws_in = a.may(13);
+    const bool given = a.flag(7), accumulate = a.flag(8), want_x = a.flag(9), want_w = a.flag(10), want_b = a.flag(11);
+    const double dtype = a.number(12);
+    const acdc_stream_t stream = a.stream(14);
+    Matrix m, g, to;
+    if (a.bad || !m.read(x) || !g.read(gy) || !g.like(m) || !width_vector(weight, m.width, m.device())) Py_RETURN_NONE;
+    const at::Device device = m.device();
+    if (saved->dim() != 2 || saved->size(0) != m.rows || saved->size(1) != 2 || saved->scalar_type() != at::kFloat ||
+        saved->device() != device || !saved->is_contiguous() || !readable(*saved) || (accumulate && !given))
+      Py_RETURN_NONE;
+    Tensor gx, gw, gb;
+    if (want_x && !target_matrix(out, m, m.rows, m.width, x->scalar_type(), false, &gx, &to)) Py_RETURN_NONE;
+    if (given) {
+      if (!width_vector(gw_in, m.width, device) || !width_vector(gb_in, m.width, device)) Py_RETURN_NONE;
+      if (want_w && gw_in != nullptr) gw = *gw_in;
+      if (want_b && gb_in != nullptr) gb = *gb_in;
+      if (gw.defined() && gb.defined() && gw.scalar_type() != gb.scalar_type()) Py_RETURN_NONE;
+    } else {
+      const at::ScalarType type = type_or(dtype, weight != nullptr ? weight->scalar_type() : at::kFloat);
+      if (want_w) gw = m.make({m.width}, type);
+      if (want_b) gb = m.make({m.width}, type);
+    }
+    const int32_t type = gw.defined() ? type_of(gw) : gb.defined() ? type_of(gb) : 0;
+    const size_t need = acdc_norm_workspace_size(m.rows, int32_t(std::min<int64_t>(m.width, 0x7fffffff)));
+    Tensor ws;
+    if (need == 0 || !m.workspace(ws_in, need, &ws)) Py_RETURN_NONE;
+    const int rc = acdc_norm_backward(x->data_ptr(), m.dtype, m.stride, gy->data_ptr(), g.dtype, g.stride, ptr<void>(weight),
+                                      weight != nullptr ? type_of(*weight) : 0, ptr(saved), ptr<void>(gx), to.stride, ptr<void>(gw),
+                                      ptr<void>(gb), type, accumulate ? 1 : 0, m.rows, int32_t(m.width), ws.data_ptr(), need, stream);
+    if (refused(rc)) Py_RETURN_NONE;
+    if (rc != ACDC_OK) return PyLong_FromLong(rc);
+    if (want_x) wrote(out);
+    if (given) {
+      if (gw.defined()) wrote(gw_in);
+      if (gb.defined()) wrote(gb_in);
+    }
+    return tuple_of({gx, gw, gb});
+  });
+}
+
+// (tokens, weight, scale, dtype, out, stream) -> rows
+PyObject* embedding(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(n, 6, [&]() -> PyObject* {
+    Args a{args};
+    const Tensor *t = a.must(0), *w = a.must(1), *out = a.may(4);
+    const double scale = a.number(2), dtype = a.number(3);
+    const acdc_stream_t stream = a.stream(5);
+    Matrix m, to;
+    if (a.bad || !m.read(w) || t->dim() != 1 || m.rows > 0x7fffffff) Py_RETURN_NONE;
+    const int64_t rows = t->size(0);
+    const int32_t bits = index_bits(*t, rows, m.device());
+    Tensor y;
+    if (bits == 0 || !target_matrix(out, m, rows, m.width, type_or(dtype, out != nullptr ? out->scalar_type() : w->scalar_type()), false, &y, &to))
+      Py_RETURN_NONE;
+    const int rc = acdc_embedding_forward(t->data_ptr(), bits, w->data_ptr(), m.dtype, m.stride, float(scale), y.data_ptr(), to.dtype,
+                                          to.stride, rows, int32_t(m.width), int32_t(m.rows), stream);
+    if (refused(rc)) Py_RETURN_NONE;
+    if (rc != ACDC_OK) return PyLong_FromLong(rc);
+    wrote(out);
+    return wrap(y);
+  });
+}
+
+// (tokens, grad_rows, classes, scale, dtype, grad_weight, accumulate, workspace, stream) -> grad_weight
+PyObject* embedding_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    Args a{args};
+    const Tensor *t = a.must(0), *g = a.must(1), *given = a.may(5), *ws_in = a.may(7);
+    if (!PyLong_Check(args[2])) Py_RETURN_NONE;
+    const long long classes = PyLong_AsLongLong(args[2]);
+    if (PyErr_Occurred()) {
+      PyErr_Clear();
+      Py_RETURN_NONE;
+    }
+    const double scale = a.number(3), dtype = a.number(4);
+    const bool accumulate = a.flag(6);
+    const acdc_stream_t stream = a.stream(8);
+    Matrix m, to;
+    if (a.bad || !m.read(g) || classes < 1 || classes > 0x7fffffff || (accumulate && given == nullptr)) Py_RETURN_NONE;
+    const int32_t bits = t->dim() == 1 ? index_bits(*t, m.rows, m.device()) : 0;
+    Tensor gw, ws;
+    if (bits == 0 ||
+        !target_matrix(given, m, classes, m.width, type_or(dtype, given != nullptr ? given->scalar_type() : g->scalar_type()), false, &gw, &to))
+      Py_RETURN_NONE;
+    const size_t need = acdc_embedding_workspace_size(m.rows, int32_t(std::min<int64_t>(m.width, 0x7fffffff)), int32_t(classes));
+    if (need == 0 || !m.workspace(ws_in, need, &ws)) Py_RETURN_NONE;
+    const int rc = acdc_embedding_backward(t->data_ptr(), bits, g->data_ptr(), m.dtype, m.stride, float(scale), gw.data_ptr(), to.dtype,
+                                           to.stride, accumulate ? 1 : 0, m.rows, int32_t(m.width), int32_t(classes), ws.data_ptr(),
+                                           need, stream);
+    if (refused(rc)) Py_RETURN_NONE;
+    if (rc != ACDC_OK) return PyLong_FromLong(rc);
+    wrote(given);
+    return wrap(gw);
+  });
+}
+
 #define ENTRY(name) {#name, (PyCFunction)(void*)name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(logprobs), ENTRY(logprobs_backward), ENTRY(policy),     ENTRY(preference),
-                         ENTRY(adamw),    ENTRY(grad_norm),         {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(adamw),    ENTRY(grad_norm),         ENTRY(vocab_logprobs), ENTRY(vocab_backward),
+                         ENTRY(vocab_loss), ENTRY(norm), ENTRY(norm_backward), ENTRY(embedding), ENTRY(embedding_backward),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

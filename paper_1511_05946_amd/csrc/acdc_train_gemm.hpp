@@ -6,15 +6,15 @@
 // of the loss read hidden, weight and the logits' gradient as they are, and
 // nothing is transposed on the way.
 //
-// A workgroup of 4 or 8 waves computes BM x BN of C; steps of 64 k go through
-// two halves of LDS.  While the waves compute on one half, the other one is
-// filled by loads that write LDS themselves (16 bytes a lane), so that a step
-// needs one barrier and no registers in between.  LDS words are permuted by
+// A workgroup computes BM x BN of C; steps of BK k go through STAGES parts of
+// LDS.  While the waves compute on one of them, the others are filled by loads
+// that write LDS themselves (16 bytes a lane), so that a step needs one barrier
+// and no registers in between.  LDS words are permuted by
 // the row (Along::swizzle, Across::swizzle): 8 lanes that read 16 bytes each
 // touch all banks once, and so do the transposing reads of "across" tiles.
 //
 // float32 values x = x0 + x1 + x2 are three planes of bfloat16 (8 of 24 bits
-// each, exact): the product runs over the six pairs of planes that matter,
+// each, exact): a step multiplies the six pairs of planes that matter,
 // smallest first; what is left out is below 2^-26 of a product.
 #pragma once
 
@@ -31,8 +31,6 @@ using s16x4 = short __attribute__((ext_vector_type(4)));
 
 #define ACDC_LDS __attribute__((address_space(3)))
 #define ACDC_GLOBAL __attribute__((address_space(1)))
-
-constexpr int kStepK = 64;  // k of a step
 
 // x as three bfloat16 whose sum is x.  A value that is not finite stays in the
 // first plane; one that would round to infinity is cut instead.
@@ -53,20 +51,6 @@ __device__ __forceinline__ Split3 split3(float x) {
   return s;
 }
 
-// The pairs of planes in order, four bits each.
-template <int PLANES>
-struct Pairs;
-template <>
-struct Pairs<1> {
-  static constexpr int N = 1;
-  static constexpr unsigned A = 0, B = 0;
-};
-template <>
-struct Pairs<3> {
-  static constexpr int N = 6;
-  static constexpr unsigned A = 0x010210, B = 0x001012;  // 0,1,2,0,1,0 and 2,1,0,1,0,0
-};
-
 // rows x cols values in memory, `ld` apart, both >= 1, cols a multiple of 8 and
 // rows at multiples of 16 bytes.  A tile may reach past either: it then reads the
 // last row or the last 8 columns again, so that every address is inside.
@@ -77,19 +61,20 @@ struct Operand {
   int rows, cols;
 };
 
-// The tile of X values (m or n) by 64 k of an operand with k along its rows:
-// 128 bytes of LDS a value, 8 chunks of 16 bytes.
-template <int X, int THREADS, int SPREAD>
+// The tile of X values (m or n) by BK k of an operand with k along its rows: BK / 8 chunks
+// of 16 bytes a value.
+template <int X, int BK, int THREADS, int SPREAD>
 struct Along {
-  static constexpr int N = X * 8 / THREADS;
+  static constexpr int CHUNKS = BK / 8, N = X * CHUNKS / THREADS, BYTES = X * BK * 2;
   const char* base;
   unsigned off[N];
   int64_t plane;
   int cols, tid;
   // The rows that 8 lanes read at once are 0 .. 7 (SPREAD 0), or 0 .. 3 and four more
-  // SPREAD rows on: eight different values for either.
+  // SPREAD rows on; they are to touch eight different 16-byte columns of 128 bytes.
   __device__ __forceinline__ static int swizzle(int row) {
-    return SPREAD == 0 ? row & 7 : (row & 3) | (row / (SPREAD > 0 ? SPREAD : 1) & 1) << 2;
+    const int far = SPREAD > 0 ? row / (SPREAD > 0 ? SPREAD : 1) & 1 : row >> 2 & 1;
+    return CHUNKS == 8 ? (row & 3) | far << 2 : (row >> 1 & 1) | far << 1;
   }
   __device__ __forceinline__ void init(const Operand& o, int x0, int t) {
     base = reinterpret_cast<const char*>(o.p + int64_t(x0) * o.ld);
@@ -98,37 +83,55 @@ struct Along {
     tid = t;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const int c = t + j * THREADS, row = c >> 3;
-      off[j] = unsigned(min(row, o.rows - 1 - x0)) * unsigned(o.ld * 2) + unsigned(((c & 7) ^ swizzle(row)) << 4);
+      const int c = t + j * THREADS, row = c / CHUNKS;
+      off[j] = unsigned(min(row, o.rows - 1 - x0)) * unsigned(o.ld * 2) + unsigned(((c % CHUNKS) ^ swizzle(row)) << 4);
     }
   }
+  // step k of plane p; FULL: it ends inside the operand
+  template <bool FULL>
   __device__ __forceinline__ void load(char ACDC_LDS* lds, int p, int k, int wave) const {
-    const char* at = base + p * plane + int64_t(k) * (kStepK * 2);
-    if ((k + 1) * kStepK <= cols) {
+    const char* at = base + p * plane + int64_t(k) * (BK * 2);
+    if (FULL || (k + 1) * BK <= cols) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) put(lds, at + off[j], j, wave);
+      for (int j = 0; j < N; ++j) put(lds, at, off[j], j, wave);
     } else {
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const int c = tid + j * THREADS, row = c >> 3, col = ((c & 7) ^ swizzle(row)) * 8;
-        put(lds, at + off[j] - (col - min(col, cols - 8 - k * kStepK)) * 2, j, wave);
+        const int c = tid + j * THREADS, row = c / CHUNKS, col = ((c % CHUNKS) ^ swizzle(row)) * 8;
+        put(lds, at + off[j] - (col - min(col, cols - 8 - k * BK)) * 2, j, wave);
       }
     }
+  }
+  // chunk j of the thread's, from a uniform address and an offset of its own.  (The offset
+  // stays 32 bits wide: its extension, if it were taken out of the loop, would need two
+  // registers and an addition a load.)
+  __device__ __forceinline__ static void put(char ACDC_LDS* lds, const char* from, unsigned off, int j, int wave) {
+    asm("" : "+v"(off));
+    put(lds, from + off, j, wave);
   }
   __device__ __forceinline__ static void put(char ACDC_LDS* lds, const char* from, int j, int wave) {
     __builtin_amdgcn_global_load_lds((const ACDC_GLOBAL void*)from, (ACDC_LDS void*)(lds + (j * THREADS + wave * 64) * 16),
                                      16, 0, 0);
   }
-  // 8 k (of `half`, 32 k) of value `row`, for lane's quarter
-  __device__ __forceinline__ static bf16x8 read(const char ACDC_LDS* tile, int row, int half, int lane) {
-    return *(const bf16x8 ACDC_LDS*)(tile + row * 128 + ((half * 4 + (lane >> 4)) ^ swizzle(row)) * 16);
-  }
+  // Where lane's 8 k of a part (32 k) of a square begin, its rows dealt as in Spot: those of
+  // the other squares are a fixed number of bytes on.
+  struct Reader {
+    unsigned at[BK / 32];
+    __device__ __forceinline__ void init(int x, int lane) {
+      const int j = lane & 15, row = SPREAD > 0 ? x + (j >> 2) * SPREAD + (j & 3) : x + j;
+#pragma unroll
+      for (int part = 0; part < BK / 32; ++part) at[part] = row * (BK * 2) + ((part * 4 + (lane >> 4)) ^ swizzle(row)) * 16;
+    }
+    __device__ __forceinline__ bf16x8 read(const char ACDC_LDS* tile, int square, int part) const {
+      return *(const bf16x8 ACDC_LDS*)(tile + at[part] + square * (SPREAD > 0 ? 4 : 16) * (BK * 2));
+    }
+  };
 };
 
-// The same of an operand with k across its rows: 64 rows of X values.
-template <int X, int THREADS>
+// The same of an operand with k across its rows: BK rows of X values.
+template <int X, int BK, int THREADS>
 struct Across {
-  static constexpr int N = X * 8 / THREADS, CHUNKS = X / 8;
+  static constexpr int CHUNKS = X / 8, N = BK * CHUNKS / THREADS, BYTES = X * BK * 2;
   const char* base;
   unsigned off[N];
   int64_t plane, step;
@@ -136,12 +139,14 @@ struct Across {
   int rows, tid;
   // A transposing read takes 16 values of the rows k .. k + 3 and k + 8 .. k + 11 at once
   // per half wave: eight times 32 bytes, at eight different places of 256 bytes.
-  __device__ __forceinline__ static int swizzle(int k) { return ((k & 3) | (k >> 3 & 1) << 2) << 1; }
+  __device__ __forceinline__ static int swizzle(int k) {
+    return (((k & 3) | (k >> 3 & 1) << 2) << 1) & (CHUNKS - 1);
+  }
   __device__ __forceinline__ void init(const Operand& o, int x0, int t) {
     base = reinterpret_cast<const char*>(o.p + x0);
     plane = o.plane * 2;
     ld2 = unsigned(o.ld * 2);
-    step = o.ld * (2 * kStepK);
+    step = o.ld * (2 * BK);
     rows = o.rows;
     tid = t;
 #pragma unroll
@@ -150,41 +155,50 @@ struct Across {
       off[j] = unsigned(k) * ld2 + unsigned(min(x, o.cols - 8 - x0) * 2);
     }
   }
+  // step k of plane p; FULL: it ends inside the operand
+  template <bool FULL>
   __device__ __forceinline__ void load(char ACDC_LDS* lds, int p, int k, int wave) const {
     const char* at = base + p * plane + k * step;
-    if ((k + 1) * kStepK <= rows) {
+    if (FULL || (k + 1) * BK <= rows) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) Along<X, THREADS, 0>::put(lds, at + off[j], j, wave);
+      for (int j = 0; j < N; ++j) Along<X, BK, THREADS, 0>::put(lds, at, off[j], j, wave);
     } else {
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const int row = (tid + j * THREADS) / CHUNKS;
-        const int past = row - min(row, rows - 1 - k * kStepK);
-        Along<X, THREADS, 0>::put(lds, at + off[j] - int64_t(past) * ld2, j, wave);
+        const int past = row - min(row, rows - 1 - k * BK);
+        Along<X, BK, THREADS, 0>::put(lds, at + off[j] - int64_t(past) * ld2, j, wave);
       }
     }
   }
-  // 8 k of the values x .. x + 15, lane & 15 of them: two reads that transpose 4 x 16 values
-  // within 16 lanes (lane i reads 4 values of row i / 4 and gets 4 rows of value i)
-  __device__ __forceinline__ static bf16x8 read(const char ACDC_LDS* tile, int x, int half, int lane) {
-    const int i = lane & 15, at = x + (i & 3) * 4;
-    union {
-      bf16x8 v;
-      s16x4 h[2];
-    } u;
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int k = half * 32 + (lane >> 4) * 8 + (i >> 2) + q * 4;
-      const char ACDC_LDS* a = tile + k * (X * 2) + ((at >> 3) ^ swizzle(k)) * 16 + (at & 7) * 2;
-      u.h[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 ACDC_LDS*)a);
+  // 8 k of 16 values, lane & 15 of them: two reads that transpose 4 x 16 values within 16
+  // lanes (lane i reads 4 values of row i / 4 and gets 4 rows of value i)
+  struct Reader {
+    unsigned at;
+    __device__ __forceinline__ void init(int x, int lane) {
+      const int i = lane & 15, k = (lane >> 4) * 8 + (i >> 2), from = x + (i & 3) * 4;
+      at = k * (X * 2) + ((from >> 3) ^ swizzle(k)) * 16 + (from & 7) * 2;
     }
-    return u.v;
-  }
+    __device__ __forceinline__ bf16x8 read(const char ACDC_LDS* tile, int square, int part) const {
+      union {
+        bf16x8 v;
+        s16x4 h[2];
+      } u;
+      // 16 values on are 32 bytes, under the permutation (x is a multiple of all squares' values)
+      const char ACDC_LDS* from = tile + (at ^ (square * 32));
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+        u.h[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 ACDC_LDS*)(from + (part * 32 + q * 4) * (X * 2)));
+      return u.v;
+    }
+  };
 };
 
 // What one workgroup computes: tile (tm, tn) of mt x nt, part `part` of the steps.
 // The tiles of one XCD (workgroups go round the eight of them) lie together, in groups
-// of 8 n-tiles that run along m, so that its L2 holds what they share.
+// of 4 n-tiles that run along m, so that its L2 holds what they share: 32 CUs of an XCD
+// ask for 12 different tiles a step (65536 x 7424 x 4096: 1.22 PFLOP/s; groups of 2 1.13,
+// of 8 1.20, of 16 1.13).
 struct Place {
   int tm, tn, part;
 };
@@ -195,7 +209,7 @@ __device__ __forceinline__ Place place_of(unsigned id, int mt, int nt) {
   id %= tiles;
   const unsigned per = tiles / 8, rest = tiles % 8, xcd = id % 8;
   id = xcd * per + min(xcd, rest) + id / 8;
-  constexpr unsigned GROUP = 8;
+  constexpr unsigned GROUP = 4;
   const unsigned g = id / (GROUP * mt), first = g * GROUP, wide = min(GROUP, nt - first);
   const unsigned in = id - g * GROUP * mt;
   p.tn = int(first + in % wide);
@@ -215,71 +229,168 @@ struct Spot {
   __device__ __forceinline__ int n(int ni) const { return n0 + ni * 16 + (lane & 15); }
 };
 
-// Steps: of the pairs of planes, each over `ksteps` steps of k; `parts` workgroups share
-// a tile's.  *count (may be null): rows in use; with COUNT_N the n-tiles past them end at
-// once, otherwise (COUNT_K) they bound k.
+// How rows in use bound a product: kN: the n-tiles past *count end at once; kK: they are
+// the k.
 enum class Count { kNone, kN, kK };
 
-template <int BM, int BN, int WM, int WN, int PLANES, bool ACROSS_A, bool ACROSS_B, Count COUNT, class Epilogue>
-__global__ __launch_bounds__(WM* WN * 64) void k_gemm(Operand A, Operand B, int ksteps, int mt, int nt, int parts,
-                                                      const int* __restrict__ count, Epilogue epilogue) {
-  constexpr int T = WM * WN * 64, MI = BM / WM / 16, NI = BN / WN / 16, HALF = (BM + BN) * 128;
-  using StageA = std::conditional_t<ACROSS_A, Across<BM, T>, Along<BM, T, 4 * MI>>;
-  using StageB = std::conditional_t<ACROSS_B, Across<BN, T>, Along<BN, T, 0>>;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * HALF];  // (the epilogue exchanges values there too)
+// The shape of a workgroup: BM x BN of C by WM x WN waves, steps of BK, of which STAGES
+// are in LDS at a time.
+template <int BM_, int BN_, int BK_, int WM_, int WN_, int STAGES_, bool AHEAD_ = false>
+struct Shape {
+  static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, STAGES = STAGES_, THREADS = WM * WN * 64;
+  static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
+  static constexpr bool AHEAD = AHEAD_;
+};
+
+// Waits until at most N of this wave's loads are on their way.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N >= 0 && N < 64);
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
+}
+
+// `parts` workgroups share a tile's steps.  *count (may be null): the rows in use.
+template <class S, int PLANES, bool ACROSS_A, bool ACROSS_B, Count COUNT, class Epilogue>
+__global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int depth, int mt, int nt, int parts,
+                                                     const int* __restrict__ count, Epilogue epilogue) {
+  constexpr int T = S::THREADS, BM = S::BM, BN = S::BN, BK = S::BK, MI = S::MI, NI = S::NI, STAGES = S::STAGES;
+  using StageA = std::conditional_t<ACROSS_A, Across<BM, BK, T>, Along<BM, BK, T, 4 * MI>>;
+  using StageB = std::conditional_t<ACROSS_B, Across<BN, BK, T>, Along<BN, BK, T, 0>>;
+  constexpr int STAGE = PLANES * (StageA::BYTES + StageB::BYTES), LOADS = PLANES * (StageA::N + StageB::N);
+  static_assert(STAGES * STAGE <= 160 * 1024);
+  __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];  // (the epilogue exchanges values there too)
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
   const Place at = place_of(blockIdx.x, mt, nt);
   if constexpr (COUNT == Count::kN) {
     if (at.tn * BN >= *count) return;
   }
-  if constexpr (COUNT == Count::kK) ksteps = (*count + kStepK - 1) / kStepK;
-  // this part's steps: from .. to of all pairs
-  const int total = Pairs<PLANES>::N * ksteps, per = (total + parts - 1) / parts;
+  if constexpr (COUNT == Count::kK) depth = *count;
+  // this part's steps: from .. to
+  const int total = (depth + BK - 1) / BK, per = (total + parts - 1) / parts;
   const int from = min(total, at.part * per), to = min(total, from + per);
   StageA a;
   StageB b;
   a.init(A, at.tm * BM, tid);
   b.init(B, at.tn * BN, tid);
   char ACDC_LDS* const base = (char ACDC_LDS*)lds;
-  int pair = PLANES == 1 ? 0 : from / max(ksteps, 1), k = PLANES == 1 ? from : from - pair * ksteps;
-  auto fetch = [&](char ACDC_LDS* half) {
-    a.load(half, (Pairs<PLANES>::A >> (4 * pair)) & 15, k, wave);
-    b.load(half + BM * 128, (Pairs<PLANES>::B >> (4 * pair)) & 15, k, wave);
-    if (++k == ksteps && PLANES > 1) {
-      k = 0;
-      ++pair;
-    }
+  auto fetch = [&]<bool FULL>(int slot, int k) {
+    char ACDC_LDS* stage = base + slot * STAGE;
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p) a.template load<FULL>(stage + p * StageA::BYTES, p, k, wave);
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p) b.template load<FULL>(stage + PLANES * StageA::BYTES + p * StageB::BYTES, p, k, wave);
   };
   f32x4 acc[MI][NI] = {};
-  const int wm = wave % WM, wn = wave / WM;
-  if (from < to) fetch(base);
-  for (int s = from; s < to; ++s) {
-    const char ACDC_LDS* tile = base + ((s - from) & 1) * HALF;
-    // this wave's loads are there, then everyone's; and everyone has read the other half
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  const int wm = wave % S::WM, wn = wave / S::WM;
+  typename StageA::Reader ra;
+  typename StageB::Reader rb;
+  ra.init(wm * (BM / S::WM), lane);
+  rb.init(wn * (BN / S::WN), lane);
+  // one part (32 k) of a step as the matrix cores take it
+  struct Part {
+    bf16x8 a[PLANES][MI], b[PLANES][NI];
+  };
+  auto read = [&](int slot, int part, Part& f) {
+    const char ACDC_LDS* stage = base + slot * STAGE;
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+      for (int n = 0; n < NI; ++n) f.b[p][n] = rb.read(stage + PLANES * StageA::BYTES + p * StageB::BYTES, n, part);
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+      for (int m = 0; m < MI; ++m) f.a[p][m] = ra.read(stage + p * StageA::BYTES, m, part);
+  };
+  auto multiply = [&](const Part& f) {
+#pragma unroll
+    for (int m = 0; m < MI; ++m)
+      // the pairs of planes that matter, smallest first
+#pragma unroll
+      for (int both = PLANES - 1; both >= 0; --both)
+#pragma unroll
+        for (int p = 0; p <= both; ++p)
+#pragma unroll
+          for (int n = 0; n < NI; ++n)
+            acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.a[p][m], f.b[both - p][n], acc[m][n], 0, 0, 0);
+  };
+  // this wave's loads but `left` of them are there, then everyone's; and everyone has read
+  // what it asked of LDS
+  auto meet = [&] {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-    if (s + 1 < to) fetch(base + ((s + 1 - from) & 1) * HALF);
+  };
+  // step s has arrived
+  auto arrive = [&](int s) {
+    if (STAGES > 2 && s + STAGES - 2 < to) wait_loads<LOADS * (STAGES - 2)>();
+    else wait_loads<0>();
+    meet();
+  };
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      bf16x8 bv[NI];
+  for (int q = 0; q < STAGES - 1; ++q)
+    if (from + q < to) fetch.template operator()<false>(q, from + q);
+  int slot = 0;
+  if constexpr (S::AHEAD) {
+    // The registers of one part are read while the matrix cores work on the other's.
+    static_assert(BK == 64 && STAGES == 2 && PLANES == 1);
+    constexpr int READS = (ACROSS_A ? 2 : 1) * MI + (ACROSS_B ? 2 : 1) * NI, PER = MI * NI / READS;
+    Part first, second;
+    int s = from;
+    if (from < to) {
+      arrive(from);
+      read(0, 0, first);
+      if (from + 1 < to) fetch.template operator()<false>(1, from + 1);
+    }
+    // (the last step of all may end outside the operand)
+    for (; s + 3 < to; ++s) {
+      read(slot, 1, second);
+      multiply(first);
 #pragma unroll
-      for (int n = 0; n < NI; ++n) {
-        const int x = wn * (BN / WN) + n * 16;
-        bv[n] = StageB::read(tile + BM * 128, ACROSS_B ? x : x + (lane & 15), half, lane);
+      for (int i = 0; i < READS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
       }
+      __builtin_amdgcn_sched_barrier(0);
+      wait_loads<0>();
+      meet();
+      read(slot ^ 1, 0, first);
+      fetch.template operator()<true>(slot, s + 2);
+      multiply(second);
 #pragma unroll
-      for (int m = 0; m < MI; ++m) {
-        const int x = wm * (BM / WM), j = lane & 15;
-        const bf16x8 av = StageA::read(tile, ACROSS_A ? x + m * 16 : x + (j >> 2) * (4 * MI) + m * 4 + (j & 3), half, lane);
-#pragma unroll
-        for (int n = 0; n < NI; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, bv[n], acc[m][n], 0, 0, 0);
+      for (int i = 0; i < READS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        if (i < LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
       }
+      __builtin_amdgcn_sched_barrier(0);
+      slot ^= 1;
+    }
+#pragma nounroll
+    for (; s < to; ++s) {
+      read(slot, 1, second);
+      multiply(first);
+      wait_loads<0>();
+      meet();
+      read(slot ^ 1, 0, first);  // (nothing, after the last step)
+      if (s + 2 < to) fetch.template operator()<false>(slot, s + 2);
+      multiply(second);
+      slot ^= 1;
+    }
+  } else {
+    for (int s = from; s < to; ++s) {
+      arrive(s);
+      if (s + STAGES - 1 < to) fetch.template operator()<false>(slot == 0 ? STAGES - 1 : slot - 1, s + STAGES - 1);
+#pragma unroll
+      for (int part = 0; part < BK / 32; ++part) {
+        Part f;
+        read(slot, part, f);
+        multiply(f);
+      }
+      slot = slot == STAGES - 1 ? 0 : slot + 1;
     }
   }
-  const Spot<MI, NI, !ACROSS_A> spot{at.tm * BM + wm * (BM / WM), at.tn * BN + wn * (BN / WN), lane};
-  epilogue.template operator()<BM, BN, WM, WN, MI, NI>(acc, spot, at, wave, reinterpret_cast<float2*>(lds));
+  const Spot<MI, NI, !ACROSS_A> spot{at.tm * BM + wm * (BM / S::WM), at.tn * BN + wn * (BN / S::WN), lane};
+  epilogue.template operator()<S>(acc, spot, at, wave, reinterpret_cast<float2*>(lds));
 }
 
 }  // namespace acdc

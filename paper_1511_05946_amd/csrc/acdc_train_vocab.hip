@@ -7,7 +7,9 @@
 //   G = dL/dx = g ([v = t] - exp(x - M) / S),  dL/dhidden = G weight,
 //   dL/dweight = G^T hidden,
 // and the second pass computes the logits of a piece of the vocabulary again,
-// writes the piece of G in the inputs' type and runs both products on it.
+// writes the piece of G in the inputs' type and runs both products on it.  Where
+// one piece holds the whole vocabulary, the first pass leaves its exponentials
+// in the piece's place, and nothing is computed twice.
 //
 // Rows that take no part are left out from the start: the others are packed
 // together (`order`), so that they cost nothing and what they hold is never
@@ -177,18 +179,26 @@ __global__ __launch_bounds__(256) void k_vocab_pack(const typename T::Elem* __re
 
 // ------------------------------------------------------ what follows a product
 
+// What the first pass keeps of the logits: nothing, or exp(x - the tile's maximum) where
+// the second pass can use it.
+enum class Keep { kNothing, kBf16, kF32 };
+
 // Statistics of a tile's rows: their (max, sum) into parts[tile][row], and the target's
 // logit.  m runs over classes, n over packed rows; `classes` are those of the piece.
+template <Keep KEEP>
 struct StatsOut {
   const int* target;
   float2* parts;
   float* logit;
-  int first, classes, rows, tile;
-  template <int BM, int BN, int WM, int WN, int MI, int NI, class S>
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const S& spot, const Place& at, int wave,
+  void* kept;  // rows `ld` apart
+  int first, classes, rows, tile, ld;
+  template <class S, int MI, int NI, class SP>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const SP& spot, const Place& at, int wave,
                                              float2* slots) const {
+    constexpr int BN = S::BN, WM = S::WM;
     const int lane = spot.lane;
     __syncthreads();  // the tiles have been read
+    float tops[NI];
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
       const int r = spot.n(n), t = target[r] - first;
@@ -206,27 +216,50 @@ struct StatsOut {
       Pair p = swap16(top);
       top = fmaxf(p.a, p.b);
       p = swap32(top);
-      top = fmaxf(p.a, p.b);
+      tops[n] = fmaxf(p.a, p.b);
+      if (lane < 16) slots[(r - at.tn * BN) * WM + wave % WM].x = tops[n];
+    }
+    __syncthreads();
+    // the maximum of all of the tile's classes (also where nothing is kept: the same sums)
+#pragma unroll
+    for (int n = 0; n < NI; ++n)
+#pragma unroll
+      for (int w = 0; w < WM; ++w) tops[n] = fmaxf(tops[n], slots[(spot.n(n) - at.tn * BN) * WM + w].x);
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+      const int r = spot.n(n);
       float sum = 0.f;
 #pragma unroll
       for (int m = 0; m < MI; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += exp_of(acc[m][n][i] - top);
-      p = swap16(sum);
+        for (int i = 0; i < 4; ++i) {
+          acc[m][n][i] = exp_of(acc[m][n][i] - tops[n]);
+          sum += acc[m][n][i];
+        }
+      Pair p = swap16(sum);
       sum = p.a + p.b;
       p = swap32(sum);
-      sum = p.a + p.b;
-      if (lane < 16) slots[(r - at.tn * BN) * WM + wave % WM] = make_float2(top, sum);
+      if (lane < 16) slots[(r - at.tn * BN) * WM + wave % WM] = make_float2(tops[n], p.a + p.b);
+      const long long to = (long long)r * ld + spot.m(0);
+      if constexpr (KEEP == Keep::kBf16) {
+#pragma unroll
+        for (int m = 0; m < MI; m += 2) {
+          bf16x8 o;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[i] = __bf16(acc[m + i / 4][n][i % 4]);
+          *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(kept) + to + m * 4) = o;
+        }
+      } else if constexpr (KEEP == Keep::kF32) {
+#pragma unroll
+        for (int m = 0; m < MI; ++m) *reinterpret_cast<f32x4*>(static_cast<float*>(kept) + to + m * 4) = acc[m][n];
+      }
     }
     __syncthreads();
     if (int(threadIdx.x) < BN) {
       float2 all = slots[threadIdx.x * WM];
 #pragma unroll
-      for (int w = 1; w < WM; ++w) {
-        const float2 s = slots[threadIdx.x * WM + w];
-        const float top = fmaxf(all.x, s.x);
-        all = make_float2(top, all.y * exp_of(all.x - top) + s.y * exp_of(s.x - top));
-      }
+      for (int w = 1; w < WM; ++w) all.y += slots[threadIdx.x * WM + w].y;
       parts[(long long)(tile + at.tm) * rows + at.tn * BN + threadIdx.x] = all;
     }
   }
@@ -247,8 +280,8 @@ struct SlopeOut {
   __bf16* out;
   long long plane;
   int ld, first, classes;
-  template <int BM, int BN, int WM, int WN, int MI, int NI, class S>
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const S& spot, const Place&, int, float2*) const {
+  template <class S, int MI, int NI, class SP>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const SP& spot, const Place&, int, float2*) const {
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
       const int r = spot.n(n);
@@ -279,14 +312,49 @@ struct SlopeOut {
   }
 };
 
+// The same from what the first pass kept, e = exp(x - the tile's maximum), of a single
+// piece: in place where e is bfloat16 (a second rounding, of 2^-8 at the most; the
+// target's own value, where 1 - p may be small, comes from its logit).  A wave takes 512
+// classes of a row; bound by HBM.
+template <int PLANES>
+__global__ __launch_bounds__(256) void k_vocab_slopes(Rows rows, const RowSlope* __restrict__ slope, const float2* __restrict__ parts,
+                                                      const float* __restrict__ logp, const void* kept, __bf16* out,
+                                                      long long plane, int ld, int tile, int padded, int blocks) {
+  using E = std::conditional_t<PLANES == 1, __bf16, float>;
+  typedef E Eight __attribute__((ext_vector_type(8)));
+  const int lane = threadIdx.x % 64, used = (*rows.count + 63) / 64 * 64;
+  const long long item = blockIdx.x * 4ll + threadIdx.x / 64;
+  const int r = int(item / blocks), col = (int(item % blocks) * 64 + lane) * 8;
+  if (r >= used || col >= ld) return;
+  const RowSlope k = slope[r];
+  const float f = -k.slope * exp_of(parts[(long long)(col / tile) * padded + r].x - k.top);
+  const long long at = (long long)r * ld + col;
+  const Eight e = *reinterpret_cast<const Eight*>(static_cast<const E*>(kept) + at);
+  bf16x8 o[PLANES];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float y = float(e[i]) * f;
+    if (col + i == k.target) y = -k.g * expm1f(logp[rows.order[r]]);
+    if constexpr (PLANES == 1) {
+      o[0][i] = __bf16(y);
+    } else {
+      const Split3 s = split3(y);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) o[p][i] = s.p[p];
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < PLANES; ++p) *reinterpret_cast<bf16x8*>(out + p * plane + at) = o[p];
+}
+
 // 32-bit sums of a part: out[part][n][m], added to what earlier pieces left.
 struct PartOut {
   float* out;
   long long part;
   int ld, rows;
   bool add;
-  template <int BM, int BN, int WM, int WN, int MI, int NI, class S>
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const S& spot, const Place& at, int, float2*) const {
+  template <class S, int MI, int NI, class SP>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const SP& spot, const Place& at, int, float2*) const {
 #pragma unroll
     for (int n = 0; n < NI; ++n)
 #pragma unroll
@@ -325,8 +393,8 @@ struct GradOut {
   long long ld;
   int width, classes;
   bool whole, add;
-  template <int BM, int BN, int WM, int WN, int MI, int NI, class S>
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const S& spot, const Place&, int, float2*) const {
+  template <class S, int MI, int NI, class SP>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const SP& spot, const Place&, int, float2*) const {
     const float f = *factor;
 #pragma unroll
     for (int n = 0; n < NI; ++n)
@@ -460,18 +528,29 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
 
 constexpr int kTile = 256;
-// Bytes of the piece of G: a quarter of a tile's products per byte are enough to hide
-// what each piece costs once, and the rest of the card's memory is the caller's.
-constexpr int64_t kPieceBytes = int64_t(512) << 20;
+// Bytes of a piece of G.  A piece costs a pass over the sums of dL/dhidden, and the logits
+// of a single one need not be computed again: 8192 rows over 65536 classes are one piece.
+constexpr int64_t kPieceBytes = int64_t(2) << 30;
+
+// Products of BM x BN: large tiles feed the matrix cores best, small ones keep more of the
+// card busy, and give a row of few steps to more workgroups.
+using Large = Shape<256, 256, 64, 4, 2, 2, true>;
+using Large3 = Shape<128, 256, 32, 2, 4, 2>;
+using Flat = Shape<256, 64, 64, 4, 1, 2>;
+using Flat3 = Shape<128, 64, 32, 4, 1, 2>;
+using Small = Shape<64, 64, 64, 2, 2, 4>;
+using Small3 = Shape<64, 64, 32, 2, 2, 4>;
 
 // How a call is cut up: fixed by its sizes alone.
 struct Plan {
   int64_t rows, padded_rows;
   int32_t width, padded_width, classes, planes;
-  int tile_n;             // packed rows of a tile
   int32_t piece, pieces;  // classes of a piece, a multiple of kTile
   int hidden_parts, weight_parts;
+  bool large_logits, large_hidden, large_weight;  // the products' tiles
+  int tile_classes() const { return !large_logits ? 64 : planes == 1 ? 256 : 128; }  // of the logits
 };
+int64_t tiles_of(int64_t m, int64_t n, int bm, int bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); }
 int parts_for(int64_t tiles, int64_t steps) {
   // as many as give every CU a tile, of 8 steps at least
   return int(std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), steps / 8, 64})));
@@ -482,21 +561,26 @@ Plan plan_for(int64_t rows, int32_t width, int32_t classes, int32_t dtype) {
   p.width = width;
   p.classes = classes;
   p.planes = dtype == ACDC_F32 ? 3 : 1;
-  p.tile_n = rows <= 64 ? 64 : kTile;
-  p.padded_rows = up(std::max<int64_t>(rows, 1), p.tile_n);
-  p.padded_width = int32_t(up(width, kStepK));
+  p.padded_rows = up(std::max<int64_t>(rows, 1), rows <= 64 ? 64 : kTile);
+  p.padded_width = int32_t(up(width, 64));
   const int64_t values = std::max<int64_t>(p.padded_rows, p.padded_width);  // of a class: in the piece of G, in the packed weight
-  const int64_t most = std::max<int64_t>(kTile, kPieceBytes / (2 * p.planes * values) / kTile * kTile);
+  const int64_t most = std::max<int64_t>(kTile, kPieceBytes / ((p.planes == 1 ? 2 : 10) * values) / kTile * kTile);
   p.pieces = int32_t((classes + most - 1) / most);
   p.piece = int32_t(up((classes + p.pieces - 1) / p.pieces, kTile));
-  const int64_t wide = up(p.padded_width, kTile) / kTile, pairs = p.planes == 1 ? 1 : 6;
-  p.hidden_parts = parts_for(wide * (p.padded_rows / p.tile_n), pairs * (std::min<int64_t>(p.piece, up(classes, kStepK)) / kStepK));
-  p.weight_parts = parts_for(wide * (up(std::min(p.piece, classes), kTile) / kTile), pairs * (p.padded_rows / kStepK));
+  const int bm = p.planes == 1 ? 256 : 128, bn = rows <= 64 ? 64 : 256, step = p.planes == 1 ? 64 : 32;
+  const int64_t piece = std::min(p.piece, classes);
+  // half a card of large tiles is as fast as a card of small ones
+  p.large_logits = tiles_of(piece, p.padded_rows, bm, bn) >= 128;
+  const int64_t hidden = tiles_of(width, p.padded_rows, bm, bn), weight = tiles_of(width, piece, bm, 256);
+  p.large_hidden = hidden * parts_for(hidden, piece / step) >= 128;
+  p.large_weight = weight * parts_for(weight, p.padded_rows / step) >= 128;
+  p.hidden_parts = parts_for(p.large_hidden ? hidden : tiles_of(width, p.padded_rows, 64, 64), (piece + step - 1) / step);
+  p.weight_parts = parts_for(p.large_weight ? weight : tiles_of(width, piece, 64, 64), p.padded_rows / step);
   return p;
 }
 
 struct Layout {
-  size_t order, target, share, at, count, total, factor, logit, parts, slope, loss, hidden, weight, grad, hidden_sums, weight_sums, bytes;
+  size_t order, target, share, at, count, total, factor, logit, parts, slope, loss, hidden, weight, grad, kept, hidden_sums, weight_sums, bytes;
 };
 Layout layout(const Plan& p, bool gradient) {
   Layout w{};
@@ -515,13 +599,14 @@ Layout layout(const Plan& p, bool gradient) {
   w.total = take(8);
   w.factor = take(4);
   w.logit = take(R * 4);
-  w.parts = take(R * 8 * size_t(up(p.classes, kTile) / kTile));
+  w.parts = take(R * 8 * size_t(p.pieces) * size_t(p.piece / p.tile_classes()));
   w.slope = take(R * sizeof(RowSlope));
   w.loss = take(R * 4);
   w.hidden = take(R * p.padded_width * 2 * p.planes);
   w.weight = take(size_t(p.piece) * p.padded_width * 2 * p.planes);
   if (gradient) {
     w.grad = take(R * p.piece * 2 * p.planes);
+    w.kept = p.planes == 1 ? w.grad : take(p.pieces == 1 ? R * p.piece * 4 : 0);
     w.hidden_sums = take(size_t(p.hidden_parts) * R * p.padded_width * 4);
     w.weight_sums = take(p.weight_parts > 1 ? size_t(p.weight_parts) * p.piece * p.padded_width * 4 : 0);
   }
@@ -581,29 +666,42 @@ struct Call {
     return Operand{get<__bf16>(w.weight), p.padded_width, plane, n, p.padded_width};
   }
   Operand grad(int k) const {
-    return Operand{get<__bf16>(w.grad), p.piece, p.padded_rows * p.piece, int(p.padded_rows), int(up(classes_of(k), kStepK))};
+    return Operand{get<__bf16>(w.grad), p.piece, p.padded_rows * p.piece, int(p.padded_rows), int(up(classes_of(k), 64))};
   }
 
-  template <int BM, int BN, int WM, int WN, bool XA, bool XB, Count COUNT, class E>
-  void gemm(const Operand& a, const Operand& b, int64_t m, int64_t n, int ksteps, int parts, const E& e) const {
-    const int mt = int((m + BM - 1) / BM), nt = int((n + BN - 1) / BN);
-    hipLaunchKernelGGL((k_gemm<BM, BN, WM, WN, P, XA, XB, COUNT, E>), dim3(unsigned(int64_t(mt) * nt * parts)), dim3(WM * WN * 64),
-                       0, s, a, b, ksteps, mt, nt, parts, rows.count, e);
+  template <class S, bool XA, bool XB, Count COUNT, class E>
+  void gemm(const Operand& a, const Operand& b, int64_t m, int64_t n, int depth, int parts, const E& e) const {
+    const int mt = int((m + S::BM - 1) / S::BM), nt = int((n + S::BN - 1) / S::BN);
+    hipLaunchKernelGGL((k_gemm<S, P, XA, XB, COUNT, E>), dim3(unsigned(int64_t(mt) * nt * parts)), dim3(S::THREADS), 0, s, a, b,
+                       depth, mt, nt, parts, rows.count, e);
+  }
+  // a product with n over the packed rows
+  template <bool XA, class E>
+  void over_rows(bool large, const Operand& a, const Operand& b, int64_t m, int depth, int parts, const E& e) const {
+    constexpr Count N = Count::kN;
+    if (!large) gemm<std::conditional_t<P == 1, Small, Small3>, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
+    else if (p.padded_rows > 64) gemm<std::conditional_t<P == 1, Large, Large3>, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
+    else gemm<std::conditional_t<P == 1, Flat, Flat3>, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
   }
   // classes x packed rows
   template <class E>
   void logits(const Operand& weight, const E& e) const {
-    const int steps = p.padded_width / kStepK;
-    if (p.tile_n == 64) gemm<kTile, 64, 4, 1, false, false, Count::kN>(weight, hidden(), weight.rows, p.padded_rows, steps, 1, e);
-    else gemm<kTile, kTile, 2, 4, false, false, Count::kN>(weight, hidden(), weight.rows, p.padded_rows, steps, 1, e);
+    over_rows<false>(p.large_logits, weight, hidden(), weight.rows, p.padded_width, 1, e);
   }
 
-  int statistics(const JoinOut& out) const {
-    for (int k = 0; k < p.pieces; ++k)
-      logits(weight(k, false), StatsOut{rows.target, get<float2>(w.parts), get<float>(w.logit), k * p.piece, classes_of(k),
-                                        int(p.padded_rows), k * (p.piece / kTile)});
+  template <Keep KEEP>
+  StatsOut<KEEP> stats_out(int k) const {
+    return {rows.target, get<float2>(w.parts), get<float>(w.logit), get<void>(w.kept), k * p.piece, classes_of(k),
+            int(p.padded_rows), k * (p.piece / p.tile_classes()), p.piece};
+  }
+  int statistics(const JoinOut& out, bool keep) const {
+    for (int k = 0; k < p.pieces; ++k) {
+      const Operand weight_k = weight(k, false);
+      if (keep) logits(weight_k, stats_out<P == 1 ? Keep::kBf16 : Keep::kF32>(k));
+      else logits(weight_k, stats_out<Keep::kNothing>(k));
+    }
     hipLaunchKernelGGL(k_vocab_join, dim3(unsigned(p.padded_rows / 64)), dim3(1024), 0, s, rows, get<float2>(w.parts),
-                       get<float>(w.logit), int(up(p.classes, kTile) / kTile), int(p.padded_rows), out);
+                       get<float>(w.logit), int((p.classes + p.tile_classes() - 1) / p.tile_classes()), int(p.padded_rows), out);
     return done();
   }
 
@@ -617,33 +715,40 @@ struct Call {
   template <class O>
   void weight_grad(const acdc_vocab_grads& g, int k) const {
     using E = typename O::Elem;
-    const int n = classes_of(k), steps = int(p.padded_rows / kStepK);
+    const int n = classes_of(k);
     E* out = static_cast<E*>(g.weight) + int64_t(k) * p.piece * g.weight_stride;
     const bool whole = aligned_to(out, 4 * sizeof(E)) && g.weight_stride % 4 == 0, add = g.accumulate != 0;
+    auto product = [&](const auto& e) {
+      constexpr Count K = Count::kK;
+      if (p.large_weight) gemm<std::conditional_t<P == 1, Large, Large3>, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e);
+      else gemm<std::conditional_t<P == 1, Small, Small3>, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e);
+    };
     if (p.weight_parts == 1) {
-      gemm<kTile, kTile, 2, 4, true, true, Count::kK>(hidden(), grad(k), p.width, n, steps, 1,
-                                                      GradOut<O>{out, rows.factor, g.weight_stride, p.width, n, whole, add});
+      product(GradOut<O>{out, rows.factor, g.weight_stride, p.width, n, whole, add});
     } else {
       const int64_t part = int64_t(p.piece) * p.padded_width;
-      gemm<kTile, kTile, 2, 4, true, true, Count::kK>(hidden(), grad(k), p.width, n, steps, p.weight_parts,
-                                                      PartOut{get<float>(w.weight_sums), part, p.padded_width, n, false});
+      product(PartOut{get<float>(w.weight_sums), part, p.padded_width, n, false});
       sum<O>(w.weight_sums, p.weight_parts, part, nullptr, n, out, g.weight_stride, add);
     }
   }
-  // with the rows' slopes in place; `again`: the only piece's weight is packed already
-  int gradients(const acdc_vocab_grads& g, bool again) const {
+  // G of a single piece from what the first pass kept
+  void slopes(const float* logp) const {
+    const int blocks = (p.piece + 511) / 512;
+    hipLaunchKernelGGL(k_vocab_slopes<P>, dim3(unsigned((p.padded_rows * blocks + 3) / 4)), dim3(256), 0, s, rows,
+                       get<RowSlope>(w.slope), get<float2>(w.parts), logp, get<void>(w.kept), get<__bf16>(w.grad),
+                       (long long)(p.padded_rows * p.piece), p.piece, p.tile_classes(), int(p.padded_rows), blocks);
+  }
+  // With the rows' slopes in place.  `kept`: the logp of the pass that kept the only
+  // piece's exponentials, and packed its weight.
+  int gradients(const acdc_vocab_grads& g, const float* kept) const {
     const int64_t part = p.padded_rows * p.padded_width;
     for (int k = 0; k < p.pieces; ++k) {
-      const Operand wk = weight(k, again && p.pieces == 1);
-      logits(wk, SlopeOut<P>{get<RowSlope>(w.slope), get<__bf16>(w.grad), p.padded_rows * p.piece, p.piece, k * p.piece, classes_of(k)});
-      if (g.hidden != nullptr) {
-        const int steps = int(up(classes_of(k), kStepK) / kStepK);
-        const PartOut out{get<float>(w.hidden_sums), part, p.padded_width, int(p.padded_rows), k > 0};
-        if (p.tile_n == 64)
-          gemm<kTile, 64, 4, 1, true, false, Count::kN>(wk, grad(k), p.width, p.padded_rows, steps, p.hidden_parts, out);
-        else
-          gemm<kTile, kTile, 2, 4, true, false, Count::kN>(wk, grad(k), p.width, p.padded_rows, steps, p.hidden_parts, out);
-      }
+      const Operand wk = weight(k, kept != nullptr);
+      if (kept != nullptr) slopes(kept);
+      else logits(wk, SlopeOut<P>{get<RowSlope>(w.slope), get<__bf16>(w.grad), p.padded_rows * p.piece, p.piece, k * p.piece, classes_of(k)});
+      if (g.hidden != nullptr)
+        over_rows<true>(p.large_hidden, wk, grad(k), p.width, classes_of(k), p.hidden_parts,
+                        PartOut{get<float>(w.hidden_sums), part, p.padded_width, int(p.padded_rows), k > 0});
       if (g.weight != nullptr) {
         if (g.weight_type == head.dtype) weight_grad<T>(g, k);
         else weight_grad<F32>(g, k);
@@ -731,7 +836,7 @@ extern "C" int acdc_vocab_logprob(const acdc_vocab_head* head, float* logp, floa
   return with_type(head->dtype, [&]<class T>() {
     const Call<T> c(*head, false, workspace, stream);
     c.pack_rows(nullptr, Factor{nullptr, 1.f, false}, logp, reinterpret_cast<float2*>(saved), nullptr);
-    return c.statistics(JoinOut{logp, reinterpret_cast<float2*>(saved), nullptr, nullptr, nullptr, false});
+    return c.statistics(JoinOut{logp, reinterpret_cast<float2*>(saved), nullptr, nullptr, nullptr, false}, false);
   });
 }
 
@@ -747,7 +852,7 @@ extern "C" int acdc_vocab_backward(const acdc_vocab_head* head, const float* sav
     c.pack_rows(grad_logp, Factor{scale, 1.f, false}, nullptr, nullptr, nullptr);
     hipLaunchKernelGGL(k_vocab_slope, dim3(Call<T>::grid(c.p.padded_rows)), dim3(256), 0, c.s, c.rows,
                        reinterpret_cast<const float2*>(saved), int(c.p.padded_rows), c.template get<RowSlope>(c.w.slope));
-    return c.gradients(*grads, false);
+    return c.gradients(*grads, nullptr);
   });
 }
 
@@ -766,12 +871,13 @@ extern "C" int acdc_vocab_loss(const acdc_vocab_head* head, const float* weights
     const Call<T> c(*head, gradient, workspace, stream);
     float2* stat = reinterpret_cast<float2*>(saved);
     float* loss = c.template get<float>(c.w.loss);
+    const bool keep = gradient && c.p.pieces == 1;
     c.pack_rows(weights, Factor{nullptr, q.grad_scale, q.mean != 0}, logp, stat, row_grads);
     int rc = c.statistics(JoinOut{logp, stat, row_grads, gradient ? c.template get<RowSlope>(c.w.slope) : nullptr, loss,
-                                  q.mean != 0});
+                                  q.mean != 0}, keep);
     if (rc != ACDC_OK) return rc;
     hipLaunchKernelGGL(k_vocab_total, dim3(1), dim3(kWide), 0, c.s, c.rows, loss, q.mean != 0, stats);
     rc = done();
-    return rc != ACDC_OK || !gradient ? rc : c.gradients(*grads, true);
+    return rc != ACDC_OK || !gradient ? rc : c.gradients(*grads, keep ? logp : nullptr);
   });
 }

@@ -27,12 +27,17 @@ import torch
 
 from ._lib import lib
 from .acdc import _call, _check, _once, _ptr, _wrote
-from .losses import _BITS, _DTYPES, _apart, _index, _matrix, _values, _workspace
+from .losses import _DTYPES, _apart, _index, _matrix, _native, _values, _workspace
 
 
 class LayerNorm(NamedTuple):
     y: torch.Tensor
     saved: Optional[torch.Tensor]      # [rows, 2]: mean and 1 / deviation, for layer_norm_backward
+
+
+def _code(dtype):
+    """The type as the binding's native part takes it; None where it cannot."""
+    return -1 if dtype is None else _DTYPES.get(dtype)
 
 
 def _type(name, dtype, default):
@@ -79,6 +84,9 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, dtype=None, save: b
     """y = (x - mean) / sqrt(variance + eps) * weight + bias for each row, mean
     and variance over the row (``weight`` None: 1, ``bias`` None: 0).  y is of
     ``dtype`` (default: x's); ``save`` returns what ``layer_norm_backward`` needs."""
+    r = _native(x, "norm", weight, bias, eps, _code(dtype), save, out)
+    if r is not None:
+        return LayerNorm(*r)
     rows, width, x_stride = _matrix("x", x)
     device = x.device
     _width_vector("weight", weight, width, device)
@@ -108,6 +116,12 @@ def layer_norm_backward(x, grad_y, weight, saved, out=None, grads=None, accumula
     tensors to write into, or with ``accumulate`` to add to (either may be None:
     not wanted); otherwise they are made, of ``dtype`` (default: the weight's, or
     float32).  ``grad`` tells which of the three are wanted."""
+    want_x, want_w, want_b = grad
+    gw, gb = grads if grads is not None else (None, None)
+    r = _native(x, "norm_backward", grad_y, weight, saved, out, gw, gb, grads is not None, accumulate, want_x, want_w, want_b,
+                _code(dtype), workspace)
+    if r is not None:
+        return r
     rows, width, x_stride = _matrix("x", x)
     device = x.device
     gy_stride = _rows_of("grad_y", grad_y, rows, width, device)
@@ -115,8 +129,7 @@ def layer_norm_backward(x, grad_y, weight, saved, out=None, grads=None, accumula
     if saved.shape != (rows, 2) or saved.dtype is not torch.float32 or saved.device != device or not saved.is_contiguous():
         raise ValueError(f"saved must be the contiguous float32 [{rows}, 2] tensor of the forward call")
     _values("saved", saved)
-    want_x, want_w, want_b = grad
-    gx = gw = gb = None
+    gx = None
     gx_stride = width
     if want_x:
         gx = torch.empty(rows, width, dtype=x.dtype, device=device) if out is None else out
@@ -125,9 +138,7 @@ def layer_norm_backward(x, grad_y, weight, saved, out=None, grads=None, accumula
             same = out.data_ptr() == grad_y.data_ptr() and gx_stride == gy_stride and out.dtype is grad_y.dtype
             _apart("out", out, ("x", x), ("weight", weight), *(() if same else (("grad_y", grad_y),)))
     if grads is not None:
-        if len(grads) != 2:
-            raise ValueError("grads must be (grad_weight, grad_bias)")
-        gw, gb = grads[0] if want_w else None, grads[1] if want_b else None
+        gw, gb = gw if want_w else None, gb if want_b else None
         for name, t in (("grad_weight", gw), ("grad_bias", gb)):
             if t is not None:
                 _width_vector(name, t, width, device)
@@ -160,6 +171,9 @@ def _embedding_bytes(rows, width, classes):
 def embedding(tokens, weight, scale: float = 1.0, dtype=None, out=None):
     """scale * weight[tokens]: [rows, width] of ``dtype`` (default: the weight's).
     A negative token gives a row of zeros, one past the weight's rows a row of NaN."""
+    r = _native(weight, "embedding", scale, _code(dtype), out, first=tokens)
+    if r is not None:
+        return r
     classes, width, stride = _matrix("weight", weight)
     device = weight.device
     rows = tokens.shape[0] if tokens.dim() == 1 else -1
@@ -186,6 +200,9 @@ def embedding_backward(tokens, grad_rows, classes: int, scale: float = 1.0, dtyp
     ``accumulate`` to add it to (a weight that the loss shares: its gradient); only
     the tokens' rows of it are read and written then.  Otherwise it is made, of
     ``dtype`` (default: that of ``grad_rows``)."""
+    r = _native(grad_rows, "embedding_backward", classes, scale, _code(dtype), grad_weight, accumulate, workspace, first=tokens)
+    if r is not None:
+        return r
     rows, width, stride = _matrix("grad_rows", grad_rows)
     device = grad_rows.device
     bits = _index("tokens", tokens, rows, device)

@@ -79,13 +79,17 @@ class VocabLoss(NamedTuple):
     row_grads: Optional[torch.Tensor]  # [rows]: dL/dlogp
 
 
-def _native(logits, name, *args):
-    """The call by the binding's native part, or None where the logits are not
-    on the current device or an argument is not plainly what it should be (the
-    code below then says what is wrong)."""
+def _native(logits, name, *args, first=None):
+    """The call by the binding's native part (``first``: an argument before the
+    logits), or None where the logits are not on the current device or an
+    argument is not plainly what it should be (the code below then says what is
+    wrong)."""
     device = logits.get_device()
     if device < 0 or device != torch._C._cuda_getDevice():
         return None
+    if first is not None:
+        args = (logits, *args)
+        logits = first
     r = getattr(binding(), name)(logits, *args, torch._C._cuda_getCurrentRawStream(device))
     if type(r) is int:
         _check(r, f"acdc_{name}")
@@ -438,6 +442,9 @@ def _wants(grad):
 def vocab_logprobs(hidden, weight, targets, save: bool = False, workspace=None) -> VocabLogprobs:
     """Log-probability of each row's target under softmax(hidden @ weight.T),
     with ``save`` what ``vocab_logprobs_backward`` needs."""
+    r = _native(hidden, "vocab_logprobs", weight, targets, save, workspace)
+    if r is not None:
+        return VocabLogprobs(*r)
     head, ws, need = _vocab_head(hidden, weight, targets, False, workspace)
     rows, device = hidden.shape[0], hidden.device
     logp = torch.empty(rows, device=device)
@@ -455,6 +462,10 @@ def vocab_logprobs_backward(hidden, weight, targets, saved, grad_logp, scale=Non
     grad_hidden into; ``grad_weight``: one to write, or with ``accumulate`` to
     add, the weight's gradient into, float32 or of the weight's type."""
     wanted = _wants(grad)
+    r = _native(hidden, "vocab_backward", weight, targets, saved, grad_logp, scale, *wanted, out, grad_weight, accumulate,
+                workspace)
+    if r is not None:
+        return r
     head, ws, need = _vocab_head(hidden, weight, targets, True, workspace)
     rows, device = hidden.shape[0], hidden.device
     if saved.shape != (rows, 2) or saved.dtype is not torch.float32 or saved.device != device or not saved.is_contiguous():
@@ -481,6 +492,10 @@ def vocab_loss(hidden, weight, targets, weights=None, mean: bool = True, grad_sc
     ``grad_scale`` multiplies the gradients.  ``save`` returns what
     ``vocab_logprobs_backward`` needs to compute them later."""
     wanted = _wants(grad)
+    r = _native(hidden, "vocab_loss", weight, targets, weights, mean, grad_scale, *wanted, save, out, grad_weight,
+                accumulate, workspace)
+    if r is not None:
+        return VocabLoss(*r)
     any_grad = wanted[0] or wanted[1]
     head, ws, need = _vocab_head(hidden, weight, targets, any_grad, workspace)
     rows, device = hidden.shape[0], hidden.device

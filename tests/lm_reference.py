@@ -56,8 +56,9 @@ class Vocab:
         for left, dl, right, bf16 in ((G, dG, self.w, bf16_hidden), (G.T, dG.T, self.h, bf16_weight)):
             ref = left @ right
             tol = dl @ np.abs(right) + (right.shape[0] + 16) * EPS * (np.abs(left) @ np.abs(right))
-            if bf16_in:   # each value of G rounded to bfloat16 on its way into the product
-                tol += SPREAD * BF16 * np.sqrt(left ** 2 @ right ** 2)
+            if bf16_in:   # each value of G is rounded to bfloat16 on its way into the product, and where the
+                # exponentials are kept they are too: 2 n roundings for n values, sqrt(2) of the spread of n
+                tol += SPREAD * BF16 * np.sqrt(2.0 * (left ** 2 @ right ** 2))
             out.append((ref, tol + out_rounding(ref, bf16) + 4 * EPS * np.abs(ref) + 1e-37))
         return out
 

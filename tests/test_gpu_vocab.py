@@ -126,16 +126,18 @@ def test_weight_gradient_is_added(env, dtype, given):
     close(total, rw, tw + 4 * R.EPS * np.abs(rw) + R.out_rounding(rw, given == "bfloat16"), "grad_weight")
 
 
-def test_pieces_of_the_vocabulary(env, monkeypatch):
-    """More classes than a piece holds: 16384 rows leave 16384 classes a piece."""
+@pytest.mark.parametrize("shape", [(16384, 16, 20000, "bfloat16", 64, 0, 0), (16384, 8, 70000, "bfloat16", 64, 0, 0),
+                                   (16384, 16, 20000, "float32", 64, 0, 0), (30000, 7, 7000, "float32", 64, 0, 0)])
+def test_pieces_of_the_vocabulary(env, shape):
+    """16384 rows leave 65536 classes of bfloat16 and 13056 of float32 a piece of 2 GiB: one piece, whose exponentials
+    are kept, and more."""
     torch, losses = env
-    rows, width, classes = 16384, 16, 20000
-    h, w, t, h64, w64, t64, _ = make(torch, (rows, width, classes, "bfloat16", 64, 0, 0), seed=3, idle=0.97)
+    h, w, t, h64, w64, t64, _ = make(torch, shape, seed=3, idle=0.985)
     on = t64 >= 0
     ref = R.Vocab(h64[on], w64, t64[on])
     r = losses.vocab_loss(h, w, t)
     close(r.logp[torch.from_numpy(on).cuda()], ref.logp, ref.logp_tol, "logp")
-    check_gradients(ref, -ref.share, r.grad_hidden[torch.from_numpy(on).cuda()], r.grad_weight, True)
+    check_gradients(ref, -ref.share, r.grad_hidden[torch.from_numpy(on).cuda()], r.grad_weight, h.dtype is torch.bfloat16)
     assert (r.grad_hidden[torch.from_numpy(~on).cuda()] == 0).all()
 
 
