@@ -2,7 +2,7 @@
 // (acdc_train_lm.h).
 //
 // The gradient of a class is the sum of the gradients of its rows.  The rows
-// are sorted by token (a stable radix sort of eight bits a pass), so that those
+// are sorted by token (a stable radix sort), so that those
 // of a class follow one another, in their order; then 64 sorted rows at a
 // time are summed class by class.  A class that begins and ends within the 64
 // is written at once; of one that goes on, each 64 leave a partial sum, which
@@ -29,151 +29,268 @@ __device__ __forceinline__ int key_of(const void* tokens, int bits, long long r,
 
 // ----------------------------------------------------------------- the lookup
 
-// A wave takes one of `split` parts of a row.
-template <class TW, class TO>
+// A wave takes one of `split` parts of ROWS rows, whose tokens and values it asks for
+// together: one row at a time it would wait for a token and then for its row.
+template <class TW, class TO, int ROWS>
 __global__ __launch_bounds__(kThreads) void k_embed(const void* __restrict__ tokens, int bits,
                                                     const typename TW::Elem* __restrict__ weight, long long weight_stride,
                                                     float scale, typename TO::Elem* __restrict__ out, long long out_stride,
                                                     int rows, int width, int classes, int split) {
   const int lane = threadIdx.x % 64;
-  const unsigned items = unsigned(rows) * unsigned(split);
+  const unsigned items = (unsigned(rows) + ROWS - 1) / ROWS * unsigned(split);
   for (unsigned item = blockIdx.x * kWaves + uniform(int(threadIdx.x / 64)); item < items; item += gridDim.x * kWaves) {
-    const long long r = item / unsigned(split);
-    const int part = int(item % unsigned(split));
-    const long long t = bits == 64 ? static_cast<const long long*>(tokens)[r] : (long long)static_cast<const int*>(tokens)[r];
-    const float fill = t < 0 ? 0.f : __builtin_nanf("");
-    const bool there = t >= 0 && t < classes;
-    const typename TW::Elem* from = weight + (there ? t : 0) * weight_stride;
-    typename TO::Elem* to = out + r * out_stride;
-#pragma unroll 4
-    for (int col = (part * 64 + lane) * kEight; col < width; col += split * 64 * kEight) {
-      float v[kEight];
-      if (there) load_some<TW>(from + col, width - col, 0.f, v);
+    const int first = int(item / unsigned(split)) * ROWS, part = int(item % unsigned(split)), many = min(ROWS, rows - first);
+    const typename TW::Elem* from[ROWS];
+    bool there[ROWS];
+    float fill[ROWS];
 #pragma unroll
-      for (int i = 0; i < kEight; ++i) v[i] = there ? v[i] * scale : fill;
-      store_some<TO>(to + col, width - col, v);
+    for (int q = 0; q < ROWS; ++q) {
+      const long long r = first + (q < many ? q : 0);
+      const long long t = bits == 64 ? static_cast<const long long*>(tokens)[r] : (long long)static_cast<const int*>(tokens)[r];
+      there[q] = t >= 0 && t < classes;
+      from[q] = weight + (there[q] ? t : 0) * weight_stride;
+      fill[q] = t < 0 ? 0.f : __builtin_nanf("");
+    }
+#pragma unroll 2
+    for (int col = (part * 64 + lane) * kEight; col < width; col += split * 64 * kEight) {
+      float v[ROWS][kEight];
+#pragma unroll
+      for (int q = 0; q < ROWS; ++q)
+        if (q < many) load_some<TW>(from[q] + col, width - col, 0.f, v[q]);
+#pragma unroll
+      for (int q = 0; q < ROWS; ++q) {
+        if (q >= many) continue;
+#pragma unroll
+        for (int i = 0; i < kEight; ++i) v[q][i] = there[q] ? v[q][i] * scale : fill[q];
+        store_some<TO>(out + (long long)(first + q) * out_stride + col, width - col, v[q]);
+      }
     }
   }
 }
 
 // ------------------------------------------------------------------- the sort
 
-// Pairs of a key and its row in tiles of kTile, a wave's kEach x 64 of them following
-// one another.
-constexpr int kEach = 8, kTile = kThreads * kEach, kDigits = 256;
-struct Pairs {
+// Stable, least digit first, in passes of up to nine bits.
+struct Sorted {
   int* key;
   int* row;
 };
+constexpr int kDigits = 512;
 
-// How often each digit comes in each tile: counts[digit][tile].  In the first pass
-// the keys come from the tokens, and each token is marked as one that is there.
-__global__ __launch_bounds__(kThreads) void k_sort_count(const void* __restrict__ tokens, int bits, int classes, Pairs in,
-                                                         int n, int shift, int tiles, int* __restrict__ counts,
+// next[wave][digit] goes from how many pairs of the digit a wave has to how many the waves
+// before it have; returns how many all have.
+template <int WAVES>
+__device__ __forceinline__ int digit_total(int (&next)[WAVES][kDigits], int digit) {
+  int all = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    const int c = next[w][digit];
+    next[w][digit] = all;
+    all += c;
+  }
+  return all;
+}
+// The exclusive sums of kDigits totals, EACH digits that follow one another for each of the
+// first threads; the whole workgroup calls it.
+template <int EACH>
+__device__ __forceinline__ void digit_bases(const int (&total)[EACH], int (&base)[EACH], int* slots) {
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  int mine = 0;
+#pragma unroll
+  for (int q = 0; q < EACH; ++q) mine += total[q];
+  int sum = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int up = __shfl_up(sum, o);
+    if (lane >= o) sum += up;
+  }
+  constexpr int WAVES = kDigits / EACH / 64;
+  if (wave < WAVES && lane == 63) slots[wave] = sum;
+  __syncthreads();
+  int at = sum - mine;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w)
+    if (w < wave) at += slots[w];
+#pragma unroll
+  for (int q = 0; q < EACH; ++q) {
+    base[q] = at;
+    at += total[q];
+  }
+}
+// The place of a pair among its wave's of the same digit; a wave's pairs come in rounds of 64.
+__device__ __forceinline__ int place_of(int* next, bool here, int digit, int bits) {
+  const int lane = threadIdx.x % 64;
+  unsigned long long same = __ballot(here);  // the lanes of this round with the same digit
+  for (int b = 0; b < bits; ++b) {
+    const unsigned long long set = __ballot(here && (digit >> b & 1));
+    same &= (digit >> b & 1) ? set : ~set;
+  }
+  const int rank = __popcll(same & ((1ull << lane) - 1)), many = __popcll(same);
+  int to = 0;
+  if (here) to = next[digit] + rank;
+  wave_sync();  // everyone has read before the last of a digit writes
+  if (here && rank == many - 1) next[digit] = to + 1;
+  wave_sync();
+  return to;
+}
+
+// Up to 8192 rows by one workgroup, in LDS.  It clears
+// and sets the marks of the tokens that are there, too.
+constexpr int kSmallThreads = 1024, kSmallEach = 8, kSmall = kSmallThreads * kSmallEach, kSmallClasses = 1 << 18;
+__global__ __launch_bounds__(kSmallThreads) void k_sort_small(const void* __restrict__ tokens, int bits, int classes, Sorted out,
+                                                             int n, int digit_bits, int passes, unsigned char* there) {
+  constexpr int WAVES = kSmallThreads / 64;
+  __shared__ int next[WAVES][kDigits];
+  __shared__ int keys[kSmall], rows[kSmall], slots[WAVES];
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, base = wave * (64 * kSmallEach);
+  for (int i = tid * 16; i < classes; i += kSmallThreads * 16) *reinterpret_cast<uint4*>(there + i) = uint4{};  // (256 bytes at a time are there)
+  __syncthreads();
+  int key[kSmallEach], row[kSmallEach];
+#pragma unroll
+  for (int q = 0; q < kSmallEach; ++q) {
+    const int i = base + q * 64 + lane;
+    key[q] = i < n ? key_of(tokens, bits, i, classes) : 0;
+    row[q] = i;
+    if (i < n && key[q] < classes) there[key[q]] = 1;
+  }
+  const int mask = (1 << digit_bits) - 1;
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * digit_bits;
+    for (int i = tid; i < WAVES * kDigits; i += kSmallThreads) next[i / kDigits][i % kDigits] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kSmallEach; ++q)
+      if (base + q * 64 + lane < n) atomicAdd(&next[wave][(key[q] >> shift) & mask], 1);  // (whole numbers: any order gives the same)
+    __syncthreads();
+    int total[1] = {0}, first[1];
+    if (tid < kDigits) total[0] = digit_total<WAVES>(next, tid);
+    digit_bases<1>(total, first, slots);
+    if (tid < kDigits) {
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) next[w][tid] += first[0];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kSmallEach; ++q) {
+      const bool here = base + q * 64 + lane < n;
+      const int to = place_of(next[wave], here, (key[q] >> shift) & mask, digit_bits);
+      if (here) {
+        keys[to] = key[q];
+        rows[to] = row[q];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kSmallEach; ++q) {
+      const int i = base + q * 64 + lane;
+      key[q] = keys[i];  // (behind the last: anything, not used)
+      row[q] = rows[i];
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int q = 0; q < kSmallEach; ++q) {
+    const int i = base + q * 64 + lane;
+    if (i < n) {
+      out.key[i] = key[q];
+      out.row[i] = row[q];
+    }
+  }
+}
+
+// More rows, in tiles: counts[tile][digit], their sums over the tiles before, and each pair
+// to its place, a pass in three launches.
+constexpr int kEach = 8, kTile = kThreads * kEach, kPerThread = kDigits / kThreads;
+
+__global__ __launch_bounds__(kThreads) void k_sort_count(const void* __restrict__ tokens, int bits, int classes, Sorted in, int n,
+                                                         int shift, int mask, int* __restrict__ counts,
                                                          unsigned char* __restrict__ there) {
   __shared__ int bins[kDigits];
-  bins[threadIdx.x] = 0;
+#pragma unroll
+  for (int d = 0; d < kPerThread; ++d) bins[d * kThreads + threadIdx.x] = 0;
   __syncthreads();
 #pragma unroll
   for (int q = 0; q < kEach; ++q) {
     const int i = blockIdx.x * kTile + q * kThreads + threadIdx.x;
     if (i < n) {
+      // in the first pass the keys come from the tokens, and are marked as there
       const int k = tokens != nullptr ? key_of(tokens, bits, i, classes) : in.key[i];
       if (tokens != nullptr && k < classes) there[k] = 1;
-      atomicAdd(&bins[(k >> shift) & (kDigits - 1)], 1);  // (whole numbers: any order gives the same)
+      atomicAdd(&bins[(k >> shift) & mask], 1);
     }
   }
   __syncthreads();
-  counts[threadIdx.x * tiles + blockIdx.x] = bins[threadIdx.x];
+#pragma unroll
+  for (int d = 0; d < kPerThread; ++d)
+    counts[(long long)blockIdx.x * kDigits + d * kThreads + threadIdx.x] = bins[d * kThreads + threadIdx.x];
 }
 
-// Exclusive sums of `n` counts, in place, by one workgroup.
-constexpr int kScan = 1024;
-__global__ __launch_bounds__(kScan) void k_sort_scan(int* __restrict__ counts, int n) {
-  __shared__ int waves[kScan / 64];
-  constexpr int EACH = 8;
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  int before = 0;
-  for (int base = 0; base < n; base += kScan * EACH) {
-    int v[EACH], mine = 0;
-    const int first = base + tid * EACH;
+// 64 digits a workgroup, 16 waves along the tiles: counts become what the tiles before
+// hold, totals[digit] what all do.
+constexpr int kSumWaves = 16;
+__global__ __launch_bounds__(64 * kSumWaves) void k_sort_sums(int* __restrict__ counts, int tiles, int* __restrict__ totals) {
+  __shared__ int slots[kSumWaves][64];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, digit = blockIdx.x * 64 + lane;
+  const int per = (tiles + kSumWaves - 1) / kSumWaves, from = min(tiles, wave * per), to = min(tiles, from + per);
+  int sum = 0;
+#pragma unroll 8
+  for (int t = from; t < to; ++t) sum += counts[(long long)t * kDigits + digit];
+  slots[wave][lane] = sum;
+  __syncthreads();
+  int before = 0, all = 0;
 #pragma unroll
-    for (int q = 0; q < EACH; ++q) {
-      v[q] = first + q < n ? counts[first + q] : 0;
-      mine += v[q];
-    }
-    int sum = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int up = __shfl_up(sum, o);
-      if (lane >= o) sum += up;
-    }
-    if (lane == 63) waves[wave] = sum;
-    __syncthreads();
-    int at = before + sum - mine;
-#pragma unroll
-    for (int w = 0; w < kScan / 64; ++w) {
-      if (w < wave) at += waves[w];
-      before += waves[w];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < EACH; ++q)
-      if (first + q < n) {
-        counts[first + q] = at;
-        at += v[q];
-      }
+  for (int w = 0; w < kSumWaves; ++w) {
+    if (w < wave) before += slots[w][lane];
+    all += slots[w][lane];
+  }
+  if (wave == 0) totals[digit] = all;
+#pragma unroll 8
+  for (int t = from; t < to; ++t) {
+    const int c = counts[(long long)t * kDigits + digit];
+    counts[(long long)t * kDigits + digit] = before;
+    before += c;
   }
 }
 
-// Each pair to its place: after those of lower digits, of earlier tiles, of earlier
-// waves, of earlier rounds and of lower lanes with the same digit.
-__global__ __launch_bounds__(kThreads) void k_sort_move(const void* __restrict__ tokens, int bits, int classes, Pairs in,
-                                                        Pairs out, int n, int shift, int tiles, const int* __restrict__ counts) {
-  __shared__ int next[kWaves][kDigits];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+// A pair comes after those of lower digits, of earlier tiles, of earlier waves, of earlier
+// rounds and of lower lanes with the same digit.
+__global__ __launch_bounds__(kThreads) void k_sort_move(const void* __restrict__ tokens, int bits, int classes, Sorted in,
+                                                        Sorted out, int n, int shift, int digit_bits,
+                                                        const int* __restrict__ counts, const int* __restrict__ totals) {
+  __shared__ int next[kWaves][kDigits], slots[kWaves];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, mask = (1 << digit_bits) - 1;
   const int base = blockIdx.x * kTile + wave * (64 * kEach);
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) next[w][threadIdx.x] = 0;
+  for (int i = threadIdx.x; i < kWaves * kDigits; i += kThreads) next[i / kDigits][i % kDigits] = 0;
   __syncthreads();
   int key[kEach], row[kEach];
 #pragma unroll
   for (int q = 0; q < kEach; ++q) {
     const int i = base + q * 64 + lane;
+    key[q] = row[q] = 0;
     if (i < n) {
       key[q] = tokens != nullptr ? key_of(tokens, bits, i, classes) : in.key[i];
       row[q] = tokens != nullptr ? i : in.row[i];
-      atomicAdd(&next[wave][(key[q] >> shift) & (kDigits - 1)], 1);
+      atomicAdd(&next[wave][(key[q] >> shift) & mask], 1);
     }
   }
-  __syncthreads();
-  {
-    int at = counts[threadIdx.x * tiles + blockIdx.x];
+  int total[kPerThread], first[kPerThread];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const int c = next[w][threadIdx.x];
-      next[w][threadIdx.x] = at;
-      at += c;
-    }
+  for (int d = 0; d < kPerThread; ++d) total[d] = totals[threadIdx.x * kPerThread + d];
+  __syncthreads();
+  digit_bases<kPerThread>(total, first, slots);
+#pragma unroll
+  for (int d = 0; d < kPerThread; ++d) {
+    const int digit = threadIdx.x * kPerThread + d;
+    digit_total<kWaves>(next, digit);
+    const int at = first[d] + counts[(long long)blockIdx.x * kDigits + digit];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) next[w][digit] += at;
   }
   __syncthreads();
 #pragma unroll
   for (int q = 0; q < kEach; ++q) {
     const bool here = base + q * 64 + lane < n;
-    const int digit = (key[q] >> shift) & (kDigits - 1);
-    // the lanes of this round with the same digit
-    unsigned long long same = __ballot(here);
-#pragma unroll
-    for (int b = 0; b < 8; ++b) {
-      const unsigned long long set = __ballot(here && (digit >> b & 1));
-      same &= (digit >> b & 1) ? set : ~set;
-    }
-    const int rank = __popcll(same & ((1ull << lane) - 1)), many = __popcll(same);
-    int to = 0;
-    if (here) to = next[wave][digit] + rank;
-    wave_sync();  // everyone has read before the last of a digit writes
-    if (here && rank == many - 1) next[wave][digit] = to + 1;
-    wave_sync();
+    const int to = place_of(next[wave], here, (key[q] >> shift) & mask, digit_bits);
     if (here) {
       out.key[to] = key[q];
       out.row[to] = row[q];
@@ -220,7 +337,7 @@ __global__ __launch_bounds__(kThreads) void k_embed_sums(SumArgs a, const typena
   float s[kEight] = {};
   int current = uniform(mine);
   bool began = current != before;  // the class begins in this piece
-  constexpr int AHEAD = 4;
+  constexpr int AHEAD = 8;
   for (int i = 0; i < to - from; i += AHEAD) {
     float v[AHEAD][kEight];
     int key[AHEAD];
@@ -256,27 +373,51 @@ __global__ __launch_bounds__(kThreads) void k_embed_sums(SumArgs a, const typena
     put_class<TW>(weight + current * a.weight_stride + col, left, s, a.scale, a.add);
 }
 
-// The class that begins in a piece and goes on behind it: its partial sums together.
+// The class that begins in a piece and goes on behind it: its partial sums together, by
+// the waves of a workgroup that each take some that follow one another.
+constexpr int kJoinWaves = 8;
 template <class TW>
-__global__ __launch_bounds__(kThreads) void k_embed_join(SumArgs a, typename TW::Elem* __restrict__ weight) {
-  const int lane = threadIdx.x % 64;
-  const long long item = (long long)blockIdx.x * kWaves + uniform(int(threadIdx.x / 64));
-  if (item >= (long long)a.pieces * a.blocks) return;
-  const int piece = int(item / a.blocks), col = (int(item % a.blocks) * 64 + lane) * kEight, left = a.width - col;
-  const int from = piece * kPiece, to = from + kPiece;
-  if (to >= a.rows || left <= 0) return;
+__global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(SumArgs a, typename TW::Elem* __restrict__ weight) {
+  __shared__ float slots[kJoinWaves][kEight][64];
+  const int lane = threadIdx.x % 64, wave = uniform(int(threadIdx.x / 64));
+  const int piece = int(blockIdx.x / unsigned(a.blocks)), col = (int(blockIdx.x % unsigned(a.blocks)) * 64 + lane) * kEight;
+  const int left = a.width - col, from = piece * kPiece, to = from + kPiece;
+  if (to >= a.rows) return;
   const int key = a.key[to];
-  if (key >= a.classes || a.key[to - 1] != key) return;        // nothing goes on
+  if (key >= a.classes || a.key[to - 1] != key) return;                  // nothing goes on
   if (a.key[from] == key && from > 0 && a.key[from - 1] == key) return;  // it began before
-  float s[kEight];
-  load_some<F32>(a.partial + ((long long)piece * 2 + 1) * a.width + col, left, 0.f, s);
-#pragma unroll 4
-  for (int p = piece + 1; p < a.pieces && a.key[p * kPiece] == key; ++p) {
-    float v[kEight];
-    load_some<F32>(a.partial + (long long)p * 2 * a.width + col, left, 0.f, v);
-#pragma unroll
-    for (int c = 0; c < kEight; ++c) s[c] += v[c];
+  // pieces that begin with it
+  int many = 0;
+  for (;;) {
+    const long long p = (long long)piece + 1 + many + lane;
+    const unsigned long long same = __ballot(p < a.pieces && a.key[min(p, (long long)a.pieces - 1) * kPiece] == key);
+    if (~same == 0ull) {
+      many += 64;
+      continue;
+    }
+    many += __ffsll((long long)~same) - 1;
+    break;
   }
+  float s[kEight] = {};
+  const int per = (many + kJoinWaves - 1) / kJoinWaves, first = min(many, wave * per), last = min(many, first + per);
+  if (left > 0) {
+    if (wave == 0) load_some<F32>(a.partial + ((long long)piece * 2 + 1) * a.width + col, left, 0.f, s);
+#pragma unroll 4
+    for (int p = first; p < last; ++p) {
+      float v[kEight];
+      load_some<F32>(a.partial + (long long)(piece + 1 + p) * 2 * a.width + col, left, 0.f, v);
+#pragma unroll
+      for (int c = 0; c < kEight; ++c) s[c] += v[c];
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < kEight; ++c) slots[wave][c][lane] = s[c];
+  __syncthreads();
+  if (wave != 0 || left <= 0) return;
+#pragma unroll
+  for (int w = 1; w < kJoinWaves; ++w)
+#pragma unroll
+    for (int c = 0; c < kEight; ++c) s[c] += slots[w][c][lane];
   put_class<TW>(weight + key * a.weight_stride + col, left, s, a.scale, a.add);
 }
 
@@ -298,7 +439,7 @@ __global__ __launch_bounds__(kThreads) void k_embed_zeros(const unsigned char* _
 
 // ------------------------------------------------------------------ on the host
 
-constexpr int64_t kMostRows = 1 << 28, kMostClasses = 1 << 30, kMostWidth = 1 << 20, kMostStride = int64_t(1) << 40;
+constexpr int64_t kMostRows = (1 << 28) - kPiece, kMostClasses = 1 << 30, kMostWidth = 1 << 20, kMostStride = int64_t(1) << 40;
 
 int done() {
   const hipError_t e = hipGetLastError();
@@ -306,7 +447,7 @@ int done() {
 }
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
 struct Layout {
-  size_t key[2], row[2], counts, there, partial, bytes;
+  size_t key[2], row[2], counts, totals, there, partial, bytes;
 };
 Layout layout(int64_t rows, int32_t width, int32_t classes) {
   Layout w{};
@@ -322,12 +463,15 @@ Layout layout(int64_t rows, int32_t width, int32_t classes) {
     w.row[k] = take(n * 4);
   }
   w.counts = take((n + kTile - 1) / kTile * kDigits * 4);
+  w.totals = take(kDigits * 4);
   w.there = take(size_t(classes));
   w.partial = take((n + kPiece - 1) / kPiece * 2 * size_t(width) * 4);
   w.bytes = next;
   return w;
 }
 bool sizes_ok(int64_t rows, int32_t width, int32_t classes) {
+  // (a grid has fewer than 2^32 lanes)
+  if (rows >= 0 && rows <= kMostRows && width >= 1 && (rows / kPiece + 1) * (int64_t(width) / (64 * kEight) + 1) > (1 << 22)) return false;
   return rows >= 0 && rows <= kMostRows && width >= 1 && width <= kMostWidth && classes >= 1 && classes <= kMostClasses;
 }
 bool matrix_ok(const void* p, int32_t dtype, int64_t stride, int64_t rows, int32_t width) {
@@ -373,11 +517,16 @@ extern "C" int acdc_embedding_forward(const void* tokens, int32_t token_bits, co
   // parts of a row where few rows would leave the card idle
   const int64_t most = (width + 64 * kEight - 1) / (64 * kEight);
   const int split = int(std::clamp<int64_t>(2048 / rows, 1, most));
-  const unsigned blocks = unsigned(std::min<int64_t>((rows * split + kWaves - 1) / kWaves, 1 << 16));
   with_types(weight_type, out_type, [&]<class TW, class TO>() {
-    hipLaunchKernelGGL((k_embed<TW, TO>), dim3(blocks), dim3(kThreads), 0, s, tokens, token_bits,
-                       static_cast<const typename TW::Elem*>(weight), (long long)weight_stride, scale,
-                       static_cast<typename TO::Elem*>(out), (long long)out_stride, int(rows), width, classes, split);
+    auto go = [&]<int ROWS>() {
+      const int64_t items = (rows + ROWS - 1) / ROWS * split;
+      hipLaunchKernelGGL((k_embed<TW, TO, ROWS>), dim3(unsigned(std::min<int64_t>((items + kWaves - 1) / kWaves, 1 << 16))),
+                         dim3(kThreads), 0, s, tokens, token_bits, static_cast<const typename TW::Elem*>(weight),
+                         (long long)weight_stride, scale, static_cast<typename TO::Elem*>(out), (long long)out_stride, int(rows),
+                         width, classes, split);
+    };
+    if (rows >= 8192) go.template operator()<4>();
+    else go.template operator()<1>();
   });
   return done();
 }
@@ -402,20 +551,28 @@ extern "C" int acdc_embedding_backward(const void* tokens, int32_t token_bits, c
   char* ws = static_cast<char*>(workspace);
   unsigned char* there = reinterpret_cast<unsigned char*>(ws + w.there);
   int* counts = reinterpret_cast<int*>(ws + w.counts);
-  Pairs pairs[2];
-  for (int k = 0; k < 2; ++k) pairs[k] = Pairs{reinterpret_cast<int*>(ws + w.key[k]), reinterpret_cast<int*>(ws + w.row[k])};
-  hipLaunchKernelGGL(k_embed_clear, dim3(unsigned(std::min<int64_t>((classes + kThreads - 1) / kThreads, 1024))), dim3(kThreads), 0, s,
-                     there, classes);
+  int* totals = reinterpret_cast<int*>(ws + w.totals);
+  Sorted pairs[2];
+  for (int k = 0; k < 2; ++k) pairs[k] = Sorted{reinterpret_cast<int*>(ws + w.key[k]), reinterpret_cast<int*>(ws + w.row[k])};
+  // passes of as many bits each; `classes` is a key too
+  int key_bits = 0;
+  while ((int64_t(classes) >> key_bits) != 0) ++key_bits;
+  const int passes = (key_bits + 8) / 9, digit_bits = (key_bits + passes - 1) / passes, n = int(rows);
   int at = 0;
-  if (rows > 0) {
-    const int n = int(rows), tiles = (n + kTile - 1) / kTile;
-    for (int shift = 0; shift == 0 || (classes >> shift) != 0; shift += 8, at ^= 1) {
-      const void* from = shift == 0 ? tokens : nullptr;
-      hipLaunchKernelGGL(k_sort_count, dim3(unsigned(tiles)), dim3(kThreads), 0, s, from, token_bits, classes, pairs[at], n, shift,
-                         tiles, counts, there);
-      hipLaunchKernelGGL(k_sort_scan, dim3(1), dim3(kScan), 0, s, counts, tiles * kDigits);
-      hipLaunchKernelGGL(k_sort_move, dim3(unsigned(tiles)), dim3(kThreads), 0, s, from, token_bits, classes, pairs[at],
-                         pairs[at ^ 1], n, shift, tiles, counts);
+  if (rows > 0 && rows <= kSmall && classes <= kSmallClasses) {
+    hipLaunchKernelGGL(k_sort_small, dim3(1), dim3(kSmallThreads), 0, s, tokens, token_bits, classes, pairs[0], n, digit_bits, passes,
+                       there);
+  } else {
+    hipLaunchKernelGGL(k_embed_clear, dim3(unsigned(std::min<int64_t>((classes + kThreads - 1) / kThreads, 1024))), dim3(kThreads), 0,
+                       s, there, classes);
+    const int tiles = (n + kTile - 1) / kTile;
+    for (int pass = 0; pass < passes && rows > 0; ++pass, at ^= 1) {
+      const void* from = pass == 0 ? tokens : nullptr;
+      hipLaunchKernelGGL(k_sort_count, dim3(unsigned(tiles)), dim3(kThreads), 0, s, from, token_bits, classes, pairs[at], n,
+                         pass * digit_bits, (1 << digit_bits) - 1, counts, there);
+      hipLaunchKernelGGL(k_sort_sums, dim3(kDigits / 64), dim3(64 * kSumWaves), 0, s, counts, tiles, totals);
+      hipLaunchKernelGGL(k_sort_move, dim3(unsigned(tiles)), dim3(kThreads), 0, s, from, token_bits, classes, pairs[at], pairs[at ^ 1],
+                         n, pass * digit_bits, digit_bits, counts, totals);
     }
   }
   with_types(out_type, weight_type, [&]<class TG, class TW>() {
@@ -429,7 +586,8 @@ extern "C" int acdc_embedding_backward(const void* tokens, int32_t token_bits, c
                     reinterpret_cast<float*>(ws + w.partial), accumulate != 0};
     const unsigned groups = unsigned((int64_t(pieces) * blocks + kWaves - 1) / kWaves);
     hipLaunchKernelGGL((k_embed_sums<TG, TW>), dim3(groups), dim3(kThreads), 0, s, a, static_cast<const typename TG::Elem*>(grad_out), out);
-    if (pieces > 1) hipLaunchKernelGGL(k_embed_join<TW>, dim3(groups), dim3(kThreads), 0, s, a, out);
+    if (pieces > 1)
+      hipLaunchKernelGGL(k_embed_join<TW>, dim3(unsigned(int64_t(pieces) * blocks)), dim3(64 * kJoinWaves), 0, s, a, out);
   });
   return done();
 }

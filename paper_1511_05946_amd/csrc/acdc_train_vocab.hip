@@ -192,6 +192,15 @@ struct StatsOut {
   float* logit;
   void* kept;  // rows `ld` apart
   int first, classes, rows, tile, ld;
+  // the classes past the last are no classes
+  template <int MI, int NI, class SP>
+  __device__ __forceinline__ void mask(f32x4 (&acc)[MI][NI], const SP& spot, int n) const {
+#pragma unroll
+    for (int m = 0; m < MI; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (spot.m(m) + i >= classes) acc[m][n][i] = -__builtin_inff();
+  }
   template <class S, int MI, int NI, class SP>
   __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const SP& spot, const Place& at, int wave,
                                              float2* slots) const {
@@ -201,18 +210,18 @@ struct StatsOut {
     float tops[NI];
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
-      const int r = spot.n(n), t = target[r] - first;
+      const int r = spot.n(n), t = target[r] - first - spot.m(0);
+      if ((at.tm + 1) * S::BM > classes) mask(acc, spot, n);
+      if (unsigned(t) < 4u * MI) {
+#pragma unroll
+        for (int v = 0; v < 4 * MI; ++v)
+          if (v == t) logit[r] = acc[v / 4][n][v % 4];
+      }
       float top = kNegMax;
 #pragma unroll
-      for (int m = 0; m < MI; ++m) {
+      for (int m = 0; m < MI; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int v = spot.m(m) + i;
-          if (v >= classes) acc[m][n][i] = -__builtin_inff();
-          else if (v == t) logit[r] = acc[m][n][i];
-          top = fmaxf(top, acc[m][n][i]);
-        }
-      }
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, acc[m][n][i]);
       Pair p = swap16(top);
       top = fmaxf(p.a, p.b);
       p = swap32(top);
