@@ -134,24 +134,29 @@ __device__ __forceinline__ int place_of(int* next, bool here, int digit, int bit
   return to;
 }
 
-// Up to 8192 rows by one workgroup, in LDS.  It clears
-// and sets the marks of the tokens that are there, too.
-constexpr int kSmallThreads = 1024, kSmallEach = 8, kSmall = kSmallThreads * kSmallEach, kSmallClasses = 1 << 18;
+// Up to 8192 rows by the first workgroup, in LDS, while the others (if there are any) write
+// zeros over the gradient.
+constexpr int kSmallThreads = 1024, kSmallEach = 8, kSmall = kSmallThreads * kSmallEach;
+template <class TW>
 __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const void* __restrict__ tokens, int bits, int classes, Sorted out,
-                                                             int n, int digit_bits, int passes, unsigned char* there) {
+                                                             int n, int digit_bits, int passes,
+                                                             typename TW::Elem* __restrict__ weight, long long weight_stride, int width) {
   constexpr int WAVES = kSmallThreads / 64;
   __shared__ int next[WAVES][kDigits];
   __shared__ int keys[kSmall], rows[kSmall], slots[WAVES];
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, base = wave * (64 * kSmallEach);
-  for (int i = tid * 16; i < classes; i += kSmallThreads * 16) *reinterpret_cast<uint4*>(there + i) = uint4{};  // (256 bytes at a time are there)
-  __syncthreads();
+  if (blockIdx.x > 0) {
+    const float zero[kEight] = {};
+    for (long long v = (blockIdx.x - 1) * WAVES + wave; v < classes; v += (gridDim.x - 1) * WAVES)
+      for (int col = lane * kEight; col < width; col += 64 * kEight) store_some<TW>(weight + v * weight_stride + col, width - col, zero);
+    return;
+  }
   int key[kSmallEach], row[kSmallEach];
 #pragma unroll
   for (int q = 0; q < kSmallEach; ++q) {
     const int i = base + q * 64 + lane;
     key[q] = i < n ? key_of(tokens, bits, i, classes) : 0;
     row[q] = i;
-    if (i < n && key[q] < classes) there[key[q]] = 1;
   }
   const int mask = (1 << digit_bits) - 1;
   for (int pass = 0; pass < passes; ++pass) {
@@ -300,12 +305,12 @@ __global__ __launch_bounds__(kThreads) void k_sort_move(const void* __restrict__
 
 // --------------------------------------------------------------- the gradient
 
-constexpr int kPiece = 64;  // sorted rows that are summed together
+constexpr int kPiece = 64, kShort = 16;  // sorted rows that are summed together
 
 struct SumArgs {
   const int* key;
   const int* row;
-  int rows, classes, width, pieces, blocks;
+  int rows, classes, width, piece, pieces, blocks;
   float scale;
   long long grad_stride, weight_stride;
   float* partial;  // [pieces][2][width]: the sum that the piece begins with, and the one it ends with
@@ -321,7 +326,7 @@ __device__ __forceinline__ void put_class(typename TW::Elem* to, int left, const
   store_some<TW>(to, left, o);
 }
 
-// A wave sums 64 sorted rows in 512 columns.
+// A wave sums a piece of the sorted rows in 512 columns.
 template <class TG, class TW>
 __global__ __launch_bounds__(kThreads) void k_embed_sums(SumArgs a, const typename TG::Elem* __restrict__ grad,
                                                          typename TW::Elem* __restrict__ weight) {
@@ -329,7 +334,7 @@ __global__ __launch_bounds__(kThreads) void k_embed_sums(SumArgs a, const typena
   const long long item = (long long)blockIdx.x * kWaves + uniform(int(threadIdx.x / 64));
   if (item >= (long long)a.pieces * a.blocks) return;
   const int piece = int(item / a.blocks), col = (int(item % a.blocks) * 64 + lane) * kEight, left = a.width - col;
-  const int from = piece * kPiece, to = min(a.rows, from + kPiece);
+  const int from = piece * a.piece, to = min(a.rows, from + a.piece);
   // one sorted row a lane; the loop passes them on
   const int mine = from + lane < to ? a.key[from + lane] : a.classes;
   const int mine_row = from + lane < to ? a.row[from + lane] : 0;
@@ -381,7 +386,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(SumArgs a, typen
   __shared__ float slots[kJoinWaves][kEight][64];
   const int lane = threadIdx.x % 64, wave = uniform(int(threadIdx.x / 64));
   const int piece = int(blockIdx.x / unsigned(a.blocks)), col = (int(blockIdx.x % unsigned(a.blocks)) * 64 + lane) * kEight;
-  const int left = a.width - col, from = piece * kPiece, to = from + kPiece;
+  const int left = a.width - col, from = piece * a.piece, to = from + a.piece;
   if (to >= a.rows) return;
   const int key = a.key[to];
   if (key >= a.classes || a.key[to - 1] != key) return;                  // nothing goes on
@@ -390,7 +395,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(SumArgs a, typen
   int many = 0;
   for (;;) {
     const long long p = (long long)piece + 1 + many + lane;
-    const unsigned long long same = __ballot(p < a.pieces && a.key[min(p, (long long)a.pieces - 1) * kPiece] == key);
+    const unsigned long long same = __ballot(p < a.pieces && a.key[min(p, (long long)a.pieces - 1) * a.piece] == key);
     if (~same == 0ull) {
       many += 64;
       continue;
@@ -446,6 +451,9 @@ int done() {
   return e == hipSuccess ? ACDC_OK : hip_fail(e);
 }
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
+int blocks_of(int32_t width) { return int((int64_t(width) + 64 * kEight - 1) / (64 * kEight)); }
+// Short pieces where long ones would leave most of the card idle.
+int piece_of(int64_t rows, int32_t width) { return rows / kPiece * blocks_of(width) < 2048 ? kShort : kPiece; }
 struct Layout {
   size_t key[2], row[2], counts, totals, there, partial, bytes;
 };
@@ -465,7 +473,7 @@ Layout layout(int64_t rows, int32_t width, int32_t classes) {
   w.counts = take((n + kTile - 1) / kTile * kDigits * 4);
   w.totals = take(kDigits * 4);
   w.there = take(size_t(classes));
-  w.partial = take((n + kPiece - 1) / kPiece * 2 * size_t(width) * 4);
+  w.partial = take((n + piece_of(rows, width) - 1) / piece_of(rows, width) * 2 * size_t(width) * 4);
   w.bytes = next;
   return w;
 }
@@ -516,7 +524,7 @@ extern "C" int acdc_embedding_forward(const void* tokens, int32_t token_bits, co
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   // parts of a row where few rows would leave the card idle
   const int64_t most = (width + 64 * kEight - 1) / (64 * kEight);
-  const int split = int(std::clamp<int64_t>(2048 / rows, 1, most));
+  const int split = int(std::clamp<int64_t>((rows >= 8192 ? 32768 : 2048) / rows, 1, most));
   with_types(weight_type, out_type, [&]<class TW, class TO>() {
     auto go = [&]<int ROWS>() {
       const int64_t items = (rows + ROWS - 1) / ROWS * split;
@@ -559,14 +567,18 @@ extern "C" int acdc_embedding_backward(const void* tokens, int32_t token_bits, c
   while ((int64_t(classes) >> key_bits) != 0) ++key_bits;
   const int passes = (key_bits + 8) / 9, digit_bits = (key_bits + passes - 1) / passes, n = int(rows);
   int at = 0;
-  if (rows > 0 && rows <= kSmall && classes <= kSmallClasses) {
-    hipLaunchKernelGGL(k_sort_small, dim3(1), dim3(kSmallThreads), 0, s, tokens, token_bits, classes, pairs[0], n, digit_bits, passes,
-                       there);
+  const bool small = rows <= kSmall;
+  if (small) {
+    const int64_t fill = accumulate != 0 ? 0 : std::min<int64_t>((classes + 15) / 16, 1023);
+    with_types(out_type, weight_type, [&]<class TG, class TW>() {
+      hipLaunchKernelGGL(k_sort_small<TW>, dim3(unsigned(1 + fill)), dim3(kSmallThreads), 0, s, tokens, token_bits, classes, pairs[0], n,
+                         digit_bits, passes, static_cast<typename TW::Elem*>(grad_weight), (long long)weight_stride, width);
+    });
   } else {
     hipLaunchKernelGGL(k_embed_clear, dim3(unsigned(std::min<int64_t>((classes + kThreads - 1) / kThreads, 1024))), dim3(kThreads), 0,
                        s, there, classes);
     const int tiles = (n + kTile - 1) / kTile;
-    for (int pass = 0; pass < passes && rows > 0; ++pass, at ^= 1) {
+    for (int pass = 0; pass < passes; ++pass, at ^= 1) {
       const void* from = pass == 0 ? tokens : nullptr;
       hipLaunchKernelGGL(k_sort_count, dim3(unsigned(tiles)), dim3(kThreads), 0, s, from, token_bits, classes, pairs[at], n,
                          pass * digit_bits, (1 << digit_bits) - 1, counts, there);
@@ -577,12 +589,12 @@ extern "C" int acdc_embedding_backward(const void* tokens, int32_t token_bits, c
   }
   with_types(out_type, weight_type, [&]<class TG, class TW>() {
     typename TW::Elem* out = static_cast<typename TW::Elem*>(grad_weight);
-    if (accumulate == 0)
+    if (accumulate == 0 && !small)
       hipLaunchKernelGGL(k_embed_zeros<TW>, dim3(unsigned(std::min<int64_t>((classes + kWaves - 1) / kWaves, 8192))), dim3(kThreads),
                          0, s, there, classes, width, out, (long long)weight_stride);
     if (rows == 0) return;
-    const int blocks = (width + 64 * kEight - 1) / (64 * kEight), pieces = int((rows + kPiece - 1) / kPiece);
-    const SumArgs a{pairs[at].key, pairs[at].row, int(rows), classes, width, pieces, blocks, scale, out_stride, weight_stride,
+    const int blocks = blocks_of(width), piece = piece_of(rows, width), pieces = int((rows + piece - 1) / piece);
+    const SumArgs a{pairs[at].key, pairs[at].row, int(rows), classes, width, piece, pieces, blocks, scale, out_stride, weight_stride,
                     reinterpret_cast<float*>(ws + w.partial), accumulate != 0};
     const unsigned groups = unsigned((int64_t(pieces) * blocks + kWaves - 1) / kWaves);
     hipLaunchKernelGGL((k_embed_sums<TG, TW>), dim3(groups), dim3(kThreads), 0, s, a, static_cast<const typename TG::Elem*>(grad_out), out);
