@@ -20,6 +20,7 @@ namespace acdc {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kSpan = 64 * kEight;  // columns that a wave takes at a time
 
 // `classes` for a row that takes no part: sorted behind all others.
 __device__ __forceinline__ int key_of(const void* tokens, int bits, long long r, int classes) {
@@ -52,17 +53,18 @@ __global__ __launch_bounds__(kThreads) void k_embed(const void* __restrict__ tok
       fill[q] = t < 0 ? 0.f : __builtin_nanf("");
     }
 #pragma unroll 2
-    for (int col = (part * 64 + lane) * kEight; col < width; col += split * 64 * kEight) {
+    for (int col = part * kSpan; col < width; col += split * kSpan) {
+      const Columns<kApart<TW, TO>> at(col, lane, width);
       float v[ROWS][kEight];
 #pragma unroll
       for (int q = 0; q < ROWS; ++q)
-        if (q < many) load_some<TW>(from[q] + col, width - col, 0.f, v[q]);
+        if (q < many) at.template load<TW>(from[q], v[q]);
 #pragma unroll
       for (int q = 0; q < ROWS; ++q) {
         if (q >= many) continue;
 #pragma unroll
         for (int i = 0; i < kEight; ++i) v[q][i] = there[q] ? v[q][i] * scale : fill[q];
-        store_some<TO>(out + (long long)(first + q) * out_stride + col, width - col, v[q]);
+        at.template store<TO>(out + (long long)(first + q) * out_stride, v[q]);
       }
     }
   }
@@ -70,12 +72,12 @@ __global__ __launch_bounds__(kThreads) void k_embed(const void* __restrict__ tok
 
 // ------------------------------------------------------------------- the sort
 
-// Stable, least digit first, in passes of up to nine bits.
+// Stable, least digit first, in passes of up to ten bits: 1000 classes take one, 2^20 two.
 struct Sorted {
   int* key;
   int* row;
 };
-constexpr int kDigits = 512;
+constexpr int kMostBits = 10, kDigits = 1 << kMostBits;
 
 // next[wave][digit] goes from how many pairs of the digit a wave has to how many the waves
 // before it have; returns how many all have.
@@ -148,7 +150,7 @@ __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const void* __rest
   if (blockIdx.x > 0) {
     const float zero[kEight] = {};
     for (long long v = (blockIdx.x - 1) * WAVES + wave; v < classes; v += (gridDim.x - 1) * WAVES)
-      for (int col = lane * kEight; col < width; col += 64 * kEight) store_some<TW>(weight + v * weight_stride + col, width - col, zero);
+      for (int col = 0; col < width; col += kSpan) Columns<kApart<TW, TW>>(col, lane, width).template store<TW>(weight + v * weight_stride, zero);
     return;
   }
   int key[kSmallEach], row[kSmallEach];
@@ -317,13 +319,13 @@ struct SumArgs {
   bool add;
 };
 
-template <class TW>
-__device__ __forceinline__ void put_class(typename TW::Elem* to, int left, const float (&v)[kEight], float scale, bool add) {
+template <class TW, class C>
+__device__ __forceinline__ void put_class(typename TW::Elem* row, const C& at, const float (&v)[kEight], float scale, bool add) {
   float o[kEight] = {};
-  if (add) load_some<TW>(to, left, 0.f, o);
+  if (add) at.template load<TW>(row, o);
 #pragma unroll
   for (int i = 0; i < kEight; ++i) o[i] += scale * v[i];
-  store_some<TW>(to, left, o);
+  at.template store<TW>(row, o);
 }
 
 // A wave sums a piece of the sorted rows in 512 columns.
@@ -333,7 +335,8 @@ __global__ __launch_bounds__(kThreads) void k_embed_sums(SumArgs a, const typena
   const int lane = threadIdx.x % 64;
   const long long item = (long long)blockIdx.x * kWaves + uniform(int(threadIdx.x / 64));
   if (item >= (long long)a.pieces * a.blocks) return;
-  const int piece = int(item / a.blocks), col = (int(item % a.blocks) * 64 + lane) * kEight, left = a.width - col;
+  const int piece = int(item / a.blocks);
+  const Columns<kApart<TG, TW>> at(int(item % a.blocks) * kSpan, lane, a.width);
   const int from = piece * a.piece, to = min(a.rows, from + a.piece);
   // one sorted row a lane; the loop passes them on
   const int mine = from + lane < to ? a.key[from + lane] : a.classes;
@@ -348,18 +351,18 @@ __global__ __launch_bounds__(kThreads) void k_embed_sums(SumArgs a, const typena
     int key[AHEAD];
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) {
-      const int at = min(i + q, to - from - 1);
-      key[q] = __builtin_amdgcn_readlane(mine, at);
-      const long long r = __builtin_amdgcn_readlane(mine_row, at);
-      if (key[q] < a.classes && left > 0) load_some<TG>(grad + r * a.grad_stride + col, left, 0.f, v[q]);
+      const int k = min(i + q, to - from - 1);
+      key[q] = __builtin_amdgcn_readlane(mine, k);
+      const long long r = __builtin_amdgcn_readlane(mine_row, k);
+      if (key[q] < a.classes && at.any()) at.template load<TG>(grad + r * a.grad_stride, v[q]);
     }
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) {
       if (i + q >= to - from) break;
       if (key[q] != current) {  // the class before ends here
-        if (left > 0) {
-          if (began) put_class<TW>(weight + current * a.weight_stride + col, left, s, a.scale, a.add);
-          else store_some<F32, false>(a.partial + (long long)piece * 2 * a.width + col, left, s);
+        if (at.any()) {
+          if (began) put_class<TW>(weight + current * a.weight_stride, at, s, a.scale, a.add);
+          else at.template store<F32, false>(a.partial + (long long)piece * 2 * a.width, s);
         }
 #pragma unroll
         for (int c = 0; c < kEight; ++c) s[c] = 0.f;
@@ -371,11 +374,9 @@ __global__ __launch_bounds__(kThreads) void k_embed_sums(SumArgs a, const typena
       for (int c = 0; c < kEight; ++c) s[c] += v[q][c];
     }
   }
-  if (current >= a.classes || left <= 0) return;
-  if (current == after || !began)
-    store_some<F32, false>(a.partial + ((long long)piece * 2 + (began ? 1 : 0)) * a.width + col, left, s);
-  else
-    put_class<TW>(weight + current * a.weight_stride + col, left, s, a.scale, a.add);
+  if (current >= a.classes || !at.any()) return;
+  if (current == after || !began) at.template store<F32, false>(a.partial + ((long long)piece * 2 + (began ? 1 : 0)) * a.width, s);
+  else put_class<TW>(weight + current * a.weight_stride, at, s, a.scale, a.add);
 }
 
 // The class that begins in a piece and goes on behind it: its partial sums together, by
@@ -385,8 +386,9 @@ template <class TW>
 __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(SumArgs a, typename TW::Elem* __restrict__ weight) {
   __shared__ float slots[kJoinWaves][kEight][64];
   const int lane = threadIdx.x % 64, wave = uniform(int(threadIdx.x / 64));
-  const int piece = int(blockIdx.x / unsigned(a.blocks)), col = (int(blockIdx.x % unsigned(a.blocks)) * 64 + lane) * kEight;
-  const int left = a.width - col, from = piece * a.piece, to = from + a.piece;
+  const int piece = int(blockIdx.x / unsigned(a.blocks));
+  const Columns<true> at(int(blockIdx.x % unsigned(a.blocks)) * kSpan, lane, a.width);
+  const int from = piece * a.piece, to = from + a.piece;
   if (to >= a.rows) return;
   const int key = a.key[to];
   if (key >= a.classes || a.key[to - 1] != key) return;                  // nothing goes on
@@ -405,12 +407,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(SumArgs a, typen
   }
   float s[kEight] = {};
   const int per = (many + kJoinWaves - 1) / kJoinWaves, first = min(many, wave * per), last = min(many, first + per);
-  if (left > 0) {
-    if (wave == 0) load_some<F32>(a.partial + ((long long)piece * 2 + 1) * a.width + col, left, 0.f, s);
+  if (at.any()) {
+    if (wave == 0) at.template load<F32>(a.partial + ((long long)piece * 2 + 1) * a.width, s);
 #pragma unroll 4
     for (int p = first; p < last; ++p) {
       float v[kEight];
-      load_some<F32>(a.partial + (long long)(piece + 1 + p) * 2 * a.width + col, left, 0.f, v);
+      at.template load<F32>(a.partial + (long long)(piece + 1 + p) * 2 * a.width, v);
 #pragma unroll
       for (int c = 0; c < kEight; ++c) s[c] += v[c];
     }
@@ -418,12 +420,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(SumArgs a, typen
 #pragma unroll
   for (int c = 0; c < kEight; ++c) slots[wave][c][lane] = s[c];
   __syncthreads();
-  if (wave != 0 || left <= 0) return;
+  if (wave != 0 || !at.any()) return;
 #pragma unroll
   for (int w = 1; w < kJoinWaves; ++w)
 #pragma unroll
     for (int c = 0; c < kEight; ++c) s[c] += slots[w][c][lane];
-  put_class<TW>(weight + key * a.weight_stride + col, left, s, a.scale, a.add);
+  put_class<TW>(weight + key * a.weight_stride, at, s, a.scale, a.add);
 }
 
 __global__ __launch_bounds__(kThreads) void k_embed_clear(unsigned char* there, int classes) {
@@ -438,7 +440,7 @@ __global__ __launch_bounds__(kThreads) void k_embed_zeros(const unsigned char* _
   const float zero[kEight] = {};
   for (int v = blockIdx.x * kWaves + threadIdx.x / 64; v < classes; v += gridDim.x * kWaves) {
     if (there[v] != 0) continue;
-    for (int col = lane * kEight; col < width; col += 64 * kEight) store_some<TW>(weight + v * weight_stride + col, width - col, zero);
+    for (int col = 0; col < width; col += kSpan) Columns<kApart<TW, TW>>(col, lane, width).template store<TW>(weight + v * weight_stride, zero);
   }
 }
 
@@ -451,7 +453,7 @@ int done() {
   return e == hipSuccess ? ACDC_OK : hip_fail(e);
 }
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
-int blocks_of(int32_t width) { return int((int64_t(width) + 64 * kEight - 1) / (64 * kEight)); }
+int blocks_of(int32_t width) { return int((int64_t(width) + kSpan - 1) / kSpan); }
 // Short pieces where long ones would leave most of the card idle.
 int piece_of(int64_t rows, int32_t width) { return rows / kPiece * blocks_of(width) < 2048 ? kShort : kPiece; }
 struct Layout {
@@ -479,7 +481,7 @@ Layout layout(int64_t rows, int32_t width, int32_t classes) {
 }
 bool sizes_ok(int64_t rows, int32_t width, int32_t classes) {
   // (a grid has fewer than 2^32 lanes)
-  if (rows >= 0 && rows <= kMostRows && width >= 1 && (rows / kPiece + 1) * (int64_t(width) / (64 * kEight) + 1) > (1 << 22)) return false;
+  if (rows >= 0 && rows <= kMostRows && width >= 1 && (rows / kPiece + 1) * (int64_t(width) / kSpan + 1) > (1 << 22)) return false;
   return rows >= 0 && rows <= kMostRows && width >= 1 && width <= kMostWidth && classes >= 1 && classes <= kMostClasses;
 }
 bool matrix_ok(const void* p, int32_t dtype, int64_t stride, int64_t rows, int32_t width) {
@@ -523,7 +525,7 @@ extern "C" int acdc_embedding_forward(const void* tokens, int32_t token_bits, co
   if (rows == 0) return ACDC_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   // parts of a row where few rows would leave the card idle
-  const int64_t most = (width + 64 * kEight - 1) / (64 * kEight);
+  const int64_t most = (width + kSpan - 1) / kSpan;
   const int split = int(std::clamp<int64_t>((rows >= 8192 ? 32768 : 2048) / rows, 1, most));
   with_types(weight_type, out_type, [&]<class TW, class TO>() {
     auto go = [&]<int ROWS>() {
@@ -565,7 +567,7 @@ extern "C" int acdc_embedding_backward(const void* tokens, int32_t token_bits, c
   // passes of as many bits each; `classes` is a key too
   int key_bits = 0;
   while ((int64_t(classes) >> key_bits) != 0) ++key_bits;
-  const int passes = (key_bits + 8) / 9, digit_bits = (key_bits + passes - 1) / passes, n = int(rows);
+  const int passes = (key_bits + kMostBits - 1) / kMostBits, digit_bits = (key_bits + passes - 1) / passes, n = int(rows);
   int at = 0;
   const bool small = rows <= kSmall;
   if (small) {

@@ -180,7 +180,8 @@ EMBED = [(1, 1, 1, "float32", "float32", 64), (3, 7, 5, "bfloat16", "float32", 3
          (65, 513, 255, "float32", "bfloat16", 64), (128, 33, 1, "bfloat16", "bfloat16", 64), (500, 64, 256, "float32", "float32", 32),
          (2048, 16, 65535, "bfloat16", "bfloat16", 64), (2049, 9, 65536, "float32", "float32", 64), (5000, 20, 7, "float32", "float32", 64),
          (30000, 3, 70000, "float32", "float32", 32), (70000, 2, 3, "bfloat16", "float32", 64), (300, 1025, 40, "bfloat16", "bfloat16", 64),
-         (16, 4096, 1000, "float32", "float32", 64)]
+         (16, 4096, 1000, "float32", "float32", 64), (9000, 10, 1023, "float32", "float32", 64),
+         (9000, 600, 1024, "bfloat16", "float32", 64), (8192, 5, 300000, "float32", "bfloat16", 64), (8193, 5, 1100000, "bfloat16", "bfloat16", 32)]
 
 
 def tokens_of(torch, n, classes, bits, gen, idle=0.1):
