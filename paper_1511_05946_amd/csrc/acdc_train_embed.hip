@@ -179,6 +179,7 @@ __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const void* __rest
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < kSmallEach; ++q) {
+      if (base + q * 64 >= n) break;
       const bool here = base + q * 64 + lane < n;
       const int to = place_of(next[wave], here, (key[q] >> shift) & mask, digit_bits);
       if (here) {

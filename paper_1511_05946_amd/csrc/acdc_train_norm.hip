@@ -43,9 +43,26 @@ struct RowSum {
   }
 };
 
-template <int LANES>
+template <int LANES, int THREADS = kThreads>
 struct Group {
-  static constexpr int WG = LANES < kThreads ? kThreads : LANES, ROWS = WG / LANES;
+  static constexpr int WG = LANES < THREADS ? THREADS : LANES, ROWS = WG / LANES;
+};
+// The two sums over the rows: where they go, and whether they are added there.
+struct Sums {
+  void *weight, *bias;  // null: not wanted
+  int32_t dtype;
+  bool add;
+  __device__ __forceinline__ void put(bool bias_too, int col, float s) const {
+    void* out = bias_too ? bias : weight;
+    if (out == nullptr) return;
+    if (dtype == ACDC_F32) {
+      float* to = static_cast<float*>(out) + col;
+      *to = add ? *to + s : s;
+    } else {
+      __bf16* to = static_cast<__bf16*>(out) + col;
+      *to = __bf16(add ? float(*to) + s : s);
+    }
+  }
 };
 
 // A row in the registers of LANES lanes, NC times eight values each.
@@ -152,12 +169,13 @@ struct BackArgs {
   const float2* saved;
   Vector weight;
   float* sums;  // [workgroups][2][width], null: not wanted
+  Sums out;     // of a single workgroup, which writes them itself
   int rows, width;
 };
 
-template <class TX, class TY, int LANES, int NC>
-__global__ __launch_bounds__(Group<LANES>::WG) void k_norm_back(BackArgs<TX, TY> a) {
-  constexpr int WG = Group<LANES>::WG, ROWS = Group<LANES>::ROWS, SPAN = LANES * NC * kEight;
+template <class TX, class TY, int LANES, int NC, int THREADS>
+__global__ __launch_bounds__((Group<LANES, THREADS>::WG)) void k_norm_back(BackArgs<TX, TY> a) {
+  constexpr int WG = Group<LANES, THREADS>::WG, ROWS = Group<LANES, THREADS>::ROWS, SPAN = LANES * NC * kEight;
   __shared__ float slots[2 * WG / 64];
   __shared__ float both[ROWS > 1 ? ROWS : 1][ROWS > 1 ? SPAN : 1];
   RowSum<LANES> sum{slots};
@@ -204,13 +222,23 @@ __global__ __launch_bounds__(Group<LANES>::WG) void k_norm_back(BackArgs<TX, TY>
   }
   if (a.sums == nullptr) return;
   float* out = a.sums + (long long)blockIdx.x * 2 * width;
+  const bool alone = gridDim.x == 1;
   if constexpr (ROWS == 1) {
 #pragma unroll
     for (int q = 0; q < NC; ++q) {
       const int col = (lane + q * LANES) * kEight;
       if (col >= width) continue;
-      store_some<F32, false>(out + col, width - col, gw[q]);
-      store_some<F32, false>(out + width + col, width - col, gb[q]);
+      if (alone) {
+#pragma unroll
+        for (int i = 0; i < kEight; ++i) {
+          if (col + i >= width) break;
+          a.out.put(false, col + i, gw[q][i]);
+          a.out.put(true, col + i, gb[q][i]);
+        }
+      } else {
+        store_some<F32, false>(out + col, width - col, gw[q]);
+        store_some<F32, false>(out + width + col, width - col, gb[q]);
+      }
     }
   } else {
 #pragma unroll
@@ -223,9 +251,10 @@ __global__ __launch_bounds__(Group<LANES>::WG) void k_norm_back(BackArgs<TX, TY>
       __syncthreads();
       for (int col = threadIdx.x; col < width; col += WG) {
         float s = 0.f;
-#pragma unroll
+#pragma unroll 16
         for (int p = 0; p < ROWS; ++p) s += both[p][col];
-        out[k * width + col] = s;
+        if (alone) a.out.put(k == 1, col, s);
+        else out[k * width + col] = s;
       }
     }
   }
@@ -295,8 +324,7 @@ __global__ __launch_bounds__(64) void k_norm_columns(BackArgs<TX, TY> a, int eac
 // The parts' sums together, in order: 64 columns a workgroup, its waves take the parts
 // in turn.
 constexpr int kSumWaves = 8;
-__global__ __launch_bounds__(64 * kSumWaves) void k_norm_sums(const float* __restrict__ sums, int parts, int width, void* gw,
-                                                             void* gb, int dtype, bool add) {
+__global__ __launch_bounds__(64 * kSumWaves) void k_norm_sums(const float* __restrict__ sums, int parts, int width, Sums out) {
   __shared__ float slots[kSumWaves][64];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, at = blockIdx.x * 64 + lane;  // of 2 width
   float s = 0.f;
@@ -310,16 +338,7 @@ __global__ __launch_bounds__(64 * kSumWaves) void k_norm_sums(const float* __res
   s = 0.f;
 #pragma unroll
   for (int w = 0; w < kSumWaves; ++w) s += slots[w][lane];
-  void* out = at < width ? gw : gb;
-  const int col = at < width ? at : at - width;
-  if (out == nullptr) return;
-  if (dtype == ACDC_F32) {
-    float* to = static_cast<float*>(out) + col;
-    *to = add ? *to + s : s;
-  } else {
-    __bf16* to = static_cast<__bf16*>(out) + col;
-    *to = __bf16(add ? float(*to) + s : s);
-  }
+  out.put(at >= width, at < width ? at : at - width, s);
 }
 
 // ------------------------------------------------------------------ on the host
@@ -364,13 +383,15 @@ Span span_of(const void* p, int64_t rows, int64_t stride, int64_t width, int32_t
 }
 bool apart(const Span& a, const Span& b) { return a.to <= b.from || b.to <= a.from; }
 
+// Few short rows: one workgroup of 1024 lanes, and a launch less.
+bool few(int64_t rows, int32_t width) { return rows <= (width <= 256 ? 64 : width <= 1024 ? 16 : 1); }
 // Parts whose columns' sums the backward pass leaves: the workgroups of its launch (long
 // rows: those of the second one).
 int parts_of(int64_t rows, int32_t width) {
   if (rows == 0) return 0;
   if (width > kHeld) return int(std::min<int64_t>(rows, 64));
   int per = 1;
-  with_row(width, [&]<int LANES, int NC>() { per = Group<LANES>::ROWS; });
+  with_row(width, [&]<int LANES, int NC>() { per = few(rows, width) ? 1024 / LANES : Group<LANES>::ROWS; });
   return int(std::min<int64_t>((rows + per - 1) / per, kMostParts));
 }
 
@@ -446,12 +467,13 @@ extern "C" int acdc_norm_backward(const void* x, int32_t x_type, int64_t x_strid
   if (!aligned_to(workspace, 16)) return ACDC_ERR_INVALID_ARG;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const int parts = parts_of(rows, width);
+  const Sums out_sums{grad_weight, grad_bias, grads_type, accumulate != 0};
   if (rows > 0 && (sums || grad_x != nullptr)) {
     const int rc = with_types(x_type, y_type, [&]<class TX, class TY>() {
       const BackArgs<TX, TY> a{static_cast<const typename TX::Elem*>(x), static_cast<const typename TY::Elem*>(grad_y),
                                static_cast<typename TX::Elem*>(grad_x), x_stride, grad_y_stride, grad_x_stride,
                                reinterpret_cast<const float2*>(saved), Vector{weight, vector_type},
-                               sums ? static_cast<float*>(workspace) : nullptr, int(rows), width};
+                               sums ? static_cast<float*>(workspace) : nullptr, out_sums, int(rows), width};
       if (width > kHeld) {
         // the sums first: grad_x may take grad_y's place
         if (sums) {
@@ -462,15 +484,21 @@ extern "C" int acdc_norm_backward(const void* x, int32_t x_type, int64_t x_strid
           hipLaunchKernelGGL((k_norm_back_long<TX, TY, 1024>), dim3(unsigned(std::min<int64_t>(rows, 1 << 16))), dim3(1024), 0, s, a);
       } else {
         with_row(width, [&]<int LANES, int NC>() {
-          hipLaunchKernelGGL((k_norm_back<TX, TY, LANES, NC>), dim3(unsigned(parts)), dim3(Group<LANES>::WG), 0, s, a);
+          if constexpr (LANES <= 64) {
+            if (few(rows, width)) {
+              hipLaunchKernelGGL((k_norm_back<TX, TY, LANES, NC, 1024>), dim3(1), dim3(1024), 0, s, a);
+              return;
+            }
+          }
+          hipLaunchKernelGGL((k_norm_back<TX, TY, LANES, NC, kThreads>), dim3(unsigned(parts)), dim3(Group<LANES>::WG), 0, s, a);
         });
       }
       return done();
     });
     if (rc != ACDC_OK) return rc;
   }
-  if (!sums || (rows == 0 && accumulate != 0)) return ACDC_OK;
+  if (!sums || (rows == 0 && accumulate != 0) || (parts == 1 && width <= kHeld)) return ACDC_OK;
   hipLaunchKernelGGL(k_norm_sums, dim3(unsigned((2 * int64_t(width) + 63) / 64)), dim3(64 * kSumWaves), 0, s,
-                     static_cast<const float*>(workspace), parts, width, grad_weight, grad_bias, grads_type, accumulate != 0);
+                     static_cast<const float*>(workspace), parts, width, out_sums);
   return done();
 }

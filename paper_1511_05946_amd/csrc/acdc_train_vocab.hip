@@ -28,6 +28,12 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kNegMax = -3.402823466e38f;
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+// The product's rounding is 2^-24 |d| of the result: float32 gradients would show it.
+template <bool EXACT>
+__device__ __forceinline__ float exp_as(float d) {
+  if constexpr (EXACT) return expf(d);
+  else return exp_of(d);
+}
 
 // ------------------------------------------------------------ the rows in use
 
@@ -134,16 +140,27 @@ __global__ __launch_bounds__(kWide) void k_vocab_rows(const void* __restrict__ t
 // Rows as the matrix cores take them: bfloat16 (three planes for float32), `padded`
 // wide, at multiples of 16 bytes.  With `order` the packed rows, zeros past *count.
 template <class T>
-__global__ __launch_bounds__(256) void k_vocab_pack(const typename T::Elem* __restrict__ x, long long stride,
-                                                    const int* __restrict__ order, const int* __restrict__ count, int rows,
-                                                    int width, __bf16* __restrict__ out, long long plane, int padded) {
-  const int per = padded / 8, used = order != nullptr ? *count : rows;
-  const long long chunks = (long long)rows * per;
+struct Pack {
+  const typename T::Elem* x;
+  long long stride;
+  const int* order;
+  int rows;
+  __bf16* out;
+  long long plane;
+};
+// Two of them in one launch (the second may have no rows).
+template <class T>
+__global__ __launch_bounds__(256) void k_vocab_pack(Pack<T> first, Pack<T> second, const int* __restrict__ count, int width,
+                                                    int padded) {
+  const int per = padded / 8, used = *count;
+  const long long split = (long long)first.rows * per, chunks = split + (long long)second.rows * per;
   for (long long c = blockIdx.x * 256ll + threadIdx.x; c < chunks; c += gridDim.x * 256ll) {
-    const int r = int(c / per), col = int(c % per) * 8;
+    const Pack<T>& job = c < split ? first : second;
+    const long long at = c < split ? c : c - split;
+    const int r = int(at / per), col = int(at % per) * 8;
     float v[8] = {};
-    if (r < used) {
-      const typename T::Elem* from = x + (order != nullptr ? order[r] : r) * stride + col;
+    if (job.order == nullptr || r < used) {
+      const typename T::Elem* from = job.x + (job.order != nullptr ? job.order[r] : r) * job.stride + col;
       if (col + 8 <= width) {
 #pragma unroll
         for (int q = 0; q < 8 / T::kPer; ++q) {
@@ -157,7 +174,7 @@ __global__ __launch_bounds__(256) void k_vocab_pack(const typename T::Elem* __re
           if (col + i < width) v[i] = T::one(from[i]);
       }
     }
-    __bf16* to = out + (long long)r * padded + col;
+    __bf16* to = job.out + (long long)r * padded + col;
     if constexpr (std::is_same_v<T, BF16>) {
       bf16x8 o;
 #pragma unroll
@@ -172,7 +189,7 @@ __global__ __launch_bounds__(256) void k_vocab_pack(const typename T::Elem* __re
         for (int p = 0; p < 3; ++p) o[p][i] = s.p[p];
       }
 #pragma unroll
-      for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8*>(to + p * plane) = o[p];
+      for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8*>(to + p * job.plane) = o[p];
     }
   }
 }
@@ -185,7 +202,7 @@ enum class Keep { kNothing, kBf16, kF32 };
 
 // Statistics of a tile's rows: their (max, sum) into parts[tile][row], and the target's
 // logit.  m runs over classes, n over packed rows; `classes` are those of the piece.
-template <Keep KEEP>
+template <Keep KEEP, bool EXACT>
 struct StatsOut {
   const int* target;
   float2* parts;
@@ -243,7 +260,7 @@ struct StatsOut {
       for (int m = 0; m < MI; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          acc[m][n][i] = exp_of(acc[m][n][i] - tops[n]);
+          acc[m][n][i] = exp_as<EXACT>(acc[m][n][i] - tops[n]);
           sum += acc[m][n][i];
         }
       Pair p = swap16(sum);
@@ -303,7 +320,7 @@ struct SlopeOut {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int v = spot.m(m + i / 4) + i % 4;
-          float y = -exp_of(acc[m + i / 4][n][i % 4] - k.top) * k.slope;
+          float y = -exp_as<PLANES == 3>(acc[m + i / 4][n][i % 4] - k.top) * k.slope;
           if (v == t) y += k.g;
           if (v >= classes) y = 0.f;
           if constexpr (PLANES == 1) {
@@ -336,7 +353,7 @@ __global__ __launch_bounds__(256) void k_vocab_slopes(Rows rows, const RowSlope*
   const int r = int(item / blocks), col = (int(item % blocks) * 64 + lane) * 8;
   if (r >= used || col >= ld) return;
   const RowSlope k = slope[r];
-  const float f = -k.slope * exp_of(parts[(long long)(col / tile) * padded + r].x - k.top);
+  const float f = -k.slope * expf(parts[(long long)(col / tile) * padded + r].x - k.top);
   const long long at = (long long)r * ld + col;
   const Eight e = *reinterpret_cast<const Eight*>(static_cast<const E*>(kept) + at);
   bf16x8 o[PLANES];
@@ -429,6 +446,7 @@ __global__ __launch_bounds__(256) void k_vocab_sum(const float* __restrict__ sum
     f32x4 v = {};
     if (from >= 0) {
       const float* p = sums + from * padded + col;
+#pragma unroll 16
       for (int k = 0; k < parts; ++k) v += *reinterpret_cast<const f32x4*>(p + k * part);
       v *= *factor;
     }
@@ -446,8 +464,15 @@ struct JoinOut {
   float* row_grads;
   RowSlope* slope;     // null: no gradient
   float* loss;         // [padded] weight times logp, null: not wanted
+  float* stats;        // up to 64 rows: the totals too, null: not here
   bool mean;
 };
+// stats = (loss, W) from the sum of weight times logp
+__device__ __forceinline__ void put_stats(float* stats, const Rows& rows, double sum, bool mean) {
+  const double total = *rows.total;
+  stats[0] = *rows.count == 0 ? 0.f : float(mean ? -sum / total : -sum);
+  stats[1] = float(total);
+}
 __global__ __launch_bounds__(1024) void k_vocab_join(Rows rows, const float2* __restrict__ parts, const float* __restrict__ logit,
                                                      int tiles, int padded, JoinOut out) {
   __shared__ float2 slots[16][64];
@@ -464,9 +489,9 @@ __global__ __launch_bounds__(1024) void k_vocab_join(Rows rows, const float2* __
       float m = top;
 #pragma unroll
       for (int q = 0; q < AHEAD; ++q) m = fmaxf(m, p[q].x);
-      sum *= exp_of(top - m);
+      sum *= expf(top - m);
 #pragma unroll
-      for (int q = 0; q < AHEAD; ++q) sum += p[q].y * exp_of(p[q].x - m);
+      for (int q = 0; q < AHEAD; ++q) sum += p[q].y * expf(p[q].x - m);
       top = m;
     }
   }
@@ -476,25 +501,31 @@ __global__ __launch_bounds__(1024) void k_vocab_join(Rows rows, const float2* __
   top = kNegMax;
   sum = 0.f;
   for (int w = 0; w < 16; ++w) top = fmaxf(top, slots[w][lane].x);
-  for (int w = 0; w < 16; ++w) sum += slots[w][lane].y * exp_of(slots[w][lane].x - top);
+  for (int w = 0; w < 16; ++w) sum += slots[w][lane].y * expf(slots[w][lane].x - top);
+  float loss = 0.f;
   if (i >= used) {
     if (out.slope != nullptr) out.slope[i] = RowSlope{0.f, 0.f, 0.f, -1};
-    if (out.loss != nullptr) out.loss[i] = 0.f;
-    return;
+  } else {
+    const int r = rows.order[i], t = rows.target[i];
+    // no class with a probability: no distribution
+    const float nan = sum > 0.f ? 0.f : __builtin_nanf("");
+    const float logp = t >= 0 ? (logit[i] - top) - logf(sum) + nan : __builtin_nanf("");
+    out.logp[r] = logp;
+    if (out.saved != nullptr) out.saved[r] = make_float2(top, sum);
+    const float w = rows.share[i];
+    loss = w * logp;
+    if (out.row_grads != nullptr) out.row_grads[r] = -(out.mean ? float(double(w) / *rows.total) : w);
+    if (out.slope != nullptr) {
+      const float g = t >= 0 ? -w : __builtin_nanf("");
+      out.slope[i] = RowSlope{top, g / sum, g, t};
+    }
   }
-  const int r = rows.order[i], t = rows.target[i];
-  // no class with a probability: no distribution
-  const float nan = sum > 0.f ? 0.f : __builtin_nanf("");
-  const float logp = t >= 0 ? (logit[i] - top) - logf(sum) + nan : __builtin_nanf("");
-  out.logp[r] = logp;
-  if (out.saved != nullptr) out.saved[r] = make_float2(top, sum);
-  if (out.loss == nullptr) return;
-  const float w = rows.share[i];
-  out.loss[i] = w * logp;
-  if (out.row_grads != nullptr) out.row_grads[r] = -(out.mean ? float(double(w) / *rows.total) : w);
-  if (out.slope != nullptr) {
-    const float g = t >= 0 ? -w : __builtin_nanf("");
-    out.slope[i] = RowSlope{top, g / sum, g, t};
+  if (out.loss != nullptr) out.loss[i] = loss;
+  if (out.stats != nullptr) {
+    double all = double(loss);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o);
+    if (lane == 0) put_stats(out.stats, rows, all, out.mean);
   }
 }
 
@@ -525,9 +556,7 @@ __global__ __launch_bounds__(kWide) void k_vocab_total(Rows rows, const float* _
   if (threadIdx.x == 0) {
     double all = 0.0;
     for (int k = 0; k < kWide / 64; ++k) all += sums[k];
-    const double total = *rows.total;
-    stats[0] = used == 0 ? 0.f : float(mean ? -all / total : -all);
-    stats[1] = float(total);
+    put_stats(stats, rows, all, mean);
   }
 }
 
@@ -560,9 +589,9 @@ struct Plan {
   int tile_classes() const { return !large_logits ? 64 : planes == 1 ? 256 : 128; }  // of the logits
 };
 int64_t tiles_of(int64_t m, int64_t n, int bm, int bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); }
-int parts_for(int64_t tiles, int64_t steps) {
-  // as many as give every CU a tile, of 8 steps at least
-  return int(std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), steps / 8, 64})));
+int parts_for(int64_t tiles, int64_t steps, int least) {
+  // as many as give every CU a tile, of `least` steps at least
+  return int(std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), steps / least, 64})));
 }
 Plan plan_for(int64_t rows, int32_t width, int32_t classes, int32_t dtype) {
   Plan p{};
@@ -581,10 +610,10 @@ Plan plan_for(int64_t rows, int32_t width, int32_t classes, int32_t dtype) {
   // half a card of large tiles is as fast as a card of small ones
   p.large_logits = tiles_of(piece, p.padded_rows, bm, bn) >= 128;
   const int64_t hidden = tiles_of(width, p.padded_rows, bm, bn), weight = tiles_of(width, piece, bm, 256);
-  p.large_hidden = hidden * parts_for(hidden, piece / step) >= 128;
-  p.large_weight = weight * parts_for(weight, p.padded_rows / step) >= 128;
-  p.hidden_parts = parts_for(p.large_hidden ? hidden : tiles_of(width, p.padded_rows, 64, 64), (piece + step - 1) / step);
-  p.weight_parts = parts_for(p.large_weight ? weight : tiles_of(width, piece, 64, 64), p.padded_rows / step);
+  p.large_hidden = hidden * parts_for(hidden, piece / step, 8) >= 128;
+  p.large_weight = weight * parts_for(weight, p.padded_rows / step, 8) >= 128;
+  p.hidden_parts = parts_for(p.large_hidden ? hidden : tiles_of(width, p.padded_rows, 64, 64), (piece + step - 1) / step, p.large_hidden ? 8 : 2);
+  p.weight_parts = parts_for(p.large_weight ? weight : tiles_of(width, piece, 64, 64), p.padded_rows / step, p.large_weight ? 8 : 2);
   return p;
 }
 
@@ -651,28 +680,35 @@ struct Call {
 
   static unsigned grid(int64_t items) { return unsigned(std::min<int64_t>((items + 255) / 256, 1 << 16)); }
 
-  void pack(const void* x, int64_t stride, const int* order, int64_t n, __bf16* to, int64_t plane) const {
-    hipLaunchKernelGGL(k_vocab_pack<T>, dim3(grid(n * (p.padded_width / 8))), dim3(256), 0, s,
-                       static_cast<const typename T::Elem*>(x), (long long)stride, order, rows.count, int(n), p.width, to,
-                       (long long)plane, p.padded_width);
+  void pack(const Pack<T>& first, const Pack<T>& second) const {
+    hipLaunchKernelGGL(k_vocab_pack<T>, dim3(grid((int64_t(first.rows) + second.rows) * (p.padded_width / 8))), dim3(256), 0, s, first,
+                       second, rows.count, p.width, p.padded_width);
+  }
+  int64_t weight_plane() const { return int64_t(p.piece) * p.padded_width; }
+  Pack<T> weight_job(int k) const {
+    const typename T::Elem* from = static_cast<const typename T::Elem*>(head.weight) + int64_t(k) * p.piece * head.weight_stride;
+    return {from, head.weight_stride, nullptr, classes_of(k), get<__bf16>(w.weight), weight_plane()};
   }
   void pack_rows(const float* weights, const Factor& factor, float* logp, float2* saved, float* row_grads) const {
     hipLaunchKernelGGL(k_vocab_rows, dim3(1), dim3(kWide), 0, s, head.targets, head.target_bits, weights, int(p.rows),
                        int(p.padded_rows), p.classes, factor, rows, logp, saved, row_grads);
-    pack(head.hidden, head.hidden_stride, rows.order, p.padded_rows, get<__bf16>(w.hidden), hidden_plane());
+    // the rows and, with them, the first piece of the weight
+    pack({static_cast<const typename T::Elem*>(head.hidden), head.hidden_stride, rows.order, int(p.padded_rows), get<__bf16>(w.hidden),
+          hidden_plane()},
+         direct ? Pack<T>{} : weight_job(0));
   }
   int64_t hidden_plane() const { return p.padded_rows * p.padded_width; }
   int classes_of(int k) const { return std::min(p.piece, p.classes - k * p.piece); }
   Operand hidden() const {
     return Operand{get<__bf16>(w.hidden), p.padded_width, hidden_plane(), int(p.padded_rows), p.padded_width};
   }
-  Operand weight(int k, bool again) const {
+  // piece k of the weight; `packed`: it is the one that was packed last
+  Operand weight(int k, bool packed) const {
     const int n = classes_of(k);
-    const typename T::Elem* from = static_cast<const typename T::Elem*>(head.weight) + int64_t(k) * p.piece * head.weight_stride;
-    if (direct) return Operand{reinterpret_cast<const __bf16*>(from), head.weight_stride, 0, n, p.width};
-    const int64_t plane = int64_t(p.piece) * p.padded_width;
-    if (!again) pack(from, head.weight_stride, nullptr, n, get<__bf16>(w.weight), plane);
-    return Operand{get<__bf16>(w.weight), p.padded_width, plane, n, p.padded_width};
+    const Pack<T> job = weight_job(k);
+    if (direct) return Operand{reinterpret_cast<const __bf16*>(job.x), head.weight_stride, 0, n, p.width};
+    if (!packed) pack(job, Pack<T>{});
+    return Operand{job.out, p.padded_width, weight_plane(), n, p.padded_width};
   }
   Operand grad(int k) const {
     return Operand{get<__bf16>(w.grad), p.piece, p.padded_rows * p.piece, int(p.padded_rows), int(up(classes_of(k), 64))};
@@ -699,13 +735,13 @@ struct Call {
   }
 
   template <Keep KEEP>
-  StatsOut<KEEP> stats_out(int k) const {
+  StatsOut<KEEP, P == 3> stats_out(int k) const {
     return {rows.target, get<float2>(w.parts), get<float>(w.logit), get<void>(w.kept), k * p.piece, classes_of(k),
             int(p.padded_rows), k * (p.piece / p.tile_classes()), p.piece};
   }
   int statistics(const JoinOut& out, bool keep) const {
     for (int k = 0; k < p.pieces; ++k) {
-      const Operand weight_k = weight(k, false);
+      const Operand weight_k = weight(k, k == 0);
       if (keep) logits(weight_k, stats_out<P == 1 ? Keep::kBf16 : Keep::kF32>(k));
       else logits(weight_k, stats_out<Keep::kNothing>(k));
     }
@@ -748,11 +784,12 @@ struct Call {
                        (long long)(p.padded_rows * p.piece), p.piece, p.tile_classes(), int(p.padded_rows), blocks);
   }
   // With the rows' slopes in place.  `kept`: the logp of the pass that kept the only
-  // piece's exponentials, and packed its weight.
-  int gradients(const acdc_vocab_grads& g, const float* kept) const {
+  // piece's exponentials; `packed`: the piece of the weight that was packed last.
+  int gradients(const acdc_vocab_grads& g, const float* kept, int packed) const {
     const int64_t part = p.padded_rows * p.padded_width;
     for (int k = 0; k < p.pieces; ++k) {
-      const Operand wk = weight(k, kept != nullptr);
+      const Operand wk = weight(k, k == packed);
+      packed = k;
       if (kept != nullptr) slopes(kept);
       else logits(wk, SlopeOut<P>{get<RowSlope>(w.slope), get<__bf16>(w.grad), p.padded_rows * p.piece, p.piece, k * p.piece, classes_of(k)});
       if (g.hidden != nullptr)
@@ -845,7 +882,7 @@ extern "C" int acdc_vocab_logprob(const acdc_vocab_head* head, float* logp, floa
   return with_type(head->dtype, [&]<class T>() {
     const Call<T> c(*head, false, workspace, stream);
     c.pack_rows(nullptr, Factor{nullptr, 1.f, false}, logp, reinterpret_cast<float2*>(saved), nullptr);
-    return c.statistics(JoinOut{logp, reinterpret_cast<float2*>(saved), nullptr, nullptr, nullptr, false}, false);
+    return c.statistics(JoinOut{logp, reinterpret_cast<float2*>(saved), nullptr, nullptr, nullptr, nullptr, false}, false);
   });
 }
 
@@ -861,7 +898,7 @@ extern "C" int acdc_vocab_backward(const acdc_vocab_head* head, const float* sav
     c.pack_rows(grad_logp, Factor{scale, 1.f, false}, nullptr, nullptr, nullptr);
     hipLaunchKernelGGL(k_vocab_slope, dim3(Call<T>::grid(c.p.padded_rows)), dim3(256), 0, c.s, c.rows,
                        reinterpret_cast<const float2*>(saved), int(c.p.padded_rows), c.template get<RowSlope>(c.w.slope));
-    return c.gradients(*grads, nullptr);
+    return c.gradients(*grads, nullptr, 0);
   });
 }
 
@@ -882,11 +919,13 @@ extern "C" int acdc_vocab_loss(const acdc_vocab_head* head, const float* weights
     float* loss = c.template get<float>(c.w.loss);
     const bool keep = gradient && c.p.pieces == 1;
     c.pack_rows(weights, Factor{nullptr, q.grad_scale, q.mean != 0}, logp, stat, row_grads);
-    int rc = c.statistics(JoinOut{logp, stat, row_grads, gradient ? c.template get<RowSlope>(c.w.slope) : nullptr, loss,
-                                  q.mean != 0}, keep);
+    const bool few = c.p.padded_rows == 64;
+    int rc = c.statistics(JoinOut{logp, stat, row_grads, gradient ? c.template get<RowSlope>(c.w.slope) : nullptr,
+                                  few ? nullptr : loss, few ? stats : nullptr, q.mean != 0},
+                          keep);
     if (rc != ACDC_OK) return rc;
-    hipLaunchKernelGGL(k_vocab_total, dim3(1), dim3(kWide), 0, c.s, c.rows, loss, q.mean != 0, stats);
+    if (!few) hipLaunchKernelGGL(k_vocab_total, dim3(1), dim3(kWide), 0, c.s, c.rows, loss, q.mean != 0, stats);
     rc = done();
-    return rc != ACDC_OK || !gradient ? rc : c.gradients(*grads, keep ? logp : nullptr);
+    return rc != ACDC_OK || !gradient ? rc : c.gradients(*grads, keep ? logp : nullptr, c.p.pieces - 1);
   });
 }
