@@ -250,13 +250,14 @@ __device__ __forceinline__ void wait_loads() {
 }
 
 // `parts` workgroups share a tile's steps.  *count (may be null): the rows in use.
-template <class S, int PLANES, bool ACROSS_A, bool ACROSS_B, Count COUNT, class Epilogue>
+template <class S, int PA, int PB, bool ACROSS_A, bool ACROSS_B, Count COUNT, class Epilogue>
 __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int depth, int mt, int nt, int parts,
                                                      const int* __restrict__ count, Epilogue epilogue) {
   constexpr int T = S::THREADS, BM = S::BM, BN = S::BN, BK = S::BK, MI = S::MI, NI = S::NI, STAGES = S::STAGES;
   using StageA = std::conditional_t<ACROSS_A, Across<BM, BK, T>, Along<BM, BK, T, 4 * MI>>;
   using StageB = std::conditional_t<ACROSS_B, Across<BN, BK, T>, Along<BN, BK, T, 0>>;
-  constexpr int STAGE = PLANES * (StageA::BYTES + StageB::BYTES), LOADS = PLANES * (StageA::N + StageB::N);
+  constexpr int STAGE = PA * StageA::BYTES + PB * StageB::BYTES, LOADS = PA * StageA::N + PB * StageB::N;
+  constexpr int MOST = PA > PB ? PA : PB;
   static_assert(STAGES * STAGE <= 160 * 1024);
   __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];  // (the epilogue exchanges values there too)
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
@@ -276,9 +277,9 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int d
   auto fetch = [&]<bool FULL>(int slot, int k) {
     char ACDC_LDS* stage = base + slot * STAGE;
 #pragma unroll
-    for (int p = 0; p < PLANES; ++p) a.template load<FULL>(stage + p * StageA::BYTES, p, k, wave);
+    for (int p = 0; p < PA; ++p) a.template load<FULL>(stage + p * StageA::BYTES, p, k, wave);
 #pragma unroll
-    for (int p = 0; p < PLANES; ++p) b.template load<FULL>(stage + PLANES * StageA::BYTES + p * StageB::BYTES, p, k, wave);
+    for (int p = 0; p < PB; ++p) b.template load<FULL>(stage + PA * StageA::BYTES + p * StageB::BYTES, p, k, wave);
   };
   f32x4 acc[MI][NI] = {};
   const int wm = wave % S::WM, wn = wave / S::WM;
@@ -288,16 +289,16 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int d
   rb.init(wn * (BN / S::WN), lane);
   // one part (32 k) of a step as the matrix cores take it
   struct Part {
-    bf16x8 a[PLANES][MI], b[PLANES][NI];
+    bf16x8 a[PA][MI], b[PB][NI];
   };
   auto read = [&](int slot, int part, Part& f) {
     const char ACDC_LDS* stage = base + slot * STAGE;
 #pragma unroll
-    for (int p = 0; p < PLANES; ++p)
+    for (int p = 0; p < PB; ++p)
 #pragma unroll
-      for (int n = 0; n < NI; ++n) f.b[p][n] = rb.read(stage + PLANES * StageA::BYTES + p * StageB::BYTES, n, part);
+      for (int n = 0; n < NI; ++n) f.b[p][n] = rb.read(stage + PA * StageA::BYTES + p * StageB::BYTES, n, part);
 #pragma unroll
-    for (int p = 0; p < PLANES; ++p)
+    for (int p = 0; p < PA; ++p)
 #pragma unroll
       for (int m = 0; m < MI; ++m) f.a[p][m] = ra.read(stage + p * StageA::BYTES, m, part);
   };
@@ -306,11 +307,11 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int d
     for (int m = 0; m < MI; ++m)
       // the pairs of planes that matter, smallest first
 #pragma unroll
-      for (int both = PLANES - 1; both >= 0; --both)
+      for (int both = MOST - 1; both >= 0; --both)
 #pragma unroll
-        for (int p = 0; p <= both; ++p)
+        for (int p = 0; p <= both && p < PA; ++p)
 #pragma unroll
-          for (int n = 0; n < NI; ++n)
+          for (int n = 0; n < NI && both - p < PB; ++n)
             acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.a[p][m], f.b[both - p][n], acc[m][n], 0, 0, 0);
   };
   // this wave's loads but `left` of them are there, then everyone's; and everyone has read
@@ -332,7 +333,7 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int d
   int slot = 0;
   if constexpr (S::AHEAD) {
     // The registers of one part are read while the matrix cores work on the other's.
-    static_assert(BK == 64 && STAGES == 2 && PLANES == 1);
+    static_assert(BK == 64 && STAGES == 2 && MOST == 1);
     constexpr int READS = (ACROSS_A ? 2 : 1) * MI + (ACROSS_B ? 2 : 1) * NI, PER = MI * NI / READS;
     Part first, second;
     int s = from;

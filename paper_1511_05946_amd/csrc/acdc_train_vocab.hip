@@ -299,6 +299,27 @@ struct RowSlope {
   int target;
 };
 
+// Values of G as 1, 2 or 3 planes of bfloat16: the one rounding between the logits and the
+// gradients, to 8, 16 or 24 bits.  Where thousands of terms are summed, that of bfloat16
+// inputs to 8 bits is lost in the inputs' own; small problems, whose time it is not, take 16.
+template <int PLANES, int N, class V>
+__device__ __forceinline__ void put_planes(__bf16* out, long long plane, const float (&y)[N]) {
+  V o[PLANES];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if constexpr (PLANES == 3) {
+      const Split3 s = split3(y[i]);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) o[p][i] = s.p[p];
+    } else {
+      o[0][i] = __bf16(y[i]);
+      if constexpr (PLANES == 2) o[1][i] = __bf16(y[i] - float(o[0][i]));
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < PLANES; ++p) *reinterpret_cast<V*>(out + p * plane) = o[p];
+}
+
 // The piece of G, rows `ld` apart, zeros past the classes and for padding rows.
 template <int PLANES>
 struct SlopeOut {
@@ -316,23 +337,15 @@ struct SlopeOut {
       __bf16* to = out + (long long)r * ld + spot.m(0);
 #pragma unroll
       for (int m = 0; m < MI; m += 2) {
-        bf16x8 o[PLANES];
+        float y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int v = spot.m(m + i / 4) + i % 4;
-          float y = -exp_as<PLANES == 3>(acc[m + i / 4][n][i % 4] - k.top) * k.slope;
-          if (v == t) y += k.g;
-          if (v >= classes) y = 0.f;
-          if constexpr (PLANES == 1) {
-            o[0][i] = __bf16(y);  // the one rounding between the logits and the gradients
-          } else {
-            const Split3 s = split3(y);
-#pragma unroll
-            for (int p = 0; p < 3; ++p) o[p][i] = s.p[p];
-          }
+          y[i] = -exp_as<(PLANES > 1)>(acc[m + i / 4][n][i % 4] - k.top) * k.slope;
+          if (v == t) y[i] += k.g;
+          if (v >= classes) y[i] = 0.f;
         }
-#pragma unroll
-        for (int p = 0; p < PLANES; ++p) *reinterpret_cast<bf16x8*>(to + p * plane + m * 4) = o[p];
+        put_planes<PLANES, 8, bf16x8>(to + m * 4, plane, y);
       }
     }
   }
@@ -342,11 +355,10 @@ struct SlopeOut {
 // piece: in place where e is bfloat16 (a second rounding, of 2^-8 at the most; the
 // target's own value, where 1 - p may be small, comes from its logit).  A wave takes 512
 // classes of a row; bound by HBM.
-template <int PLANES>
+template <int PLANES, class E>
 __global__ __launch_bounds__(256) void k_vocab_slopes(Rows rows, const RowSlope* __restrict__ slope, const float2* __restrict__ parts,
                                                       const float* __restrict__ logp, const void* kept, __bf16* out,
                                                       long long plane, int ld, int tile, int padded, int blocks) {
-  using E = std::conditional_t<PLANES == 1, __bf16, float>;
   typedef E Eight __attribute__((ext_vector_type(8)));
   const int lane = threadIdx.x % 64, used = (*rows.count + 63) / 64 * 64;
   const long long item = blockIdx.x * 4ll + threadIdx.x / 64;
@@ -356,21 +368,59 @@ __global__ __launch_bounds__(256) void k_vocab_slopes(Rows rows, const RowSlope*
   const float f = -k.slope * expf(parts[(long long)(col / tile) * padded + r].x - k.top);
   const long long at = (long long)r * ld + col;
   const Eight e = *reinterpret_cast<const Eight*>(static_cast<const E*>(kept) + at);
-  bf16x8 o[PLANES];
+  float y[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    float y = float(e[i]) * f;
-    if (col + i == k.target) y = -k.g * expm1f(logp[rows.order[r]]);
-    if constexpr (PLANES == 1) {
-      o[0][i] = __bf16(y);
-    } else {
-      const Split3 s = split3(y);
-#pragma unroll
-      for (int p = 0; p < 3; ++p) o[p][i] = s.p[p];
-    }
+    y[i] = float(e[i]) * f;
+    if (col + i == k.target) y[i] = -k.g * expm1f(logp[rows.order[r]]);
   }
-#pragma unroll
-  for (int p = 0; p < PLANES; ++p) *reinterpret_cast<bf16x8*>(out + p * plane + at) = o[p];
+  put_planes<PLANES, 8, bf16x8>(out + at, plane, y);
+}
+
+// A product of few tiles with many steps leaves its logits as sums of parts; a wave adds
+// them up for 64 classes of a row.
+struct FewLogits {
+  const float* sums;
+  const int* count;
+  long long part;
+  int parts, ld, tiles, first, classes;
+  // this wave's row and its lane's class and logit; false: nothing to do
+  __device__ __forceinline__ bool read(int& r, int& v, float& x) const {
+    const long long item = blockIdx.x * 4ll + threadIdx.x / 64;
+    r = int(item / tiles);
+    v = int(item % tiles) * 64 + threadIdx.x % 64;
+    if (r >= (*count + 63) / 64 * 64) return false;
+    x = 0.f;
+    const float* p = sums + (long long)r * ld + v;
+#pragma unroll 8
+    for (int k = 0; k < parts; ++k) x += p[k * part];
+    return true;
+  }
+};
+template <class E>
+__global__ __launch_bounds__(256) void k_vocab_few_stats(FewLogits l, const int* __restrict__ target, float2* __restrict__ parts,
+                                                         float* __restrict__ logit, E* __restrict__ kept, int padded) {
+  int r, v;
+  float x;
+  if (!l.read(r, v, x)) return;
+  if (v >= l.classes) x = -__builtin_inff();
+  const float top = fmaxf(wave_max(x), kNegMax), e = expf(x - top), sum = wave_sum(e);
+  if (v == target[r] - l.first) logit[r] = x;
+  if (threadIdx.x % 64 == 0) parts[(long long)((l.first + v) / 64) * padded + r] = make_float2(top, sum);
+  if (kept != nullptr) kept[(long long)r * l.ld + v] = E(e);
+}
+template <int PLANES>
+__global__ __launch_bounds__(256) void k_vocab_few_slopes(FewLogits l, const RowSlope* __restrict__ slope, __bf16* __restrict__ out,
+                                                          long long plane) {
+  typedef __bf16 One __attribute__((ext_vector_type(1)));
+  int r, v;
+  float x;
+  if (!l.read(r, v, x)) return;
+  const RowSlope k = slope[r];
+  float y[1] = {-expf(x - k.top) * k.slope};
+  if (v == k.target - l.first) y[0] += k.g;
+  if (v >= l.classes) y[0] = 0.f;
+  put_planes<PLANES, 1, One>(out + (long long)r * l.ld + v, plane, y);
 }
 
 // 32-bit sums of a part: out[part][n][m], added to what earlier pieces left.
@@ -586,6 +636,8 @@ struct Plan {
   int32_t piece, pieces;  // classes of a piece, a multiple of kTile
   int hidden_parts, weight_parts;
   bool large_logits, large_hidden, large_weight;  // the products' tiles
+  int logits_parts;                               // more than one: FewLogits
+  int grad_planes;
   int tile_classes() const { return !large_logits ? 64 : planes == 1 ? 256 : 128; }  // of the logits
 };
 int64_t tiles_of(int64_t m, int64_t n, int bm, int bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); }
@@ -613,12 +665,15 @@ Plan plan_for(int64_t rows, int32_t width, int32_t classes, int32_t dtype) {
   p.large_hidden = hidden * parts_for(hidden, piece / step, 8) >= 128;
   p.large_weight = weight * parts_for(weight, p.padded_rows / step, 8) >= 128;
   p.hidden_parts = parts_for(p.large_hidden ? hidden : tiles_of(width, p.padded_rows, 64, 64), (piece + step - 1) / step, p.large_hidden ? 8 : 2);
+  const int64_t few = tiles_of(piece, p.padded_rows, 64, 64);
+  p.logits_parts = p.large_logits || few > 64 ? 1 : parts_for(few, p.padded_width / step, 8);
+  p.grad_planes = p.planes == 3 ? 3 : p.large_hidden || p.large_weight ? 1 : 2;
   p.weight_parts = parts_for(p.large_weight ? weight : tiles_of(width, piece, 64, 64), p.padded_rows / step, p.large_weight ? 8 : 2);
   return p;
 }
 
 struct Layout {
-  size_t order, target, share, at, count, total, factor, logit, parts, slope, loss, hidden, weight, grad, kept, hidden_sums, weight_sums, bytes;
+  size_t order, target, share, at, count, total, factor, logit, parts, slope, loss, hidden, weight, logits_sums, grad, kept, hidden_sums, weight_sums, bytes;
 };
 Layout layout(const Plan& p, bool gradient) {
   Layout w{};
@@ -642,9 +697,10 @@ Layout layout(const Plan& p, bool gradient) {
   w.loss = take(R * 4);
   w.hidden = take(R * p.padded_width * 2 * p.planes);
   w.weight = take(size_t(p.piece) * p.padded_width * 2 * p.planes);
+  w.logits_sums = take(p.logits_parts > 1 ? size_t(p.logits_parts) * R * p.piece * 4 : 0);
   if (gradient) {
-    w.grad = take(R * p.piece * 2 * p.planes);
-    w.kept = p.planes == 1 ? w.grad : take(p.pieces == 1 ? R * p.piece * 4 : 0);
+    w.grad = take(R * p.piece * 2 * p.grad_planes);
+    w.kept = p.grad_planes == 1 ? w.grad : take(p.pieces == 1 ? R * p.piece * 4 : 0);
     w.hidden_sums = take(size_t(p.hidden_parts) * R * p.padded_width * 4);
     w.weight_sums = take(p.weight_parts > 1 ? size_t(p.weight_parts) * p.piece * p.padded_width * 4 : 0);
   }
@@ -714,36 +770,55 @@ struct Call {
     return Operand{get<__bf16>(w.grad), p.piece, p.padded_rows * p.piece, int(p.padded_rows), int(up(classes_of(k), 64))};
   }
 
-  template <class S, bool XA, bool XB, Count COUNT, class E>
+  template <class S, int PB, bool XA, bool XB, Count COUNT, class E>
   void gemm(const Operand& a, const Operand& b, int64_t m, int64_t n, int depth, int parts, const E& e) const {
     const int mt = int((m + S::BM - 1) / S::BM), nt = int((n + S::BN - 1) / S::BN);
-    hipLaunchKernelGGL((k_gemm<S, P, XA, XB, COUNT, E>), dim3(unsigned(int64_t(mt) * nt * parts)), dim3(S::THREADS), 0, s, a, b,
+    hipLaunchKernelGGL((k_gemm<S, P, PB, XA, XB, COUNT, E>), dim3(unsigned(int64_t(mt) * nt * parts)), dim3(S::THREADS), 0, s, a, b,
                        depth, mt, nt, parts, rows.count, e);
   }
-  // a product with n over the packed rows
-  template <bool XA, class E>
+  // a product with n over the packed rows; b of PB planes
+  template <int PB, bool XA, class E>
   void over_rows(bool large, const Operand& a, const Operand& b, int64_t m, int depth, int parts, const E& e) const {
     constexpr Count N = Count::kN;
-    if (!large) gemm<std::conditional_t<P == 1, Small, Small3>, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
-    else if (p.padded_rows > 64) gemm<std::conditional_t<P == 1, Large, Large3>, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
-    else gemm<std::conditional_t<P == 1, Flat, Flat3>, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
+    if (!large) {
+      gemm<std::conditional_t<P == 1, Small, Small3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
+    } else if constexpr (PB == P) {  // (two planes of G are for small tiles)
+      if (p.padded_rows > 64) gemm<std::conditional_t<P == 1, Large, Large3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
+      else gemm<std::conditional_t<P == 1, Flat, Flat3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
+    }
   }
   // classes x packed rows
   template <class E>
-  void logits(const Operand& weight, const E& e) const {
-    over_rows<false>(p.large_logits, weight, hidden(), weight.rows, p.padded_width, 1, e);
+  void logits(const Operand& weight, int parts, const E& e) const {
+    over_rows<P, false>(p.large_logits, weight, hidden(), weight.rows, p.padded_width, parts, e);
   }
+  // the same as sums of parts, and what a wave for each 64 of a row's classes reads
+  FewLogits few_logits(const Operand& weight, int k) const {
+    const int64_t part = p.padded_rows * p.piece;
+    logits(weight, p.logits_parts, PartOut{get<float>(w.logits_sums), part, p.piece, int(p.padded_rows), false});
+    return {get<float>(w.logits_sums), rows.count, part, p.logits_parts, p.piece, (classes_of(k) + 63) / 64, k * p.piece, classes_of(k)};
+  }
+  unsigned few_grid(const FewLogits& l) const { return unsigned((p.padded_rows * l.tiles + 3) / 4); }
 
   template <Keep KEEP>
-  StatsOut<KEEP, P == 3> stats_out(int k) const {
-    return {rows.target, get<float2>(w.parts), get<float>(w.logit), get<void>(w.kept), k * p.piece, classes_of(k),
-            int(p.padded_rows), k * (p.piece / p.tile_classes()), p.piece};
+  void statistics_of(const Operand& weight, int k) const {
+    if (p.logits_parts > 1) {
+      using E = std::conditional_t<KEEP == Keep::kBf16, __bf16, float>;
+      const FewLogits l = few_logits(weight, k);
+      hipLaunchKernelGGL(k_vocab_few_stats<E>, dim3(few_grid(l)), dim3(256), 0, s, l, rows.target, get<float2>(w.parts), get<float>(w.logit),
+                         KEEP == Keep::kNothing ? nullptr : get<E>(w.kept), int(p.padded_rows));
+      return;
+    }
+    logits(weight, 1,
+           StatsOut<KEEP, P == 3>{rows.target, get<float2>(w.parts), get<float>(w.logit), get<void>(w.kept), k * p.piece, classes_of(k),
+                                  int(p.padded_rows), k * (p.piece / p.tile_classes()), p.piece});
   }
   int statistics(const JoinOut& out, bool keep) const {
     for (int k = 0; k < p.pieces; ++k) {
       const Operand weight_k = weight(k, k == 0);
-      if (keep) logits(weight_k, stats_out<P == 1 ? Keep::kBf16 : Keep::kF32>(k));
-      else logits(weight_k, stats_out<Keep::kNothing>(k));
+      if (!keep) statistics_of<Keep::kNothing>(weight_k, k);
+      else if (p.grad_planes == 1) statistics_of<Keep::kBf16>(weight_k, k);
+      else statistics_of<Keep::kF32>(weight_k, k);
     }
     hipLaunchKernelGGL(k_vocab_join, dim3(unsigned(p.padded_rows / 64)), dim3(1024), 0, s, rows, get<float2>(w.parts),
                        get<float>(w.logit), int((p.classes + p.tile_classes() - 1) / p.tile_classes()), int(p.padded_rows), out);
@@ -757,7 +832,7 @@ struct Call {
     hipLaunchKernelGGL(k_vocab_sum<O>, dim3(grid(n * ((p.width + 3) / 4))), dim3(256), 0, s, get<float>(at), parts,
                        (long long)part, p.padded_width, place, rows.factor, (long long)n, p.width, static_cast<E*>(out), (long long)ld, whole, add);
   }
-  template <class O>
+  template <int GP, class O>
   void weight_grad(const acdc_vocab_grads& g, int k) const {
     using E = typename O::Elem;
     const int n = classes_of(k);
@@ -765,8 +840,10 @@ struct Call {
     const bool whole = aligned_to(out, 4 * sizeof(E)) && g.weight_stride % 4 == 0, add = g.accumulate != 0;
     auto product = [&](const auto& e) {
       constexpr Count K = Count::kK;
-      if (p.large_weight) gemm<std::conditional_t<P == 1, Large, Large3>, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e);
-      else gemm<std::conditional_t<P == 1, Small, Small3>, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e);
+      if (!p.large_weight)
+        gemm<std::conditional_t<P == 1, Small, Small3>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e);
+      else if constexpr (GP == P)
+        gemm<std::conditional_t<P == 1, Large, Large3>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e);
     };
     if (p.weight_parts == 1) {
       product(GradOut<O>{out, rows.factor, g.weight_stride, p.width, n, whole, add});
@@ -777,27 +854,48 @@ struct Call {
     }
   }
   // G of a single piece from what the first pass kept
+  template <int GP>
   void slopes(const float* logp) const {
     const int blocks = (p.piece + 511) / 512;
-    hipLaunchKernelGGL(k_vocab_slopes<P>, dim3(unsigned((p.padded_rows * blocks + 3) / 4)), dim3(256), 0, s, rows,
-                       get<RowSlope>(w.slope), get<float2>(w.parts), logp, get<void>(w.kept), get<__bf16>(w.grad),
+    hipLaunchKernelGGL((k_vocab_slopes<GP, std::conditional_t<GP == 1, __bf16, float>>), dim3(unsigned((p.padded_rows * blocks + 3) / 4)),
+                       dim3(256), 0, s, rows, get<RowSlope>(w.slope), get<float2>(w.parts), logp, get<void>(w.kept), get<__bf16>(w.grad),
                        (long long)(p.padded_rows * p.piece), p.piece, p.tile_classes(), int(p.padded_rows), blocks);
+  }
+  // G of piece k from its logits, computed again
+  template <int GP>
+  void slopes_again(const Operand& weight, int k) const {
+    const int64_t plane = p.padded_rows * p.piece;
+    if (p.logits_parts > 1) {
+      const FewLogits l = few_logits(weight, k);
+      hipLaunchKernelGGL(k_vocab_few_slopes<GP>, dim3(few_grid(l)), dim3(256), 0, s, l, get<RowSlope>(w.slope), get<__bf16>(w.grad),
+                         (long long)plane);
+    } else {
+      logits(weight, 1, SlopeOut<GP>{get<RowSlope>(w.slope), get<__bf16>(w.grad), plane, p.piece, k * p.piece, classes_of(k)});
+    }
   }
   // With the rows' slopes in place.  `kept`: the logp of the pass that kept the only
   // piece's exponentials; `packed`: the piece of the weight that was packed last.
   int gradients(const acdc_vocab_grads& g, const float* kept, int packed) const {
+    if constexpr (P == 3) {
+      return gradients_of<3>(g, kept, packed);
+    } else {
+      return p.grad_planes == 1 ? gradients_of<1>(g, kept, packed) : gradients_of<2>(g, kept, packed);
+    }
+  }
+  template <int GP>
+  int gradients_of(const acdc_vocab_grads& g, const float* kept, int packed) const {
     const int64_t part = p.padded_rows * p.padded_width;
     for (int k = 0; k < p.pieces; ++k) {
       const Operand wk = weight(k, k == packed);
       packed = k;
-      if (kept != nullptr) slopes(kept);
-      else logits(wk, SlopeOut<P>{get<RowSlope>(w.slope), get<__bf16>(w.grad), p.padded_rows * p.piece, p.piece, k * p.piece, classes_of(k)});
+      if (kept != nullptr) slopes<GP>(kept);
+      else slopes_again<GP>(wk, k);
       if (g.hidden != nullptr)
-        over_rows<true>(p.large_hidden, wk, grad(k), p.width, classes_of(k), p.hidden_parts,
-                        PartOut{get<float>(w.hidden_sums), part, p.padded_width, int(p.padded_rows), k > 0});
+        over_rows<GP, true>(p.large_hidden, wk, grad(k), p.width, classes_of(k), p.hidden_parts,
+                            PartOut{get<float>(w.hidden_sums), part, p.padded_width, int(p.padded_rows), k > 0});
       if (g.weight != nullptr) {
-        if (g.weight_type == head.dtype) weight_grad<T>(g, k);
-        else weight_grad<F32>(g, k);
+        if (g.weight_type == head.dtype) weight_grad<GP, T>(g, k);
+        else weight_grad<GP, F32>(g, k);
       }
     }
     if (g.hidden != nullptr) sum<T>(w.hidden_sums, p.hidden_parts, part, rows.at, p.rows, g.hidden, g.hidden_stride, false);

@@ -26,7 +26,10 @@ SHAPES = [(1, 1, 1, "float32", 64, 0, 0), (1, 1, 1, "bfloat16", 32, 0, 0), (2, 3
           (257, 72, 513, "bfloat16", 64, 8, 16), (300, 200, 777, "float32", 64, 0, 1), (70, 264, 2049, "bfloat16", 64, 4, 8),
           (130, 520, 300, "bfloat16", 64, 0, 0), (1000, 96, 1500, "bfloat16", 32, 0, 0), (5, 1000, 4100, "float32", 64, 0, 0),
           (20, 4096, 130, "bfloat16", 64, 0, 0), (520, 31, 90, "float32", 64, 1, 0), (8, 136, 33000, "bfloat16", 64, 0, 0),
-          (2100, 40, 50, "bfloat16", 64, 0, 0), (40, 1, 300, "float32", 64, 0, 0)]
+          (2100, 40, 50, "bfloat16", 64, 0, 0), (40, 1, 300, "float32", 64, 0, 0),
+          # few tiles of many steps
+          (3, 8128, 10, "float32", 64, 0, 0), (70, 5000, 100, "bfloat16", 64, 0, 8), (300, 2500, 70, "float32", 32, 1, 0),
+          (2, 20000, 3, "bfloat16", 64, 0, 0)]
 
 
 def values(torch, gen, rows, width, extra, dtype, std):
