@@ -327,14 +327,64 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int d
     else wait_loads<0>();
     meet();
   };
+  constexpr int READS = PA * (ACROSS_A ? 2 : 1) * MI + PB * (ACROSS_B ? 2 : 1) * NI;
 #pragma unroll
   for (int q = 0; q < STAGES - 1; ++q)
     if (from + q < to) fetch.template operator()<false>(q, from + q);
   int slot = 0;
-  if constexpr (S::AHEAD) {
+  if constexpr (S::AHEAD && BK == 32) {
+    // The registers of one step are read while the matrix cores work on the other's.
+    static_assert(STAGES == 2 && PA == PB);
+    constexpr int PER = PA * (PA + 1) / 2 * MI * NI / READS;
+    Part even, odd;
+    int s = from;
+    if (from < to) {
+      if (from + 1 < to) {
+        fetch.template operator()<false>(1, from + 1);
+        wait_loads<LOADS>();
+      } else {
+        wait_loads<0>();
+      }
+      meet();
+      read(0, 0, even);
+    }
+    // step s is in `now`, and step s + 2 takes its place in LDS
+    auto step = [&]<bool FULL>(const Part& now, Part& then) {
+      wait_loads<0>();
+      meet();
+      read(slot ^ 1, 0, then);  // (nothing, after the last step)
+      if constexpr (FULL) {
+        fetch.template operator()<true>(slot, s + 2);
+      } else {
+        if (s + 2 < to) fetch.template operator()<false>(slot, s + 2);
+      }
+      multiply(now);
+      if constexpr (FULL) {
+#pragma unroll
+        for (int i = 0; i < READS; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          if (i < LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      slot ^= 1;
+      ++s;
+    };
+    // (the last step of all may end outside the operand)
+    while (s + 4 < to) {
+      step.template operator()<true>(even, odd);
+      step.template operator()<true>(odd, even);
+    }
+#pragma nounroll
+    while (s < to) {
+      step.template operator()<false>(even, odd);
+      if (s < to) step.template operator()<false>(odd, even);
+    }
+  } else if constexpr (S::AHEAD) {
     // The registers of one part are read while the matrix cores work on the other's.
     static_assert(BK == 64 && STAGES == 2 && MOST == 1);
-    constexpr int READS = (ACROSS_A ? 2 : 1) * MI + (ACROSS_B ? 2 : 1) * NI, PER = MI * NI / READS;
+    constexpr int PER = MI * NI / READS;
     Part first, second;
     int s = from;
     if (from < to) {

@@ -154,10 +154,17 @@ __global__ __launch_bounds__(256) void k_vocab_pack(Pack<T> first, Pack<T> secon
                                                     int padded) {
   const int per = padded / 8, used = *count;
   const long long split = (long long)first.rows * per, chunks = split + (long long)second.rows * per;
-  for (long long c = blockIdx.x * 256ll + threadIdx.x; c < chunks; c += gridDim.x * 256ll) {
-    const Pack<T>& job = c < split ? first : second;
-    const long long at = c < split ? c : c - split;
-    const int r = int(at / per), col = int(at % per) * 8;
+  for (long long base = blockIdx.x * 256ll; base < chunks; base += gridDim.x * 256ll) {
+    // (one long division for the workgroup, a short one for the lane)
+    const bool in_first = base < split;
+    const long long begin = in_first ? base : base - split;
+    const int row = int(begin / per);
+    unsigned at = unsigned(begin - (long long)row * per) + threadIdx.x;
+    const bool over = in_first && base + threadIdx.x >= split;  // the job changes within the workgroup
+    if (over) at = unsigned(base + threadIdx.x - split);
+    if (base + threadIdx.x >= chunks) break;
+    const Pack<T>& job = in_first && !over ? first : second;
+    const int r = (over ? 0 : row) + int(at / unsigned(per)), col = int(at % unsigned(per)) * 8;
     float v[8] = {};
     if (job.order == nullptr || r < used) {
       const typename T::Elem* from = job.x + (job.order != nullptr ? job.order[r] : r) * job.stride + col;
@@ -624,6 +631,7 @@ constexpr int64_t kPieceBytes = int64_t(2) << 30;
 // card busy, and give a row of few steps to more workgroups.
 using Large = Shape<256, 256, 64, 4, 2, 2, true>;
 using Large3 = Shape<128, 256, 32, 2, 4, 2>;
+using Wide3 = Shape<128, 256, 32, 2, 2, 2, true>;  // where an operand lies across: 1.29 PFLOP/s for 1.17
 using Flat = Shape<256, 64, 64, 4, 1, 2>;
 using Flat3 = Shape<128, 64, 32, 4, 1, 2>;
 using Small = Shape<64, 64, 64, 2, 2, 4>;
@@ -783,7 +791,7 @@ struct Call {
     if (!large) {
       gemm<std::conditional_t<P == 1, Small, Small3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
     } else if constexpr (PB == P) {  // (two planes of G are for small tiles)
-      if (p.padded_rows > 64) gemm<std::conditional_t<P == 1, Large, Large3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
+      if (p.padded_rows > 64) gemm<std::conditional_t<P == 1, Large, std::conditional_t<XA, Wide3, Large3>>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
       else gemm<std::conditional_t<P == 1, Flat, Flat3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
     }
   }
@@ -843,7 +851,7 @@ struct Call {
       if (!p.large_weight)
         gemm<std::conditional_t<P == 1, Small, Small3>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e);
       else if constexpr (GP == P)
-        gemm<std::conditional_t<P == 1, Large, Large3>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e);
+        gemm<std::conditional_t<P == 1, Large, Wide3>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e);
     };
     if (p.weight_parts == 1) {
       product(GradOut<O>{out, rows.factor, g.weight_stride, p.width, n, whole, add});
