@@ -27,7 +27,7 @@ import torch
 
 from ._lib import lib
 from .acdc import _call, _check, _once, _ptr, _wrote
-from .losses import _DTYPES, _apart, _index, _matrix, _native, _values, _workspace
+from .losses import _DTYPES, _aligned_workspace, _apart, _index, _matrix, _native, _values, _workspace
 
 
 class LayerNorm(NamedTuple):
@@ -218,9 +218,7 @@ def embedding_backward(tokens, grad_rows, classes: int, scale: float = 1.0, dtyp
                                               _type("dtype", dtype, grad_weight.dtype))
         _apart("grad_weight", gw, ("grad_rows", grad_rows), ("tokens", tokens))
     need = _embedding_bytes(rows, width, classes)
-    ws = _workspace(workspace, need, device)
-    if ws.data_ptr() % 256 != 0:
-        raise ValueError("workspace must begin at a multiple of 256 bytes")
+    ws = _aligned_workspace(workspace, need, device)
     rc = _call(lib().acdc_embedding_backward, device, tokens.data_ptr(), bits, grad_rows.data_ptr(), _DTYPES[grad_rows.dtype], stride,
                scale, gw.data_ptr(), _DTYPES[gw.dtype], gw_stride, 1 if accumulate else 0, rows, width, classes, ws.data_ptr(), need)
     _check(rc, "acdc_embedding_backward")

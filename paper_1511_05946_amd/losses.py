@@ -377,14 +377,13 @@ def _vocab_head(hidden, weight, targets, grad, workspace):
     need = _vocab_bytes(rows, width, classes, dtype, 1 if grad else 0)
     head = struct.pack("3Q3q4i", hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), stride, weight_stride, rows,
                        width, classes, dtype, bits)
-    return head, _vocab_workspace(workspace, need, device), need
+    return head, _aligned_workspace(workspace, need, device), need
 
 
-def _vocab_workspace(ws, need, device):
-    ws = _workspace(ws, need, device)
-    if ws.data_ptr() % 256 != 0:
+def _aligned_workspace(ws, need, device):
+    if ws is not None and ws.data_ptr() % 256 != 0:
         raise ValueError("workspace must begin at a multiple of 256 bytes")
-    return ws
+    return _workspace(ws, need, device)
 
 
 def _apart(name, out, *others):

@@ -1,0 +1,267 @@
+"""The language-model operators as they are used: a whole training step around a
+cascade, in a graph and against autograd and 64 bits; tensors past 32-bit offsets;
+calls at the same time; what the binding's native part hands back to its checks."""
+
+import numpy as np
+import pytest
+
+import lm_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1511_05946_amd import acdc, layers, losses, optim
+    return torch, acdc, layers, losses, optim
+
+
+def model(torch, N, K, V, seed=0):
+    """Embedding (and head), two norms, diagonals and bias."""
+    gen = torch.Generator().manual_seed(seed)
+    draw = lambda mean, std, *shape: (mean + std * torch.randn(*shape, generator=gen)).cuda()  # noqa: E731
+    return [draw(0, 0.05, V, N), draw(1, 0.1, N), draw(0, 0.1, N), draw(1, 0.1, K, N), draw(1, 0.1, K, N), draw(0, 0.02, K, N),
+            draw(1, 0.1, N), draw(0, 0.1, N)]
+
+
+def explicit(env, p, tokens, targets, scale, head_type=None):
+    """Loss and the gradients of all parameters; the embedding and the head share a weight."""
+    torch, acdc, layers, losses, _ = env
+    W, g1, b1, A, D, bias, g2, b2 = p
+    x = layers.embedding(tokens, W, scale)
+    n1 = layers.layer_norm(x, g1, b1, save=True)
+    y, saved = acdc.forward(n1.y, A, D, save=True, bias=bias)
+    n2 = layers.layer_norm(y, g2, b2, dtype=head_type, save=True)
+    head = W if head_type is None else W.to(head_type)
+    gW = torch.empty_like(W)
+    r = losses.vocab_loss(n2.y, head, targets, grad_weight=gW)
+    gy, gg2, gb2 = layers.layer_norm_backward(y, r.grad_hidden, g2, n2.saved)
+    gn, gA, gD, gbias = acdc.backward(n1.y, gy, A, D, saved=saved, bias=bias)
+    gx, gg1, gb1 = layers.layer_norm_backward(x, gn, g1, n1.saved)
+    layers.embedding_backward(tokens, gx, W.shape[0], scale, grad_weight=gW, accumulate=True)
+    return r, [gW, gg1, gb1, gA, gD, gbias, gg2, gb2]
+
+
+def batch(torch, T, V, seed=1):
+    gen = torch.Generator().manual_seed(seed)
+    tokens = torch.randint(0, V, (T,), generator=gen)
+    targets = torch.randint(0, V, (T,), generator=gen)
+    tokens[3], targets[::5] = -1, -1
+    return tokens.cuda(), targets.cuda()
+
+
+def test_step_matches_autograd(env):
+    torch, acdc, layers, losses, _ = env
+    N, K, V, T = 64, 3, 300, 90
+    p = model(torch, N, K, V)
+    tokens, targets = batch(torch, T, V)
+    r, want = explicit(env, p, tokens, targets, 8.0)
+    leaves = [t.clone().requires_grad_(True) for t in p]
+    W, g1, b1, A, D, bias, g2, b2 = leaves
+    x = layers.embedding_autograd(tokens, W, 8.0)
+    y = acdc.acdc_cascade(layers.layer_norm_autograd(x, g1, b1), A, D, None, 0, bias)
+    loss, _, logp = losses.vocab_loss_autograd(layers.layer_norm_autograd(y, g2, b2), W, targets)
+    loss.backward()
+    assert torch.equal(loss, r.stats[0]) and torch.equal(logp, r.logp)
+    for leaf, g in zip(leaves, want):
+        # the same kernels but for the loss's gradient, which the differentiable form rounds once more
+        assert (leaf.grad - g).abs().max().item() <= 1e-5 * g.abs().max().item()
+
+
+def test_step_matches_64_bits(env):
+    """Every gradient of the step against differences of the loss in 64 bits, along random
+    directions (the cascade by the oracle)."""
+    torch, *_ = env
+    from oracle import acdc_oracle as O
+    N, K, V, T = 32, 2, 50, 40
+    p = model(torch, N, K, V, seed=2)
+    tokens, targets = batch(torch, T, V, seed=3)
+    r, got = explicit(env, p, tokens, targets, 5.0)
+    p64 = [t.double().cpu().numpy() for t in p]
+    tok, tgt = tokens.cpu().numpy(), targets.cpu().numpy()
+
+    def loss(q):
+        W, g1, b1, A, D, bias, g2, b2 = q
+        y = O.forward(R.Norm(R.embedding(tok, W, 5.0), g1, b1, 1e-5).y, A, D, B=bias)
+        return R.Vocab(R.Norm(y[0] if isinstance(y, tuple) else y, g2, b2, 1e-5).y, W, tgt).loss
+
+    assert abs(r.stats[0].item() - loss(p64)) <= 1e-5 * abs(loss(p64))
+    rng = np.random.RandomState(5)
+    for i, g in enumerate(got):
+        g = g.double().cpu().numpy()
+        for _ in range(3):
+            d = rng.randn(*g.shape)
+            h = 1e-6 / np.abs(d).max()
+            vals = []
+            for sign in (1, -1):
+                q = list(p64)
+                q[i] = p64[i] + sign * h * d
+                vals.append(loss(q))
+            diff = (vals[0] - vals[1]) / (2 * h)
+            # 32-bit gradients (the cascade's within 1e-4 of their size), and the differences' own 1e-16 / h
+            assert abs((g * d).sum() - diff) <= 1e-4 * np.linalg.norm(g) * np.linalg.norm(d) / np.sqrt(g.size) + 1e-8, (i, diff)
+
+
+@pytest.mark.parametrize("head", [None, "bfloat16"])
+def test_step_in_a_graph(env, head):
+    torch, acdc, layers, losses, optim = env
+    N, K, V, T = 256, 2, 700, 200
+    head_type = None if head is None else getattr(torch, head)
+    tokens, targets = batch(torch, T, V, seed=6)
+    start = model(torch, N, K, V, seed=7)
+    acdc.prepare(N)
+
+    def fresh():
+        p = [t.clone() for t in start]
+        return p, [optim.moments(t, 8) for t in p]
+
+    def step(p, m):
+        r, g = explicit(env, p, tokens, targets, 16.0, head_type)
+        clip = optim.grad_norm(g, max_norm=1.0)
+        optim.adamw_step(p, g, m, 1, lr=1e-3, grad_scale=clip[1:])
+        return r.stats, clip
+
+    eager, captured = fresh(), fresh()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(*fresh())
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        stats, clip = step(*captured)
+    for k in range(4):
+        if k == 2:   # another batch, with other rows that take part
+            tokens.copy_(tokens.flip(0))
+            targets.copy_(targets.roll(2))
+        graph.replay()
+        want, want_clip = step(*eager)
+        torch.cuda.synchronize()
+        assert torch.equal(stats, want) and torch.equal(clip, want_clip), k
+        assert all(torch.equal(a, b) for a, b in zip(captured[0], eager[0])), k
+        junk = torch.randn(1 << 20, device="cuda").sum().item()
+        assert junk == junk
+
+
+def test_calls_at_the_same_time(env):
+    """Two streams, each with tensors and workspaces of its own."""
+    torch, _, layers, losses, _ = env
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    jobs = []
+    for k in range(2):
+        gen = torch.Generator().manual_seed(k)
+        h, w = torch.randn(300, 200, generator=gen).cuda(), torch.randn(2000, 200, generator=gen).cuda()
+        jobs.append((h, w, torch.randint(-1, 2000, (300,), generator=gen).cuda(), torch.randint(0, 2000, (3000,), generator=gen).cuda(),
+                     torch.randn(3000, 200, generator=gen).cuda()))
+
+    def run(h, w, t, tok, g):
+        r = losses.vocab_loss(h, w, t)
+        n = layers.layer_norm(g, save=True)
+        return (r.stats, r.grad_hidden, r.grad_weight, *layers.layer_norm_backward(g, n.y, None, n.saved),
+                layers.embedding_backward(tok, g, 2000))
+
+    want = [run(*j) for j in jobs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for k, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[k].append(run(*jobs[k]))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for g in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(g, want[k]))
+
+
+def test_weights_past_32_bit_offsets(env):
+    """600000 x 4096 values, 2^31.2 of them: the last classes are those that count."""
+    torch, _, layers, losses, _ = env
+    V, N = 600_000, 4096
+    print("[case] weight of 600000 x 4096 bfloat16", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    w = torch.empty(V, N, dtype=torch.bfloat16, device="cuda")
+    for r in range(0, V, 50_000):
+        w[r:r + 50_000] = torch.randn(50_000, N, generator=gen, device="cuda") / 64
+    tokens = torch.tensor([V - 1, 5, V - 1, 524_289, V - 2, 524_288], device="cuda")
+    assert torch.equal(layers.embedding(tokens, w), w[tokens])
+    g = torch.randint(-4, 5, (6, N), generator=gen, device="cuda").bfloat16()
+    total = torch.ones(V, N, dtype=torch.bfloat16, device="cuda")
+    layers.embedding_backward(tokens, g, V, grad_weight=total, accumulate=True)
+    want = 1 + g.float()
+    want[0] += g[2].float()
+    assert all(torch.equal(total[tokens[i]].float(), want[i]) for i in (0, 1, 3, 4, 5))
+    touched = torch.zeros(V, dtype=torch.bool, device="cuda")
+    touched[tokens] = True
+    for r in range(0, V, 100_000):
+        assert (total[r:r + 100_000][~touched[r:r + 100_000]] == 1).all()
+    # the loss: logits and gradients of the last classes
+    h = torch.randn(5, N, generator=gen, device="cuda").bfloat16()
+    t = tokens[:5]
+    r = losses.vocab_loss(h, w, t, grad_weight=total)
+    x = torch.cat([h.double() @ w[k:k + 50_000].double().t().contiguous() for k in range(0, V, 50_000)], 1)
+    logp = x.log_softmax(1)
+    lp = logp.gather(1, t[:, None]).squeeze(1)
+    # sums of 4096 products of size 1/64 at the most, in 32 bits: (N + 16) 2^-24 of sum |h w| (below 80)
+    assert (r.logp.double() - lp).abs().max().item() <= 2 * (N + 16) * R.EPS * 80 + 64 * R.EPS
+    G = logp.exp()
+    G[torch.arange(5, device="cuda"), t] -= 1
+    G /= 5
+    rows = torch.tensor([0, 5, 262_144, 524_288, 524_289, V - 2, V - 1], device="cuda")
+    ref = G[:, rows].t().contiguous() @ h.double()
+    # the gradient of the logits is rounded to bfloat16 once, at most twice, and the result again
+    tol = 3 * R.BF16 * (G[:, rows].abs().t().contiguous() @ h.double().abs()) + R.BF16 * ref.abs() + 1e-30
+    assert ((total[rows].double() - ref).abs() <= tol).all()
+    gh = sum(G[:, k:k + 50_000] @ w[k:k + 50_000].double() for k in range(0, V, 50_000))
+    size = sum(G[:, k:k + 50_000].square() @ w[k:k + 50_000].double().square() for k in range(0, V, 50_000)).sqrt()
+    assert ((r.grad_hidden.double() - gh).abs() <= 2 * R.SPREAD * R.BF16 * size + R.BF16 * gh.abs() + 1e-7).all()
+
+
+def test_rows_past_32_bit_offsets(env):
+    torch, _, layers, *_ = env
+    rows, N = 600_000, 4096
+    print("[case] rows of 600000 x 4096 bfloat16", flush=True)
+    x = torch.randn(1000, N, generator=torch.Generator().manual_seed(2)).bfloat16().cuda().repeat(600, 1)
+    r = layers.layer_norm(x, save=True)
+    first = layers.layer_norm(x[:1000], save=True)
+    assert torch.equal(r.y[-1000:], first.y) and torch.equal(r.saved[-1000:], first.saved)
+    gx, gw, gb = layers.layer_norm_backward(x, r.y, None, r.saved)
+    assert torch.equal(gx[-1000:], layers.layer_norm_backward(x[:1000], first.y, None, first.saved)[0])
+    u = (x[:1000].double() - first.saved[:, :1].double()) * first.saved[:, 1:].double()
+    g = first.y.double()
+    # 600000 terms in 512 parts of 1172, in 32 bits: their partial sums are off by (1172 + 512) 2^-24 at the most
+    for got, ref, size in ((gw, 600 * (g * u).sum(0), 600 * (g * u).abs().sum(0)), (gb, 600 * g.sum(0), 600 * g.abs().sum(0))):
+        assert ((got.double() - ref).abs() <= 1700 * R.EPS * size).all()
+
+
+def test_native_refusals_are_put_into_words(env):
+    """What the native part of the binding does not take is refused like on the CPU, before a launch."""
+    torch, _, layers, losses, _ = env
+    h, w, t = torch.randn(6, 10, device="cuda"), torch.randn(12, 10, device="cuda"), torch.zeros(6, dtype=torch.int64, device="cuda")
+    u, saved, f = torch.ones(10, device="cuda"), torch.zeros(6, 2, device="cuda"), torch.zeros(6, device="cuda")
+    before = h.clone()
+    for call, words in ((lambda: losses.vocab_loss(h, w.bfloat16(), t), "one type"), (lambda: losses.vocab_loss(h, w, t, out=h), "overlaps"),
+                        (lambda: losses.vocab_loss(h, w, t, grad_weight=w), "overlaps"), (lambda: losses.vocab_loss(h, w, t.cpu()), "targets"),
+                        (lambda: losses.vocab_loss(h, w[:, ::2], t), "contiguous"), (lambda: losses.vocab_loss(h, w, t, grad="x"), "grad must"),
+                        (lambda: losses.vocab_loss(h, w, t, accumulate=True), "accumulate"),
+                        (lambda: losses.vocab_logprobs(h, w, t[:-1]), "targets"),
+                        (lambda: losses.vocab_logprobs_backward(h, w, t, saved[:-1], f), "saved"),
+                        (lambda: layers.layer_norm(h, u, eps=-1.0), "eps"), (lambda: layers.layer_norm(h, u, out=h), "overlaps"),
+                        (lambda: layers.layer_norm(h, u, dtype=torch.float16), "dtype"), (lambda: layers.layer_norm(h, u[:-1]), "weight"),
+                        (lambda: layers.layer_norm_backward(h, h, u, saved, out=h.t()), "out"),
+                        (lambda: layers.layer_norm_backward(h, h, u, saved, grads=(u, None)), "overlaps"),
+                        (lambda: layers.embedding(t, w, float("nan")), ""), (lambda: layers.embedding(t, w, out=w[:6]), "overlaps"),
+                        (lambda: layers.embedding(t.cpu(), w), "tokens"), (lambda: layers.embedding_backward(t, h, 0), "classes"),
+                        (lambda: layers.embedding_backward(t, h, 12, grad_weight=w.double()), "grad_weight")):
+        with pytest.raises((ValueError, RuntimeError), match=words):
+            call()
+    assert torch.equal(h, before)
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        a = h.clone().requires_grad_(True)
+        gw = torch.empty_like(w)
+        y = (a @ gw.t()).sum()
+        losses.vocab_loss(h, w, t, grad_weight=gw)
+        y.backward()
