@@ -104,8 +104,9 @@ int acdc_norm_forward(const void* x, int32_t x_type, int64_t x_stride, const voi
  * grad_y is of y_type, grad_x of x_type, grad_weight and grad_bias of
  * grads_type; each may be null (not wanted), and with accumulate != 0 the two
  * sums are added to what is there.  grad_x may be grad_y's own memory (same
- * type, pointer and stride).  The sums run in 32 bits over 512 parts of the rows
- * at the most and then over the parts. */
+ * type, pointer and stride).  The sums run in 32 bits over 1024 parts of the
+ * rows at the most and then over the parts.  A
+ * workspace of 256 bytes stands for none: it may be null. */
 int acdc_norm_backward(const void* x, int32_t x_type, int64_t x_stride, const void* grad_y, int32_t y_type,
                        int64_t grad_y_stride, const void* weight, int32_t vector_type, const float* saved, void* grad_x,
                        int64_t grad_x_stride, void* grad_weight, void* grad_bias, int32_t grads_type, int32_t accumulate,

@@ -703,10 +703,10 @@ PyObject* norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int32_t type = gw.defined() ? type_of(gw) : gb.defined() ? type_of(gb) : 0;
     const size_t need = acdc_norm_workspace_size(m.rows, int32_t(std::min<int64_t>(m.width, 0x7fffffff)));
     Tensor ws;
-    if (need == 0 || !m.workspace(ws_in, need, &ws)) Py_RETURN_NONE;
+    if (need == 0 || ((need > 256 || ws_in != nullptr) && !m.workspace(ws_in, need, &ws))) Py_RETURN_NONE;
     const int rc = acdc_norm_backward(x->data_ptr(), m.dtype, m.stride, gy->data_ptr(), g.dtype, g.stride, ptr<void>(weight),
                                       weight != nullptr ? type_of(*weight) : 0, ptr(saved), ptr<void>(gx), to.stride, ptr<void>(gw),
-                                      ptr<void>(gb), type, accumulate ? 1 : 0, m.rows, int32_t(m.width), ws.data_ptr(), need, stream);
+                                      ptr<void>(gb), type, accumulate ? 1 : 0, m.rows, int32_t(m.width), ptr<void>(ws), need, stream);
     if (refused(rc)) Py_RETURN_NONE;
     if (rc != ACDC_OK) return PyLong_FromLong(rc);
     if (want_x) wrote(out);

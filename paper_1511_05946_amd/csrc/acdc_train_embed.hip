@@ -136,6 +136,15 @@ __device__ __forceinline__ int place_of(int* next, bool here, int digit, int bit
   return to;
 }
 
+// Zeros over the rows v, v + step, ... of the gradient, by a wave.
+template <class TW>
+__device__ __forceinline__ void fill_zeros(typename TW::Elem* weight, long long stride, int width, int classes, long long v, int step) {
+  const float zero[kEight] = {};
+  for (; v < classes; v += step)
+    for (int col = 0; col < width; col += kSpan)
+      Columns<kApart<TW, TW>>(col, threadIdx.x % 64, width).template store<TW>(weight + v * stride, zero);
+}
+
 // Up to 8192 rows by the first workgroup, in LDS, while the others (if there are any) write
 // zeros over the gradient.
 constexpr int kSmallThreads = 1024, kSmallEach = 8, kSmall = kSmallThreads * kSmallEach;
@@ -148,9 +157,7 @@ __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const void* __rest
   __shared__ int keys[kSmall], rows[kSmall], slots[WAVES];
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, base = wave * (64 * kSmallEach);
   if (blockIdx.x > 0) {
-    const float zero[kEight] = {};
-    for (long long v = (blockIdx.x - 1) * WAVES + wave; v < classes; v += (gridDim.x - 1) * WAVES)
-      for (int col = 0; col < width; col += kSpan) Columns<kApart<TW, TW>>(col, lane, width).template store<TW>(weight + v * weight_stride, zero);
+    fill_zeros<TW>(weight, weight_stride, width, classes, (blockIdx.x - 1) * WAVES + wave, (gridDim.x - 1) * WAVES);
     return;
   }
   int key[kSmallEach], row[kSmallEach];
@@ -210,10 +217,18 @@ __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const void* __rest
 // to its place, a pass in three launches.
 constexpr int kEach = 8, kTile = kThreads * kEach, kPerThread = kDigits / kThreads;
 
+// The tokens that are there are marked in `there` or, where that is null, the workgroups past
+// the tiles (if there are any) write zeros over the gradient.
+template <class TW>
 __global__ __launch_bounds__(kThreads) void k_sort_count(const void* __restrict__ tokens, int bits, int classes, Sorted in, int n,
                                                          int shift, int mask, int* __restrict__ counts,
-                                                         unsigned char* __restrict__ there) {
+                                                         unsigned char* __restrict__ there, int tiles,
+                                                         typename TW::Elem* __restrict__ weight, long long weight_stride, int width) {
   __shared__ int bins[kDigits];
+  if (int(blockIdx.x) >= tiles) {
+    fill_zeros<TW>(weight, weight_stride, width, classes, (blockIdx.x - tiles) * kWaves + threadIdx.x / 64, (gridDim.x - tiles) * kWaves);
+    return;
+  }
 #pragma unroll
   for (int d = 0; d < kPerThread; ++d) bins[d * kThreads + threadIdx.x] = 0;
   __syncthreads();
@@ -223,7 +238,7 @@ __global__ __launch_bounds__(kThreads) void k_sort_count(const void* __restrict_
     if (i < n) {
       // in the first pass the keys come from the tokens, and are marked as there
       const int k = tokens != nullptr ? key_of(tokens, bits, i, classes) : in.key[i];
-      if (tokens != nullptr && k < classes) there[k] = 1;
+      if (there != nullptr && k < classes) there[k] = 1;
       atomicAdd(&bins[(k >> shift) & mask], 1);
     }
   }
@@ -571,6 +586,9 @@ extern "C" int acdc_embedding_backward(const void* tokens, int32_t token_bits, c
   const int passes = (key_bits + kMostBits - 1) / kMostBits, digit_bits = (key_bits + passes - 1) / passes, n = int(rows);
   int at = 0;
   const bool small = rows <= kSmall;
+  // zeros over everything before the sums are written, or only where no token is: the first
+  // writes up to `rows` rows twice, the second takes two launches
+  const bool mark = !small && accumulate == 0 && classes > rows / 4;
   if (small) {
     const int64_t fill = accumulate != 0 ? 0 : std::min<int64_t>((classes + 15) / 16, 1023);
     with_types(out_type, weight_type, [&]<class TG, class TW>() {
@@ -578,13 +596,18 @@ extern "C" int acdc_embedding_backward(const void* tokens, int32_t token_bits, c
                          digit_bits, passes, static_cast<typename TW::Elem*>(grad_weight), (long long)weight_stride, width);
     });
   } else {
-    hipLaunchKernelGGL(k_embed_clear, dim3(unsigned(std::min<int64_t>((classes + kThreads - 1) / kThreads, 1024))), dim3(kThreads), 0,
-                       s, there, classes);
+    if (mark)
+      hipLaunchKernelGGL(k_embed_clear, dim3(unsigned(std::min<int64_t>((classes + kThreads - 1) / kThreads, 1024))), dim3(kThreads), 0,
+                         s, there, classes);
     const int tiles = (n + kTile - 1) / kTile;
     for (int pass = 0; pass < passes; ++pass, at ^= 1) {
       const void* from = pass == 0 ? tokens : nullptr;
-      hipLaunchKernelGGL(k_sort_count, dim3(unsigned(tiles)), dim3(kThreads), 0, s, from, token_bits, classes, pairs[at], n,
-                         pass * digit_bits, (1 << digit_bits) - 1, counts, there);
+      const int fill = pass == 0 && accumulate == 0 && !mark ? int(std::min<int64_t>((classes + kWaves - 1) / kWaves, 2048)) : 0;
+      with_types(out_type, weight_type, [&]<class TG, class TW>() {
+        hipLaunchKernelGGL(k_sort_count<TW>, dim3(unsigned(tiles + fill)), dim3(kThreads), 0, s, from, token_bits, classes, pairs[at], n,
+                           pass * digit_bits, (1 << digit_bits) - 1, counts, pass == 0 && mark ? there : nullptr, tiles,
+                           static_cast<typename TW::Elem*>(grad_weight), (long long)weight_stride, width);
+      });
       hipLaunchKernelGGL(k_sort_sums, dim3(kDigits / 64), dim3(64 * kSumWaves), 0, s, counts, tiles, totals);
       hipLaunchKernelGGL(k_sort_move, dim3(unsigned(tiles)), dim3(kThreads), 0, s, from, token_bits, classes, pairs[at], pairs[at ^ 1],
                          n, pass * digit_bits, digit_bits, counts, totals);
@@ -592,7 +615,7 @@ extern "C" int acdc_embedding_backward(const void* tokens, int32_t token_bits, c
   }
   with_types(out_type, weight_type, [&]<class TG, class TW>() {
     typename TW::Elem* out = static_cast<typename TW::Elem*>(grad_weight);
-    if (accumulate == 0 && !small)
+    if (mark)
       hipLaunchKernelGGL(k_embed_zeros<TW>, dim3(unsigned(std::min<int64_t>((classes + kWaves - 1) / kWaves, 8192))), dim3(kThreads),
                          0, s, there, classes, width, out, (long long)weight_stride);
     if (rows == 0) return;

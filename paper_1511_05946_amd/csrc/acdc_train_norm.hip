@@ -45,6 +45,7 @@ struct RowSum {
 
 template <int LANES, int THREADS = kThreads>
 struct Group {
+  static_assert(LANES <= 64 || LANES >= kThreads, "rows that share a workgroup have no barrier");
   static constexpr int WG = LANES < THREADS ? THREADS : LANES, ROWS = WG / LANES;
 };
 // The two sums over the rows: where they go, and whether they are added there.
@@ -168,8 +169,8 @@ struct BackArgs {
   long long x_stride, gy_stride, gx_stride;
   const float2* saved;
   Vector weight;
-  float* sums;  // [workgroups][2][width], null: not wanted
-  Sums out;     // of a single workgroup, which writes them itself
+  float* sums;  // [workgroups][2][width]; null: a single workgroup writes `out` itself
+  Sums out;
   int rows, width;
 };
 
@@ -187,28 +188,21 @@ __global__ __launch_bounds__((Group<LANES, THREADS>::WG)) void k_norm_back(BackA
     const int col = (lane + q * LANES) * kEight;
     load_vector(a.weight, col, width - col, 1.f, w[q]);
   }
-  for (int r = blockIdx.x * ROWS + group; r < a.rows; r += gridDim.x * ROWS) {
-    const float2 st = a.saved[r];
-    float u[NC][kEight], g[NC][kEight];
-#pragma unroll
-    for (int q = 0; q < NC; ++q) {
-      const int col = (lane + q * LANES) * kEight;
-      load_some<TX>(a.x + r * a.x_stride + col, width - col, st.x, u[q]);
-      load_some<TY>(a.gy + r * a.gy_stride + col, width - col, 0.f, g[q]);
-    }
+  // a row less what it needs of the workgroup
+  float u[NC][kEight], g[NC][kEight];
+  auto finish = [&](int r, const float2& st) {
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int q = 0; q < NC; ++q)
 #pragma unroll
       for (int i = 0; i < kEight; ++i) {
-        u[q][i] = (u[q][i] - st.x) * st.y;
         gb[q][i] += g[q][i];
         gw[q][i] += g[q][i] * u[q][i];
         g[q][i] *= w[q][i];
         s1 += g[q][i];
         s2 += g[q][i] * u[q][i];
       }
-    if (a.gx == nullptr) continue;
+    if (a.gx == nullptr) return;
     const float m1 = sum(s1) * inv, m2 = sum(s2) * inv;
     typename TX::Elem* to = a.gx + r * a.gx_stride;
 #pragma unroll
@@ -219,10 +213,51 @@ __global__ __launch_bounds__((Group<LANES, THREADS>::WG)) void k_norm_back(BackA
       for (int i = 0; i < kEight; ++i) g[q][i] = st.y * (g[q][i] - m1 - u[q][i] * m2);
       store_some<TX>(to + col, width - col, g[q]);
     }
+  };
+  const int step = gridDim.x * ROWS;
+  int r = blockIdx.x * ROWS + group;
+  if constexpr (NC == 1) {
+    // the next row is on its way while this one is summed and written
+    Raw8<TX> x;
+    Raw8<TY> gy;
+    float2 next = make_float2(0.f, 0.f);
+    const int col = lane * kEight;
+    auto ask = [&](int from) {
+      if (from >= a.rows) return;
+      next = a.saved[from];
+      x.load(a.x + from * a.x_stride + col, width - col);
+      gy.load(a.gy + from * a.gy_stride + col, width - col);
+    };
+    ask(r);
+    for (; r < a.rows; r += step) {
+      const float2 st = next;
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) {
+        u[0][i] = (x.get(i) - st.x) * st.y;
+        g[0][i] = gy.get(i);
+      }
+      ask(r + step);
+      finish(r, st);
+    }
+  } else {
+    for (; r < a.rows; r += step) {
+      const float2 st = a.saved[r];
+#pragma unroll
+      for (int q = 0; q < NC; ++q) {
+        const int col = (lane + q * LANES) * kEight;
+        load_some<TX>(a.x + r * a.x_stride + col, width - col, st.x, u[q]);
+        load_some<TY>(a.gy + r * a.gy_stride + col, width - col, 0.f, g[q]);
+      }
+#pragma unroll
+      for (int q = 0; q < NC; ++q)
+#pragma unroll
+        for (int i = 0; i < kEight; ++i) u[q][i] = (u[q][i] - st.x) * st.y;
+      finish(r, st);
+    }
   }
-  if (a.sums == nullptr) return;
+  if (a.out.weight == nullptr && a.out.bias == nullptr) return;
+  const bool alone = a.sums == nullptr;
   float* out = a.sums + (long long)blockIdx.x * 2 * width;
-  const bool alone = gridDim.x == 1;
   if constexpr (ROWS == 1) {
 #pragma unroll
     for (int q = 0; q < NC; ++q) {
@@ -323,7 +358,7 @@ __global__ __launch_bounds__(64) void k_norm_columns(BackArgs<TX, TY> a, int eac
 
 // The parts' sums together, in order: 64 columns a workgroup, its waves take the parts
 // in turn.
-constexpr int kSumWaves = 8;
+constexpr int kSumWaves = 16;
 __global__ __launch_bounds__(64 * kSumWaves) void k_norm_sums(const float* __restrict__ sums, int parts, int width, Sums out) {
   __shared__ float slots[kSumWaves][64];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, at = blockIdx.x * 64 + lane;  // of 2 width
@@ -344,14 +379,14 @@ __global__ __launch_bounds__(64 * kSumWaves) void k_norm_sums(const float* __res
 // ------------------------------------------------------------------ on the host
 
 constexpr int kMostWidth = 1 << 24;
-constexpr int kHeld = 16384;  // values of a row that registers hold
-constexpr int kMostParts = 512;
+constexpr int kHeld = 32768, kHeldBack = 16384;  // values of a row that registers hold, forward and backward
+constexpr int kMostParts = 512;  // of rows of a workgroup; twice as many where a workgroup has several
 
 int done() {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? ACDC_OK : hip_fail(e);
 }
-// f.template operator()<LANES, NC>() for rows of up to kHeld values.
+// f.template operator()<LANES, NC>() for rows of up to kHeld values (kHeldBack below).
 template <class F>
 void with_row(int width, F&& f) {
   if (width <= 128) f.template operator()<16, 1>();
@@ -361,7 +396,20 @@ void with_row(int width, F&& f) {
   else if (width <= 2048) f.template operator()<256, 1>();
   else if (width <= 4096) f.template operator()<256, 2>();
   else if (width <= 8192) f.template operator()<512, 2>();
-  else f.template operator()<512, 4>();
+  else if (width <= 16384) f.template operator()<512, 4>();
+  else f.template operator()<1024, 4>();
+}
+// The same for the backward pass, which has more to hold.
+template <class F>
+void with_row_back(int width, F&& f) {
+  if (width <= 128) f.template operator()<16, 1>();
+  else if (width <= 256) f.template operator()<16, 2>();
+  else if (width <= 512) f.template operator()<64, 1>();
+  else if (width <= 1024) f.template operator()<64, 2>();
+  else if (width <= 2048) f.template operator()<256, 1>();
+  else if (width <= 4096) f.template operator()<512, 1>();
+  else if (width <= 8192) f.template operator()<1024, 1>();
+  else f.template operator()<1024, 2>();
 }
 template <class F>
 int with_types(int32_t x, int32_t y, F&& f) {
@@ -389,11 +437,14 @@ bool few(int64_t rows, int32_t width) { return rows <= (width <= 256 ? 64 : widt
 // rows: those of the second one).
 int parts_of(int64_t rows, int32_t width) {
   if (rows == 0) return 0;
-  if (width > kHeld) return int(std::min<int64_t>(rows, 64));
+  if (width > kHeldBack) return int(std::min<int64_t>(rows, 64));
   int per = 1;
-  with_row(width, [&]<int LANES, int NC>() { per = few(rows, width) ? 1024 / LANES : Group<LANES>::ROWS; });
-  return int(std::min<int64_t>((rows + per - 1) / per, kMostParts));
+  with_row_back(width, [&]<int LANES, int NC>() { per = few(rows, width) ? 1024 / LANES : Group<LANES>::ROWS; });
+  return int(std::min<int64_t>((rows + per - 1) / per, width <= 2048 ? 2 * kMostParts : width <= 8192 ? kMostParts : kMostParts / 2));
 }
+
+// One workgroup writes the sums itself and needs no workspace.
+bool alone(int64_t rows, int32_t width) { return width <= kHeldBack && parts_of(rows, width) <= 1; }
 
 }  // namespace
 }  // namespace acdc
@@ -434,7 +485,8 @@ extern "C" int acdc_norm_forward(const void* x, int32_t x_type, int64_t x_stride
 }
 
 extern "C" size_t acdc_norm_workspace_size(int64_t rows, int32_t width) {
-  return sizes_ok(rows, width) ? std::max<size_t>(256, size_t(parts_of(rows, width)) * 2 * size_t(width) * 4) : 0;
+  if (!sizes_ok(rows, width)) return 0;
+  return alone(rows, width) ? 256 : std::max<size_t>(512, size_t(parts_of(rows, width)) * 2 * size_t(width) * 4);
 }
 
 extern "C" int acdc_norm_backward(const void* x, int32_t x_type, int64_t x_stride, const void* grad_y, int32_t y_type,
@@ -463,7 +515,7 @@ extern "C" int acdc_norm_backward(const void* x, int32_t x_type, int64_t x_strid
   }
   const bool sums = grad_weight != nullptr || grad_bias != nullptr;
   const size_t need = acdc_norm_workspace_size(rows, width);
-  if (sums && (workspace == nullptr || workspace_bytes < need)) return ACDC_ERR_WORKSPACE;
+  if (sums && !alone(rows, width) && (workspace == nullptr || workspace_bytes < need)) return ACDC_ERR_WORKSPACE;
   if (!aligned_to(workspace, 16)) return ACDC_ERR_INVALID_ARG;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const int parts = parts_of(rows, width);
@@ -473,8 +525,8 @@ extern "C" int acdc_norm_backward(const void* x, int32_t x_type, int64_t x_strid
       const BackArgs<TX, TY> a{static_cast<const typename TX::Elem*>(x), static_cast<const typename TY::Elem*>(grad_y),
                                static_cast<typename TX::Elem*>(grad_x), x_stride, grad_y_stride, grad_x_stride,
                                reinterpret_cast<const float2*>(saved), Vector{weight, vector_type},
-                               sums ? static_cast<float*>(workspace) : nullptr, out_sums, int(rows), width};
-      if (width > kHeld) {
+                               alone(rows, width) ? nullptr : static_cast<float*>(workspace), out_sums, int(rows), width};
+      if (width > kHeldBack) {
         // the sums first: grad_x may take grad_y's place
         if (sums) {
           const int each = int((rows + parts - 1) / parts), blocks = (width + 64 * kEight - 1) / (64 * kEight);
@@ -483,7 +535,7 @@ extern "C" int acdc_norm_backward(const void* x, int32_t x_type, int64_t x_strid
         if (grad_x != nullptr)
           hipLaunchKernelGGL((k_norm_back_long<TX, TY, 1024>), dim3(unsigned(std::min<int64_t>(rows, 1 << 16))), dim3(1024), 0, s, a);
       } else {
-        with_row(width, [&]<int LANES, int NC>() {
+        with_row_back(width, [&]<int LANES, int NC>() {
           if constexpr (LANES <= 64) {
             if (few(rows, width)) {
               hipLaunchKernelGGL((k_norm_back<TX, TY, LANES, NC, 1024>), dim3(1), dim3(1024), 0, s, a);
@@ -497,7 +549,7 @@ extern "C" int acdc_norm_backward(const void* x, int32_t x_type, int64_t x_strid
     });
     if (rc != ACDC_OK) return rc;
   }
-  if (!sums || (rows == 0 && accumulate != 0) || (parts == 1 && width <= kHeld)) return ACDC_OK;
+  if (!sums || (rows == 0 && accumulate != 0) || (rows > 0 && alone(rows, width))) return ACDC_OK;
   hipLaunchKernelGGL(k_norm_sums, dim3(unsigned((2 * int64_t(width) + 63) / 64)), dim3(64 * kSumWaves), 0, s,
                      static_cast<const float*>(workspace), parts, width, out_sums);
   return done();

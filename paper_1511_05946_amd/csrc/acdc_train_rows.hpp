@@ -43,6 +43,25 @@ __device__ __forceinline__ void store_some(typename T::Elem* p, int left, const 
   }
 }
 
+// Eight as they lie in memory (those behind `left` are 0), to be asked for ahead.
+template <class T>
+struct Raw8 {
+  typename T::Raw raw[kEight / T::kPer];
+  __device__ __forceinline__ void load(const typename T::Elem* p, int left) {
+    if (left >= kEight) {
+#pragma unroll
+      for (int q = 0; q < kEight / T::kPer; ++q) raw[q] = load_chunk<T>(p + q * T::kPer);
+    } else {
+      float v[kEight];
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) v[i] = i < left ? T::one(p[i]) : 0.f;
+#pragma unroll
+      for (int q = 0; q < kEight / T::kPer; ++q) raw[q] = T::pack(v + q * T::kPer);
+    }
+  }
+  __device__ __forceinline__ float get(int i) const { return T::get(raw[i / T::kPer], i % T::kPer); }
+};
+
 // The same in 512 columns from `col` on, for the lanes of a wave: eight columns a lane
 // that follow one another or, with APART, four and 256 columns on four more.  32 bytes a
 // lane would be two instructions that each touch half of every line.

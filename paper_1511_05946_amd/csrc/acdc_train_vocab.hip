@@ -55,6 +55,13 @@ struct Factor {
   bool mean;
 };
 
+__device__ __forceinline__ void finish_rows(const Factor& factor, const Rows& out, double sum, int used) {
+  *out.total = sum;
+  *out.count = used;
+  const float f = factor.device != nullptr ? *factor.device : factor.host;
+  *out.factor = !factor.mean ? f : sum == 0.0 ? 0.f : float(double(f) / sum);
+}
+
 constexpr int kWide = 1024, kEach = 8;
 
 // Packs the rows in use, in order, and clears the outputs of the others.  One
@@ -130,12 +137,61 @@ __global__ __launch_bounds__(kWide) void k_vocab_rows(const void* __restrict__ t
   if (tid == 0) {
     double all = 0.0;
     for (int k = 0; k < kWide / 64; ++k) all += sums[k];
-    *out.total = all;
-    *out.count = done;
-    const float f = factor.device != nullptr ? *factor.device : factor.host;
-    *out.factor = !factor.mean ? f : all == 0.0 ? 0.f : float(double(f) / all);
+    finish_rows(factor, out, all, done);
   }
 }
+
+// The same of up to 64 rows by a wave, a row a lane.
+struct FewRows {
+  const void* targets;
+  const float* weights;
+  int bits, rows, classes;
+  Factor factor;
+  Rows out;
+  float* logp;
+  float2* saved;
+  float* row_grads;
+  // `at` (LDS) gets the rows in use in order; returns their number.  All waves of a workgroup
+  // write the same; `first` writes what is kept.
+  __device__ __forceinline__ int order(int* at, bool first) const {
+    const int r = threadIdx.x % 64;
+    int t = -1;
+    float w = 1.f;
+    if (r < rows) {
+      const long long v = bits == 64 ? static_cast<const long long*>(targets)[r] : (long long)static_cast<const int*>(targets)[r];
+      t = v < 0 ? -1 : v >= classes ? -2 : int(v);
+      if (weights != nullptr) w = weights[r];
+    }
+    const bool in_use = t != -1 && w != 0.f;
+    const unsigned long long all = __ballot(in_use);
+    const int place = __popcll(all & ((1ull << r) - 1)), used = __popcll(all);
+    if (in_use) at[place] = r;
+    if (!first || threadIdx.x >= 64) return used;
+    double sum = in_use ? double(w) : 0.0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if (in_use) {
+      out.order[place] = r;
+      out.target[place] = t;
+      out.share[place] = w;
+    } else {
+      const int behind = used + __popcll(~all & ((1ull << r) - 1));   // the places that are left, of 64
+      out.order[behind] = 0;
+      out.target[behind] = -1;
+      out.share[behind] = 0.f;
+    }
+    if (r < rows) {
+      out.at[r] = in_use ? place : -1;
+      if (!in_use) {
+        if (logp != nullptr) logp[r] = 0.f;
+        if (saved != nullptr) saved[r] = make_float2(0.f, 1.f);
+        if (row_grads != nullptr) row_grads[r] = 0.f;
+      }
+    }
+    if (r == 0) finish_rows(factor, out, sum, used);
+    return used;
+  }
+};
 
 // Rows as the matrix cores take them: bfloat16 (three planes for float32), `padded`
 // wide, at multiples of 16 bytes.  With `order` the packed rows, zeros past *count.
@@ -148,11 +204,21 @@ struct Pack {
   __bf16* out;
   long long plane;
 };
-// Two of them in one launch (the second may have no rows).
-template <class T>
-__global__ __launch_bounds__(256) void k_vocab_pack(Pack<T> first, Pack<T> second, const int* __restrict__ count, int width,
-                                                    int padded) {
-  const int per = padded / 8, used = *count;
+// Two of them in one launch (the second may have no rows).  FEW: up to 64 rows, which every
+// wave puts in order by itself, and the first one for the launches to come.
+template <class T, bool FEW>
+__global__ __launch_bounds__(256) void k_vocab_pack(Pack<T> first, Pack<T> second, FewRows few, const int* __restrict__ count,
+                                                    int width, int padded) {
+  __shared__ int order[64];
+  int used;
+  if constexpr (FEW) {
+    used = few.order(order, blockIdx.x == 0);
+    __syncthreads();
+    first.order = order;
+  } else {
+    used = *count;
+  }
+  const int per = padded / 8;
   const long long split = (long long)first.rows * per, chunks = split + (long long)second.rows * per;
   for (long long base = blockIdx.x * 256ll; base < chunks; base += gridDim.x * 256ll) {
     // (one long division for the workgroup, a short one for the lane)
@@ -430,6 +496,23 @@ __global__ __launch_bounds__(256) void k_vocab_few_slopes(FewLogits l, const Row
   put_planes<PLANES, 1, One>(out + (long long)r * l.ld + v, plane, y);
 }
 
+// f(n, m) for the squares of a wave: with bounds where the tile reaches past M or N.
+template <class S, int MI, int NI, class SP, class F>
+__device__ __forceinline__ void squares(const SP& spot, const Place& at, int M, int N, F&& f) {
+  if ((at.tm + 1) * S::BM <= M && (at.tn + 1) * S::BN <= N) {
+#pragma unroll
+    for (int n = 0; n < NI; ++n)
+#pragma unroll
+      for (int m = 0; m < MI; ++m) f.template operator()<true>(n, m);
+  } else {
+#pragma unroll
+    for (int n = 0; n < NI; ++n)
+#pragma unroll
+      for (int m = 0; m < MI; ++m)
+        if (spot.m(m) < M && spot.n(n) < N) f.template operator()<false>(n, m);
+  }
+}
+
 // 32-bit sums of a part: out[part][n][m], added to what earlier pieces left.
 struct PartOut {
   float* out;
@@ -438,14 +521,16 @@ struct PartOut {
   bool add;
   template <class S, int MI, int NI, class SP>
   __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const SP& spot, const Place& at, int, float2*) const {
-#pragma unroll
-    for (int n = 0; n < NI; ++n)
-#pragma unroll
-      for (int m = 0; m < MI; ++m) {
-        if (spot.m(m) >= ld || spot.n(n) >= rows) continue;
-        f32x4* to = reinterpret_cast<f32x4*>(out + at.part * part + (long long)spot.n(n) * ld + spot.m(m));
-        *to = add ? *to + acc[m][n] : acc[m][n];
-      }
+    float* to = out + at.part * part;
+    auto each = [&]<bool ADD>() {
+      squares<S, MI, NI>(spot, at, ld, rows, [&]<bool INSIDE>(int n, int m) {
+        f32x4* p = reinterpret_cast<f32x4*>(to + (long long)spot.n(n) * ld + spot.m(m));
+        if constexpr (ADD) *p += acc[m][n];
+        else *p = acc[m][n];
+      });
+    };
+    if (add) each.template operator()<true>();
+    else each.template operator()<false>();
   }
 };
 
@@ -477,14 +562,17 @@ struct GradOut {
   int width, classes;
   bool whole, add;
   template <class S, int MI, int NI, class SP>
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const SP& spot, const Place&, int, float2*) const {
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const SP& spot, const Place& at, int, float2*) const {
     const float f = *factor;
-#pragma unroll
-    for (int n = 0; n < NI; ++n)
-#pragma unroll
-      for (int m = 0; m < MI; ++m)
-        if (spot.n(n) < classes)
-          put4<T>(out + spot.n(n) * ld + spot.m(m), acc[m][n] * f, width - spot.m(m), whole, add);
+    auto each = [&]<bool PLAIN>() {
+      squares<S, MI, NI>(spot, at, width, classes, [&]<bool INSIDE>(int n, int m) {
+        typename T::Elem* to = out + spot.n(n) * ld + spot.m(m);
+        if constexpr (PLAIN && INSIDE) put4<T>(to, acc[m][n] * f, 4, true, false);
+        else put4<T>(to, acc[m][n] * f, width - spot.m(m), whole, add);
+      });
+    };
+    if (whole && !add) each.template operator()<true>();
+    else each.template operator()<false>();
   }
 };
 
@@ -744,22 +832,29 @@ struct Call {
 
   static unsigned grid(int64_t items) { return unsigned(std::min<int64_t>((items + 255) / 256, 1 << 16)); }
 
-  void pack(const Pack<T>& first, const Pack<T>& second) const {
-    hipLaunchKernelGGL(k_vocab_pack<T>, dim3(grid((int64_t(first.rows) + second.rows) * (p.padded_width / 8))), dim3(256), 0, s, first,
-                       second, rows.count, p.width, p.padded_width);
+  unsigned pack_grid(const Pack<T>& first, const Pack<T>& second) const {
+    return grid((int64_t(first.rows) + second.rows) * (p.padded_width / 8));
   }
   int64_t weight_plane() const { return int64_t(p.piece) * p.padded_width; }
   Pack<T> weight_job(int k) const {
     const typename T::Elem* from = static_cast<const typename T::Elem*>(head.weight) + int64_t(k) * p.piece * head.weight_stride;
     return {from, head.weight_stride, nullptr, classes_of(k), get<__bf16>(w.weight), weight_plane()};
   }
+  // the rows in use and, with them, the first piece of the weight
   void pack_rows(const float* weights, const Factor& factor, float* logp, float2* saved, float* row_grads) const {
-    hipLaunchKernelGGL(k_vocab_rows, dim3(1), dim3(kWide), 0, s, head.targets, head.target_bits, weights, int(p.rows),
-                       int(p.padded_rows), p.classes, factor, rows, logp, saved, row_grads);
-    // the rows and, with them, the first piece of the weight
-    pack({static_cast<const typename T::Elem*>(head.hidden), head.hidden_stride, rows.order, int(p.padded_rows), get<__bf16>(w.hidden),
-          hidden_plane()},
-         direct ? Pack<T>{} : weight_job(0));
+    const Pack<T> hidden{static_cast<const typename T::Elem*>(head.hidden), head.hidden_stride, rows.order, int(p.padded_rows),
+                         get<__bf16>(w.hidden), hidden_plane()};
+    const Pack<T> weight = direct ? Pack<T>{} : weight_job(0);
+    const FewRows few{head.targets, weights, head.target_bits, int(p.rows), p.classes, factor, rows, logp, saved, row_grads};
+    if (p.rows <= 64) {
+      hipLaunchKernelGGL((k_vocab_pack<T, true>), dim3(pack_grid(hidden, weight)), dim3(256), 0, s, hidden, weight, few, rows.count,
+                         p.width, p.padded_width);
+    } else {
+      hipLaunchKernelGGL(k_vocab_rows, dim3(1), dim3(kWide), 0, s, head.targets, head.target_bits, weights, int(p.rows),
+                         int(p.padded_rows), p.classes, factor, rows, logp, saved, row_grads);
+      hipLaunchKernelGGL((k_vocab_pack<T, false>), dim3(pack_grid(hidden, weight)), dim3(256), 0, s, hidden, weight, few, rows.count,
+                         p.width, p.padded_width);
+    }
   }
   int64_t hidden_plane() const { return p.padded_rows * p.padded_width; }
   int classes_of(int k) const { return std::min(p.piece, p.classes - k * p.piece); }
@@ -771,7 +866,9 @@ struct Call {
     const int n = classes_of(k);
     const Pack<T> job = weight_job(k);
     if (direct) return Operand{reinterpret_cast<const __bf16*>(job.x), head.weight_stride, 0, n, p.width};
-    if (!packed) pack(job, Pack<T>{});
+    if (!packed)
+      hipLaunchKernelGGL((k_vocab_pack<T, false>), dim3(pack_grid(job, Pack<T>{})), dim3(256), 0, s, job, Pack<T>{}, FewRows{},
+                         rows.count, p.width, p.padded_width);
     return Operand{job.out, p.padded_width, weight_plane(), n, p.padded_width};
   }
   Operand grad(int k) const {

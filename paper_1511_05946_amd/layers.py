@@ -21,6 +21,7 @@ differentiable forms (first derivatives; a second one raises).
 from __future__ import annotations
 
 import functools
+import math
 from typing import NamedTuple, Optional
 
 import torch
@@ -168,6 +169,11 @@ def _embedding_bytes(rows, width, classes):
     return lib().acdc_embedding_workspace_size(rows, width, classes)
 
 
+def _finite(scale):
+    if not math.isfinite(scale):
+        raise ValueError(f"scale must be finite, got {scale}")
+
+
 def embedding(tokens, weight, scale: float = 1.0, dtype=None, out=None):
     """scale * weight[tokens]: [rows, width] of ``dtype`` (default: the weight's).
     A negative token gives a row of zeros, one past the weight's rows a row of NaN."""
@@ -180,6 +186,7 @@ def embedding(tokens, weight, scale: float = 1.0, dtype=None, out=None):
     bits = _index("tokens", tokens, rows, device)
     if classes < 1:
         raise ValueError("weight must have a class at least")
+    _finite(scale)
     if out is None:
         y = torch.empty(rows, width, dtype=_type("dtype", dtype, weight.dtype), device=device)
         y_stride = width
@@ -208,6 +215,7 @@ def embedding_backward(tokens, grad_rows, classes: int, scale: float = 1.0, dtyp
     bits = _index("tokens", tokens, rows, device)
     if classes < 1:
         raise ValueError(f"classes must be positive, got {classes}")
+    _finite(scale)
     if grad_weight is None:
         if accumulate:
             raise ValueError("accumulate needs the grad_weight to add to")

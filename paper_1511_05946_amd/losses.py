@@ -31,6 +31,7 @@ second one raises).
 from __future__ import annotations
 
 import functools
+import math
 import struct
 from typing import NamedTuple, Optional
 
@@ -499,6 +500,8 @@ def vocab_loss(hidden, weight, targets, weights=None, mean: bool = True, grad_sc
     head, ws, need = _vocab_head(hidden, weight, targets, any_grad, workspace)
     rows, device = hidden.shape[0], hidden.device
     _vector("weights", weights, rows, device)
+    if not math.isfinite(grad_scale):
+        raise ValueError(f"grad_scale must be finite, got {grad_scale}")
     record, gh, gw = _vocab_grads(hidden, weight, out, grad_weight, accumulate, wanted) if any_grad else (None, None, None)
     stats, logp = torch.empty(2, device=device), torch.empty(rows, device=device)
     saved = torch.empty(rows, 2, device=device) if save else None

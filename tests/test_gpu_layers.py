@@ -32,7 +32,8 @@ NORM = [(1, 1, 0, "float32", "float32", "float32"), (2, 2, 1, "bfloat16", "float
         (4, 8200, 0, "bfloat16", "float32", "float32"), (520, 9216, 0, "float32", "float32", "float32"),
         (3, 16384, 0, "bfloat16", "bfloat16", "float32"), (3, 16385, 0, "float32", "bfloat16", "float32"),
         (70, 33001, 7, "bfloat16", "bfloat16", "bfloat16"), (2, 65536, 0, "float32", "float32", "float32"),
-        (9000, 16, 0, "float32", "float32", "float32"), (20000, 3, 2, "bfloat16", "float32", "float32")]
+        (9000, 16, 0, "float32", "float32", "float32"), (20000, 3, 2, "bfloat16", "float32", "float32"),
+        (82, 3, 0, "float32", "float32", "float32"), (65, 1, 0, "bfloat16", "bfloat16", "float32"), (17, 300, 0, "float32", "float32", "bfloat16")]
 
 
 def make(torch, shape, seed=0, offset=0.5):

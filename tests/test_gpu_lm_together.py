@@ -253,7 +253,7 @@ def test_native_refusals_are_put_into_words(env):
                         (lambda: layers.layer_norm(h, u, dtype=torch.float16), "dtype"), (lambda: layers.layer_norm(h, u[:-1]), "weight"),
                         (lambda: layers.layer_norm_backward(h, h, u, saved, out=h.t()), "out"),
                         (lambda: layers.layer_norm_backward(h, h, u, saved, grads=(u, None)), "overlaps"),
-                        (lambda: layers.embedding(t, w, float("nan")), ""), (lambda: layers.embedding(t, w, out=w[:6]), "overlaps"),
+                        (lambda: layers.embedding(t, w, float("nan")), "scale"), (lambda: layers.embedding(t, w, out=w[:6]), "overlaps"),
                         (lambda: layers.embedding(t.cpu(), w), "tokens"), (lambda: layers.embedding_backward(t, h, 0), "classes"),
                         (lambda: layers.embedding_backward(t, h, 12, grad_weight=w.double()), "grad_weight")):
         with pytest.raises((ValueError, RuntimeError), match=words):

@@ -110,7 +110,8 @@ def test_norm_calls(L):
                 dict(gx=x), dict(gx=y + 40), dict(gx=y, gxs=11), dict(gx=y, yt=1), dict(gw=gb), dict(gw=w), dict(gb=x), dict(gb=gx),
                 dict(ws=ws + 4)):
         assert backward(**bad) == EINVAL, bad
-    assert backward(ws=None) == EWS and backward(wsb=8) == EWS
+    many = dict(rows=65, xt=1, yt=1)   # more rows than one workgroup takes
+    assert backward(**many, ws=None) == EWS and backward(**many, wsb=8) == EWS
     assert L.acdc_norm_workspace_size(4, 10) > 0 and L.acdc_norm_workspace_size(-1, 10) == 0 and L.acdc_norm_workspace_size(4, 0) == 0
 
 
@@ -214,7 +215,7 @@ def test_binding_of_the_vocabulary_losses(host):
                dict(saved=neg(saved)), dict(g=f[:-1]), dict(g=f[:1].expand(R)), dict(g=f.double()), dict(g=neg(f)), dict(scale=f)):
         with pytest.raises(ValueError):
             back(**kw)
-    for kw in (dict(weights=f[:-1]), dict(weights=f.double()), dict(weights=f[:1].expand(R)), dict(weights=neg(f))):
+    for kw in (dict(grad_scale=NAN), dict(grad_scale=INF), dict(weights=f[:-1]), dict(weights=f.double()), dict(weights=f[:1].expand(R)), dict(weights=neg(f))):
         with pytest.raises(ValueError):
             loss(**kw)
     big = torch.zeros(1, (1 << 17) + 1)
@@ -267,7 +268,7 @@ def test_binding_of_the_layers(host):
             (norm_back, dict(g=place.bfloat16(), out=place[:-1])), (norm_back, dict(grads=(u,))), (norm_back, dict(grads=(u[:-1], None))),
             (norm_back, dict(grads=(torch.zeros(N), torch.zeros(N).bfloat16()))), (norm_back, dict(accumulate=True)),
             (norm_back, dict(grads=(u, None))), (norm_back, dict(dtype=torch.float64)),
-            (norm_back, dict(workspace=torch.zeros(4, dtype=torch.uint8))), (embed, dict(t=t.float())), (embed, dict(t=t.view(2, 3))),
+            (norm_back, dict(workspace=torch.zeros(4, dtype=torch.uint8))), (embed, dict(scale=NAN)), (embed_back, dict(scale=INF)), (embed, dict(t=t.float())), (embed, dict(t=t.view(2, 3))),
             (embed, dict(t=torch.zeros(2 * R, dtype=torch.int64)[::2])), (embed, dict(t=t.to("meta"))), (embed, dict(w=w[:0])),
             (embed, dict(w=w.half())), (embed, dict(w=w[0])), (embed, dict(w=neg(w))), (embed, dict(out=wide)), (embed, dict(out=w[:R])),
             (embed, dict(dtype=torch.int32)), (embed_back, dict(t=t[:-1])), (embed_back, dict(classes=0)), (embed_back, dict(classes=-3)),
