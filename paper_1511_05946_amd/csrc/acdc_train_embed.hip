@@ -323,7 +323,7 @@ __global__ __launch_bounds__(kThreads) void k_sort_move(const void* __restrict__
 
 // --------------------------------------------------------------- the gradient
 
-constexpr int kPiece = 64, kShort = 16;  // sorted rows that are summed together
+constexpr int kPiece = 64, kShort = 16;  // sorted rows that are summed together, at the most and at the least
 
 struct SumArgs {
   const int* key;
@@ -470,8 +470,12 @@ int done() {
 }
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
 int blocks_of(int32_t width) { return int((int64_t(width) + kSpan - 1) / kSpan); }
-// Short pieces where long ones would leave most of the card idle.
-int piece_of(int64_t rows, int32_t width) { return rows / kPiece * blocks_of(width) < 2048 ? kShort : kPiece; }
+// Shorter pieces where long ones would leave most of the card idle.
+int piece_of(int64_t rows, int32_t width) {
+  int piece = kPiece;
+  while (piece > kShort && rows / piece * blocks_of(width) < 4096) piece /= 2;
+  return piece;
+}
 struct Layout {
   size_t key[2], row[2], counts, totals, there, partial, bytes;
 };

@@ -138,9 +138,10 @@ struct Across {
   unsigned ld2;
   int rows, tid;
   // A transposing read takes 16 values of the rows k .. k + 3 and k + 8 .. k + 11 at once
-  // per half wave: eight times 32 bytes, at eight different places of 256 bytes.
+  // per half wave: eight times 32 bytes, at eight different places of 256 bytes (of which
+  // rows of 64 values fill half, so that k's lowest bit already tells two of them apart).
   __device__ __forceinline__ static int swizzle(int k) {
-    return (((k & 3) | (k >> 3 & 1) << 2) << 1) & (CHUNKS - 1);
+    return CHUNKS == 8 ? ((k >> 1 & 1) | (k >> 3 & 1) << 1) << 1 : ((k & 3) | (k >> 3 & 1) << 2) << 1;
   }
   __device__ __forceinline__ void init(const Operand& o, int x0, int t) {
     base = reinterpret_cast<const char*>(o.p + x0);
@@ -195,20 +196,21 @@ struct Across {
 };
 
 // What one workgroup computes: tile (tm, tn) of mt x nt, part `part` of the steps.
-// The tiles of one XCD (workgroups go round the eight of them) lie together, in groups
-// of 4 n-tiles that run along m, so that its L2 holds what they share: 32 CUs of an XCD
-// ask for 12 different tiles a step (65536 x 7424 x 4096: 1.22 PFLOP/s; groups of 2 1.13,
-// of 8 1.20, of 16 1.13).
+// What one XCD computes (workgroups go round the eight of them) lies together: a part, whose
+// tiles read the same steps of both operands (2048 rows of G over 32768 classes times a weight
+// of 1024, 32 tiles in 8 parts: 250 MB from HBM, for 740 with an eighth of the tiles of every
+// part), and of a part groups of 4 n-tiles that run along m: 32 CUs ask for 12 different tiles a
+// step (65536 x 7424 x 4096: 1.22 PFLOP/s; groups of 2 1.13, of 8 1.20, of 16 1.13).
 struct Place {
   int tm, tn, part;
 };
-__device__ __forceinline__ Place place_of(unsigned id, int mt, int nt) {
-  const unsigned tiles = unsigned(mt) * unsigned(nt);
+__device__ __forceinline__ Place place_of(unsigned id, int mt, int nt, int parts) {
+  const unsigned tiles = unsigned(mt) * unsigned(nt), all = tiles * unsigned(parts);
+  const unsigned per = all / 8, rest = all % 8, xcd = id % 8;
+  id = xcd * per + min(xcd, rest) + id / 8;
   Place p;
   p.part = int(id / tiles);
   id %= tiles;
-  const unsigned per = tiles / 8, rest = tiles % 8, xcd = id % 8;
-  id = xcd * per + min(xcd, rest) + id / 8;
   constexpr unsigned GROUP = 4;
   const unsigned g = id / (GROUP * mt), first = g * GROUP, wide = min(GROUP, nt - first);
   const unsigned in = id - g * GROUP * mt;
@@ -261,7 +263,7 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int d
   static_assert(STAGES * STAGE <= 160 * 1024);
   __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];  // (the epilogue exchanges values there too)
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
-  const Place at = place_of(blockIdx.x, mt, nt);
+  const Place at = place_of(blockIdx.x, mt, nt, parts);
   if constexpr (COUNT == Count::kN) {
     if (at.tn * BN >= *count) return;
   }
