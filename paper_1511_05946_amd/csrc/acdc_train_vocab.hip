@@ -615,7 +615,7 @@ struct JoinOut {
 // stats = (loss, W) from the sum of weight times logp
 __device__ __forceinline__ void put_stats(float* stats, const Rows& rows, double sum, bool mean) {
   const double total = *rows.total;
-  stats[0] = *rows.count == 0 ? 0.f : float(mean ? -sum / total : -sum);
+  stats[0] = *rows.count == 0 || (mean && total == 0.0) ? 0.f : float(mean ? -sum / total : -sum);
   stats[1] = float(total);
 }
 __global__ __launch_bounds__(1024) void k_vocab_join(Rows rows, const float2* __restrict__ parts, const float* __restrict__ logit,
@@ -659,7 +659,10 @@ __global__ __launch_bounds__(1024) void k_vocab_join(Rows rows, const float2* __
     if (out.saved != nullptr) out.saved[r] = make_float2(top, sum);
     const float w = rows.share[i];
     loss = w * logp;
-    if (out.row_grads != nullptr) out.row_grads[r] = -(out.mean ? float(double(w) / *rows.total) : w);
+    if (out.row_grads != nullptr) {
+      const double total = out.mean ? *rows.total : 1.0;
+      out.row_grads[r] = total == 0.0 ? 0.f : -float(double(w) / total);
+    }
     if (out.slope != nullptr) {
       const float g = t >= 0 ? -w : __builtin_nanf("");
       out.slope[i] = RowSlope{top, g / sum, g, t};

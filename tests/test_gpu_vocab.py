@@ -162,6 +162,24 @@ def test_no_row_takes_part(env):
     assert gh.shape == (0, 24) and (gw == 0).all()
 
 
+@pytest.mark.parametrize("rows", [2, 64, 300])
+def test_weights_that_cancel(env, rows):
+    """The mean over weights whose sum is 0: a loss and gradients of 0."""
+    torch, losses = env
+    h, w = torch.randn(rows, 24, device="cuda"), torch.randn(50, 24, device="cuda")
+    t = torch.arange(rows, device="cuda") % 50
+    weights = torch.ones(rows, device="cuda")
+    weights[1::2] = -1
+    r = losses.vocab_loss(h, w, t, weights=weights, save=True)
+    assert r.stats.tolist() == [0, 0] and all((x == 0).all() for x in (r.grad_hidden, r.grad_weight, r.row_grads))
+    assert (r.logp < 0).all()
+    want = -(weights.double() * r.logp.double()).sum().item()
+    r = losses.vocab_loss(h, w, t, weights=weights, mean=False, save=True)
+    # one rounding of each product and one of the sum
+    assert abs(r.stats[0].item() - want) <= 2 ** -24 * (r.logp.abs().double().sum().item() + abs(want)) and r.stats[1].item() == 0
+    assert torch.equal(r.row_grads, -weights) and (r.grad_weight != 0).any()
+
+
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_what_is_not_a_number(env, dtype):
     """A target past the classes and hidden values that are not finite give NaN for their
