@@ -13,7 +13,9 @@
 
 #include <ATen/ATen.h>
 #include <ATen/EmptyTensor.h>
+#include <torch/csrc/autograd/function.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/autograd/variable.h>
 
 #include <vector>
 
@@ -774,10 +776,28 @@ PyObject* embedding_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// (tensors...) -> whether a node that computes one of them, or sums up its gradient, was
+// made on the default stream
+PyObject* made_on_default_stream(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(n, n, [&]() -> PyObject* {
+    Args a{args};
+    for (Py_ssize_t i = 0; i < n; ++i) {
+      const Tensor* t = a.may(int(i));
+      if (t == nullptr || !t->requires_grad()) continue;
+      const auto node = t->grad_fn() ? t->grad_fn() : torch::autograd::impl::try_get_grad_accumulator(*t);
+      if (!node) continue;
+      const auto stream = node->stream();
+      if (stream && stream->id() == 0) Py_RETURN_TRUE;
+    }
+    Py_RETURN_FALSE;
+  });
+}
+
 #define ENTRY(name) {#name, (PyCFunction)(void*)name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(logprobs), ENTRY(logprobs_backward), ENTRY(policy),     ENTRY(preference),
                          ENTRY(adamw),    ENTRY(grad_norm),         ENTRY(vocab_logprobs), ENTRY(vocab_backward),
                          ENTRY(vocab_loss), ENTRY(norm), ENTRY(norm_backward), ENTRY(embedding), ENTRY(embedding_backward),
+                         ENTRY(made_on_default_stream),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_train_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -28,7 +28,7 @@ import torch
 
 from ._lib import lib
 from .acdc import _call, _check, _once, _ptr, _wrote
-from .losses import _DTYPES, _aligned_workspace, _apart, _index, _matrix, _native, _values, _workspace
+from .losses import _DTYPES, _aligned_workspace, _apart, _capturable, _index, _matrix, _native, _values, _workspace
 
 
 class LayerNorm(NamedTuple):
@@ -274,9 +274,11 @@ class _Embedding(torch.autograd.Function):
 
 def layer_norm_autograd(x, weight=None, bias=None, eps: float = 1e-5, dtype=None):
     """``layer_norm(...).y``, differentiable in x, weight and bias."""
+    _capturable("layer_norm_autograd", x, weight, bias)
     return _LayerNorm.apply(x, weight, bias, eps, dtype)
 
 
 def embedding_autograd(tokens, weight, scale: float = 1.0, dtype=None):
     """``embedding(...)``, differentiable in the weight."""
+    _capturable("embedding_autograd", weight)
     return _Embedding.apply(tokens, weight, scale, dtype)

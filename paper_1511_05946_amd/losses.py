@@ -556,6 +556,16 @@ class _Loss(torch.autograd.Function):
         return _once(ctx.call, grad, logits, grad_loss), None, None, None, None
 
 
+def _capturable(call, *inputs):
+    """Refuses to take into a captured graph what was made outside of it on the default
+    stream: its backward pass would make that stream wait for the captured one, which
+    ends the process.  A leaf is made there with the first operation on it, and stays
+    while any result of one lives."""
+    if inputs[0].is_cuda and torch.cuda.is_current_stream_capturing() and binding().made_on_default_stream(*inputs):
+        raise RuntimeError(f"{call} is captured while results of its inputs that were computed on the default stream are "
+                           "alive: drop them (and their losses) before the capture, or compute them on another stream")
+
+
 class _VocabLogprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, hidden, weight, targets):
@@ -597,12 +607,14 @@ class _VocabLoss(torch.autograd.Function):
 
 def vocab_logprobs_autograd(hidden, weight, targets):
     """``vocab_logprobs(...).logp``, differentiable in hidden and weight."""
+    _capturable("vocab_logprobs_autograd", hidden, weight)
     return _VocabLogprobs.apply(hidden, weight, targets)
 
 
 def vocab_loss_autograd(hidden, weight, targets, weights=None, mean: bool = True, grad_scale: float = 1.0):
     """(loss, stats, logp) of ``vocab_loss``; the loss is differentiable in hidden
     and weight, and ``grad_scale`` multiplies their gradients as it does there."""
+    _capturable("vocab_loss_autograd", hidden, weight)
     return _VocabLoss.apply(hidden, weight, targets, weights, mean, grad_scale)
 
 

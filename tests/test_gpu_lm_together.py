@@ -147,6 +147,56 @@ def test_step_in_a_graph(env, head):
         assert junk == junk
 
 
+def test_backward_in_a_graph(env):
+    """Differentiable forms captured, forward and backward, replayed with new inputs; refused
+    while a result of the same leaves lives that was computed on the default stream."""
+    torch, _, layers, losses, _ = env
+    N, V, T = 48, 200, 70
+    W, g, b = (x.requires_grad_(True) for x in (torch.randn(V, N, device="cuda"), torch.ones(N, device="cuda"), torch.zeros(N, device="cuda")))
+    tokens, targets = batch(torch, T, V)
+    leaves = (W, g, b)
+
+    def run():
+        h = layers.layer_norm_autograd(layers.embedding_autograd(tokens, W), g, b)
+        loss, _, logp = losses.vocab_loss_autograd(h, W, targets)
+        return loss.detach(), torch.autograd.grad(loss + losses.vocab_logprobs_autograd(h, W, targets).sum(), leaves)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for k in range(3):
+        if k == 1:
+            tokens.copy_(tokens.flip(0))
+            targets.copy_(targets.roll(3))
+        graph.replay()
+        want = run()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and all(torch.equal(x, y) for x, y in zip(got[1], want[1])), k
+    x, h = torch.randn(T, N, device="cuda"), torch.randn(T, N, device="cuda", requires_grad=True)
+    calls = {"embedding_autograd": (W, lambda: layers.embedding_autograd(tokens, W)),
+             "layer_norm_autograd": (b, lambda: layers.layer_norm_autograd(x, g, b)),
+             "vocab_loss_autograd": (W, lambda: losses.vocab_loss_autograd(h, W, targets)),
+             "vocab_logprobs_autograd": (h, lambda: losses.vocab_logprobs_autograd(h, W, targets))}
+    for name, (leaf, call) in calls.items():
+        for made in (lambda: leaf * 2, call):   # its results' leaf, and the call's own
+            alive = made()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                x + 1
+                with pytest.raises(RuntimeError, match=name):
+                    call()
+            del alive
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+
+
 def test_calls_at_the_same_time(env):
     """Two streams, each with tensors and workspaces of its own."""
     torch, _, layers, losses, _ = env
