@@ -26,9 +26,10 @@ extern "C" {
  * once more.  Per row with M = max_v x_rv, S = sum_v exp(x_rv - M):
  *   logp = x_rt - M - log S
  * bfloat16 values are multiplied exactly and summed in 32 bits; float32
- * values in products as exact as 32-bit ones.  dL/dx is rounded to the type
- * of the inputs before the products that give the two gradients (float32:
- * not rounded).
+ * values in products as exact as 32-bit ones.  Before the products that give
+ * the two gradients dL/dx is rounded, for float32 inputs to 24 bits, for
+ * bfloat16 ones to 8 (acdc_vocab_loss may round the exponentials in it to 8
+ * bits as well) or, where the products are small, to 16.
  *
  * hidden: rows x width, weight: classes x width, both of type `dtype`, rows
  * hidden_stride and weight_stride apart (in elements, >= width).  targets as in
@@ -36,7 +37,10 @@ extern "C" {
  * values may hold anything; its outputs and gradient are 0), one >= classes
  * makes its row NaN, and with it the weight's gradient.  hidden and weight
  * are finite; a row of hidden that is not gives NaN for itself and for the
- * weight's gradient.  1 <= width <= 2^17, classes <= 2^27, rows <= 2^24. */
+ * weight's gradient.  1 <= width <= 2^17, 1 <= classes <= 2^27, rows <= 2^24.
+ * bfloat16 weights are read where they lie if they begin at 16 bytes and width
+ * and weight_stride are multiples of 8, weight_stride below 2^22; any other
+ * weight is copied into the workspace, piece by piece. */
 typedef struct acdc_vocab_head {
   const void* hidden;
   const void* weight;
@@ -93,7 +97,8 @@ size_t acdc_vocab_workspace_size(int64_t rows, int32_t width, int32_t classes, i
  *   rstd = 1 / sqrt(variance + eps),  y = (x - mean) rstd weight + bias
  * x: rows x width of x_type, y of y_type, rows x_stride and y_stride apart.
  * weight and bias: width values of vector_type (either may be null: 1 and 0).
- * saved [rows][2] = (mean, rstd), 8-byte aligned (optional). */
+ * saved [rows][2] = (mean, rstd), 8-byte aligned (optional).  1 <= width <=
+ * 2^24, rows < 2^30. */
 int acdc_norm_forward(const void* x, int32_t x_type, int64_t x_stride, const void* weight, const void* bias,
                       int32_t vector_type, float eps, void* y, int32_t y_type, int64_t y_stride, float* saved, int64_t rows,
                       int32_t width, acdc_stream_t stream);
@@ -105,8 +110,8 @@ int acdc_norm_forward(const void* x, int32_t x_type, int64_t x_stride, const voi
  * grads_type; each may be null (not wanted), and with accumulate != 0 the two
  * sums are added to what is there.  grad_x may be grad_y's own memory (same
  * type, pointer and stride).  The sums run in 32 bits over 1024 parts of the
- * rows at the most and then over the parts.  A
- * workspace of 256 bytes stands for none: it may be null. */
+ * rows at the most and then over the parts.  A workspace size of 256 stands for
+ * none: the workspace may be null. */
 int acdc_norm_backward(const void* x, int32_t x_type, int64_t x_stride, const void* grad_y, int32_t y_type,
                        int64_t grad_y_stride, const void* weight, int32_t vector_type, const float* saved, void* grad_x,
                        int64_t grad_x_stride, void* grad_weight, void* grad_bias, int32_t grads_type, int32_t accumulate,
@@ -117,14 +122,16 @@ size_t acdc_norm_workspace_size(int64_t rows, int32_t width);
  *
  * out[r] = scale * weight[tokens[r]]: weight classes x width of weight_type,
  * out rows x width of out_type, rows weight_stride and out_stride apart.
- * A negative token gives a row of zeros, one >= classes a row of NaN. */
+ * A negative token gives a row of zeros, one >= classes a row of NaN.
+ * 1 <= width <= 2^20, 1 <= classes <= 2^30, rows <= 2^28 - 64, and
+ * (rows / 64 + 1) (width / 512 + 1) <= 2^22, here and below. */
 int acdc_embedding_forward(const void* tokens, int32_t token_bits, const void* weight, int32_t weight_type,
                            int64_t weight_stride, float scale, void* out, int32_t out_type, int64_t out_stride, int64_t rows,
                            int32_t width, int32_t classes, acdc_stream_t stream);
 
 /* grad_weight[v] = scale * sum of grad_out[r] over the rows r with token v, in
- * the order of the rows (in pieces of 64 for long sums), 0 for a class without
- * rows; with accumulate != 0 added to what is there.  Rows whose token is
+ * the order of the rows (long sums in pieces of 16 to 64 sorted rows, by the
+ * sizes alone), 0 for a class without rows; with accumulate != 0 added to what is there.  Rows whose token is
  * negative or >= classes take no part and are not read. */
 int acdc_embedding_backward(const void* tokens, int32_t token_bits, const void* grad_out, int32_t out_type,
                             int64_t out_stride, float scale, void* grad_weight, int32_t weight_type, int64_t weight_stride,
