@@ -215,11 +215,11 @@ __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const void* __rest
 
 // More rows, in tiles: counts[tile][digit], their sums over the tiles before, and each pair
 // to its place, a pass in three launches.
-constexpr int kEach = 8, kTile = kThreads * kEach, kPerThread = kDigits / kThreads;
+constexpr int kPerThread = kDigits / kThreads;
 
 // The tokens that are there are marked in `there` or, where that is null, the workgroups past
 // the tiles (if there are any) write zeros over the gradient.
-template <class TW>
+template <class TW, int EACH>
 __global__ __launch_bounds__(kThreads) void k_sort_count(const void* __restrict__ tokens, int bits, int classes, Sorted in, int n,
                                                          int shift, int mask, int* __restrict__ counts,
                                                          unsigned char* __restrict__ there, int tiles,
@@ -233,8 +233,8 @@ __global__ __launch_bounds__(kThreads) void k_sort_count(const void* __restrict_
   for (int d = 0; d < kPerThread; ++d) bins[d * kThreads + threadIdx.x] = 0;
   __syncthreads();
 #pragma unroll
-  for (int q = 0; q < kEach; ++q) {
-    const int i = blockIdx.x * kTile + q * kThreads + threadIdx.x;
+  for (int q = 0; q < EACH; ++q) {
+    const int i = (blockIdx.x * EACH + q) * kThreads + threadIdx.x;
     if (i < n) {
       // in the first pass the keys come from the tokens, and are marked as there
       const int k = tokens != nullptr ? key_of(tokens, bits, i, classes) : in.key[i];
@@ -277,17 +277,18 @@ __global__ __launch_bounds__(64 * kSumWaves) void k_sort_sums(int* __restrict__ 
 
 // A pair comes after those of lower digits, of earlier tiles, of earlier waves, of earlier
 // rounds and of lower lanes with the same digit.
+template <int EACH>
 __global__ __launch_bounds__(kThreads) void k_sort_move(const void* __restrict__ tokens, int bits, int classes, Sorted in,
                                                         Sorted out, int n, int shift, int digit_bits,
                                                         const int* __restrict__ counts, const int* __restrict__ totals) {
   __shared__ int next[kWaves][kDigits], slots[kWaves];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, mask = (1 << digit_bits) - 1;
-  const int base = blockIdx.x * kTile + wave * (64 * kEach);
+  const int base = (blockIdx.x * kThreads + wave * 64) * EACH;
   for (int i = threadIdx.x; i < kWaves * kDigits; i += kThreads) next[i / kDigits][i % kDigits] = 0;
   __syncthreads();
-  int key[kEach], row[kEach];
+  int key[EACH], row[EACH];
 #pragma unroll
-  for (int q = 0; q < kEach; ++q) {
+  for (int q = 0; q < EACH; ++q) {
     const int i = base + q * 64 + lane;
     key[q] = row[q] = 0;
     if (i < n) {
@@ -311,7 +312,7 @@ __global__ __launch_bounds__(kThreads) void k_sort_move(const void* __restrict__
   }
   __syncthreads();
 #pragma unroll
-  for (int q = 0; q < kEach; ++q) {
+  for (int q = 0; q < EACH; ++q) {
     const bool here = base + q * 64 + lane < n;
     const int to = place_of(next[wave], here, (key[q] >> shift) & mask, digit_bits);
     if (here) {
@@ -395,53 +396,81 @@ __global__ __launch_bounds__(kThreads) void k_embed_sums(SumArgs a, const typena
   else put_class<TW>(weight + current * a.weight_stride, at, s, a.scale, a.add);
 }
 
-// The class that begins in a piece and goes on behind it: its partial sums together, by
-// the waves of a workgroup that each take some that follow one another.
-constexpr int kJoinWaves = 8;
+// The class that begins in a piece and goes on behind it: its partial sums together.  A
+// wave does that for its piece; more than kAlone of them are shared by the waves of the
+// workgroup, which each take some that follow one another.
+constexpr int kJoinWaves = 8, kAlone = 8;
 template <class TW>
 __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(SumArgs a, typename TW::Elem* __restrict__ weight) {
   __shared__ float slots[kJoinWaves][kEight][64];
+  __shared__ int shared[kJoinWaves];  // pieces that a wave's class goes on for, where that is shared
   const int lane = threadIdx.x % 64, wave = uniform(int(threadIdx.x / 64));
-  const int piece = int(blockIdx.x / unsigned(a.blocks));
+  const int first_piece = int(blockIdx.x / unsigned(a.blocks)) * kJoinWaves;
   const Columns<true> at(int(blockIdx.x % unsigned(a.blocks)) * kSpan, lane, a.width);
-  const int from = piece * a.piece, to = from + a.piece;
-  if (to >= a.rows) return;
-  const int key = a.key[to];
-  if (key >= a.classes || a.key[to - 1] != key) return;                  // nothing goes on
-  if (a.key[from] == key && from > 0 && a.key[from - 1] == key) return;  // it began before
-  // pieces that begin with it
-  int many = 0;
-  for (;;) {
-    const long long p = (long long)piece + 1 + many + lane;
-    const unsigned long long same = __ballot(p < a.pieces && a.key[min(p, (long long)a.pieces - 1) * a.piece] == key);
-    if (~same == 0ull) {
-      many += 64;
-      continue;
-    }
-    many += __ffsll((long long)~same) - 1;
-    break;
-  }
-  float s[kEight] = {};
-  const int per = (many + kJoinWaves - 1) / kJoinWaves, first = min(many, wave * per), last = min(many, first + per);
-  if (at.any()) {
-    if (wave == 0) at.template load<F32>(a.partial + ((long long)piece * 2 + 1) * a.width, s);
-#pragma unroll 4
-    for (int p = first; p < last; ++p) {
-      float v[kEight];
-      at.template load<F32>(a.partial + (long long)(piece + 1 + p) * 2 * a.width, v);
+  // the class that begins in a piece and the pieces behind it that begin with it: 0, none
+  auto goes_on = [&](int piece) {
+    const long long from = (long long)piece * a.piece, to = from + a.piece;
+    if (to >= a.rows) return 0;
+    const int key = a.key[to];
+    if (key >= a.classes || a.key[to - 1] != key) return 0;                  // nothing goes on
+    if (a.key[from] == key && from > 0 && a.key[from - 1] == key) return 0;  // it began before
+    // (those that do follow one another: of 64 at `step` from each other the first ones)
+    auto count = [&](int first, int step) {
+      const long long p = (long long)piece + first + (long long)(lane + 1) * step;
+      const unsigned long long same = __ballot(p < a.pieces && a.key[min(p, (long long)a.pieces - 1) * a.piece] == key);
+      return ~same == 0ull ? 64 : __ffsll((long long)~same) - 1;
+    };
+    int many = count(0, 1);
+    if (many < 64) return many;
+    for (int more = 64; more == 64; many += more * 64) more = count(many, 64);
+    return many + count(many, 1);
+  };
+  // partial sums first .. last - 1 of those behind `piece` on top of s
+  auto add = [&](int piece, int first, int last, float (&s)[kEight]) {
+    constexpr int AHEAD = 8;
+    for (int p = first; p < last; p += AHEAD) {
+      float v[AHEAD][kEight];
 #pragma unroll
-      for (int c = 0; c < kEight; ++c) s[c] += v[c];
-    }
-  }
+      for (int q = 0; q < AHEAD; ++q) at.template load<F32>(a.partial + (long long)(piece + 1 + min(p + q, last - 1)) * 2 * a.width, v[q]);
 #pragma unroll
-  for (int c = 0; c < kEight; ++c) slots[wave][c][lane] = s[c];
+      for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+        for (int c = 0; c < kEight; ++c) s[c] += p + q < last ? v[q][c] : 0.f;
+    }
+  };
+  auto begin = [&](int piece, float (&s)[kEight]) { at.template load<F32>(a.partial + ((long long)piece * 2 + 1) * a.width, s); };
+  auto put = [&](int piece, const float (&s)[kEight]) {
+    put_class<TW>(weight + a.key[(long long)(piece + 1) * a.piece] * a.weight_stride, at, s, a.scale, a.add);
+  };
+  const int mine = first_piece + wave, many = goes_on(mine);
+  if (lane == 0) shared[wave] = many > kAlone ? many : 0;
+  if (many > 0 && many <= kAlone && at.any()) {
+    float s[kEight];
+    begin(mine, s);
+    add(mine, 0, many, s);
+    put(mine, s);
+  }
   __syncthreads();
-  if (wave != 0 || !at.any()) return;
+  for (int w = 0; w < kJoinWaves; ++w) {
+    const int all = shared[w], piece = first_piece + w;
+    if (all == 0) continue;
+    float s[kEight] = {};
+    const int per = (all + kJoinWaves - 1) / kJoinWaves, first = min(all, wave * per);
+    if (at.any()) {
+      if (wave == 0) begin(piece, s);
+      add(piece, first, min(all, first + per), s);
+    }
+    __syncthreads();  // the slots of the class before have been read
 #pragma unroll
-  for (int w = 1; w < kJoinWaves; ++w)
+    for (int c = 0; c < kEight; ++c) slots[wave][c][lane] = s[c];
+    __syncthreads();
+    if (wave != 0 || !at.any()) continue;
 #pragma unroll
-    for (int c = 0; c < kEight; ++c) s[c] += slots[w][c][lane];
-  put_class<TW>(weight + key * a.weight_stride, at, s, a.scale, a.add);
+    for (int k = 1; k < kJoinWaves; ++k)
+#pragma unroll
+      for (int c = 0; c < kEight; ++c) s[c] += slots[k][c][lane];
+    put(piece, s);
+  }
 }
 
 __global__ __launch_bounds__(kThreads) void k_embed_clear(unsigned char* there, int classes) {
@@ -476,6 +505,8 @@ int piece_of(int64_t rows, int32_t width) {
   while (piece > kShort && rows / piece * blocks_of(width) < 4096) piece /= 2;
   return piece;
 }
+// Pairs of a thread in a tile of the sort: fewer where that gives more CUs a tile.
+int each_of(int64_t rows) { return rows >= 256 * kThreads * 8 ? 8 : 2; }
 struct Layout {
   size_t key[2], row[2], counts, totals, there, partial, bytes;
 };
@@ -492,7 +523,8 @@ Layout layout(int64_t rows, int32_t width, int32_t classes) {
     w.key[k] = take(n * 4);
     w.row[k] = take(n * 4);
   }
-  w.counts = take((n + kTile - 1) / kTile * kDigits * 4);
+  const size_t tile = size_t(kThreads) * each_of(rows);
+  w.counts = take((n + tile - 1) / tile * kDigits * 4);
   w.totals = take(kDigits * 4);
   w.there = take(size_t(classes));
   w.partial = take((n + piece_of(rows, width) - 1) / piece_of(rows, width) * 2 * size_t(width) * 4);
@@ -603,17 +635,17 @@ extern "C" int acdc_embedding_backward(const void* tokens, int32_t token_bits, c
     if (mark)
       hipLaunchKernelGGL(k_embed_clear, dim3(unsigned(std::min<int64_t>((classes + kThreads - 1) / kThreads, 1024))), dim3(kThreads), 0,
                          s, there, classes);
-    const int tiles = (n + kTile - 1) / kTile;
+    const int each = each_of(rows), tile = kThreads * each, tiles = (n + tile - 1) / tile;
     for (int pass = 0; pass < passes; ++pass, at ^= 1) {
       const void* from = pass == 0 ? tokens : nullptr;
       const int fill = pass == 0 && accumulate == 0 && !mark ? int(std::min<int64_t>((classes + kWaves - 1) / kWaves, 2048)) : 0;
       with_types(out_type, weight_type, [&]<class TG, class TW>() {
-        hipLaunchKernelGGL(k_sort_count<TW>, dim3(unsigned(tiles + fill)), dim3(kThreads), 0, s, from, token_bits, classes, pairs[at], n,
+        hipLaunchKernelGGL((each == 8 ? k_sort_count<TW, 8> : k_sort_count<TW, 2>), dim3(unsigned(tiles + fill)), dim3(kThreads), 0, s, from, token_bits, classes, pairs[at], n,
                            pass * digit_bits, (1 << digit_bits) - 1, counts, pass == 0 && mark ? there : nullptr, tiles,
                            static_cast<typename TW::Elem*>(grad_weight), (long long)weight_stride, width);
       });
       hipLaunchKernelGGL(k_sort_sums, dim3(kDigits / 64), dim3(64 * kSumWaves), 0, s, counts, tiles, totals);
-      hipLaunchKernelGGL(k_sort_move, dim3(unsigned(tiles)), dim3(kThreads), 0, s, from, token_bits, classes, pairs[at], pairs[at ^ 1],
+      hipLaunchKernelGGL((each == 8 ? k_sort_move<8> : k_sort_move<2>), dim3(unsigned(tiles)), dim3(kThreads), 0, s, from, token_bits, classes, pairs[at], pairs[at ^ 1],
                          n, pass * digit_bits, digit_bits, counts, totals);
     }
   }
@@ -629,7 +661,8 @@ extern "C" int acdc_embedding_backward(const void* tokens, int32_t token_bits, c
     const unsigned groups = unsigned((int64_t(pieces) * blocks + kWaves - 1) / kWaves);
     hipLaunchKernelGGL((k_embed_sums<TG, TW>), dim3(groups), dim3(kThreads), 0, s, a, static_cast<const typename TG::Elem*>(grad_out), out);
     if (pieces > 1)
-      hipLaunchKernelGGL(k_embed_join<TW>, dim3(unsigned(int64_t(pieces) * blocks)), dim3(64 * kJoinWaves), 0, s, a, out);
+      hipLaunchKernelGGL(k_embed_join<TW>, dim3(unsigned(int64_t((pieces + kJoinWaves - 1) / kJoinWaves) * blocks)),
+                         dim3(64 * kJoinWaves), 0, s, a, out);
   });
   return done();
 }

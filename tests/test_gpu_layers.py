@@ -247,9 +247,11 @@ def test_tokens_past_the_classes_and_none(env):
     assert (layers.embedding_backward(t[2:3], g[2:3], 10) == 0).all()   # no token takes part
 
 
-@pytest.mark.parametrize("n,first", [(64, 64), (128, 64), (129, 65), (200, 63), (640, 320)])
+@pytest.mark.parametrize("n,first", [(64, 64), (128, 64), (129, 65), (200, 63), (288, 144), (640, 320), (2100, 1041),
+                                     (140000, 70001), (600000, 590001)])
 def test_runs_at_the_pieces_borders(env, n, first):
-    """`first` rows of one class, then another: runs that end at, before and behind a multiple of 64."""
+    """`first` rows of one class, then another: runs that end at, before and behind a multiple of
+    64, and of 9 to 9000 pieces.  (Sums of whole numbers below 2^24: exact.)"""
     torch, layers = env
     print(f"[case] runs {n} {first}", flush=True)
     t = torch.tensor([2] * first + [5] * (n - first), device="cuda")
