@@ -140,8 +140,12 @@ struct Along {
 template <int X, int BK, int THREADS>
 struct Across {
   static constexpr int CHUNKS = X / 8, N = BK * CHUNKS / THREADS, BYTES = X * BK * 2;
+  // Chunk j of a thread's is j EVERY rows on; 16 rows on the permutation is the same, so
+  // that KEPT offsets are enough.
+  static constexpr int EVERY = THREADS / CHUNKS, KEPT = EVERY < 16 ? 16 / EVERY : 1;
+  static_assert(N % KEPT == 0);
   const char* base;
-  unsigned off[N];
+  unsigned off[KEPT];
   int64_t plane, step;
   unsigned ld2;
   int rows, tid;
@@ -159,8 +163,8 @@ struct Across {
     rows = o.rows;
     tid = t;
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int c = t + j * THREADS, k = c / CHUNKS, x = ((c % CHUNKS) ^ swizzle(k)) * 8;
+    for (int j = 0; j < KEPT; ++j) {
+      const int k = t / CHUNKS + j * EVERY, x = ((t % CHUNKS) ^ swizzle(k)) * 8;
       off[j] = unsigned(k) * ld2 + unsigned(min(x, o.cols - 8 - x0) * 2);
     }
   }
@@ -170,13 +174,13 @@ struct Across {
     const char* at = base + p * plane + k * step;
     if (FULL || (k + 1) * BK <= rows) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) Along<X, BK, THREADS, 0>::put(lds, at, off[j], j, wave);
+      for (int j = 0; j < N; ++j) Along<X, BK, THREADS, 0>::put(lds, at + int64_t(j / KEPT * KEPT * EVERY) * ld2, off[j % KEPT], j, wave);
     } else {
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const int row = (tid + j * THREADS) / CHUNKS;
+        const int row = tid / CHUNKS + j * EVERY;
         const int past = row - min(row, rows - 1 - k * BK);
-        Along<X, BK, THREADS, 0>::put(lds, at + off[j] - int64_t(past) * ld2, j, wave);
+        Along<X, BK, THREADS, 0>::put(lds, at + off[j % KEPT] + int64_t(j / KEPT * KEPT * EVERY - past) * ld2, j, wave);
       }
     }
   }
@@ -259,19 +263,42 @@ __device__ __forceinline__ void wait_loads() {
   __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
 }
 
-// `parts` workgroups share a tile's steps.  *count (may be null): the rows in use.
+// The parts of LDS, each an object of its own: only so does the compiler see that a transposing
+// read of one of them need not wait for the loads on their way into another.
+struct Stages {
+  char ACDC_LDS* at[4];
+};
+// STAGE bytes for each of STAGES of them.
+#define ACDC_STAGES(name, STAGE, STAGES)                                                     \
+  __shared__ __attribute__((aligned(1024))) char name##_0[STAGE], name##_1[STAGE],           \
+      name##_2[STAGES > 2 ? STAGE : 16], name##_3[STAGES > 3 ? STAGE : 16];                  \
+  const Stages name{{(char ACDC_LDS*)name##_0, (char ACDC_LDS*)name##_1, (char ACDC_LDS*)name##_2, \
+                     (char ACDC_LDS*)name##_3}}
+
+// A product and what follows it: mt x nt tiles, whose steps `parts` workgroups share each.
 template <class S, int PA, int PB, bool ACROSS_A, bool ACROSS_B, Count COUNT, class Epilogue>
-__global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int depth, int mt, int nt, int parts,
-                                                     const int* __restrict__ count, Epilogue epilogue) {
-  constexpr int T = S::THREADS, BM = S::BM, BN = S::BN, BK = S::BK, MI = S::MI, NI = S::NI, STAGES = S::STAGES;
+struct Product {
+  using Shape = S;
+  static constexpr int T = S::THREADS, BM = S::BM, BN = S::BN, BK = S::BK, MI = S::MI, NI = S::NI, STAGES = S::STAGES;
   using StageA = std::conditional_t<ACROSS_A, Across<BM, BK, T>, Along<BM, BK, T, 4 * MI>>;
   using StageB = std::conditional_t<ACROSS_B, Across<BN, BK, T>, Along<BN, BK, T, 0>>;
-  constexpr int STAGE = PA * StageA::BYTES + PB * StageB::BYTES, LOADS = PA * StageA::N + PB * StageB::N;
-  constexpr int MOST = PA > PB ? PA : PB;
+  static constexpr int STAGE = PA * StageA::BYTES + PB * StageB::BYTES, LOADS = PA * StageA::N + PB * StageB::N;
   static_assert(STAGES * STAGE <= 160 * 1024);
-  __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];  // (the epilogue exchanges values there too)
+  Operand A, B;
+  int depth, mt, nt, parts;
+  Epilogue epilogue;
+  unsigned groups() const { return unsigned(int64_t(mt) * nt * parts); }
+  __device__ __forceinline__ void run(unsigned id, const Stages& lds, const int* __restrict__ count) const;
+};
+
+// Workgroup `id` of the product's.  *count (may be null): the rows in use.
+template <class S, int PA, int PB, bool ACROSS_A, bool ACROSS_B, Count COUNT, class Epilogue>
+__device__ __forceinline__ void Product<S, PA, PB, ACROSS_A, ACROSS_B, COUNT, Epilogue>::run(unsigned id, const Stages& lds,
+                                                                                             const int* __restrict__ count) const {
+  constexpr int MOST = PA > PB ? PA : PB;
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
-  const Place at = place_of(blockIdx.x, mt, nt, parts);
+  const Place at = place_of(id, mt, nt, parts);
+  int depth = this->depth;
   if constexpr (COUNT == Count::kN) {
     if (at.tn * BN >= *count) return;
   }
@@ -283,9 +310,8 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int d
   StageB b;
   a.init(A, at.tm * BM, tid);
   b.init(B, at.tn * BN, tid);
-  char ACDC_LDS* const base = (char ACDC_LDS*)lds;
   auto fetch = [&]<bool FULL>(int slot, int k) {
-    char ACDC_LDS* stage = base + slot * STAGE;
+    char ACDC_LDS* stage = lds.at[slot];
 #pragma unroll
     for (int p = 0; p < PA; ++p) a.template load<FULL>(stage + p * StageA::BYTES, p, k, wave);
 #pragma unroll
@@ -302,7 +328,7 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int d
     bf16x8 a[PA][MI], b[PB][NI];
   };
   auto read = [&](int slot, int part, Part& f) {
-    const char ACDC_LDS* stage = base + slot * STAGE;
+    const char ACDC_LDS* stage = lds.at[slot];
 #pragma unroll
     for (int p = 0; p < PB; ++p)
 #pragma unroll
@@ -341,7 +367,7 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int d
 #pragma unroll
   for (int q = 0; q < STAGES - 1; ++q)
     if (from + q < to) fetch.template operator()<false>(q, from + q);
-  int slot = 0;
+  // (step s is in part (s - from) % STAGES of LDS, a constant wherever one is used)
   if constexpr (S::AHEAD && BK == 32) {
     // The registers of one step are read while the matrix cores work on the other's.
     static_assert(STAGES == 2 && PA == PB);
@@ -359,14 +385,14 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int d
       read(0, 0, even);
     }
     // step s is in `now`, and step s + 2 takes its place in LDS
-    auto step = [&]<bool FULL>(const Part& now, Part& then) {
+    auto step = [&]<bool FULL, int SLOT>(const Part& now, Part& then) {
       wait_loads<0>();
       meet();
-      read(slot ^ 1, 0, then);  // (nothing, after the last step)
+      read(SLOT ^ 1, 0, then);  // (nothing, after the last step)
       if constexpr (FULL) {
-        fetch.template operator()<true>(slot, s + 2);
+        fetch.template operator()<true>(SLOT, s + 2);
       } else {
-        if (s + 2 < to) fetch.template operator()<false>(slot, s + 2);
+        if (s + 2 < to) fetch.template operator()<false>(SLOT, s + 2);
       }
       multiply(now);
       if constexpr (FULL) {
@@ -378,18 +404,17 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int d
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      slot ^= 1;
       ++s;
     };
     // (the last step of all may end outside the operand)
     while (s + 4 < to) {
-      step.template operator()<true>(even, odd);
-      step.template operator()<true>(odd, even);
+      step.template operator()<true, 0>(even, odd);
+      step.template operator()<true, 1>(odd, even);
     }
 #pragma nounroll
     while (s < to) {
-      step.template operator()<false>(even, odd);
-      if (s < to) step.template operator()<false>(odd, even);
+      step.template operator()<false, 0>(even, odd);
+      if (s < to) step.template operator()<false, 1>(odd, even);
     }
   } else if constexpr (S::AHEAD) {
     // The registers of one part are read while the matrix cores work on the other's.
@@ -403,8 +428,8 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int d
       if (from + 1 < to) fetch.template operator()<false>(1, from + 1);
     }
     // (the last step of all may end outside the operand)
-    for (; s + 3 < to; ++s) {
-      read(slot, 1, second);
+    auto step = [&]<int SLOT>() {
+      read(SLOT, 1, second);
       multiply(first);
 #pragma unroll
       for (int i = 0; i < READS; ++i) {
@@ -414,8 +439,8 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int d
       __builtin_amdgcn_sched_barrier(0);
       wait_loads<0>();
       meet();
-      read(slot ^ 1, 0, first);
-      fetch.template operator()<true>(slot, s + 2);
+      read(SLOT ^ 1, 0, first);
+      fetch.template operator()<true>(SLOT, s + 2);
       multiply(second);
 #pragma unroll
       for (int i = 0; i < READS; ++i) {
@@ -424,34 +449,62 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(Operand A, Operand B, int d
         __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
-      slot ^= 1;
-    }
-#pragma nounroll
-    for (; s < to; ++s) {
-      read(slot, 1, second);
+      ++s;
+    };
+    auto last = [&]<int SLOT>() {
+      read(SLOT, 1, second);
       multiply(first);
       wait_loads<0>();
       meet();
-      read(slot ^ 1, 0, first);  // (nothing, after the last step)
-      if (s + 2 < to) fetch.template operator()<false>(slot, s + 2);
+      read(SLOT ^ 1, 0, first);  // (nothing, after the last step)
+      if (s + 2 < to) fetch.template operator()<false>(SLOT, s + 2);
       multiply(second);
-      slot ^= 1;
+      ++s;
+    };
+    while (s + 4 < to) {
+      step.template operator()<0>();
+      step.template operator()<1>();
+    }
+#pragma nounroll
+    while (s < to) {
+      last.template operator()<0>();
+      if (s < to) last.template operator()<1>();
     }
   } else {
-    for (int s = from; s < to; ++s) {
-      arrive(s);
-      if (s + STAGES - 1 < to) fetch.template operator()<false>(slot == 0 ? STAGES - 1 : slot - 1, s + STAGES - 1);
+    for (int s = from; s < to; s += STAGES) {
 #pragma unroll
-      for (int part = 0; part < BK / 32; ++part) {
-        Part f;
-        read(slot, part, f);
-        multiply(f);
+      for (int q = 0; q < STAGES; ++q) {
+        if (s + q >= to) break;
+        arrive(s + q);
+        if (s + q + STAGES - 1 < to) fetch.template operator()<false>((q + STAGES - 1) % STAGES, s + q + STAGES - 1);
+#pragma unroll
+        for (int part = 0; part < BK / 32; ++part) {
+          Part f;
+          read(q, part, f);
+          multiply(f);
+        }
       }
-      slot = slot == STAGES - 1 ? 0 : slot + 1;
     }
   }
   const Spot<MI, NI, !ACROSS_A> spot{at.tm * BM + wm * (BM / S::WM), at.tn * BN + wn * (BN / S::WN), lane};
-  epilogue.template operator()<S>(acc, spot, at, wave, reinterpret_cast<float2*>(lds));
+  epilogue.template operator()<S>(acc, spot, at, wave, (float2*)(char*)lds.at[0]);
+}
+
+// (the epilogue exchanges values in the LDS of the tiles)
+template <class P>
+__global__ __launch_bounds__(P::T) void k_gemm(P product, const int* __restrict__ count) {
+  ACDC_STAGES(lds, P::STAGE, P::STAGES);
+  product.run(blockIdx.x, lds, count);
+}
+
+// Two products in one launch, the second from workgroup `first` on (a multiple of 8: the
+// XCDs): its tiles fill the CUs that the first one's last round leaves idle.
+template <class P, class Q>
+__global__ __launch_bounds__(P::T) void k_gemm_both(P p, Q q, unsigned first, const int* __restrict__ count) {
+  static_assert(P::T == Q::T && P::STAGE == Q::STAGE && P::STAGES == Q::STAGES);
+  ACDC_STAGES(lds, P::STAGE, P::STAGES);
+  if (blockIdx.x >= first) q.run(blockIdx.x - first, lds, count);
+  else if (blockIdx.x < unsigned(p.mt * p.nt * p.parts)) p.run(blockIdx.x, lds, count);
 }
 
 }  // namespace acdc

@@ -879,26 +879,37 @@ struct Call {
   }
 
   template <class S, int PB, bool XA, bool XB, Count COUNT, class E>
-  void gemm(const Operand& a, const Operand& b, int64_t m, int64_t n, int depth, int parts, const E& e) const {
-    const int mt = int((m + S::BM - 1) / S::BM), nt = int((n + S::BN - 1) / S::BN);
-    hipLaunchKernelGGL((k_gemm<S, P, PB, XA, XB, COUNT, E>), dim3(unsigned(int64_t(mt) * nt * parts)), dim3(S::THREADS), 0, s, a, b,
-                       depth, mt, nt, parts, rows.count, e);
+  static Product<S, P, PB, XA, XB, COUNT, E> product(const Operand& a, const Operand& b, int64_t m, int64_t n, int depth, int parts,
+                                                     const E& e) {
+    return {a, b, depth, int((m + S::BM - 1) / S::BM), int((n + S::BN - 1) / S::BN), parts, e};
   }
-  // a product with n over the packed rows; b of PB planes
-  template <int PB, bool XA, class E>
-  void over_rows(bool large, const Operand& a, const Operand& b, int64_t m, int depth, int parts, const E& e) const {
+  template <class G>
+  void launch(const G& g) const {
+    hipLaunchKernelGGL(k_gemm<G>, dim3(g.groups()), dim3(G::T), 0, s, g, rows.count);
+  }
+  template <class G, class H>
+  void launch(const G& g, const H& h) const {
+    const unsigned first = unsigned(up(g.groups(), 8));
+    hipLaunchKernelGGL((k_gemm_both<G, H>), dim3(first + h.groups()), dim3(G::T), 0, s, g, h, first, rows.count);
+  }
+  // f(a product with n over the packed rows); b of PB planes
+  template <int PB, bool XA, class E, class F>
+  void over_rows(bool large, const Operand& a, const Operand& b, int64_t m, int depth, int parts, const E& e, F&& f) const {
     constexpr Count N = Count::kN;
     if (!large) {
-      gemm<std::conditional_t<P == 1, Small, Small3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
+      f(product<std::conditional_t<P == 1, Small, Small3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
     } else if constexpr (PB == P) {  // (two planes of G are for small tiles)
-      if (p.padded_rows > 64) gemm<std::conditional_t<P == 1, Large, std::conditional_t<XA, Wide3, Large3>>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
-      else gemm<std::conditional_t<P == 1, Flat, Flat3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e);
+      if (p.padded_rows > 64)
+        f(product<std::conditional_t<P == 1, Large, std::conditional_t<XA, Wide3, Large3>>, PB, XA, false, N>(a, b, m, p.padded_rows,
+                                                                                                              depth, parts, e));
+      else
+        f(product<std::conditional_t<P == 1, Flat, Flat3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
     }
   }
   // classes x packed rows
   template <class E>
   void logits(const Operand& weight, int parts, const E& e) const {
-    over_rows<P, false>(p.large_logits, weight, hidden(), weight.rows, p.padded_width, parts, e);
+    over_rows<P, false>(p.large_logits, weight, hidden(), weight.rows, p.padded_width, parts, e, [&](const auto& g) { launch(g); });
   }
   // the same as sums of parts, and what a wave for each 64 of a row's classes reads
   FewLogits few_logits(const Operand& weight, int k) const {
@@ -940,24 +951,25 @@ struct Call {
     hipLaunchKernelGGL(k_vocab_sum<O>, dim3(grid(n * ((p.width + 3) / 4))), dim3(256), 0, s, get<float>(at), parts,
                        (long long)part, p.padded_width, place, rows.factor, (long long)n, p.width, static_cast<E*>(out), (long long)ld, whole, add);
   }
-  template <int GP, class O>
-  void weight_grad(const acdc_vocab_grads& g, int k) const {
+  // f(the product for piece k of the weight's gradient), and what the piece needs after it
+  template <int GP, class O, class F>
+  void weight_grad(const acdc_vocab_grads& g, int k, F&& f) const {
     using E = typename O::Elem;
     const int n = classes_of(k);
     E* out = static_cast<E*>(g.weight) + int64_t(k) * p.piece * g.weight_stride;
     const bool whole = aligned_to(out, 4 * sizeof(E)) && g.weight_stride % 4 == 0, add = g.accumulate != 0;
-    auto product = [&](const auto& e) {
+    auto with = [&](const auto& e) {
       constexpr Count K = Count::kK;
       if (!p.large_weight)
-        gemm<std::conditional_t<P == 1, Small, Small3>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e);
+        f(product<std::conditional_t<P == 1, Small, Small3>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e));
       else if constexpr (GP == P)
-        gemm<std::conditional_t<P == 1, Large, Wide3>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e);
+        f(product<std::conditional_t<P == 1, Large, Wide3>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e));
     };
     if (p.weight_parts == 1) {
-      product(GradOut<O>{out, rows.factor, g.weight_stride, p.width, n, whole, add});
+      with(GradOut<O>{out, rows.factor, g.weight_stride, p.width, n, whole, add});
     } else {
       const int64_t part = int64_t(p.piece) * p.padded_width;
-      product(PartOut{get<float>(w.weight_sums), part, p.padded_width, n, false});
+      with(PartOut{get<float>(w.weight_sums), part, p.padded_width, n, false});
       sum<O>(w.weight_sums, p.weight_parts, part, nullptr, n, out, g.weight_stride, add);
     }
   }
@@ -990,6 +1002,18 @@ struct Call {
       return p.grad_planes == 1 ? gradients_of<1>(g, kept, packed) : gradients_of<2>(g, kept, packed);
     }
   }
+  // Both gradients' products: in one launch where their tiles are of one shape.
+  template <int GP, class G, class H>
+  void both(const G& dh, const H& dw) const {
+    // (one plane of G for bfloat16 inputs means large tiles in one of them at least, two in none)
+    constexpr bool IS_SMALL = std::is_same_v<typename G::Shape, Small>;
+    if constexpr (std::is_same_v<typename G::Shape, typename H::Shape> && !(GP == 1 && IS_SMALL)) {
+      launch(dh, dw);
+    } else {
+      launch(dh);
+      launch(dw);
+    }
+  }
   template <int GP>
   int gradients_of(const acdc_vocab_grads& g, const float* kept, int packed) const {
     const int64_t part = p.padded_rows * p.padded_width;
@@ -998,13 +1022,19 @@ struct Call {
       packed = k;
       if (kept != nullptr) slopes<GP>(kept);
       else slopes_again<GP>(wk, k);
-      if (g.hidden != nullptr)
-        over_rows<GP, true>(p.large_hidden, wk, grad(k), p.width, classes_of(k), p.hidden_parts,
-                            PartOut{get<float>(w.hidden_sums), part, p.padded_width, int(p.padded_rows), k > 0});
-      if (g.weight != nullptr) {
-        if (g.weight_type == head.dtype) weight_grad<GP, T>(g, k);
-        else weight_grad<GP, F32>(g, k);
+      auto weight_too = [&](auto&& f) {
+        if (g.weight_type == head.dtype) weight_grad<GP, T>(g, k, f);
+        else weight_grad<GP, F32>(g, k, f);
+      };
+      if (g.hidden == nullptr) {
+        weight_too([&](const auto& dw) { launch(dw); });
+        continue;
       }
+      over_rows<GP, true>(p.large_hidden, wk, grad(k), p.width, classes_of(k), p.hidden_parts,
+                          PartOut{get<float>(w.hidden_sums), part, p.padded_width, int(p.padded_rows), k > 0}, [&](const auto& dh) {
+                            if (g.weight == nullptr) return launch(dh);
+                            weight_too([&](const auto& dw) { both<GP>(dh, dw); });
+                          });
     }
     if (g.hidden != nullptr) sum<T>(w.hidden_sums, p.hidden_parts, part, rows.at, p.rows, g.hidden, g.hidden_stride, false);
     return done();
