@@ -71,17 +71,17 @@ struct Operand {
 
 // The tile of X values (m or n) by BK k of an operand with k along its rows: BK / 8 chunks
 // of 16 bytes a value.
-template <int X, int BK, int THREADS, int SPREAD>
+template <int X, int BK, int THREADS, bool DEALT>
 struct Along {
   static constexpr int CHUNKS = BK / 8, N = X * CHUNKS / THREADS, BYTES = X * BK * 2;
   const char* base;
   unsigned off[N];
   int64_t plane;
   int cols, tid;
-  // The rows that 8 lanes read at once are 0 .. 7 (SPREAD 0), or 0 .. 3 and four more
-  // SPREAD rows on; they are to touch eight different 16-byte columns of 128 bytes.
+  // The rows that 8 lanes read at once are 0 .. 7 or, dealt as in Spot, 0 .. 3 and 8 .. 11;
+  // they are to touch eight different 16-byte columns of 128 bytes.
   __device__ __forceinline__ static int swizzle(int row) {
-    const int far = SPREAD > 0 ? row / (SPREAD > 0 ? SPREAD : 1) & 1 : row >> 2 & 1;
+    const int far = DEALT ? row >> 3 & 1 : row >> 2 & 1;
     return CHUNKS == 8 ? (row & 3) | far << 2 : (row >> 1 & 1) | far << 1;
   }
   __device__ __forceinline__ void init(const Operand& o, int x0, int t) {
@@ -121,17 +121,17 @@ struct Along {
     __builtin_amdgcn_global_load_lds((const ACDC_GLOBAL void*)from, (ACDC_LDS void*)(lds + (j * THREADS + wave * 64) * 16),
                                      16, 0, 0);
   }
-  // Where lane's 8 k of a part (32 k) of a square begin, its rows dealt as in Spot: those of
-  // the other squares are a fixed number of bytes on.
+  // Where a lane's 8 k of a part (32 k) of the first square begin: those of the others are a
+  // fixed number of bytes on.
   struct Reader {
     unsigned at[BK / 32];
     __device__ __forceinline__ void init(int x, int lane) {
-      const int j = lane & 15, row = SPREAD > 0 ? x + (j >> 2) * SPREAD + (j & 3) : x + j;
+      const int j = lane & 15, row = DEALT ? x + (j >> 2) * 8 + (j & 3) : x + j;
 #pragma unroll
       for (int part = 0; part < BK / 32; ++part) at[part] = row * (BK * 2) + ((part * 4 + (lane >> 4)) ^ swizzle(row)) * 16;
     }
     __device__ __forceinline__ bf16x8 read(const char ACDC_LDS* tile, int square, int part) const {
-      return *(const bf16x8 ACDC_LDS*)(tile + at[part] + square * (SPREAD > 0 ? 4 : 16) * (BK * 2));
+      return *(const bf16x8 ACDC_LDS*)(tile + at[part] + (DEALT ? square / 2 * 32 + square % 2 * 4 : square * 16) * (BK * 2));
     }
   };
 };
@@ -174,13 +174,13 @@ struct Across {
     const char* at = base + p * plane + k * step;
     if (FULL || (k + 1) * BK <= rows) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) Along<X, BK, THREADS, 0>::put(lds, at + int64_t(j / KEPT * KEPT * EVERY) * ld2, off[j % KEPT], j, wave);
+      for (int j = 0; j < N; ++j) Along<X, BK, THREADS, false>::put(lds, at + int64_t(j / KEPT * KEPT * EVERY) * ld2, off[j % KEPT], j, wave);
     } else {
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const int row = tid / CHUNKS + j * EVERY;
         const int past = row - min(row, rows - 1 - k * BK);
-        Along<X, BK, THREADS, 0>::put(lds, at + off[j % KEPT] + int64_t(j / KEPT * KEPT * EVERY - past) * ld2, j, wave);
+        Along<X, BK, THREADS, false>::put(lds, at + off[j % KEPT] + int64_t(j / KEPT * KEPT * EVERY - past) * ld2, j, wave);
       }
     }
   }
@@ -232,13 +232,14 @@ __device__ __forceinline__ Place place_of(unsigned id, int mt, int nt, int parts
 }
 
 // Where a lane's results stand: of MI x NI squares of 16 x 16, acc[mi][ni][i] is
-// m = m(mi) + i, n = n(ni).  With A along, the rows of a wave's tile are dealt to the
-// squares so that a lane's 4 MI values of m follow one another.
-template <int MI, int NI, bool RUN>
+// m = m(mi) + i, n = n(ni).  With A along, the rows of a wave's tile are dealt to pairs of
+// squares so that a lane has eight values of m that follow one another, and four lanes 32
+// (64 bytes of bfloat16).
+template <int MI, int NI, bool DEALT>
 struct Spot {
   int m0, n0, lane;
   __device__ __forceinline__ int m(int mi) const {
-    return RUN ? m0 + (lane >> 4) * (4 * MI) + mi * 4 : m0 + mi * 16 + (lane >> 4) * 4;
+    return DEALT ? m0 + mi / 2 * 32 + (lane >> 4) * 8 + mi % 2 * 4 : m0 + mi * 16 + (lane >> 4) * 4;
   }
   __device__ __forceinline__ int n(int ni) const { return n0 + ni * 16 + (lane & 15); }
 };
@@ -280,8 +281,8 @@ template <class S, int PA, int PB, bool ACROSS_A, bool ACROSS_B, Count COUNT, cl
 struct Product {
   using Shape = S;
   static constexpr int T = S::THREADS, BM = S::BM, BN = S::BN, BK = S::BK, MI = S::MI, NI = S::NI, STAGES = S::STAGES;
-  using StageA = std::conditional_t<ACROSS_A, Across<BM, BK, T>, Along<BM, BK, T, 4 * MI>>;
-  using StageB = std::conditional_t<ACROSS_B, Across<BN, BK, T>, Along<BN, BK, T, 0>>;
+  using StageA = std::conditional_t<ACROSS_A, Across<BM, BK, T>, Along<BM, BK, T, true>>;
+  using StageB = std::conditional_t<ACROSS_B, Across<BN, BK, T>, Along<BN, BK, T, false>>;
   static constexpr int STAGE = PA * StageA::BYTES + PB * StageB::BYTES, LOADS = PA * StageA::N + PB * StageB::N;
   static_assert(STAGES * STAGE <= 160 * 1024);
   Operand A, B;

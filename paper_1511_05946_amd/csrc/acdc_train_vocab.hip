@@ -302,10 +302,10 @@ struct StatsOut {
     for (int n = 0; n < NI; ++n) {
       const int r = spot.n(n), t = target[r] - first - spot.m(0);
       if ((at.tm + 1) * S::BM > classes) mask(acc, spot, n);
-      if (unsigned(t) < 4u * MI) {
+      if (unsigned(t) < 16u * MI && t % 32 < 8) {
 #pragma unroll
         for (int v = 0; v < 4 * MI; ++v)
-          if (v == t) logit[r] = acc[v / 4][n][v % 4];
+          if (v == t / 32 * 8 + t % 32) logit[r] = acc[v / 4][n][v % 4];
       }
       float top = kNegMax;
 #pragma unroll
@@ -340,18 +340,18 @@ struct StatsOut {
       sum = p.a + p.b;
       p = swap32(sum);
       if (lane < 16) slots[(r - at.tn * BN) * WM + wave % WM] = make_float2(tops[n], p.a + p.b);
-      const long long to = (long long)r * ld + spot.m(0);
+      const long long to = (long long)r * ld;
       if constexpr (KEEP == Keep::kBf16) {
 #pragma unroll
         for (int m = 0; m < MI; m += 2) {
           bf16x8 o;
 #pragma unroll
           for (int i = 0; i < 8; ++i) o[i] = __bf16(acc[m + i / 4][n][i % 4]);
-          *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(kept) + to + m * 4) = o;
+          *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(kept) + to + spot.m(m)) = o;
         }
       } else if constexpr (KEEP == Keep::kF32) {
 #pragma unroll
-        for (int m = 0; m < MI; ++m) *reinterpret_cast<f32x4*>(static_cast<float*>(kept) + to + m * 4) = acc[m][n];
+        for (int m = 0; m < MI; ++m) *reinterpret_cast<f32x4*>(static_cast<float*>(kept) + to + spot.m(m)) = acc[m][n];
       }
     }
     __syncthreads();
@@ -407,7 +407,7 @@ struct SlopeOut {
       const int r = spot.n(n);
       const RowSlope k = row[r];
       const int t = k.target - first;
-      __bf16* to = out + (long long)r * ld + spot.m(0);
+      __bf16* to = out + (long long)r * ld;
 #pragma unroll
       for (int m = 0; m < MI; m += 2) {
         float y[8];
@@ -418,7 +418,7 @@ struct SlopeOut {
           if (v == t) y[i] += k.g;
           if (v >= classes) y[i] = 0.f;
         }
-        put_planes<PLANES, 8, bf16x8>(to + m * 4, plane, y);
+        put_planes<PLANES, 8, bf16x8>(to + spot.m(m), plane, y);
       }
     }
   }
@@ -450,8 +450,8 @@ __global__ __launch_bounds__(256) void k_vocab_slopes(Rows rows, const RowSlope*
   put_planes<PLANES, 8, bf16x8>(out + at, plane, y);
 }
 
-// A product of few tiles with many steps leaves its logits as sums of parts; a wave adds
-// them up for 64 classes of a row.
+// A product of few tiles leaves its logits as sums of parts.  Where they are of several pieces
+// of the vocabulary, or come from saved statistics, a wave adds them up for 64 classes of a row.
 struct FewLogits {
   const float* sums;
   const int* count;
@@ -470,9 +470,8 @@ struct FewLogits {
     return true;
   }
 };
-template <class E>
 __global__ __launch_bounds__(256) void k_vocab_few_stats(FewLogits l, const int* __restrict__ target, float2* __restrict__ parts,
-                                                         float* __restrict__ logit, E* __restrict__ kept, int padded) {
+                                                         float* __restrict__ logit, int padded) {
   int r, v;
   float x;
   if (!l.read(r, v, x)) return;
@@ -480,7 +479,6 @@ __global__ __launch_bounds__(256) void k_vocab_few_stats(FewLogits l, const int*
   const float top = fmaxf(wave_max(x), kNegMax), e = expf(x - top), sum = wave_sum(e);
   if (v == target[r] - l.first) logit[r] = x;
   if (threadIdx.x % 64 == 0) parts[(long long)((l.first + v) / 64) * padded + r] = make_float2(top, sum);
-  if (kept != nullptr) kept[(long long)r * l.ld + v] = E(e);
 }
 template <int PLANES>
 __global__ __launch_bounds__(256) void k_vocab_few_slopes(FewLogits l, const RowSlope* __restrict__ slope, __bf16* __restrict__ out,
@@ -576,15 +574,51 @@ struct GradOut {
   }
 };
 
+// stats = (loss, W) from the sum of weight times logp
+__device__ __forceinline__ void put_stats(float* stats, const Rows& rows, double sum, bool mean) {
+  const double total = *rows.total;
+  stats[0] = *rows.count == 0 || (mean && total == 0.0) ? 0.f : float(mean ? -sum / total : -sum);
+  stats[1] = float(total);
+}
+// The same from the rows' own, summed in 64 bits by one workgroup.
+struct Totals {
+  Rows rows;
+  const float* loss;  // [padded] weight times logp
+  float* stats;       // null: not here
+  bool mean;
+  __device__ __forceinline__ void run() const {
+    __shared__ double sums[4];
+    constexpr int AHEAD = 16;
+    const int used = *rows.count;
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < used; i += 256 * AHEAD) {
+      float v[AHEAD];
+#pragma unroll
+      for (int q = 0; q < AHEAD; ++q) v[q] = i + 256 * q < used ? loss[i + 256 * q] : 0.f;
+#pragma unroll
+      for (int q = 0; q < AHEAD; ++q) sum += double(v[q]);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) put_stats(stats, rows, ((sums[0] + sums[1]) + sums[2]) + sums[3], mean);
+  }
+};
+__global__ __launch_bounds__(256) void k_vocab_total(Totals totals) { totals.run(); }
+
 // The parts of a sum together, in order, into the gradient's rows.  With `at` the rows
-// that take no part get zeros.
+// that take no part get zeros.  The last workgroup does `totals` instead, if there are any.
 template <class T>
 __global__ __launch_bounds__(256) void k_vocab_sum(const float* __restrict__ sums, int parts, long long part, int padded,
                                                    const int* __restrict__ at, const float* __restrict__ factor,
                                                    long long rows, int width,
-                                                   typename T::Elem* __restrict__ out, long long ld, bool whole, bool add) {
+                                                   typename T::Elem* __restrict__ out, long long ld, bool whole, bool add,
+                                                   Totals totals) {
   const int per = (width + 3) / 4;
-  for (long long c = blockIdx.x * 256ll + threadIdx.x; c < rows * per; c += gridDim.x * 256ll) {
+  const unsigned groups = gridDim.x - (totals.stats != nullptr ? 1 : 0);
+  if (blockIdx.x == groups) return totals.run();
+  for (long long c = blockIdx.x * 256ll + threadIdx.x; c < rows * per; c += groups * 256ll) {
     const long long r = c / per;
     const int col = int(c % per) * 4;
     const long long from = at != nullptr ? at[r] : r;
@@ -612,11 +646,24 @@ struct JoinOut {
   float* stats;        // up to 64 rows: the totals too, null: not here
   bool mean;
 };
-// stats = (loss, W) from the sum of weight times logp
-__device__ __forceinline__ void put_stats(float* stats, const Rows& rows, double sum, bool mean) {
-  const double total = *rows.total;
-  stats[0] = *rows.count == 0 || (mean && total == 0.0) ? 0.f : float(mean ? -sum / total : -sum);
-  stats[1] = float(total);
+// What packed row i leaves: its logp, loss and g = dL/dlogp without the common factor.
+struct Joined {
+  float logp, loss, g;
+};
+__device__ __forceinline__ Joined join_row(const Rows& rows, int i, int t, float top, float sum, float logit) {
+  // no class with a probability: no distribution
+  const float nan = sum > 0.f ? 0.f : __builtin_nanf(""), w = rows.share[i];
+  const float logp = t >= 0 ? (logit - top) - logf(sum) + nan : __builtin_nanf("");
+  return {logp, w * logp, t >= 0 ? -w : __builtin_nanf("")};
+}
+__device__ __forceinline__ void put_row(const Rows& rows, const JoinOut& out, int i, const Joined& j, float top, float sum) {
+  const int r = rows.order[i];
+  out.logp[r] = j.logp;
+  if (out.saved != nullptr) out.saved[r] = make_float2(top, sum);
+  if (out.row_grads != nullptr) {
+    const double total = out.mean ? *rows.total : 1.0;
+    out.row_grads[r] = total == 0.0 ? 0.f : -float(double(rows.share[i]) / total);
+  }
 }
 __global__ __launch_bounds__(1024) void k_vocab_join(Rows rows, const float2* __restrict__ parts, const float* __restrict__ logit,
                                                      int tiles, int padded, JoinOut out) {
@@ -651,22 +698,11 @@ __global__ __launch_bounds__(1024) void k_vocab_join(Rows rows, const float2* __
   if (i >= used) {
     if (out.slope != nullptr) out.slope[i] = RowSlope{0.f, 0.f, 0.f, -1};
   } else {
-    const int r = rows.order[i], t = rows.target[i];
-    // no class with a probability: no distribution
-    const float nan = sum > 0.f ? 0.f : __builtin_nanf("");
-    const float logp = t >= 0 ? (logit[i] - top) - logf(sum) + nan : __builtin_nanf("");
-    out.logp[r] = logp;
-    if (out.saved != nullptr) out.saved[r] = make_float2(top, sum);
-    const float w = rows.share[i];
-    loss = w * logp;
-    if (out.row_grads != nullptr) {
-      const double total = out.mean ? *rows.total : 1.0;
-      out.row_grads[r] = total == 0.0 ? 0.f : -float(double(w) / total);
-    }
-    if (out.slope != nullptr) {
-      const float g = t >= 0 ? -w : __builtin_nanf("");
-      out.slope[i] = RowSlope{top, g / sum, g, t};
-    }
+    const int t = rows.target[i];
+    const Joined j = join_row(rows, i, t, top, sum, logit[i]);
+    put_row(rows, out, i, j, top, sum);
+    loss = j.loss;
+    if (out.slope != nullptr) out.slope[i] = RowSlope{top, j.g / sum, j.g, t};
   }
   if (out.loss != nullptr) out.loss[i] = loss;
   if (out.stats != nullptr) {
@@ -674,6 +710,73 @@ __global__ __launch_bounds__(1024) void k_vocab_join(Rows rows, const float2* __
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o);
     if (lane == 0) put_stats(out.stats, rows, all, out.mean);
+  }
+}
+
+// A product of few tiles over all classes: what the tiles' statistics, k_vocab_join and
+// k_vocab_slopes do, by a workgroup for each packed row, which holds its logits in
+// registers.  One launch for two, and a product that splits its steps (64 rows of 256 over
+// 1000 classes in float32: 29.2 us a call before).
+constexpr int kFewClasses = 4096, kFewEach = kFewClasses / 1024;
+template <int PLANES>
+__global__ __launch_bounds__(256) void k_vocab_few(FewLogits l, Rows rows, JoinOut out, __bf16* __restrict__ grad, long long plane) {
+  __shared__ float tops[4], sums[4], logit;
+  const int i = blockIdx.x, tid = threadIdx.x, used = *rows.count;
+  if (i >= (used + 63) / 64 * 64) return;
+  const int t = i < used ? rows.target[i] : -1;
+  const float* from = l.sums + (long long)i * l.ld;
+  f32x4 x[kFewEach];
+  float top = kNegMax;
+#pragma unroll
+  for (int c = 0; c < kFewEach; ++c) {
+    const int v = (c * 256 + tid) * 4;
+    x[c] = f32x4{};
+    if (v < l.ld) {
+#pragma unroll 8
+      for (int k = 0; k < l.parts; ++k) x[c] += *reinterpret_cast<const f32x4*>(from + k * l.part + v);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (v + q == t) logit = x[c][q];
+      if (v + q >= l.classes) x[c][q] = -__builtin_inff();
+      top = fmaxf(top, x[c][q]);
+    }
+  }
+  top = wave_max(top);
+  if (tid % 64 == 0) tops[tid / 64] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  float sum = 0.f;
+#pragma unroll
+  for (int c = 0; c < kFewEach; ++c)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      x[c][q] = expf(x[c][q] - top);
+      sum += x[c][q];
+    }
+  sum = wave_sum(sum);
+  if (tid % 64 == 0) sums[tid / 64] = sum;
+  __syncthreads();
+  sum = ((sums[0] + sums[1]) + sums[2]) + sums[3];
+  Joined j{0.f, 0.f, 0.f};
+  if (i < used) {
+    j = join_row(rows, i, t, top, sum, logit);
+    if (tid == 0) {
+      put_row(rows, out, i, j, top, sum);
+      if (out.loss != nullptr) out.loss[i] = j.loss;
+    }
+  }
+  if constexpr (PLANES > 0) {
+    const float f = -(j.g / sum), own = -j.g * expm1f(j.logp);  // (1 - p may be small)
+#pragma unroll
+    for (int c = 0; c < kFewEach; ++c) {
+      const int v = (c * 256 + tid) * 4;
+      if (v >= l.ld) break;
+      float y[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) y[q] = v + q == t ? own : x[c][q] * f;
+      put_planes<PLANES, 4, bf16x4>(grad + (long long)i * l.ld + v, plane, y);
+    }
   }
 }
 
@@ -691,23 +794,6 @@ __global__ __launch_bounds__(256) void k_vocab_slope(Rows rows, const float2* __
   slope[i] = RowSlope{st.x, g / st.y, g, t};
 }
 
-// stats = (loss, W), summed in 64 bits by one workgroup.
-__global__ __launch_bounds__(kWide) void k_vocab_total(Rows rows, const float* __restrict__ loss, bool mean, float* stats) {
-  __shared__ double sums[kWide / 64];
-  const int used = *rows.count;
-  double sum = 0.0;
-  for (int i = threadIdx.x; i < used; i += kWide) sum += double(loss[i]);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    double all = 0.0;
-    for (int k = 0; k < kWide / 64; ++k) all += sums[k];
-    put_stats(stats, rows, all, mean);
-  }
-}
-
 // ------------------------------------------------------------------ on the host
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -721,8 +807,7 @@ constexpr int64_t kPieceBytes = int64_t(2) << 30;
 // Products of BM x BN: large tiles feed the matrix cores best, small ones keep more of the
 // card busy, and give a row of few steps to more workgroups.
 using Large = Shape<256, 256, 64, 4, 2, 2, true>;
-using Large3 = Shape<128, 256, 32, 2, 4, 2>;
-using Wide3 = Shape<128, 256, 32, 2, 2, 2, true>;  // where an operand lies across: 1.29 PFLOP/s for 1.17
+using Large3 = Shape<128, 256, 32, 2, 2, 2, true>;
 using Flat = Shape<256, 64, 64, 4, 1, 2>;
 using Flat3 = Shape<128, 64, 32, 4, 1, 2>;
 using Small = Shape<64, 64, 64, 2, 2, 4>;
@@ -735,7 +820,8 @@ struct Plan {
   int32_t piece, pieces;  // classes of a piece, a multiple of kTile
   int hidden_parts, weight_parts;
   bool large_logits, large_hidden, large_weight;  // the products' tiles
-  int logits_parts;                               // more than one: FewLogits
+  bool few_logits;                                // the logits as sums of parts: FewLogits
+  int logits_parts;
   int grad_planes;
   int tile_classes() const { return !large_logits ? 64 : planes == 1 ? 256 : 128; }  // of the logits
 };
@@ -765,7 +851,8 @@ Plan plan_for(int64_t rows, int32_t width, int32_t classes, int32_t dtype) {
   p.large_weight = weight * parts_for(weight, p.padded_rows / step, 8) >= 128;
   p.hidden_parts = parts_for(p.large_hidden ? hidden : tiles_of(width, p.padded_rows, 64, 64), (piece + step - 1) / step, p.large_hidden ? 8 : 2);
   const int64_t few = tiles_of(piece, p.padded_rows, 64, 64);
-  p.logits_parts = p.large_logits || few > 64 ? 1 : parts_for(few, p.padded_width / step, 8);
+  p.few_logits = !p.large_logits && few <= kFewClasses / 64;
+  p.logits_parts = p.few_logits ? parts_for(few, p.padded_width / step, 2) : 1;
   p.grad_planes = p.planes == 3 ? 3 : p.large_hidden || p.large_weight ? 1 : 2;
   p.weight_parts = parts_for(p.large_weight ? weight : tiles_of(width, piece, 64, 64), p.padded_rows / step, p.large_weight ? 8 : 2);
   return p;
@@ -796,10 +883,10 @@ Layout layout(const Plan& p, bool gradient) {
   w.loss = take(R * 4);
   w.hidden = take(R * p.padded_width * 2 * p.planes);
   w.weight = take(size_t(p.piece) * p.padded_width * 2 * p.planes);
-  w.logits_sums = take(p.logits_parts > 1 ? size_t(p.logits_parts) * R * p.piece * 4 : 0);
+  w.logits_sums = take(p.few_logits ? size_t(p.logits_parts) * R * p.piece * 4 : 0);
   if (gradient) {
     w.grad = take(R * p.piece * 2 * p.grad_planes);
-    w.kept = p.grad_planes == 1 ? w.grad : take(p.pieces == 1 ? R * p.piece * 4 : 0);
+    w.kept = p.grad_planes == 1 ? w.grad : take(p.pieces == 1 && !p.few_logits ? R * p.piece * 4 : 0);
     w.hidden_sums = take(size_t(p.hidden_parts) * R * p.padded_width * 4);
     w.weight_sums = take(p.weight_parts > 1 ? size_t(p.weight_parts) * p.piece * p.padded_width * 4 : 0);
   }
@@ -900,8 +987,7 @@ struct Call {
       f(product<std::conditional_t<P == 1, Small, Small3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
     } else if constexpr (PB == P) {  // (two planes of G are for small tiles)
       if (p.padded_rows > 64)
-        f(product<std::conditional_t<P == 1, Large, std::conditional_t<XA, Wide3, Large3>>, PB, XA, false, N>(a, b, m, p.padded_rows,
-                                                                                                              depth, parts, e));
+        f(product<std::conditional_t<P == 1, Large, Large3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
       else
         f(product<std::conditional_t<P == 1, Flat, Flat3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
     }
@@ -921,21 +1007,32 @@ struct Call {
 
   template <Keep KEEP>
   void statistics_of(const Operand& weight, int k) const {
-    if (p.logits_parts > 1) {
-      using E = std::conditional_t<KEEP == Keep::kBf16, __bf16, float>;
-      const FewLogits l = few_logits(weight, k);
-      hipLaunchKernelGGL(k_vocab_few_stats<E>, dim3(few_grid(l)), dim3(256), 0, s, l, rows.target, get<float2>(w.parts), get<float>(w.logit),
-                         KEEP == Keep::kNothing ? nullptr : get<E>(w.kept), int(p.padded_rows));
-      return;
-    }
     logits(weight, 1,
            StatsOut<KEEP, P == 3>{rows.target, get<float2>(w.parts), get<float>(w.logit), get<void>(w.kept), k * p.piece, classes_of(k),
                                   int(p.padded_rows), k * (p.piece / p.tile_classes()), p.piece});
   }
+  // few tiles and a single piece: everything up to G (PLANES 0: of no gradient)
+  template <int PLANES>
+  int few(const JoinOut& out) const {
+    const FewLogits l = few_logits(weight(0, true), 0);
+    hipLaunchKernelGGL(k_vocab_few<PLANES>, dim3(unsigned(p.padded_rows)), dim3(256), 0, s, l, rows, out,
+                       PLANES > 0 ? get<__bf16>(w.grad) : nullptr, (long long)(p.padded_rows * p.piece));
+    return done();
+  }
+  bool few() const { return p.few_logits && p.pieces == 1; }
   int statistics(const JoinOut& out, bool keep) const {
+    if (few()) {
+      if (!keep) return few<0>(out);
+      if constexpr (P == 3) return few<3>(out);
+      else return p.grad_planes == 1 ? few<1>(out) : few<2>(out);
+    }
     for (int k = 0; k < p.pieces; ++k) {
       const Operand weight_k = weight(k, k == 0);
-      if (!keep) statistics_of<Keep::kNothing>(weight_k, k);
+      if (p.few_logits) {
+        const FewLogits l = few_logits(weight_k, k);
+        hipLaunchKernelGGL(k_vocab_few_stats, dim3(few_grid(l)), dim3(256), 0, s, l, rows.target, get<float2>(w.parts),
+                           get<float>(w.logit), int(p.padded_rows));
+      } else if (!keep) statistics_of<Keep::kNothing>(weight_k, k);
       else if (p.grad_planes == 1) statistics_of<Keep::kBf16>(weight_k, k);
       else statistics_of<Keep::kF32>(weight_k, k);
     }
@@ -945,11 +1042,11 @@ struct Call {
   }
 
   template <class O>
-  void sum(size_t at, int parts, int64_t part, const int* place, int64_t n, void* out, int64_t ld, bool add) const {
+  void sum(size_t at, int parts, int64_t part, const int* place, int64_t n, void* out, int64_t ld, bool add, const Totals& totals) const {
     using E = typename O::Elem;
     const bool whole = aligned_to(out, 4 * sizeof(E)) && ld % 4 == 0;
-    hipLaunchKernelGGL(k_vocab_sum<O>, dim3(grid(n * ((p.width + 3) / 4))), dim3(256), 0, s, get<float>(at), parts,
-                       (long long)part, p.padded_width, place, rows.factor, (long long)n, p.width, static_cast<E*>(out), (long long)ld, whole, add);
+    hipLaunchKernelGGL(k_vocab_sum<O>, dim3(grid(n * ((p.width + 3) / 4)) + (totals.stats != nullptr ? 1 : 0)), dim3(256), 0, s, get<float>(at), parts,
+                       (long long)part, p.padded_width, place, rows.factor, (long long)n, p.width, static_cast<E*>(out), (long long)ld, whole, add, totals);
   }
   // f(the product for piece k of the weight's gradient), and what the piece needs after it
   template <int GP, class O, class F>
@@ -963,14 +1060,14 @@ struct Call {
       if (!p.large_weight)
         f(product<std::conditional_t<P == 1, Small, Small3>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e));
       else if constexpr (GP == P)
-        f(product<std::conditional_t<P == 1, Large, Wide3>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e));
+        f(product<std::conditional_t<P == 1, Large, Large3>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e));
     };
     if (p.weight_parts == 1) {
       with(GradOut<O>{out, rows.factor, g.weight_stride, p.width, n, whole, add});
     } else {
       const int64_t part = int64_t(p.piece) * p.padded_width;
       with(PartOut{get<float>(w.weight_sums), part, p.padded_width, n, false});
-      sum<O>(w.weight_sums, p.weight_parts, part, nullptr, n, out, g.weight_stride, add);
+      sum<O>(w.weight_sums, p.weight_parts, part, nullptr, n, out, g.weight_stride, add, Totals{});
     }
   }
   // G of a single piece from what the first pass kept
@@ -985,7 +1082,7 @@ struct Call {
   template <int GP>
   void slopes_again(const Operand& weight, int k) const {
     const int64_t plane = p.padded_rows * p.piece;
-    if (p.logits_parts > 1) {
+    if (p.few_logits) {
       const FewLogits l = few_logits(weight, k);
       hipLaunchKernelGGL(k_vocab_few_slopes<GP>, dim3(few_grid(l)), dim3(256), 0, s, l, get<RowSlope>(w.slope), get<__bf16>(w.grad),
                          (long long)plane);
@@ -993,13 +1090,14 @@ struct Call {
       logits(weight, 1, SlopeOut<GP>{get<RowSlope>(w.slope), get<__bf16>(w.grad), plane, p.piece, k * p.piece, classes_of(k)});
     }
   }
-  // With the rows' slopes in place.  `kept`: the logp of the pass that kept the only
-  // piece's exponentials; `packed`: the piece of the weight that was packed last.
-  int gradients(const acdc_vocab_grads& g, const float* kept, int packed) const {
+  // With the rows' slopes or, of few tiles, G itself in place.  `kept`: the logp of the pass
+  // that kept the only piece's exponentials (or G); `packed`: the piece of the weight that was
+  // packed last; `totals`: for the last launch if it is one over rows.
+  int gradients(const acdc_vocab_grads& g, const float* kept, int packed, const Totals& totals) const {
     if constexpr (P == 3) {
-      return gradients_of<3>(g, kept, packed);
+      return gradients_of<3>(g, kept, packed, totals);
     } else {
-      return p.grad_planes == 1 ? gradients_of<1>(g, kept, packed) : gradients_of<2>(g, kept, packed);
+      return p.grad_planes == 1 ? gradients_of<1>(g, kept, packed, totals) : gradients_of<2>(g, kept, packed, totals);
     }
   }
   // Both gradients' products: in one launch where their tiles are of one shape.
@@ -1015,13 +1113,13 @@ struct Call {
     }
   }
   template <int GP>
-  int gradients_of(const acdc_vocab_grads& g, const float* kept, int packed) const {
+  int gradients_of(const acdc_vocab_grads& g, const float* kept, int packed, const Totals& totals) const {
     const int64_t part = p.padded_rows * p.padded_width;
     for (int k = 0; k < p.pieces; ++k) {
       const Operand wk = weight(k, k == packed);
       packed = k;
-      if (kept != nullptr) slopes<GP>(kept);
-      else slopes_again<GP>(wk, k);
+      if (kept == nullptr) slopes_again<GP>(wk, k);
+      else if (!few()) slopes<GP>(kept);
       auto weight_too = [&](auto&& f) {
         if (g.weight_type == head.dtype) weight_grad<GP, T>(g, k, f);
         else weight_grad<GP, F32>(g, k, f);
@@ -1036,7 +1134,7 @@ struct Call {
                             weight_too([&](const auto& dw) { both<GP>(dh, dw); });
                           });
     }
-    if (g.hidden != nullptr) sum<T>(w.hidden_sums, p.hidden_parts, part, rows.at, p.rows, g.hidden, g.hidden_stride, false);
+    if (g.hidden != nullptr && p.rows > 0) sum<T>(w.hidden_sums, p.hidden_parts, part, rows.at, p.rows, g.hidden, g.hidden_stride, false, totals);
     return done();
   }
 };
@@ -1134,7 +1232,7 @@ extern "C" int acdc_vocab_backward(const acdc_vocab_head* head, const float* sav
     c.pack_rows(grad_logp, Factor{scale, 1.f, false}, nullptr, nullptr, nullptr);
     hipLaunchKernelGGL(k_vocab_slope, dim3(Call<T>::grid(c.p.padded_rows)), dim3(256), 0, c.s, c.rows,
                        reinterpret_cast<const float2*>(saved), int(c.p.padded_rows), c.template get<RowSlope>(c.w.slope));
-    return c.gradients(*grads, nullptr, 0);
+    return c.gradients(*grads, nullptr, 0, Totals{});
   });
 }
 
@@ -1155,13 +1253,15 @@ extern "C" int acdc_vocab_loss(const acdc_vocab_head* head, const float* weights
     float* loss = c.template get<float>(c.w.loss);
     const bool keep = gradient && c.p.pieces == 1;
     c.pack_rows(weights, Factor{nullptr, q.grad_scale, q.mean != 0}, logp, stat, row_grads);
-    const bool few = c.p.padded_rows == 64;
+    // the totals: with the rows' own, in the last launch, or in one of their own
+    const bool joined = c.p.padded_rows == 64 && !c.few(), last = gradient && grads->hidden != nullptr && head->rows > 0;
+    const Totals totals{c.rows, loss, joined ? nullptr : stats, q.mean != 0};
     int rc = c.statistics(JoinOut{logp, stat, row_grads, gradient ? c.template get<RowSlope>(c.w.slope) : nullptr,
-                                  few ? nullptr : loss, few ? stats : nullptr, q.mean != 0},
+                                  joined ? nullptr : loss, joined ? stats : nullptr, q.mean != 0},
                           keep);
     if (rc != ACDC_OK) return rc;
-    if (!few) hipLaunchKernelGGL(k_vocab_total, dim3(1), dim3(kWide), 0, c.s, c.rows, loss, q.mean != 0, stats);
+    if (!joined && !last) hipLaunchKernelGGL(k_vocab_total, dim3(1), dim3(256), 0, c.s, totals);
     rc = done();
-    return rc != ACDC_OK || !gradient ? rc : c.gradients(*grads, keep ? logp : nullptr, c.p.pieces - 1);
+    return rc != ACDC_OK || !gradient ? rc : c.gradients(*grads, keep ? logp : nullptr, c.p.pieces - 1, last ? totals : Totals{});
   });
 }

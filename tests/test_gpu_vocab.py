@@ -1,6 +1,8 @@
 """Losses over a vocabulary without its logits, on the GPU, against their
 definitions in 64 bits."""
 
+import struct
+
 import numpy as np
 import pytest
 
@@ -160,6 +162,16 @@ def test_no_row_takes_part(env):
     s = losses.vocab_logprobs(h[:0], w, t[:0], save=True)
     gh, gw = losses.vocab_logprobs_backward(h[:0], w, t[:0], s.saved, s.logp)
     assert gh.shape == (0, 24) and (gw == 0).all()
+    # the C call with no row and a pointer to where its gradient would go
+    from paper_1511_05946_amd import acdc
+    from paper_1511_05946_amd._lib import lib
+    spare, stats, gw = torch.full((24,), 3.0, device="cuda"), torch.ones(2, device="cuda"), torch.ones_like(w)
+    ws = torch.empty(losses.vocab_workspace_bytes(h[:0], w), dtype=torch.uint8, device="cuda")
+    head = struct.pack("3Q3q4i", h.data_ptr(), w.data_ptr(), t.data_ptr(), 24, 24, 0, 24, 300, 0, 64)
+    record = struct.pack("2Q2q2i", spare.data_ptr(), gw.data_ptr(), 24, 24, 0, 0)
+    rc = acdc._call(lib().acdc_vocab_loss, h.device, head, None, struct.pack("fi", 1.0, 1), stats.data_ptr(), None, None, None, record,
+                    ws.data_ptr(), ws.numel())
+    assert rc == 0 and stats.tolist() == [0, 0] and (spare == 3).all() and (gw == 0).all()
 
 
 @pytest.mark.parametrize("rows", [2, 64, 300])
