@@ -31,7 +31,7 @@ SHAPES = [(1, 1, 1, "float32", 64, 0, 0), (1, 1, 1, "bfloat16", 32, 0, 0), (2, 3
           (2100, 40, 50, "bfloat16", 64, 0, 0), (40, 1, 300, "float32", 64, 0, 0),
           # few tiles of many steps
           (3, 8128, 10, "float32", 64, 0, 0), (70, 5000, 100, "bfloat16", 64, 0, 8), (300, 2500, 70, "float32", 32, 1, 0),
-          (2, 20000, 3, "bfloat16", 64, 0, 0)]
+          (2, 20000, 3, "bfloat16", 64, 0, 0), (5, 8192, 4000, "bfloat16", 64, 0, 0)]
 
 
 def values(torch, gen, rows, width, extra, dtype, std):
@@ -132,7 +132,8 @@ def test_weight_gradient_is_added(env, dtype, given):
 
 
 @pytest.mark.parametrize("shape", [(16384, 16, 20000, "bfloat16", 64, 0, 0), (16384, 8, 70000, "bfloat16", 64, 0, 0),
-                                   (16384, 16, 20000, "float32", 64, 0, 0), (30000, 7, 7000, "float32", 64, 0, 0)])
+                                   (16384, 16, 20000, "float32", 64, 0, 0), (30000, 7, 7000, "float32", 64, 0, 0),
+                                   (3, 131072, 1600, "float32", 64, 0, 0)])
 def test_pieces_of_the_vocabulary(env, shape):
     """16384 rows leave 65536 classes of bfloat16 and 13056 of float32 a piece of 2 GiB: one piece, whose exponentials
     are kept, and more."""
