@@ -299,11 +299,15 @@ struct StatsOut {
                                              float2* slots) const {
     constexpr int BN = S::BN, WM = S::WM;
     const int lane = spot.lane;
+    // (asked for together, not one after the other between the stores below)
+    int targets[NI];
+#pragma unroll
+    for (int n = 0; n < NI; ++n) targets[n] = target[spot.n(n)];
     __syncthreads();  // the tiles have been read
     float tops[NI];
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
-      const int r = spot.n(n), t = target[r] - first - spot.m(0);
+      const int r = spot.n(n), t = targets[n] - first - spot.m(0);
       if ((at.tm + 1) * S::BM > classes) mask(acc, spot, n);
       if (unsigned(t) < 16u * MI && t % 32 < 8) {
 #pragma unroll
@@ -405,10 +409,13 @@ struct SlopeOut {
   int ld, first, classes;
   template <class S, int MI, int NI, class SP>
   __device__ __forceinline__ void operator()(f32x4 (&acc)[MI][NI], const SP& spot, const Place&, int, float2*) const {
+    RowSlope slopes[NI];
+#pragma unroll
+    for (int n = 0; n < NI; ++n) slopes[n] = row[spot.n(n)];
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
       const int r = spot.n(n);
-      const RowSlope k = row[r];
+      const RowSlope k = slopes[n];
       const int t = k.target - first;
       __bf16* to = out + (long long)r * ld;
 #pragma unroll
