@@ -13,13 +13,14 @@
 // (Along::swizzle, Across::swizzle): 8 lanes that read 16 bytes each touch all
 // banks once, and so do the transposing reads of "across" tiles.
 //
-// 65536 x 7424 x 4096 in tiles of 256 x 256, steps of 64, eight waves: 1.16 to 1.21
-// PFLOP/s with both operands along, 1.05 to 1.09 with A across, 1.14 to 1.21
-// with both; the products of float32 planes 1.19, 1.06 and 1.29.  The loop is bound
-// by its loads into LDS that miss L2: 1.47 PFLOP/s where all of them hit, 1.61
-// with no load into LDS, 1.95 with the matrix instructions alone.  Slower:
-// steps of 32 in four or five parts of LDS (0.98, 1.11), four waves of 128 x
-// 128 each (registers run out), squares of 32 x 32 (1.86 for 2.10 alone).
+// 7373 rows of 4096 over 65536 classes in tiles of 256 x 256, steps of 64, eight waves:
+// 1.42 PFLOP/s in the main loop with both operands along, 1.32 as a launch of
+// the two products of the gradients.  The loop is bound by its loads into LDS that
+// miss L2 (with both operands along, before: 1.21 PFLOP/s, 1.47 where all of them hit,
+// 1.61 with no load into LDS, 1.95 with the matrix instructions alone).  Slower:
+// steps of 32 in four or five parts of LDS (0.98, 1.11), tiles of 128 x 256 of which a CU has
+// two (9.65 ms a call became 11.8), four waves of 128 x 128 each (registers
+// run out), squares of 32 x 32 (1.86 for 2.10 alone).
 //
 // float32 values x = x0 + x1 + x2 are three planes of bfloat16 (8 of 24 bits
 // each, exact): a step multiplies the six pairs of planes that matter,
@@ -265,7 +266,9 @@ __device__ __forceinline__ void wait_loads() {
 }
 
 // The parts of LDS, each an object of its own: only so does the compiler see that a transposing
-// read of one of them need not wait for the loads on their way into another.
+// read of one of them need not wait for the loads on their way into another (7373 rows of 4096
+// over 65536 classes 10.34 ms a call with one object, 9.50 so; float32 1000 of 1024 over 20001
+// 772 and 698 us).
 struct Stages {
   char ACDC_LDS* at[4];
 };
@@ -499,7 +502,9 @@ __global__ __launch_bounds__(P::T) void k_gemm(P product, const int* __restrict_
 }
 
 // Two products in one launch, the second from workgroup `first` on (a multiple of 8: the
-// XCDs): its tiles fill the CUs that the first one's last round leaves idle.
+// XCDs): its tiles fill the CUs that the first one's last round leaves idle, and small
+// products cost one launch (64 rows of 256 over 1000 classes: 32.1 us a call in two, 28.8 so;
+// 1000 of 1024 over 20001: 786 and 772).
 template <class P, class Q>
 __global__ __launch_bounds__(P::T) void k_gemm_both(P p, Q q, unsigned first, const int* __restrict__ count) {
   static_assert(P::T == Q::T && P::STAGE == Q::STAGE && P::STAGES == Q::STAGES);
