@@ -122,8 +122,12 @@ __global__ __launch_bounds__(Group<LANES>::WG) void k_norm(const typename TX::El
   }
 }
 
-// Rows of more than 32768 values: a workgroup reads its row three times, the second and
-// third time from its XCD's L2.
+// Rows of more than 32768 values: a workgroup reads its row twice.  Mean and squares about it
+// of eight values at a time, joined to a lane's own before:
+//   mean' = mean + (m - mean) c / (n + c),  squares' = squares + q + (m - mean)^2 n c / (n + c),
+// and then to those of all lanes, in the same way (1810 rows of 54837 float32 values 227 us,
+// 3.5 TB/s, for 269 with a reading more; 2000 of 65536 bfloat16 133 for 130.  Twice as many
+// values in registers: 271 and 283).
 template <class TX, class TY, int LANES>
 __global__ __launch_bounds__(LANES) void k_norm_long(const typename TX::Elem* __restrict__ x, long long x_stride, Vector weight,
                                                      Vector bias, float eps, typename TY::Elem* __restrict__ y,
@@ -133,22 +137,24 @@ __global__ __launch_bounds__(LANES) void k_norm_long(const typename TX::Elem* __
   const float inv = 1.f / float(width);
   for (int r = blockIdx.x; r < rows; r += gridDim.x) {
     const typename TX::Elem* row = x + r * x_stride;
-    float s = 0.f, v[kEight];
+    float v[kEight], n = 0.f, own = 0.f, squares = 0.f;  // of the lane's values so far
 #pragma unroll 4
     for (int col = threadIdx.x * kEight; col < width; col += LANES * kEight) {
       load_some<TX>(row + col, width - col, 0.f, v);
+      const int left = min(kEight, width - col);
+      const float c = float(left);
+      float s = 0.f, q = 0.f;
 #pragma unroll
       for (int i = 0; i < kEight; ++i) s += v[i];
-    }
-    const float mean = sum(s) * inv;
-    s = 0.f;
-#pragma unroll 4
-    for (int col = threadIdx.x * kEight; col < width; col += LANES * kEight) {
-      load_some<TX>(row + col, width - col, mean, v);
+      const float m = s / c, d = m - own, f = c / (n + c);
 #pragma unroll
-      for (int i = 0; i < kEight; ++i) s += (v[i] - mean) * (v[i] - mean);
+      for (int i = 0; i < kEight; ++i) q += i < left ? (v[i] - m) * (v[i] - m) : 0.f;
+      own += d * f;
+      squares += q + d * d * (n * f);
+      n += c;
     }
-    const float rstd = 1.f / sqrtf(sum(s) * inv + eps);
+    const float mean = sum(n * own) * inv;
+    const float rstd = 1.f / sqrtf(sum(squares + n * (own - mean) * (own - mean)) * inv + eps);
     if (saved != nullptr && threadIdx.x == 0) saved[r] = make_float2(mean, rstd);
     typename TY::Elem* to = y + r * y_stride;
 #pragma unroll 2
