@@ -247,7 +247,7 @@ struct Spot {
 
 // How rows in use bound a product: kN: the n-tiles past *count end at once; kK: they are
 // the k.
-enum class Count { kNone, kN, kK };
+enum class Count { kN = 1, kK };
 
 // The shape of a workgroup: BM x BN of C by WM x WN waves, steps of BK, of which STAGES
 // are in LDS at a time.
@@ -295,7 +295,7 @@ struct Product {
   __device__ __forceinline__ void run(unsigned id, const Stages& lds, const int* __restrict__ count) const;
 };
 
-// Workgroup `id` of the product's.  *count (may be null): the rows in use.
+// Workgroup `id` of the product's.  *count: the rows in use.
 template <class S, int PA, int PB, bool ACROSS_A, bool ACROSS_B, Count COUNT, class Epilogue>
 __device__ __forceinline__ void Product<S, PA, PB, ACROSS_A, ACROSS_B, COUNT, Epilogue>::run(unsigned id, const Stages& lds,
                                                                                              const int* __restrict__ count) const {
