@@ -31,14 +31,16 @@ __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f
 // The product's rounding is 2^-24 |d| of the result: float32 gradients would show it.  EXACT:
 // e^d = 2^p (1 + r log 2) with p + r = d log2(e) and p rounded, for d <= 0 (half the
 // instructions of expf, which also looks after large d and results that are no normal
-// numbers: of these 0 is made).  d = -inf: p = -inf, e = 0 and r = NaN, which the maximum
-// takes out; otherwise |r| is far below 1.  (6075 rows of 64 over 98566 classes: 918 us a call for
+// numbers: of these 0 is made).  Where e is not 0, |r| is below 2^-16.  Where e is 0, r may be
+// anything: it grows with |d|, is infinite where p leaves 32 bits (d below -2.36e38, a class
+// switched off by the type's lowest value) and NaN at d = -inf; the median of r, -1 and 1 is
+// finite (-1 for NaN), and 0 stays 0.  (6075 rows of 64 over 98566 classes: 918 us a call for
 // 1062, float32 1000 of 1024 over 20001 681 for 684.)
 template <bool EXACT>
 __device__ __forceinline__ float exp_as(float d) {
   if constexpr (EXACT) {
     constexpr float kLow = 1.925963033500e-8f;  // log2(e) - kLog2e
-    const float p = d * kLog2e, r = fmaxf(fmaf(d, kLow, fmaf(d, kLog2e, -p)), -1.f);
+    const float p = d * kLog2e, r = __builtin_amdgcn_fmed3f(fmaf(d, kLow, fmaf(d, kLog2e, -p)), -1.f, 1.f);
     const float e = __builtin_amdgcn_exp2f(p);
     return fmaf(e * 0.693147180559945f, r, e);
   } else {

@@ -1,0 +1,101 @@
+"""Logits of every size in the losses over a vocabulary, in calls of few tiles and of many,
+of one piece of the vocabulary and of several, on the GPU, against the definitions in 64 bits."""
+
+import numpy as np
+import pytest
+
+import lm_reference as R
+from test_gpu_vocab import check_gradients, close, env, make  # noqa: F401 (env: a fixture)
+
+pytestmark = pytest.mark.gpu
+
+# few tiles; small tiles that keep their exponentials or not (few rows); large tiles; more than
+# one piece of the vocabulary
+SIZES = [(90, 40, 100), (100, 30, 1500), (8, 40, 5000), (300, 16, 8300), (1100, 512, 16500)]
+CASES = [(*s, dtype) for s in SIZES for dtype in ("float32", "bfloat16")] + [(16384, 8, 14000, "float32")]
+
+
+def switched_off(torch, case, seed):
+    """A column of ones beside hidden, and beside the weight one that is 0, or the type's
+    lowest value for each third class: hidden, weight, targets among the others, those classes."""
+    rows, width, classes, dtype = case
+    h, w, t, h64, w64, t64, share = make(torch, (rows, width, classes, dtype, 64, 0, 0), seed=seed, idle=0.97 if rows > 10000 else 0.25)
+    off = torch.arange(classes, device="cuda") % 3 == 1
+    t64 = np.where(t64 < 0, t64, t64 - (t64 % 3 == 1))
+    column = torch.where(off, torch.finfo(w.dtype).min, 0.0).to(w.dtype)
+    h = torch.cat((h, torch.ones(rows, 1, dtype=h.dtype, device="cuda")), 1)
+    w = torch.cat((w, column[:, None]), 1)
+    h64 = np.concatenate((h64, np.ones((rows, 1))), 1)
+    w64 = np.concatenate((w64, np.zeros((classes, 1))), 1)
+    return h, w, torch.from_numpy(t64).cuda(), h64, w64, t64, off
+
+
+@pytest.mark.parametrize("case", CASES)
+def test_classes_switched_off(env, case):  # noqa: F811
+    """Classes whose logit is the type's lowest value: as if they were not there."""
+    torch, losses = env
+    h, w, t, h64, w64, t64, off = switched_off(torch, case, 11)
+    on, rows = (~off).cpu().numpy(), t64 >= 0
+    # the definition over the other classes, and their numbers among themselves
+    number = np.cumsum(on) - 1
+    ref = R.Vocab(h64[rows], w64[on], number[t64[rows]])
+    there = torch.from_numpy(rows).cuda()
+
+    def check(logp, gh, gw):
+        close(logp[there], ref.logp, ref.logp_tol, "logp")
+        check_gradients(ref, -ref.share, gh[there], gw[~off], case[3] == "bfloat16")
+        assert (gw[off] == 0).all() and (gh[~there] == 0).all()
+
+    r = losses.vocab_loss(h, w, t, save=True)
+    assert abs(r.stats[0].item() - ref.loss) <= ref.loss_tol
+    check(r.logp, r.grad_hidden, r.grad_weight)
+    s = losses.vocab_logprobs(h, w, t, save=True)
+    close(s.logp[there], ref.logp, ref.logp_tol, "logp")
+    check(s.logp, *losses.vocab_logprobs_backward(h, w, t, s.saved, r.row_grads))
+    # one of them as a target: its log-probability is as low, and no row is NaN
+    t[torch.nonzero(there)[0]] = 1
+    r = losses.vocab_loss(h, w, t)
+    assert r.logp.min().item() <= torch.finfo(h.dtype).min and not torch.isnan(r.logp).any()
+    assert torch.isfinite(r.grad_weight[~off]).all()
+
+
+@pytest.mark.parametrize("case", CASES)
+def test_what_is_not_a_number(env, case):  # noqa: F811
+    """A target past the classes and hidden values that are not finite: NaN for their own
+    row and the weight's gradient, and no other row."""
+    torch, losses = env
+    rows, width, classes, dtype = case
+    h, w, t, h64, w64, t64, _ = make(torch, (rows, width, classes, dtype, 64, 0, 0), seed=12, idle=0.97 if rows > 10000 else 0.25)
+    t64 = np.where(np.arange(rows) < 3, 7, t64)
+    t = torch.from_numpy(t64).cuda()
+    t[0], h[1, 3], h[2, 0] = classes, float("inf"), float("nan")
+    h[1, :3] = 1.0
+    on = t64 >= 0
+    on[:3] = False
+    ref = R.Vocab(h64[on], w64, t64[on])
+    there, idle = torch.from_numpy(on).cuda(), torch.from_numpy(t64 < 0).cuda()
+    r = losses.vocab_loss(h, w, t, mean=False, save=True)
+    s = losses.vocab_logprobs(h, w, t, save=True)
+    again = losses.vocab_logprobs_backward(h, w, t, s.saved, r.row_grads.nan_to_num(-1.0))
+    assert torch.isnan(r.stats[0])
+    for logp, gh, gw in ((r.logp, r.grad_hidden, r.grad_weight), (s.logp, *again)):
+        close(logp[there], ref.logp, ref.logp_tol, "logp")
+        assert torch.isnan(logp[:3]).all() and torch.isnan(gh[:3]).all() and torch.isnan(gw).all()
+        assert torch.isfinite(gh[there]).all() and (gh[idle] == 0).all() and (logp[idle] == 0).all()
+
+
+@pytest.mark.parametrize("case", CASES)
+def test_far_logits(env, case):  # noqa: F811
+    """Rows whose softmax is one class: logits up to thousands apart."""
+    torch, losses = env
+    rows, width, classes, dtype = case
+    h, w, t, h64, w64, t64, _ = make(torch, (rows, width, classes, dtype, 64, 0, 0), seed=13, idle=0.97 if rows > 10000 else 0.25)
+    on = t64 >= 0
+    w = (w.float() * 1000.0).to(w.dtype)
+    ref = R.Vocab(h64[on], w.double().cpu().numpy(), t64[on])
+    there = torch.from_numpy(on).cuda()
+    r = losses.vocab_loss(h, w, t, save=True)
+    close(r.logp[there], ref.logp, ref.logp_tol, "logp")
+    again = losses.vocab_logprobs_backward(h, w, t, r.saved, r.row_grads)
+    for g in (r.grad_hidden, r.grad_weight, *again):
+        assert torch.isfinite(g).all()
