@@ -27,9 +27,10 @@ extern "C" {
  *   logp = x_rt - M - log S
  * bfloat16 values are multiplied exactly and summed in 32 bits; float32
  * values in products as exact as 32-bit ones.  Before the products that give
- * the two gradients dL/dx is rounded, for float32 inputs to 24 bits, for
- * bfloat16 ones to 8 (acdc_vocab_loss may round the exponentials in it to 8
- * bits as well) or, where the products are small, to 16.
+ * the two gradients dL/dx is rounded: for float32 inputs to 24 bits, for
+ * bfloat16 ones to 16 or, in large products of 1024 rows and 1024 classes or
+ * more, to 8 (where acdc_vocab_loss may round the exponentials in it to 8 bits
+ * as well).
  *
  * hidden: rows x width, weight: classes x width, both of type `dtype`, rows
  * hidden_stride and weight_stride apart (in elements, >= width).  targets as in

@@ -368,14 +368,16 @@ __device__ __forceinline__ void Product<S, PA, PB, ACROSS_A, ACROSS_B, COUNT, Ep
     meet();
   };
   constexpr int READS = PA * (ACROSS_A ? 2 : 1) * MI + PB * (ACROSS_B ? 2 : 1) * NI;
+  constexpr int PAIRS = PA == PB ? PA * (PA + 1) / 2 : MOST;  // of planes
+  static_assert(PA == PB || PA == 1);
 #pragma unroll
   for (int q = 0; q < STAGES - 1; ++q)
     if (from + q < to) fetch.template operator()<false>(q, from + q);
   // (step s is in part (s - from) % STAGES of LDS, a constant wherever one is used)
   if constexpr (S::AHEAD && BK == 32) {
     // The registers of one step are read while the matrix cores work on the other's.
-    static_assert(STAGES == 2 && PA == PB);
-    constexpr int PER = PA * (PA + 1) / 2 * MI * NI / READS;
+    static_assert(STAGES == 2);
+    constexpr int PER = PAIRS * MI * NI / READS;
     Part even, odd;
     int s = from;
     if (from < to) {

@@ -393,8 +393,9 @@ struct RowSlope {
 };
 
 // Values of G as 1, 2 or 3 planes of bfloat16: the one rounding between the logits and the
-// gradients, to 8, 16 or 24 bits.  Where thousands of terms are summed, that of bfloat16
-// inputs to 8 bits is lost in the inputs' own; small problems, whose time it is not, take 16.
+// gradients, to 8, 16 or 24 bits.  float32 inputs take 24 and bfloat16 ones 16, of which nothing
+// is seen in a gradient of 8 or 32 bits.  Only large products of bfloat16 inputs, of kMany terms
+// or more each, take 8 (see there).
 template <int PLANES, int N, class V>
 __device__ __forceinline__ void put_planes(__bf16* out, long long plane, const float (&y)[N]) {
   V o[PLANES];
@@ -833,18 +834,37 @@ constexpr int kTile = 256;
 // Bytes of a piece of G.  A piece costs a pass over the sums of dL/dhidden, and the logits
 // of a single one need not be computed again: 8192 rows over 65536 classes are one piece.
 constexpr int64_t kPieceBytes = int64_t(2) << 30;
+// Terms from which on, in both gradients, G of bfloat16 inputs may be rounded to 8 bits: it is
+// multiplied by values of 8 bits, and as their roundings do, those of G fall either way, so that
+// against the sizes of n terms together a sum is off by 2^-9 / sqrt(n) or so.  (A sum that few of
+// its terms decide is off by as much as they are, 2^-8 at the most where G was rounded twice.)
+// 16 bits cost few rows nothing and many the second product of every pair: with 16 and with 8
+// bits 1 row of 4096 over 8192 classes 88 and 90 us, 64 of 4096 over 65536 499 and 498, 256 of
+// 1024 over 32768 153 and 125, 1000 of 4096 over 65536 2.31 and 1.50 ms, 2048 of 1024 over 32768
+// 0.78 and 0.46, 8192 of 4096 over 65536 18.6 and 10.4.
+constexpr int kMany = 1024;
 
 // Products of BM x BN: large tiles feed the matrix cores best, small ones keep more of the
 // card busy, and give a row of few steps to more workgroups.  Four waves of 64 x 128 for
 // float32: eight of 64 x 64 have no registers for reading ahead (1000 x 1024 over 20001
 // classes 676 us a call, 696 with those where no operand lies across), and half the tile saves
-// nothing where it fills the last round (685 for 684).
+// nothing where it fills the last round (685 for 684).  Large2: bfloat16 times two planes of G,
+// for which steps of 64 do not fit and reading ahead spills (1000 of 4096 over 65536 classes in
+// tiles of 256 x 256 2.31 ms a call, of 128 x 256 that read ahead 2.99, in three parts of LDS 3.31).
 using Large = Shape<256, 256, 64, 4, 2, 2, true>;
 using Large3 = Shape<128, 256, 32, 2, 2, 2, true>;
+using Large2 = Shape<256, 256, 32, 4, 2, 3>;
 using Flat = Shape<256, 64, 64, 4, 1, 2>;
 using Flat3 = Shape<128, 64, 32, 4, 1, 2>;
 using Small = Shape<64, 64, 64, 2, 2, 4>;
 using Small3 = Shape<64, 64, 32, 2, 2, 4>;
+// The shapes for P planes of one operand and PB of the other.
+template <int P, int PB>
+using LargeOf = std::conditional_t<PB == 1, Large, std::conditional_t<P == 1, Large2, Large3>>;
+template <int P, int PB>
+using FlatOf = std::conditional_t<P == 1, Flat, Flat3>;
+template <int P>
+using SmallOf = std::conditional_t<P == 1, Small, Small3>;
 
 // How a call is cut up: fixed by its sizes alone.
 struct Plan {
@@ -871,8 +891,11 @@ Plan plan_for(int64_t rows, int32_t width, int32_t classes, int32_t dtype) {
   p.planes = dtype == ACDC_F32 ? 3 : 1;
   p.padded_rows = up(std::max<int64_t>(rows, 1), rows <= 64 ? 64 : kTile);
   p.padded_width = int32_t(up(width, 64));
-  const int64_t values = std::max<int64_t>(p.padded_rows, p.padded_width);  // of a class: in the piece of G, in the packed weight
-  const int64_t most = std::max<int64_t>(kTile, kPieceBytes / ((p.planes == 1 ? 2 : 10) * values) / kTile * kTile);
+  const bool many = rows >= kMany && classes >= kMany;
+  // bytes of a class in the piece of G (with what the first pass keeps for it) and in the packed weight
+  const int64_t bytes = p.planes == 3 ? 10 * std::max<int64_t>(p.padded_rows, p.padded_width)
+                                      : std::max<int64_t>((many ? 2 : 8) * p.padded_rows, 2 * int64_t(p.padded_width));
+  const int64_t most = std::max<int64_t>(kTile, kPieceBytes / bytes / kTile * kTile);
   p.pieces = int32_t((classes + most - 1) / most);
   p.piece = int32_t(up((classes + p.pieces - 1) / p.pieces, kTile));
   const int bm = p.planes == 1 ? 256 : 128, bn = rows <= 64 ? 64 : 256, step = p.planes == 1 ? 64 : 32;
@@ -888,7 +911,7 @@ Plan plan_for(int64_t rows, int32_t width, int32_t classes, int32_t dtype) {
   const int64_t few = tiles_of(piece, p.padded_rows, 64, 64);
   p.few_logits = !p.large_logits && few <= kFewClasses / 64;
   p.logits_parts = p.few_logits ? parts_for(few, p.padded_width / step, 2) : 1;
-  p.grad_planes = p.planes == 3 ? 3 : p.large_hidden || p.large_weight ? 1 : 2;
+  p.grad_planes = p.planes == 3 ? 3 : many && (p.large_hidden || p.large_weight) ? 1 : 2;
   p.weight_parts = parts_for(p.large_weight ? weight : tiles_of(width, piece, 64, 64), p.padded_rows / step, p.large_weight ? 8 : 2);
   return p;
 }
@@ -1018,14 +1041,9 @@ struct Call {
   template <int PB, bool XA, class E, class F>
   void over_rows(bool large, const Operand& a, const Operand& b, int64_t m, int depth, int parts, const E& e, F&& f) const {
     constexpr Count N = Count::kN;
-    if (!large) {
-      f(product<std::conditional_t<P == 1, Small, Small3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
-    } else if constexpr (PB == P) {  // (two planes of G are for small tiles)
-      if (p.padded_rows > 64)
-        f(product<std::conditional_t<P == 1, Large, Large3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
-      else
-        f(product<std::conditional_t<P == 1, Flat, Flat3>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
-    }
+    if (!large) f(product<SmallOf<P>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
+    else if (p.padded_rows > 64) f(product<LargeOf<P, PB>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
+    else f(product<FlatOf<P, PB>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
   }
   // classes x packed rows
   template <class E>
@@ -1092,10 +1110,8 @@ struct Call {
     const bool whole = aligned_to(out, 4 * sizeof(E)) && g.weight_stride % 4 == 0, add = g.accumulate != 0;
     auto with = [&](const auto& e) {
       constexpr Count K = Count::kK;
-      if (!p.large_weight)
-        f(product<std::conditional_t<P == 1, Small, Small3>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e));
-      else if constexpr (GP == P)
-        f(product<std::conditional_t<P == 1, Large, Large3>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e));
+      if (!p.large_weight) f(product<SmallOf<P>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e));
+      else f(product<LargeOf<P, GP>, GP, true, true, K>(hidden(), grad(k), p.width, n, 0, p.weight_parts, e));
     };
     if (p.weight_parts == 1) {
       with(GradOut<O>{out, rows.factor, g.weight_stride, p.width, n, whole, add});
@@ -1139,7 +1155,7 @@ struct Call {
   // parts: the weight's alone (in the same kernel, which holds its loop in registers).
   template <int GP, class G, class H>
   void both(const G& dh, const H& dw) const {
-    // (one plane of G for bfloat16 inputs means large tiles in one of them at least, two in none)
+    // (one plane of G means large tiles in one of them at least)
     constexpr bool IS_SMALL = std::is_same_v<typename G::Shape, Small>;
     if constexpr (std::is_same_v<typename G::Shape, typename H::Shape> && !(GP == 1 && IS_SMALL)) {
       launch(dh, dw);

@@ -99,3 +99,37 @@ def test_far_logits(env, case):  # noqa: F811
     again = losses.vocab_logprobs_backward(h, w, t, r.saved, r.row_grads)
     for g in (r.grad_hidden, r.grad_weight, *again):
         assert torch.isfinite(g).all()
+
+
+# sums of few terms, in products of large tiles: few rows for the weight's gradient, few classes for hidden's
+@pytest.mark.parametrize("case", [(1, 4096, 8192), (8, 1024, 33000), (64, 1024, 8192), (200, 520, 16500), (1000, 520, 16500),
+                                  (20000, 512, 700)])
+def test_few_terms_of_bfloat16(env, case):  # noqa: F811
+    """Gradients of bfloat16 inputs whose sums have few terms: dL/dlogits keeps 16 bits, and only the
+    rounding of the gradient itself is seen."""
+    torch, losses = env
+    h, w, t, h64, w64, t64, share = make(torch, (*case, "bfloat16", 64, 0, 0), seed=14)
+    on = t64 >= 0
+    there = torch.from_numpy(on).cuda()
+    ref = R.Vocab(h64[on], w64, t64[on], share.double().numpy()[on])
+    rows = np.arange(on.sum())
+
+    def check(g, gh, gw):
+        G = -g[:, None] * ref.p
+        G[rows, t64[on]] += g
+        # two roundings to 8 bits one of what the other leaves: 2^-16 of every value
+        for got, (want, tol), left, right in ((gh[there], ref.gradients(g, False, True, True)[0], G, w64),
+                                              (gw, ref.gradients(g, False, True, True)[1], G.T, h64[on])):
+            close(got, want, tol + R.BF16 ** 2 * (np.abs(left) @ np.abs(right)), "gradient")
+
+    r = losses.vocab_loss(h, w, t, weights=share.cuda(), save=True)
+    check(-ref.share, r.grad_hidden, r.grad_weight)
+    g = torch.randn(case[0], generator=torch.Generator().manual_seed(3))
+    check(g.double().numpy()[on], *losses.vocab_logprobs_backward(h, w, t, r.saved, g.cuda()))
+    # the weight's gradient in float32: no rounding but that one
+    full = torch.zeros(w.shape, device="cuda")
+    losses.vocab_loss(h, w, t, weights=share.cuda(), grad_weight=full)
+    want, tol = ref.gradients(-ref.share, False, False, False)[1]
+    G = ref.share[:, None] * ref.p
+    G[rows, t64[on]] -= ref.share
+    close(full, want, tol + R.BF16 ** 2 * (np.abs(G).T @ np.abs(h64[on])), "float32 gradient")
