@@ -60,20 +60,26 @@ struct Rows {
   int* count;    // rows in use
   double* total;  // sum of the weights
   float* factor;  // what the gradients of the products are multiplied by
+  float* peak;    // the largest finite |share|, 1 where there is none
 };
-// The factor all rows share: grad_scale, over the weights' sum for a mean, or *scale.
+// The factor all rows share: grad_scale, over the weights' sum for a mean, or *scale; and the
+// largest share, by which every row's is divided before dL/dx is rounded.
 struct Factor {
   const float* device;
   float host;
   bool mean;
 };
 
-__device__ __forceinline__ void finish_rows(const Factor& factor, const Rows& out, double sum, int used) {
+__device__ __forceinline__ void finish_rows(const Factor& factor, const Rows& out, double sum, int used, float peak) {
   *out.total = sum;
   *out.count = used;
-  const float f = factor.device != nullptr ? *factor.device : factor.host;
-  *out.factor = !factor.mean ? f : sum == 0.0 ? 0.f : float(double(f) / sum);
+  peak = peak > 0.f ? peak : 1.f;
+  *out.peak = peak;
+  const double f = double(factor.device != nullptr ? *factor.device : factor.host) * double(peak);
+  *out.factor = !factor.mean ? float(f) : sum == 0.0 ? 0.f : float(f / sum);
 }
+// |w|, 0 where it is not finite
+__device__ __forceinline__ float finite_size(float w) { return fabsf(w) <= -kNegMax ? fabsf(w) : 0.f; }
 
 constexpr int kWide = 1024, kEach = 8;
 
@@ -84,9 +90,11 @@ __global__ __launch_bounds__(kWide) void k_vocab_rows(const void* __restrict__ t
                                                       Factor factor, Rows out, float* logp, float2* saved, float* row_grads) {
   __shared__ int counts[kWide / 64];
   __shared__ double sums[kWide / 64];
+  __shared__ float peaks[kWide / 64];
   const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
   int done = 0;
   double sum = 0.0;
+  float peak = 0.f;
   for (int base = 0; base < rows; base += kWide * kEach) {
     const int first = base + tid * kEach;
     int t[kEach];
@@ -130,6 +138,7 @@ __global__ __launch_bounds__(kWide) void k_vocab_rows(const void* __restrict__ t
         out.share[place] = w[q];
         out.at[r] = place++;
         sum += double(w[q]);
+        peak = fmaxf(peak, finite_size(w[q]));
       } else {
         out.at[r] = -1;
         if (logp != nullptr) logp[r] = 0.f;
@@ -145,12 +154,19 @@ __global__ __launch_bounds__(kWide) void k_vocab_rows(const void* __restrict__ t
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  if (lane == 0) sums[wave] = sum;
+  peak = wave_max(peak);
+  if (lane == 0) {
+    sums[wave] = sum;
+    peaks[wave] = peak;
+  }
   __syncthreads();
   if (tid == 0) {
     double all = 0.0;
-    for (int k = 0; k < kWide / 64; ++k) all += sums[k];
-    finish_rows(factor, out, all, done);
+    for (int k = 0; k < kWide / 64; ++k) {
+      all += sums[k];
+      peak = fmaxf(peak, peaks[k]);
+    }
+    finish_rows(factor, out, all, done, peak);
   }
 }
 
@@ -201,7 +217,8 @@ struct FewRows {
         if (row_grads != nullptr) row_grads[r] = 0.f;
       }
     }
-    if (r == 0) finish_rows(factor, out, sum, used);
+    const float peak = wave_max(in_use ? finite_size(w) : 0.f);
+    if (r == 0) finish_rows(factor, out, sum, used, peak);
     return used;
   }
 };
@@ -386,7 +403,9 @@ struct StatsOut {
 
 // What turns a row's logits into G: M, g / S, g and the target.  g without the factor that
 // all rows share, which the sums of the products are multiplied by: 1 / W in every target's
-// g would be rounded to bfloat16 the same way in all of them, and the errors add up.
+// g would be rounded to bfloat16 the same way in all of them, and the errors add up.  A caller
+// may give dL/dlogp with such a factor in it: the largest share is taken out of all, so that
+// equal ones become 1.
 struct RowSlope {
   float top, slope, g;
   int target;
@@ -668,7 +687,7 @@ struct JoinOut {
   float* loss;         // [padded] weight times logp, null: not wanted
   bool mean;
 };
-// What packed row i leaves: its logp, loss and g = dL/dlogp without the common factor.
+// What packed row i leaves: its logp, loss and g = dL/dlogp without the common factors.
 struct Joined {
   float logp, loss, g;
 };
@@ -676,7 +695,7 @@ __device__ __forceinline__ Joined join_row(const Rows& rows, int i, int t, float
   // no class with a probability: no distribution
   const float nan = sum > 0.f ? 0.f : __builtin_nanf(""), w = rows.share[i];
   const float logp = t >= 0 ? (logit - top) - logf(sum) + nan : __builtin_nanf("");
-  return {logp, w * logp, t >= 0 ? -w : __builtin_nanf("")};
+  return {logp, w * logp, t >= 0 ? -w / *rows.peak : __builtin_nanf("")};
 }
 __device__ __forceinline__ void put_row(const Rows& rows, const JoinOut& out, int i, const Joined& j, float top, float sum) {
   const int r = rows.order[i];
@@ -821,7 +840,7 @@ __global__ __launch_bounds__(256) void k_vocab_slope(Rows rows, const float2* __
   }
   const float2 st = saved[rows.order[i]];
   const int t = rows.target[i];
-  const float g = t >= 0 ? rows.share[i] : __builtin_nanf("");
+  const float g = t >= 0 ? rows.share[i] / *rows.peak : __builtin_nanf("");
   slope[i] = RowSlope{st.x, g / st.y, g, t};
 }
 
@@ -836,8 +855,9 @@ constexpr int kTile = 256;
 constexpr int64_t kPieceBytes = int64_t(2) << 30;
 // Terms from which on, in both gradients, G of bfloat16 inputs may be rounded to 8 bits: it is
 // multiplied by values of 8 bits, and as their roundings do, those of G fall either way, so that
-// against the sizes of n terms together a sum is off by 2^-9 / sqrt(n) or so.  (A sum that few of
-// its terms decide is off by as much as they are, 2^-8 at the most where G was rounded twice.)
+// against the sizes of n terms together a sum is off by 2^-9 / sqrt(n) or so.  (Where few terms
+// decide, or rows alike are rounded alike, it is by 2^-8 of them at the most, as by its own
+// rounding, and 2^-7 where the exponentials were rounded too.)
 // 16 bits cost few rows nothing and many the second product of every pair: with 16 and with 8
 // bits 1 row of 4096 over 8192 classes 88 and 90 us, 64 of 4096 over 65536 499 and 498, 256 of
 // 1024 over 32768 153 and 125, 1000 of 4096 over 65536 2.31 and 1.50 ms, 2048 of 1024 over 32768
@@ -917,7 +937,7 @@ Plan plan_for(int64_t rows, int32_t width, int32_t classes, int32_t dtype) {
 }
 
 struct Layout {
-  size_t order, target, share, at, count, total, factor, logit, parts, slope, loss, hidden, weight, logits_sums, grad, kept, hidden_sums, weight_sums, bytes;
+  size_t order, target, share, at, count, total, factor, peak, logit, parts, slope, loss, hidden, weight, logits_sums, grad, kept, hidden_sums, weight_sums, bytes;
 };
 Layout layout(const Plan& p, bool gradient) {
   Layout w{};
@@ -935,6 +955,7 @@ Layout layout(const Plan& p, bool gradient) {
   w.count = take(4);
   w.total = take(8);
   w.factor = take(4);
+  w.peak = take(4);
   w.logit = take(R * 4);
   w.parts = take(R * 8 * size_t(p.pieces) * size_t(p.piece / p.tile_classes()));
   w.slope = take(R * sizeof(RowSlope));
@@ -972,7 +993,7 @@ struct Call {
   Call(const acdc_vocab_head& h, bool gradient, void* workspace, acdc_stream_t stream)
       : head(h), p(plan_for(h.rows, h.width, h.classes, h.dtype)), w(layout(p, gradient)), ws(static_cast<char*>(workspace)),
         s(reinterpret_cast<hipStream_t>(stream)) {
-    rows = Rows{get<int>(w.order), get<int>(w.target), get<float>(w.share), get<int>(w.at), get<int>(w.count), get<double>(w.total), get<float>(w.factor)};
+    rows = Rows{get<int>(w.order), get<int>(w.target), get<float>(w.share), get<int>(w.at), get<int>(w.count), get<double>(w.total), get<float>(w.factor), get<float>(w.peak)};
     direct = P == 1 && h.width % 8 == 0 && h.weight_stride % 8 == 0 && h.weight_stride < (1 << 22) && aligned_to(h.weight, 16);
   }
   template <class E>

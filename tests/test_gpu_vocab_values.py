@@ -133,3 +133,52 @@ def test_few_terms_of_bfloat16(env, case):  # noqa: F811
     G = ref.share[:, None] * ref.p
     G[rows, t64[on]] -= ref.share
     close(full, want, tol + R.BF16 ** 2 * (np.abs(G).T @ np.abs(h64[on])), "float32 gradient")
+
+
+# products of 8 bits of dL/dlogits, of 16 in large and in small tiles, of few tiles, and float32
+@pytest.mark.parametrize("case", [(5500, 256, 16640, "bfloat16"), (300, 512, 16640, "bfloat16"), (300, 16, 8300, "bfloat16"),
+                                  (90, 40, 100, "bfloat16"), (50, 40, 100, "bfloat16"), (300, 16, 8300, "float32")])
+def test_factor_of_all_rows(env, case):  # noqa: F811
+    """dL/dlogp of -1 / W in every row is -1 under a scale of 1 / W, bit for bit: the factor is not
+    rounded with each target's value, where it would be off the same way in all of them."""
+    torch, losses = env
+    rows, width, classes, dtype = case
+    h, w, t, h64, w64, t64, share = make(torch, (*case, 64, 0, 0), seed=15)
+    s = losses.vocab_logprobs(h, w, t, save=True)
+    inverse = torch.tensor([1.0 / rows], device="cuda")
+    ones = torch.full((rows,), -1.0, device="cuda")
+    want = losses.vocab_logprobs_backward(h, w, t, s.saved, ones, scale=inverse)
+    got = losses.vocab_logprobs_backward(h, w, t, s.saved, ones * inverse)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    # the same with rows of both signs and sizes, an infinite one among them
+    g = torch.randn(rows, generator=torch.Generator().manual_seed(4)).cuda()
+    g[0], t[0] = float("inf"), 0
+    gh, gw = losses.vocab_logprobs_backward(h, w, t, s.saved, g)
+    assert not torch.isfinite(gh[0]).any() and torch.isfinite(gh[1:]).all() and not torch.isfinite(gw[0]).any()
+
+
+def test_many_rows_of_one_class(env):  # noqa: F811
+    """The gradient of a class that thousands of rows have as their target, of rows alike: errors of
+    the same sign add up."""
+    torch, losses = env
+    rows, width, classes = 5500, 256, 16640
+    h, w, t, h64, w64, t64, _ = make(torch, (rows, width, classes, "bfloat16", 64, 0, 0), seed=16, idle=0.0)
+    h[:] = (torch.ones(width, device="cuda") + 0.1 * torch.randn(rows, width, device="cuda", generator=torch.Generator("cuda").manual_seed(6))).to(h.dtype)
+    t[:] = 3
+    h64, t64 = h.double().cpu().numpy(), t.cpu().numpy()
+    ref = R.Vocab(h64, w64, t64)
+    want, tol = ref.gradients(-ref.share, True, True, False)[1]
+    # rows alike have a p alike: 1 - p, of class 3 in every row, is rounded the same way in all of
+    # them, so that these roundings are not of mean 0, as the tolerance has it, and their sizes
+    # add up.  (p is 0.001 to 0.004 or so; in [1/2, 1] bfloat16 values are 2^-8 apart.)
+    q = 1 - ref.p[:, 3]
+    tol[3] += (ref.share * np.abs(np.round(q * 256) / 256 - q)) @ np.abs(h64)
+    r = losses.vocab_loss(h, w, t, save=True, grad_weight=torch.zeros(classes, width, device="cuda"))
+    close(r.grad_weight, want, tol, "vocab_loss")
+    full = torch.zeros(classes, width, device="cuda")
+    losses.vocab_logprobs_backward(h, w, t, r.saved, r.row_grads, grad_weight=full)
+    close(full, want, tol, "vocab_logprobs_backward")
+    # the differentiable form
+    b = w.clone().requires_grad_(True)
+    losses.vocab_loss_autograd(h, b, t)[0].backward()
+    close(b.grad, want, tol + R.out_rounding(want, True), "vocab_loss_autograd")
