@@ -28,7 +28,7 @@ import torch
 
 from ._lib import lib
 from .acdc import _call, _check, _once, _ptr, _wrote
-from .losses import _DTYPES, _aligned_workspace, _apart, _capturable, _index, _matrix, _native, _values, _workspace
+from .losses import _DTYPES, _aligned_workspace, _apart, _capturable, _index, _matrix, _native, _sizes, _values, _workspace
 
 
 class LayerNorm(NamedTuple):
@@ -78,6 +78,7 @@ def _one_type(name, a, b):
 
 @functools.lru_cache(maxsize=512)
 def _norm_bytes(rows, width):
+    _sizes(rows=rows, columns=width)
     return lib().acdc_norm_workspace_size(rows, width)
 
 
@@ -166,6 +167,7 @@ def layer_norm_backward(x, grad_y, weight, saved, out=None, grads=None, accumula
 
 @functools.lru_cache(maxsize=512)
 def _embedding_bytes(rows, width, classes):
+    _sizes(rows=rows, columns=width, classes=classes)
     return lib().acdc_embedding_workspace_size(rows, width, classes)
 
 
@@ -215,6 +217,7 @@ def embedding_backward(tokens, grad_rows, classes: int, scale: float = 1.0, dtyp
     bits = _index("tokens", tokens, rows, device)
     if classes < 1:
         raise ValueError(f"classes must be positive, got {classes}")
+    _sizes(classes=classes)
     _finite(scale)
     if grad_weight is None:
         if accumulate:

@@ -104,12 +104,20 @@ def _values(name, t):
         raise ValueError(f"{name} is without memory: its storage was freed")
 
 
+def _sizes(**sizes):
+    """Sizes that the C entry points take in 32 bits: a longer one would come there as another."""
+    for name, n in sizes.items():
+        if n > 0x7fffffff:
+            raise ValueError(f"{n} {name}: at most 2^31 - 1 are supported")
+
+
 def _logits(x, name="logits"):
     if x.dim() != 2:
         raise ValueError(f"{name} must be [rows, classes], got {tuple(x.shape)}")
     rows, classes = x.shape
     if classes < 1:
         raise ValueError(f"{name} must have a class at least")
+    _sizes(rows=rows, classes=classes)
     if x.dtype not in _DTYPES:
         raise ValueError(f"{name} must be float32 or bfloat16, not {x.dtype}")
     stride, inner = x.stride()
@@ -337,6 +345,7 @@ def _matrix(name, t, device=None):
     rows, width = t.shape
     if width < 1:
         raise ValueError(f"{name} must have a column at least")
+    _sizes(rows=rows, columns=width)
     stride, inner = t.stride()
     if width > 1 and inner != 1:
         raise ValueError(f"{name} must have contiguous rows (stride 1 along the width, got {inner})")
@@ -350,6 +359,7 @@ def _matrix(name, t, device=None):
 
 @functools.lru_cache(maxsize=512)
 def _vocab_bytes(rows, width, classes, dtype, gradient):
+    _sizes(rows=rows, columns=width, classes=classes)
     need = lib().acdc_vocab_workspace_size(rows, width, classes, dtype, gradient)
     if need == 0:
         raise ValueError(f"{rows} rows of {width} over {classes} classes: at most 2^24 rows, a width of 2^17 and 2^27 classes "
