@@ -8,7 +8,8 @@
  * host synchronisation, nothing allocated, everything checked on the host
  * before the first launch, sums in a fixed order and without atomics on
  * values.  An output overlaps no input and no other output, unless stated
- * otherwise.  A workspace belongs to one call at a time.
+ * otherwise, and the workspace none of them.  A workspace belongs to one call
+ * at a time.
  */
 #ifndef ACDC_TRAIN_LM_H_
 #define ACDC_TRAIN_LM_H_

@@ -16,7 +16,7 @@
 
 #include <algorithm>
 
-#include "acdc_train_lm.h"
+#include "acdc_train_lm.hpp"
 #include "acdc_train_rows.hpp"
 
 namespace acdc {
@@ -548,14 +548,6 @@ bool matrix_ok(const void* p, int32_t dtype, int64_t stride, int64_t rows, int32
 bool tokens_ok(const void* tokens, int32_t bits, int64_t rows) {
   return (bits == 32 || bits == 64) && aligned_to(tokens, size_t(bits) / 8) && (rows == 0 || tokens != nullptr);
 }
-bool apart(const void* p, int64_t rows, int64_t stride, int32_t type, const void* q, int64_t others, int64_t other_stride,
-           int32_t other_type, int64_t width) {
-  if (rows == 0 || others == 0) return true;
-  const char *a = static_cast<const char*>(p), *b = static_cast<const char*>(q);
-  const char* a_end = a + (size_t(rows - 1) * size_t(stride) + size_t(width)) * dtype_bytes(type);
-  const char* b_end = b + (size_t(others - 1) * size_t(other_stride) + size_t(width)) * dtype_bytes(other_type);
-  return a_end <= b || b_end <= a;
-}
 template <class F>
 void with_types(int32_t a, int32_t b, F&& f) {
   if (a == ACDC_F32) {
@@ -577,7 +569,9 @@ extern "C" int acdc_embedding_forward(const void* tokens, int32_t token_bits, co
                                       int64_t rows, int32_t width, int32_t classes, acdc_stream_t stream) {
   if (!sizes_ok(rows, width, classes) || !tokens_ok(tokens, token_bits, rows) ||
       !matrix_ok(weight, weight_type, weight_stride, classes, width) || !matrix_ok(out, out_type, out_stride, rows, width) ||
-      !(scale - scale == 0.f) || !apart(out, rows, out_stride, out_type, weight, classes, weight_stride, weight_type, width))
+      !(scale - scale == 0.f) ||
+      !all_apart({span_of(out, rows, out_stride, width, dtype_bytes(out_type))},
+                 {span_of(weight, classes, weight_stride, width, dtype_bytes(weight_type)), span_of(tokens, rows, size_t(token_bits) / 8)}))
     return ACDC_ERR_INVALID_ARG;
   if (rows == 0) return ACDC_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
@@ -610,11 +604,14 @@ extern "C" int acdc_embedding_backward(const void* tokens, int32_t token_bits, c
                                        int32_t classes, void* workspace, size_t workspace_bytes, acdc_stream_t stream) {
   if (!sizes_ok(rows, width, classes) || !tokens_ok(tokens, token_bits, rows) ||
       !matrix_ok(grad_out, out_type, out_stride, rows, width) || !matrix_ok(grad_weight, weight_type, weight_stride, classes, width) ||
-      !(scale - scale == 0.f) || !aligned_to(workspace, 256) ||
-      !apart(grad_weight, classes, weight_stride, weight_type, grad_out, rows, out_stride, out_type, width))
+      !(scale - scale == 0.f) || !aligned_to(workspace, 256))
     return ACDC_ERR_INVALID_ARG;
+  const Span gw = span_of(grad_weight, classes, weight_stride, width, dtype_bytes(weight_type)),
+             g = span_of(grad_out, rows, out_stride, width, dtype_bytes(out_type)), t = span_of(tokens, rows, size_t(token_bits) / 8);
+  if (!all_apart({gw}, {g, t})) return ACDC_ERR_INVALID_ARG;
   const Layout w = layout(rows, width, classes);
   if (workspace == nullptr || workspace_bytes < w.bytes) return ACDC_ERR_WORKSPACE;
+  if (!all_apart({span_of(workspace, int64_t(w.bytes), 1)}, {gw, g, t})) return ACDC_ERR_INVALID_ARG;
   if (rows == 0 && accumulate != 0) return ACDC_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);

@@ -16,7 +16,7 @@
 
 #include <algorithm>
 
-#include "acdc_train_lm.h"
+#include "acdc_train_lm.hpp"
 #include "acdc_train_rows.hpp"
 
 namespace acdc {
@@ -435,15 +435,6 @@ bool rows_ok(const void* p, int32_t dtype, int64_t stride, int64_t rows, int32_t
   return e != 0 && stride >= width && stride <= (int64_t(1) << 40) && aligned_to(p, e) && (rows == 0 || p != nullptr);
 }
 bool sizes_ok(int64_t rows, int32_t width) { return rows >= 0 && rows <= 0x3fffffff && width >= 1 && width <= kMostWidth; }
-struct Span {
-  const char* from;
-  const char* to;
-};
-Span span_of(const void* p, int64_t rows, int64_t stride, int64_t width, int32_t dtype) {
-  const char* a = static_cast<const char*>(p);
-  return {a, p == nullptr || rows == 0 ? a : a + (size_t(rows - 1) * size_t(stride) + size_t(width)) * dtype_bytes(dtype)};
-}
-bool apart(const Span& a, const Span& b) { return a.to <= b.from || b.to <= a.from; }
 
 // Few short rows, more than a workgroup of 256 lanes takes at once: one of 1024, and a
 // launch less (64 rows of 256 5.2 us for 7.0, 16 of 1024 5.3 for 7.1; 100 of 256 would be 8.4 for 6.7).
@@ -474,9 +465,8 @@ extern "C" int acdc_norm_forward(const void* x, int32_t x_type, int64_t x_stride
     return ACDC_ERR_INVALID_ARG;
   const size_t e = dtype_bytes(vector_type);
   if (e == 0 || !aligned_to(weight, e) || !aligned_to(bias, e)) return ACDC_ERR_INVALID_ARG;
-  const Span out = span_of(y, rows, y_stride, width, y_type);
-  if (rows > 0 && (!apart(out, span_of(x, rows, x_stride, width, x_type)) || !apart(out, span_of(weight, 1, width, width, vector_type)) ||
-                   !apart(out, span_of(bias, 1, width, width, vector_type))))
+  if (!all_apart({span_of(y, rows, y_stride, width, dtype_bytes(y_type)), span_of(saved, 2 * rows, 4)},
+                 {span_of(x, rows, x_stride, width, dtype_bytes(x_type)), span_of(weight, width, e), span_of(bias, width, e)}))
     return ACDC_ERR_INVALID_ARG;
   if (rows == 0) return ACDC_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
@@ -515,23 +505,19 @@ extern "C" int acdc_norm_backward(const void* x, int32_t x_type, int64_t x_strid
   const size_t e = dtype_bytes(vector_type), ge = dtype_bytes(grads_type);
   if (e == 0 || ge == 0 || !aligned_to(weight, e) || !aligned_to(grad_weight, ge) || !aligned_to(grad_bias, ge))
     return ACDC_ERR_INVALID_ARG;
-  const Span in[3] = {span_of(x, rows, x_stride, width, x_type), span_of(grad_y, rows, grad_y_stride, width, y_type),
-                      span_of(weight, 1, width, width, vector_type)};
-  const Span out[3] = {span_of(grad_x, grad_x != nullptr ? rows : 0, grad_x_stride, width, x_type),
-                       span_of(grad_weight, 1, width, width, grads_type), span_of(grad_bias, 1, width, width, grads_type)};
   if (grad_x != nullptr && !rows_ok(grad_x, x_type, grad_x_stride, rows, width)) return ACDC_ERR_INVALID_ARG;
   // in place of grad_y: each value is read by the lane that writes it, before it does
   const bool in_place = grad_x == grad_y && grad_x_stride == grad_y_stride && x_type == y_type;
-  for (int o = 0; o < 3; ++o) {
-    for (int i = 0; i < 3; ++i)
-      if (!(o == 0 && i == 1 && in_place) && !apart(out[o], in[i])) return ACDC_ERR_INVALID_ARG;
-    for (int q = 0; q < o; ++q)
-      if (!apart(out[o], out[q])) return ACDC_ERR_INVALID_ARG;
-  }
+  const Span x_span = span_of(x, rows, x_stride, width, dtype_bytes(x_type)), st = span_of(saved, 2 * rows, 4),
+             gy = span_of(grad_y, rows, grad_y_stride, width, dtype_bytes(y_type)), w = span_of(weight, width, e),
+             gx = span_of(grad_x, rows, grad_x_stride, width, dtype_bytes(x_type)), gw = span_of(grad_weight, width, ge),
+             gb = span_of(grad_bias, width, ge);
+  if (!all_apart({gx, gw, gb}, {x_span, in_place ? Span{} : gy, w, st}) || !apart(gw, gy) || !apart(gb, gy)) return ACDC_ERR_INVALID_ARG;
   const bool sums = grad_weight != nullptr || grad_bias != nullptr;
   const size_t need = acdc_norm_workspace_size(rows, width);
   if (sums && !alone(rows, width) && (workspace == nullptr || workspace_bytes < need)) return ACDC_ERR_WORKSPACE;
   if (!aligned_to(workspace, 16)) return ACDC_ERR_INVALID_ARG;
+  if (sums && !alone(rows, width) && !all_apart({span_of(workspace, int64_t(need), 1)}, {x_span, gy, w, st, gx, gw, gb})) return ACDC_ERR_INVALID_ARG;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const int parts = parts_of(rows, width);
   const Sums out_sums{grad_weight, grad_bias, grads_type, accumulate != 0};

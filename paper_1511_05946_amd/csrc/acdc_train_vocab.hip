@@ -20,7 +20,7 @@
 #include <type_traits>
 
 #include "acdc_train_gemm.hpp"
-#include "acdc_train_lm.h"
+#include "acdc_train_lm.hpp"
 
 namespace acdc {
 namespace {
@@ -1216,15 +1216,6 @@ bool sizes_ok(int64_t rows, int32_t width, int32_t classes, int32_t dtype) {
   return dtype_bytes(dtype) != 0 && rows >= 0 && rows <= kMostRows && width >= 1 && width <= kMostWidth && classes >= 1 &&
          classes <= kMostClasses;
 }
-struct Span {
-  const char* from;
-  const char* to;
-};
-Span span_of(const void* p, int64_t rows, int64_t stride, int64_t width, size_t bytes) {
-  const char* a = static_cast<const char*>(p);
-  return {a, p == nullptr || rows == 0 ? a : a + (size_t(rows - 1) * size_t(stride) + size_t(width)) * bytes};
-}
-bool apart(const Span& a, const Span& b) { return a.to <= b.from || b.to <= a.from; }
 
 bool head_ok(const acdc_vocab_head* h) {
   if (h == nullptr || !sizes_ok(h->rows, h->width, h->classes, h->dtype) || (h->target_bits != 32 && h->target_bits != 64))
@@ -1237,30 +1228,39 @@ bool head_ok(const acdc_vocab_head* h) {
                           aligned_to(h->targets, size_t(h->target_bits) / 8));
 }
 bool grads_ok(const acdc_vocab_head& h, const acdc_vocab_grads& g) {
-  const size_t e = dtype_bytes(h.dtype);
-  const Span x = span_of(h.hidden, h.rows, h.hidden_stride, h.width, e), w = span_of(h.weight, h.classes, h.weight_stride, h.width, e);
-  Span gx{}, gw{};
-  if (g.hidden != nullptr) {
-    if (!aligned_to(g.hidden, e) || g.hidden_stride < h.width || g.hidden_stride > kMostStride) return false;
-    gx = span_of(g.hidden, h.rows, g.hidden_stride, h.width, e);
-    if (!apart(gx, x) || !apart(gx, w)) return false;
-  }
-  if (g.weight != nullptr) {
-    const size_t we = dtype_bytes(g.weight_type);
-    if ((g.weight_type != ACDC_F32 && g.weight_type != h.dtype) || !aligned_to(g.weight, we) || g.weight_stride < h.width ||
-        g.weight_stride > kMostStride)
-      return false;
-    gw = span_of(g.weight, h.classes, g.weight_stride, h.width, we);
-    if (!apart(gw, x) || !apart(gw, w) || (g.hidden != nullptr && !apart(gw, gx))) return false;
-  }
-  return true;
+  if (g.hidden != nullptr && (!aligned_to(g.hidden, dtype_bytes(h.dtype)) || g.hidden_stride < h.width || g.hidden_stride > kMostStride))
+    return false;
+  return g.weight == nullptr || ((g.weight_type == ACDC_F32 || g.weight_type == h.dtype) && aligned_to(g.weight, dtype_bytes(g.weight_type)) &&
+                                 g.weight_stride >= h.width && g.weight_stride <= kMostStride);
 }
+// What a call reads and writes, to be compared: the head, `read` rows of values (4 bytes each), and
+// the gradients, `written` ones and the workspace's part that the call uses.
+struct Touched {
+  Span x, w, t, read[3], written[4], gx, gw;
+  Touched(const acdc_vocab_head& h, const acdc_vocab_grads* g) {
+    const size_t e = dtype_bytes(h.dtype);
+    x = span_of(h.hidden, h.rows, h.hidden_stride, h.width, e);
+    w = span_of(h.weight, h.classes, h.weight_stride, h.width, e);
+    t = span_of(h.targets, h.rows, size_t(h.target_bits) / 8);
+    if (g == nullptr) return;
+    gx = span_of(g->hidden, h.rows, g->hidden_stride, h.width, e);
+    gw = span_of(g->weight, h.classes, g->weight_stride, h.width, dtype_bytes(g->weight_type));
+  }
+  bool ok() const {
+    return all_apart({gx, gw, written[0], written[1], written[2], written[3]}, {x, w, t, read[0], read[1], read[2]});
+  }
+  bool ok(const void* workspace, size_t bytes) const {
+    return all_apart({span_of(workspace, int64_t(bytes), 1)},
+                     {x, w, t, read[0], read[1], read[2], gx, gw, written[0], written[1], written[2], written[3]});
+  }
+};
 bool wants(const acdc_vocab_grads* g) { return g != nullptr && (g->hidden != nullptr || g->weight != nullptr); }
 
-int workspace_ok(const acdc_vocab_head& h, bool gradient, const void* workspace, size_t bytes) {
+int workspace_ok(const acdc_vocab_head& h, bool gradient, const void* workspace, size_t bytes, const Touched& touched) {
   if (!aligned_to(workspace, 256)) return ACDC_ERR_INVALID_ARG;
-  if (workspace == nullptr || bytes < layout(plan_for(h.rows, h.width, h.classes, h.dtype), gradient).bytes) return ACDC_ERR_WORKSPACE;
-  return ACDC_OK;
+  const size_t need = layout(plan_for(h.rows, h.width, h.classes, h.dtype), gradient).bytes;
+  if (workspace == nullptr || bytes < need) return ACDC_ERR_WORKSPACE;
+  return touched.ok(workspace, need) ? ACDC_OK : ACDC_ERR_INVALID_ARG;
 }
 template <class F>
 int with_type(int32_t dtype, F&& f) {
@@ -1281,7 +1281,11 @@ extern "C" int acdc_vocab_logprob(const acdc_vocab_head* head, float* logp, floa
   if (!head_ok(head)) return ACDC_ERR_INVALID_ARG;
   if (head->rows == 0) return ACDC_OK;
   if (logp == nullptr || !aligned_to(logp, 4) || !aligned_to(saved, 8)) return ACDC_ERR_INVALID_ARG;
-  if (const int rc = workspace_ok(*head, false, workspace, workspace_bytes); rc != ACDC_OK) return rc;
+  Touched touched(*head, nullptr);
+  touched.written[0] = span_of(logp, head->rows, 4);
+  touched.written[1] = span_of(saved, 2 * head->rows, 4);
+  if (!touched.ok()) return ACDC_ERR_INVALID_ARG;
+  if (const int rc = workspace_ok(*head, false, workspace, workspace_bytes, touched); rc != ACDC_OK) return rc;
   return with_type(head->dtype, [&]<class T>() {
     const Call<T> c(*head, false, workspace, stream);
     c.pack_rows(nullptr, Factor{nullptr, 1.f, false}, logp, reinterpret_cast<float2*>(saved), nullptr);
@@ -1294,8 +1298,13 @@ extern "C" int acdc_vocab_backward(const acdc_vocab_head* head, const float* sav
   if (!head_ok(head) || grads == nullptr || !grads_ok(*head, *grads) || !aligned_to(scale, 4)) return ACDC_ERR_INVALID_ARG;
   if (head->rows > 0 && (saved == nullptr || !aligned_to(saved, 8) || grad_logp == nullptr || !aligned_to(grad_logp, 4)))
     return ACDC_ERR_INVALID_ARG;
+  Touched touched(*head, grads);
+  touched.read[0] = span_of(saved, 2 * head->rows, 4);
+  touched.read[1] = span_of(grad_logp, head->rows, 4);
+  touched.read[2] = span_of(scale, 1, 4);
+  if (!touched.ok()) return ACDC_ERR_INVALID_ARG;
   if (!wants(grads)) return ACDC_OK;
-  if (const int rc = workspace_ok(*head, true, workspace, workspace_bytes); rc != ACDC_OK) return rc;
+  if (const int rc = workspace_ok(*head, true, workspace, workspace_bytes, touched); rc != ACDC_OK) return rc;
   return with_type(head->dtype, [&]<class T>() {
     const Call<T> c(*head, true, workspace, stream);
     c.pack_rows(grad_logp, Factor{scale, 1.f, false}, nullptr, nullptr, nullptr);
@@ -1315,7 +1324,14 @@ extern "C" int acdc_vocab_loss(const acdc_vocab_head* head, const float* weights
   if (!(q.grad_scale - q.grad_scale == 0.f) || (head->rows > 0 && logp == nullptr) || (grads != nullptr && !grads_ok(*head, *grads)))
     return ACDC_ERR_INVALID_ARG;
   const bool gradient = wants(grads);
-  if (const int rc = workspace_ok(*head, gradient, workspace, workspace_bytes); rc != ACDC_OK) return rc;
+  Touched touched(*head, grads);
+  touched.read[0] = span_of(weights, head->rows, 4);
+  touched.written[0] = span_of(stats, 2, 4);
+  touched.written[1] = span_of(logp, head->rows, 4);
+  touched.written[2] = span_of(saved, 2 * head->rows, 4);
+  touched.written[3] = span_of(row_grads, head->rows, 4);
+  if (!touched.ok()) return ACDC_ERR_INVALID_ARG;
+  if (const int rc = workspace_ok(*head, gradient, workspace, workspace_bytes, touched); rc != ACDC_OK) return rc;
   return with_type(head->dtype, [&]<class T>() {
     const Call<T> c(*head, gradient, workspace, stream);
     float2* stat = reinterpret_cast<float2*>(saved);

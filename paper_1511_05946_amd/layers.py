@@ -138,13 +138,14 @@ def layer_norm_backward(x, grad_y, weight, saved, out=None, grads=None, accumula
         if out is not None:
             gx_stride = _rows_of("out", out, rows, width, device, x.dtype)
             same = out.data_ptr() == grad_y.data_ptr() and gx_stride == gy_stride and out.dtype is grad_y.dtype
-            _apart("out", out, ("x", x), ("weight", weight), *(() if same else (("grad_y", grad_y),)))
+            _apart("out", out, ("x", x), ("weight", weight), ("saved", saved), *(() if same else (("grad_y", grad_y),)))
     if grads is not None:
         gw, gb = gw if want_w else None, gb if want_b else None
         for name, t in (("grad_weight", gw), ("grad_bias", gb)):
             if t is not None:
                 _width_vector(name, t, width, device)
-                _apart(name, t, ("x", x), ("grad_y", grad_y), ("weight", weight), ("out", out), ("grad_bias", gb if t is gw else None))
+                _apart(name, t, ("x", x), ("grad_y", grad_y), ("weight", weight), ("saved", saved), ("out", gx),
+                       ("grad_bias", gb if t is gw else None))
     else:
         if accumulate:
             raise ValueError("accumulate needs the gradient tensors to add into (grads=...)")

@@ -412,8 +412,9 @@ def _apart(name, out, *others):
                 raise ValueError(f"{name} overlaps {other}")
 
 
-def _vocab_grads(hidden, weight, out, grad_weight, accumulate, wanted):
-    """(packed description, grad_hidden, grad_weight) for the gradients in `wanted`."""
+def _vocab_grads(hidden, weight, out, grad_weight, accumulate, wanted, *read):
+    """(packed description, grad_hidden, grad_weight) for the gradients in `wanted`; `read`: what
+    else the call reads, (name, tensor) each."""
     gh = gw = None
     gh_stride = gw_stride = 0
     if wanted[0]:
@@ -432,9 +433,9 @@ def _vocab_grads(hidden, weight, out, grad_weight, accumulate, wanted):
         if gw.shape != weight.shape or (gw.dtype is not weight.dtype and gw.dtype is not torch.float32):
             raise ValueError(f"grad_weight must be {tuple(weight.shape)} {weight.dtype} or float32, got {tuple(gw.shape)} {gw.dtype}")
     if out is not None and gh is not None:
-        _apart("out", gh, ("hidden", hidden), ("weight", weight), ("grad_weight", gw))
+        _apart("out", gh, ("hidden", hidden), ("weight", weight), ("grad_weight", gw), *read)
     if grad_weight is not None and gw is not None:
-        _apart("grad_weight", gw, ("hidden", hidden), ("weight", weight))
+        _apart("grad_weight", gw, ("hidden", hidden), ("weight", weight), *read)
     record = struct.pack("2Q2q2i", 0 if gh is None else gh.data_ptr(), 0 if gw is None else gw.data_ptr(), gh_stride, gw_stride,
                          0 if gw is None else _DTYPES[gw.dtype], 1 if accumulate else 0)
     return record, gh, gw
@@ -484,7 +485,8 @@ def vocab_logprobs_backward(hidden, weight, targets, saved, grad_logp, scale=Non
     _vector("grad_logp", grad_logp, rows, device)
     if scale is not None:
         _vector("scale", scale.reshape(-1), 1, device)
-    record, gh, gw = _vocab_grads(hidden, weight, out, grad_weight, accumulate, wanted)
+    record, gh, gw = _vocab_grads(hidden, weight, out, grad_weight, accumulate, wanted, ("targets", targets), ("saved", saved),
+                                  ("grad_logp", grad_logp), ("scale", scale))
     rc = _call(lib().acdc_vocab_backward, device, head, saved.data_ptr(), grad_logp.data_ptr(), _ptr(scale), record,
                ws.data_ptr(), need)
     _check(rc, "acdc_vocab_backward")
@@ -512,7 +514,8 @@ def vocab_loss(hidden, weight, targets, weights=None, mean: bool = True, grad_sc
     _vector("weights", weights, rows, device)
     if not math.isfinite(grad_scale):
         raise ValueError(f"grad_scale must be finite, got {grad_scale}")
-    record, gh, gw = _vocab_grads(hidden, weight, out, grad_weight, accumulate, wanted) if any_grad else (None, None, None)
+    record, gh, gw = _vocab_grads(hidden, weight, out, grad_weight, accumulate, wanted, ("targets", targets),
+                                  ("weights", weights)) if any_grad else (None, None, None)
     stats, logp = torch.empty(2, device=device), torch.empty(rows, device=device)
     saved = torch.empty(rows, 2, device=device) if save else None
     row_grads = torch.empty(rows, device=device) if save else None
