@@ -573,8 +573,9 @@ def _capturable(call, *inputs):
     """Refuses to take into a captured graph what was made outside of it on the default
     stream: its backward pass would make that stream wait for the captured one, which
     ends the process.  A leaf is made there with the first operation on it, and stays
-    while any result of one lives."""
-    if inputs[0].is_cuda and torch.cuda.is_current_stream_capturing() and binding().made_on_default_stream(*inputs):
+    while any result of one lives.  Without gradients there is no backward pass."""
+    if torch.is_grad_enabled() and inputs[0].is_cuda and torch.cuda.is_current_stream_capturing() and \
+            binding().made_on_default_stream(*inputs):
         raise RuntimeError(f"{call} is captured while results of its inputs that were computed on the default stream are "
                            "alive: drop them (and their losses) before the capture, or compute them on another stream")
 
