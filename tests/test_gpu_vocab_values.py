@@ -101,6 +101,27 @@ def test_far_logits(env, case):  # noqa: F811
         assert torch.isfinite(g).all()
 
 
+@pytest.mark.parametrize("case", CASES)
+def test_likely_targets(env, case):  # noqa: F811
+    """Targets of a probability near 1, whose 1 - p has few digits left: of the loss, which may take it
+    from kept exponentials, and of the backward call, which computes the logits again."""
+    torch, losses = env
+    rows, width, classes, dtype = case
+    h, w, t, h64, w64, t64, _ = make(torch, (rows, width, classes, dtype, 64, 0, 0), seed=17, idle=0.97 if rows > 10000 else 0.25)
+    on = t64 >= 0
+    w = (w.float() * 6.0).to(w.dtype)
+    w64 = w.double().cpu().numpy()
+    t64 = np.where(on, (np.where(on[:, None], h64, 0.0) @ w64.T).argmax(1), t64)
+    t.copy_(torch.from_numpy(t64))
+    ref = R.Vocab(h64[on], w64, t64[on])
+    there = torch.from_numpy(on).cuda()
+    r = losses.vocab_loss(h, w, t, save=True)
+    close(r.logp[there], ref.logp, ref.logp_tol, "logp")
+    check_gradients(ref, -ref.share, r.grad_hidden[there], r.grad_weight, dtype == "bfloat16")
+    gh, gw = losses.vocab_logprobs_backward(h, w, t, r.saved, r.row_grads)
+    check_gradients(ref, -ref.share, gh[there], gw, dtype == "bfloat16")
+
+
 # sums of few terms, in products of large tiles: few rows for the weight's gradient, few classes for hidden's
 # (the last one: two pieces of the vocabulary)
 @pytest.mark.parametrize("case", [(1, 4096, 8192), (8, 1024, 33000), (64, 1024, 8192), (200, 520, 16500), (1000, 520, 16500),
