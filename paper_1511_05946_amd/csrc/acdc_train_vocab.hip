@@ -865,6 +865,7 @@ constexpr int64_t kPieceBytes = int64_t(2) << 30;
 // 1024 over 32768 153 and 125, 1000 of 4096 over 65536 2.31 and 1.50 ms, 2048 of 1024 over 32768
 // 0.78 and 0.46, 8192 of 4096 over 65536 18.6 and 10.4.
 constexpr int kMany = 1024;
+static_assert((kMany / 64) * (kMany / 64) > kFewClasses / 64, "8 bits of G: more rows than Flat takes, and no FewLogits");
 
 // Products of BM x BN: large tiles feed the matrix cores best, small ones keep more of the
 // card busy, and give a row of few steps to more workgroups.  Four waves of 64 x 128 for
@@ -883,7 +884,7 @@ using Small3 = Shape<64, 64, 32, 2, 2, 4>;
 // The shapes for P planes of one operand and PB of the other.
 template <int P, int PB>
 using LargeOf = std::conditional_t<PB == 1, Large, std::conditional_t<P == 1, Large2, Large3>>;
-template <int P, int PB>
+template <int P>
 using FlatOf = std::conditional_t<P == 1, Flat, Flat3>;
 template <int P>
 using SmallOf = std::conditional_t<P == 1, Small, Small3>;
@@ -1060,32 +1061,36 @@ struct Call {
     const unsigned first = unsigned(up(g.groups(), 8));
     hipLaunchKernelGGL((k_gemm_both<G, H>), dim3(first + h.groups()), dim3(G::T), 0, s, g, h, first, rows.count);
   }
-  // f(a product with n over the packed rows); b of PB planes
-  template <int PB, bool XA, class E, class F>
+  // f(a product with n over the packed rows); b of PB planes.  FEW: there may be 64 rows or less
+  template <int PB, bool XA, bool FEW, class E, class F>
   void over_rows(bool large, const Operand& a, const Operand& b, int64_t m, int depth, int parts, const E& e, F&& f) const {
     constexpr Count N = Count::kN;
-    if (!large) f(product<SmallOf<P>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
-    else if (p.padded_rows > 64) f(product<LargeOf<P, PB>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
-    else f(product<FlatOf<P, PB>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
+    if (!large) {
+      f(product<SmallOf<P>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
+    } else if (!FEW || p.padded_rows > 64) {
+      f(product<LargeOf<P, PB>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
+    } else if constexpr (FEW) {
+      f(product<FlatOf<P>, PB, XA, false, N>(a, b, m, p.padded_rows, depth, parts, e));
+    }
   }
   // classes x packed rows
-  template <class E>
+  template <bool FEW, class E>
   void logits(const Operand& weight, int parts, const E& e) const {
-    over_rows<P, false>(p.large_logits, weight, hidden(), weight.rows, p.padded_width, parts, e, [&](const auto& g) { launch(g); });
+    over_rows<P, false, FEW>(p.large_logits, weight, hidden(), weight.rows, p.padded_width, parts, e, [&](const auto& g) { launch(g); });
   }
   // the same as sums of parts, and what a wave for each 64 of a row's classes reads
   FewLogits few_logits(const Operand& weight, int k) const {
     const int64_t part = p.padded_rows * p.piece;
-    logits(weight, p.logits_parts, PartOut{get<float>(w.logits_sums), part, p.piece, int(p.padded_rows), false});
+    logits<true>(weight, p.logits_parts, PartOut{get<float>(w.logits_sums), part, p.piece, int(p.padded_rows), false});
     return {get<float>(w.logits_sums), rows.count, part, p.logits_parts, p.piece, (classes_of(k) + 63) / 64, k * p.piece, classes_of(k)};
   }
   unsigned few_grid(const FewLogits& l) const { return unsigned((p.padded_rows * l.tiles + 3) / 4); }
 
   template <Keep KEEP>
   void statistics_of(const Operand& weight, int k) const {
-    logits(weight, 1,
-           StatsOut<KEEP, P == 3>{rows.target, get<float2>(w.parts), get<float>(w.logit), get<void>(w.kept), k * p.piece, classes_of(k),
-                                  int(p.padded_rows), k * (p.piece / p.tile_classes()), p.piece});
+    const StatsOut<KEEP, P == 3> out{rows.target, get<float2>(w.parts), get<float>(w.logit), get<void>(w.kept), k * p.piece, classes_of(k),
+                                     int(p.padded_rows), k * (p.piece / p.tile_classes()), p.piece};
+    logits<KEEP != Keep::kBf16>(weight, 1, out);
   }
   // few tiles and a single piece: everything up to G (PLANES 0: of no gradient)
   template <int PLANES>
@@ -1099,8 +1104,7 @@ struct Call {
   int statistics(const JoinOut& out, bool keep) const {
     if (few()) {
       if (!keep) return few<0>(out);
-      if constexpr (P == 3) return few<3>(out);
-      else return p.grad_planes == 1 ? few<1>(out) : few<2>(out);
+      return few<P == 3 ? 3 : 2>(out);  // (one plane of G is of many tiles)
     }
     for (int k = 0; k < p.pieces; ++k) {
       const Operand weight_k = weight(k, k == 0);
@@ -1108,9 +1112,13 @@ struct Call {
         const FewLogits l = few_logits(weight_k, k);
         hipLaunchKernelGGL(k_vocab_few_stats, dim3(few_grid(l)), dim3(256), 0, s, l, rows.target, get<float2>(w.parts),
                            get<float>(w.logit), int(p.padded_rows));
-      } else if (!keep) statistics_of<Keep::kNothing>(weight_k, k);
-      else if (p.grad_planes == 1) statistics_of<Keep::kBf16>(weight_k, k);
-      else statistics_of<Keep::kF32>(weight_k, k);
+      } else if (!keep) {
+        statistics_of<Keep::kNothing>(weight_k, k);
+      } else if (p.grad_planes > 1) {
+        statistics_of<Keep::kF32>(weight_k, k);
+      } else if constexpr (P == 1) {
+        statistics_of<Keep::kBf16>(weight_k, k);
+      }
     }
     hipLaunchKernelGGL(k_vocab_join, dim3(unsigned(p.padded_rows / 16)), dim3(1024), 0, s, rows, get<float2>(w.parts),
                        get<float>(w.logit), int((p.classes + p.tile_classes() - 1) / p.tile_classes()), int(p.padded_rows), out);
@@ -1156,13 +1164,15 @@ struct Call {
   template <int GP>
   void slopes_again(const Operand& weight, int k) const {
     const int64_t plane = p.padded_rows * p.piece;
-    if (p.few_logits) {
-      const FewLogits l = few_logits(weight, k);
-      hipLaunchKernelGGL(k_vocab_few_slopes<GP>, dim3(few_grid(l)), dim3(256), 0, s, l, get<RowSlope>(w.slope), get<__bf16>(w.grad),
-                         (long long)plane);
-    } else {
-      logits(weight, 1, SlopeOut<GP>{get<RowSlope>(w.slope), get<__bf16>(w.grad), plane, p.piece, k * p.piece, classes_of(k)});
+    if constexpr (GP > 1) {
+      if (p.few_logits) {
+        const FewLogits l = few_logits(weight, k);
+        hipLaunchKernelGGL(k_vocab_few_slopes<GP>, dim3(few_grid(l)), dim3(256), 0, s, l, get<RowSlope>(w.slope), get<__bf16>(w.grad),
+                           (long long)plane);
+        return;
+      }
     }
+    logits<(GP > 1)>(weight, 1, SlopeOut<GP>{get<RowSlope>(w.slope), get<__bf16>(w.grad), plane, p.piece, k * p.piece, classes_of(k)});
   }
   // With the rows' slopes or, of few tiles, G itself in place.  `kept`: the logp of the pass
   // that kept the only piece's exponentials (or G); `packed`: the piece of the weight that was
@@ -1199,7 +1209,7 @@ struct Call {
         if (g.weight_type == head.dtype) weight_grad<GP, T>(g, k, f);
         else weight_grad<GP, F32>(g, k, f);
       };
-      over_rows<GP, true>(p.large_hidden, wk, grad(k), p.width, classes_of(k), g.hidden != nullptr ? p.hidden_parts : 0,
+      over_rows<GP, true, (GP > 1)>(p.large_hidden, wk, grad(k), p.width, classes_of(k), g.hidden != nullptr ? p.hidden_parts : 0,
                           PartOut{get<float>(w.hidden_sums), part, p.padded_width, int(p.padded_rows), k > 0}, [&](const auto& dh) {
                             if (g.weight == nullptr) return launch(dh);
                             weight_too([&](const auto& dw) { both<GP>(dh, dw); });
