@@ -13,6 +13,8 @@ pytestmark = pytest.mark.gpu
 # one piece of the vocabulary
 SIZES = [(90, 40, 100), (100, 30, 1500), (8, 40, 5000), (300, 16, 8300), (1100, 512, 16500)]
 CASES = [(*s, dtype) for s in SIZES for dtype in ("float32", "bfloat16")] + [(16384, 8, 14000, "float32")]
+# small tiles of logits and large ones of gradients, of 8 bits of dL/dlogits and of 16
+CASES += [(1100, 8200, 1030, "bfloat16"), (40, 33000, 100, "bfloat16")]
 
 
 def switched_off(torch, case, seed):
